@@ -576,6 +576,168 @@ typedef struct aires_tile_stats {
 /* Errors: AIRES_E_INVALID_ARG (NULL, t out of range), AIRES_E_HIP. */
 aires_status aires_plan_tile_stats(const aires_plan *plan, int64_t t, aires_tile_stats *stats);
 
+/* ------------------------------------------------------------------------
+ * Training on aggregated features.  What a model does with the features
+ * that the aggregation and combination steps give it: layer norm, a softmax
+ * cross entropy against classes or against the rows of a table, and an
+ * update of its weights.  These calls take dense row-major device arrays,
+ * allocate nothing, enqueue their kernels on `stream` and return; outputs
+ * are valid once the stream reaches the end of that work, and must not
+ * overlap inputs.  Calls on different streams are independent as long as
+ * their outputs and workspaces are.  Results do not depend on the run: there
+ * are no atomics whose order matters.
+ */
+
+/* Element type of a dense array. */
+typedef enum aires_dtype {
+    AIRES_F32 = 0,
+    AIRES_BF16 = 1,
+    AIRES_F16 = 2
+} aires_dtype;
+
+/* Dense row-major device matrix (borrowed): element (i, j) at data[i*ld + j].
+   ld >= ncols; data needs the alignment of one element only. */
+typedef struct aires_dense {
+    int64_t nrows, ncols, ld;
+    int32_t dtype;              /* aires_dtype                             */
+    int32_t _reserved;
+    void *data;
+} aires_dense;
+
+/*
+ * aires_layer_norm -- each row of X normalised over its n columns:
+ *   mu = sum_j x_j / n,  r = 1 / sqrt(sum_j (x_j - mu)^2 / n + eps),
+ *   y_j = (x_j - mu) * r * gamma_j + beta_j.
+ * Sums and statistics are fp32 (the deviations are summed around mu, not as
+ * a difference of squares).  gamma, beta: n values of w_dtype, or NULL for
+ * ones and zeros.  Y (same size as X) may have another type.  mean, rstd: m
+ * fp32 values each, both NULL if not wanted (the backward pass reads them).
+ * A row whose values are all equal gives y = beta up to the rounding of mu
+ * (r = eps^-1/2); a NaN or
+ * an infinity makes its own row NaN and no other.
+ * Errors: AIRES_E_INVALID_ARG (NULL, bad type, ld < ncols, eps negative or
+ * not finite, only one of mean and rstd), AIRES_E_DIM (sizes differ),
+ * AIRES_E_UNSUPPORTED (n >= 2^31), AIRES_E_HIP.
+ */
+aires_status aires_layer_norm(const aires_dense *X, const void *gamma, const void *beta, int32_t w_dtype, double eps,
+                              const aires_dense *Y, float *mean, float *rstd, void *stream);
+
+/* Bytes of workspace that aires_layer_norm_backward needs for m rows of n
+   columns (0 where gamma's and beta's gradients are not asked for).
+   Errors: AIRES_E_INVALID_ARG, AIRES_E_DIM, AIRES_E_UNSUPPORTED. */
+aires_status aires_layer_norm_workspace(int64_t m, int64_t n, int64_t *bytes);
+
+/*
+ * aires_layer_norm_backward -- gradients of aires_layer_norm from dY, X and
+ * the mean and rstd that it returned.  With xh = (x - mu) r and g = dy gamma:
+ *   dx = r (g - mean_j(g) - xh mean_j(g xh)),
+ *   dgamma_j = sum over rows of dy xh,  dbeta_j = sum over rows of dy.
+ * dX has X's size, any type; dgamma and dbeta have n values of w_dtype,
+ * summed in fp32 in an order that depends on the sizes only and rounded
+ * once.  Either may be NULL; so may gamma (ones) and dX.  With no rows
+ * dgamma and dbeta are zeros.  workspace (16-byte aligned) is scratch.
+ * Errors: as aires_layer_norm, and AIRES_E_CAPACITY (workspace too small).
+ */
+aires_status aires_layer_norm_backward(const aires_dense *dY, const aires_dense *X, const float *mean,
+                                       const float *rstd, const void *gamma, int32_t w_dtype, const aires_dense *dX,
+                                       void *dgamma, void *dbeta, void *workspace, int64_t workspace_bytes,
+                                       void *stream);
+
+/* How aires_linear_xent reduces the rows' losses. */
+typedef enum aires_reduction {
+    AIRES_REDUCE_MEAN = 0,      /* sum over labelled rows / their number   */
+    AIRES_REDUCE_SUM = 1
+} aires_reduction;
+
+/* Bytes of workspace that aires_linear_xent needs for H (t x d) and W (v x
+   d) of one type; grads = 0 for the loss alone.
+   Errors: AIRES_E_INVALID_ARG, AIRES_E_DIM, AIRES_E_UNSUPPORTED. */
+aires_status aires_linear_xent_workspace(int64_t t, int64_t d, int64_t v, int32_t dtype, int32_t grads,
+                                         int64_t *bytes);
+
+/*
+ * aires_linear_xent -- softmax cross entropy of the scores z = H W^T (t x v)
+ * against labels, without storing the scores:
+ *   row_loss_i = log sum_j exp(z_ij) - z_i,label(i),
+ *   loss = sum_i row_loss_i / c, c = number of labelled rows (MEAN) or 1,
+ * and, where dH and dW are given (both or neither), with
+ * dz_ij = grad_scale (exp(z_ij) / sum_k exp(z_ik) - [j = label(i)]) / c:
+ *   dH = dz W,  dW = dz^T H.
+ * H: t x d features, W: v x d, one row per class or per table entry, of H's
+ * type.  labels: t values, int32 or int64 (labels_i64).  A label outside
+ * [0, v) marks a row without a target: it adds nothing to the loss, its
+ * row_loss and its row of dH are 0.  With no labelled row the loss and the
+ * gradients are 0.  row_loss: t fp32 values, or NULL.  loss: one fp32 value.
+ * dH and dW have H's and W's sizes and type.
+ * Scores, row statistics and sums over rows and classes are fp32; the table
+ * is gone through in pieces, whose probabilities go to the workspace in the
+ * operands' precision (16 bits for 16-bit operands).  A NaN in a row of
+ * H makes that row's loss and dH NaN, and dW with them.
+ * Errors: AIRES_E_INVALID_ARG (NULL, bad type or reduction, ld < ncols, one
+ * of dH and dW, grad_scale not finite), AIRES_E_DIM (sizes or types differ,
+ * v or d = 0 with t > 0), AIRES_E_UNSUPPORTED (t, d or v >= 2^31),
+ * AIRES_E_CAPACITY (workspace too small), AIRES_E_HIP.
+ */
+aires_status aires_linear_xent(const aires_dense *H, const aires_dense *W, const void *labels, int32_t labels_i64,
+                               int32_t reduction, double grad_scale, float *loss, float *row_loss,
+                               const aires_dense *dH, const aires_dense *dW, void *workspace,
+                               int64_t workspace_bytes, void *stream);
+
+/* Values that share one scale where AdamW's states are held in 8 bits. */
+#define AIRES_ADAMW_BLOCK 256
+
+/*
+ * One tensor of an AdamW step: n values, contiguous.  exp_avg and
+ * exp_avg_sq are fp32 with NULL scales, or 8 bits wide: then value i is
+ * code i times scale i / 256 (ceil(n / 256) fp32 scales each), codes of the
+ * first moment being OCP e4m3 (largest 448) and those of the second e5m2
+ * (largest 57344).  All zeros is the state before the first step.  copy: n
+ * values of copy_dtype that receive the rounded parameters, or NULL.
+ */
+typedef struct aires_adamw_tensor {
+    int64_t n;
+    void *param;                /* of param_dtype, updated                 */
+    const void *grad;           /* of grad_dtype                           */
+    void *exp_avg, *exp_avg_sq; /* updated                                 */
+    float *exp_avg_scale, *exp_avg_sq_scale;
+    void *copy;
+    int32_t param_dtype, grad_dtype, copy_dtype, _reserved;
+} aires_adamw_tensor;
+
+typedef struct aires_adamw_opts {
+    uint32_t struct_size;       /* = sizeof(aires_adamw_opts)              */
+    uint32_t seed;              /* of the rounding of 8-bit states         */
+    int64_t step;               /* 1 for the first step                    */
+    double lr, beta1, beta2, eps, weight_decay;
+    double grad_scale;          /* gradients are multiplied with it        */
+} aires_adamw_opts;
+
+/*
+ * aires_adamw -- one AdamW step (decoupled weight decay) over `count`
+ * tensors, in as few launches as hold their descriptors.  With g the scaled
+ * gradient and k the step:
+ *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *   p = p (1 - lr weight_decay)
+ *       - lr / (1 - beta1^k) * m / (sqrt(v) / sqrt(1 - beta2^k) + eps),
+ * in fp32 from the exact new moments; parameters of 16 bits are rounded to
+ * nearest.  New moments of 8 bits are rounded after that, per block: scale =
+ * largest finite magnitude / largest code (0 where that magnitude is below
+ * 2^-110, and then all codes are 0), and a value between two codes goes to
+ * either at random with the probability that keeps its mean: to the upper
+ * one where its distance from the lower, in units of the distance between
+ * them, plus (r + 1/2) / 2^16 reaches 1.  r is 16 bits of a hash of the
+ * value's index, its tensor's position in the call and opts->seed (the low
+ * half for m, the high half for v), so a step's result is a function of its
+ * inputs.  A positive second moment is never rounded to 0.  Values that are
+ * not finite are stored as NaN and leave their block's scale alone.
+ * Errors: AIRES_E_INVALID_ARG (NULL, bad type or struct_size, step < 1,
+ * betas outside [0, 1), options not finite, eps < 0, one scale without the
+ * other), AIRES_E_DIM (negative n), AIRES_E_UNSUPPORTED (n above 2^40),
+ * AIRES_E_OOM (host memory), AIRES_E_HIP.
+ */
+aires_status aires_adamw(const aires_adamw_tensor *tensors, int64_t count, const aires_adamw_opts *opts,
+                         void *stream);
+
 /* Release C's arrays through the allocator that made them; zeroes *C. */
 void aires_csr_out_free(aires_csr_out *C);
 void aires_plan_destroy(aires_plan *plan);

@@ -9,6 +9,10 @@ Python names mirror the C-ABI of include/aires.h:
   spgemm(plan, stream=None)         -> Output     (aires_spgemm)
   stream_tiles(plan, ...)           -> Output     (aires_stream_tiles)
   plan_info / plan_tile / plan_stats
+Training on the aggregated features (train.py):
+  layer_norm / layer_norm_backward                (aires_layer_norm...)
+  linear_xent(H, W, labels, ...)    -> Xent       (aires_linear_xent)
+  adamw(params, grads, m, v, ...)                 (aires_adamw)
 A and B are (nrows, ncols, row_ptr, col_idx, vals) tuples or objects with
 those attributes (``nrows, ncols, rp, col, val``); arrays are device torch
 tensors, pinned host torch tensors, or numpy arrays (planning only).
@@ -22,7 +26,8 @@ from . import _binding as B_
 
 __all__ = ["tile_plan", "tile_plan_file", "read_csr_file", "spgemm", "spmm", "stream_tiles", "plan_info",
            "plan_tile", "plan_stats", "plan_tile_stats", "spgemm_noalloc", "Plan", "Output", "AiresError",
-           "to_device", "to_pinned"]
+           "to_device", "to_pinned", "layer_norm", "layer_norm_backward", "linear_xent", "Xent", "adamw",
+           "adamw_state"]
 
 AiresError = B_.AiresError
 
@@ -370,3 +375,6 @@ def to_pinned(M):
     n, k, rp, col, val = _parts(M)
     return (n, k, torch.from_numpy(rp).pin_memory(), torch.from_numpy(col).pin_memory(),
             torch.from_numpy(val).pin_memory())
+
+
+from .train import Xent, adamw, adamw_state, layer_norm, layer_norm_backward, linear_xent  # noqa: E402

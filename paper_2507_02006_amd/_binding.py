@@ -101,6 +101,28 @@ class ReadStats(ctypes.Structure):
     _fields_ = [("bytes_read", c_i64), ("read_ms", c_dbl), ("total_ms", c_dbl)]
 
 
+DTYPE_F32, DTYPE_BF16, DTYPE_F16 = 0, 1, 2
+REDUCE_MEAN, REDUCE_SUM = 0, 1
+ADAMW_BLOCK = 256  # AIRES_ADAMW_BLOCK
+
+
+class Dense(ctypes.Structure):
+    _fields_ = [("nrows", c_i64), ("ncols", c_i64), ("ld", c_i64), ("dtype", c_i32), ("_reserved", c_i32),
+                ("data", c_vp)]
+
+
+class AdamWTensor(ctypes.Structure):
+    _fields_ = [("n", c_i64)] + \
+               [(n, c_vp) for n in ("param", "grad", "exp_avg", "exp_avg_sq", "exp_avg_scale", "exp_avg_sq_scale",
+                                    "copy")] + \
+               [(n, c_i32) for n in ("param_dtype", "grad_dtype", "copy_dtype", "_reserved")]
+
+
+class AdamWOpts(ctypes.Structure):
+    _fields_ = [("struct_size", c_u32), ("seed", c_u32), ("step", c_i64)] + \
+               [(n, c_dbl) for n in ("lr", "beta1", "beta2", "eps", "weight_decay", "grad_scale")]
+
+
 _lib = None
 
 
@@ -139,6 +161,14 @@ def load() -> ctypes.CDLL:
         "aires_plan_destroy": (None, [c_vp]),
         "aires_spmm": (ctypes.c_int, [P(Csr), c_vp, c_i64, c_i64, c_vp, c_i64, ctypes.c_int, ctypes.c_int,
                                        c_vp]),
+        "aires_layer_norm": (ctypes.c_int, [P(Dense), c_vp, c_vp, c_i32, c_dbl, P(Dense), c_vp, c_vp, c_vp]),
+        "aires_layer_norm_workspace": (ctypes.c_int, [c_i64, c_i64, P(c_i64)]),
+        "aires_layer_norm_backward": (ctypes.c_int, [P(Dense), P(Dense), c_vp, c_vp, c_vp, c_i32, P(Dense), c_vp,
+                                                     c_vp, c_vp, c_i64, c_vp]),
+        "aires_linear_xent_workspace": (ctypes.c_int, [c_i64, c_i64, c_i64, c_i32, c_i32, P(c_i64)]),
+        "aires_linear_xent": (ctypes.c_int, [P(Dense), P(Dense), c_vp, c_i32, c_i32, c_dbl, c_vp, c_vp, P(Dense),
+                                             P(Dense), c_vp, c_i64, c_vp]),
+        "aires_adamw": (ctypes.c_int, [P(AdamWTensor), c_i64, P(AdamWOpts), c_vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)

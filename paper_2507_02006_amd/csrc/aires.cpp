@@ -23,12 +23,17 @@
 
 #include "kernels.h"
 #include "scratch.h"
+#include "status.h"
 
 using namespace aires;
 
 namespace {
 
 thread_local std::string g_last_error;
+
+}  // namespace
+
+namespace aires {
 
 aires_status fail(aires_status s, const char* fmt, ...) {
   char buf[512];
@@ -40,18 +45,9 @@ aires_status fail(aires_status s, const char* fmt, ...) {
   return s;
 }
 
-#define HIP_TRY(expr)                                                                 \
-  do {                                                                                \
-    hipError_t e_ = (expr);                                                           \
-    if (e_ != hipSuccess)                                                             \
-      return fail(AIRES_E_HIP, "%s failed: %s", #expr, hipGetErrorString(e_));        \
-  } while (0)
+}  // namespace aires
 
-#define ST_TRY(expr)                       \
-  do {                                     \
-    aires_status s_ = (expr);              \
-    if (s_ != AIRES_OK) return s_;         \
-  } while (0)
+namespace {
 
 constexpr int64_t kDenseWaveMaxN = 2048;     // widest dense row one wavefront holds
 constexpr int64_t kDenseMaxCols = 16384;     // widest dense row a workgroup holds

@@ -1,0 +1,632 @@
+"""Layer norm, softmax cross entropy against a table and AdamW against their
+formulas in 64 bits (GPU).
+
+Tolerances are bounds, derived before the kernels ran: U = 2^-24 is the unit
+roundoff of fp32, a sum of any order and a chain of at most c additions is off
+by c U times the sum of magnitudes, c = 256 covers every chain of the layer
+norm kernels at these sizes; a result rounded to bf16 (fp16) is off by
+2^-8 (2^-11: 8 and 11 significant bits) of its magnitude more, fp16 by 2^-25
+at least.
+"""
+import itertools
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+import paper_2507_02006_amd as aires  # noqa: E402
+from paper_2507_02006_amd import _binding as B_  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+ROUND = {F32: U, BF16: 2.0 ** -8, F16: 2.0 ** -11}
+LEAST = {F32: 2.0 ** -149, BF16: 2.0 ** -133, F16: 2.0 ** -25}
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def near(got, want, tol, what):
+    got, want, tol = got.double().cpu(), want.cpu(), tol.cpu()
+    bad = ~((got - want).abs() <= tol)
+    assert not bad.any(), "%s: %d of %d off, worst %g against %g" % (
+        what, int(bad.sum()), bad.numel(), float((got - want).abs()[bad].max()), float(tol[bad].min()))
+
+
+# -------------------------------------------------------------- layer norm
+
+def norm_ref(x, gamma, beta, eps):
+    x = x.double()
+    mu = x.mean(1)
+    r = ((x - mu[:, None]).square().mean(1) + eps).rsqrt()
+    y = (x - mu[:, None]) * r[:, None] * gamma + beta
+    return y, mu, r
+
+
+def norm_data(m, n, xt, seed, pad=0):
+    g = gen(seed)
+    x = (torch.randn(m, n + pad, generator=g) * torch.rand(m, 1, generator=g).mul(3).exp() + torch.randn(m, 1, generator=g))
+    gamma = 1 + 0.3 * torch.randn(n, generator=g)
+    beta = torch.randn(n, generator=g)
+    return x.to(xt)[:, pad:], gamma, beta
+
+
+SIZES = [(1, 1), (1, 2), (3, 1), (5, 7), (64, 32), (129, 41), (33, 64), (70, 100), (257, 128), (31, 200), (100, 256),
+         (17, 511), (65, 512), (9, 513), (12, 1000), (40, 1024), (11, 2047), (7, 2049), (5, 6001), (600, 2300), (3, 12000),
+         (2, 17000), (3, 33000), (4099, 48)]
+
+
+@pytest.mark.parametrize("m,n", SIZES)
+def test_layer_norm_forward(m, n):
+    for xt, yt in ((F32, F32), (BF16, F16), (F16, BF16), (F32, BF16)):
+        x, gamma, beta = norm_data(m, n, xt, m * 31 + n)
+        Y, mean, rstd = aires.layer_norm(x.cuda(), gamma.cuda(), beta.cuda(), eps=1e-5, out_dtype=yt)
+        y, mu, r = norm_ref(x, gamma.double(), beta.double(), 1e-5)
+        big = x.double().abs().amax(1, keepdim=True)
+        assert Y.dtype == yt and mean.dtype == rstd.dtype == F32
+        near(mean, mu, 256 * U * big[:, 0], "mean")
+        # the deviations are off by 256 U max|x|, so their squares' mean by twice that against sqrt(mean)
+        near(rstd, r, r * (256 * U + 512 * U * big[:, 0] * r), "rstd")
+        spread = big * r[:, None]
+        near(Y, y, 256 * U * ((spread + 2 * spread * spread) * gamma.double().abs() + beta.double().abs()) + ROUND[yt] * y.abs()
+             + LEAST[yt], "Y")
+
+
+@pytest.mark.parametrize("m,n", SIZES)
+@pytest.mark.parametrize("xt,yt", [(F32, F32), (F32, BF16), (F16, F16), (BF16, F32)])
+def test_layer_norm_backward(m, n, xt, yt):
+    x, gamma, _ = norm_data(m, n, xt, m * 37 + n)
+    dy = torch.randn(m, n, generator=gen(n)).to(yt)
+    _, mu, r = norm_ref(x, 1.0, 0.0, 1e-5)
+    mu, r = mu.float(), r.float()
+    dX, dgamma, dbeta = aires.layer_norm_backward(dy.cuda(), x.cuda(), mu.cuda(), r.cuda(), gamma.cuda())
+    assert dX.dtype == xt and dgamma.dtype == dbeta.dtype == F32
+    X, D, M, R, G = x.double(), dy.double(), mu.double()[:, None], r.double()[:, None], gamma.double()
+    xh, g = (X - M) * R, D * G
+    m1, m2 = g.mean(1, keepdim=True), (g * xh).mean(1, keepdim=True)
+    dx = R * (g - m1 - xh * m2)
+    exh = 4 * U * (X.abs() + M.abs()) * R  # rounding of xh
+    a1, a2 = g.abs().mean(1, keepdim=True), (g * xh).abs().mean(1, keepdim=True)
+    e2 = 256 * U * a2 + (g.abs() * exh).mean(1, keepdim=True)
+    tol = R * (256 * U * (a1 + xh.abs() * a2) + 8 * U * g.abs() + xh.abs() * e2 + exh * a2)
+    near(dX, dx, tol + ROUND[xt] * dx.abs() + LEAST[xt], "dX")
+    near(dgamma, (D * xh).sum(0), 256 * U * (D * xh).abs().sum(0) + (D.abs() * exh).sum(0), "dgamma")
+    near(dbeta, D.sum(0), 256 * U * D.abs().sum(0), "dbeta")
+
+
+def test_layer_norm_backward_against_differences():
+    m, n, h = 6, 37, 1e-6
+    x, gamma, beta = (t.double() for t in norm_data(m, n, F32, 5))
+    c = torch.randn(m, n, generator=gen(8)).double()
+
+    def value(x, gamma, beta):
+        return (norm_ref(x, gamma, beta, 1e-5)[0] * c).sum()
+
+    def slope(f, at):
+        out = torch.empty_like(at)
+        for i in range(at.numel()):
+            d = torch.zeros_like(at).view(-1)
+            d[i] = h
+            d = d.view(at.shape)
+            out.view(-1)[i] = (f(at + d) - f(at - d)) / (2 * h)
+        return out
+
+    _, mean, rstd = aires.layer_norm(x.float().cuda(), gamma.float().cuda(), beta.float().cuda())
+    got = aires.layer_norm_backward(c.float().cuda(), x.float().cuda(), mean, rstd, gamma.float().cuda())
+    want = (slope(lambda v: value(v, gamma, beta), x), slope(lambda v: value(x, v, beta), gamma),
+            slope(lambda v: value(x, gamma, v), beta))
+    for a, b, name in zip(got, want, ("dX", "dgamma", "dbeta")):
+        # central differences: h^2 f''' and 2^-52 |f| / h, below 1e-7 here; fp32 sums of 37 terms
+        near(a, b, 1e-5 * (1 + b.abs()), name)
+
+
+def test_layer_norm_forms():
+    x, gamma, beta = norm_data(50, 77, F32, 3)
+    X = x.cuda()
+    # strides, an odd offset, an output of the caller's, weights of 16 bits, no weights, no statistics
+    wide = torch.zeros(50, 99, device="cuda")
+    wide[:, 5:82] = X
+    Y0, mean, rstd = aires.layer_norm(X, gamma.cuda(), beta.cuda())
+    Y1, m1, r1 = aires.layer_norm(wide[:, 5:82], gamma.cuda(), beta.cuda())
+    assert torch.equal(Y0, Y1) and torch.equal(mean, m1) and torch.equal(rstd, r1)
+    hold = torch.full((50, 101), 7.0, device="cuda")
+    Y2, none, _ = aires.layer_norm(X, gamma.cuda(), beta.cuda(), stats=False, out=hold[:, 3:80])
+    assert none is None and torch.equal(hold[:, 3:80], Y0) and bool((hold[:, :3] == 7).all()) and bool((hold[:, 80:] == 7).all())
+    g16, b16 = gamma.to(BF16), beta.to(BF16)
+    Y3, _, _ = aires.layer_norm(X, g16.cuda(), b16.cuda())
+    Y4, _, _ = aires.layer_norm(X, g16.float().cuda(), b16.float().cuda())
+    assert torch.equal(Y3, Y4)
+    Y5, _, _ = aires.layer_norm(X)
+    Y6, _, _ = aires.layer_norm(X, torch.ones(77, device="cuda"), torch.zeros(77, device="cuda"))
+    assert torch.equal(Y5, Y6)
+    odd = torch.zeros(50 * 77 + 1, dtype=F16, device="cuda")[1:].view(50, 77)  # base at an odd element
+    odd.copy_(X)
+    Y7, _, _ = aires.layer_norm(odd, out_dtype=F32)
+    Y8, _, _ = aires.layer_norm(odd.clone(), out_dtype=F32)
+    assert torch.equal(Y7, Y8)
+    dy = torch.randn(50, 77, generator=gen(4)).cuda()
+    full = aires.layer_norm_backward(dy, X, mean, rstd, gamma.cuda())
+    dX, no, _ = aires.layer_norm_backward(dy, X, mean, rstd, gamma.cuda(), need_weights=False)
+    assert no is None and torch.equal(dX, full[0])
+    none, dg, db = aires.layer_norm_backward(dy, X, mean, rstd, gamma.cuda(), need_dx=False)
+    assert none is None and torch.equal(dg, full[1]) and torch.equal(db, full[2])
+    d16 = aires.layer_norm_backward(dy, X, mean, rstd, g16.cuda(), dx_dtype=BF16)
+    assert d16[0].dtype == d16[1].dtype == d16[2].dtype == BF16
+    assert torch.equal(d16[2], db.to(BF16))
+
+
+def test_layer_norm_edges():
+    # no rows: gradients of the weights are zeros; no columns
+    e = torch.empty(0, 9, device="cuda")
+    Y, mean, rstd = aires.layer_norm(e)
+    assert Y.shape == (0, 9) and mean.numel() == 0
+    dX, dg, db = aires.layer_norm_backward(e, e, mean, rstd, torch.ones(9, device="cuda"))
+    assert dX.shape == (0, 9) and not dg.any() and not db.any()
+    z = torch.empty(4, 0, device="cuda")
+    assert aires.layer_norm(z, stats=False)[0].shape == (4, 0)
+    # rows of equal values, a NaN and an infinity stay in their rows
+    x = torch.randn(6, 300, generator=gen(1))
+    x[1] = 0
+    x[2] = 4.0
+    x[3, 7] = float("nan")
+    x[4, 250] = float("inf")
+    Y, mean, rstd = aires.layer_norm(x.cuda(), None, torch.full((300,), 0.5, device="cuda"))
+    Y, rstd = Y.cpu(), rstd.cpu()
+    assert bool((Y[1:3] == 0.5).all()) and torch.allclose(rstd[1:3], torch.tensor(1e-5 ** -0.5), rtol=1e-6)
+    assert bool(Y[3:5].isnan().all())
+    want = norm_ref(x[[0, 5]], 1.0, 0.5, 1e-5)[0]
+    near(Y[[0, 5]], want, 1e-4 * torch.ones_like(want), "rows next to it")
+    # one column: y = beta and no gradient reaches x
+    x1 = torch.randn(10, 1, generator=gen(2)).cuda()
+    Y, mean, rstd = aires.layer_norm(x1, torch.tensor([3.0], device="cuda"), torch.tensor([-2.0], device="cuda"))
+    assert bool((Y == -2).all())
+    assert not aires.layer_norm_backward(torch.ones_like(x1), x1, mean, rstd, torch.tensor([3.3], device="cuda"))[0].any()
+
+
+def test_layer_norm_same_result_each_time_and_on_other_streams():
+    x, gamma, beta = norm_data(5000, 300, F32, 9)
+    X, G, Bt = x.cuda(), gamma.cuda(), beta.cuda()
+    dy = torch.randn(5000, 300, generator=gen(1)).cuda()
+    Y, mean, rstd = aires.layer_norm(X, G, Bt)
+    first = aires.layer_norm_backward(dy, X, mean, rstd, G)
+    torch.cuda.synchronize()
+    for stream in (torch.cuda.Stream(), torch.cuda.Stream()):
+        Y1, m1, r1 = aires.layer_norm(X, G, Bt, stream=stream)
+        got = aires.layer_norm_backward(dy, X, m1, r1, G, stream=stream)
+        stream.synchronize()
+        assert torch.equal(Y, Y1) and all(torch.equal(a, b) for a, b in zip(first, got))
+
+
+# ----------------------------------------------------------- cross entropy
+
+def xent_data(t, d, v, dt, seed, labels="some"):
+    g = gen(seed)
+    H = torch.randn(t, d, generator=g).to(dt)
+    W = (torch.randn(v, d, generator=g) * 2 / max(1.0, d ** 0.5)).to(dt)
+    y = torch.randint(0, max(v, 1), (t,), generator=g)
+    if labels == "some":
+        y[torch.rand(t, generator=g) < 0.3] = -1
+        y[torch.rand(t, generator=g) < 0.1] = v + 5
+    elif labels == "none":
+        y[:] = -100
+    return H, W, y
+
+
+def xent_ref(H, W, y, mean=True, scale=1.0):
+    """Results in 64 bits and their tolerances."""
+    H, W, dt = H.double().cuda(), W.double().cuda(), H.dtype
+    y = y.cuda()
+    t, d = H.shape
+    v = W.shape[0]
+    z = H @ W.t()
+    lse = torch.logsumexp(z, 1)
+    there = (y >= 0) & (y < v)
+    hot = there.nonzero().squeeze(1)
+    c = max(1, int(there.sum())) if mean else 1
+    rl = torch.zeros(t, dtype=torch.float64, device="cuda")
+    rl[hot] = lse[hot] - z[hot, y[hot]]
+    p = torch.exp(z - lse[:, None])
+    hotm = torch.zeros_like(p)
+    hotm[hot, y[hot]] = 1
+    k = there.double()[:, None] * scale / c
+    dz = (p - hotm) * k
+    # scores: d products and additions in fp32, at most 4 U a product more
+    # where an fp32 operand is split into parts
+    ez = ((d + 8) * U * (H.abs() @ W.abs().t())).amax(1)
+    el = ez + 256 * U * (1 + lse.abs() + z.abs().amax(1))
+    tol_rl = 2 * el
+    # dz: exp of a score off by ez and of lse off by el; rounded to the
+    # operands' type (fp16 is scaled by 2^10 first, so 2^-35 is its least)
+    rel = 2 * (ez + el)[:, None] + 16 * U
+    least = {F32: 2.0 ** -40, BF16: 2.0 ** -60, F16: 2.0 ** -35}[dt]
+    edz = (p * rel + ROUND[dt] * (p - hotm).abs() + least + 2 * U * hotm) * k.abs()
+    # gradient products: chains of at most 1024 additions between joins
+    eh = edz @ W.abs() + 1024 * U * (dz.abs() @ W.abs())
+    ew = edz.t() @ H.abs() + 1024 * U * (dz.abs().t() @ H.abs())
+    dH, dW = dz @ W, dz.t() @ H
+    return {"loss": (rl.sum() / c, (tol_rl * there).sum() / c + 64 * U * rl.abs().sum() / c),
+            "row_loss": (rl, tol_rl * there),
+            "dH": (dH, eh + ROUND[dt] * dH.abs() + LEAST[dt]), "dW": (dW, ew + ROUND[dt] * dW.abs() + LEAST[dt])}
+
+
+def xent_check(got, ref, grads=True):
+    for name in ("loss", "row_loss") + (("dH", "dW") if grads else ()):
+        near(getattr(got, name), *ref[name], name)
+
+
+XENT = [(1, 1, 1), (1, 8, 2), (2, 3, 5), (7, 16, 64), (1, 64, 1000), (5, 31, 333), (16, 128, 4097), (17, 40, 129),
+        (33, 200, 513), (64, 64, 64), (100, 100, 41), (129, 65, 257), (200, 512, 300), (300, 256, 2), (1000, 24, 7),
+        (257, 96, 1025), (513, 130, 700), (40, 1024, 600), (1030, 41, 1031), (64, 256, 9000), (3000, 72, 100),
+        (9000, 33, 41), (5000, 300, 24)]
+
+
+@pytest.mark.parametrize("dt", [F32, BF16, F16])
+@pytest.mark.parametrize("t,d,v", XENT)
+def test_linear_xent(t, d, v, dt):
+    H, W, y = xent_data(t, d, v, dt, t + 3 * d + 7 * v)
+    y[0] = v // 2
+    ref = xent_ref(H, W, y)
+    xent_check(aires.linear_xent(H.cuda(), W.cuda(), y.cuda()), ref)
+    xent_check(aires.linear_xent(H.cuda(), W.cuda(), y.int().cuda(), grads=False), ref, False)
+
+
+def test_linear_xent_large_table():
+    """More of the table than one piece of the workspace holds."""
+    t, d, v = 3000, 40, 150001
+    for dt in (BF16, F32):
+        H, W, y = xent_data(t, d, v, dt, 12)
+        xent_check(aires.linear_xent(H.cuda(), W.cuda(), y.cuda()), xent_ref(H, W, y))
+
+
+@pytest.mark.parametrize("dt", [F32, BF16, F16])
+def test_linear_xent_reductions_and_scale(dt):
+    H, W, y = xent_data(90, 50, 70, dt, 4)
+    for red, scale in (("sum", 1.0), ("sum", -0.25), ("mean", 8.0)):
+        xent_check(aires.linear_xent(H.cuda(), W.cuda(), y.cuda(), reduction=red, grad_scale=scale),
+                   xent_ref(H, W, y, red == "mean", scale))
+
+
+def test_linear_xent_against_differences():
+    H, W, y = xent_data(5, 9, 11, F32, 6)
+    got = aires.linear_xent(H.cuda(), W.cuda(), y.cuda())
+    h = 1e-6
+
+    def value(H, W):
+        z = H @ W.t()
+        ok = (y >= 0) & (y < 11)
+        rows = torch.logsumexp(z, 1)[ok] - z[ok, y[ok]]
+        return rows.mean()
+
+    for name, k in (("dH", 0), ("dW", 1)):
+        at = [H.double(), W.double()]
+        want = torch.empty_like(at[k])
+        for i in range(want.numel()):
+            hi, lo = [a.clone() for a in at], [a.clone() for a in at]
+            hi[k].view(-1)[i] += h
+            lo[k].view(-1)[i] -= h
+            want.view(-1)[i] = (value(*hi) - value(*lo)) / (2 * h)
+        near(getattr(got, name), want, 1e-5 * (1 + want.abs()), name)
+
+
+@pytest.mark.parametrize("t,d,v", [(5, 20, 30), (300, 64, 50), (64, 64, 3000)])
+@pytest.mark.parametrize("dt", [F32, BF16, F16])
+def test_linear_xent_rows_without_a_label(t, d, v, dt):
+    H, W, y = xent_data(t, d, v, dt, 8, "none")
+    r = aires.linear_xent(H.cuda(), W.cuda(), y.cuda())
+    assert float(r.loss) == 0 and not r.row_loss.any() and not r.dH.any() and not r.dW.any()
+    # one labelled row among them, and values that are no numbers in a row without a label
+    y[1] = 3
+    ref = xent_ref(H, W, y)
+    xent_check(aires.linear_xent(H.cuda(), W.cuda(), y.cuda()), ref)
+    r = aires.linear_xent(H.cuda(), W.cuda(), y.cuda())
+    assert not r.row_loss[0].any() and not r.dH[0].any() and not r.dH[2:].any()
+
+
+@pytest.mark.parametrize("dt", [F32, BF16, F16])
+@pytest.mark.parametrize("t,d,v", [(9, 40, 60), (200, 64, 41), (130, 130, 2000)])
+def test_linear_xent_extreme_scores(t, d, v, dt):
+    """Scores far apart (the others' probabilities are 0), equal scores, and a
+    row with a NaN, which makes its own loss and gradient NaN and no other
+    row's."""
+    H, W, y = xent_data(t, d, v, F32, 5)
+    y[:] = torch.arange(t) % v
+    H *= 40
+    H[1] = 0
+    H, W = H.to(dt), W.to(dt)
+    ref = xent_ref(H, W, y)
+    got = aires.linear_xent(H.cuda(), W.cuda(), y.cuda())
+    xent_check(got, ref)
+    H[2, 5] = float("nan")
+    bad = aires.linear_xent(H.cuda(), W.cuda(), y.cuda())
+    assert bool(bad.row_loss[2].isnan()) and bool(bad.loss.isnan()) and bool(bad.dH[2].isnan().all())
+    keep = torch.arange(t, device="cuda") != 2
+    near(bad.row_loss[keep], ref["row_loss"][0][keep], ref["row_loss"][1][keep], "row_loss")
+    near(bad.dH[keep], ref["dH"][0][keep], ref["dH"][1][keep], "dH")
+
+
+def test_linear_xent_strides_and_streams():
+    for dt in (F32, BF16, F16):
+        H, W, y = xent_data(150, 72, 400, dt, 2)
+        ref = xent_ref(H, W, y)
+        wide = torch.full((150, 91), float("nan"), dtype=dt, device="cuda")
+        wide[:, 11:83] = H.cuda()
+        tall = torch.full((400, 77), float("nan"), dtype=dt, device="cuda")
+        tall[:, 5:77] = W.cuda()
+        xent_check(aires.linear_xent(wide[:, 11:83], tall[:, 5:77], y.cuda()), ref)
+        plain = aires.linear_xent(H.cuda(), W.cuda(), y.cuda())
+        torch.cuda.synchronize()
+        Hd, Wd, yd = H.cuda(), W.cuda(), y.cuda()
+        torch.cuda.synchronize()
+        for s in (torch.cuda.Stream(), torch.cuda.Stream()):
+            got = aires.linear_xent(Hd, Wd, yd, stream=s)
+            s.synchronize()
+            for n in ("loss", "row_loss", "dH", "dW"):
+                assert torch.equal(getattr(got, n), getattr(plain, n)), n
+
+
+def test_linear_xent_no_rows():
+    W = torch.randn(30, 20, device="cuda")
+    r = aires.linear_xent(torch.empty(0, 20, device="cuda"), W, torch.empty(0, dtype=torch.int64, device="cuda"))
+    assert float(r.loss) == 0 and r.dH.shape == (0, 20) and not r.dW.any()
+
+
+# ------------------------------------------------------------------- AdamW
+
+TOP = {"m": 448.0, "v": 57344.0}
+BITS = {"m": (3, -6), "v": (2, -14)}
+
+
+def hash_of(n, seed, k):
+    i = np.arange(n, dtype=np.uint64)
+    s = ((seed + k * 0x632BE5AB) * 0x85157AF5) % 2 ** 32
+    x = (i * 0x9E3779B1 + s) % 2 ** 32
+    x = ((x ^ (x >> np.uint64(16))) * 0x7C2E9D35) % 2 ** 32
+    x = ((x ^ (x >> np.uint64(15))) * 0x6A8F3B47) % 2 ** 32
+    x = x ^ (x >> np.uint64(16))
+    return {"m": (x % 65536).astype(np.float64), "v": (x // 65536).astype(np.float64)}
+
+
+def adam_ref(p, g, m, v, step, lr, b1, b2, eps, wd, gs):
+    g = g * gs
+    m = b1 * m + (1 - b1) * g
+    v = b2 * v + (1 - b2) * g * g
+    d = lr / (1 - b1 ** step) * m / (np.sqrt(v) / np.sqrt(1 - b2 ** step) + eps)
+    return p * (1 - lr * wd) - d, m, v, np.abs(p) + np.abs(d)
+
+
+HYPER = dict(step=3, lr=2e-2, betas=(0.9, 0.99), eps=1e-7, weight_decay=0.1)
+SHAPES = [(1,), (3,), (255,), (256,), (257,), (1023,), (4096,), (4097,), (77, 33), (0,), (20000,), (5, 1000)]
+
+
+def f64(t):
+    return t.double().cpu().numpy().reshape(-1)
+
+
+@pytest.mark.parametrize("pt,gt", list(itertools.product([F32, BF16, F16], [F32, BF16, F16])))
+def test_adamw_32(pt, gt):
+    g = gen(7)
+    params = [torch.randn(s, generator=g).to(pt) for s in SHAPES]
+    grads = [(torch.randn(s, generator=g) * 1e-2).to(gt) for s in SHAPES]
+    ms = [torch.randn(s, generator=g) * 1e-2 for s in SHAPES]
+    vs = [torch.rand(s, generator=g) * 1e-3 for s in SHAPES]
+    P, M, V = ([x.cuda() for x in y] for y in (params, ms, vs))
+    C = [torch.zeros_like(p, dtype=BF16) if k % 2 else None for k, p in enumerate(P)]
+    aires.adamw(P, [x.cuda() for x in grads], M, V, grad_scale=0.5, copies=C, **HYPER)
+    for k in range(len(SHAPES)):
+        p, m, v, mag = adam_ref(f64(params[k]), f64(grads[k]), f64(ms[k]), f64(vs[k]), 3, 2e-2, 0.9, 0.99, 1e-7, 0.1, 0.5)
+        mags = 0.9 * np.abs(f64(ms[k])) + 0.1 * np.abs(0.5 * f64(grads[k]))
+        # two products of rounded factors and a sum; den by the hardware's root and reciprocal
+        near(torch.from_numpy(f64(M[k])), torch.from_numpy(m), torch.from_numpy(8 * U * mags + 1e-44), "m")
+        near(torch.from_numpy(f64(V[k])), torch.from_numpy(v), torch.from_numpy(16 * U * v + 1e-44), "v")
+        # the update carries the error of m, which may have cancelled
+        den = np.sqrt(v) / np.sqrt(1 - 0.99 ** 3) + 1e-7
+        tol = 32 * U * mag + 2e-2 / (1 - 0.9 ** 3) * 8 * U * mags / den
+        near(torch.from_numpy(f64(P[k])), torch.from_numpy(p),
+             torch.from_numpy(tol + ROUND[pt] * np.abs(p) + LEAST[pt]), "p")
+        if C[k] is not None:
+            near(torch.from_numpy(f64(C[k])), torch.from_numpy(p), torch.from_numpy(tol + ROUND[BF16] * np.abs(p) * 1.01 + LEAST[BF16]), "copy")
+
+
+def check_codes(name, got, scale, x, r):
+    """Codes against the definition: floor of the distance plus the random
+    number, where rounding of x (16 U of it) may move a value across."""
+    n = x.size
+    bits, low = BITS[name]
+    blocks = np.zeros(-(-n // 256) * 256)
+    blocks[:n] = np.abs(x)
+    top = blocks.reshape(-1, 256).max(1)
+    want = np.where(top >= 2.0 ** -110, top / TOP[name], 0)
+    assert np.all(np.abs(scale - want) <= 32 * U * want), name
+    each = np.repeat(scale.astype(np.float64), 256)[:n]
+    y = np.divide(np.abs(x), each, out=np.zeros(n), where=each > 0)
+    e = np.maximum(np.floor(np.log2(np.maximum(y, 1e-300))), low)
+    lo, hi = [], []
+    for z, out in ((y * (1 - 64 * U) - 2.0 ** -30, lo), (y * (1 + 64 * U) + 2.0 ** -30, hi)):
+        z = np.maximum(z, 0)
+        unit = 2.0 ** (np.maximum(np.floor(np.log2(np.maximum(z, 1e-300))), low) - bits)
+        q = np.minimum(np.floor(z / unit + (r + 0.5) / 65536) * unit, TOP[name])
+        out.append(q)
+    assert e.size == n
+    lo, hi = lo[0], hi[0]
+    if name == "v":
+        hi = np.where((y > 0) & (hi == 0), 2.0 ** -16, hi)
+        lo = np.where((y > 2.0 ** -29) & (lo == 0), 2.0 ** -16, lo)
+    a = np.abs(got)
+    bad = ~((a >= lo) & (a <= hi))
+    assert not bad.any(), (name, int(bad.sum()), a[bad][:4], lo[bad][:4], hi[bad][:4])
+    assert np.all((got == 0) | (np.sign(got) == np.sign(x)))
+    assert np.mean(lo != hi) < 0.01  # the test says something
+
+
+@pytest.mark.parametrize("pt,gt", [(F32, F32), (F32, BF16), (BF16, F16), (F16, BF16)])
+def test_adamw_8(pt, gt):
+    g = gen(11)
+    params = [torch.randn(s, generator=g).to(pt) for s in SHAPES]
+    P = [p.cuda() for p in params]
+    M, V = aires.adamw_state(P, bits=8)
+    C = [torch.zeros_like(p, dtype=F16) if k % 3 else None for k, p in enumerate(P)]
+    old = [p.clone() for p in params]
+    for step, seed in ((1, 5), (2, 2 ** 32 - 1), (3, 77)):
+        grads = [(torch.randn(s, generator=g) * torch.randn(s, generator=g).mul(2).exp() * 1e-3).to(gt) for s in SHAPES]
+        before = [[f64(c) * np.repeat(f64(s), 256)[:c.numel()] for c, s in x] for x in (M, V)]
+        aires.adamw(P, [x.cuda() for x in grads], M, V, step=step, lr=2e-2, betas=(0.9, 0.99), eps=1e-7, weight_decay=0.1,
+                    seed=seed, copies=C)
+        for k, s in enumerate(SHAPES):
+            if params[k].numel() == 0:
+                continue
+            p, m, v, mag = adam_ref(f64(old[k]), f64(grads[k]), before[0][k], before[1][k], step, 2e-2, 0.9, 0.99, 1e-7, 0.1, 1.0)
+            mags = 0.9 * np.abs(before[0][k]) + 0.1 * np.abs(f64(grads[k]))
+            den = np.sqrt(v) / np.sqrt(1 - 0.99 ** step) + 1e-7
+            tol = 64 * U * mag + 2e-2 / (1 - 0.9 ** step) * 8 * U * mags / den
+            near(torch.from_numpy(f64(P[k])), torch.from_numpy(p), torch.from_numpy(tol + ROUND[pt] * np.abs(p) + LEAST[pt]), "p")
+            r = hash_of(params[k].numel(), seed, k)
+            # exact moments up to a few roundings: cancelled first moments are left to their neighbours
+            clear = np.abs(m) >= 0.05 * mags
+            x = np.where(clear, m, 0)
+            got = np.where(clear, f64(M[k][0]), 0)
+            whole = np.zeros(-(-m.size // 256) * 256)
+            whole[:m.size] = np.abs(m)
+            if np.array_equal(whole.reshape(-1, 256).argmax(1),
+                              np.pad(np.abs(x), (0, whole.size - m.size)).reshape(-1, 256).argmax(1)):
+                check_codes("m", got, f64(M[k][1]), x, r["m"])
+            check_codes("v", f64(V[k][0]), f64(V[k][1]), v, r["v"])
+            assert bool((V[k][0].float()[torch.from_numpy(v).view(params[k].shape).cuda() > 0] > 0).all())
+        old = [x.clone().cpu() for x in P]
+
+
+def test_adamw_8_rounding_keeps_the_mean():
+    """Over many seeds the rounded second moment has the mean of the exact one
+    (rounding to nearest would return the old code every time)."""
+    n, seeds = 256, 400
+    v0 = torch.full((n,), 1.0)
+    v0[:128] = torch.linspace(0.01, 0.9, 128)
+    total = np.zeros(n)
+    want = None
+    for seed in range(seeds):
+        p, g = torch.zeros(n, device="cuda"), torch.full((n,), 0.05, device="cuda")
+        M, V = aires.adamw_state([p], bits=8)
+        code = (v0 * 57344).to(torch.float8_e5m2)
+        V[0][0].copy_(code.cuda())
+        V[0][1].fill_(1 / 57344)
+        aires.adamw([p], [g], M, V, step=1, lr=0.0, betas=(0.9, 0.999), seed=seed)
+        total += f64(V[0][0]) * f64(V[0][1])
+        want = 0.999 * f64(code) * np.float64(np.float32(1 / 57344)) + 0.001 * 0.05 ** 2
+    # codes are a quarter apart at most: deviation of the mean 0.125 / sqrt(seeds), six of them
+    assert np.all(np.abs(total / seeds - want) <= 6 * 0.125 / seeds ** 0.5 * want)
+    assert abs((total / seeds).sum() / want.sum() - 1) < 6 * 0.125 / (seeds * n) ** 0.5
+
+
+def test_adamw_values_that_are_not_finite_stay_where_they_are():
+    n = 600
+    g = torch.randn(n, generator=gen(3)) * 1e-2
+    clean = [torch.zeros(n, device="cuda")]
+    M0, V0 = aires.adamw_state(clean, bits=8)
+    aires.adamw(clean, [g.cuda()], M0, V0, step=1, lr=1e-2)
+    bad = g.clone()
+    at = [5, 300, 599]
+    bad[at[0]], bad[at[1]], bad[at[2]] = float("inf"), float("nan"), -float("inf")
+    for bits in (8, 32):
+        P = [torch.zeros(n, device="cuda")]
+        M, V = aires.adamw_state(P, bits=bits)
+        aires.adamw(P, [bad.cuda()], M, V, step=1, lr=1e-2)
+        rest = torch.ones(n, dtype=torch.bool)
+        rest[at] = False
+        assert bool(P[0].cpu()[at].isnan().all()) and bool(P[0].cpu()[rest].isfinite().all())
+        assert torch.equal(P[0].cpu()[rest], clean[0].cpu()[rest])
+        if bits == 8:
+            assert bool(M[0][0].float().cpu()[at].isnan().all()) and bool(M[0][0].float().cpu()[rest].isfinite().all())
+            # a value left out does not change the others' scale unless it was the largest
+            assert bool(M[0][1].isfinite().all()) and bool(V[0][1].isfinite().all())
+    # nothing at all: zero gradients on zero moments leave zeros and parameters that only decay
+    P = [torch.ones(n, device="cuda")]
+    M, V = aires.adamw_state(P, bits=8)
+    aires.adamw(P, [torch.zeros(n, device="cuda")], M, V, step=1, lr=1e-2, weight_decay=0.5)
+    assert not M[0][0].float().any() and not M[0][1].any() and not V[0][0].float().any() and not V[0][1].any()
+    assert bool((P[0] == np.float32(1 - 0.005)).all())
+
+
+def test_adamw_many_tensors_and_offsets():
+    """More tensors than one launch describes, 8- and 32-bit moments mixed,
+    views at odd offsets: the same as one by one."""
+    g = gen(13)
+    n = 97
+    shapes = [(1 + 37 * k,) for k in range(n)]
+    flat = torch.randn(sum(s[0] for s in shapes) + 3, generator=g).cuda()
+    grads_flat = (torch.randn(flat.numel(), generator=g) * 1e-2).cuda().to(BF16)
+    at, P, G = 3, [], []
+    for s in shapes:
+        P.append(flat[at:at + s[0]])
+        G.append(grads_flat[at:at + s[0]])
+        at += s[0]
+    M8, V8 = aires.adamw_state(P, bits=8)
+    M32, V32 = aires.adamw_state(P, bits=32)
+    M = [M8[k] if k % 3 else M32[k] for k in range(n)]
+    V = [V8[k] if k % 3 else V32[k] for k in range(n)]
+    alone = [p.clone() for p in P]
+    A8, B8 = aires.adamw_state(P, bits=8)
+    A32, B32 = aires.adamw_state(P, bits=32)
+    for step in (1, 2):
+        aires.adamw(P, G, M, V, step=step, lr=1e-2, seed=step)
+        for k in range(n):
+            a, b = (A8[k], B8[k]) if k % 3 else (A32[k], B32[k])
+            # the tensor's position in the call is part of what its rounding is drawn from
+            seed = (step + k * 0x632BE5AB) % 2 ** 32
+            aires.adamw([alone[k]], [G[k].clone()], [a], [b], step=step, lr=1e-2, seed=seed)
+    for k in range(n):
+        assert torch.equal(alone[k], P[k]), k
+        if k % 3:
+            assert torch.equal(A8[k][0].view(torch.uint8), M8[k][0].view(torch.uint8)) and torch.equal(A8[k][1], M8[k][1])
+            assert torch.equal(B8[k][0].view(torch.uint8), V8[k][0].view(torch.uint8)) and torch.equal(B8[k][1], V8[k][1])
+
+
+def test_adamw_on_another_stream():
+    P = [torch.ones(10000, device="cuda")]
+    G = [torch.full((10000,), 0.1, device="cuda")]
+    M, V = aires.adamw_state(P, bits=32)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    for step in (1, 2, 3):
+        aires.adamw(P, G, M, V, step=step, lr=1e-2, weight_decay=0.0, stream=s)
+    s.synchronize()
+    assert torch.allclose(P[0], torch.full_like(P[0], 0.97), rtol=1e-6)
+
+
+# ---------------------------------------------------------------- refusals
+
+def test_refusals_of_the_binding():
+    X = torch.zeros(4, 6, device="cuda")
+    one = torch.ones(6, device="cuda")
+    st = torch.zeros(4, device="cuda")
+    y = torch.zeros(4, dtype=torch.int64, device="cuda")
+    for call in (lambda: aires.layer_norm(X.t()), lambda: aires.layer_norm(X, one[:5]), lambda: aires.layer_norm(X[0]),
+                 lambda: aires.layer_norm(X.cpu()), lambda: aires.layer_norm(X[:1].expand(4, 6)),
+                 lambda: aires.layer_norm(X, one.repeat(2)[::2]),
+                 lambda: aires.layer_norm_backward(X[:3], X, st, st), lambda: aires.layer_norm_backward(X, X, st[:3], st),
+                 lambda: aires.linear_xent(X, X[:, :5], y), lambda: aires.linear_xent(X, X, y[:3]),
+                 lambda: aires.linear_xent(X, X.half(), y), lambda: aires.linear_xent(X, X, y, reduction="none"),
+                 lambda: aires.adamw([X], [X[:2]], [X], [X], step=1, lr=1.0),
+                 lambda: aires.adamw([X], [X], [X], [], step=1, lr=1.0),
+                 lambda: aires.adamw([X.t()], [X.t()], [X], [X], step=1, lr=1.0),
+                 lambda: aires.adamw([X], [X], [X.half()], [X], step=1, lr=1.0),
+                 lambda: aires.adamw_state([X], bits=4)):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: aires.layer_norm(X.double()), lambda: aires.layer_norm(X, one, one.half()),
+                 lambda: aires.layer_norm(X, out=torch.zeros_like(X), out_dtype=F16),
+                 lambda: aires.layer_norm_backward(X, X, st.double(), st), lambda: aires.linear_xent(X, X, st)):
+        with pytest.raises(TypeError):
+            call()
+    for call in (lambda: aires.layer_norm(X, eps=-1.0), lambda: aires.layer_norm(X, eps=float("nan")),
+                 lambda: aires.linear_xent(X, X, y, grad_scale=float("inf")),
+                 lambda: aires.adamw([X], [X], [X.clone()], [X.clone()], step=0, lr=1.0),
+                 lambda: aires.adamw([X], [X], [X.clone()], [X.clone()], step=1, lr=1.0, betas=(1.0, 0.9)),
+                 lambda: aires.adamw([X], [X], [X.clone()], [X.clone()], step=1, lr=float("nan"))):
+        with pytest.raises(aires.AiresError) as e:
+            call()
+        assert e.value.status == B_.E_INVALID_ARG
+    with pytest.raises(aires.AiresError) as e:
+        aires.linear_xent(X, torch.zeros(0, 6, device="cuda"), y)
+    assert e.value.status == B_.E_DIM
