@@ -1,0 +1,244 @@
+// Matrix-core tile products of 16-bit operands (gfx950, wave64).
+//
+// acc(m, n) = sum_k A(m, k) B(n, k) for a tile of TM x TN by four wavefronts,
+// each WM x WN in 32 x 32 x 16 MFMAs.  An operand is either K-contiguous (row
+// m holds its k) or K-major (row k holds its m); both are staged as they lie
+// in memory, 32 k a step, by loads that go from global memory straight to
+// LDS (no registers, no transposed copies).  K-contiguous fragments are read
+// 16 bytes a lane; K-major ones with the transposing LDS read, which hands a
+// lane four k of its column.  16-byte chunks are placed XORed with their row
+// so that neither read meets bank conflicts: the swap is made on the global
+// address of each lane, since the destination of such a load is fixed.
+//
+// Three stages: while step i is multiplied, the loads of i + 1 have had one
+// step to arrive and those of i + 2 are issued, with one barrier a step.
+// 72 KB for 256 x 128: two workgroups a CU, so one's epilogue and barriers run
+// under the other's products.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace aires {
+namespace kern {
+namespace {
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr int BK = 32;        // k of a stage
+constexpr int STAGES = 3;
+constexpr int TILE_BLOCK = 256;
+
+// An operand in memory.  K-contiguous: `rows` are m, `cols` k (a multiple of
+// BK, rows 16-byte aligned).  K-major: `rows` are k, `cols` m (a multiple of
+// 8).  An fp32 operand is three 16-bit planes, `plane` elements apart.
+struct Panel {
+  const uint16_t* data;
+  int64_t plane, ld, rows, cols;
+};
+
+// Products of planes that make up an fp32 product: all but those below its
+// own rounding (planes 1 and 2, 2 and 2).  Small ones come first.
+__device__ __forceinline__ int plane_a(int seg) { return (0x001102 >> (4 * seg)) & 15; }
+__device__ __forceinline__ int plane_b(int seg) { return (0x010120 >> (4 * seg)) & 15; }
+
+template <bool F16>
+__device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
+  if constexpr (F16)
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(1))) void global_void;
+
+// One operand's share of a stage: SPAN x 32 elements, 1 KB an instruction.
+template <int SPAN, bool KMAJOR>
+struct Stager {
+  static constexpr int COUNT = SPAN / 64;   // instructions a wavefront issues
+  static constexpr int BYTES = SPAN * BK * 2;
+  const char* base;      // first row of the tile, advanced along k
+  int64_t step;          // bytes a step
+  uint32_t off[COUNT];
+  int64_t ld2, left;     // K-major: bytes a row, rows from the tile's k on
+
+  // m0: first m of the tile (m0 < extent of m); k0: first k, a multiple of BK
+  __device__ void init(const Panel& p, int plane, int64_t m0, int64_t k0, int wave, int lane) {
+    const char* d = reinterpret_cast<const char*>(p.data + plane * p.plane);
+    ld2 = p.ld * 2;
+    if constexpr (!KMAJOR) {
+      base = d + m0 * ld2 + k0 * 2;
+      step = BK * 2;
+      const int64_t last = p.rows - 1 - m0;
+#pragma unroll
+      for (int j = 0; j < COUNT; ++j) {
+        const int r = (wave * COUNT + j) * 16 + lane / 4;
+        const int c = (lane & 3) ^ ((r >> 1) & 3);
+        // rows past the end repeat the last one; their results are not used
+        off[j] = (uint32_t)((r < last ? r : last) * ld2 + c * 16);
+      }
+    } else {
+      base = d + k0 * ld2 + m0 * 2;
+      step = BK * ld2;
+      left = p.rows - k0;
+      place(p.cols - 8 - m0, wave, lane);
+    }
+  }
+  // K-major offsets; rows past the end of k repeat the last one (the other
+  // operand holds zeros there).
+  __device__ void place(int64_t last_col, int wave, int lane) {
+    constexpr int chunks = SPAN / 8, rows = 64 / chunks;
+#pragma unroll
+    for (int j = 0; j < COUNT; ++j) {
+      const int k = (wave * COUNT + j) * rows + lane / chunks;
+      const int c = ((lane % chunks) ^ ((k & 3) * 2)) * 8;
+      off[j] = (uint32_t)((k < left ? k : left - 1) * ld2 + (c < last_col ? c : last_col) * 2);
+    }
+  }
+  __device__ void issue(char* lds, int wave) const {
+#pragma unroll
+    for (int j = 0; j < COUNT; ++j)
+      __builtin_amdgcn_global_load_lds((global_void*)(base + off[j]), (lds_void*)(lds + (wave * COUNT + j) * 1024), 16,
+                                       0, 0);
+  }
+};
+
+// Fragment reads of one operand: W consecutive m of the tile from `first`.
+template <int SPAN, bool KMAJOR>
+struct Reader {
+  uint32_t at[2];
+  __device__ Reader(int first, int lane) {
+    if constexpr (!KMAJOR) {
+      const int r = first + (lane & 31), s = (r >> 1) & 3;
+      at[0] = (uint32_t)(r * (BK * 2) + (((lane >> 5) ^ s) << 4));
+      at[1] = at[0] ^ 32;  // the second 16 k: chunks 2 and 3
+    } else {
+      const int g = lane >> 4, i = lane & 15;
+      const int k = 8 * (g >> 1) + i / 4;
+      const int c = first / 8 + (g & 1) * 2 + ((i & 3) >> 1);
+#pragma unroll
+      for (int odd = 0; odd < 2; ++odd)
+        at[odd] = (uint32_t)(k * (SPAN * 2) + (((c + 4 * odd) ^ ((i / 4) * 2)) << 4) + (i & 1) * 8);
+    }
+  }
+  // rows [32 t, 32 t + 32) of the wavefront's span, k [16 kk, 16 kk + 16)
+  __device__ __forceinline__ s16x8 get(const char* lds, int t, int kk) const {
+    if constexpr (!KMAJOR) {
+      return *reinterpret_cast<const s16x8*>(lds + at[kk] + t * (32 * BK * 2));
+    } else {
+      typedef __attribute__((address_space(3))) s16x4 lds4;
+      const char* p = lds + at[t & 1] + (t >> 1) * 128 + kk * 16 * (SPAN * 2);
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)p);
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(p + 4 * (SPAN * 2)));
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+  }
+};
+
+template <int TM, int TN, int WM, int WN, bool AK, bool BK_, bool F16>
+struct Tile {
+  static_assert(TM / WM * (TN / WN) == 4, "four wavefronts");
+  static constexpr int MT = WM / 32, NT = WN / 32;
+  static constexpr int STAGE = (TM + TN) * BK * 2;
+  static constexpr int LDS = STAGE * STAGES;
+  static constexpr int LOADS = TM / 64 + TN / 64;  // a wavefront's loads of a stage
+
+  // Products over k steps [s0, s1) of BK, for each of `segs` plane pairs.
+  static __device__ __forceinline__ void run(const Panel& A, int64_t m0, const Panel& B, int64_t n0, int s0, int s1,
+                                             int segs, char* lds, f32x16 (&acc)[MT][NT]) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / (TN / WN), wn = wave % (TN / WN);
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+    Stager<TM, AK> sa;
+    Stager<TN, BK_> sb;
+    const Reader<TM, AK> ra(wm * WM, lane);
+    const Reader<TN, BK_> rb(wn * WN, lane);
+    const int per = s1 - s0, total = per * segs;
+    int seg = 0, at = 0;  // of the next stage to issue
+    auto issue = [&](int stage) {
+      if (at == per || (seg == 0 && at == 0)) {
+        if (at == per) {
+          at = 0;
+          ++seg;
+        }
+        const int pa = segs == 1 ? 0 : plane_a(seg), pb = segs == 1 ? 0 : plane_b(seg);
+        sa.init(A, pa, m0, (int64_t)s0 * BK, wave, lane);
+        sb.init(B, pb, n0, (int64_t)s0 * BK, wave, lane);
+      }
+      if constexpr (AK)
+        if (sa.left < BK) sa.place(A.cols - 8 - m0, wave, lane);
+      if constexpr (BK_)
+        if (sb.left < BK) sb.place(B.cols - 8 - n0, wave, lane);
+      char* to = lds + stage * STAGE;
+      sa.issue(to, wave);
+      sb.issue(to + TM * BK * 2, wave);
+      sa.base += sa.step;
+      sb.base += sb.step;
+      if constexpr (AK) sa.left -= BK;
+      if constexpr (BK_) sb.left -= BK;
+      ++at;
+    };
+    issue(0);
+    if (total > 1) issue(1);
+    int cur = 0;
+    for (int s = 0; s < total; ++s) {
+      // this step's loads are the older ones; LDS reads of the last step are
+      // done before any wavefront overwrites their stage
+      if (s + 1 < total) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LOADS) : "memory");
+      else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      if (s + 2 < total) issue(cur == 0 ? 2 : cur - 1);
+      const char* a = lds + cur * STAGE;
+      const char* b = a + TM * BK * 2;
+#pragma unroll
+      for (int kk = 0; kk < BK / 16; ++kk) {
+        s16x8 fa[MT], fb[NT];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) fa[i] = ra.get(a, i, kk);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) fb[j] = rb.get(b, j, kk);
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int j = 0; j < NT; ++j) acc[i][j] = mfma<F16>(fa[i], fb[j], acc[i][j]);
+      }
+      cur = cur == 2 ? 0 : cur + 1;
+    }
+  }
+
+  // m and n of register r of acc[i][j] within the tile
+  static __device__ __forceinline__ int row(int i, int r) {
+    const int lane = threadIdx.x & 63, wm = (threadIdx.x >> 6) / (TN / WN);
+    return wm * WM + i * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
+  }
+  static __device__ __forceinline__ int col(int j) {
+    const int lane = threadIdx.x & 63, wn = (threadIdx.x >> 6) % (TN / WN);
+    return wn * WN + j * 32 + (lane & 31);
+  }
+};
+
+// Workgroups go round-robin to the 8 XCDs: give each XCD one run of tiles, in
+// groups of `group` rows by all columns, so that its L2 sees the same panels
+// again.  b of total -> (y, x) in a grid of ny by nx.
+__device__ __forceinline__ void place_tile(int64_t b, int64_t ny, int64_t nx, int group, int64_t& y, int64_t& x) {
+  const int64_t total = ny * nx, per = total / 8, more = total % 8, xcd = b % 8;
+  const int64_t id = xcd * per + (xcd < more ? xcd : more) + b / 8;
+  const int64_t band = id / (group * nx), first = band * group;
+  const int64_t high = ny - first < group ? ny - first : group, in = id - band * group * nx;
+  y = first + in % high;
+  x = in / high;
+}
+
+}  // namespace
+}  // namespace kern
+}  // namespace aires

@@ -1,206 +1,415 @@
 // Softmax cross entropy of scores H W^T against labels, with both gradients,
 // without storing the scores (gfx950).
 //
-// With z = H W^T, s_i = log sum_j exp(z_ij): row_loss_i = s_i - z_i,label and
-// dz_ij = scale (exp(z_ij - s_i) - [j = label(i)]) for labelled rows, 0 for
-// others; dH = dz W, dW = dz^T H.  Scores are computed twice: once for the
-// maxima and sums of exponentials of each tile's rows, joined to s, and once
-// more in pieces of the table for dz, which goes to the workspace for the
-// two gradient products.
+// With z = H W^T and s_i = log sum_j exp(z_ij): row_loss_i = s_i - z_i,label,
+// dz_ij = scale (exp(z_ij - s_i) - [j = label(i)]) for labelled rows and 0 for
+// others, dH = dz W, dW = dz^T H.  2 T V D flops make the scores and as many
+// each gradient.  The scores are made twice, 8 T V D in all: once for each
+// tile's row maxima and sums of exponentials, joined to those of the row, and
+// once more in pieces of the table for dz, which goes to the workspace in 16
+// bits (a piece fits the 256 MB cache) and is read by both gradient products.
+//
+// All four products run on the matrix cores (tile.h).  fp32 operands are
+// split into three bf16 planes, whose sum is exact, and six of the nine
+// products of planes are added: what is left out is below fp32's own
+// rounding.  Scores are laid out with the table along the accumulator's
+// registers, so that a lane holds 64 scores of one row and its maximum and sum
+// need a single exchange between lanes.
 #include "train.h"
 
 #include <algorithm>
 
 #include "dense.h"
+#include "tile.h"
 
 namespace aires {
 namespace kern {
 namespace {
 
-constexpr int TILE = 64, KSTEP = 16, BLOCK = 256;
+constexpr int TV = 256, TT = 128;      // a tile of scores: table by rows of H
+constexpr int GM = 256, GN = 128;      // a tile of a gradient product
 constexpr int64_t kPieceBytes = int64_t(256) << 20;  // dz of one piece of the table
+constexpr int ROWS = 64, SLICES = 16;  // k_rows: rows of a workgroup, shares of the tiles
+constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.693147180559945309417f;
+constexpr float F16_UP = 1024.f;       // dz in fp16 is held times this: 2^-35 is its least step
 
 __device__ __forceinline__ int64_t label_at(const void* labels, int i64, int64_t i) {
   return i64 ? static_cast<const int64_t*>(labels)[i] : (int64_t)static_cast<const int32_t*>(labels)[i];
 }
 
-// acc[i][j] += sum_k A(m0 + 4 ty + i, k) B(n0 + 4 tx + j, k): element (r, k)
-// of an operand is at data[r * row + k * step].
-struct Operand {
-  const void* data;
-  int type;
-  int64_t rows, row, step;
-};
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-__device__ __forceinline__ void tile_product(const Operand& A, int64_t m0, const Operand& B, int64_t n0, int64_t K,
-                                             float (&a)[KSTEP][TILE + 4], float (&b)[KSTEP][TILE + 4],
-                                             float (&acc)[4][4]) {
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+// Joins two (maximum, sum of exponentials) in base 2; equal maxima (of minus
+// infinity too) need no scaling.
+__device__ __forceinline__ void join(float& m, float& s, float m1, float s1) {
+  const float top = fmaxf(m, m1);
+  s = (m == top ? s : s * exp2_fast(m - top)) + (m1 == top ? s1 : s1 * exp2_fast(m1 - top));
+  m = top;
+}
+
+// ---------------------------------------------------------------- operands
+
+// Rows of X as 16-bit planes of `width` columns, zeros past the end.
+__global__ __launch_bounds__(256) void k_pack(Mat X, uint16_t* to, int64_t plane, int64_t width, int planes) {
+  const int64_t per = width / 4, total = X.rows * per;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / per, c = (i - r * per) * 4, at = r * X.ld + c;
+    uint16_t* out = to + r * width + c;
+    if (planes == 1) {
+      const uint16_t* x = static_cast<const uint16_t*>(X.data);
+      u16x4_el v = {0, 0, 0, 0};
+      if (c + 4 <= X.cols) v = *reinterpret_cast<const u16x4_el*>(x + at);
+      else
+        for (int k = 0; k < 4; ++k)
+          if (c + k < X.cols) v[k] = x[at + k];
+      *reinterpret_cast<u16x4_el*>(out) = v;
+    } else {
+      float x[4];
+      if (c + 4 <= X.cols) load4<DT_F32>(X.data, at, x);
+      else
+        for (int k = 0; k < 4; ++k) x[k] = c + k < X.cols ? load1<DT_F32>(X.data, at + k) : 0.f;
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+      for (int p = 0; p < 3; ++p) {
+        u16x4_el v;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
-  for (int64_t k0 = 0; k0 < K; k0 += KSTEP) {
-    for (int e = threadIdx.x; e < KSTEP * TILE; e += BLOCK) {
-      // neighbouring threads along the operand's contiguous direction
-      const int ra = A.step == 1 ? e / KSTEP : e % TILE, ka = A.step == 1 ? e % KSTEP : e / TILE;
-      a[ka][ra] = m0 + ra < A.rows && k0 + ka < K ? load1(A.data, A.type, (m0 + ra) * A.row + (k0 + ka) * A.step) : 0.f;
-      const int rb = B.step == 1 ? e / KSTEP : e % TILE, kb = B.step == 1 ? e % KSTEP : e / TILE;
-      b[kb][rb] = n0 + rb < B.rows && k0 + kb < K ? load1(B.data, B.type, (n0 + rb) * B.row + (k0 + kb) * B.step) : 0.f;
+        for (int k = 0; k < 4; ++k) {
+          v[k] = f32_to_bf16(x[k]);
+          x[k] -= bf16_to_f32(v[k]);
+        }
+        *reinterpret_cast<u16x4_el*>(out + p * plane) = v;
+      }
     }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < KSTEP; ++k)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] += a[k][ty * 4 + i] * b[k][tx * 4 + j];
-    __syncthreads();
   }
 }
+
+// ------------------------------------------------------------------ scores
 
 struct Scores {
-  Operand H, W;
-  int64_t D;
+  Panel W, H;
+  int64_t T, V, v0, v1;   // the piece [v0, v1) of the table
+  int steps, segs;
+  float2* part;           // [tile][t]: maximum, sum (base 2)
+  const float* top; const float* inv;  // of whole rows
   const void* labels; int i64;
-  float2* part;      // [tile of the table][t]: maximum, sum of exp(z - maximum)
-  float* target;     // z of the row's label
-  const float* lse;
-  const float* count;
-  float grad_scale;
-  int64_t v0, v1;    // piece of the table
-  float* dz; int64_t ldz;
+  uint16_t* dz; int64_t plane, ldz;
 };
 
-// Tile of scores: statistics of its rows (GRAD false) or dz.
-template <bool GRAD>
-__global__ __launch_bounds__(BLOCK) void k_scores(Scores s) {
-  __shared__ float a[KSTEP][TILE + 4], b[KSTEP][TILE + 4];
-  const int64_t t0 = (int64_t)blockIdx.y * TILE, v0 = s.v0 + (int64_t)blockIdx.x * TILE;
-  Operand W = s.W;
-  W.rows = s.v1;
-  float acc[4][4];
-  tile_product(s.H, t0, W, v0, s.D, a, b, acc);
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+template <bool GRAD, int TYPE>
+__global__ __launch_bounds__(TILE_BLOCK, 2) void k_scores(Scores s) {
+  constexpr bool F16 = TYPE == DT_F16;
+  constexpr int PLANES = TYPE == DT_F32 ? 3 : 1;
+  using T_ = Tile<TV, TT, 128, 64, false, false, F16>;
+  __shared__ __attribute__((aligned(16))) char lds[T_::LDS];
+  int64_t vt, tt;
+  place_tile(blockIdx.x, (s.v1 - s.v0 + TV - 1) / TV, (s.T + TT - 1) / TT, 8, vt, tt);
+  const int64_t v0 = s.v0 + vt * TV, t0 = tt * TT;
+  f32x16 acc[T_::MT][T_::NT];
+  T_::run(s.W, v0, s.H, t0, 0, s.steps, s.segs, lds, acc);
+  const int lane = threadIdx.x & 63, wm = threadIdx.x >> 7;
+  __syncthreads();  // the stages' LDS changes its use
+
+  if constexpr (!GRAD) {
+    if (v0 + TV > s.V) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int64_t t = t0 + ty * 4 + i;
-    const bool row = t < s.H.rows;
-    const int64_t label = row ? label_at(s.labels, s.i64, t) : -1;
-    if constexpr (GRAD) {
-      if (!row) continue;
-      const bool there = label >= 0 && label < s.W.rows;
-      const float scale = there ? s.grad_scale / s.count[0] : 0.f, lse = s.lse[t];
+      for (int i = 0; i < T_::MT; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int64_t v = v0 + tx * 4 + j;
-        if (v < s.v1)
-          s.dz[t * s.ldz + (v - s.v0)] = there ? scale * (expf(acc[i][j] - lse) - (v == label ? 1.f : 0.f)) : 0.f;
-      }
-    } else {
+        for (int r = 0; r < 16; ++r)
+          if (v0 + T_::row(i, r) >= s.V)
+#pragma unroll
+            for (int j = 0; j < T_::NT; ++j) acc[i][j][r] = -INFINITY;
+    }
+    float2* half = reinterpret_cast<float2*>(lds);  // of the upper half of the table's rows
+#pragma unroll
+    for (int j = 0; j < T_::NT; ++j) {
       float top = -INFINITY;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int64_t v = v0 + tx * 4 + j;
-        if (v < s.v1) top = fmaxf(top, acc[i][j]);
-        if (v == label && v < s.v1) s.target[t] = acc[i][j];
-      }
+      for (int i = 0; i < T_::MT; ++i)
 #pragma unroll
-      for (int o = 1; o < 16; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, acc[i][j][r]);
+      top = fmaxf(top, __shfl_xor(top, 32)) * LOG2E;
+      const float from = top == -INFINITY ? 0.f : top;  // a NaN still reaches the sum
       float sum = 0.f;
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (v0 + tx * 4 + j < s.v1) sum += top == -INFINITY && acc[i][j] == top ? 0.f : expf(acc[i][j] - top);
+      for (int i = 0; i < T_::MT; ++i)
 #pragma unroll
-      for (int o = 1; o < 16; o <<= 1) sum += __shfl_xor(sum, o);
-      if (row && tx == 0) s.part[(int64_t)blockIdx.x * s.H.rows + t] = make_float2(top, sum);
+        for (int r = 0; r < 16; ++r) sum += exp2_fast(fmaf(acc[i][j][r], LOG2E, -from));
+      sum += __shfl_xor(sum, 32);
+      const int c = T_::col(j);
+      if (wm == 1 && lane < 32) half[c] = make_float2(top, sum);
+      acc[0][j][0] = top;
+      acc[0][j][1] = sum;
+    }
+    __syncthreads();
+    if (wm == 0 && lane < 32)
+#pragma unroll
+      for (int j = 0; j < T_::NT; ++j) {
+        const int c = T_::col(j);
+        float m = acc[0][j][0], x = acc[0][j][1];
+        join(m, x, half[c].x, half[c].y);
+        if (t0 + c < s.T) s.part[vt * s.T + t0 + c] = make_float2(m, x);
+      }
+  } else {
+#pragma unroll
+    for (int j = 0; j < T_::NT; ++j) {
+      const int64_t t = t0 + T_::col(j);
+      const int64_t label = t < s.T ? label_at(s.labels, s.i64, t) : -1;
+      const bool there = label >= 0 && label < s.V;
+      const float top = there ? s.top[t] : 0.f, inv = there ? s.inv[t] * (F16 ? F16_UP : 1.f) : 0.f;
+#pragma unroll
+      for (int i = 0; i < T_::MT; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float p = exp2_fast(fmaf(acc[i][j][r], LOG2E, -top)) * inv;
+          acc[i][j][r] = there ? p : 0.f;  // a score that is no number stays out of rows without a label
+        }
+      const int64_t first = v0 + wm * 128;
+      if (__any(there && label >= first && label < first + 128)) {
+        const int at = there && label >= first && label < first + 128 ? (int)(label - v0) : -1;
+#pragma unroll
+        for (int i = 0; i < T_::MT; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (T_::row(i, r) == at) acc[i][j][r] -= F16 ? F16_UP : 1.f;
+      }
+    }
+    if (v0 + TV > s.v1) {
+#pragma unroll
+      for (int i = 0; i < T_::MT; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (v0 + T_::row(i, r) >= s.v1)
+#pragma unroll
+            for (int j = 0; j < T_::NT; ++j) acc[i][j][r] = 0.f;
+    }
+    // through LDS, so that rows of dz are written 512 bytes at a time
+#pragma unroll
+    for (int p = 0; p < PLANES; ++p) {
+      if (p) __syncthreads();
+#pragma unroll
+      for (int j = 0; j < T_::NT; ++j) {
+        const int c = T_::col(j);
+#pragma unroll
+        for (int i = 0; i < T_::MT; ++i)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            u16x4_el v;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const float x = acc[i][j][q * 4 + k];
+              v[k] = F16 ? f32_to_f16(x) : f32_to_bf16(x);
+              if constexpr (PLANES > 1) acc[i][j][q * 4 + k] = x - bf16_to_f32(v[k]);
+            }
+            const int at = T_::row(i, q * 4);
+            *reinterpret_cast<uint64_t*>(lds + c * (TV * 2) + (((at >> 3) ^ (c & 31)) << 4) + (at & 4) * 2) =
+                __builtin_bit_cast(uint64_t, v);
+          }
+      }
+      __syncthreads();
+      uint16_t* to = s.dz + p * s.plane + t0 * s.ldz + (v0 - s.v0);
+      const int ch = threadIdx.x & 31;
+#pragma unroll 4
+      for (int c = threadIdx.x >> 5; c < TT; c += TILE_BLOCK / 32)
+        *reinterpret_cast<uint4*>(to + c * s.ldz + ch * 8) =
+            *reinterpret_cast<const uint4*>(lds + c * (TV * 2) + ((ch ^ (c & 31)) << 4));
     }
   }
 }
 
-// s_i of each row from its tiles' statistics; row_loss.
-__global__ __launch_bounds__(BLOCK) void k_rows(Scores s, int64_t tiles, float* lse, float* row_loss) {
-  const int64_t t = (int64_t)blockIdx.x * BLOCK + threadIdx.x;
-  if (t >= s.H.rows) return;
-  float top = -INFINITY, sum = 0.f;
-  for (int64_t i = 0; i < tiles; ++i) {
-    const float2 p = s.part[i * s.H.rows + t];
-    const float up = fmaxf(top, p.x);
-    // exp(-inf - -inf) is no number: a side without a score adds nothing
-    sum = (top == -INFINITY ? 0.f * sum : sum * expf(top - up)) + (p.x == -INFINITY ? p.y : p.y * expf(p.x - up));
-    top = up;
-  }
-  const float l = top + logf(sum);
-  lse[t] = l;
-  const int64_t label = label_at(s.labels, s.i64, t);
-  row_loss[t] = label >= 0 && label < s.W.rows ? l - s.target[t] : 0.f;
-}
+// ---------------------------------------------------------- rows and loss
 
-// loss and the divisor c, by one workgroup in a fixed order.
-__global__ __launch_bounds__(1024) void k_loss(const void* labels, int i64, int64_t T, int64_t V, int mean,
-                                               const float* row_loss, float* count, float* loss) {
-  __shared__ double sums[1024];
-  __shared__ int64_t counts[1024];
-  double x = 0;
-  int64_t n = 0;
-  for (int64_t t = threadIdx.x; t < T; t += 1024) {
-    const int64_t l = label_at(labels, i64, t);
-    if (l >= 0 && l < V) {
-      ++n;
-      x += row_loss[t];
+struct Rows {
+  Mat H, W;
+  const void* labels; int i64;
+  const float2* part; int64_t tiles;
+  float* top; float* inv; float* row_loss;
+  double2* sums;  // a workgroup's losses and labelled rows
+};
+
+// Maximum and sum of each row from its tiles', and its loss: 64 rows, a
+// sixteenth of the tiles to each wavefront, then four rows' label scores.
+__global__ __launch_bounds__(ROWS * SLICES) void k_rows(Rows a) {
+  __shared__ float2 buf[SLICES][ROWS];
+  __shared__ float lse[ROWS];
+  __shared__ double2 sums[SLICES];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int64_t T = a.H.rows, t0 = (int64_t)blockIdx.x * ROWS, t = t0 + lane;
+  float m = -INFINITY, s = 0.f;
+  if (t < T) {
+#pragma unroll 4
+    for (int64_t i = w; i < a.tiles; i += SLICES) {
+      const float2 p = a.part[i * T + t];
+      join(m, s, p.x, p.y);
     }
   }
-  sums[threadIdx.x] = x;
-  counts[threadIdx.x] = n;
+  buf[w][lane] = make_float2(m, s);
   __syncthreads();
-  for (int o = 512; o > 0; o >>= 1) {
+  if (w == 0 && t < T) {
+    for (int i = 1; i < SLICES; ++i) join(m, s, buf[i][lane].x, buf[i][lane].y);
+    a.top[t] = m;
+    a.inv[t] = 1.f / s;
+    lse[lane] = (m + log2f(s)) * LN2;
+  }
+  __syncthreads();
+  double loss = 0, count = 0;
+  for (int i = 0; i < ROWS / SLICES; ++i) {
+    const int r = w * (ROWS / SLICES) + i;
+    const int64_t row = t0 + r;
+    if (row >= T) break;
+    const int64_t label = label_at(a.labels, a.i64, row);
+    float x = 0.f;
+    if (label >= 0 && label < a.W.rows) {
+      for (int64_t d = lane; d < a.H.cols; d += 64)
+        x = fmaf(load1(a.H.data, a.H.type, row * a.H.ld + d), load1(a.W.data, a.W.type, label * a.W.ld + d), x);
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o);
+      x = lse[r] - x;
+      loss += x;
+      count += 1;
+    }
+    if (lane == 0) a.row_loss[row] = x;
+  }
+  if (lane == 0) sums[w] = make_double2(loss, count);
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < SLICES; ++i) {
+      loss += sums[i].x;
+      count += sums[i].y;
+    }
+    a.sums[blockIdx.x] = make_double2(loss, count);
+  }
+}
+
+// loss, and what dz is multiplied with; one workgroup, a fixed order.
+__global__ __launch_bounds__(256) void k_loss(const double2* sums, int64_t n, int mean, float grad_scale, float* scale,
+                                              float* loss) {
+  __shared__ double2 buf[256];
+  double x = 0, c = 0;
+  for (int64_t i = threadIdx.x; i < n; i += 256) {
+    x += sums[i].x;
+    c += sums[i].y;
+  }
+  buf[threadIdx.x] = make_double2(x, c);
+  __syncthreads();
+  for (int o = 128; o > 0; o >>= 1) {
     if ((int)threadIdx.x < o) {
-      sums[threadIdx.x] += sums[threadIdx.x + o];
-      counts[threadIdx.x] += counts[threadIdx.x + o];
+      buf[threadIdx.x].x += buf[threadIdx.x + o].x;
+      buf[threadIdx.x].y += buf[threadIdx.x + o].y;
     }
     __syncthreads();
   }
   if (threadIdx.x == 0) {
-    const double c = mean ? (double)(counts[0] > 0 ? counts[0] : 1) : 1.0;
-    *count = (float)c;
-    *loss = (float)(sums[0] / c);
+    const double div = mean && buf[0].y > 0 ? buf[0].y : 1.0;
+    *scale = (float)(grad_scale / div);
+    *loss = (float)(buf[0].x / div);
   }
 }
 
-// out (+)= A B^T; the first piece overwrites, the last rounds to `type`.
-__global__ __launch_bounds__(BLOCK) void k_product(Operand A, Operand B, int64_t K, float* sum, int add, void* out,
-                                                   int type, int64_t ldo) {
-  __shared__ float a[KSTEP][TILE + 4], b[KSTEP][TILE + 4];
-  const int64_t m0 = (int64_t)blockIdx.y * TILE, n0 = (int64_t)blockIdx.x * TILE;
-  float acc[4][4];
-  tile_product(A, m0, B, n0, K, a, b, acc);
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+// --------------------------------------------------------------- gradients
+
+// out(m, n) = scale sum_k A(m, k) B(n, k), in `slices` shares of k.
+struct Product {
+  Panel A, B;
+  int64_t ny, nx, rows, cols;  // tiles, and what is there of the result
+  int steps, per, slices;      // of BK; steps of a slice
+  float* part; int64_t ldp;    // fp32 sums [slice][rows][ldp], or NULL:
+  int add;                     //   added to what is there
+  void* out; int64_t ldo;      // the result itself
+  int type;
+  int64_t blocks() const { return ny * nx * slices; }
+};
+
+struct Gradients {
+  Product dh, dw;
+  int64_t first_dw;  // workgroups before it make dH
+  int segs;
+  const float* scale;
+};
+
+template <class T_>
+__device__ __forceinline__ void product(const Product& p, int64_t b, int segs, const float* scale, char* lds) {
+  int64_t y, x;
+  place_tile(b, p.ny * p.slices, p.nx, 8, y, x);
+  const int slice = (int)(y / p.ny);
+  const int64_t m0 = (y - slice * p.ny) * GM, n0 = x * GN;
+  const int s0 = slice * p.per, s1 = s0 + p.per < p.steps ? s0 + p.per : p.steps;
+  f32x16 acc[T_::MT][T_::NT];
+  T_::run(p.A, m0, p.B, n0, s0, s1, segs, lds, acc);
+  const float k = p.part ? 1.f : *scale;
+  float* part = p.part ? p.part + slice * p.rows * p.ldp : nullptr;
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int j = 0; j < T_::NT; ++j) {
+    const int64_t n = n0 + T_::col(j);
+    if (n >= p.cols) continue;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int64_t m = m0 + ty * 4 + i, n = n0 + tx * 4 + j;
-      if (m >= A.rows || n >= B.rows) continue;
-      float x = acc[i][j];
-      if (add) x += sum[m * B.rows + n];
-      if (out) store1(out, type, m * ldo + n, x);
-      else sum[m * B.rows + n] = x;
-    }
+    for (int i = 0; i < T_::MT; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int64_t m = m0 + T_::row(i, r);
+        if (m >= p.rows) continue;
+        if (part) {
+          float* at = part + m * p.ldp + n;
+          *at = p.add ? *at + acc[i][j][r] : acc[i][j][r];
+        } else {
+          store1(p.out, p.type, m * p.ldo + n, acc[i][j][r] * k);
+        }
+      }
+  }
 }
 
-__global__ void k_zero(void* out, int type, int64_t rows, int64_t cols, int64_t ld) {
-  for (int64_t i = (int64_t)blockIdx.x * BLOCK + threadIdx.x; i < rows * cols; i += (int64_t)gridDim.x * BLOCK)
+template <bool F16>
+__global__ __launch_bounds__(TILE_BLOCK, 2) void k_gradients(Gradients g) {
+  using TH = Tile<GM, GN, 128, 64, false, true, F16>;
+  using TW = Tile<GM, GN, 128, 64, true, true, F16>;
+  __shared__ __attribute__((aligned(16))) char lds[TH::LDS];
+  if ((int64_t)blockIdx.x < g.first_dw) product<TH>(g.dh, blockIdx.x, g.segs, g.scale, lds);
+  else product<TW>(g.dw, blockIdx.x - g.first_dw, g.segs, g.scale, lds);
+}
+
+// out = scale times the sum of the slices.
+__global__ __launch_bounds__(256) void k_finish(const float* part, int slices, int64_t rows, int64_t cols, int64_t ldp,
+                                                const float* scale, void* out, int type, int64_t ldo) {
+  const int64_t per = (cols + 3) / 4, total = rows * per;
+  const float k = *scale;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / per, c = (i - r * per) * 4;
+    float x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int s = 0; s < slices; ++s) {
+      const float4 v = *reinterpret_cast<const float4*>(part + (s * rows + r) * ldp + c);
+      x[0] += v.x; x[1] += v.y; x[2] += v.z; x[3] += v.w;
+    }
+    for (int j = 0; j < 4; ++j)
+      if (c + j < cols) store1(out, type, r * ldo + c + j, x[j] * k);
+  }
+}
+
+__global__ __launch_bounds__(256) void k_zero(void* out, int type, int64_t rows, int64_t cols, int64_t ld) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * cols; i += (int64_t)gridDim.x * 256)
     store1(out, type, i / cols * ld + i % cols, 0.f);
 }
 
-int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
-unsigned tiles_of(int64_t n) { return (unsigned)((n + TILE - 1) / TILE); }
+// -------------------------------------------------------------------- host
 
+int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+unsigned grid_of(int64_t items, int64_t per) {
+  return (unsigned)std::max<int64_t>(1, std::min<int64_t>(16384, (items + per - 1) / per));
+}
+
+// Sizes and places in the workspace.
 struct Layout {
-  int64_t count, lse, target, rows, part, dh, dz, bytes, piece;
+  int64_t width, planes, segs;         // columns of the packed operands
+  int64_t piece, Tp;                   // table entries of a piece, rows of dz
+  int dh_steps, dh_per, dh_slices, dw_per, dw_slices;
+  int64_t scale, top, inv, rows, sums, part, h, w, dh, dw, dz, bytes;
 };
 
-Layout layout_of(int64_t T, int64_t D, int64_t V, bool grads) {
+void slices_of(int steps, int64_t ideal, int& per, int& slices) {
+  slices = (int)std::max<int64_t>(1, (steps + ideal / 2) / ideal);
+  per = std::max(1, (steps + slices - 1) / slices);
+  slices = std::max(1, (steps + per - 1) / per);
+}
+
+Layout layout_of(int64_t T, int64_t D, int64_t V, int type, bool grads) {
   Layout l{};
   int64_t at = 0;
   auto take = [&](int64_t n) {
@@ -208,72 +417,127 @@ Layout layout_of(int64_t T, int64_t D, int64_t V, bool grads) {
     at = up(at + n, 256);
     return here;
   };
-  l.count = take(4);
-  l.lse = take(4 * T);
-  l.target = take(4 * T);
+  l.width = up(D, BK);
+  l.planes = type == DT_F32 ? 3 : 1;
+  l.segs = type == DT_F32 ? 6 : 1;
+  l.Tp = up(T, TT);
+  l.scale = take(4);
+  l.top = take(4 * T);
+  l.inv = take(4 * T);
   l.rows = take(4 * T);
-  l.part = take(8 * T * tiles_of(V));
+  l.sums = take(16 * (up(T, ROWS) / ROWS));
+  l.part = take(8 * T * (up(V, TV) / TV));
+  l.h = take(2 * l.planes * T * l.width);
+  l.w = take(2 * l.planes * V * l.width);
   if (grads) {
-    l.piece = std::min(up(V, TILE), std::max<int64_t>(TILE, kPieceBytes / 4 / std::max<int64_t>(T, 1) / TILE * TILE));
-    l.dh = take(4 * T * D);
-    l.dz = take(4 * T * l.piece);
+    l.piece = std::min(up(V, TV), std::max<int64_t>(TV, kPieceBytes / (2 * l.planes * std::max<int64_t>(l.Tp, 1)) / TV * TV));
+    // shares of about equal length that fill two workgroups a CU
+    const int64_t nx = up(D, GN) / GN, th = up(T, GM) / GM * nx, tw = l.piece / GM * nx;
+    l.dh_steps = (int)(up(std::min(l.piece, V), BK) / BK);
+    const int dw_steps = (int)(up(T, BK) / BK);
+    const int64_t ideal = std::max<int64_t>(8, (th * l.dh_steps + tw * dw_steps) / 512);
+    slices_of(l.dh_steps, ideal, l.dh_per, l.dh_slices);
+    slices_of(dw_steps, ideal, l.dw_per, l.dw_slices);
+    if (l.dh_slices > 1 || l.piece < V) l.dh = take(4 * l.dh_slices * T * l.width);
+    if (l.dw_slices > 1) l.dw = take(4 * l.dw_slices * l.piece * l.width);
+    l.dz = take(2 * l.planes * l.Tp * l.piece);
   }
   l.bytes = at;
   return l;
 }
 
+// X as it lies, where the tiles can read it, else packed into ws.
+Panel panel_of(const Mat& X, const Layout& l, char* ws, hipStream_t s) {
+  if (l.planes == 1 && X.cols == l.width && X.ld % 8 == 0 && X.ld < (int64_t(1) << 22) &&
+      (reinterpret_cast<uintptr_t>(X.data) & 15) == 0)
+    return Panel{static_cast<const uint16_t*>(X.data), 0, X.ld, X.rows, X.cols};
+  uint16_t* to = reinterpret_cast<uint16_t*>(ws);
+  const int64_t plane = X.rows * l.width;
+  k_pack<<<grid_of(X.rows * (l.width / 4), 1024), 256, 0, s>>>(X, to, plane, l.width, (int)l.planes);
+  return Panel{to, plane, l.width, X.rows, l.width};
+}
+
 }  // namespace
 
-int64_t linear_xent_workspace(int64_t T, int64_t D, int64_t V, int, bool grads) {
-  return layout_of(T, D, V, grads).bytes;
+int64_t linear_xent_workspace(int64_t T, int64_t D, int64_t V, int type, bool grads) {
+  return layout_of(T, D, V, type, grads).bytes;
 }
 
 hipError_t linear_xent(const XentArgs& x, hipStream_t s) {
   const int64_t T = x.H.rows, D = x.H.cols, V = x.W.rows;
-  const bool grads = x.dH.data || x.dW.data;
-  const Layout l = layout_of(T, D, V, grads);
+  const bool grads = x.dW.data != nullptr || x.dH.data != nullptr;
+  const int type = x.H.type;
+  const bool f16 = type == DT_F16;
+  const Layout l = layout_of(T, D, V, type, grads);
   char* ws = static_cast<char*>(x.ws);
-  float* count = (float*)(ws + l.count);
-  float* row_loss = x.row_loss ? x.row_loss : (float*)(ws + l.rows);
-  if (T > 0) {
-    Scores sc{};
-    sc.H = Operand{x.H.data, x.H.type, T, x.H.ld, 1};
-    sc.W = Operand{x.W.data, x.W.type, V, x.W.ld, 1};
-    sc.D = D;
-    sc.labels = x.labels; sc.i64 = x.labels_i64;
-    sc.part = (float2*)(ws + l.part);
-    sc.target = (float*)(ws + l.target);
-    sc.v0 = 0; sc.v1 = V;
-    k_scores<false><<<dim3(tiles_of(V), tiles_of(T)), BLOCK, 0, s>>>(sc);
-    float* lse = (float*)(ws + l.lse);
-    k_rows<<<(unsigned)((T + BLOCK - 1) / BLOCK), BLOCK, 0, s>>>(sc, tiles_of(V), lse, row_loss);
-    sc.lse = lse;
-    sc.count = count;
-    sc.grad_scale = x.grad_scale;
-    k_loss<<<1, 1024, 0, s>>>(x.labels, x.labels_i64, T, V, x.mean, row_loss, count, x.loss);
-    if (grads) {
-      sc.dz = (float*)(ws + l.dz);
-      float* dh = (float*)(ws + l.dh);
-      for (int64_t v0 = 0; v0 < V; v0 += l.piece) {
-        const int64_t n = std::min(l.piece, V - v0);
-        sc.v0 = v0; sc.v1 = v0 + n; sc.ldz = n;
-        k_scores<true><<<dim3(tiles_of(n), tiles_of(T)), BLOCK, 0, s>>>(sc);
-        const int size = dtype_bytes(x.W.type);
-        const bool last = v0 + n == V;
-        k_product<<<dim3(tiles_of(D), tiles_of(T)), BLOCK, 0, s>>>(
-            Operand{sc.dz, DT_F32, T, n, 1},
-            Operand{(const char*)x.W.data + v0 * x.W.ld * size, x.W.type, D, 1, x.W.ld}, n, dh, v0 > 0,
-            last ? x.dH.data : nullptr, x.dH.type, x.dH.ld);
-        k_product<<<dim3(tiles_of(D), tiles_of(n)), BLOCK, 0, s>>>(
-            Operand{sc.dz, DT_F32, n, 1, n}, Operand{x.H.data, x.H.type, D, 1, x.H.ld}, T, nullptr, 0,
-            (char*)x.dW.data + v0 * x.dW.ld * size, x.dW.type, x.dW.ld);
-      }
-    }
-  } else {
-    k_loss<<<1, 1024, 0, s>>>(nullptr, 0, 0, V, x.mean, nullptr, count, x.loss);
-    if (grads && V > 0 && D > 0)
-      k_zero<<<(unsigned)std::min<int64_t>(4096, (V * D + BLOCK - 1) / BLOCK), BLOCK, 0, s>>>(x.dW.data, x.dW.type, V, D, x.dW.ld);
+  float* scale = (float*)(ws + l.scale);
+  double2* sums = (double2*)(ws + l.sums);
+  if (T == 0) {
+    k_loss<<<1, 256, 0, s>>>(sums, 0, x.mean, x.grad_scale, scale, x.loss);
+    if (grads && V > 0 && D > 0) k_zero<<<grid_of(V * D, 1024), 256, 0, s>>>(x.dW.data, type, V, D, x.dW.ld);
+    return hipGetLastError();
   }
+  Scores sc{};
+  sc.H = panel_of(x.H, l, ws + l.h, s);
+  sc.W = panel_of(x.W, l, ws + l.w, s);
+  sc.T = T; sc.V = V; sc.v0 = 0; sc.v1 = V;
+  sc.steps = (int)(l.width / BK);
+  sc.segs = (int)l.segs;
+  sc.part = (float2*)(ws + l.part);
+  sc.labels = x.labels; sc.i64 = x.labels_i64;
+  auto scores = [&](bool grad) {
+    const unsigned grid = (unsigned)(up(sc.v1 - sc.v0, TV) / TV * (l.Tp / TT));
+    if (type == DT_F32) grad ? k_scores<true, DT_F32><<<grid, TILE_BLOCK, 0, s>>>(sc) : k_scores<false, DT_F32><<<grid, TILE_BLOCK, 0, s>>>(sc);
+    else if (type == DT_BF16) grad ? k_scores<true, DT_BF16><<<grid, TILE_BLOCK, 0, s>>>(sc) : k_scores<false, DT_BF16><<<grid, TILE_BLOCK, 0, s>>>(sc);
+    else grad ? k_scores<true, DT_F16><<<grid, TILE_BLOCK, 0, s>>>(sc) : k_scores<false, DT_F16><<<grid, TILE_BLOCK, 0, s>>>(sc);
+  };
+  scores(false);
+  Rows rw{};
+  rw.H = x.H; rw.W = x.W; rw.labels = x.labels; rw.i64 = x.labels_i64;
+  rw.part = sc.part; rw.tiles = up(V, TV) / TV;
+  rw.top = (float*)(ws + l.top); rw.inv = (float*)(ws + l.inv);
+  rw.row_loss = x.row_loss ? x.row_loss : (float*)(ws + l.rows);
+  rw.sums = sums;
+  const int64_t blocks = up(T, ROWS) / ROWS;
+  k_rows<<<(unsigned)blocks, ROWS * SLICES, 0, s>>>(rw);
+  // fp16 dz is held times F16_UP
+  k_loss<<<1, 256, 0, s>>>(sums, blocks, x.mean, x.grad_scale * (f16 ? 1.f / F16_UP : 1.f), scale, x.loss);
+  if (!grads) return hipGetLastError();
+  sc.top = rw.top; sc.inv = rw.inv;
+  sc.dz = (uint16_t*)(ws + l.dz);
+  sc.ldz = l.piece;
+  sc.plane = l.Tp * l.piece;
+  const Panel dz{sc.dz, sc.plane, l.piece, l.Tp, l.piece};
+  const int64_t nx = up(D, GN) / GN;
+  const int size = dtype_bytes(type);
+  for (int64_t v0 = 0; v0 < V; v0 += l.piece) {
+    const int64_t n = std::min(l.piece, V - v0);
+    sc.v0 = v0; sc.v1 = v0 + n;
+    scores(true);
+    Gradients g{};
+    g.segs = (int)l.segs;
+    g.scale = scale;
+    Panel w = sc.W;
+    w.data += v0 * w.ld;
+    w.rows = n;
+    g.dh = Product{dz, w, up(T, GM) / GM, nx, T, D, (int)(up(n, BK) / BK), l.dh_per, 0,
+                   l.dh ? (float*)(ws + l.dh) : nullptr, l.width, v0 > 0, x.dH.data, x.dH.ld, type};
+    g.dh.slices = (g.dh.steps + l.dh_per - 1) / l.dh_per;
+    Mat out = x.dW;
+    out.data = (char*)x.dW.data + v0 * x.dW.ld * size;
+    g.dw = Product{dz, sc.H, up(n, GM) / GM, nx, n, D, (int)(up(T, BK) / BK), l.dw_per, l.dw_slices,
+                   l.dw ? (float*)(ws + l.dw) : nullptr, l.width, 0, out.data, out.ld, type};
+    g.first_dw = g.dh.blocks();
+    const unsigned grid = (unsigned)(g.first_dw + g.dw.blocks());
+    if (f16) k_gradients<true><<<grid, TILE_BLOCK, 0, s>>>(g);
+    else k_gradients<false><<<grid, TILE_BLOCK, 0, s>>>(g);
+    if (l.dw)
+      k_finish<<<grid_of(n * ((D + 3) / 4), 256), 256, 0, s>>>((float*)(ws + l.dw), l.dw_slices, n, D, l.width, scale,
+                                                               out.data, type, out.ld);
+  }
+  if (l.dh)
+    k_finish<<<grid_of(T * ((D + 3) / 4), 256), 256, 0, s>>>((float*)(ws + l.dh), l.dh_slices, T, D, l.width, scale,
+                                                             x.dH.data, type, x.dH.ld);
   return hipGetLastError();
 }
 
