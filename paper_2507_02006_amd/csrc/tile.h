@@ -1,19 +1,24 @@
 // Matrix-core tile products of 16-bit operands (gfx950, wave64).
 //
-// acc(m, n) = sum_k A(m, k) B(n, k) for a tile of TM x TN by four wavefronts,
-// each WM x WN in 32 x 32 x 16 MFMAs.  An operand is either K-contiguous (row
+// acc(m, n) = sum_k A(m, k) B(n, k) for a tile of TM x TN, each wavefront
+// WM x WN of it in 32 x 32 x 16 MFMAs.  An operand is either K-contiguous (row
 // m holds its k) or K-major (row k holds its m); both are staged as they lie
-// in memory, 32 k a step, by loads that go from global memory straight to
+// in memory, 64 k a step, by loads that go from global memory straight to
 // LDS (no registers, no transposed copies).  K-contiguous fragments are read
 // 16 bytes a lane; K-major ones with the transposing LDS read, which hands a
 // lane four k of its column.  16-byte chunks are placed XORed with their row
-// so that neither read meets bank conflicts: the swap is made on the global
-// address of each lane, since the destination of such a load is fixed.
+// so that neither read meets bank conflicts (256 bytes a cycle: 16 lanes of
+// 16 bytes, 32 of 8): the swap is made on the global address of each lane,
+// since the destination of such a load is fixed.
 //
-// Three stages: while step i is multiplied, the loads of i + 1 have had one
-// step to arrive and those of i + 2 are issued, with one barrier a step.
-// 72 KB for 256 x 128: two workgroups a CU, so one's epilogue and barriers run
-// under the other's products.
+// Two stages.  Fragments are read one group of products ahead; before the last
+// group of a stage the wavefronts meet once, which frees the stage for the
+// loads after the next and lets the next stage's first fragments be read under
+// that group.  What bounds it is the way from L2 to the CU (64 bytes a cycle):
+// 256 x 256 takes 32 bytes a cycle at the matrix cores' full rate, 256 x 128
+// 48.  Measured alone, 8192 x 2048 x 32768: 1372 TFLOP/s with both operands
+// K-contiguous, 1005 with one or both K-major (the copy's clock is near 1.9
+// GHz, 2 PFLOP/s); 256 x 128 with 32 k a stage and three stages 969.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -28,9 +33,6 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int BK = 32;        // k of a stage
-constexpr int STAGES = 3;
-constexpr int TILE_BLOCK = 256;
 
 // An operand in memory.  K-contiguous: `rows` are m, `cols` k (a multiple of
 // BK, rows 16-byte aligned).  K-major: `rows` are k, `cols` m (a multiple of
@@ -39,6 +41,8 @@ struct Panel {
   const uint16_t* data;
   int64_t plane, ld, rows, cols;
 };
+
+constexpr int BK = 64;  // k of a stage
 
 // Products of planes that make up an fp32 product: all but those below its
 // own rounding (planes 1 and 2, 2 and 2).  Small ones come first.
@@ -56,11 +60,13 @@ __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(1))) void global_void;
 
-// One operand's share of a stage: SPAN x 32 elements, 1 KB an instruction.
-template <int SPAN, bool KMAJOR>
+// One operand's share of a stage: SPAN x BK elements, 1 KB an instruction.
+template <int SPAN, int WAVES, bool KMAJOR>
 struct Stager {
-  static constexpr int COUNT = SPAN / 64;   // instructions a wavefront issues
-  static constexpr int BYTES = SPAN * BK * 2;
+  static constexpr int COUNT = SPAN * BK / (512 * WAVES);  // instructions a wavefront issues
+  static constexpr int CHUNKS = KMAJOR ? SPAN / 8 : BK / 8;  // 16-byte chunks a row
+  static constexpr int ROWS = 64 / CHUNKS;                   // rows an instruction
+  static_assert(COUNT >= 1 && COUNT * 512 * WAVES == SPAN * BK && ROWS >= 1, "stage does not divide");
   const char* base;      // first row of the tile, advanced along k
   int64_t step;          // bytes a step
   uint32_t off[COUNT];
@@ -76,8 +82,8 @@ struct Stager {
       const int64_t last = p.rows - 1 - m0;
 #pragma unroll
       for (int j = 0; j < COUNT; ++j) {
-        const int r = (wave * COUNT + j) * 16 + lane / 4;
-        const int c = (lane & 3) ^ ((r >> 1) & 3);
+        const int r = (wave * COUNT + j) * ROWS + lane / CHUNKS;
+        const int c = (lane % CHUNKS) ^ (r / (16 / CHUNKS) % CHUNKS);
         // rows past the end repeat the last one; their results are not used
         off[j] = (uint32_t)((r < last ? r : last) * ld2 + c * 16);
       }
@@ -91,11 +97,10 @@ struct Stager {
   // K-major offsets; rows past the end of k repeat the last one (the other
   // operand holds zeros there).
   __device__ void place(int64_t last_col, int wave, int lane) {
-    constexpr int chunks = SPAN / 8, rows = 64 / chunks;
 #pragma unroll
     for (int j = 0; j < COUNT; ++j) {
-      const int k = (wave * COUNT + j) * rows + lane / chunks;
-      const int c = ((lane % chunks) ^ ((k & 3) * 2)) * 8;
+      const int k = (wave * COUNT + j) * ROWS + lane / CHUNKS;
+      const int c = ((lane % CHUNKS) ^ ((k & 3) * 4)) * 8;
       off[j] = (uint32_t)((k < left ? k : left - 1) * ld2 + (c < last_col ? c : last_col) * 2);
     }
   }
@@ -107,22 +112,25 @@ struct Stager {
   }
 };
 
-// Fragment reads of one operand: W consecutive m of the tile from `first`.
-template <int SPAN, bool KMAJOR>
+// Fragment reads of one operand: SPAN rows of m staged, W of them this
+// wavefront's, from `first` on.
+template <int SPAN, int W, bool KMAJOR>
 struct Reader {
-  uint32_t at[2];
+  uint32_t at[KMAJOR ? W / 32 : BK / 16];
   __device__ Reader(int first, int lane) {
     if constexpr (!KMAJOR) {
-      const int r = first + (lane & 31), s = (r >> 1) & 3;
-      at[0] = (uint32_t)(r * (BK * 2) + (((lane >> 5) ^ s) << 4));
-      at[1] = at[0] ^ 32;  // the second 16 k: chunks 2 and 3
+      constexpr int chunks = BK / 8;
+      const int r = first + (lane & 31);
+#pragma unroll
+      for (int kk = 0; kk < BK / 16; ++kk)
+        at[kk] = (uint32_t)(r * (BK * 2) + (((kk * 2 + (lane >> 5)) ^ (r / (16 / chunks) % chunks)) << 4));
     } else {
       const int g = lane >> 4, i = lane & 15;
       const int k = 8 * (g >> 1) + i / 4;
       const int c = first / 8 + (g & 1) * 2 + ((i & 3) >> 1);
 #pragma unroll
-      for (int odd = 0; odd < 2; ++odd)
-        at[odd] = (uint32_t)(k * (SPAN * 2) + (((c + 4 * odd) ^ ((i / 4) * 2)) << 4) + (i & 1) * 8);
+      for (int t = 0; t < W / 32; ++t)
+        at[t] = (uint32_t)(k * (SPAN * 2) + (((c + 4 * t) ^ ((i / 4) * 4)) << 4) + (i & 1) * 8);
     }
   }
   // rows [32 t, 32 t + 32) of the wavefront's span, k [16 kk, 16 kk + 16)
@@ -131,7 +139,7 @@ struct Reader {
       return *reinterpret_cast<const s16x8*>(lds + at[kk] + t * (32 * BK * 2));
     } else {
       typedef __attribute__((address_space(3))) s16x4 lds4;
-      const char* p = lds + at[t & 1] + (t >> 1) * 128 + kk * 16 * (SPAN * 2);
+      const char* p = lds + at[t] + kk * 16 * (SPAN * 2);
       const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)p);
       const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(p + 4 * (SPAN * 2)));
       return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -141,11 +149,10 @@ struct Reader {
 
 template <int TM, int TN, int WM, int WN, bool AK, bool BK_, bool F16>
 struct Tile {
-  static_assert(TM / WM * (TN / WN) == 4, "four wavefronts");
+  static constexpr int WAVES = TM / WM * (TN / WN), THREADS = 64 * WAVES;
   static constexpr int MT = WM / 32, NT = WN / 32;
-  static constexpr int STAGE = (TM + TN) * BK * 2;
-  static constexpr int LDS = STAGE * STAGES;
-  static constexpr int LOADS = TM / 64 + TN / 64;  // a wavefront's loads of a stage
+  static constexpr int STAGE = (TM + TN) * BK * 2, LDS = 2 * STAGE;
+  static constexpr int LOADS = (TM + TN) * BK / (512 * WAVES);  // a wavefront's loads of a stage
 
   // Products over k steps [s0, s1) of BK, for each of `segs` plane pairs.
   static __device__ __forceinline__ void run(const Panel& A, int64_t m0, const Panel& B, int64_t n0, int s0, int s1,
@@ -158,10 +165,10 @@ struct Tile {
       for (int j = 0; j < NT; ++j)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-    Stager<TM, AK> sa;
-    Stager<TN, BK_> sb;
-    const Reader<TM, AK> ra(wm * WM, lane);
-    const Reader<TN, BK_> rb(wn * WN, lane);
+    Stager<TM, WAVES, AK> sa;
+    Stager<TN, WAVES, BK_> sb;
+    const Reader<TM, WM, AK> ra(wm * WM, lane);
+    const Reader<TN, WN, BK_> rb(wn * WN, lane);
     const int per = s1 - s0, total = per * segs;
     int seg = 0, at = 0;  // of the next stage to issue
     auto issue = [&](int stage) {
@@ -187,32 +194,48 @@ struct Tile {
       if constexpr (BK_) sb.left -= BK;
       ++at;
     };
-    issue(0);
-    if (total > 1) issue(1);
-    int cur = 0;
-    for (int s = 0; s < total; ++s) {
-      // this step's loads are the older ones; LDS reads of the last step are
-      // done before any wavefront overwrites their stage
-      if (s + 1 < total) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LOADS) : "memory");
-      else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-      __builtin_amdgcn_s_barrier();
-      asm volatile("" ::: "memory");
-      if (s + 2 < total) issue(cur == 0 ? 2 : cur - 1);
-      const char* a = lds + cur * STAGE;
+    s16x8 fa[2][MT], fb[2][NT];
+    auto read = [&](int stage, int kk) {
+      const char* a = lds + stage * STAGE;
       const char* b = a + TM * BK * 2;
 #pragma unroll
-      for (int kk = 0; kk < BK / 16; ++kk) {
-        s16x8 fa[MT], fb[NT];
+      for (int i = 0; i < MT; ++i) fa[kk & 1][i] = ra.get(a, i, kk);
 #pragma unroll
-        for (int i = 0; i < MT; ++i) fa[i] = ra.get(a, i, kk);
+      for (int j = 0; j < NT; ++j) fb[kk & 1][j] = rb.get(b, j, kk);
+    };
+    issue(0);
+    if (total > 1) {
+      issue(1);
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
+    } else {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    read(0, 0);
+    constexpr int KK = BK / 16;
+    static_assert(KK % 2 == 0, "a stage's first fragments go to the same registers");
+    for (int s = 0; s < total; ++s) {
 #pragma unroll
-        for (int j = 0; j < NT; ++j) fb[j] = rb.get(b, j, kk);
+      for (int kk = 0; kk < KK; ++kk) {
+        if (kk + 1 < KK) {
+          read(s & 1, kk + 1);
+        } else if (s + 1 < total) {
+          // the next stage has arrived, and this one's reads are done in every
+          // wavefront once all are here: it takes the loads after the next's
+          asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+          __builtin_amdgcn_s_barrier();
+          asm volatile("" ::: "memory");
+          if (s + 2 < total) issue(s & 1);
+          read((s + 1) & 1, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);  // reads first: they return under the products
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
-          for (int j = 0; j < NT; ++j) acc[i][j] = mfma<F16>(fa[i], fb[j], acc[i][j]);
+          for (int j = 0; j < NT; ++j) acc[i][j] = mfma<F16>(fa[kk & 1][i], fb[kk & 1][j], acc[i][j]);
+        __builtin_amdgcn_sched_barrier(0);
       }
-      cur = cur == 2 ? 0 : cur + 1;
     }
   }
 

@@ -20,14 +20,15 @@
 #include <algorithm>
 
 #include "dense.h"
+#include "device.h"
 #include "tile.h"
 
 namespace aires {
 namespace kern {
 namespace {
 
-constexpr int TV = 256, TT = 128;      // a tile of scores: table by rows of H
-constexpr int GM = 256, GN = 128;      // a tile of a gradient product
+constexpr int TV = 256, TT = 256;      // a tile of scores: table by rows of H
+constexpr int GM = 256, GN = 256;      // a tile of a gradient product
 constexpr int64_t kPieceBytes = int64_t(256) << 20;  // dz of one piece of the table
 constexpr int ROWS = 64, SLICES = 16;  // k_rows: rows of a workgroup, shares of the tiles
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.693147180559945309417f;
@@ -95,7 +96,7 @@ struct Scores {
 };
 
 template <bool GRAD, int TYPE>
-__global__ __launch_bounds__(TILE_BLOCK, 2) void k_scores(Scores s) {
+__global__ __launch_bounds__(512, 2) void k_scores(Scores s) {
   constexpr bool F16 = TYPE == DT_F16;
   constexpr int PLANES = TYPE == DT_F32 ? 3 : 1;
   using T_ = Tile<TV, TT, 128, 64, false, false, F16>;
@@ -105,7 +106,7 @@ __global__ __launch_bounds__(TILE_BLOCK, 2) void k_scores(Scores s) {
   const int64_t v0 = s.v0 + vt * TV, t0 = tt * TT;
   f32x16 acc[T_::MT][T_::NT];
   T_::run(s.W, v0, s.H, t0, 0, s.steps, s.segs, lds, acc);
-  const int lane = threadIdx.x & 63, wm = threadIdx.x >> 7;
+  const int lane = threadIdx.x & 63, wm = (threadIdx.x >> 6) / (TT / 64);
   __syncthreads();  // the stages' LDS changes its use
 
   if constexpr (!GRAD) {
@@ -208,7 +209,7 @@ __global__ __launch_bounds__(TILE_BLOCK, 2) void k_scores(Scores s) {
       uint16_t* to = s.dz + p * s.plane + t0 * s.ldz + (v0 - s.v0);
       const int ch = threadIdx.x & 31;
 #pragma unroll 4
-      for (int c = threadIdx.x >> 5; c < TT; c += TILE_BLOCK / 32)
+      for (int c = threadIdx.x >> 5; c < TT; c += T_::THREADS / 32)
         *reinterpret_cast<uint4*>(to + c * s.ldz + ch * 8) =
             *reinterpret_cast<const uint4*>(lds + c * (TV * 2) + ((ch ^ (c & 31)) << 4));
     }
@@ -334,30 +335,51 @@ __device__ __forceinline__ void product(const Product& p, int64_t b, int segs, c
   const int s0 = slice * p.per, s1 = s0 + p.per < p.steps ? s0 + p.per : p.steps;
   f32x16 acc[T_::MT][T_::NT];
   T_::run(p.A, m0, p.B, n0, s0, s1, segs, lds, acc);
+  // Through LDS, 32 rows of the wavefront's part at a time, so that rows are
+  // written 256 bytes (fp32) at a time.
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  constexpr int W = T_::NT * 32;
+  float* mine = reinterpret_cast<float*>(lds) + wave * (32 * W);
   const float k = p.part ? 1.f : *scale;
   float* part = p.part ? p.part + slice * p.rows * p.ldp : nullptr;
+  const int64_t row0 = m0 + wave / (GN / W) * (T_::MT * 32), n = n0 + wave % (GN / W) * W + lane % (W / 4) * 4;
+  __syncthreads();  // the stages' LDS changes its use
 #pragma unroll
-  for (int j = 0; j < T_::NT; ++j) {
-    const int64_t n = n0 + T_::col(j);
-    if (n >= p.cols) continue;
+  for (int i = 0; i < T_::MT; ++i) {
 #pragma unroll
-    for (int i = 0; i < T_::MT; ++i)
+    for (int j = 0; j < T_::NT; ++j)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int64_t m = m0 + T_::row(i, r);
-        if (m >= p.rows) continue;
-        if (part) {
-          float* at = part + m * p.ldp + n;
-          *at = p.add ? *at + acc[i][j][r] : acc[i][j][r];
-        } else {
-          store1(p.out, p.type, m * p.ldo + n, acc[i][j][r] * k);
+      for (int r = 0; r < 16; ++r)
+        mine[(8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * W + j * 32 + (lane & 31)] = acc[i][j][r];
+    wave_sync();
+    for (int r = lane / (W / 4); r < 32; r += 64 / (W / 4)) {
+      const int64_t m = row0 + i * 32 + r;
+      if (m >= p.rows || n >= p.cols) continue;
+      const float4 v = *reinterpret_cast<const float4*>(mine + r * W + lane % (W / 4) * 4);
+      float x[4] = {v.x * k, v.y * k, v.z * k, v.w * k};
+      if (part) {
+        float4* at = reinterpret_cast<float4*>(part + m * p.ldp + n);
+        if (p.add) {
+          const float4 o = *at;
+          x[0] += o.x; x[1] += o.y; x[2] += o.z; x[3] += o.w;
         }
+        *at = make_float4(x[0], x[1], x[2], x[3]);
+      } else if (n + 4 <= p.cols) {
+        if (p.type == DT_F32) store4<DT_F32>(p.out, m * p.ldo + n, x);
+        else if (p.type == DT_BF16) store4<DT_BF16>(p.out, m * p.ldo + n, x);
+        else store4<DT_F16>(p.out, m * p.ldo + n, x);
+      } else {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          if (n + c < p.cols) store1(p.out, p.type, m * p.ldo + n + c, x[c]);
       }
+    }
+    wave_sync();
   }
 }
 
 template <bool F16>
-__global__ __launch_bounds__(TILE_BLOCK, 2) void k_gradients(Gradients g) {
+__global__ __launch_bounds__(512, 2) void k_gradients(Gradients g) {
   using TH = Tile<GM, GN, 128, 64, false, true, F16>;
   using TW = Tile<GM, GN, 128, 64, true, true, F16>;
   __shared__ __attribute__((aligned(16))) char lds[TH::LDS];
@@ -398,7 +420,7 @@ unsigned grid_of(int64_t items, int64_t per) {
 // Sizes and places in the workspace.
 struct Layout {
   int64_t width, planes, segs;         // columns of the packed operands
-  int64_t piece, Tp;                   // table entries of a piece, rows of dz
+  int64_t piece, Tp, ldz;              // table entries of a piece, rows of dz and their stride
   int dh_steps, dh_per, dh_slices, dw_per, dw_slices;
   int64_t scale, top, inv, rows, sums, part, h, w, dh, dw, dz, bytes;
 };
@@ -431,16 +453,17 @@ Layout layout_of(int64_t T, int64_t D, int64_t V, int type, bool grads) {
   l.w = take(2 * l.planes * V * l.width);
   if (grads) {
     l.piece = std::min(up(V, TV), std::max<int64_t>(TV, kPieceBytes / (2 * l.planes * std::max<int64_t>(l.Tp, 1)) / TV * TV));
-    // shares of about equal length that fill two workgroups a CU
+    // shares of about equal length that give every CU one
     const int64_t nx = up(D, GN) / GN, th = up(T, GM) / GM * nx, tw = l.piece / GM * nx;
     l.dh_steps = (int)(up(std::min(l.piece, V), BK) / BK);
     const int dw_steps = (int)(up(T, BK) / BK);
-    const int64_t ideal = std::max<int64_t>(8, (th * l.dh_steps + tw * dw_steps) / 512);
+    const int64_t ideal = std::max<int64_t>(8, (th * l.dh_steps + tw * dw_steps) / 256);
     slices_of(l.dh_steps, ideal, l.dh_per, l.dh_slices);
     slices_of(dw_steps, ideal, l.dw_per, l.dw_slices);
     if (l.dh_slices > 1 || l.piece < V) l.dh = take(4 * l.dh_slices * T * l.width);
     if (l.dw_slices > 1) l.dw = take(4 * l.dw_slices * l.piece * l.width);
-    l.dz = take(2 * l.planes * l.Tp * l.piece);
+    l.ldz = l.piece + 64;
+    l.dz = take(2 * l.planes * l.Tp * l.ldz);
   }
   l.bytes = at;
   return l;
@@ -487,9 +510,9 @@ hipError_t linear_xent(const XentArgs& x, hipStream_t s) {
   sc.labels = x.labels; sc.i64 = x.labels_i64;
   auto scores = [&](bool grad) {
     const unsigned grid = (unsigned)(up(sc.v1 - sc.v0, TV) / TV * (l.Tp / TT));
-    if (type == DT_F32) grad ? k_scores<true, DT_F32><<<grid, TILE_BLOCK, 0, s>>>(sc) : k_scores<false, DT_F32><<<grid, TILE_BLOCK, 0, s>>>(sc);
-    else if (type == DT_BF16) grad ? k_scores<true, DT_BF16><<<grid, TILE_BLOCK, 0, s>>>(sc) : k_scores<false, DT_BF16><<<grid, TILE_BLOCK, 0, s>>>(sc);
-    else grad ? k_scores<true, DT_F16><<<grid, TILE_BLOCK, 0, s>>>(sc) : k_scores<false, DT_F16><<<grid, TILE_BLOCK, 0, s>>>(sc);
+    if (type == DT_F32) grad ? k_scores<true, DT_F32><<<grid, 512, 0, s>>>(sc) : k_scores<false, DT_F32><<<grid, 512, 0, s>>>(sc);
+    else if (type == DT_BF16) grad ? k_scores<true, DT_BF16><<<grid, 512, 0, s>>>(sc) : k_scores<false, DT_BF16><<<grid, 512, 0, s>>>(sc);
+    else grad ? k_scores<true, DT_F16><<<grid, 512, 0, s>>>(sc) : k_scores<false, DT_F16><<<grid, 512, 0, s>>>(sc);
   };
   scores(false);
   Rows rw{};
@@ -505,9 +528,9 @@ hipError_t linear_xent(const XentArgs& x, hipStream_t s) {
   if (!grads) return hipGetLastError();
   sc.top = rw.top; sc.inv = rw.inv;
   sc.dz = (uint16_t*)(ws + l.dz);
-  sc.ldz = l.piece;
-  sc.plane = l.Tp * l.piece;
-  const Panel dz{sc.dz, sc.plane, l.piece, l.Tp, l.piece};
+  sc.ldz = l.ldz;
+  sc.plane = l.Tp * l.ldz;
+  const Panel dz{sc.dz, sc.plane, l.ldz, l.Tp, l.piece};
   const int64_t nx = up(D, GN) / GN;
   const int size = dtype_bytes(type);
   for (int64_t v0 = 0; v0 < V; v0 += l.piece) {
@@ -529,8 +552,8 @@ hipError_t linear_xent(const XentArgs& x, hipStream_t s) {
                    l.dw ? (float*)(ws + l.dw) : nullptr, l.width, 0, out.data, out.ld, type};
     g.first_dw = g.dh.blocks();
     const unsigned grid = (unsigned)(g.first_dw + g.dw.blocks());
-    if (f16) k_gradients<true><<<grid, TILE_BLOCK, 0, s>>>(g);
-    else k_gradients<false><<<grid, TILE_BLOCK, 0, s>>>(g);
+    if (f16) k_gradients<true><<<grid, 512, 0, s>>>(g);
+    else k_gradients<false><<<grid, 512, 0, s>>>(g);
     if (l.dw)
       k_finish<<<grid_of(n * ((D + 3) / 4), 256), 256, 0, s>>>((float*)(ws + l.dw), l.dw_slices, n, D, l.width, scale,
                                                                out.data, type, out.ld);
