@@ -104,11 +104,18 @@ struct Stager {
       off[j] = (uint32_t)((k < left ? k : left - 1) * ld2 + (c < last_col ? c : last_col) * 2);
     }
   }
-  __device__ void issue(char* lds, int wave) const {
+  __device__ __forceinline__ void issue(char* lds, int wave) const {
+    // a scalar base and a 32-bit offset a lane: no vector arithmetic a load
+    const uint64_t b = reinterpret_cast<uint64_t>(base);
+    const char* from = reinterpret_cast<const char*>(
+        ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(b >> 32)) << 32) |
+        (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)b));
 #pragma unroll
-    for (int j = 0; j < COUNT; ++j)
-      __builtin_amdgcn_global_load_lds((global_void*)(base + off[j]), (lds_void*)(lds + (wave * COUNT + j) * 1024), 16,
-                                       0, 0);
+    for (int j = 0; j < COUNT; ++j) {
+      uint32_t o = off[j];
+      asm("" : "+v"(o));
+      __builtin_amdgcn_global_load_lds((global_void*)(from + o), (lds_void*)(lds + (wave * COUNT + j) * 1024), 16, 0, 0);
+    }
   }
 };
 
@@ -226,10 +233,10 @@ struct Tile {
           asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
           __builtin_amdgcn_s_barrier();
           asm volatile("" ::: "memory");
-          if (s + 2 < total) issue(s & 1);
           read((s + 1) & 1, 0);
         }
         __builtin_amdgcn_sched_barrier(0);  // reads first: they return under the products
+        if (kk + 1 == KK && s + 2 < total) issue(s & 1);
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
