@@ -168,7 +168,7 @@ def load() -> ctypes.CDLL:
         "aires_linear_xent_workspace": (ctypes.c_int, [c_i64, c_i64, c_i64, c_i32, c_i32, P(c_i64)]),
         "aires_linear_xent": (ctypes.c_int, [P(Dense), P(Dense), c_vp, c_i32, c_i32, c_dbl, c_vp, c_vp, P(Dense),
                                              P(Dense), c_vp, c_i64, c_vp]),
-        "aires_adamw": (ctypes.c_int, [P(AdamWTensor), c_i64, P(AdamWOpts), c_vp]),
+        "aires_adamw": (ctypes.c_int, [c_vp, c_i64, P(AdamWOpts), c_vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)

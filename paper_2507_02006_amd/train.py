@@ -18,15 +18,25 @@ from typing import Any
 from . import _binding as B_
 
 _DTYPES: dict = {}
+_torch = None
+
+
+def _load_torch():
+    """torch, imported with the first call (the package itself does not)."""
+    global _torch
+    import torch
+    _torch = torch
+    return torch
 
 
 def _dtype(t) -> int:
-    if not _DTYPES:
-        import torch
-        _DTYPES.update({torch.float32: B_.DTYPE_F32, torch.bfloat16: B_.DTYPE_BF16, torch.float16: B_.DTYPE_F16})
     d = _DTYPES.get(t)
     if d is None:
-        raise TypeError("expected float32, bfloat16 or float16, got %s" % (t,))
+        torch = _torch or _load_torch()
+        _DTYPES.update({torch.float32: B_.DTYPE_F32, torch.bfloat16: B_.DTYPE_BF16, torch.float16: B_.DTYPE_F16})
+        d = _DTYPES.get(t)
+        if d is None:
+            raise TypeError("expected float32, bfloat16 or float16, got %s" % (t,))
     return d
 
 
@@ -34,15 +44,18 @@ def _dense(x, name: str) -> B_.Dense:
     if x.dim() != 2 or not x.is_cuda:
         raise ValueError("%s must be a device matrix" % name)
     m, n = x.shape
-    ld = x.stride(0) if m > 1 else n
-    if (n > 1 and x.stride(1) != 1) or (m > 1 and ld < n):
-        raise ValueError("%s needs unit column stride and rows that do not overlap" % name)
+    ld = n
+    if not x.is_contiguous():
+        if m > 1:
+            ld = x.stride(0)
+        if (n > 1 and x.stride(1) != 1) or (m > 1 and ld < n):
+            raise ValueError("%s needs unit column stride and rows that do not overlap" % name)
     return B_.Dense(m, n, ld, _dtype(x.dtype), 0, x.data_ptr())
 
 
 def _vector(x, n: int, name: str, dtype=None) -> int:
     """Address of a contiguous device vector of n values."""
-    if x.dim() != 1 or x.shape[0] != n or not x.is_cuda or (n > 1 and x.stride(0) != 1):
+    if x.dim() != 1 or x.shape[0] != n or not x.is_cuda or not x.is_contiguous():
         raise ValueError("%s must be a contiguous device vector of %d values" % (name, n))
     if dtype is not None and x.dtype != dtype:
         raise TypeError("%s must be %s" % (name, dtype))
@@ -50,14 +63,15 @@ def _vector(x, n: int, name: str, dtype=None) -> int:
 
 
 def _same_device(first, *others) -> None:
+    d = first.get_device()
     for x in others:
-        if x is not None and x.device != first.device:
+        if x is not None and x.get_device() != d:
             raise ValueError("tensors on %s and %s" % (first.device, x.device))
 
 
 @contextlib.contextmanager
 def _other_stream(device, stream):
-    import torch
+    torch = _torch or _load_torch()
     if isinstance(stream, int):
         stream = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
     with torch.cuda.device(device), torch.cuda.stream(stream):
@@ -66,7 +80,7 @@ def _other_stream(device, stream):
 
 @contextlib.contextmanager
 def _current(device):
-    import torch
+    torch = _torch or _load_torch()
     with torch.cuda.device(device):
         yield torch.cuda.current_stream(device).cuda_stream
 
@@ -86,14 +100,23 @@ class _Here:
         return False
 
 
+def _raw_stream(device: int) -> int:
+    """hipStream_t of the device's current stream (0.1 us where torch hands
+    out the handle itself, 2 us through a stream object)."""
+    torch = _torch or _load_torch()
+    f = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return f(device) if f is not None else torch.cuda.current_stream(device).cuda_stream
+
+
 def _on(x, stream):
     """Context in which allocations belong to ``stream`` on x's device; gives
     the hipStream_t."""
-    import torch
+    torch = _torch or _load_torch()
     if stream is not None:
         return _other_stream(x.device, stream)
-    if x.device.index == torch.cuda.current_device():
-        return _Here(torch.cuda.current_stream(x.device).cuda_stream)
+    d = x.get_device()
+    if d == torch.cuda.current_device():
+        return _Here(_raw_stream(d))
     return _current(x.device)
 
 
@@ -104,7 +127,7 @@ def layer_norm(X, gamma=None, beta=None, *, eps: float = 1e-5, out_dtype=None, s
     ``out_dtype`` (X's type by default) unless ``out`` is given.  Returns
     (Y, mean, rstd); mean and rstd (float32, for ``layer_norm_backward``)
     are None when ``stats`` is false."""
-    import torch
+    torch = _torch or _load_torch()
     dx = _dense(X, "X")
     m, n = X.shape
     if gamma is not None and beta is not None and gamma.dtype != beta.dtype:
@@ -115,16 +138,16 @@ def layer_norm(X, gamma=None, beta=None, *, eps: float = 1e-5, out_dtype=None, s
     _same_device(X, gamma, beta, out)
     with _on(X, stream) as s:
         if out is None:
-            out = torch.empty((m, n), dtype=out_dtype or X.dtype, device=X.device)
+            out = X.new_empty((m, n), dtype=out_dtype)
         elif out_dtype is not None and out.dtype != out_dtype:
             raise TypeError("out is %s, out_dtype %s" % (out.dtype, out_dtype))
         dy = _dense(out, "out")
-        st = torch.empty((2, m), dtype=torch.float32, device=X.device) if stats else None
+        st = X.new_empty((2, m), dtype=torch.float32) if stats else None
         at = st.data_ptr() if stats else 0
         B_.check(B_.load().aires_layer_norm(ctypes.byref(dx), g, b, _dtype(w.dtype) if w is not None else 0, eps,
                                             ctypes.byref(dy), at or None, at + 4 * m if at else None, s),
                  "aires_layer_norm")
-    return (out, st[0], st[1]) if stats else (out, None, None)
+    return (out, *st.unbind()) if stats else (out, None, None)
 
 
 def layer_norm_backward(dY, X, mean, rstd, gamma=None, *, need_dx: bool = True, need_weights: bool = True,
@@ -133,7 +156,7 @@ def layer_norm_backward(dY, X, mean, rstd, gamma=None, *, need_dx: bool = True, 
     the statistics that the forward call returned.  Returns (dX, dgamma,
     dbeta): dX of ``dx_dtype`` (X's type by default), dgamma and dbeta of
     gamma's type (float32 without gamma); None where not needed."""
-    import torch
+    torch = _torch or _load_torch()
     dy, dx = _dense(dY, "dY"), _dense(X, "X")
     m, n = X.shape
     if tuple(dY.shape) != (m, n):
@@ -144,13 +167,13 @@ def layer_norm_backward(dY, X, mean, rstd, gamma=None, *, need_dx: bool = True, 
     lib = B_.load()
     with _on(X, stream) as s:
         wt = gamma.dtype if gamma is not None else torch.float32
-        out = torch.empty((m, n), dtype=dx_dtype or X.dtype, device=X.device) if need_dx else None
+        out = X.new_empty((m, n), dtype=dx_dtype) if need_dx else None
         dg = db = work = None
         need = ctypes.c_int64(0)
         if need_weights:
             B_.check(lib.aires_layer_norm_workspace(m, n, ctypes.byref(need)), "aires_layer_norm_workspace")
-            dg, db = torch.empty(n, dtype=wt, device=X.device), torch.empty(n, dtype=wt, device=X.device)
-            work = torch.empty(need.value, dtype=torch.uint8, device=X.device)
+            dg, db = X.new_empty((2, n), dtype=wt).unbind()
+            work = X.new_empty(need.value, dtype=torch.uint8)
         B_.check(lib.aires_layer_norm_backward(
             ctypes.byref(dy), ctypes.byref(dx), mu, r, g, _dtype(wt), ctypes.byref(_dense(out, "dX")) if need_dx else None,
             dg.data_ptr() if need_weights else None, db.data_ptr() if need_weights else None,
@@ -176,7 +199,7 @@ def linear_xent(H, W, labels, *, reduction: str = "mean", grads: bool = True, gr
     labels: t integers (int32 or int64), a label outside [0, v) marks a row
     without a target.  reduction: "mean" over labelled rows or "sum".  dH and
     dW (of H's and W's type) are multiplied with ``grad_scale``."""
-    import torch
+    torch = _torch or _load_torch()
     if reduction not in ("mean", "sum"):
         raise ValueError("reduction must be 'mean' or 'sum'")
     if labels.dtype not in (torch.int32, torch.int64):
@@ -193,11 +216,11 @@ def linear_xent(H, W, labels, *, reduction: str = "mean", grads: bool = True, gr
         need = ctypes.c_int64(0)
         B_.check(lib.aires_linear_xent_workspace(t, d, v, h.dtype, int(grads), ctypes.byref(need)),
                  "aires_linear_xent_workspace")
-        work = torch.empty(need.value, dtype=torch.uint8, device=H.device)
-        loss = torch.empty((), dtype=torch.float32, device=H.device)
-        rows = torch.empty(t, dtype=torch.float32, device=H.device)
-        dH = torch.empty((t, d), dtype=H.dtype, device=H.device) if grads else None
-        dW = torch.empty((v, d), dtype=W.dtype, device=H.device) if grads else None
+        work = H.new_empty(need.value, dtype=torch.uint8)
+        loss = H.new_empty((), dtype=torch.float32)
+        rows = H.new_empty(t, dtype=torch.float32)
+        dH = H.new_empty((t, d)) if grads else None
+        dW = H.new_empty((v, d)) if grads else None
         B_.check(lib.aires_linear_xent(
             ctypes.byref(h), ctypes.byref(w), y, int(labels.dtype == torch.int64),
             B_.REDUCE_MEAN if reduction == "mean" else B_.REDUCE_SUM, grad_scale, loss.data_ptr(), rows.data_ptr(),
@@ -211,7 +234,7 @@ def adamw_state(params, bits: int = 32):
     bits: float32 tensors.  8 bits: (codes, scales) pairs, codes of the
     parameter's shape in float8_e4m3fn (first moment) and float8_e5m2 (second),
     one float32 scale for each 256 values."""
-    import torch
+    torch = _torch or _load_torch()
     if bits == 32:
         return tuple([torch.zeros_like(p, dtype=torch.float32) for p in params] for _ in range(2))
     if bits != 8:
@@ -221,20 +244,17 @@ def adamw_state(params, bits: int = 32):
                   for p in params] for kind in (torch.float8_e4m3fn, torch.float8_e5m2))
 
 
-def _moment(x, p, kind):
-    """(address, address of the scales) of one moment of parameter p."""
-    import torch
-    if isinstance(x, tuple):
-        codes, scales = x
-        if codes.dtype != kind or codes.shape != p.shape or not codes.is_contiguous() or codes.device != p.device:
-            raise ValueError("expected contiguous %s codes of the parameter's shape" % kind)
-        if scales.dtype != torch.float32 or scales.numel() != -(-p.numel() // B_.ADAMW_BLOCK) or \
-                not scales.is_contiguous() or scales.device != p.device:
-            raise ValueError("expected one float32 scale for each %d values" % B_.ADAMW_BLOCK)
-        return codes.data_ptr(), scales.data_ptr()
-    if x.dtype != torch.float32 or x.shape != p.shape or not x.is_contiguous() or x.device != p.device:
-        raise ValueError("expected a contiguous float32 moment of the parameter's shape")
-    return x.data_ptr(), None
+def _codes(x, p, kind):
+    """(address, address of the scales) of an 8-bit moment of parameter p."""
+    torch = _torch or _load_torch()
+    codes, scales = x
+    if codes.dtype != kind or codes.shape != p.shape or not codes.is_contiguous():
+        raise ValueError("expected contiguous %s codes of the parameter's shape" % kind)
+    if scales.dtype != torch.float32 or scales.numel() != -(-p.numel() // B_.ADAMW_BLOCK) or not scales.is_contiguous():
+        raise ValueError("expected one float32 scale for each %d values" % B_.ADAMW_BLOCK)
+    if not codes.get_device() == scales.get_device() == p.get_device():
+        raise ValueError("all tensors must be on one device")
+    return codes.data_ptr(), scales.data_ptr()
 
 
 def adamw(params, grads, exp_avg, exp_avg_sq, *, step: int, lr: float, betas=(0.9, 0.999), eps: float = 1e-8,
@@ -245,28 +265,39 @@ def adamw(params, grads, exp_avg, exp_avg_sq, *, step: int, lr: float, betas=(0.
     then drives their rounding: pass another one each step); copies:
     tensors that receive the updated parameters in their own type (or None,
     also for single entries).  ``step`` counts from 1."""
-    import torch
+    torch = _torch or _load_torch()
     n = len(params)
     if not (len(grads) == len(exp_avg) == len(exp_avg_sq) == n) or (copies is not None and len(copies) != n):
         raise ValueError("params, grads, moments and copies differ in number")
     if n == 0:
         return
-    table = (B_.AdamWTensor * n)()
-    device = params[0].device
-    for k, p in enumerate(params):
-        g = grads[k]
-        if g.shape != p.shape or not p.is_contiguous() or not g.is_contiguous():
-            raise ValueError("parameter %d and its gradient must be contiguous and of one shape" % k)
-        if not p.is_cuda or p.device != device or g.device != device:
+    f32 = torch.float32
+    device = params[0].get_device()
+    if device < 0:
+        raise ValueError("parameters must be on a device")
+    rows = []  # the tensors' descriptors, ten 64-bit words each
+    for p, g, m, v, c in zip(params, grads, exp_avg, exp_avg_sq, copies or (None,) * n):
+        shape = p.shape
+        if g.shape != shape or not p.is_contiguous() or not g.is_contiguous():
+            raise ValueError("a parameter and its gradient must be contiguous and of one shape")
+        if p.get_device() != device or g.get_device() != device:
             raise ValueError("all tensors must be on one device")
-        m, ms = _moment(exp_avg[k], p, torch.float8_e4m3fn)
-        v, vs = _moment(exp_avg_sq[k], p, torch.float8_e5m2)
-        c = copies[k] if copies is not None else None
-        if c is not None and (c.shape != p.shape or not c.is_contiguous() or c.device != device):
-            raise ValueError("copy %d must be contiguous and of its parameter's shape" % k)
-        table[k] = (p.numel(), p.data_ptr(), g.data_ptr(), m, v, ms, vs, c.data_ptr() if c is not None else None,
-                    _dtype(p.dtype), _dtype(g.dtype), _dtype(c.dtype) if c is not None else 0, 0)
+        ms = vs = cp = ct = 0
+        if isinstance(m, tuple):
+            m, ms = _codes(m, p, torch.float8_e4m3fn)
+            v, vs = _codes(v, p, torch.float8_e5m2)
+        else:
+            for x in (m, v):
+                if x.dtype != f32 or x.shape != shape or not x.is_contiguous() or x.get_device() != device:
+                    raise ValueError("expected contiguous float32 moments of the parameter's shape")
+            m, v = m.data_ptr(), v.data_ptr()
+        if c is not None:
+            if c.shape != shape or not c.is_contiguous() or c.get_device() != device:
+                raise ValueError("a copy must be contiguous and of its parameter's shape")
+            cp, ct = c.data_ptr(), _dtype(c.dtype)
+        rows += (p.numel(), p.data_ptr(), g.data_ptr(), m, v, ms, vs, cp, _dtype(p.dtype) | _dtype(g.dtype) << 32, ct)
+    table = (ctypes.c_int64 * (10 * n))(*rows)
     o = B_.AdamWOpts(ctypes.sizeof(B_.AdamWOpts), int(seed) & 0xFFFFFFFF, int(step), lr, betas[0], betas[1], eps,
                      weight_decay, grad_scale)
     with _on(params[0], stream) as s:
-        B_.check(B_.load().aires_adamw(table, n, ctypes.byref(o), s), "aires_adamw")
+        B_.check(B_.load().aires_adamw(ctypes.addressof(table), n, ctypes.byref(o), s), "aires_adamw")
