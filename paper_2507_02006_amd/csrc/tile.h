@@ -34,9 +34,9 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 
-// An operand in memory.  K-contiguous: `rows` are m, `cols` k (a multiple of
-// BK, rows 16-byte aligned).  K-major: `rows` are k, `cols` m (a multiple of
-// 8).  An fp32 operand is three 16-bit planes, `plane` elements apart.
+// An operand in memory, rows 16-byte aligned, `cols` a multiple of 8.
+// K-contiguous: `rows` are m, `cols` k; k past `cols` repeats the row's last
+// chunk (the other operand holds zeros there).  K-major: `rows` are k, `cols` m.  An fp32 operand is three 16-bit planes, `plane` elements apart.
 struct Panel {
   const uint16_t* data;
   int64_t plane, ld, rows, cols;
@@ -70,38 +70,33 @@ struct Stager {
   const char* base;      // first row of the tile, advanced along k
   int64_t step;          // bytes a step
   uint32_t off[COUNT];
-  int64_t ld2, left;     // K-major: bytes a row, rows from the tile's k on
+  int64_t ld2;           // bytes a row
+  int64_t left;          // k that there are from the next stage's first on
 
   // m0: first m of the tile (m0 < extent of m); k0: first k, a multiple of BK
   __device__ void init(const Panel& p, int plane, int64_t m0, int64_t k0, int wave, int lane) {
     const char* d = reinterpret_cast<const char*>(p.data + plane * p.plane);
     ld2 = p.ld * 2;
-    if constexpr (!KMAJOR) {
-      base = d + m0 * ld2 + k0 * 2;
-      step = BK * 2;
-      const int64_t last = p.rows - 1 - m0;
-#pragma unroll
-      for (int j = 0; j < COUNT; ++j) {
-        const int r = (wave * COUNT + j) * ROWS + lane / CHUNKS;
-        const int c = (lane % CHUNKS) ^ (r / (16 / CHUNKS) % CHUNKS);
-        // rows past the end repeat the last one; their results are not used
-        off[j] = (uint32_t)((r < last ? r : last) * ld2 + c * 16);
-      }
-    } else {
-      base = d + k0 * ld2 + m0 * 2;
-      step = BK * ld2;
-      left = p.rows - k0;
-      place(p.cols - 8 - m0, wave, lane);
-    }
+    base = d + (KMAJOR ? k0 * ld2 + m0 * 2 : m0 * ld2 + k0 * 2);
+    step = KMAJOR ? BK * ld2 : BK * 2;
+    left = (KMAJOR ? p.rows : p.cols) - k0;
+    place(p, m0, wave, lane);
   }
-  // K-major offsets; rows past the end of k repeat the last one (the other
-  // operand holds zeros there).
-  __device__ void place(int64_t last_col, int wave, int lane) {
+  // Offsets within a stage.  m past the end repeats the last one (its results
+  // are not used), and so does k (the other operand holds zeros there).
+  __device__ void place(const Panel& p, int64_t m0, int wave, int lane) {
 #pragma unroll
     for (int j = 0; j < COUNT; ++j) {
-      const int k = (wave * COUNT + j) * ROWS + lane / CHUNKS;
-      const int c = ((lane % CHUNKS) ^ ((k & 3) * 4)) * 8;
-      off[j] = (uint32_t)((k < left ? k : left - 1) * ld2 + (c < last_col ? c : last_col) * 2);
+      const int r = (wave * COUNT + j) * ROWS + lane / CHUNKS;
+      if constexpr (KMAJOR) {
+        const int64_t last = p.cols - 8 - m0;
+        const int c = ((lane % CHUNKS) ^ ((r & 3) * 4)) * 8;
+        off[j] = (uint32_t)((r < left ? r : left - 1) * ld2 + (c < last ? c : last) * 2);
+      } else {
+        const int64_t last = p.rows - 1 - m0;
+        const int c = ((lane % CHUNKS) ^ (r / (16 / CHUNKS) % CHUNKS)) * 8;
+        off[j] = (uint32_t)((r < last ? r : last) * ld2 + (c < left ? c : left - 8) * 2);
+      }
     }
   }
   __device__ __forceinline__ void issue(char* lds, int wave) const {
@@ -188,17 +183,15 @@ struct Tile {
         sa.init(A, pa, m0, (int64_t)s0 * BK, wave, lane);
         sb.init(B, pb, n0, (int64_t)s0 * BK, wave, lane);
       }
-      if constexpr (AK)
-        if (sa.left < BK) sa.place(A.cols - 8 - m0, wave, lane);
-      if constexpr (BK_)
-        if (sb.left < BK) sb.place(B.cols - 8 - n0, wave, lane);
+      if (sa.left < BK) sa.place(A, m0, wave, lane);
+      if (sb.left < BK) sb.place(B, n0, wave, lane);
       char* to = lds + stage * STAGE;
       sa.issue(to, wave);
       sb.issue(to + TM * BK * 2, wave);
       sa.base += sa.step;
       sb.base += sb.step;
-      if constexpr (AK) sa.left -= BK;
-      if constexpr (BK_) sb.left -= BK;
+      sa.left -= BK;
+      sb.left -= BK;
       ++at;
     };
     s16x8 fa[2][MT], fb[2][NT];

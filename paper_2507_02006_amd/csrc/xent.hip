@@ -27,10 +27,8 @@ namespace aires {
 namespace kern {
 namespace {
 
-constexpr int TV = 256, TT = 256;      // a tile of scores: table by rows of H
-constexpr int GM = 256, GN = 256;      // a tile of a gradient product
+constexpr int TV = 256;  // table entries of a tile of scores
 constexpr int64_t kPieceBytes = int64_t(256) << 20;  // dz of one piece of the table
-constexpr int ROWS = 64, SLICES = 16;  // k_rows: rows of a workgroup, shares of the tiles
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.693147180559945309417f;
 constexpr float F16_UP = 1024.f;       // dz in fp16 is held times this: 2^-35 is its least step
 
@@ -93,20 +91,29 @@ struct Scores {
   const float* top; const float* inv;  // of whole rows
   const void* labels; int i64;
   uint16_t* dz; int64_t plane, ldz;
+  uint32_t* ticket;       // cleared here for the workgroups of k_rows
 };
 
-template <bool GRAD, int TYPE>
-__global__ __launch_bounds__(512, 2) void k_scores(Scores s) {
+// TT rows of H a tile.  256: eight wavefronts of 128 x 64; 128: of 64 x 64;
+// 32: four of 64 x 32, two workgroups a CU, for the few rows whose scores only
+// cost the reading of the table (T = 1, 262144 x 512 bf16: 41 us against 71
+// with 256 rows).
+template <int TT, bool F16>
+using ScoreTile = Tile<TV, TT, TT == 256 ? 128 : 64, TT == 32 ? 32 : 64, false, false, F16>;
+
+template <bool GRAD, int TYPE, int TT>
+__global__ __launch_bounds__(TT == 32 ? 256 : 512, 2) void k_scores(Scores s) {
   constexpr bool F16 = TYPE == DT_F16;
   constexpr int PLANES = TYPE == DT_F32 ? 3 : 1;
-  using T_ = Tile<TV, TT, 128, 64, false, false, F16>;
+  using T_ = ScoreTile<TT, F16>;
+  constexpr int SPAN = T_::MT * 32, NWM = TV / SPAN;  // table entries of a wavefront, wavefronts along the table
   __shared__ __attribute__((aligned(16))) char lds[T_::LDS];
   int64_t vt, tt;
   place_tile(blockIdx.x, (s.v1 - s.v0 + TV - 1) / TV, (s.T + TT - 1) / TT, 8, vt, tt);
   const int64_t v0 = s.v0 + vt * TV, t0 = tt * TT;
   f32x16 acc[T_::MT][T_::NT];
   T_::run(s.W, v0, s.H, t0, 0, s.steps, s.segs, lds, acc);
-  const int lane = threadIdx.x & 63, wm = (threadIdx.x >> 6) / (TT / 64);
+  const int lane = threadIdx.x & 63, wm = (threadIdx.x >> 6) / (T_::WAVES / NWM);
   __syncthreads();  // the stages' LDS changes its use
 
   if constexpr (!GRAD) {
@@ -119,7 +126,8 @@ __global__ __launch_bounds__(512, 2) void k_scores(Scores s) {
 #pragma unroll
             for (int j = 0; j < T_::NT; ++j) acc[i][j][r] = -INFINITY;
     }
-    float2* half = reinterpret_cast<float2*>(lds);  // of the upper half of the table's rows
+    if (blockIdx.x == 0 && threadIdx.x == 0) *s.ticket = 0;
+    float2* others = reinterpret_cast<float2*>(lds);  // of the wavefronts after the first along the table
 #pragma unroll
     for (int j = 0; j < T_::NT; ++j) {
       float top = -INFINITY;
@@ -136,7 +144,7 @@ __global__ __launch_bounds__(512, 2) void k_scores(Scores s) {
         for (int r = 0; r < 16; ++r) sum += exp2_fast(fmaf(acc[i][j][r], LOG2E, -from));
       sum += __shfl_xor(sum, 32);
       const int c = T_::col(j);
-      if (wm == 1 && lane < 32) half[c] = make_float2(top, sum);
+      if (wm > 0 && lane < 32) others[(wm - 1) * TT + c] = make_float2(top, sum);
       acc[0][j][0] = top;
       acc[0][j][1] = sum;
     }
@@ -146,7 +154,8 @@ __global__ __launch_bounds__(512, 2) void k_scores(Scores s) {
       for (int j = 0; j < T_::NT; ++j) {
         const int c = T_::col(j);
         float m = acc[0][j][0], x = acc[0][j][1];
-        join(m, x, half[c].x, half[c].y);
+#pragma unroll
+        for (int w = 0; w < NWM - 1; ++w) join(m, x, others[w * TT + c].x, others[w * TT + c].y);
         if (t0 + c < s.T) s.part[vt * s.T + t0 + c] = make_float2(m, x);
       }
   } else {
@@ -163,9 +172,9 @@ __global__ __launch_bounds__(512, 2) void k_scores(Scores s) {
           const float p = exp2_fast(fmaf(acc[i][j][r], LOG2E, -top)) * inv;
           acc[i][j][r] = there ? p : 0.f;  // a score that is no number stays out of rows without a label
         }
-      const int64_t first = v0 + wm * 128;
-      if (__any(there && label >= first && label < first + 128)) {
-        const int at = there && label >= first && label < first + 128 ? (int)(label - v0) : -1;
+      const int64_t first = v0 + wm * SPAN;
+      if (__any(there && label >= first && label < first + SPAN)) {
+        const int at = there && label >= first && label < first + SPAN ? (int)(label - v0) : -1;
 #pragma unroll
         for (int i = 0; i < T_::MT; ++i)
 #pragma unroll
@@ -223,47 +232,58 @@ struct Rows {
   const void* labels; int i64;
   const float2* part; int64_t tiles;
   float* top; float* inv; float* row_loss;
-  double2* sums;  // a workgroup's losses and labelled rows
+  double2* sums;      // a workgroup's losses and labelled rows
+  uint32_t* ticket;
+  int mean; float grad_scale;
+  float* scale; float* loss;
 };
 
-// Maximum and sum of each row from its tiles', and its loss: 64 rows, a
-// sixteenth of the tiles to each wavefront, then four rows' label scores.
-__global__ __launch_bounds__(ROWS * SLICES) void k_rows(Rows a) {
+// Maximum and sum of each row from its tiles', and its loss: ROWS rows a
+// workgroup, 1024 / ROWS threads to a row's tiles, then a wavefront to each
+// row's label score.  The last workgroup to finish adds up the loss, in the
+// order of the workgroups, and what dz is multiplied with.
+template <int ROWS>
+__global__ __launch_bounds__(1024) void k_rows(Rows a) {
+  constexpr int SLICES = 1024 / ROWS, WAVES = 16;
   __shared__ float2 buf[SLICES][ROWS];
   __shared__ float lse[ROWS];
-  __shared__ double2 sums[SLICES];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int64_t T = a.H.rows, t0 = (int64_t)blockIdx.x * ROWS, t = t0 + lane;
+  __shared__ double2 sums[1024];
+  __shared__ bool last;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, r = tid % ROWS, slice = tid / ROWS;
+  const int64_t T = a.H.rows, t0 = (int64_t)blockIdx.x * ROWS, t = t0 + r;
   float m = -INFINITY, s = 0.f;
   if (t < T) {
 #pragma unroll 4
-    for (int64_t i = w; i < a.tiles; i += SLICES) {
+    for (int64_t i = slice; i < a.tiles; i += SLICES) {
       const float2 p = a.part[i * T + t];
       join(m, s, p.x, p.y);
     }
   }
-  buf[w][lane] = make_float2(m, s);
+  buf[slice][r] = make_float2(m, s);
   __syncthreads();
-  if (w == 0 && t < T) {
-    for (int i = 1; i < SLICES; ++i) join(m, s, buf[i][lane].x, buf[i][lane].y);
+  for (int o = SLICES / 2; o > 0; o >>= 1) {
+    if (slice < o) {
+      join(m, s, buf[slice + o][r].x, buf[slice + o][r].y);
+      buf[slice][r] = make_float2(m, s);
+    }
+    __syncthreads();
+  }
+  if (slice == 0 && t < T) {
     a.top[t] = m;
     a.inv[t] = 1.f / s;
-    lse[lane] = (m + log2f(s)) * LN2;
+    lse[r] = (m + log2f(s)) * LN2;
   }
   __syncthreads();
   double loss = 0, count = 0;
-  for (int i = 0; i < ROWS / SLICES; ++i) {
-    const int r = w * (ROWS / SLICES) + i;
-    const int64_t row = t0 + r;
+  for (int i = w; i < ROWS; i += WAVES) {
+    const int64_t row = t0 + i;
     if (row >= T) break;
     const int64_t label = label_at(a.labels, a.i64, row);
     float x = 0.f;
     if (label >= 0 && label < a.W.rows) {
       for (int64_t d = lane; d < a.H.cols; d += 64)
         x = fmaf(load1(a.H.data, a.H.type, row * a.H.ld + d), load1(a.W.data, a.W.type, label * a.W.ld + d), x);
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o);
-      x = lse[r] - x;
+      x = lse[i] - wave_sum_f32(x);
       loss += x;
       count += 1;
     }
@@ -271,37 +291,37 @@ __global__ __launch_bounds__(ROWS * SLICES) void k_rows(Rows a) {
   }
   if (lane == 0) sums[w] = make_double2(loss, count);
   __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int i = 1; i < SLICES; ++i) {
+  if (tid == 0) {
+    for (int i = 1; i < WAVES; ++i) {
       loss += sums[i].x;
       count += sums[i].y;
     }
     a.sums[blockIdx.x] = make_double2(loss, count);
+    // the sums are visible to whoever draws a later number
+    last = gridDim.x == 1 ||
+           __hip_atomic_fetch_add(a.ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
   }
-}
-
-// loss, and what dz is multiplied with; one workgroup, a fixed order.
-__global__ __launch_bounds__(256) void k_loss(const double2* sums, int64_t n, int mean, float grad_scale, float* scale,
-                                              float* loss) {
-  __shared__ double2 buf[256];
-  double x = 0, c = 0;
-  for (int64_t i = threadIdx.x; i < n; i += 256) {
-    x += sums[i].x;
-    c += sums[i].y;
-  }
-  buf[threadIdx.x] = make_double2(x, c);
   __syncthreads();
-  for (int o = 128; o > 0; o >>= 1) {
-    if ((int)threadIdx.x < o) {
-      buf[threadIdx.x].x += buf[threadIdx.x + o].x;
-      buf[threadIdx.x].y += buf[threadIdx.x + o].y;
+  if (!last) return;
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+  loss = count = 0;
+  for (int64_t i = tid; i < (int64_t)gridDim.x; i += 1024) {
+    loss += a.sums[i].x;
+    count += a.sums[i].y;
+  }
+  sums[tid] = make_double2(loss, count);
+  __syncthreads();
+  for (int o = 512; o > 0; o >>= 1) {
+    if (tid < o) {
+      sums[tid].x += sums[tid + o].x;
+      sums[tid].y += sums[tid + o].y;
     }
     __syncthreads();
   }
-  if (threadIdx.x == 0) {
-    const double div = mean && buf[0].y > 0 ? buf[0].y : 1.0;
-    *scale = (float)(grad_scale / div);
-    *loss = (float)(buf[0].x / div);
+  if (tid == 0) {
+    const double div = a.mean && sums[0].y > 0 ? sums[0].y : 1.0;
+    *a.scale = (float)(a.grad_scale / div);
+    *a.loss = (float)(sums[0].x / div);
   }
 }
 
@@ -326,12 +346,12 @@ struct Gradients {
   const float* scale;
 };
 
-template <class T_>
+template <class T_, int G>
 __device__ __forceinline__ void product(const Product& p, int64_t b, int segs, const float* scale, char* lds) {
   int64_t y, x;
   place_tile(b, p.ny * p.slices, p.nx, 8, y, x);
   const int slice = (int)(y / p.ny);
-  const int64_t m0 = (y - slice * p.ny) * GM, n0 = x * GN;
+  const int64_t m0 = (y - slice * p.ny) * G, n0 = x * G;
   const int s0 = slice * p.per, s1 = s0 + p.per < p.steps ? s0 + p.per : p.steps;
   f32x16 acc[T_::MT][T_::NT];
   T_::run(p.A, m0, p.B, n0, s0, s1, segs, lds, acc);
@@ -342,7 +362,7 @@ __device__ __forceinline__ void product(const Product& p, int64_t b, int segs, c
   float* mine = reinterpret_cast<float*>(lds) + wave * (32 * W);
   const float k = p.part ? 1.f : *scale;
   float* part = p.part ? p.part + slice * p.rows * p.ldp : nullptr;
-  const int64_t row0 = m0 + wave / (GN / W) * (T_::MT * 32), n = n0 + wave % (GN / W) * W + lane % (W / 4) * 4;
+  const int64_t row0 = m0 + wave / (G / W) * (T_::MT * 32), n = n0 + wave % (G / W) * W + lane % (W / 4) * 4;
   __syncthreads();  // the stages' LDS changes its use
 #pragma unroll
   for (int i = 0; i < T_::MT; ++i) {
@@ -378,31 +398,63 @@ __device__ __forceinline__ void product(const Product& p, int64_t b, int segs, c
   }
 }
 
-template <bool F16>
-__global__ __launch_bounds__(512, 2) void k_gradients(Gradients g) {
-  using TH = Tile<GM, GN, 128, 64, false, true, F16>;
-  using TW = Tile<GM, GN, 128, 64, true, true, F16>;
+// G x G tiles: 256 by eight wavefronts of 128 x 64, or 128 by four of 64 x 64
+// (two workgroups a CU).
+template <bool F16, int G>
+__global__ __launch_bounds__(G == 256 ? 512 : 256, 2) void k_gradients(Gradients g) {
+  using TH = Tile<G, G, G / 2, 64, false, true, F16>;
+  using TW = Tile<G, G, G / 2, 64, true, true, F16>;
   __shared__ __attribute__((aligned(16))) char lds[TH::LDS];
-  if ((int64_t)blockIdx.x < g.first_dw) product<TH>(g.dh, blockIdx.x, g.segs, g.scale, lds);
-  else product<TW>(g.dw, blockIdx.x - g.first_dw, g.segs, g.scale, lds);
+  if ((int64_t)blockIdx.x < g.first_dw) product<TH, G>(g.dh, blockIdx.x, g.segs, g.scale, lds);
+  else product<TW, G>(g.dw, blockIdx.x - g.first_dw, g.segs, g.scale, lds);
 }
 
-// out = scale times the sum of the slices.
+// out = scale times the sum of the slices; GROUPS threads to an element's
+// slices (16 where there are many).
+template <int GROUPS>
 __global__ __launch_bounds__(256) void k_finish(const float* part, int slices, int64_t rows, int64_t cols, int64_t ldp,
                                                 const float* scale, void* out, int type, int64_t ldo) {
+  constexpr int ITEMS = 256 / GROUPS;
+  __shared__ float4 buf[GROUPS][ITEMS];
   const int64_t per = (cols + 3) / 4, total = rows * per;
+  const int item = threadIdx.x % ITEMS, group = threadIdx.x / ITEMS;
   const float k = *scale;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / per, c = (i - r * per) * 4;
-    float x[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int64_t i0 = (int64_t)blockIdx.x * ITEMS; i0 < total; i0 += (int64_t)gridDim.x * ITEMS) {
+    const int64_t i = i0 + item, r = i / per, c = (i - r * per) * 4;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (i < total) {
 #pragma unroll 4
-    for (int s = 0; s < slices; ++s) {
-      const float4 v = *reinterpret_cast<const float4*>(part + (s * rows + r) * ldp + c);
-      x[0] += v.x; x[1] += v.y; x[2] += v.z; x[3] += v.w;
+      for (int s = group; s < slices; s += GROUPS) {
+        const float4 v = *reinterpret_cast<const float4*>(part + (s * rows + r) * ldp + c);
+        x.x += v.x; x.y += v.y; x.z += v.z; x.w += v.w;
+      }
     }
+    if constexpr (GROUPS > 1) {
+      buf[group][item] = x;
+      __syncthreads();
+      if (group == 0)
+        for (int q = 1; q < GROUPS; ++q) {
+          const float4 v = buf[q][item];
+          x.x += v.x; x.y += v.y; x.z += v.z; x.w += v.w;
+        }
+      __syncthreads();
+    }
+    if (group != 0 || i >= total) continue;
+    const float o[4] = {x.x * k, x.y * k, x.z * k, x.w * k};
+#pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (c + j < cols) store1(out, type, r * ldo + c + j, x[j] * k);
+      if (c + j < cols) store1(out, type, r * ldo + c + j, o[j]);
   }
+}
+
+void finish(const float* part, int slices, int64_t rows, int64_t cols, int64_t ldp, const float* scale, void* out,
+            int type, int64_t ldo, hipStream_t s) {
+  const int64_t items = rows * ((cols + 3) / 4);
+  const unsigned most = 8192;
+  if (slices > 8)
+    k_finish<16><<<(unsigned)std::min<int64_t>(most, (items + 15) / 16), 256, 0, s>>>(part, slices, rows, cols, ldp, scale, out, type, ldo);
+  else
+    k_finish<1><<<(unsigned)std::min<int64_t>(most, (items + 255) / 256), 256, 0, s>>>(part, slices, rows, cols, ldp, scale, out, type, ldo);
 }
 
 __global__ __launch_bounds__(256) void k_zero(void* out, int type, int64_t rows, int64_t cols, int64_t ld) {
@@ -420,9 +472,10 @@ unsigned grid_of(int64_t items, int64_t per) {
 // Sizes and places in the workspace.
 struct Layout {
   int64_t width, planes, segs;         // columns of the packed operands
+  int TT, G, rows_at_once;             // tiles; rows of a workgroup of k_rows
   int64_t piece, Tp, ldz;              // table entries of a piece, rows of dz and their stride
-  int dh_steps, dh_per, dh_slices, dw_per, dw_slices;
-  int64_t scale, top, inv, rows, sums, part, h, w, dh, dw, dz, bytes;
+  int dh_per, dh_slices, dw_per, dw_slices;
+  int64_t ticket, scale, top, inv, rows, sums, part, h, w, dh, dw, dz, bytes;
 };
 
 void slices_of(int steps, int64_t ideal, int& per, int& slices) {
@@ -442,23 +495,27 @@ Layout layout_of(int64_t T, int64_t D, int64_t V, int type, bool grads) {
   l.width = up(D, BK);
   l.planes = type == DT_F32 ? 3 : 1;
   l.segs = type == DT_F32 ? 6 : 1;
-  l.Tp = up(T, TT);
+  l.TT = T <= 32 ? 32 : T <= 128 ? 128 : 256;
+  l.rows_at_once = T <= 2048 ? 8 : 64;
+  l.Tp = up(T, l.TT);
+  l.ticket = take(4);
   l.scale = take(4);
   l.top = take(4 * T);
   l.inv = take(4 * T);
   l.rows = take(4 * T);
-  l.sums = take(16 * (up(T, ROWS) / ROWS));
+  l.sums = take(16 * std::max<int64_t>(1, up(T, l.rows_at_once) / l.rows_at_once));
   l.part = take(8 * T * (up(V, TV) / TV));
   l.h = take(2 * l.planes * T * l.width);
   l.w = take(2 * l.planes * V * l.width);
   if (grads) {
     l.piece = std::min(up(V, TV), std::max<int64_t>(TV, kPieceBytes / (2 * l.planes * std::max<int64_t>(l.Tp, 1)) / TV * TV));
-    // shares of about equal length that give every CU one
-    const int64_t nx = up(D, GN) / GN, th = up(T, GM) / GM * nx, tw = l.piece / GM * nx;
-    l.dh_steps = (int)(up(std::min(l.piece, V), BK) / BK);
-    const int dw_steps = (int)(up(T, BK) / BK);
-    const int64_t ideal = std::max<int64_t>(8, (th * l.dh_steps + tw * dw_steps) / 256);
-    slices_of(l.dh_steps, ideal, l.dh_per, l.dh_slices);
+    const int dh_steps = (int)(up(std::min(l.piece, V), BK) / BK), dw_steps = (int)(up(T, BK) / BK);
+    // small tiles where a side would leave half of a large one empty
+    l.G = std::min({T, D, V}) <= 128 ? 128 : 256;
+    // shares of k of about equal length, one workgroup (of 256, else two) a CU
+    const int64_t nx = up(D, l.G) / l.G, th = up(T, l.G) / l.G * nx, tw = up(std::min(l.piece, V), l.G) / l.G * nx;
+    const int64_t ideal = std::max<int64_t>(8, (th * dh_steps + tw * dw_steps) / (l.G == 256 ? 256 : 512));
+    slices_of(dh_steps, ideal, l.dh_per, l.dh_slices);
     slices_of(dw_steps, ideal, l.dw_per, l.dw_slices);
     if (l.dh_slices > 1 || l.piece < V) l.dh = take(4 * l.dh_slices * T * l.width);
     if (l.dw_slices > 1) l.dw = take(4 * l.dw_slices * l.piece * l.width);
@@ -469,15 +526,32 @@ Layout layout_of(int64_t T, int64_t D, int64_t V, int type, bool grads) {
   return l;
 }
 
-// X as it lies, where the tiles can read it, else packed into ws.
-Panel panel_of(const Mat& X, const Layout& l, char* ws, hipStream_t s) {
-  if (l.planes == 1 && X.cols == l.width && X.ld % 8 == 0 && X.ld < (int64_t(1) << 22) &&
+// X as it lies, where the tiles can read it, else packed into ws with zeros
+// to the next multiple of BK columns.  Of the two operands of the scores one
+// has to hold zeros there: H (whole), which is the smaller one as a rule.
+Panel panel_of(const Mat& X, const Layout& l, bool whole, char* ws, hipStream_t s) {
+  if (l.planes == 1 && X.cols % (whole ? BK : 8) == 0 && X.ld % 8 == 0 && X.ld < (int64_t(1) << 22) &&
       (reinterpret_cast<uintptr_t>(X.data) & 15) == 0)
     return Panel{static_cast<const uint16_t*>(X.data), 0, X.ld, X.rows, X.cols};
   uint16_t* to = reinterpret_cast<uint16_t*>(ws);
   const int64_t plane = X.rows * l.width;
   k_pack<<<grid_of(X.rows * (l.width / 4), 1024), 256, 0, s>>>(X, to, plane, l.width, (int)l.planes);
   return Panel{to, plane, l.width, X.rows, l.width};
+}
+
+template <bool GRAD, int TYPE>
+void scores(const Scores& sc, int TT, hipStream_t s) {
+  const unsigned grid = (unsigned)(up(sc.v1 - sc.v0, TV) / TV * (up(sc.T, TT) / TT));
+  if (TT == 32) k_scores<GRAD, TYPE, 32><<<grid, 256, 0, s>>>(sc);
+  else if (TT == 128) k_scores<GRAD, TYPE, 128><<<grid, 512, 0, s>>>(sc);
+  else k_scores<GRAD, TYPE, 256><<<grid, 512, 0, s>>>(sc);
+}
+
+template <bool GRAD>
+void scores(const Scores& sc, int type, int TT, hipStream_t s) {
+  if (type == DT_F32) scores<GRAD, DT_F32>(sc, TT, s);
+  else if (type == DT_BF16) scores<GRAD, DT_BF16>(sc, TT, s);
+  else scores<GRAD, DT_F16>(sc, TT, s);
 }
 
 }  // namespace
@@ -494,73 +568,69 @@ hipError_t linear_xent(const XentArgs& x, hipStream_t s) {
   const Layout l = layout_of(T, D, V, type, grads);
   char* ws = static_cast<char*>(x.ws);
   float* scale = (float*)(ws + l.scale);
-  double2* sums = (double2*)(ws + l.sums);
-  if (T == 0) {
-    k_loss<<<1, 256, 0, s>>>(sums, 0, x.mean, x.grad_scale, scale, x.loss);
-    if (grads && V > 0 && D > 0) k_zero<<<grid_of(V * D, 1024), 256, 0, s>>>(x.dW.data, type, V, D, x.dW.ld);
-    return hipGetLastError();
-  }
   Scores sc{};
-  sc.H = panel_of(x.H, l, ws + l.h, s);
-  sc.W = panel_of(x.W, l, ws + l.w, s);
-  sc.T = T; sc.V = V; sc.v0 = 0; sc.v1 = V;
-  sc.steps = (int)(l.width / BK);
-  sc.segs = (int)l.segs;
-  sc.part = (float2*)(ws + l.part);
-  sc.labels = x.labels; sc.i64 = x.labels_i64;
-  auto scores = [&](bool grad) {
-    const unsigned grid = (unsigned)(up(sc.v1 - sc.v0, TV) / TV * (l.Tp / TT));
-    if (type == DT_F32) grad ? k_scores<true, DT_F32><<<grid, 512, 0, s>>>(sc) : k_scores<false, DT_F32><<<grid, 512, 0, s>>>(sc);
-    else if (type == DT_BF16) grad ? k_scores<true, DT_BF16><<<grid, 512, 0, s>>>(sc) : k_scores<false, DT_BF16><<<grid, 512, 0, s>>>(sc);
-    else grad ? k_scores<true, DT_F16><<<grid, 512, 0, s>>>(sc) : k_scores<false, DT_F16><<<grid, 512, 0, s>>>(sc);
-  };
-  scores(false);
+  if (T > 0) {
+    sc.H = panel_of(x.H, l, true, ws + l.h, s);
+    sc.W = panel_of(x.W, l, false, ws + l.w, s);
+    sc.T = T; sc.V = V; sc.v0 = 0; sc.v1 = V;
+    sc.steps = (int)(l.width / BK);
+    sc.segs = (int)l.segs;
+    sc.part = (float2*)(ws + l.part);
+    sc.labels = x.labels; sc.i64 = x.labels_i64;
+    sc.ticket = (uint32_t*)(ws + l.ticket);
+    scores<false>(sc, type, l.TT, s);
+  }
   Rows rw{};
   rw.H = x.H; rw.W = x.W; rw.labels = x.labels; rw.i64 = x.labels_i64;
   rw.part = sc.part; rw.tiles = up(V, TV) / TV;
   rw.top = (float*)(ws + l.top); rw.inv = (float*)(ws + l.inv);
   rw.row_loss = x.row_loss ? x.row_loss : (float*)(ws + l.rows);
-  rw.sums = sums;
-  const int64_t blocks = up(T, ROWS) / ROWS;
-  k_rows<<<(unsigned)blocks, ROWS * SLICES, 0, s>>>(rw);
-  // fp16 dz is held times F16_UP
-  k_loss<<<1, 256, 0, s>>>(sums, blocks, x.mean, x.grad_scale * (f16 ? 1.f / F16_UP : 1.f), scale, x.loss);
+  rw.sums = (double2*)(ws + l.sums);
+  rw.ticket = sc.ticket;
+  rw.mean = x.mean;
+  rw.grad_scale = x.grad_scale * (f16 ? 1.f / F16_UP : 1.f);  // fp16 dz is held times F16_UP
+  rw.scale = scale; rw.loss = x.loss;
+  const unsigned blocks = (unsigned)std::max<int64_t>(1, up(T, l.rows_at_once) / l.rows_at_once);
+  if (l.rows_at_once == 8) k_rows<8><<<blocks, 1024, 0, s>>>(rw);
+  else k_rows<64><<<blocks, 1024, 0, s>>>(rw);
   if (!grads) return hipGetLastError();
+  if (T == 0) {
+    if (V > 0 && D > 0) k_zero<<<grid_of(V * D, 1024), 256, 0, s>>>(x.dW.data, type, V, D, x.dW.ld);
+    return hipGetLastError();
+  }
   sc.top = rw.top; sc.inv = rw.inv;
   sc.dz = (uint16_t*)(ws + l.dz);
   sc.ldz = l.ldz;
   sc.plane = l.Tp * l.ldz;
   const Panel dz{sc.dz, sc.plane, l.ldz, l.Tp, l.piece};
-  const int64_t nx = up(D, GN) / GN;
+  const int64_t nx = up(D, l.G) / l.G;
   const int size = dtype_bytes(type);
   for (int64_t v0 = 0; v0 < V; v0 += l.piece) {
     const int64_t n = std::min(l.piece, V - v0);
     sc.v0 = v0; sc.v1 = v0 + n;
-    scores(true);
+    scores<true>(sc, type, l.TT, s);
     Gradients g{};
     g.segs = (int)l.segs;
     g.scale = scale;
     Panel w = sc.W;
     w.data += v0 * w.ld;
     w.rows = n;
-    g.dh = Product{dz, w, up(T, GM) / GM, nx, T, D, (int)(up(n, BK) / BK), l.dh_per, 0,
+    g.dh = Product{dz, w, up(T, l.G) / l.G, nx, T, D, (int)(up(n, BK) / BK), l.dh_per, 0,
                    l.dh ? (float*)(ws + l.dh) : nullptr, l.width, v0 > 0, x.dH.data, x.dH.ld, type};
     g.dh.slices = (g.dh.steps + l.dh_per - 1) / l.dh_per;
     Mat out = x.dW;
     out.data = (char*)x.dW.data + v0 * x.dW.ld * size;
-    g.dw = Product{dz, sc.H, up(n, GM) / GM, nx, n, D, (int)(up(T, BK) / BK), l.dw_per, l.dw_slices,
+    g.dw = Product{dz, sc.H, up(n, l.G) / l.G, nx, n, D, (int)(up(T, BK) / BK), l.dw_per, l.dw_slices,
                    l.dw ? (float*)(ws + l.dw) : nullptr, l.width, 0, out.data, out.ld, type};
     g.first_dw = g.dh.blocks();
     const unsigned grid = (unsigned)(g.first_dw + g.dw.blocks());
-    if (f16) k_gradients<true><<<grid, 512, 0, s>>>(g);
-    else k_gradients<false><<<grid, 512, 0, s>>>(g);
-    if (l.dw)
-      k_finish<<<grid_of(n * ((D + 3) / 4), 256), 256, 0, s>>>((float*)(ws + l.dw), l.dw_slices, n, D, l.width, scale,
-                                                               out.data, type, out.ld);
+    if (l.G == 256 && f16) k_gradients<true, 256><<<grid, 512, 0, s>>>(g);
+    else if (l.G == 256) k_gradients<false, 256><<<grid, 512, 0, s>>>(g);
+    else if (f16) k_gradients<true, 128><<<grid, 256, 0, s>>>(g);
+    else k_gradients<false, 128><<<grid, 256, 0, s>>>(g);
+    if (l.dw) finish((float*)(ws + l.dw), l.dw_slices, n, D, l.width, scale, out.data, type, out.ld, s);
   }
-  if (l.dh)
-    k_finish<<<grid_of(T * ((D + 3) / 4), 256), 256, 0, s>>>((float*)(ws + l.dh), l.dh_slices, T, D, l.width, scale,
-                                                             x.dH.data, type, x.dH.ld);
+  if (l.dh) finish((float*)(ws + l.dh), l.dh_slices, T, D, l.width, scale, x.dH.data, type, x.dH.ld, s);
   return hipGetLastError();
 }
 
