@@ -9,7 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB = os.path.join(HERE, "libaires.so")
 SOURCES = [os.path.join(HERE, "csrc", n) for n in
            ("aires.cpp", "train.cpp", "kernels.hip", "narrow.hip", "spmm.hip", "normalize.hip", "scratch.hip",
-            "layernorm.hip", "adamw.hip", "xent.hip")]
+            "layernorm.hip", "adamw.hip", "xent.hip", "xent_few.hip")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",

@@ -1,0 +1,34 @@
+// Shared by the cross entropy's kernels: xent.hip (any table) and
+// xent_few.hip (few classes).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "train.h"
+
+namespace aires {
+namespace kern {
+
+// out (rows x cols of `type`) = *scale times the sum of fp32 slices
+// [slice][rows][ldp], in a fixed order; ldp a multiple of 4.
+void finish(const float* part, int slices, int64_t rows, int64_t cols, int64_t ldp, const float* scale, void* out,
+            int type, int64_t ldo, hipStream_t s);
+
+// Few classes: whether this shape takes that path, its workspace, and the call.
+bool xent_few_fits(int64_t T, int64_t D, int64_t V);
+int64_t xent_few_workspace(int64_t T, int64_t D, int64_t V, bool grads);
+hipError_t xent_few(const XentArgs& x, hipStream_t s);
+
+namespace {
+
+constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.693147180559945309417f;
+
+__device__ __forceinline__ int64_t label_at(const void* labels, int i64, int64_t i) {
+  return i64 ? static_cast<const int64_t*>(labels)[i] : (int64_t)static_cast<const int32_t*>(labels)[i];
+}
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+}  // namespace
+}  // namespace kern
+}  // namespace aires

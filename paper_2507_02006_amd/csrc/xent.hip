@@ -22,6 +22,7 @@
 #include "dense.h"
 #include "device.h"
 #include "tile.h"
+#include "xent.h"
 
 namespace aires {
 namespace kern {
@@ -29,14 +30,7 @@ namespace {
 
 constexpr int TV = 256;  // table entries of a tile of scores
 constexpr int64_t kPieceBytes = int64_t(256) << 20;  // dz of one piece of the table
-constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.693147180559945309417f;
 constexpr float F16_UP = 1024.f;       // dz in fp16 is held times this: 2^-35 is its least step
-
-__device__ __forceinline__ int64_t label_at(const void* labels, int i64, int64_t i) {
-  return i64 ? static_cast<const int64_t*>(labels)[i] : (int64_t)static_cast<const int32_t*>(labels)[i];
-}
-
-__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // Joins two (maximum, sum of exponentials) in base 2; equal maxima (of minus
 // infinity too) need no scaling.
@@ -447,6 +441,8 @@ __global__ __launch_bounds__(256) void k_finish(const float* part, int slices, i
   }
 }
 
+}  // namespace
+
 void finish(const float* part, int slices, int64_t rows, int64_t cols, int64_t ldp, const float* scale, void* out,
             int type, int64_t ldo, hipStream_t s) {
   const int64_t items = rows * ((cols + 3) / 4);
@@ -456,6 +452,8 @@ void finish(const float* part, int slices, int64_t rows, int64_t cols, int64_t l
   else
     k_finish<1><<<(unsigned)std::min<int64_t>(most, (items + 255) / 256), 256, 0, s>>>(part, slices, rows, cols, ldp, scale, out, type, ldo);
 }
+
+namespace {
 
 __global__ __launch_bounds__(256) void k_zero(void* out, int type, int64_t rows, int64_t cols, int64_t ld) {
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * cols; i += (int64_t)gridDim.x * 256)
@@ -557,6 +555,7 @@ void scores(const Scores& sc, int type, int TT, hipStream_t s) {
 }  // namespace
 
 int64_t linear_xent_workspace(int64_t T, int64_t D, int64_t V, int type, bool grads) {
+  if (xent_few_fits(T, D, V)) return xent_few_workspace(T, D, V, grads);
   return layout_of(T, D, V, type, grads).bytes;
 }
 
@@ -565,6 +564,7 @@ hipError_t linear_xent(const XentArgs& x, hipStream_t s) {
   const bool grads = x.dW.data != nullptr || x.dH.data != nullptr;
   const int type = x.H.type;
   const bool f16 = type == DT_F16;
+  if (xent_few_fits(T, D, V)) return xent_few(x, s);
   const Layout l = layout_of(T, D, V, type, grads);
   char* ws = static_cast<char*>(x.ws);
   float* scale = (float*)(ws + l.scale);
