@@ -3,18 +3,23 @@
 //
 // With few classes the products are small and what bounds the work is the
 // bytes of H and dH, so each row is read once and everything that it is needed
-// for happens while it is in LDS: scores z = H W^T, the row's softmax and
-// loss, dH = dz W and its share of dW = dz^T H.  A workgroup holds W in LDS and
-// takes blocks of TB rows in turn, the next block's rows on their way to
-// registers meanwhile; dW stays in the accumulators until the end, when each
-// workgroup writes its sum for a second launch to add up in a fixed order.
+// for happens while a workgroup holds it: scores z = H W^T, the row's softmax
+// and loss, dH = dz W and its share of dW = dz^T H.
+//
+// Every wavefront owns DT tiles of 16 columns: it alone reads them of H, with
+// its columns of W in registers for the scores and for dH, and sums its
+// columns of dW in the accumulators over all its rows.  The wavefronts meet
+// only over the scores: each writes its share of the sum over columns to LDS,
+// and reads dz there.  Rows go from global memory to registers (the scores'
+// operand), from there through the wavefront's own LDS to the layout of dW's
+// operand, while the next block's are on their way.  A workgroup's dW is
+// written once, at the end; a second launch adds them up in a fixed order.
 //
 // Products run in fp32 on the matrix cores (16 x 16 x 4) for every type: fp32
 // rows are not rounded anywhere.  A lane's k within a step is free as long as
-// both operands agree on it, so four steps' values come in one 16-byte read:
-// k = 16 i + 4 (lane / 16) + j for step j of group i.  With row strides that
-// are 4 modulo 8 words the same order also keeps the reads along columns
-// (dW) free of bank conflicts.
+// both operands agree on it: k = 16 i + 4 (lane / 16) + j for step j of group i,
+// so that a lane's four steps are one 16-byte read.  Strides that are 4 modulo
+// 16 words keep both directions of reading free of bank conflicts.
 #include "xent.h"
 
 #include <algorithm>
@@ -28,10 +33,9 @@ namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int THREADS = 512, WAVES = 8;
+constexpr int ROWS = 32;            // of a block
 constexpr int COUNT_BLOCK = 1024;   // labels a workgroup of k_count looks at, at least
 constexpr int MAX_COUNTS = 256;
-constexpr int64_t LDS_BYTES = 160 * 1024;
 
 struct Few {
   Mat H, W, dH;
@@ -63,30 +67,40 @@ __global__ __launch_bounds__(256) void k_count(const void* labels, int i64, int6
   }
 }
 
-// Words of LDS: W, a block of H, partial scores, dz.
-constexpr int words(int VT, int TB, int Dp) {
-  return (VT * 16 + TB) * (Dp + 4) + (WAVES / (TB / 16) + 1) * TB * (VT * 16 + 4);
+// Sums and maxima over rows of 16 lanes, in every lane (rotations within the
+// row, no LDS).
+template <int CTRL>
+__device__ __forceinline__ float rotated(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float row_sum(float x) {
+  x += rotated<0x128>(x);
+  x += rotated<0x124>(x);
+  x += rotated<0x122>(x);
+  return x + rotated<0x121>(x);
+}
+__device__ __forceinline__ float row_max(float x) {
+  x = fmaxf(x, rotated<0x128>(x));
+  x = fmaxf(x, rotated<0x124>(x));
+  x = fmaxf(x, rotated<0x122>(x));
+  return fmaxf(x, rotated<0x121>(x));
 }
 
-// VT tiles of 16 classes, DT tiles of 16 columns a wavefront, TB rows a block.
-template <int VT, int DT, int TB, bool GRAD>
-__global__ __launch_bounds__(THREADS, 2) void k_few(Few a) {
-  constexpr int Vp = VT * 16, ZS = Vp + 4;         // classes; stride of score rows
-  constexpr int RT = TB / 16, KS = WAVES / RT;     // row tiles, shares of k
-  constexpr int PF = TB * DT / 16;                 // 4-column chunks a thread fetches
-  constexpr int PER = THREADS / TB, CW = Vp / PER; // threads and classes a thread of a row
-  extern __shared__ __attribute__((aligned(16))) float lds[];
-  const int Dp = a.Dp, HS = Dp + 4;
-  float* const w = lds;                            // [Vp][HS]
-  float* const h = w + Vp * HS;                    // [TB][HS]
-  float* const z = h + TB * HS;                    // [KS][TB][ZS]
-  float* const dz = z + KS * TB * ZS;              // [TB][ZS]
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n16 = lane & 15, q = lane >> 4;
-  const int64_t T = a.H.rows;
-  const int D = a.D, V = a.V, groups = Dp / 16;
-
-  // what dz is multiplied with
+// VT tiles of 16 classes, DT tiles of 16 columns to each of WAVES wavefronts.
+// Two wavefronts a SIMD: two workgroups of four a CU, whose meetings do not
+// coincide, where their registers hold VT DT <= 12 tiles, else one of eight.
+template <int VT, int DT, int WAVES, bool GRAD>
+__global__ __launch_bounds__(WAVES * 64, 2) void k_few(Few a) {
+  constexpr int THREADS = WAVES * 64, TB = ROWS, RT = TB / 16, ZS = VT * 16 + 4, HS = DT * 16 + 4;
+  __shared__ __attribute__((aligned(16))) float z[WAVES][TB][ZS];
+  __shared__ __attribute__((aligned(16))) float dz[TB][ZS];
+  __shared__ __attribute__((aligned(16))) float hall[GRAD ? WAVES : 1][TB][HS];
   __shared__ int total;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n16 = lane & 15, q = lane >> 4;
+  float(*const h)[HS] = hall[GRAD ? wave : 0];
+  const int64_t T = a.H.rows;
+  const int D = a.D, V = a.V;
+
   if (wave == 0) {
     int c = 0;
     for (int i = lane; i < a.ncounts; i += 64) c += a.counts[i];
@@ -94,50 +108,49 @@ __global__ __launch_bounds__(THREADS, 2) void k_few(Few a) {
     for (int o = 1; o < 64; o <<= 1) c += __shfl_xor(c, o);
     if (lane == 0) total = c;
   }
-  for (int i = tid; i < Vp * (Dp / 4); i += THREADS) {
-    const int r = i / (Dp / 4), c = (i - r * (Dp / 4)) * 4;
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      w[r * HS + c + k] = r < V && c + k < D ? load1(a.W.data, a.W.type, (int64_t)r * a.W.ld + c + k) : 0.f;
-  }
   __syncthreads();
   const double div = a.mean ? (double)(total > 0 ? total : 1) : 1.0;
-  const float scale = (float)(a.grad_scale / div);
+  const float scale = (float)(a.grad_scale / div);  // what dz is multiplied with
   if (blockIdx.x == 0 && tid == 0) *a.scale = scale;
 
-  // W as dH's operand stays in registers: columns of this wavefront's tiles
-  float wk[GRAD ? DT : 1][VT][4];
+  // this wavefront's columns of W, for the scores (class n16, columns 4 q ...)
+  // and for dH (classes 16 i + 4 q + j, column n16)
+  const int c0 = wave * DT * 16;
+  auto w = [&](int v, int c) { return v < V && c < D ? load1(a.W.data, a.W.type, (int64_t)v * a.W.ld + c) : 0.f; };
+  float wn[VT][DT][4], wk[GRAD ? DT : 1][VT][4];
   f32x4 acc[GRAD ? VT : 1][DT];
-  if constexpr (GRAD) {
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
+  for (int v = 0; v < VT; ++v)
 #pragma unroll
-      for (int i = 0; i < VT; ++i) {
-        const int tile = wave + d * WAVES;
+    for (int d = 0; d < DT; ++d) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) wk[d][i][j] = tile < groups ? w[(16 * i + 4 * q + j) * HS + tile * 16 + n16] : 0.f;
-        acc[i][d] = f32x4{0.f, 0.f, 0.f, 0.f};
-      }
-  }
-
-  // this thread's chunks of a block of H
-  const int per_row = Dp / 4;
-  float next[PF][4];
-  auto fetch = [&](int64_t t0) {
+      for (int j = 0; j < 4; ++j) wn[v][d][j] = w(v * 16 + n16, c0 + d * 16 + 4 * q + j);
+      if constexpr (GRAD) {
 #pragma unroll
-    for (int e = 0; e < PF; ++e) {
-      const int i = e * THREADS + tid, r = i / per_row, c = (i - r * per_row) * 4;
-      const int64_t t = t0 + r, at = t * a.H.ld + c;
-      const bool in = r < TB && t < T;
-      if (in && c + 4 <= D) {
-        if (a.H.type == DT_F32) load4<DT_F32>(a.H.data, at, next[e]);
-        else if (a.H.type == DT_BF16) load4<DT_BF16>(a.H.data, at, next[e]);
-        else load4<DT_F16>(a.H.data, at, next[e]);
-      } else {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) next[e][k] = in && c + k < D ? load1(a.H.data, a.H.type, at + k) : 0.f;
+        for (int j = 0; j < 4; ++j) wk[d][v][j] = w(16 * v + 4 * q + j, c0 + d * 16 + n16);
+        acc[v][d] = f32x4{0.f, 0.f, 0.f, 0.f};
       }
     }
+
+  // rows n16 of each row tile, columns 4 q ... of each column tile
+  float x[RT][DT][4];
+  auto fetch = [&](int64_t t0) {
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        const int64_t t = t0 + rt * 16 + n16;
+        const int c = c0 + d * 16 + 4 * q;
+        const int64_t at = t * a.H.ld + c;
+        if (t < T && c + 4 <= D) {
+          if (a.H.type == DT_F32) load4<DT_F32>(a.H.data, at, x[rt][d]);
+          else if (a.H.type == DT_BF16) load4<DT_BF16>(a.H.data, at, x[rt][d]);
+          else load4<DT_F16>(a.H.data, at, x[rt][d]);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) x[rt][d][k] = t < T && c + k < D ? load1(a.H.data, a.H.type, at + k) : 0.f;
+        }
+      }
   };
 
   const int64_t blocks = (T + TB - 1) / TB;
@@ -146,72 +159,67 @@ __global__ __launch_bounds__(THREADS, 2) void k_few(Few a) {
   if (b < blocks) fetch(b * TB);
   for (; b < blocks; b += gridDim.x) {
     const int64_t t0 = b * TB;
+    // scores over this wavefront's columns
 #pragma unroll
-    for (int e = 0; e < PF; ++e) {
-      const int i = e * THREADS + tid, r = i / per_row, c = (i - r * per_row) * 4;
-      if (r < TB) *reinterpret_cast<f32x4*>(h + r * HS + c) = f32x4{next[e][0], next[e][1], next[e][2], next[e][3]};
-    }
-    __syncthreads();
-    if (b + gridDim.x < blocks) fetch((b + gridDim.x) * TB);
-
-    {  // scores of 16 rows over this wavefront's share of k
-      const int rt = wave % RT, ks = wave / RT;
-      const int i0 = groups * ks / KS, i1 = groups * (ks + 1) / KS;
+    for (int rt = 0; rt < RT; ++rt) {
       f32x4 s[VT];
 #pragma unroll
       for (int v = 0; v < VT; ++v) s[v] = f32x4{0.f, 0.f, 0.f, 0.f};
-      for (int i = i0; i < i1; ++i) {
-        const f32x4 x = *reinterpret_cast<const f32x4*>(h + (rt * 16 + n16) * HS + 16 * i + 4 * q);
 #pragma unroll
-        for (int v = 0; v < VT; ++v) {
-          const f32x4 y = *reinterpret_cast<const f32x4*>(w + (v * 16 + n16) * HS + 16 * i + 4 * q);
+      for (int d = 0; d < DT; ++d)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) s[v] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], y[j], s[v], 0, 0, 0);
-        }
-      }
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int v = 0; v < VT; ++v)
+            s[v] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[rt][d][j], wn[v][d][j], s[v], 0, 0, 0);
 #pragma unroll
       for (int v = 0; v < VT; ++v)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) z[(ks * TB + rt * 16 + 4 * q + r) * ZS + v * 16 + n16] = s[v][r];
+        for (int r = 0; r < 4; ++r) z[wave][rt * 16 + 4 * q + r][v * 16 + n16] = s[v][r];
+      if constexpr (GRAD) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+          *reinterpret_cast<f32x4*>(&h[rt * 16 + n16][d * 16 + 4 * q]) =
+              f32x4{x[rt][d][0], x[rt][d][1], x[rt][d][2], x[rt][d][3]};
+      }
     }
+    if (b + gridDim.x < blocks) fetch((b + gridDim.x) * TB);
     __syncthreads();
 
-    {  // softmax and loss: PER threads a row, CW classes each
-      const int r = tid / PER, p = tid % PER;
+    // softmax and loss: 16 threads a row
+#pragma unroll
+    for (int r = tid >> 4; r < TB; r += THREADS / 16) {
+      const int p = tid & 15;
       const int64_t t = t0 + r;
       const int64_t label = t < T ? label_at(a.labels, a.i64, t) : -1;
       const bool there = label >= 0 && label < V;
-      float x[CW], top = -INFINITY, target = 0.f;
+      float y[VT], top = -INFINITY, target = 0.f;
 #pragma unroll
-      for (int k = 0; k < CW; ++k) {
-        const int v = p + k * PER;
+      for (int k = 0; k < VT; ++k) {
+        const int v = p + k * 16;
         float s = 0.f;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) s += z[(ks * TB + r) * ZS + v];
-        x[k] = v < V ? s : -INFINITY;
-        top = fmaxf(top, x[k]);
+        for (int w = 0; w < WAVES; ++w) s += z[w][r][v];
+        y[k] = v < V ? s : -INFINITY;
+        top = fmaxf(top, y[k]);
         if (v == label) target = s;
       }
-#pragma unroll
-      for (int o = 1; o < PER; o <<= 1) {
-        top = fmaxf(top, __shfl_xor(top, o));
-        target += __shfl_xor(target, o);
-      }
+      top = row_max(top);
+      target = row_sum(target);
       const float top2 = top * LOG2E, from = top2 == -INFINITY ? 0.f : top2;
       float sum = 0.f;
 #pragma unroll
-      for (int k = 0; k < CW; ++k) {
-        x[k] = exp2_fast(fmaf(x[k], LOG2E, -from));
-        sum += x[k];
+      for (int k = 0; k < VT; ++k) {
+        y[k] = exp2_fast(fmaf(y[k], LOG2E, -from));
+        sum += y[k];
       }
-#pragma unroll
-      for (int o = 1; o < PER; o <<= 1) sum += __shfl_xor(sum, o);
+      sum = row_sum(sum);
       if constexpr (GRAD) {
         const float inv = 1.f / sum;
 #pragma unroll
-        for (int k = 0; k < CW; ++k) {
-          const int v = p + k * PER;
-          dz[r * ZS + v] = there && v < V ? x[k] * inv - (v == label ? 1.f : 0.f) : 0.f;
+        for (int k = 0; k < VT; ++k) {
+          const int v = p + k * 16;
+          dz[r][v] = there && v < V ? y[k] * inv - (v == label ? 1.f : 0.f) : 0.f;
         }
       }
       if (p == 0 && t < T) {
@@ -223,64 +231,70 @@ __global__ __launch_bounds__(THREADS, 2) void k_few(Few a) {
     __syncthreads();
 
     if constexpr (GRAD) {
+      // dH, 16 columns by 16 rows: four columns of a row a lane
 #pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        const int tile = wave + d * WAVES;
-        if (tile >= groups) continue;
-        // dH, 16 columns by 16 rows: four columns of a row a lane
-        const int c = tile * 16 + 4 * q;
+      for (int rt = 0; rt < RT; ++rt) {
+        f32x4 o[DT];
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-          f32x4 o = {0.f, 0.f, 0.f, 0.f};
+        for (int d = 0; d < DT; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int i = 0; i < VT; ++i) {
-            const f32x4 y = *reinterpret_cast<const f32x4*>(dz + (rt * 16 + n16) * ZS + 16 * i + 4 * q);
+        for (int i = 0; i < VT; ++i) {
+          const f32x4 y = *reinterpret_cast<const f32x4*>(&dz[rt * 16 + n16][16 * i + 4 * q]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) o = __builtin_amdgcn_mfma_f32_16x16x4f32(wk[d][i][j], y[j], o, 0, 0, 0);
-          }
-          const int64_t t = t0 + rt * 16 + n16;
-          if (t < T) {
-            const float x[4] = {o[0] * scale, o[1] * scale, o[2] * scale, o[3] * scale};
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(wk[d][i][j], y[j], o[d], 0, 0, 0);
+        }
+        const int64_t t = t0 + rt * 16 + n16;
+        if (t < T) {
+#pragma unroll
+          for (int d = 0; d < DT; ++d) {
+            const int c = c0 + d * 16 + 4 * q;
+            const float y[4] = {o[d][0] * scale, o[d][1] * scale, o[d][2] * scale, o[d][3] * scale};
             const int64_t at = t * a.dH.ld + c;
             if (c + 4 <= D) {
-              if (a.dH.type == DT_F32) store4<DT_F32>(a.dH.data, at, x);
-              else if (a.dH.type == DT_BF16) store4<DT_BF16>(a.dH.data, at, x);
-              else store4<DT_F16>(a.dH.data, at, x);
+              if (a.dH.type == DT_F32) store4<DT_F32>(a.dH.data, at, y);
+              else if (a.dH.type == DT_BF16) store4<DT_BF16>(a.dH.data, at, y);
+              else store4<DT_F16>(a.dH.data, at, y);
             } else {
 #pragma unroll
               for (int k = 0; k < 4; ++k)
-                if (c + k < D) store1(a.dH.data, a.dH.type, at + k, x[k]);
+                if (c + k < D) store1(a.dH.data, a.dH.type, at + k, y[k]);
             }
           }
         }
-        // dW
-#pragma unroll
-        for (int i = 0; i < RT; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int k = 16 * i + 4 * q + j;
-            const float y = h[k * HS + tile * 16 + n16];
-#pragma unroll
-            for (int v = 0; v < VT; ++v)
-              acc[v][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(dz[k * ZS + v * 16 + n16], y, acc[v][d], 0, 0, 0);
-          }
       }
-      __syncthreads();  // h and dz are free
+      // dW
+#pragma unroll
+      for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int k = 16 * i + 4 * q + j;
+          float y[VT];
+#pragma unroll
+          for (int v = 0; v < VT; ++v) y[v] = dz[k][v * 16 + n16];
+#pragma unroll
+          for (int d = 0; d < DT; ++d) {
+            const float g = h[k][d * 16 + n16];
+#pragma unroll
+            for (int v = 0; v < VT; ++v) acc[v][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(y[v], g, acc[v][d], 0, 0, 0);
+          }
+        }
     }
   }
 
   if constexpr (GRAD) {
-    float* part = a.part + (int64_t)blockIdx.x * V * Dp;
+    float* part = a.part + (int64_t)blockIdx.x * V * a.Dp;
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
-      const int tile = wave + d * WAVES;
-      if (tile >= groups) continue;
+      const int c = c0 + d * 16 + n16;
+      if (c >= a.Dp) continue;
 #pragma unroll
       for (int v = 0; v < VT; ++v)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int row = v * 16 + 4 * q + r;
-          if (row < V) part[(int64_t)row * Dp + tile * 16 + n16] = acc[v][d][r];
+          if (row < V) part[(int64_t)row * a.Dp + c] = acc[v][d][r];
         }
     }
   }
@@ -313,20 +327,20 @@ __global__ __launch_bounds__(THREADS, 2) void k_few(Few a) {
 
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
-// Whether a block of TB rows fits LDS next to W and the kernel's own arrays,
-// and the registers (64 rows of more than 384 columns do not).
-constexpr bool fits(int VT, int TB, int Dp) {
-  return (TB == 32 || Dp <= 384) && (int64_t)words(VT, TB, Dp) * 4 + THREADS * 8 + 64 <= LDS_BYTES;
+// Tiles of 16 columns a wavefront and wavefronts of a workgroup.
+struct Shape {
+  int DT, waves;
+};
+
+Shape shape_of(int64_t D, int64_t V) {
+  const int VT = (int)((V + 15) / 16), tiles = (int)((D + 15) / 16), DT = (tiles + 3) / 4;
+  if (DT <= 4 && VT * DT <= 12) return {DT, 4};
+  return {(tiles + 7) / 8, 8};
 }
 
-// Rows a block: 64, or 32 where a wider W leaves no room for more; 0: neither.
-int rows_of(int64_t D, int64_t V) {
-  if (V > 64 || D > 512) return 0;
-  const int VT = (int)((V + 15) / 16), Dp = (int)up(D, 16);
-  return fits(VT, 64, Dp) ? 64 : fits(VT, 32, Dp) ? 32 : 0;
+int64_t groups_of(int64_t T, int64_t D, int64_t V) {
+  return std::max<int64_t>(1, std::min<int64_t>(shape_of(D, V).waves == 4 ? 512 : 256, (T + ROWS - 1) / ROWS));
 }
-
-int64_t groups_of(int64_t T, int TB) { return std::max<int64_t>(1, std::min<int64_t>(256, (T + TB - 1) / TB)); }
 
 struct Layout {
   int64_t counts, ticket, scale, rows, sums, part, bytes;
@@ -340,7 +354,7 @@ Layout layout_of(int64_t T, int64_t D, int64_t V, bool grads) {
     at = up(at + n, 256);
     return here;
   };
-  const int64_t g = groups_of(T, rows_of(D, V));
+  const int64_t g = groups_of(T, D, V);
   l.counts = take(4 * MAX_COUNTS);
   l.ticket = take(4);
   l.scale = take(4);
@@ -351,46 +365,31 @@ Layout layout_of(int64_t T, int64_t D, int64_t V, bool grads) {
   return l;
 }
 
-template <int VT, int DT, int TB>
-hipError_t launch(const Few& f, unsigned grid, bool grads, hipStream_t s) {
-  // widths of DT tiles a wavefront: from the first to `most`, where rows_of gives TB
-  constexpr int first = (DT - 1) * WAVES * 16 + 16, most = DT * WAVES * 16;
-  if constexpr (fits(VT, TB, first) && (TB == 64 || !fits(VT, 64, most))) {
-    const int bytes = words(VT, TB, f.Dp) * 4;
-    auto run = [&](auto kernel) {
-      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
-                                               hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-      if (e != hipSuccess) return e;
-      kernel<<<grid, THREADS, bytes, s>>>(f);
-      return hipGetLastError();
-    };
-    return grads ? run(k_few<VT, DT, TB, true>) : run(k_few<VT, DT, TB, false>);
+template <int VT, int DT, int WAVES>
+void launch(const Few& f, unsigned grid, bool grads, hipStream_t s) {
+  if (grads) k_few<VT, DT, WAVES, true><<<grid, WAVES * 64, 0, s>>>(f);
+  else k_few<VT, DT, WAVES, false><<<grid, WAVES * 64, 0, s>>>(f);
+}
+
+template <int VT>
+void launch(const Few& f, unsigned grid, bool grads, hipStream_t s) {
+  const Shape sh = shape_of(f.D, f.V);
+  if (sh.waves == 4) {
+    if (sh.DT == 1) launch<VT, 1, 4>(f, grid, grads, s);
+    else if (sh.DT == 2) launch<VT, 2, 4>(f, grid, grads, s);
+    else if (sh.DT == 3) launch<VT, 3, 4>(f, grid, grads, s);
+    else if constexpr (VT <= 3) launch<VT, 4, 4>(f, grid, grads, s);
   } else {
-    return hipErrorInvalidConfiguration;  // no width comes here
+    if constexpr (VT == 4)
+      if (sh.DT == 2) launch<VT, 2, 8>(f, grid, grads, s);  // (fewer classes: four wavefronts)
+    if (sh.DT == 3) launch<VT, 3, 8>(f, grid, grads, s);
+    else if (sh.DT == 4) launch<VT, 4, 8>(f, grid, grads, s);
   }
-}
-
-template <int VT, int TB>
-hipError_t launch(const Few& f, unsigned grid, bool grads, hipStream_t s) {
-  const int DT = (f.Dp / 16 + WAVES - 1) / WAVES;
-  return DT == 1   ? launch<VT, 1, TB>(f, grid, grads, s)
-         : DT == 2 ? launch<VT, 2, TB>(f, grid, grads, s)
-         : DT == 3 ? launch<VT, 3, TB>(f, grid, grads, s)
-                   : launch<VT, 4, TB>(f, grid, grads, s);
-}
-
-template <int TB>
-hipError_t launch(const Few& f, unsigned grid, bool grads, hipStream_t s) {
-  const int VT = (f.V + 15) / 16;
-  return VT == 1   ? launch<1, TB>(f, grid, grads, s)
-         : VT == 2 ? launch<2, TB>(f, grid, grads, s)
-         : VT == 3 ? launch<3, TB>(f, grid, grads, s)
-                   : launch<4, TB>(f, grid, grads, s);
 }
 
 }  // namespace
 
-bool xent_few_fits(int64_t T, int64_t D, int64_t V) { return T > 0 && rows_of(D, V) > 0; }
+bool xent_few_fits(int64_t T, int64_t D, int64_t V) { return T > 0 && V <= 64 && D <= 512; }
 
 int64_t xent_few_workspace(int64_t T, int64_t D, int64_t V, bool grads) { return layout_of(T, D, V, grads).bytes; }
 
@@ -411,10 +410,12 @@ hipError_t xent_few(const XentArgs& x, hipStream_t s) {
   f.part = grads ? (float*)(ws + l.part) : nullptr;
   f.D = (int)D; f.V = (int)V; f.Dp = (int)up(D, 16);
   k_count<<<(unsigned)f.ncounts, 256, 0, s>>>(x.labels, x.labels_i64, T, V, (int*)(ws + l.counts), f.ticket);
-  const int TB = rows_of(D, V);
-  const unsigned grid = (unsigned)groups_of(T, TB);
-  const hipError_t e = TB == 64 ? launch<64>(f, grid, grads, s) : launch<32>(f, grid, grads, s);
-  if (e != hipSuccess) return e;
+  const unsigned grid = (unsigned)groups_of(T, D, V);
+  const int VT = (f.V + 15) / 16;
+  if (VT == 1) launch<1>(f, grid, grads, s);
+  else if (VT == 2) launch<2>(f, grid, grads, s);
+  else if (VT == 3) launch<3>(f, grid, grads, s);
+  else launch<4>(f, grid, grads, s);
   if (grads) finish(f.part, (int)grid, V, D, f.Dp, f.scale, x.dW.data, x.dW.type, x.dW.ld, s);
   return hipGetLastError();
 }
