@@ -237,27 +237,36 @@ __global__ __launch_bounds__(BLOCK) void k_adamw_8(Table tab) {
       }
     }
   }
+  float m[PER][4], v[PER][4], big = 0.f;
 #pragma unroll
   for (int q = 0; q < PER; ++q) {
-    float m[4], v[4];
-    decode<false>(cm[q], sm[q], m);
-    decode<true>(cv[q], sv[q], v);
+    decode<false>(cm[q], sm[q], m[q]);
+    decode<true>(cv[q], sv[q], v[q]);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) update(tab.o, g[q][j], p[q][j], m[j], v[j]);
-    const float bm = block_max(m), bv = block_max(v);
-    const bool um = bm >= TINY, uv = bv >= TINY;
-    sm[q] = um ? bm / TOP_M : 0.f;
-    sv[q] = uv ? bv / TOP_V : 0.f;
-    const float im = um ? TOP_M / bm : 0.f, iv = uv ? TOP_V / bv : 0.f;
+    for (int j = 0; j < 4; ++j) update(tab.o, g[q][j], p[q][j], m[q][j], v[q][j]);
+    // lane 2 q keeps block q's largest first moment, lane 2 q + 1 its second
+    const float bm = block_max(m[q]), bv = block_max(v[q]);
+    big = lane == 2 * q ? bm : lane == 2 * q + 1 ? bv : big;
+  }
+  // all scales and their inverses at once: the divisions are what they cost
+  const bool used = big >= TINY;
+  const float top = lane & 1 ? TOP_V : TOP_M;
+  const float scale = used ? big / top : 0.f, inverse = used ? top / big : 0.f;
+  auto of = [](float x, int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), l)); };
+#pragma unroll
+  for (int q = 0; q < PER; ++q) {
+    const float im = of(inverse, 2 * q), iv = of(inverse, 2 * q + 1);
+    sm[q] = of(scale, 2 * q);
+    sv[q] = of(scale, 2 * q + 1);
     const uint32_t x0 = (uint32_t)(i0 + q * BLOCK) * kIndexStep + t.seed;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const uint32_t r = noise(x0 + j * kIndexStep);
-      m[j] = round_code<false>(m[j] * im, r & 0xffffu);
-      v[j] = round_code<true>(v[j] * iv, r >> 16);
+      m[q][j] = round_code<false>(m[q][j] * im, r & 0xffffu);
+      v[q][j] = round_code<true>(v[q][j] * iv, r >> 16);
     }
-    cm[q] = encode<false>(m);
-    cv[q] = encode<true>(v);
+    cm[q] = encode<false>(m[q]);
+    cv[q] = encode<true>(v[q]);
   }
   if (whole) {
 #pragma unroll

@@ -75,6 +75,39 @@ __device__ __forceinline__ T wave_sum(T v) {
   return wave_last(wave_incl_scan(v));
 }
 
+// x of the lane that CTRL names: quad_perm 0xB1 and 0x4E exchange lanes 1 and 2
+// apart, row_half_mirror 0x141 the quads of 8 lanes, row_mirror 0x140 the
+// halves of 16 (quads and halves that hold one value each).
+template <int CTRL>
+__device__ __forceinline__ float dpp_f32(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, false));
+}
+
+// fp32 sum over groups of W lanes, in every lane.
+template <int W>
+__device__ __forceinline__ float group_sum_f32(float v) {
+  static_assert(W == 8 || W == 16 || W == 32 || W == 64, "lanes of a group");
+  v += dpp_f32<0xB1>(v);
+  v += dpp_f32<0x4E>(v);
+  v += dpp_f32<0x141>(v);
+  if constexpr (W >= 16) v += dpp_f32<0x140>(v);
+  if constexpr (W == 32) v += __shfl_xor(v, 16);
+  if constexpr (W == 64) {  // one lane of each row of 16
+    const int x = __float_as_int(v);
+    v = (__int_as_float(__builtin_amdgcn_readlane(x, 0)) + __int_as_float(__builtin_amdgcn_readlane(x, 16))) +
+        (__int_as_float(__builtin_amdgcn_readlane(x, 32)) + __int_as_float(__builtin_amdgcn_readlane(x, 48)));
+  }
+  return v;
+}
+
+// fp32 maximum over groups of 16 lanes, in every lane.
+__device__ __forceinline__ float group16_max_f32(float v) {
+  v = fmaxf(v, dpp_f32<0xB1>(v));
+  v = fmaxf(v, dpp_f32<0x4E>(v));
+  v = fmaxf(v, dpp_f32<0x141>(v));
+  return fmaxf(v, dpp_f32<0x140>(v));
+}
+
 // fp32 sum over the wavefront, in every lane (butterfly over lane pairs).
 __device__ __forceinline__ float wave_sum_f32(float v) {
 #pragma unroll

@@ -18,6 +18,7 @@
 #include <algorithm>
 
 #include "dense.h"
+#include "device.h"
 
 namespace aires {
 namespace kern {
@@ -43,19 +44,12 @@ struct Args {
   int64_t m; int n; float eps, inv_n;
 };
 
-template <int W>
-__device__ __forceinline__ float lanes_sum(float v) {
-#pragma unroll
-  for (int o = 1; o < W; o <<= 1) v += __shfl_xor(v, o);
-  return v;
-}
-
 // Sums of K values over a team, in every lane.  L = 0: over the workgroup,
 // through `buf` (two halves used in turn, so one barrier a call is enough).
 template <int L, int K>
 __device__ __forceinline__ void team_sum(float (&v)[K], float* buf, int& turn) {
 #pragma unroll
-  for (int k = 0; k < K; ++k) v[k] = lanes_sum<L == 0 ? 64 : L>(v[k]);
+  for (int k = 0; k < K; ++k) v[k] = group_sum_f32<L == 0 ? 64 : L>(v[k]);
   if constexpr (L == 0) {
     const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     float* b = buf + (turn & 1) * (2 * (MAX_BLOCK / 64));
@@ -331,24 +325,25 @@ __global__ __launch_bounds__(TEAM_BLOCK) void k_ln_columns_wide(Args a) {
   a.part[((int64_t)blockIdx.y * 2 + 1) * a.n + c] = sb;
 }
 
-// dgamma and dbeta: the workgroups' partial sums, 64 of them side by side
-// for 16 columns, added in a fixed order.  count = 0 writes zeros.
+// dgamma and dbeta: the workgroups' partial sums, 32 shares of them side by
+// side for 32 columns, added in a fixed order.  count = 0 writes zeros.
 __global__ __launch_bounds__(1024) void k_ln_columns(const float* part, int64_t count, int n, void* dgamma,
                                                      void* dbeta, int wt) {
-  __shared__ float buf[64][17];
-  const int c = threadIdx.x & 15, w = threadIdx.x >> 4;
-  const int64_t col = (int64_t)blockIdx.x * 16 + c;
+  __shared__ float buf[32][33];
+  const int c = threadIdx.x & 31, w = threadIdx.x >> 5;
+  const int64_t col = (int64_t)blockIdx.x * 32 + c;
   const int which = blockIdx.y;
   float v = 0.f;
   if (col < n) {
-#pragma unroll 4
-    for (int64_t i = w; i < count; i += 64) v += part[(i * 2 + which) * n + col];
+#pragma unroll 8
+    for (int64_t i = w; i < count; i += 32) v += part[(i * 2 + which) * n + col];
   }
   buf[w][c] = v;
   __syncthreads();
   if (w == 0 && col < n) {
     v = 0.f;
-    for (int i = 0; i < 64; ++i) v += buf[i][c];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v += buf[i][c];
     void* dst = which ? dbeta : dgamma;
     if (dst) store1(dst, wt, col, v);
   }
@@ -432,7 +427,7 @@ hipError_t layer_norm_backward(const Mat& dY, const Mat& X, const float* mean, c
                                int wt, const Mat& dX, void* dgamma, void* dbeta, float* ws, hipStream_t s) {
   const bool weights = dgamma || dbeta;
   const int n = (int)X.cols;
-  const dim3 cgrid((unsigned)((n + 15) / 16), 2);
+  const dim3 cgrid((unsigned)((n + 31) / 32), 2);
   if (n == 0 || (X.rows == 0 && !weights)) return hipSuccess;
   if (X.rows == 0) {
     k_ln_columns<<<cgrid, 1024, 0, s>>>(nullptr, 0, n, dgamma, dbeta, wt);

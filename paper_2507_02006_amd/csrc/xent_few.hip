@@ -67,25 +67,6 @@ __global__ __launch_bounds__(256) void k_count(const void* labels, int i64, int6
   }
 }
 
-// Sums and maxima over rows of 16 lanes, in every lane (rotations within the
-// row, no LDS).
-template <int CTRL>
-__device__ __forceinline__ float rotated(float x) {
-  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, false));
-}
-__device__ __forceinline__ float row_sum(float x) {
-  x += rotated<0x128>(x);
-  x += rotated<0x124>(x);
-  x += rotated<0x122>(x);
-  return x + rotated<0x121>(x);
-}
-__device__ __forceinline__ float row_max(float x) {
-  x = fmaxf(x, rotated<0x128>(x));
-  x = fmaxf(x, rotated<0x124>(x));
-  x = fmaxf(x, rotated<0x122>(x));
-  return fmaxf(x, rotated<0x121>(x));
-}
-
 // VT tiles of 16 classes, DT tiles of 16 columns to each of WAVES wavefronts.
 // Two wavefronts a SIMD: two workgroups of four a CU, whose meetings do not
 // coincide, where their registers hold VT DT <= 12 tiles, else one of eight.
@@ -204,8 +185,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_few(Few a) {
         top = fmaxf(top, y[k]);
         if (v == label) target = s;
       }
-      top = row_max(top);
-      target = row_sum(target);
+      top = group16_max_f32(top);
+      target = group_sum_f32<16>(target);
       const float top2 = top * LOG2E, from = top2 == -INFINITY ? 0.f : top2;
       float sum = 0.f;
 #pragma unroll
@@ -213,7 +194,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_few(Few a) {
         y[k] = exp2_fast(fmaf(y[k], LOG2E, -from));
         sum += y[k];
       }
-      sum = row_sum(sum);
+      sum = group_sum_f32<16>(sum);
       if constexpr (GRAD) {
         const float inv = 1.f / sum;
 #pragma unroll
