@@ -10,7 +10,7 @@ LIB = os.path.join(HERE, "libaires.so")
 CALLS = os.path.join(HERE, "_calls.so")  # the training calls over torch tensors
 SOURCES = [os.path.join(HERE, "csrc", n) for n in
            ("aires.cpp", "train.cpp", "kernels.hip", "narrow.hip", "spmm.hip", "normalize.hip", "scratch.hip",
-            "layernorm.hip", "adamw.hip", "xent.hip", "xent_few.hip")]
+            "layernorm.hip", "adamw.hip", "xent.hip", "xent_few.hip", "xent_rows.hip")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",

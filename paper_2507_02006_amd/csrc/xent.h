@@ -1,5 +1,5 @@
-// Shared by the cross entropy's kernels: xent.hip (any table) and
-// xent_few.hip (few classes).
+// Shared by the cross entropy's kernels: xent.hip (any table),
+// xent_few.hip (few classes) and xent_rows.hip (few rows).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -14,10 +14,21 @@ namespace kern {
 void finish(const float* part, int slices, int64_t rows, int64_t cols, int64_t ldp, const float* scale, void* out,
             int type, int64_t ldo, hipStream_t s);
 
-// Few classes: whether this shape takes that path, its workspace, and the call.
+// Rows' maxima, inverse sums and losses from the statistics [tile][t] of
+// `tiles` tiles of the table, the loss, and *scale = grad_scale / c.  *ticket
+// is 0 before; sums: rows_and_loss_workspace(T) bytes.
+int64_t rows_and_loss_workspace(int64_t T);
+void rows_and_loss(const XentArgs& x, const float2* part, int64_t tiles, float* top, float* inv, float* row_loss,
+                   void* sums, uint32_t* ticket, float grad_scale, float* scale, hipStream_t s);
+
+// Few rows, few classes: whether this shape takes that path, its workspace, and the
+// call.
 bool xent_few_fits(int64_t T, int64_t D, int64_t V);
 int64_t xent_few_workspace(int64_t T, int64_t D, int64_t V, bool grads);
 hipError_t xent_few(const XentArgs& x, hipStream_t s);
+bool xent_rows_fits(int64_t T, int64_t D, int64_t V, int type);
+int64_t xent_rows_workspace(int64_t T, int64_t D, int64_t V, bool grads);
+hipError_t xent_rows(const XentArgs& x, hipStream_t s);
 
 namespace {
 
@@ -28,6 +39,14 @@ __device__ __forceinline__ int64_t label_at(const void* labels, int i64, int64_t
 }
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Joins two (maximum, sum of exponentials) in base 2; equal maxima (of minus
+// infinity too) need no scaling.
+__device__ __forceinline__ void join(float& m, float& s, float m1, float s1) {
+  const float top = fmaxf(m, m1);
+  s = (m == top ? s : s * exp2_fast(m - top)) + (m1 == top ? s1 : s1 * exp2_fast(m1 - top));
+  m = top;
+}
 
 }  // namespace
 }  // namespace kern

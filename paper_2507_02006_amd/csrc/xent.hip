@@ -32,14 +32,6 @@ constexpr int TV = 256;  // table entries of a tile of scores
 constexpr int64_t kPieceBytes = int64_t(256) << 20;  // dz of one piece of the table
 constexpr float F16_UP = 1024.f;       // dz in fp16 is held times this: 2^-35 is its least step
 
-// Joins two (maximum, sum of exponentials) in base 2; equal maxima (of minus
-// infinity too) need no scaling.
-__device__ __forceinline__ void join(float& m, float& s, float m1, float s1) {
-  const float top = fmaxf(m, m1);
-  s = (m == top ? s : s * exp2_fast(m - top)) + (m1 == top ? s1 : s1 * exp2_fast(m1 - top));
-  m = top;
-}
-
 // ---------------------------------------------------------------- operands
 
 // Rows of X as 16-bit planes of `width` columns, zeros past the end.
@@ -319,6 +311,27 @@ __global__ __launch_bounds__(1024) void k_rows(Rows a) {
   }
 }
 
+constexpr int64_t kFewRows = 2048;  // T up to which a workgroup takes 8 rows
+
+}  // namespace
+
+int64_t rows_and_loss_workspace(int64_t T) {
+  const int64_t rows = T <= kFewRows ? 8 : 64;
+  return 16 * std::max<int64_t>(1, (T + rows - 1) / rows);
+}
+
+void rows_and_loss(const XentArgs& x, const float2* part, int64_t tiles, float* top, float* inv, float* row_loss,
+                   void* sums, uint32_t* ticket, float grad_scale, float* scale, hipStream_t s) {
+  const int64_t T = x.H.rows;
+  const Rows rw{x.H, x.W, x.labels, x.labels_i64, part, tiles, top, inv, row_loss, (double2*)sums, ticket, x.mean,
+                grad_scale, scale, x.loss};
+  const unsigned blocks = (unsigned)(rows_and_loss_workspace(T) / 16);
+  if (T <= kFewRows) k_rows<8><<<blocks, 1024, 0, s>>>(rw);
+  else k_rows<64><<<blocks, 1024, 0, s>>>(rw);
+}
+
+namespace {
+
 // --------------------------------------------------------------- gradients
 
 // out(m, n) = scale sum_k A(m, k) B(n, k), in `slices` shares of k.
@@ -470,7 +483,7 @@ unsigned grid_of(int64_t items, int64_t per) {
 // Sizes and places in the workspace.
 struct Layout {
   int64_t width, planes, segs;         // columns of the packed operands
-  int TT, G, rows_at_once;             // tiles; rows of a workgroup of k_rows
+  int TT, G;                           // tiles
   int64_t piece, Tp, ldz;              // table entries of a piece, rows of dz and their stride
   int dh_per, dh_slices, dw_per, dw_slices;
   int64_t ticket, scale, top, inv, rows, sums, part, h, w, dh, dw, dz, bytes;
@@ -494,14 +507,13 @@ Layout layout_of(int64_t T, int64_t D, int64_t V, int type, bool grads) {
   l.planes = type == DT_F32 ? 3 : 1;
   l.segs = type == DT_F32 ? 6 : 1;
   l.TT = T <= 32 ? 32 : T <= 128 ? 128 : 256;
-  l.rows_at_once = T <= 2048 ? 8 : 64;
   l.Tp = up(T, l.TT);
   l.ticket = take(4);
   l.scale = take(4);
   l.top = take(4 * T);
   l.inv = take(4 * T);
   l.rows = take(4 * T);
-  l.sums = take(16 * std::max<int64_t>(1, up(T, l.rows_at_once) / l.rows_at_once));
+  l.sums = take(rows_and_loss_workspace(T));
   l.part = take(8 * T * (up(V, TV) / TV));
   l.h = take(2 * l.planes * T * l.width);
   l.w = take(2 * l.planes * V * l.width);
@@ -556,6 +568,7 @@ void scores(const Scores& sc, int type, int TT, hipStream_t s) {
 
 int64_t linear_xent_workspace(int64_t T, int64_t D, int64_t V, int type, bool grads) {
   if (xent_few_fits(T, D, V)) return xent_few_workspace(T, D, V, grads);
+  if (xent_rows_fits(T, D, V, type)) return xent_rows_workspace(T, D, V, grads);
   return layout_of(T, D, V, type, grads).bytes;
 }
 
@@ -565,6 +578,7 @@ hipError_t linear_xent(const XentArgs& x, hipStream_t s) {
   const int type = x.H.type;
   const bool f16 = type == DT_F16;
   if (xent_few_fits(T, D, V)) return xent_few(x, s);
+  if (xent_rows_fits(T, D, V, type)) return xent_rows(x, s);
   const Layout l = layout_of(T, D, V, type, grads);
   char* ws = static_cast<char*>(x.ws);
   float* scale = (float*)(ws + l.scale);
@@ -580,25 +594,16 @@ hipError_t linear_xent(const XentArgs& x, hipStream_t s) {
     sc.ticket = (uint32_t*)(ws + l.ticket);
     scores<false>(sc, type, l.TT, s);
   }
-  Rows rw{};
-  rw.H = x.H; rw.W = x.W; rw.labels = x.labels; rw.i64 = x.labels_i64;
-  rw.part = sc.part; rw.tiles = up(V, TV) / TV;
-  rw.top = (float*)(ws + l.top); rw.inv = (float*)(ws + l.inv);
-  rw.row_loss = x.row_loss ? x.row_loss : (float*)(ws + l.rows);
-  rw.sums = (double2*)(ws + l.sums);
-  rw.ticket = sc.ticket;
-  rw.mean = x.mean;
-  rw.grad_scale = x.grad_scale * (f16 ? 1.f / F16_UP : 1.f);  // fp16 dz is held times F16_UP
-  rw.scale = scale; rw.loss = x.loss;
-  const unsigned blocks = (unsigned)std::max<int64_t>(1, up(T, l.rows_at_once) / l.rows_at_once);
-  if (l.rows_at_once == 8) k_rows<8><<<blocks, 1024, 0, s>>>(rw);
-  else k_rows<64><<<blocks, 1024, 0, s>>>(rw);
+  float *top = (float*)(ws + l.top), *inv = (float*)(ws + l.inv);
+  // fp16 dz is held times F16_UP
+  rows_and_loss(x, sc.part, up(V, TV) / TV, top, inv, x.row_loss ? x.row_loss : (float*)(ws + l.rows), ws + l.sums,
+                sc.ticket, x.grad_scale * (f16 ? 1.f / F16_UP : 1.f), scale, s);
   if (!grads) return hipGetLastError();
   if (T == 0) {
     if (V > 0 && D > 0) k_zero<<<grid_of(V * D, 1024), 256, 0, s>>>(x.dW.data, type, V, D, x.dW.ld);
     return hipGetLastError();
   }
-  sc.top = rw.top; sc.inv = rw.inv;
+  sc.top = top; sc.inv = inv;
   sc.dz = (uint16_t*)(ws + l.dz);
   sc.ldz = l.ldz;
   sc.plane = l.Tp * l.ldz;

@@ -273,6 +273,22 @@ def test_linear_xent(t, d, v, dt):
     xent_check(aires.linear_xent(H.cuda(), W.cuda(), y.int().cuda(), grads=False), ref, False)
 
 
+@pytest.mark.parametrize("dt", [F32, BF16, F16])
+@pytest.mark.parametrize("t,d,v", [(6, 815, 3001), (2, 9, 5000), (24, 700, 900), (64, 256, 3000), (48, 300, 2000),
+                                   (17, 1024, 1500), (33, 513, 777), (1, 1024, 70), (31, 511, 20000), (64, 512, 65),
+                                   (3000, 800, 4), (777, 1000, 20), (500, 600, 33), (5000, 1024, 16), (40000, 8, 3)])
+def test_linear_xent_few_rows_or_classes(t, d, v, dt):
+    """A short side kept whole, wide rows, rows at odd offsets."""
+    H, W, y = xent_data(t, d, v, dt, 2 * t + d + v)
+    y[0] = v - 1
+    ref = xent_ref(H, W, y)
+    xent_check(aires.linear_xent(H.cuda(), W.cuda(), y.cuda()), ref)
+    wide = torch.full((v, d + 3), float("nan"), dtype=dt, device="cuda")
+    wide[:, 1:d + 1] = W.cuda()
+    xent_check(aires.linear_xent(H.cuda(), wide[:, 1:d + 1], y.int().cuda()), ref)
+    xent_check(aires.linear_xent(H.cuda(), wide[:, 1:d + 1], y.cuda(), grads=False), ref, False)
+
+
 def test_linear_xent_large_table():
     """More of the table than one piece of the workspace holds."""
     t, d, v = 3000, 40, 150001
