@@ -224,22 +224,78 @@ struct Rows {
   float* scale; float* loss;
 };
 
+// Sum over d of H(row, d) W(label, d), LPR lanes a row, in each of them.
+template <int TYPE, int LPR>
+__device__ __forceinline__ float label_score(const Rows& a, int64_t row, int64_t label, int lane) {
+  const int64_t h = row * a.H.ld, w = label * a.W.ld, D = a.H.cols;
+  float s = 0.f;
+#pragma unroll 2
+  for (int64_t d = 4 * lane; d < D; d += 4 * LPR) {
+    float x[4] = {}, y[4] = {};
+    if (d + 4 <= D) {
+      load4<TYPE>(a.H.data, h + d, x);
+      load4<TYPE>(a.W.data, w + d, y);
+    } else {
+      for (int k = 0; d + k < D; ++k) {
+        x[k] = load1<TYPE>(a.H.data, h + d + k);
+        y[k] = load1<TYPE>(a.W.data, w + d + k);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) s = fmaf(x[k], y[k], s);
+  }
+  return group_sum_f32<LPR>(s);
+}
+
+__device__ __forceinline__ double2 wave_sum2(double2 v) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    v.x += __shfl_xor(v.x, o);
+    v.y += __shfl_xor(v.y, o);
+  }
+  return v;
+}
+
+// The workgroups' shares of the loss in a fixed order, by one workgroup.
+template <int THREADS>
+__device__ __forceinline__ void total_loss(const Rows& a, int64_t n) {
+  __shared__ double2 buf[THREADS / 64];
+  double2 v = {0, 0};
+  for (int64_t i = threadIdx.x; i < n; i += THREADS) {
+    v.x += a.sums[i].x;
+    v.y += a.sums[i].y;
+  }
+  v = wave_sum2(v);
+  if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < THREADS / 64; ++i) {
+      v.x += buf[i].x;
+      v.y += buf[i].y;
+    }
+    const double div = a.mean && v.y > 0 ? v.y : 1.0;
+    *a.scale = (float)(a.grad_scale / div);
+    *a.loss = (float)(v.x / div);
+  }
+}
+
+__global__ __launch_bounds__(256) void k_total(Rows a, int64_t n) { total_loss<256>(a, n); }
+
 // Maximum and sum of each row from its tiles', and its loss: ROWS rows a
-// workgroup, 1024 / ROWS threads to a row's tiles, then a wavefront to each
-// row's label score.  The last workgroup to finish adds up the loss, in the
-// order of the workgroups, and what dz is multiplied with.
-template <int ROWS>
-__global__ __launch_bounds__(1024) void k_rows(Rows a) {
-  constexpr int SLICES = 1024 / ROWS, WAVES = 16;
+// workgroup, SLICES threads to a row's tiles, then lanes to each row's label
+// score.  With a ticket the last workgroup to finish adds up the loss.
+template <int ROWS, int SLICES>
+__global__ __launch_bounds__(ROWS * SLICES) void k_rows(Rows a) {
+  constexpr int THREADS = ROWS * SLICES, LPR = SLICES > 64 ? 64 : SLICES < 16 ? 16 : SLICES;
   __shared__ float2 buf[SLICES][ROWS];
   __shared__ float lse[ROWS];
-  __shared__ double2 sums[1024];
+  __shared__ double2 sums[THREADS / 64];
   __shared__ bool last;
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, r = tid % ROWS, slice = tid / ROWS;
+  const int tid = threadIdx.x, r = tid % ROWS, slice = tid / ROWS;
   const int64_t T = a.H.rows, t0 = (int64_t)blockIdx.x * ROWS, t = t0 + r;
   float m = -INFINITY, s = 0.f;
   if (t < T) {
-#pragma unroll 4
+#pragma unroll 8
     for (int64_t i = slice; i < a.tiles; i += SLICES) {
       const float2 p = a.part[i * T + t];
       join(m, s, p.x, p.y);
@@ -260,74 +316,65 @@ __global__ __launch_bounds__(1024) void k_rows(Rows a) {
     lse[r] = (m + log2f(s)) * LN2;
   }
   __syncthreads();
-  double loss = 0, count = 0;
-  for (int i = w; i < ROWS; i += WAVES) {
+  double2 mine = {0, 0};
+  for (int i = tid / LPR; i < ROWS; i += THREADS / LPR) {
     const int64_t row = t0 + i;
     if (row >= T) break;
     const int64_t label = label_at(a.labels, a.i64, row);
     float x = 0.f;
     if (label >= 0 && label < a.W.rows) {
-      for (int64_t d = lane; d < a.H.cols; d += 64)
-        x = fmaf(load1(a.H.data, a.H.type, row * a.H.ld + d), load1(a.W.data, a.W.type, label * a.W.ld + d), x);
-      x = lse[i] - wave_sum_f32(x);
-      loss += x;
-      count += 1;
+      const int l = tid % LPR;
+      x = a.H.type == DT_F32    ? label_score<DT_F32, LPR>(a, row, label, l)
+          : a.H.type == DT_BF16 ? label_score<DT_BF16, LPR>(a, row, label, l)
+                                : label_score<DT_F16, LPR>(a, row, label, l);
+      x = lse[i] - x;
+      if (l == 0) {
+        mine.x += x;
+        mine.y += 1;
+      }
     }
-    if (lane == 0) a.row_loss[row] = x;
+    if (tid % LPR == 0) a.row_loss[row] = x;
   }
-  if (lane == 0) sums[w] = make_double2(loss, count);
+  mine = wave_sum2(mine);
+  if ((tid & 63) == 0) sums[tid >> 6] = mine;
   __syncthreads();
   if (tid == 0) {
-    for (int i = 1; i < WAVES; ++i) {
-      loss += sums[i].x;
-      count += sums[i].y;
+    for (int i = 1; i < THREADS / 64; ++i) {
+      mine.x += sums[i].x;
+      mine.y += sums[i].y;
     }
-    a.sums[blockIdx.x] = make_double2(loss, count);
-    // the sums are visible to whoever draws a later number
+    a.sums[blockIdx.x] = mine;
+    // the share is visible to whoever draws a later number
     last = gridDim.x == 1 ||
-           __hip_atomic_fetch_add(a.ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
+           (a.ticket && __hip_atomic_fetch_add(a.ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1);
   }
   __syncthreads();
   if (!last) return;
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-  loss = count = 0;
-  for (int64_t i = tid; i < (int64_t)gridDim.x; i += 1024) {
-    loss += a.sums[i].x;
-    count += a.sums[i].y;
-  }
-  sums[tid] = make_double2(loss, count);
-  __syncthreads();
-  for (int o = 512; o > 0; o >>= 1) {
-    if (tid < o) {
-      sums[tid].x += sums[tid + o].x;
-      sums[tid].y += sums[tid + o].y;
-    }
-    __syncthreads();
-  }
-  if (tid == 0) {
-    const double div = a.mean && sums[0].y > 0 ? sums[0].y : 1.0;
-    *a.scale = (float)(a.grad_scale / div);
-    *a.loss = (float)(sums[0].x / div);
-  }
+  total_loss<THREADS>(a, gridDim.x);
 }
 
-constexpr int64_t kFewRows = 2048;  // T up to which a workgroup takes 8 rows
+// Rows of a workgroup: 8 with 128 threads each for few rows, 16 with 64 where
+// a row has many tiles, 64 with 4 where it has few.
+int rows_of(int64_t T, int64_t tiles) { return T <= 2048 ? 8 : tiles >= 32 ? 16 : 64; }
 
 }  // namespace
 
-int64_t rows_and_loss_workspace(int64_t T) {
-  const int64_t rows = T <= kFewRows ? 8 : 64;
-  return 16 * std::max<int64_t>(1, (T + rows - 1) / rows);
-}
+int64_t rows_and_loss_workspace(int64_t T) { return 16 * std::max<int64_t>(1, (T + 7) / 8); }
 
 void rows_and_loss(const XentArgs& x, const float2* part, int64_t tiles, float* top, float* inv, float* row_loss,
                    void* sums, uint32_t* ticket, float grad_scale, float* scale, hipStream_t s) {
   const int64_t T = x.H.rows;
-  const Rows rw{x.H, x.W, x.labels, x.labels_i64, part, tiles, top, inv, row_loss, (double2*)sums, ticket, x.mean,
-                grad_scale, scale, x.loss};
-  const unsigned blocks = (unsigned)(rows_and_loss_workspace(T) / 16);
-  if (T <= kFewRows) k_rows<8><<<blocks, 1024, 0, s>>>(rw);
-  else k_rows<64><<<blocks, 1024, 0, s>>>(rw);
+  const int rows = rows_of(T, tiles);
+  const unsigned blocks = (unsigned)std::max<int64_t>(1, (T + rows - 1) / rows);
+  // A ticket costs 20 ns a workgroup, one after the other, another launch 5 us.
+  const bool drawn = blocks <= 128;
+  const Rows rw{x.H, x.W, x.labels, x.labels_i64, part, tiles, top, inv, row_loss, (double2*)sums,
+                drawn ? ticket : nullptr, x.mean, grad_scale, scale, x.loss};
+  if (rows == 8) k_rows<8, 128><<<blocks, 1024, 0, s>>>(rw);
+  else if (rows == 16) k_rows<16, 64><<<blocks, 1024, 0, s>>>(rw);
+  else k_rows<64, 4><<<blocks, 256, 0, s>>>(rw);
+  if (!drawn) k_total<<<1, 256, 0, s>>>(rw, blocks);
 }
 
 namespace {
