@@ -542,6 +542,15 @@ void slices_of(int steps, int64_t ideal, int& per, int& slices) {
   slices = std::max(1, (steps + per - 1) / per);
 }
 
+// Rows of a tile of scores: no more than there are, and as many as still make
+// a tile for every other CU (500 x 2000 scores, 64 columns, f32: the
+// whole call 80 us so, 102 in tiles of 256 rows).
+int score_rows(int64_t T, int64_t V) {
+  for (int TT : {256, 128})
+    if (T > TT / 2 && up(T, TT) / TT * (up(V, TV) / TV) >= 128) return TT;
+  return 32;
+}
+
 Layout layout_of(int64_t T, int64_t D, int64_t V, int type, bool grads) {
   Layout l{};
   int64_t at = 0;
@@ -553,7 +562,7 @@ Layout layout_of(int64_t T, int64_t D, int64_t V, int type, bool grads) {
   l.width = up(D, BK);
   l.planes = type == DT_F32 ? 3 : 1;
   l.segs = type == DT_F32 ? 6 : 1;
-  l.TT = T <= 32 ? 32 : T <= 128 ? 128 : 256;
+  l.TT = score_rows(T, V);
   l.Tp = up(T, l.TT);
   l.ticket = take(4);
   l.scale = take(4);
@@ -571,7 +580,7 @@ Layout layout_of(int64_t T, int64_t D, int64_t V, int type, bool grads) {
     l.G = std::min({T, D, V}) <= 128 ? 128 : 256;
     // shares of k of about equal length, one workgroup (of 256, else two) a CU
     const int64_t nx = up(D, l.G) / l.G, th = up(T, l.G) / l.G * nx, tw = up(std::min(l.piece, V), l.G) / l.G * nx;
-    const int64_t ideal = std::max<int64_t>(8, (th * dh_steps + tw * dw_steps) / (l.G == 256 ? 256 : 512));
+    const int64_t ideal = std::max<int64_t>(l.segs == 1 ? 4 : 2, (th * dh_steps + tw * dw_steps) / (l.G == 256 ? 256 : 512));
     slices_of(dh_steps, ideal, l.dh_per, l.dh_slices);
     slices_of(dw_steps, ideal, l.dw_per, l.dw_slices);
     if (l.dh_slices > 1 || l.piece < V) l.dh = take(4 * l.dh_slices * T * l.width);
