@@ -34,20 +34,15 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 
-// An operand in memory, rows 16-byte aligned, `cols` a multiple of 8.
+// A 16-bit operand in memory, rows 16-byte aligned, `cols` a multiple of 8.
 // K-contiguous: `rows` are m, `cols` k; k past `cols` repeats the row's last
-// chunk (the other operand holds zeros there).  K-major: `rows` are k, `cols` m.  An fp32 operand is three 16-bit planes, `plane` elements apart.
+// chunk (the other operand holds zeros there).  K-major: `rows` are k, `cols` m.
 struct Panel {
   const uint16_t* data;
-  int64_t plane, ld, rows, cols;
+  int64_t ld, rows, cols;
 };
 
 constexpr int BK = 64;  // k of a stage
-
-// Products of planes that make up an fp32 product: all but those below its
-// own rounding (planes 1 and 2, 2 and 2).  Small ones come first.
-__device__ __forceinline__ int plane_a(int seg) { return (0x001102 >> (4 * seg)) & 15; }
-__device__ __forceinline__ int plane_b(int seg) { return (0x010120 >> (4 * seg)) & 15; }
 
 template <bool F16>
 __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
@@ -59,6 +54,22 @@ __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
 
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(1))) void global_void;
+
+// COUNT loads of 1 KB by a wavefront, straight to its part of a stage: a
+// scalar base and a 32-bit offset a lane, so no vector arithmetic a load.
+template <int COUNT>
+__device__ __forceinline__ void load_chunks(const char* base, const uint32_t (&off)[COUNT], char* lds, int wave) {
+  const uint64_t b = reinterpret_cast<uint64_t>(base);
+  const char* from = reinterpret_cast<const char*>(
+      ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(b >> 32)) << 32) |
+      (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)b));
+#pragma unroll
+  for (int j = 0; j < COUNT; ++j) {
+    uint32_t o = off[j];
+    asm("" : "+v"(o));
+    __builtin_amdgcn_global_load_lds((global_void*)(from + o), (lds_void*)(lds + (wave * COUNT + j) * 1024), 16, 0, 0);
+  }
+}
 
 // One operand's share of a stage: SPAN x BK elements, 1 KB an instruction.
 template <int SPAN, int WAVES, bool KMAJOR>
@@ -74,8 +85,8 @@ struct Stager {
   int64_t left;          // k that there are from the next stage's first on
 
   // m0: first m of the tile (m0 < extent of m); k0: first k, a multiple of BK
-  __device__ void init(const Panel& p, int plane, int64_t m0, int64_t k0, int wave, int lane) {
-    const char* d = reinterpret_cast<const char*>(p.data + plane * p.plane);
+  __device__ void init(const Panel& p, int64_t m0, int64_t k0, int wave, int lane) {
+    const char* d = reinterpret_cast<const char*>(p.data);
     ld2 = p.ld * 2;
     base = d + (KMAJOR ? k0 * ld2 + m0 * 2 : m0 * ld2 + k0 * 2);
     step = KMAJOR ? BK * ld2 : BK * 2;
@@ -99,19 +110,7 @@ struct Stager {
       }
     }
   }
-  __device__ __forceinline__ void issue(char* lds, int wave) const {
-    // a scalar base and a 32-bit offset a lane: no vector arithmetic a load
-    const uint64_t b = reinterpret_cast<uint64_t>(base);
-    const char* from = reinterpret_cast<const char*>(
-        ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(b >> 32)) << 32) |
-        (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)b));
-#pragma unroll
-    for (int j = 0; j < COUNT; ++j) {
-      uint32_t o = off[j];
-      asm("" : "+v"(o));
-      __builtin_amdgcn_global_load_lds((global_void*)(from + o), (lds_void*)(lds + (wave * COUNT + j) * 1024), 16, 0, 0);
-    }
-  }
+  __device__ __forceinline__ void issue(char* lds, int wave) const { load_chunks<COUNT>(base, off, lds, wave); }
 };
 
 // Fragment reads of one operand: SPAN rows of m staged, W of them this
@@ -156,9 +155,11 @@ struct Tile {
   static constexpr int STAGE = (TM + TN) * BK * 2, LDS = 2 * STAGE;
   static constexpr int LOADS = (TM + TN) * BK / (512 * WAVES);  // a wavefront's loads of a stage
 
-  // Products over k steps [s0, s1) of BK, for each of `segs` plane pairs.
+  static constexpr int STEP = BK;  // k of a step
+
+  // Products over steps [s0, s1).
   static __device__ __forceinline__ void run(const Panel& A, int64_t m0, const Panel& B, int64_t n0, int s0, int s1,
-                                             int segs, char* lds, f32x16 (&acc)[MT][NT]) {
+                                             char* lds, f32x16 (&acc)[MT][NT]) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / (TN / WN), wn = wave % (TN / WN);
 #pragma unroll
@@ -171,18 +172,10 @@ struct Tile {
     Stager<TN, WAVES, BK_> sb;
     const Reader<TM, WM, AK> ra(wm * WM, lane);
     const Reader<TN, WN, BK_> rb(wn * WN, lane);
-    const int per = s1 - s0, total = per * segs;
-    int seg = 0, at = 0;  // of the next stage to issue
+    sa.init(A, m0, (int64_t)s0 * BK, wave, lane);
+    sb.init(B, n0, (int64_t)s0 * BK, wave, lane);
+    const int total = s1 - s0;
     auto issue = [&](int stage) {
-      if (at == per || (seg == 0 && at == 0)) {
-        if (at == per) {
-          at = 0;
-          ++seg;
-        }
-        const int pa = segs == 1 ? 0 : plane_a(seg), pb = segs == 1 ? 0 : plane_b(seg);
-        sa.init(A, pa, m0, (int64_t)s0 * BK, wave, lane);
-        sb.init(B, pb, n0, (int64_t)s0 * BK, wave, lane);
-      }
       if (sa.left < BK) sa.place(A, m0, wave, lane);
       if (sb.left < BK) sb.place(B, n0, wave, lane);
       char* to = lds + stage * STAGE;
@@ -192,7 +185,6 @@ struct Tile {
       sb.base += sb.step;
       sa.left -= BK;
       sb.left -= BK;
-      ++at;
     };
     s16x8 fa[2][MT], fb[2][NT];
     auto read = [&](int stage, int kk) {
@@ -236,6 +228,179 @@ struct Tile {
           for (int j = 0; j < NT; ++j) acc[i][j] = mfma<F16>(fa[kk & 1][i], fb[kk & 1][j], acc[i][j]);
         __builtin_amdgcn_sched_barrier(0);
       }
+    }
+  }
+
+  // m and n of register r of acc[i][j] within the tile
+  static __device__ __forceinline__ int row(int i, int r) {
+    const int lane = threadIdx.x & 63, wm = (threadIdx.x >> 6) / (TN / WN);
+    return wm * WM + i * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
+  }
+  static __device__ __forceinline__ int col(int j) {
+    const int lane = threadIdx.x & 63, wn = (threadIdx.x >> 6) % (TN / WN);
+    return wn * WN + j * 32 + (lane & 31);
+  }
+};
+
+// ------------------------------------------------------------ fp32 products
+
+// An fp32 operand is three bf16 planes (x = x0 + x1 + x2 exactly), laid out
+// [row][column / 16][plane][16], so that 16 columns of all planes are 96
+// contiguous bytes in either reading.  Of the nine products of planes the six
+// that are not below fp32's own rounding are added, small ones first.  A stage
+// holds 16 k of all three planes: every byte that comes to LDS takes part in
+// two products on average, which halves the loads and LDS reads of six
+// separate products (4099 x 256 x 30011 scores twice and both gradients: P3A
+// us, P3B as six passes over the planes).
+
+// One operand's share of a stage: SPAN x 16 x 3 planes, 6 SPAN chunks.
+template <int SPAN, int WAVES, bool KMAJOR>
+struct Stager3 {
+  static constexpr int COUNT = SPAN * 6 / (64 * WAVES);
+  static_assert(COUNT >= 1 && COUNT * 64 * WAVES == SPAN * 6, "stage does not divide");
+  const char* base;
+  int64_t step, ld2, left;
+  uint32_t off[COUNT];
+
+  // p.ld in 16-bit elements, p.rows and p.cols in rows and fp32 columns
+  __device__ void init(const Panel& p, int64_t m0, int64_t k0, int wave, int lane) {
+    const char* d = reinterpret_cast<const char*>(p.data);
+    ld2 = p.ld * 2;
+    base = d + (KMAJOR ? k0 * ld2 + m0 * 6 : m0 * ld2 + k0 * 6);
+    step = KMAJOR ? 16 * ld2 : 96;
+    left = (KMAJOR ? p.rows : p.cols) - k0;
+    place(p, m0, wave, lane);
+  }
+  // As in Stager; k past the end of a K-contiguous row is there (zeros).
+  __device__ void place(const Panel& p, int64_t m0, int wave, int lane) {
+#pragma unroll
+    for (int j = 0; j < COUNT; ++j) {
+      const int i = (wave * COUNT + j) * 64 + lane;
+      if constexpr (KMAJOR) {
+        const int64_t last = (p.cols - m0) / 16 * 6 - 1;  // chunks there are
+        const int r = i / (SPAN * 3 / 8), c = (i % (SPAN * 3 / 8)) ^ ((r & 3) * 4);
+        off[j] = (uint32_t)((r < left ? r : left - 1) * ld2 + (c < last ? c : last) * 16);
+      } else {
+        const int64_t last = p.rows - 1 - m0;
+        const int r = i / 6, c = (i % 6) ^ ((r >> 3) & 1);
+        off[j] = (uint32_t)((r < last ? r : last) * ld2 + c * 16);
+      }
+    }
+  }
+};
+
+template <int SPAN, int W, bool KMAJOR>
+struct Reader3 {
+  uint32_t at[KMAJOR ? W / 32 : 1];
+  int odd;
+  __device__ Reader3(int first, int lane) {
+    if constexpr (!KMAJOR) {
+      const int r = first + (lane & 31);  // (32 rows on: the same swap)
+      odd = (r >> 3) & 1;
+      at[0] = (uint32_t)(r * 96 + (((lane >> 5) ^ odd) << 4));
+    } else {
+      const int g = lane >> 4, i = lane & 15;
+      odd = 0;
+#pragma unroll
+      for (int t = 0; t < W / 32; ++t)
+        at[t] = (uint32_t)((8 * (g >> 1) + i / 4) * (SPAN * 6) + (i & 1) * 8) |
+                (uint32_t)(((first + 32 * t) / 16 + (g & 1)) * 6 + ((i & 3) >> 1)) << 20;
+    }
+  }
+  // rows [32 t, 32 t + 32) of the wavefront's span in one plane
+  __device__ __forceinline__ s16x8 get(const char* lds, int t, int plane, int lane) const {
+    if constexpr (!KMAJOR) {
+      return *reinterpret_cast<const s16x8*>(lds + at[0] + t * (32 * 96) + plane * 32);
+    } else {
+      typedef __attribute__((address_space(3))) s16x4 lds4;
+      const uint32_t c = (at[t] >> 20) + plane * 2;
+      const char* p = lds + (at[t] & 0xfffff) + ((c ^ (((lane & 15) / 4) * 4)) << 4);
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)p);
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(p + 4 * (SPAN * 6)));
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+  }
+};
+
+template <int TM, int TN, int WM, int WN, int STAGES, bool AK, bool BK_>
+struct Tile3 {
+  static constexpr int WAVES = TM / WM * (TN / WN), THREADS = 64 * WAVES;
+  static constexpr int MT = WM / 32, NT = WN / 32;
+  static constexpr int STAGE = (TM + TN) * 96, LDS = STAGES * STAGE;
+  static constexpr int STEP = 16;
+  static constexpr int LOADS = (TM + TN) * 6 / (64 * WAVES);
+
+  static __device__ __forceinline__ void run(const Panel& A, int64_t m0, const Panel& B, int64_t n0, int s0, int s1,
+                                             char* lds, f32x16 (&acc)[MT][NT]) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / (TN / WN), wn = wave % (TN / WN);
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+    Stager3<TM, WAVES, AK> sa;
+    Stager3<TN, WAVES, BK_> sb;
+    const Reader3<TM, WM, AK> ra(wm * WM, lane);
+    const Reader3<TN, WN, BK_> rb(wn * WN, lane);
+    sa.init(A, m0, (int64_t)s0 * STEP, wave, lane);
+    sb.init(B, n0, (int64_t)s0 * STEP, wave, lane);
+    const int total = s1 - s0;
+    auto issue = [&](int stage) {
+      if constexpr (AK)
+        if (sa.left < STEP) sa.place(A, m0, wave, lane);
+      if constexpr (BK_)
+        if (sb.left < STEP) sb.place(B, n0, wave, lane);
+      char* to = lds + stage * STAGE;
+      load_chunks(sa.base, sa.off, to, wave);
+      load_chunks(sb.base, sb.off, to + TM * 96, wave);
+      sa.base += sa.step;
+      sb.base += sb.step;
+      sa.left -= STEP;
+      sb.left -= STEP;
+    };
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s)
+      if (s < total) issue(s);
+    int cur = 0;
+    for (int s = 0; s < total; ++s) {
+      // this step's loads are the oldest ones; the reads of the step before
+      // are done before any wavefront overwrites their stage
+      if (s + STAGES - 2 < total) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LOADS * (STAGES - 2)) : "memory");
+      else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      const char* a = lds + cur * STAGE;
+      const char* b = a + TM * 96;
+      s16x8 fa[3][MT], fb[3][NT];
+      // in the order of their use
+      auto read = [&](int p, int q) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) fa[p][i] = ra.get(a, i, p, lane);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) fb[q][j] = rb.get(b, j, q, lane);
+      };
+      auto multiply = [&](int p, int q) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int j = 0; j < NT; ++j) acc[i][j] = mfma<false>(fa[p][i], fb[q][j], acc[i][j]);
+      };
+      read(2, 0);
+      read(0, 2);
+      __builtin_amdgcn_sched_barrier(0);
+      if (s + STAGES - 1 < total) issue(cur == 0 ? STAGES - 1 : cur - 1);
+      multiply(2, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      read(1, 1);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(0, 2);
+      multiply(1, 1);
+      multiply(1, 0);
+      multiply(0, 1);
+      multiply(0, 0);
+      cur = cur == STAGES - 1 ? 0 : cur + 1;
     }
   }
 

@@ -18,6 +18,7 @@
 #include "train.h"
 
 #include <algorithm>
+#include <type_traits>
 
 #include "dense.h"
 #include "device.h"
@@ -34,25 +35,27 @@ constexpr float F16_UP = 1024.f;       // dz in fp16 is held times this: 2^-35 i
 
 // ---------------------------------------------------------------- operands
 
-// Rows of X as 16-bit planes of `width` columns, zeros past the end.
-__global__ __launch_bounds__(256) void k_pack(Mat X, uint16_t* to, int64_t plane, int64_t width, int planes) {
+// Rows of X at a stride of `width` columns, zeros past the end: 16-bit values
+// as they are, fp32 as three planes of bf16 (tile.h).
+template <bool PLANES>
+__global__ __launch_bounds__(256) void k_pack(Mat X, uint16_t* to, int64_t width) {
   const int64_t per = width / 4, total = X.rows * per;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
     const int64_t r = i / per, c = (i - r * per) * 4, at = r * X.ld + c;
-    uint16_t* out = to + r * width + c;
-    if (planes == 1) {
+    if constexpr (!PLANES) {
       const uint16_t* x = static_cast<const uint16_t*>(X.data);
       u16x4_el v = {0, 0, 0, 0};
       if (c + 4 <= X.cols) v = *reinterpret_cast<const u16x4_el*>(x + at);
       else
         for (int k = 0; k < 4; ++k)
           if (c + k < X.cols) v[k] = x[at + k];
-      *reinterpret_cast<u16x4_el*>(out) = v;
+      *reinterpret_cast<u16x4_el*>(to + r * width + c) = v;
     } else {
       float x[4];
       if (c + 4 <= X.cols) load4<DT_F32>(X.data, at, x);
       else
         for (int k = 0; k < 4; ++k) x[k] = c + k < X.cols ? load1<DT_F32>(X.data, at + k) : 0.f;
+      uint16_t* out = to + r * width * 3 + c / 16 * 48 + c % 16;
 #pragma unroll
       for (int p = 0; p < 3; ++p) {
         u16x4_el v;
@@ -61,7 +64,7 @@ __global__ __launch_bounds__(256) void k_pack(Mat X, uint16_t* to, int64_t plane
           v[k] = f32_to_bf16(x[k]);
           x[k] -= bf16_to_f32(v[k]);
         }
-        *reinterpret_cast<u16x4_el*>(out + p * plane) = v;
+        *reinterpret_cast<u16x4_el*>(out + p * 16) = v;
       }
     }
   }
@@ -72,11 +75,11 @@ __global__ __launch_bounds__(256) void k_pack(Mat X, uint16_t* to, int64_t plane
 struct Scores {
   Panel W, H;
   int64_t T, V, v0, v1;   // the piece [v0, v1) of the table
-  int steps, segs;
+  int steps;
   float2* part;           // [tile][t]: maximum, sum (base 2)
   const float* top; const float* inv;  // of whole rows
   const void* labels; int i64;
-  uint16_t* dz; int64_t plane, ldz;
+  uint16_t* dz; int64_t ldz;  // of 16-bit elements
   uint32_t* ticket;       // cleared here for the workgroups of k_rows
 };
 
@@ -84,21 +87,24 @@ struct Scores {
 // 32: four of 64 x 32, two workgroups a CU, for the few rows whose scores only
 // cost the reading of the table (T = 1, 262144 x 512 bf16: 41 us against 71
 // with 256 rows).
-template <int TT, bool F16>
-using ScoreTile = Tile<TV, TT, TT == 256 ? 128 : 64, TT == 32 ? 32 : 64, false, false, F16>;
+template <int TT, int TYPE>
+using ScoreTile = std::conditional_t<TYPE == DT_F32, Tile3<TV, TT, 128, 64, TT == 256 ? 3 : 2, false, false>,
+                                     Tile<TV, TT, TT == 256 ? 128 : 64, TT == 32 ? 32 : 64, false, false, TYPE == DT_F16>>;
+
+constexpr int score_threads(int type, int TT) { return TT == 256 || (TT == 128 && type != DT_F32) ? 512 : 256; }
 
 template <bool GRAD, int TYPE, int TT>
-__global__ __launch_bounds__(TT == 32 ? 256 : 512, 2) void k_scores(Scores s) {
+__global__ __launch_bounds__(score_threads(TYPE, TT), 2) void k_scores(Scores s) {
   constexpr bool F16 = TYPE == DT_F16;
   constexpr int PLANES = TYPE == DT_F32 ? 3 : 1;
-  using T_ = ScoreTile<TT, F16>;
+  using T_ = ScoreTile<TT, TYPE>;
   constexpr int SPAN = T_::MT * 32, NWM = TV / SPAN;  // table entries of a wavefront, wavefronts along the table
   __shared__ __attribute__((aligned(16))) char lds[T_::LDS];
   int64_t vt, tt;
   place_tile(blockIdx.x, (s.v1 - s.v0 + TV - 1) / TV, (s.T + TT - 1) / TT, 8, vt, tt);
   const int64_t v0 = s.v0 + vt * TV, t0 = tt * TT;
   f32x16 acc[T_::MT][T_::NT];
-  T_::run(s.W, v0, s.H, t0, 0, s.steps, s.segs, lds, acc);
+  T_::run(s.W, v0, s.H, t0, 0, s.steps, lds, acc);
   const int lane = threadIdx.x & 63, wm = (threadIdx.x >> 6) / (T_::WAVES / NWM);
   __syncthreads();  // the stages' LDS changes its use
 
@@ -201,11 +207,11 @@ __global__ __launch_bounds__(TT == 32 ? 256 : 512, 2) void k_scores(Scores s) {
           }
       }
       __syncthreads();
-      uint16_t* to = s.dz + p * s.plane + t0 * s.ldz + (v0 - s.v0);
       const int ch = threadIdx.x & 31;
+      uint16_t* to = s.dz + t0 * s.ldz + (PLANES == 1 ? v0 - s.v0 + ch * 8 : (v0 - s.v0) * 3 + ch / 2 * 48 + p * 16 + ch % 2 * 8);
 #pragma unroll 4
       for (int c = threadIdx.x >> 5; c < TT; c += T_::THREADS / 32)
-        *reinterpret_cast<uint4*>(to + c * s.ldz + ch * 8) =
+        *reinterpret_cast<uint4*>(to + c * s.ldz) =
             *reinterpret_cast<const uint4*>(lds + c * (TV * 2) + ((ch ^ (c & 31)) << 4));
     }
   }
@@ -396,19 +402,18 @@ struct Product {
 struct Gradients {
   Product dh, dw;
   int64_t first_dw;  // workgroups before it make dH
-  int segs;
   const float* scale;
 };
 
 template <class T_, int G>
-__device__ __forceinline__ void product(const Product& p, int64_t b, int segs, const float* scale, char* lds) {
+__device__ __forceinline__ void product(const Product& p, int64_t b, const float* scale, char* lds) {
   int64_t y, x;
   place_tile(b, p.ny * p.slices, p.nx, 8, y, x);
   const int slice = (int)(y / p.ny);
   const int64_t m0 = (y - slice * p.ny) * G, n0 = x * G;
   const int s0 = slice * p.per, s1 = s0 + p.per < p.steps ? s0 + p.per : p.steps;
   f32x16 acc[T_::MT][T_::NT];
-  T_::run(p.A, m0, p.B, n0, s0, s1, segs, lds, acc);
+  T_::run(p.A, m0, p.B, n0, s0, s1, lds, acc);
   // Through LDS, 32 rows of the wavefront's part at a time, so that rows are
   // written 256 bytes (fp32) at a time.
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -454,13 +459,24 @@ __device__ __forceinline__ void product(const Product& p, int64_t b, int segs, c
 
 // G x G tiles: 256 by eight wavefronts of 128 x 64, or 128 by four of 64 x 64
 // (two workgroups a CU).
-template <bool F16, int G>
+template <int TYPE, int G, bool AK>
+using GradientTile = std::conditional_t<TYPE == DT_F32, Tile3<G, G, G / 2, 64, 3, AK, true>,
+                                        Tile<G, G, G / 2, 64, AK, true, TYPE == DT_F16>>;
+
+template <int TYPE, int G>
 __global__ __launch_bounds__(G == 256 ? 512 : 256, 2) void k_gradients(Gradients g) {
-  using TH = Tile<G, G, G / 2, 64, false, true, F16>;
-  using TW = Tile<G, G, G / 2, 64, true, true, F16>;
+  using TH = GradientTile<TYPE, G, false>;
+  using TW = GradientTile<TYPE, G, true>;
   __shared__ __attribute__((aligned(16))) char lds[TH::LDS];
-  if ((int64_t)blockIdx.x < g.first_dw) product<TH, G>(g.dh, blockIdx.x, g.segs, g.scale, lds);
-  else product<TW, G>(g.dw, blockIdx.x - g.first_dw, g.segs, g.scale, lds);
+  if ((int64_t)blockIdx.x < g.first_dw) product<TH, G>(g.dh, blockIdx.x, g.scale, lds);
+  else product<TW, G>(g.dw, blockIdx.x - g.first_dw, g.scale, lds);
+}
+
+template <int TYPE>
+void gradients(const Gradients& g, int G, hipStream_t s) {
+  const unsigned grid = (unsigned)(g.first_dw + g.dw.blocks());
+  if (G == 256) k_gradients<TYPE, 256><<<grid, 512, 0, s>>>(g);
+  else k_gradients<TYPE, 128><<<grid, 256, 0, s>>>(g);
 }
 
 // out = scale times the sum of the slices; GROUPS threads to an element's
@@ -529,7 +545,7 @@ unsigned grid_of(int64_t items, int64_t per) {
 
 // Sizes and places in the workspace.
 struct Layout {
-  int64_t width, planes, segs;         // columns of the packed operands
+  int64_t width, planes, step;         // columns and planes of the packed operands, k of a step
   int TT, G;                           // tiles
   int64_t piece, Tp, ldz;              // table entries of a piece, rows of dz and their stride
   int dh_per, dh_slices, dw_per, dw_slices;
@@ -545,10 +561,10 @@ void slices_of(int steps, int64_t ideal, int& per, int& slices) {
 // Rows of a tile of scores: no more than there are, and as many as still make
 // a tile for every other CU (500 x 2000 scores, 64 columns, f32: the
 // whole call 80 us so, 102 in tiles of 256 rows).
-int score_rows(int64_t T, int64_t V) {
+int score_rows(int64_t T, int64_t V, int type) {
   for (int TT : {256, 128})
     if (T > TT / 2 && up(T, TT) / TT * (up(V, TV) / TV) >= 128) return TT;
-  return 32;
+  return type == DT_F32 ? 128 : 32;
 }
 
 Layout layout_of(int64_t T, int64_t D, int64_t V, int type, bool grads) {
@@ -559,10 +575,10 @@ Layout layout_of(int64_t T, int64_t D, int64_t V, int type, bool grads) {
     at = up(at + n, 256);
     return here;
   };
-  l.width = up(D, BK);
   l.planes = type == DT_F32 ? 3 : 1;
-  l.segs = type == DT_F32 ? 6 : 1;
-  l.TT = score_rows(T, V);
+  l.step = type == DT_F32 ? 16 : BK;
+  l.width = up(D, l.step);
+  l.TT = score_rows(T, V, type);
   l.Tp = up(T, l.TT);
   l.ticket = take(4);
   l.scale = take(4);
@@ -575,18 +591,18 @@ Layout layout_of(int64_t T, int64_t D, int64_t V, int type, bool grads) {
   l.w = take(2 * l.planes * V * l.width);
   if (grads) {
     l.piece = std::min(up(V, TV), std::max<int64_t>(TV, kPieceBytes / (2 * l.planes * std::max<int64_t>(l.Tp, 1)) / TV * TV));
-    const int dh_steps = (int)(up(std::min(l.piece, V), BK) / BK), dw_steps = (int)(up(T, BK) / BK);
+    const int dh_steps = (int)(up(std::min(l.piece, V), l.step) / l.step), dw_steps = (int)(up(T, l.step) / l.step);
     // small tiles where a side would leave half of a large one empty
     l.G = std::min({T, D, V}) <= 128 ? 128 : 256;
     // shares of k of about equal length, one workgroup (of 256, else two) a CU
     const int64_t nx = up(D, l.G) / l.G, th = up(T, l.G) / l.G * nx, tw = up(std::min(l.piece, V), l.G) / l.G * nx;
-    const int64_t ideal = std::max<int64_t>(l.segs == 1 ? 4 : 2, (th * dh_steps + tw * dw_steps) / (l.G == 256 ? 256 : 512));
+    const int64_t ideal = std::max<int64_t>(l.planes == 1 ? 4 : 8, (th * dh_steps + tw * dw_steps) / (l.G == 256 ? 256 : 512));
     slices_of(dh_steps, ideal, l.dh_per, l.dh_slices);
     slices_of(dw_steps, ideal, l.dw_per, l.dw_slices);
     if (l.dh_slices > 1 || l.piece < V) l.dh = take(4 * l.dh_slices * T * l.width);
     if (l.dw_slices > 1) l.dw = take(4 * l.dw_slices * l.piece * l.width);
-    l.ldz = l.piece + 64;
-    l.dz = take(2 * l.planes * l.Tp * l.ldz);
+    l.ldz = l.planes * l.piece + 64;
+    l.dz = take(2 * l.Tp * l.ldz);
   }
   l.bytes = at;
   return l;
@@ -596,21 +612,23 @@ Layout layout_of(int64_t T, int64_t D, int64_t V, int type, bool grads) {
 // to the next multiple of BK columns.  Of the two operands of the scores one
 // has to hold zeros there: H (whole), which is the smaller one as a rule.
 Panel panel_of(const Mat& X, const Layout& l, bool whole, char* ws, hipStream_t s) {
-  if (l.planes == 1 && X.cols % (whole ? BK : 8) == 0 && X.ld % 8 == 0 && X.ld < (int64_t(1) << 22) &&
+  if (l.planes == 1 && X.cols % (whole ? l.step : 8) == 0 && X.ld % 8 == 0 && X.ld < (int64_t(1) << 22) &&
       (reinterpret_cast<uintptr_t>(X.data) & 15) == 0)
-    return Panel{static_cast<const uint16_t*>(X.data), 0, X.ld, X.rows, X.cols};
+    return Panel{static_cast<const uint16_t*>(X.data), X.ld, X.rows, X.cols};
   uint16_t* to = reinterpret_cast<uint16_t*>(ws);
-  const int64_t plane = X.rows * l.width;
-  k_pack<<<grid_of(X.rows * (l.width / 4), 1024), 256, 0, s>>>(X, to, plane, l.width, (int)l.planes);
-  return Panel{to, plane, l.width, X.rows, l.width};
+  const unsigned grid = grid_of(X.rows * (l.width / 4), 1024);
+  if (l.planes == 1) k_pack<false><<<grid, 256, 0, s>>>(X, to, l.width);
+  else k_pack<true><<<grid, 256, 0, s>>>(X, to, l.width);
+  return Panel{to, l.planes * l.width, X.rows, l.width};
 }
 
 template <bool GRAD, int TYPE>
 void scores(const Scores& sc, int TT, hipStream_t s) {
   const unsigned grid = (unsigned)(up(sc.v1 - sc.v0, TV) / TV * (up(sc.T, TT) / TT));
-  if (TT == 32) k_scores<GRAD, TYPE, 32><<<grid, 256, 0, s>>>(sc);
-  else if (TT == 128) k_scores<GRAD, TYPE, 128><<<grid, 512, 0, s>>>(sc);
-  else k_scores<GRAD, TYPE, 256><<<grid, 512, 0, s>>>(sc);
+  if constexpr (TYPE != DT_F32)
+    if (TT == 32) k_scores<GRAD, TYPE, 32><<<grid, 256, 0, s>>>(sc);
+  if (TT == 128) k_scores<GRAD, TYPE, 128><<<grid, score_threads(TYPE, 128), 0, s>>>(sc);
+  else if (TT == 256) k_scores<GRAD, TYPE, 256><<<grid, 512, 0, s>>>(sc);
 }
 
 template <bool GRAD>
@@ -643,8 +661,7 @@ hipError_t linear_xent(const XentArgs& x, hipStream_t s) {
     sc.H = panel_of(x.H, l, true, ws + l.h, s);
     sc.W = panel_of(x.W, l, false, ws + l.w, s);
     sc.T = T; sc.V = V; sc.v0 = 0; sc.v1 = V;
-    sc.steps = (int)(l.width / BK);
-    sc.segs = (int)l.segs;
+    sc.steps = (int)(l.width / l.step);
     sc.part = (float2*)(ws + l.part);
     sc.labels = x.labels; sc.i64 = x.labels_i64;
     sc.ticket = (uint32_t*)(ws + l.ticket);
@@ -662,8 +679,7 @@ hipError_t linear_xent(const XentArgs& x, hipStream_t s) {
   sc.top = top; sc.inv = inv;
   sc.dz = (uint16_t*)(ws + l.dz);
   sc.ldz = l.ldz;
-  sc.plane = l.Tp * l.ldz;
-  const Panel dz{sc.dz, sc.plane, l.ldz, l.Tp, l.piece};
+  const Panel dz{sc.dz, l.ldz, l.Tp, l.piece};
   const int64_t nx = up(D, l.G) / l.G;
   const int size = dtype_bytes(type);
   for (int64_t v0 = 0; v0 < V; v0 += l.piece) {
@@ -671,24 +687,21 @@ hipError_t linear_xent(const XentArgs& x, hipStream_t s) {
     sc.v0 = v0; sc.v1 = v0 + n;
     scores<true>(sc, type, l.TT, s);
     Gradients g{};
-    g.segs = (int)l.segs;
     g.scale = scale;
     Panel w = sc.W;
     w.data += v0 * w.ld;
     w.rows = n;
-    g.dh = Product{dz, w, up(T, l.G) / l.G, nx, T, D, (int)(up(n, BK) / BK), l.dh_per, 0,
+    g.dh = Product{dz, w, up(T, l.G) / l.G, nx, T, D, (int)(up(n, l.step) / l.step), l.dh_per, 0,
                    l.dh ? (float*)(ws + l.dh) : nullptr, l.width, v0 > 0, x.dH.data, x.dH.ld, type};
     g.dh.slices = (g.dh.steps + l.dh_per - 1) / l.dh_per;
     Mat out = x.dW;
     out.data = (char*)x.dW.data + v0 * x.dW.ld * size;
-    g.dw = Product{dz, sc.H, up(n, l.G) / l.G, nx, n, D, (int)(up(T, BK) / BK), l.dw_per, l.dw_slices,
+    g.dw = Product{dz, sc.H, up(n, l.G) / l.G, nx, n, D, (int)(up(T, l.step) / l.step), l.dw_per, l.dw_slices,
                    l.dw ? (float*)(ws + l.dw) : nullptr, l.width, 0, out.data, out.ld, type};
     g.first_dw = g.dh.blocks();
-    const unsigned grid = (unsigned)(g.first_dw + g.dw.blocks());
-    if (l.G == 256 && f16) k_gradients<true, 256><<<grid, 512, 0, s>>>(g);
-    else if (l.G == 256) k_gradients<false, 256><<<grid, 512, 0, s>>>(g);
-    else if (f16) k_gradients<true, 128><<<grid, 256, 0, s>>>(g);
-    else k_gradients<false, 128><<<grid, 256, 0, s>>>(g);
+    if (type == DT_F32) gradients<DT_F32>(g, l.G, s);
+    else if (type == DT_BF16) gradients<DT_BF16>(g, l.G, s);
+    else gradients<DT_F16>(g, l.G, s);
     if (l.dw) finish((float*)(ws + l.dw), l.dw_slices, n, D, l.width, scale, out.data, type, out.ld, s);
   }
   if (l.dh) finish((float*)(ws + l.dh), l.dh_slices, T, D, l.width, scale, x.dH.data, type, x.dH.ld, s);
