@@ -55,10 +55,18 @@ __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(1))) void global_void;
 
-// COUNT loads of 1 KB by a wavefront, straight to its part of a stage: a
-// scalar base and a 32-bit offset a lane, so no vector arithmetic a load.
-template <int COUNT>
-__device__ __forceinline__ void load_chunks(const char* base, const uint32_t (&off)[COUNT], char* lds, int wave) {
+// Load j of a wavefront fills 1 KB of the stage.  Where the stage has fewer
+// than every wavefront's share, the last one is loaded more than once.
+template <int TOTAL, int WAVES>
+__device__ __forceinline__ int part_of(int j, int wave) {
+  const int i = j * WAVES + wave;
+  return TOTAL % WAVES == 0 || i < TOTAL ? i : TOTAL - 1;
+}
+
+// A wavefront's loads of a stage, straight to LDS: a scalar base and a 32-bit
+// offset a lane, so no vector arithmetic a load.
+template <int TOTAL, int WAVES, int COUNT>
+__device__ __forceinline__ void load_parts(const char* base, const uint32_t (&off)[COUNT], char* lds, int wave) {
   const uint64_t b = reinterpret_cast<uint64_t>(base);
   const char* from = reinterpret_cast<const char*>(
       ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(b >> 32)) << 32) |
@@ -67,17 +75,18 @@ __device__ __forceinline__ void load_chunks(const char* base, const uint32_t (&o
   for (int j = 0; j < COUNT; ++j) {
     uint32_t o = off[j];
     asm("" : "+v"(o));
-    __builtin_amdgcn_global_load_lds((global_void*)(from + o), (lds_void*)(lds + (wave * COUNT + j) * 1024), 16, 0, 0);
+    __builtin_amdgcn_global_load_lds((global_void*)(from + o), (lds_void*)(lds + part_of<TOTAL, WAVES>(j, wave) * 1024), 16, 0,
+                                     0);
   }
 }
 
 // One operand's share of a stage: SPAN x BK elements, 1 KB an instruction.
 template <int SPAN, int WAVES, bool KMAJOR>
 struct Stager {
-  static constexpr int COUNT = SPAN * BK / (512 * WAVES);  // instructions a wavefront issues
+  static constexpr int TOTAL = SPAN * BK / 512, COUNT = (TOTAL + WAVES - 1) / WAVES;  // loads, a wavefront's
   static constexpr int CHUNKS = KMAJOR ? SPAN / 8 : BK / 8;  // 16-byte chunks a row
   static constexpr int ROWS = 64 / CHUNKS;                   // rows an instruction
-  static_assert(COUNT >= 1 && COUNT * 512 * WAVES == SPAN * BK && ROWS >= 1, "stage does not divide");
+  static_assert(ROWS >= 1, "a load holds whole rows");
   const char* base;      // first row of the tile, advanced along k
   int64_t step;          // bytes a step
   uint32_t off[COUNT];
@@ -98,7 +107,7 @@ struct Stager {
   __device__ void place(const Panel& p, int64_t m0, int wave, int lane) {
 #pragma unroll
     for (int j = 0; j < COUNT; ++j) {
-      const int r = (wave * COUNT + j) * ROWS + lane / CHUNKS;
+      const int r = part_of<TOTAL, WAVES>(j, wave) * ROWS + lane / CHUNKS;
       if constexpr (KMAJOR) {
         const int64_t last = p.cols - 8 - m0;
         const int c = ((lane % CHUNKS) ^ ((r & 3) * 4)) * 8;
@@ -110,7 +119,7 @@ struct Stager {
       }
     }
   }
-  __device__ __forceinline__ void issue(char* lds, int wave) const { load_chunks<COUNT>(base, off, lds, wave); }
+  __device__ __forceinline__ void issue(char* lds, int wave) const { load_parts<TOTAL, WAVES>(base, off, lds, wave); }
 };
 
 // Fragment reads of one operand: SPAN rows of m staged, W of them this
@@ -153,7 +162,7 @@ struct Tile {
   static constexpr int WAVES = TM / WM * (TN / WN), THREADS = 64 * WAVES;
   static constexpr int MT = WM / 32, NT = WN / 32;
   static constexpr int STAGE = (TM + TN) * BK * 2, LDS = 2 * STAGE;
-  static constexpr int LOADS = (TM + TN) * BK / (512 * WAVES);  // a wavefront's loads of a stage
+  static constexpr int LOADS = Stager<TM, WAVES, AK>::COUNT + Stager<TN, WAVES, BK_>::COUNT;  // a wavefront's, a stage
 
   static constexpr int STEP = BK;  // k of a step
 
@@ -256,8 +265,7 @@ struct Tile {
 // One operand's share of a stage: SPAN x 16 x 3 planes, 6 SPAN chunks.
 template <int SPAN, int WAVES, bool KMAJOR>
 struct Stager3 {
-  static constexpr int COUNT = SPAN * 6 / (64 * WAVES);
-  static_assert(COUNT >= 1 && COUNT * 64 * WAVES == SPAN * 6, "stage does not divide");
+  static constexpr int TOTAL = SPAN * 6 / 64, COUNT = (TOTAL + WAVES - 1) / WAVES;
   const char* base;
   int64_t step, ld2, left;
   uint32_t off[COUNT];
@@ -275,7 +283,7 @@ struct Stager3 {
   __device__ void place(const Panel& p, int64_t m0, int wave, int lane) {
 #pragma unroll
     for (int j = 0; j < COUNT; ++j) {
-      const int i = (wave * COUNT + j) * 64 + lane;
+      const int i = part_of<TOTAL, WAVES>(j, wave) * 64 + lane;
       if constexpr (KMAJOR) {
         const int64_t last = (p.cols - m0) / 16 * 6 - 1;  // chunks there are
         const int r = i / (SPAN * 3 / 8), c = (i % (SPAN * 3 / 8)) ^ ((r & 3) * 4);
@@ -328,7 +336,7 @@ struct Tile3 {
   static constexpr int MT = WM / 32, NT = WN / 32;
   static constexpr int STAGE = (TM + TN) * 96, LDS = STAGES * STAGE;
   static constexpr int STEP = 16;
-  static constexpr int LOADS = (TM + TN) * 6 / (64 * WAVES);
+  static constexpr int LOADS = Stager3<TM, WAVES, AK>::COUNT + Stager3<TN, WAVES, BK_>::COUNT;
 
   static __device__ __forceinline__ void run(const Panel& A, int64_t m0, const Panel& B, int64_t n0, int s0, int s1,
                                              char* lds, f32x16 (&acc)[MT][NT]) {
@@ -353,8 +361,8 @@ struct Tile3 {
       if constexpr (BK_)
         if (sb.left < STEP) sb.place(B, n0, wave, lane);
       char* to = lds + stage * STAGE;
-      load_chunks(sa.base, sa.off, to, wave);
-      load_chunks(sb.base, sb.off, to + TM * 96, wave);
+      load_parts<sa.TOTAL, WAVES>(sa.base, sa.off, to, wave);
+      load_parts<sb.TOTAL, WAVES>(sb.base, sb.off, to + TM * 96, wave);
       sa.base += sa.step;
       sb.base += sb.step;
       sa.left -= STEP;

@@ -88,7 +88,7 @@ struct Scores {
 // cost the reading of the table (T = 1, 262144 x 512 bf16: 41 us against 71
 // with 256 rows).
 template <int TT, int TYPE>
-using ScoreTile = std::conditional_t<TYPE == DT_F32, Tile3<TV, TT, 128, 64, TT == 256 ? 3 : 2, false, false>,
+using ScoreTile = std::conditional_t<TYPE == DT_F32, Tile3<TV, TT, TT == 32 ? 64 : 128, TT == 32 ? 32 : 64, TT == 256 ? 3 : 2, false, false>,
                                      Tile<TV, TT, TT == 256 ? 128 : 64, TT == 32 ? 32 : 64, false, false, TYPE == DT_F16>>;
 
 constexpr int score_threads(int type, int TT) { return TT == 256 || (TT == 128 && type != DT_F32) ? 512 : 256; }
@@ -183,10 +183,8 @@ __global__ __launch_bounds__(score_threads(TYPE, TT), 2) void k_scores(Scores s)
 #pragma unroll
             for (int j = 0; j < T_::NT; ++j) acc[i][j][r] = 0.f;
     }
-    // through LDS, so that rows of dz are written 512 bytes at a time
-#pragma unroll
-    for (int p = 0; p < PLANES; ++p) {
-      if (p) __syncthreads();
+    if constexpr (PLANES == 1) {
+      // through LDS, so that rows of dz are written 512 bytes at a time
 #pragma unroll
       for (int j = 0; j < T_::NT; ++j) {
         const int c = T_::col(j);
@@ -199,7 +197,6 @@ __global__ __launch_bounds__(score_threads(TYPE, TT), 2) void k_scores(Scores s)
             for (int k = 0; k < 4; ++k) {
               const float x = acc[i][j][q * 4 + k];
               v[k] = F16 ? f32_to_f16(x) : f32_to_bf16(x);
-              if constexpr (PLANES > 1) acc[i][j][q * 4 + k] = x - bf16_to_f32(v[k]);
             }
             const int at = T_::row(i, q * 4);
             *reinterpret_cast<uint64_t*>(lds + c * (TV * 2) + (((at >> 3) ^ (c & 31)) << 4) + (at & 4) * 2) =
@@ -208,11 +205,51 @@ __global__ __launch_bounds__(score_threads(TYPE, TT), 2) void k_scores(Scores s)
       }
       __syncthreads();
       const int ch = threadIdx.x & 31;
-      uint16_t* to = s.dz + t0 * s.ldz + (PLANES == 1 ? v0 - s.v0 + ch * 8 : (v0 - s.v0) * 3 + ch / 2 * 48 + p * 16 + ch % 2 * 8);
+      uint16_t* to = s.dz + t0 * s.ldz + (v0 - s.v0) + ch * 8;
 #pragma unroll 4
       for (int c = threadIdx.x >> 5; c < TT; c += T_::THREADS / 32)
         *reinterpret_cast<uint4*>(to + c * s.ldz) =
             *reinterpret_cast<const uint4*>(lds + c * (TV * 2) + ((ch ^ (c & 31)) << 4));
+    } else {
+      // each wavefront through LDS of its own, 64 table entries of 32 rows at a
+      // time: 384 bytes a row with all planes
+      char* mine = lds + (threadIdx.x >> 6) * (32 * 384);
+      static_assert(T_::WAVES * 32 * 384 <= T_::LDS && T_::MT % 2 == 0, "dz is staged in the stages' LDS");
+      const int c32 = lane & 31;
+#pragma unroll
+      for (int j = 0; j < T_::NT; ++j)
+#pragma unroll
+        for (int i0 = 0; i0 < T_::MT; i0 += 2) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              float x[4];
+#pragma unroll
+              for (int k = 0; k < 4; ++k) x[k] = acc[i0 + i][j][q * 4 + k];
+#pragma unroll
+              for (int p = 0; p < 3; ++p) {
+                u16x4_el v;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                  v[k] = f32_to_bf16(x[k]);
+                  x[k] -= bf16_to_f32(v[k]);
+                }
+                // 16 columns of a plane: chunks 6 (2 i + q / 2) + 2 p and the next
+                const int ch = 6 * (2 * i + (q >> 1)) + 2 * p + (q & 1);
+                *reinterpret_cast<uint64_t*>(mine + c32 * 384 + ((ch ^ (c32 & 7)) << 4) + (lane >> 5) * 8) =
+                    __builtin_bit_cast(uint64_t, v);
+              }
+            }
+          wave_sync();
+          uint16_t* to = s.dz + (t0 + T_::col(j) - c32) * s.ldz + (v0 - s.v0 + wm * SPAN + i0 * 32) * 3;
+          for (int it = lane; it < 32 * 24; it += 64) {
+            const int r = it / 24, ch = it % 24;
+            *reinterpret_cast<uint4*>(to + r * s.ldz + ch * 8) =
+                *reinterpret_cast<const uint4*>(mine + r * 384 + ((ch ^ (r & 7)) << 4));
+          }
+          wave_sync();
+        }
     }
   }
 }
@@ -561,10 +598,10 @@ void slices_of(int steps, int64_t ideal, int& per, int& slices) {
 // Rows of a tile of scores: no more than there are, and as many as still make
 // a tile for every other CU (500 x 2000 scores, 64 columns, f32: the
 // whole call 80 us so, 102 in tiles of 256 rows).
-int score_rows(int64_t T, int64_t V, int type) {
+int score_rows(int64_t T, int64_t V) {
   for (int TT : {256, 128})
     if (T > TT / 2 && up(T, TT) / TT * (up(V, TV) / TV) >= 128) return TT;
-  return type == DT_F32 ? 128 : 32;
+  return 32;
 }
 
 Layout layout_of(int64_t T, int64_t D, int64_t V, int type, bool grads) {
@@ -578,7 +615,7 @@ Layout layout_of(int64_t T, int64_t D, int64_t V, int type, bool grads) {
   l.planes = type == DT_F32 ? 3 : 1;
   l.step = type == DT_F32 ? 16 : BK;
   l.width = up(D, l.step);
-  l.TT = score_rows(T, V, type);
+  l.TT = score_rows(T, V);
   l.Tp = up(T, l.TT);
   l.ticket = take(4);
   l.scale = take(4);
@@ -625,10 +662,9 @@ Panel panel_of(const Mat& X, const Layout& l, bool whole, char* ws, hipStream_t 
 template <bool GRAD, int TYPE>
 void scores(const Scores& sc, int TT, hipStream_t s) {
   const unsigned grid = (unsigned)(up(sc.v1 - sc.v0, TV) / TV * (up(sc.T, TT) / TT));
-  if constexpr (TYPE != DT_F32)
-    if (TT == 32) k_scores<GRAD, TYPE, 32><<<grid, 256, 0, s>>>(sc);
-  if (TT == 128) k_scores<GRAD, TYPE, 128><<<grid, score_threads(TYPE, 128), 0, s>>>(sc);
-  else if (TT == 256) k_scores<GRAD, TYPE, 256><<<grid, 512, 0, s>>>(sc);
+  if (TT == 32) k_scores<GRAD, TYPE, 32><<<grid, 256, 0, s>>>(sc);
+  else if (TT == 128) k_scores<GRAD, TYPE, 128><<<grid, score_threads(TYPE, 128), 0, s>>>(sc);
+  else k_scores<GRAD, TYPE, 256><<<grid, 512, 0, s>>>(sc);
 }
 
 template <bool GRAD>
