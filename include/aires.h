@@ -670,12 +670,13 @@ aires_status aires_linear_xent_workspace(int64_t t, int64_t d, int64_t v, int32_
  * gradients are 0.  row_loss: t fp32 values, or NULL.  loss: one fp32 value.
  * dH and dW have H's and W's sizes and type.
  * Scores, row statistics and sums over rows and classes are fp32; the table
- * is gone through in pieces, whose probabilities go to the workspace in the
- * operands' precision (16 bits for 16-bit operands).  A NaN in a row of
- * H makes that row's loss and dH NaN, and dW with them.
+ * is gone through in pieces, whose dz goes to the workspace in the operands'
+ * precision (16 bits for 16-bit operands, all of fp32's for fp32).  A NaN in a
+ * row of H makes that row's loss and dH NaN, and dW with them.  W is finite.
  * Errors: AIRES_E_INVALID_ARG (NULL, bad type or reduction, ld < ncols, one
  * of dH and dW, grad_scale not finite), AIRES_E_DIM (sizes or types differ,
- * v or d = 0 with t > 0), AIRES_E_UNSUPPORTED (t, d or v >= 2^31),
+ * v or d = 0 with t > 0), AIRES_E_UNSUPPORTED (t or v >= 2^31, d >= 2^21, more
+ * than 2^31 tiles of 32 x 256 scores),
  * AIRES_E_CAPACITY (workspace too small), AIRES_E_HIP.
  */
 aires_status aires_linear_xent(const aires_dense *H, const aires_dense *W, const void *labels, int32_t labels_i64,

@@ -2,6 +2,7 @@
 // launchers of train.h.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <exception>
 #include <vector>
@@ -51,7 +52,9 @@ aires_status check_norm_size(int64_t m, int64_t n) {
 aires_status check_xent_size(int64_t t, int64_t d, int64_t v) {
   if (t < 0 || d < 0 || v < 0 || (t > 0 && (d == 0 || v == 0)))
     return fail(AIRES_E_DIM, "%lld rows, %lld features, %lld classes", (long long)t, (long long)d, (long long)v);
-  if (t >= kMaxSize || d >= kMaxSize || v >= kMaxSize)
+  // a stage's offsets are 32 bits wide, a launch has 2^31 tiles
+  const int64_t tiles = ((t + 31) / 32) * ((v + 255) / 256), outs = ((std::max(t, v) + 127) / 128) * ((d + 127) / 128);
+  if (t >= kMaxSize || v >= kMaxSize || d >= (int64_t(1) << 21) || tiles >= kMaxSize || outs >= kMaxSize / 4)
     return fail(AIRES_E_UNSUPPORTED, "%lld rows, %lld features, %lld classes", (long long)t, (long long)d,
                 (long long)v);
   return AIRES_OK;
