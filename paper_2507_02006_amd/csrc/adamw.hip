@@ -57,7 +57,7 @@ __device__ __forceinline__ int find(const Table& tab, uint32_t b) {
 template <int T, int STRIDE>
 __device__ __forceinline__ void load_all_t(const void* p, int64_t i, float (&x)[PER][4]) {
 #pragma unroll
-  for (int q = 0; q < PER; ++q) load4<T>(p, i + q * STRIDE, x[q]);
+  for (int q = 0; q < PER; ++q) load4<T, true>(p, i + q * STRIDE, x[q]);
 }
 
 template <int STRIDE>
@@ -70,7 +70,7 @@ __device__ __forceinline__ void load_all(const void* p, int t, int64_t i, float 
 template <int T, int STRIDE>
 __device__ __forceinline__ void store_all_t(void* p, int64_t i, const float (&x)[PER][4]) {
 #pragma unroll
-  for (int q = 0; q < PER; ++q) store4<T>(p, i + q * STRIDE, x[q]);
+  for (int q = 0; q < PER; ++q) store4<T, true>(p, i + q * STRIDE, x[q]);
 }
 
 template <int STRIDE>
@@ -210,8 +210,8 @@ __global__ __launch_bounds__(BLOCK) void k_adamw_8(Table tab) {
   if (whole) {
 #pragma unroll
     for (int q = 0; q < PER; ++q) {
-      cm[q] = *reinterpret_cast<const u32_any*>(mc + i0 + q * BLOCK);
-      cv[q] = *reinterpret_cast<const u32_any*>(vc + i0 + q * BLOCK);
+      cm[q] = load_vec<true>(reinterpret_cast<const u32_any*>(mc + i0 + q * BLOCK));
+      cv[q] = load_vec<true>(reinterpret_cast<const u32_any*>(vc + i0 + q * BLOCK));
       sm[q] = t.ms[base / BLOCK + q];
       sv[q] = t.vs[base / BLOCK + q];
     }
@@ -271,8 +271,8 @@ __global__ __launch_bounds__(BLOCK) void k_adamw_8(Table tab) {
   if (whole) {
 #pragma unroll
     for (int q = 0; q < PER; ++q) {
-      *reinterpret_cast<u32_any*>(mc + i0 + q * BLOCK) = cm[q];
-      *reinterpret_cast<u32_any*>(vc + i0 + q * BLOCK) = cv[q];
+      store_vec<true, u32_any>(reinterpret_cast<u32_any*>(mc + i0 + q * BLOCK), cm[q]);
+      store_vec<true, u32_any>(reinterpret_cast<u32_any*>(vc + i0 + q * BLOCK), cv[q]);
     }
     store_all<BLOCK>(t.p, t.pt, i0, p);
     if (t.c) store_all<BLOCK>(t.c, t.ct, i0, p);

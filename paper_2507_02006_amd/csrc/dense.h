@@ -49,31 +49,44 @@ __device__ __forceinline__ void store1(void* p, int t, int64_t i, float x) {
   else store1<DT_F16>(p, i, x);
 }
 
-template <int T>
+// ONCE: the value is not needed again soon; it does not push others out of
+// the caches.
+template <bool ONCE, typename V>
+__device__ __forceinline__ V load_vec(const V* p) {
+  if constexpr (ONCE) return __builtin_nontemporal_load(p);
+  else return *p;
+}
+template <bool ONCE, typename V>
+__device__ __forceinline__ void store_vec(V* p, V v) {
+  if constexpr (ONCE) __builtin_nontemporal_store(v, p);
+  else *p = v;
+}
+
+template <int T, bool ONCE = false>
 __device__ __forceinline__ void load4(const void* p, int64_t i, float x[4]) {
   if constexpr (T == DT_F32) {
-    const f32x4_el v = *reinterpret_cast<const f32x4_el*>(static_cast<const float*>(p) + i);
+    const f32x4_el v = load_vec<ONCE>(reinterpret_cast<const f32x4_el*>(static_cast<const float*>(p) + i));
 #pragma unroll
     for (int k = 0; k < 4; ++k) x[k] = v[k];
   } else {
-    const u16x4_el v = *reinterpret_cast<const u16x4_el*>(static_cast<const uint16_t*>(p) + i);
+    const u16x4_el v = load_vec<ONCE>(reinterpret_cast<const u16x4_el*>(static_cast<const uint16_t*>(p) + i));
 #pragma unroll
     for (int k = 0; k < 4; ++k) x[k] = T == DT_BF16 ? bf16_to_f32(v[k]) : f16_to_f32(v[k]);
   }
 }
 
-template <int T>
+template <int T, bool ONCE = false>
 __device__ __forceinline__ void store4(void* p, int64_t i, const float x[4]) {
   if constexpr (T == DT_F32) {
     f32x4_el v;
 #pragma unroll
     for (int k = 0; k < 4; ++k) v[k] = x[k];
-    *reinterpret_cast<f32x4_el*>(static_cast<float*>(p) + i) = v;
+    store_vec<ONCE>(reinterpret_cast<f32x4_el*>(static_cast<float*>(p) + i), v);
   } else {
     u16x4_el v;
 #pragma unroll
     for (int k = 0; k < 4; ++k) v[k] = T == DT_BF16 ? f32_to_bf16(x[k]) : f32_to_f16(x[k]);
-    *reinterpret_cast<u16x4_el*>(static_cast<uint16_t*>(p) + i) = v;
+    store_vec<ONCE>(reinterpret_cast<u16x4_el*>(static_cast<uint16_t*>(p) + i), v);
   }
 }
 
