@@ -183,74 +183,47 @@ __global__ __launch_bounds__(score_threads(TYPE, TT), 2) void k_scores(Scores s)
 #pragma unroll
             for (int j = 0; j < T_::NT; ++j) acc[i][j][r] = 0.f;
     }
-    if constexpr (PLANES == 1) {
-      // through LDS, so that rows of dz are written 512 bytes at a time
+    // Each wavefront through LDS of its own, 32 rows at a time, so that rows of
+    // dz are written 256 bytes (three planes of 64 entries: 384) at a time.
+    constexpr int IS = PLANES == 1 ? T_::MT : 2;  // tiles of 32 entries at once
+    constexpr int ROW = IS * 64 * PLANES, CH = ROW / 16;
+    static_assert(T_::WAVES * 32 * ROW <= T_::LDS && T_::MT % IS == 0, "dz is staged in the stages' LDS");
+    char* mine = lds + (threadIdx.x >> 6) * (32 * ROW);
+    const int c32 = lane & 31;
 #pragma unroll
-      for (int j = 0; j < T_::NT; ++j) {
-        const int c = T_::col(j);
+    for (int j = 0; j < T_::NT; ++j)
 #pragma unroll
-        for (int i = 0; i < T_::MT; ++i)
+      for (int i0 = 0; i0 < T_::MT; i0 += IS) {
+#pragma unroll
+        for (int i = 0; i < IS; ++i)
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
-            u16x4_el v;
+            float x[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const float x = acc[i][j][q * 4 + k];
-              v[k] = F16 ? f32_to_f16(x) : f32_to_bf16(x);
-            }
-            const int at = T_::row(i, q * 4);
-            *reinterpret_cast<uint64_t*>(lds + c * (TV * 2) + (((at >> 3) ^ (c & 31)) << 4) + (at & 4) * 2) =
-                __builtin_bit_cast(uint64_t, v);
-          }
-      }
-      __syncthreads();
-      const int ch = threadIdx.x & 31;
-      uint16_t* to = s.dz + t0 * s.ldz + (v0 - s.v0) + ch * 8;
-#pragma unroll 4
-      for (int c = threadIdx.x >> 5; c < TT; c += T_::THREADS / 32)
-        *reinterpret_cast<uint4*>(to + c * s.ldz) =
-            *reinterpret_cast<const uint4*>(lds + c * (TV * 2) + ((ch ^ (c & 31)) << 4));
-    } else {
-      // each wavefront through LDS of its own, 64 table entries of 32 rows at a
-      // time: 384 bytes a row with all planes
-      char* mine = lds + (threadIdx.x >> 6) * (32 * 384);
-      static_assert(T_::WAVES * 32 * 384 <= T_::LDS && T_::MT % 2 == 0, "dz is staged in the stages' LDS");
-      const int c32 = lane & 31;
+            for (int k = 0; k < 4; ++k) x[k] = acc[i0 + i][j][q * 4 + k];
 #pragma unroll
-      for (int j = 0; j < T_::NT; ++j)
+            for (int p = 0; p < PLANES; ++p) {
+              u16x4_el v;
 #pragma unroll
-        for (int i0 = 0; i0 < T_::MT; i0 += 2) {
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              float x[4];
-#pragma unroll
-              for (int k = 0; k < 4; ++k) x[k] = acc[i0 + i][j][q * 4 + k];
-#pragma unroll
-              for (int p = 0; p < 3; ++p) {
-                u16x4_el v;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                  v[k] = f32_to_bf16(x[k]);
-                  x[k] -= bf16_to_f32(v[k]);
-                }
-                // 16 columns of a plane: chunks 6 (2 i + q / 2) + 2 p and the next
-                const int ch = 6 * (2 * i + (q >> 1)) + 2 * p + (q & 1);
-                *reinterpret_cast<uint64_t*>(mine + c32 * 384 + ((ch ^ (c32 & 7)) << 4) + (lane >> 5) * 8) =
-                    __builtin_bit_cast(uint64_t, v);
+              for (int k = 0; k < 4; ++k) {
+                v[k] = F16 ? f32_to_f16(x[k]) : f32_to_bf16(x[k]);
+                if constexpr (PLANES > 1) x[k] -= bf16_to_f32(v[k]);
               }
+              // 16 columns of a plane are two chunks
+              const int ch = (2 * i + (q >> 1)) * (2 * PLANES) + 2 * p + (q & 1);
+              *reinterpret_cast<uint64_t*>(mine + c32 * ROW + ((ch ^ (c32 & 7)) << 4) + (lane >> 5) * 8) =
+                  __builtin_bit_cast(uint64_t, v);
             }
-          wave_sync();
-          uint16_t* to = s.dz + (t0 + T_::col(j) - c32) * s.ldz + (v0 - s.v0 + wm * SPAN + i0 * 32) * 3;
-          for (int it = lane; it < 32 * 24; it += 64) {
-            const int r = it / 24, ch = it % 24;
-            *reinterpret_cast<uint4*>(to + r * s.ldz + ch * 8) =
-                *reinterpret_cast<const uint4*>(mine + r * 384 + ((ch ^ (r & 7)) << 4));
           }
-          wave_sync();
+        wave_sync();
+        uint16_t* to = s.dz + (t0 + T_::col(j) - c32) * s.ldz + (v0 - s.v0 + wm * SPAN + i0 * 32) * PLANES;
+        for (int it = lane; it < 32 * CH; it += 64) {
+          const int r = it / CH, ch = it % CH;
+          *reinterpret_cast<uint4*>(to + r * s.ldz + ch * 8) =
+              *reinterpret_cast<const uint4*>(mine + r * ROW + ((ch ^ (r & 7)) << 4));
         }
-    }
+        wave_sync();
+      }
   }
 }
 
@@ -629,11 +602,19 @@ Layout layout_of(int64_t T, int64_t D, int64_t V, int type, bool grads) {
   if (grads) {
     l.piece = std::min(up(V, TV), std::max<int64_t>(TV, kPieceBytes / (2 * l.planes * std::max<int64_t>(l.Tp, 1)) / TV * TV));
     const int dh_steps = (int)(up(std::min(l.piece, V), l.step) / l.step), dw_steps = (int)(up(T, l.step) / l.step);
-    // small tiles where a side would leave half of a large one empty
-    l.G = std::min({T, D, V}) <= 128 ? 128 : 256;
-    // shares of k of about equal length, one workgroup (of 256, else two) a CU
-    const int64_t nx = up(D, l.G) / l.G, th = up(T, l.G) / l.G * nx, tw = up(std::min(l.piece, V), l.G) / l.G * nx;
-    const int64_t ideal = std::max<int64_t>(l.planes == 1 ? 4 : 8, (th * dh_steps + tw * dw_steps) / (l.G == 256 ? 256 : 512));
+    // Shares of k of about equal length, one workgroup a CU with large tiles,
+    // two with small ones; none shorter than `least` steps.  Small tiles where
+    // a side would leave half of a large one empty, or where large ones do not
+    // make twice that share for every CU (300 x 130 x 3000 bf16: 54 us for the
+    // call with large ones, 44 with small ones; 4099 x 256 x 30011 f32 1581 and
+    // 1893).
+    const int64_t least = l.planes == 1 ? 4 : 8;
+    auto work = [&](int64_t G) {
+      const int64_t nx = up(D, G) / G;
+      return up(T, G) / G * nx * dh_steps + up(std::min(l.piece, V), G) / G * nx * dw_steps;
+    };
+    l.G = std::min({T, D, V}) <= 128 || work(256) < 256 * 2 * least ? 128 : 256;
+    const int64_t ideal = std::max<int64_t>(least, work(l.G) / (l.G == 256 ? 256 : 512));
     slices_of(dh_steps, ideal, l.dh_per, l.dh_slices);
     slices_of(dw_steps, ideal, l.dw_per, l.dw_slices);
     if (l.dh_slices > 1 || l.piece < V) l.dh = take(4 * l.dh_slices * T * l.width);
