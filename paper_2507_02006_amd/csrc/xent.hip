@@ -224,6 +224,13 @@ __global__ __launch_bounds__(score_threads(TYPE, TT), 2) void k_scores(Scores s)
         }
         wave_sync();
       }
+    // The products of 16-bit operands read 64 rows of dz a step: behind an odd
+    // number of tiles of 32 the other half of the last step is zeros.
+    if constexpr (PLANES == 1 && TT < BK)
+      if (tt == (s.T - 1) / TT && (t0 + TT) % BK != 0)
+        for (int it = threadIdx.x; it < (BK - TT) * (TV / 8); it += T_::THREADS)
+          *reinterpret_cast<uint4*>(s.dz + (t0 + TT + it / (TV / 8)) * s.ldz + (v0 - s.v0) + it % (TV / 8) * 8) =
+              make_uint4(0, 0, 0, 0);
   }
 }
 
@@ -589,7 +596,7 @@ Layout layout_of(int64_t T, int64_t D, int64_t V, int type, bool grads) {
   l.step = type == DT_F32 ? 16 : BK;
   l.width = up(D, l.step);
   l.TT = score_rows(T, V);
-  l.Tp = up(T, l.TT);
+  l.Tp = up(T, std::max<int64_t>(l.TT, l.step));
   l.ticket = take(4);
   l.scale = take(4);
   l.top = take(4 * T);

@@ -289,6 +289,19 @@ def test_linear_xent_few_rows_or_classes(t, d, v, dt):
     xent_check(aires.linear_xent(H.cuda(), wide[:, 1:d + 1], y.cuda(), grads=False), ref, False)
 
 
+@pytest.mark.parametrize("dt", [F32, BF16, F16])
+@pytest.mark.parametrize("t,d,v", [(32, 64, 1000), (96, 64, 1000), (160, 128, 700), (224, 40, 300), (64, 64, 300),
+                                   (65, 72, 2000), (31, 8, 70), (352, 256, 9000)])
+def test_linear_xent_rows_at_the_end_of_a_step(t, d, v, dt):
+    """Row numbers that fill tiles of scores but not the steps of the gradients' products."""
+    H, W, y = xent_data(t, d, v, dt, 5 * t + d + v)
+    y[-1] = v - 1
+    ref = xent_ref(H, W, y)
+    filled = torch.full((1 << 22,), float("nan"), dtype=dt, device="cuda")  # what the workspace may find
+    del filled
+    xent_check(aires.linear_xent(H.cuda(), W.cuda(), y.cuda()), ref)
+
+
 def test_linear_xent_large_table():
     """More of the table than one piece of the workspace holds."""
     t, d, v = 3000, 40, 150001
