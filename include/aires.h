@@ -672,12 +672,13 @@ aires_status aires_linear_xent_workspace(int64_t t, int64_t d, int64_t v, int32_
  * Scores, row statistics and sums over rows and classes are fp32; the table
  * is gone through in pieces, whose dz goes to the workspace in the operands'
  * precision (16 bits for 16-bit operands, all of fp32's for fp32).  A NaN in a
- * row of H makes that row's loss and dH NaN, and dW with them.  W is finite.
+ * row of H makes that row's loss and dH NaN, if it has a label, and dW in any
+ * case (its share of dW is 0 times NaN).  W is finite.
  * Errors: AIRES_E_INVALID_ARG (NULL, bad type or reduction, ld < ncols, one
  * of dH and dW, grad_scale not finite), AIRES_E_DIM (sizes or types differ,
- * v or d = 0 with t > 0), AIRES_E_UNSUPPORTED (t or v >= 2^31, d >= 2^21, more
- * than 2^31 tiles of 32 x 256 scores),
- * AIRES_E_CAPACITY (workspace too small), AIRES_E_HIP.
+ * v or d = 0 with t > 0), AIRES_E_UNSUPPORTED (t > 2^29, v >= 2^31, d >= 2^21,
+ * H or W of more than 2^23 blocks of 128 x 128), AIRES_E_CAPACITY
+ * (workspace too small), AIRES_E_HIP.
  */
 aires_status aires_linear_xent(const aires_dense *H, const aires_dense *W, const void *labels, int32_t labels_i64,
                                int32_t reduction, double grad_scale, float *loss, float *row_loss,

@@ -52,9 +52,10 @@ aires_status check_norm_size(int64_t m, int64_t n) {
 aires_status check_xent_size(int64_t t, int64_t d, int64_t v) {
   if (t < 0 || d < 0 || v < 0 || (t > 0 && (d == 0 || v == 0)))
     return fail(AIRES_E_DIM, "%lld rows, %lld features, %lld classes", (long long)t, (long long)d, (long long)v);
-  // a stage's offsets are 32 bits wide, a launch has 2^31 tiles
-  const int64_t tiles = ((t + 31) / 32) * ((v + 255) / 256), outs = ((std::max(t, v) + 127) / 128) * ((d + 127) / 128);
-  if (t >= kMaxSize || v >= kMaxSize || d >= (int64_t(1) << 21) || tiles >= kMaxSize || outs >= kMaxSize / 4)
+  // a stage's offsets are 32 bits wide, a launch has fewer than 2^32 threads
+  // (tiles of 128 x 128 of a gradient are 2^23 at most)
+  const int64_t outs = ((std::max(t, v) + 127) / 128) * ((d + 127) / 128);
+  if (t > (int64_t(1) << 29) || v >= kMaxSize || d >= (int64_t(1) << 21) || outs > (int64_t(1) << 23))
     return fail(AIRES_E_UNSUPPORTED, "%lld rows, %lld features, %lld classes", (long long)t, (long long)d,
                 (long long)v);
   return AIRES_OK;

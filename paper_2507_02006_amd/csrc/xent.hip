@@ -378,8 +378,9 @@ __global__ __launch_bounds__(ROWS * SLICES) void k_rows(Rows a) {
 }
 
 // Rows of a workgroup: 8 with 128 threads each for few rows, 16 with 64 where
-// a row has many tiles, 64 with 4 where it has few.
-int rows_of(int64_t T, int64_t tiles) { return T <= 2048 ? 8 : tiles >= 32 ? 16 : 64; }
+// a row has many tiles, 64 with 4 where it has few or the launch would be too
+// large.
+int rows_of(int64_t T, int64_t tiles) { return T <= 2048 ? 8 : tiles >= 32 && T <= (1 << 24) ? 16 : 64; }
 
 }  // namespace
 
@@ -684,16 +685,21 @@ hipError_t linear_xent(const XentArgs& x, hipStream_t s) {
   if (T > 0) {
     sc.H = panel_of(x.H, l, true, ws + l.h, s);
     sc.W = panel_of(x.W, l, false, ws + l.w, s);
-    sc.T = T; sc.V = V; sc.v0 = 0; sc.v1 = V;
+    sc.T = T; sc.V = V;
     sc.steps = (int)(l.width / l.step);
-    sc.part = (float2*)(ws + l.part);
     sc.labels = x.labels; sc.i64 = x.labels_i64;
     sc.ticket = (uint32_t*)(ws + l.ticket);
-    scores<false>(sc, type, l.TT, s);
+    // (a launch holds fewer than 2^32 threads)
+    const int64_t most = std::max<int64_t>(1, (int64_t(1) << 22) / (up(T, l.TT) / l.TT)) * TV;
+    for (int64_t v0 = 0; v0 < V; v0 += most) {
+      sc.v0 = v0; sc.v1 = std::min(V, v0 + most);
+      sc.part = (float2*)(ws + l.part) + v0 / TV * T;
+      scores<false>(sc, type, l.TT, s);
+    }
   }
   float *top = (float*)(ws + l.top), *inv = (float*)(ws + l.inv);
   // fp16 dz is held times F16_UP
-  rows_and_loss(x, sc.part, up(V, TV) / TV, top, inv, x.row_loss ? x.row_loss : (float*)(ws + l.rows), ws + l.sums,
+  rows_and_loss(x, (float2*)(ws + l.part), up(V, TV) / TV, top, inv, x.row_loss ? x.row_loss : (float*)(ws + l.rows), ws + l.sums,
                 sc.ticket, x.grad_scale * (f16 ? 1.f / F16_UP : 1.f), scale, s);
   if (!grads) return hipGetLastError();
   if (T == 0) {

@@ -310,6 +310,19 @@ def test_linear_xent_large_table():
         xent_check(aires.linear_xent(H.cuda(), W.cuda(), y.cuda()), xent_ref(H, W, y))
 
 
+def test_linear_xent_more_scores_than_a_launch_holds():
+    """2^23 tiles of 256 x 256 scores: as many threads as a launch may not have."""
+    t, d, v = (1 << 19) + 5, 8, 1 << 20
+    H, W, y = xent_data(t, d, v, BF16, 13)
+    H, W, y = H.cuda(), W.cuda(), y.cuda()
+    got = aires.linear_xent(H, W, y, grads=False)
+    some = torch.cat([torch.arange(100), torch.arange(t - 100, t)]).cuda()
+    ref = xent_ref(H[some], W, y[some])
+    near(got.row_loss[some], *ref["row_loss"], "row_loss")
+    there = ((y >= 0) & (y < v)).sum()
+    near(got.loss, got.row_loss.double().sum() / there, 4 * U * got.row_loss.double().sum() / there, "loss")
+
+
 @pytest.mark.parametrize("dt", [F32, BF16, F16])
 def test_linear_xent_reductions_and_scale(dt):
     H, W, y = xent_data(90, 50, 70, dt, 4)

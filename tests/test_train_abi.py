@@ -99,6 +99,13 @@ def test_linear_xent_sizes(lib):
     assert lib.aires_linear_xent_workspace(8, 8, 8, 5, 1, ctypes.byref(n)) == B_.E_INVALID_ARG
 
 
+def test_linear_xent_sizes_that_no_launch_holds(lib):
+    n = ctypes.c_int64()
+    q = lambda t, d, v, g=1: lib.aires_linear_xent_workspace(t, d, v, 1, g, ctypes.byref(n))  # noqa: E731
+    assert q(2 ** 29 + 1, 8, 100) == q(2 ** 20, 2 ** 20, 8) == q(8, 2 ** 20, 2 ** 20) == B_.E_UNSUPPORTED
+    assert q(2 ** 29, 8, 100) == q(2 ** 19, 8, 2 ** 30, 0) == B_.OK
+
+
 def test_adamw(lib):
     o = dict(struct_size=ctypes.sizeof(B_.AdamWOpts), seed=0, step=1, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8,
              weight_decay=0.0, grad_scale=1.0)
