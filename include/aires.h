@@ -613,11 +613,10 @@ typedef struct aires_dense {
  * ones and zeros.  Y (same size as X) may have another type.  mean, rstd: m
  * fp32 values each, both NULL if not wanted (the backward pass reads them).
  * A row whose values are all equal gives y = beta up to the rounding of mu
- * (r = eps^-1/2); a NaN or
- * an infinity makes its own row NaN and no other.
+ * (r = eps^-1/2); a NaN or an infinity makes its own row NaN and no other.
  * Errors: AIRES_E_INVALID_ARG (NULL, bad type, ld < ncols, eps negative or
  * not finite, only one of mean and rstd), AIRES_E_DIM (sizes differ),
- * AIRES_E_UNSUPPORTED (n >= 2^31), AIRES_E_HIP.
+ * AIRES_E_UNSUPPORTED (m > 2^40, n > 2^30), AIRES_E_HIP.
  */
 aires_status aires_layer_norm(const aires_dense *X, const void *gamma, const void *beta, int32_t w_dtype, double eps,
                               const aires_dense *Y, float *mean, float *rstd, void *stream);
@@ -734,7 +733,7 @@ typedef struct aires_adamw_opts {
  * not finite are stored as NaN and leave their block's scale alone.
  * Errors: AIRES_E_INVALID_ARG (NULL, bad type or struct_size, step < 1,
  * betas outside [0, 1), options not finite, eps < 0, one scale without the
- * other), AIRES_E_DIM (negative n), AIRES_E_UNSUPPORTED (n above 2^40),
+ * other), AIRES_E_DIM (negative n), AIRES_E_UNSUPPORTED (n above 2^35),
  * AIRES_E_OOM (host memory), AIRES_E_HIP.
  */
 aires_status aires_adamw(const aires_adamw_tensor *tensors, int64_t count, const aires_adamw_opts *opts,

@@ -81,12 +81,15 @@ __device__ __forceinline__ void store_all(void* p, int t, int64_t i, const float
 }
 
 // New moments, and the parameter from them.  The square root and the
-// reciprocal are the hardware's, within one unit in the last place.
+// reciprocal are the hardware's, within one unit in the last place; the square
+// root takes denormal numbers for 0, so small ones are raised by 2^64 before.
 __device__ __forceinline__ void update(const AdamWStep& o, float g, float& p, float& m, float& v) {
   g *= o.grad_scale;
   m = m * o.beta1 + g * o.one_beta1;
   v = v * o.beta2 + (g * g) * o.one_beta2;
-  const float den = __builtin_amdgcn_sqrtf(v) * o.inv_root + o.eps;
+  const bool low = v < 0x1p-96f;
+  const float root = __builtin_amdgcn_sqrtf(low ? v * 0x1p64f : v) * (low ? 0x1p-32f : 1.f);
+  const float den = root * o.inv_root + o.eps;
   p = p * o.decay - o.rate * (m * __builtin_amdgcn_rcpf(den));
 }
 
@@ -306,7 +309,7 @@ uint32_t adamw_seed(uint32_t seed, int64_t tensor) {
 }
 
 hipError_t adamw(const AdamWTensor* tensors, int64_t count, const AdamWStep& step, hipStream_t s) {
-  constexpr int64_t kMost = int64_t(1) << 30;  // workgroups of a launch
+  constexpr int64_t kMost = int64_t(1) << 23;  // workgroups of a launch (2^31 threads), and of a tensor at most
   for (int eight = 0; eight < 2; ++eight) {
     Table tab;
     tab.o = step;

@@ -45,7 +45,9 @@ kern::Mat mat(const aires_dense* m) {
 
 aires_status check_norm_size(int64_t m, int64_t n) {
   if (m < 0 || n < 0) return fail(AIRES_E_DIM, "%lld rows of %lld columns", (long long)m, (long long)n);
-  if (n >= kMaxSize) return fail(AIRES_E_UNSUPPORTED, "%lld columns", (long long)n);
+  // (column numbers are 32 bits wide, and stepped on past the last)
+  if (m > (int64_t(1) << 40) || n > (int64_t(1) << 30))
+    return fail(AIRES_E_UNSUPPORTED, "%lld rows of %lld columns", (long long)m, (long long)n);
   return AIRES_OK;
 }
 
@@ -178,7 +180,7 @@ aires_status aires_adamw(const aires_adamw_tensor* tensors, int64_t count, const
     if (!type_ok(t.param_dtype) || !type_ok(t.grad_dtype) || (t.copy && !type_ok(t.copy_dtype)))
       return fail(AIRES_E_INVALID_ARG, "tensor %lld: invalid type", at);
     if (t.n == 0) continue;
-    if (t.n > (int64_t(1) << 40)) return fail(AIRES_E_UNSUPPORTED, "tensor %lld has %lld values", at, (long long)t.n);
+    if (t.n > (int64_t(1) << 35)) return fail(AIRES_E_UNSUPPORTED, "tensor %lld has %lld values", at, (long long)t.n);
     if (!t.param || !t.grad || !t.exp_avg || !t.exp_avg_sq)
       return fail(AIRES_E_INVALID_ARG, "tensor %lld: NULL array", at);
     if (!t.exp_avg_scale != !t.exp_avg_sq_scale)

@@ -590,6 +590,22 @@ def test_adamw_values_that_are_not_finite_stay_where_they_are():
     assert bool((P[0] == np.float32(1 - 0.005)).all())
 
 
+def test_adamw_second_moments_below_normal_numbers():
+    """With eps = 0 the step is m / sqrt(v) however small v is (and the call's own weight decay, 0.01)."""
+    n, b1, b2, lr = 5000, 0.9, 0.999, 1e-2
+    g = (10.0 ** (-18 - 4 * torch.rand(n, generator=gen(21), dtype=torch.float64))).float()
+    p = [torch.ones(n, device="cuda")]
+    M, V = aires.adamw_state(p)
+    aires.adamw(p, [g.cuda()], M, V, step=1, lr=lr, betas=(b1, b2), eps=0.0)
+    m, v = f64(M[0]), f64(V[0])
+    some = v > 0  # (below 2^-149 / 1e-3 a square is lost)
+    assert some.mean() > 0.5 and (v[some] < 2.0 ** -126).any()
+    want = 1 - lr * 0.01 - lr / (1 - b1) * m / (np.sqrt(v, where=some, out=np.ones(n)) / np.sqrt(1 - b2))
+    got = f64(p[0])
+    # ten roundings of the step, and the parameter's own; b1 and b2 themselves are rounded
+    assert np.all(np.abs(got - want)[some] <= 16 * U * (1 + 1e3 * np.abs(want - 1)[some]))
+
+
 def test_adamw_many_tensors_and_offsets():
     """More tensors than one launch describes, 8- and 32-bit moments mixed,
     views at odd offsets: the same as one by one."""

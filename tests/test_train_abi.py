@@ -129,3 +129,16 @@ def test_adamw(lib):
         assert call(t=bad) == B_.E_INVALID_ARG
     assert call(t=dict(n=-1)) == B_.E_DIM
     assert call(t=dict(n=2 ** 41)) == B_.E_UNSUPPORTED
+
+
+def test_layer_norm_sizes(lib):
+    n = ctypes.c_int64()
+    q = lambda m, c: lib.aires_layer_norm_workspace(m, c, ctypes.byref(n))  # noqa: E731
+    assert q(1, 2 ** 30) == q(2 ** 40, 1) == B_.OK
+    assert q(1, 2 ** 30 + 1) == q(1, 2 ** 31 - 1) == q(2 ** 40 + 1, 1) == q(2 ** 62, 2 ** 31) == B_.E_UNSUPPORTED
+
+
+def test_adamw_sizes(lib):
+    row = B_.AdamWTensor(2 ** 35 + 1, FAKE, FAKE, FAKE, FAKE, None, None, None, 0, 0, 0, 0)
+    opts = B_.AdamWOpts(ctypes.sizeof(B_.AdamWOpts), 0, 1, 1e-3, 0.9, 0.999, 1e-8, 0.0, 1.0)
+    assert lib.aires_adamw(ctypes.addressof(row), 1, ctypes.byref(opts), None) == B_.E_UNSUPPORTED
