@@ -9,6 +9,10 @@
 // rounding), so bandwidth bounds it.  The tensors' descriptors travel as
 // kernel arguments; a workgroup finds its tensor from its number and updates
 // 4096 values, all of whose loads are issued before the first is used.
+// Measured: 32-bit moments, bf16 gradients and copies, 262144 x 512 values, 630
+// us (6.0 TB/s of 28 bytes a value); 8-bit moments, bf16 gradients, 1048576 x
+// 256 values, 620 to 640 us (5.9 to 6.1 TB/s of 14 bytes a value); 19 tensors of
+// 1.4 million values in all, f32, 7 us.
 //
 // 8-bit moments: blocks of 256 values share a scale, so that a block is four
 // values a lane of one wavefront and its maximum a scan within the registers.

