@@ -53,10 +53,10 @@ struct Few {
   uint32_t* ticket;                 // cleared by STATS
   float* part;                      // [workgroup][NK][Dp]: shares of dK
   // CLASSES
-  const int* counts; int ncounts;
+  const int* counts; int ncounts;   // TRAIN: labelled rows; ncounts = 0: counted here
   int mean; float grad_scale;
   float* row_loss;
-  double* sums;                     // a workgroup's share of the loss
+  double2* sums;                    // a workgroup's losses and labelled rows
   // STATS, DZ
   float2* stats;                    // [workgroup][NK]: maximum, sum (base 2)
   const float* top; const float* inv;
@@ -75,7 +75,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_few(Few a) {
   __shared__ __attribute__((aligned(16))) float z[WAVES][TB][ZS];
   __shared__ __attribute__((aligned(16))) float dz[GRAD ? TB : 1][ZS];
   __shared__ __attribute__((aligned(16))) float hall[GRAD ? WAVES : 1][GRAD ? TB : 1][HS];
-  __shared__ int total;
+  __shared__ int totals[WAVES];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n16 = lane & 15, q = lane >> 4;
   const int p16 = tid & 15;                         // kept rows p16 + 16 k are this thread's between the products
   float(*const h)[HS] = hall[GRAD ? wave : 0];
@@ -83,18 +83,24 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_few(Few a) {
   const int D = a.D, NK = a.NK;
 
   float scale = 1.f;
-  double div = 1.0;
-  if constexpr (CLASSES) {
-    if (wave == 0) {
-      int c = 0;
+  if constexpr (MODE == FEW_CLASSES_TRAIN) {
+    int c = 0;
+    if (a.ncounts == 0) {
+      for (int64_t t = tid; t < N; t += THREADS) {
+        const int64_t l = label_at(a.labels, a.i64, t);
+        c += l >= 0 && l < NK;
+      }
+    } else if (wave == 0) {
       for (int i = lane; i < a.ncounts; i += 64) c += a.counts[i];
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) c += __shfl_xor(c, o);
-      if (lane == 0) total = c;
     }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) c += __shfl_xor(c, o);
+    if (lane == 0) totals[wave] = c;
     __syncthreads();
-    div = a.mean ? (double)(total > 0 ? total : 1) : 1.0;
-    scale = (float)(a.grad_scale / div);
+    c = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) c += totals[w];
+    scale = (float)(a.grad_scale / (a.mean && c > 0 ? (double)c : 1.0));
     if (blockIdx.x == 0 && tid == 0) *a.scale = scale;
   }
   if constexpr (MODE == FEW_DZ) scale = *a.scale;
@@ -198,7 +204,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_few(Few a) {
   };
 
   const int64_t blocks = (N + TB - 1) / TB;
-  double loss = 0;
+  double2 loss = {0, 0};
   int64_t b = blockIdx.x;
   if (b < blocks) fetch(b * TB);
   for (; b < blocks; b += gridDim.x) {
@@ -278,7 +284,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_few(Few a) {
         if (p16 == 0 && row < N) {
           const float x = there ? (big + log2f(sum)) * LN2 - target : 0.f;
           a.row_loss[row] = x;
-          loss += x;
+          loss.x += x;
+          loss.y += there ? 1.0 : 0.0;
         }
       }
       if constexpr (MODE == FEW_STATS) {
@@ -385,14 +392,16 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_few(Few a) {
   }
 
   if constexpr (CLASSES) {
-    __shared__ double sums[WAVES];
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) loss += __shfl_xor(loss, o);
+    __shared__ double2 sums[WAVES];
+    loss = wave_sum2(loss);
     if (lane == 0) sums[wave] = loss;
     __syncthreads();
     if (tid == 0) {
-      for (int i = 1; i < WAVES; ++i) loss += sums[i];
-      a.sums[blockIdx.x] = loss / div;
+      for (int i = 1; i < WAVES; ++i) {
+        loss.x += sums[i].x;
+        loss.y += sums[i].y;
+      }
+      a.sums[blockIdx.x] = loss;
     }
   }
 }

@@ -10,9 +10,17 @@ namespace aires {
 namespace kern {
 
 // out (rows x cols of `type`) = *scale times the sum of fp32 slices
-// [slice][rows][ldp], in a fixed order; ldp a multiple of 4.
-void finish(const float* part, int slices, int64_t rows, int64_t cols, int64_t ldp, const float* scale, void* out,
-            int type, int64_t ldo, hipStream_t s);
+// [slice][rows][ldp], in a fixed order; ldp a multiple of 4.  part NULL: none.
+struct Finish {
+  const float* part; int slices;
+  int64_t rows, cols, ldp;
+  void* out; int type; int64_t ldo;
+};
+
+// Both, and the loss from `sums` (losses, labelled rows) where that is given, in
+// one launch.
+void finish(const Finish& a, const Finish& b, const float* scale, const double2* sums, int nsums, int mean, float* loss,
+            hipStream_t s);
 
 // Rows' maxima, inverse sums and losses from the statistics [tile][t] of
 // `tiles` tiles of the table, the loss, and *scale = grad_scale / c.  *ticket
@@ -39,6 +47,15 @@ __device__ __forceinline__ int64_t label_at(const void* labels, int i64, int64_t
 }
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+__device__ __forceinline__ double2 wave_sum2(double2 v) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    v.x += __shfl_xor(v.x, o);
+    v.y += __shfl_xor(v.y, o);
+  }
+  return v;
+}
 
 // Joins two (maximum, sum of exponentials) in base 2; equal maxima (of minus
 // infinity too) need no scaling.

@@ -40,12 +40,24 @@ constexpr float F16_UP = 1024.f;       // dz in fp16 is held times this: 2^-35 i
 
 // ---------------------------------------------------------------- operands
 
-// Rows of X at a stride of `width` columns, zeros past the end: 16-bit values
-// as they are, fp32 as three planes of bf16 (tile.h).
+// Rows of X and Y at a stride of `width` columns, zeros past the end: 16-bit
+// values as they are, fp32 as three planes of bf16 (tile.h).  The first
+// `first` workgroups take X.
+struct Pack {
+  Mat X, Y;
+  uint16_t *x, *y;
+  int64_t width;
+  unsigned first;
+};
+
 template <bool PLANES>
-__global__ __launch_bounds__(256) void k_pack(Mat X, uint16_t* to, int64_t width) {
-  const int64_t per = width / 4, total = X.rows * per;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+__global__ __launch_bounds__(256) void k_pack(Pack a) {
+  const bool is_x = blockIdx.x < a.first;
+  const Mat X = is_x ? a.X : a.Y;
+  uint16_t* const to = is_x ? a.x : a.y;
+  const int64_t width = a.width, per = width / 4, total = X.rows * per;
+  const int64_t b = is_x ? blockIdx.x : blockIdx.x - a.first, step = is_x ? a.first : gridDim.x - a.first;
+  for (int64_t i = b * 256 + threadIdx.x; i < total; i += step * 256) {
     const int64_t r = i / per, c = (i - r * per) * 4, at = r * X.ld + c;
     if constexpr (!PLANES) {
       const uint16_t* x = static_cast<const uint16_t*>(X.data);
@@ -275,15 +287,6 @@ __device__ __forceinline__ float label_score(const Rows& a, int64_t row, int64_t
   return group_sum_f32<LPR>(s);
 }
 
-__device__ __forceinline__ double2 wave_sum2(double2 v) {
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    v.x += __shfl_xor(v.x, o);
-    v.y += __shfl_xor(v.y, o);
-  }
-  return v;
-}
-
 // The workgroups' shares of the loss in a fixed order, by one workgroup.
 template <int THREADS>
 __device__ __forceinline__ void total_loss(const Rows& a, int64_t n) {
@@ -507,29 +510,26 @@ void gradients(const Gradients& g, int G, hipStream_t s) {
 // out = scale times the sum of the slices; GROUPS threads to an element's
 // slices (16 where there are many).
 template <int GROUPS>
-__global__ __launch_bounds__(256) void k_finish(const float* part, int slices, int64_t rows, int64_t cols, int64_t ldp,
-                                                const float* scale, void* out, int type, int64_t ldo) {
+__device__ __forceinline__ void finish_part(const Finish& f, float k, int64_t b, int64_t blocks, float4* buf) {
   constexpr int ITEMS = 256 / GROUPS;
-  __shared__ float4 buf[GROUPS][ITEMS];
-  const int64_t per = (cols + 3) / 4, total = rows * per;
+  const int64_t per = (f.cols + 3) / 4, total = f.rows * per;
   const int item = threadIdx.x % ITEMS, group = threadIdx.x / ITEMS;
-  const float k = *scale;
-  for (int64_t i0 = (int64_t)blockIdx.x * ITEMS; i0 < total; i0 += (int64_t)gridDim.x * ITEMS) {
+  for (int64_t i0 = b * ITEMS; i0 < total; i0 += blocks * ITEMS) {
     const int64_t i = i0 + item, r = i / per, c = (i - r * per) * 4;
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
     if (i < total) {
 #pragma unroll 4
-      for (int s = group; s < slices; s += GROUPS) {
-        const float4 v = *reinterpret_cast<const float4*>(part + (s * rows + r) * ldp + c);
+      for (int s = group; s < f.slices; s += GROUPS) {
+        const float4 v = *reinterpret_cast<const float4*>(f.part + (s * f.rows + r) * f.ldp + c);
         x.x += v.x; x.y += v.y; x.z += v.z; x.w += v.w;
       }
     }
     if constexpr (GROUPS > 1) {
-      buf[group][item] = x;
+      buf[threadIdx.x] = x;
       __syncthreads();
       if (group == 0)
         for (int q = 1; q < GROUPS; ++q) {
-          const float4 v = buf[q][item];
+          const float4 v = buf[q * ITEMS + item];
           x.x += v.x; x.y += v.y; x.z += v.z; x.w += v.w;
         }
       __syncthreads();
@@ -538,20 +538,60 @@ __global__ __launch_bounds__(256) void k_finish(const float* part, int slices, i
     const float o[4] = {x.x * k, x.y * k, x.z * k, x.w * k};
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (c + j < cols) store1(out, type, r * ldo + c + j, o[j]);
+      if (c + j < f.cols) store1(f.out, f.type, r * f.ldo + c + j, o[j]);
   }
+}
+
+// The loss from workgroups' shares and labelled rows, in a fixed order.
+__device__ __forceinline__ void sum_shares(const double2* sums, int n, int mean, float* loss, double2* buf) {
+  double2 x = {0, 0};
+  for (int i = threadIdx.x; i < n; i += 256) {
+    x.x += sums[i].x;
+    x.y += sums[i].y;
+  }
+  x = wave_sum2(x);
+  if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = x;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  for (int i = 1; i < 4; ++i) {
+    x.x += buf[i].x;
+    x.y += buf[i].y;
+  }
+  *loss = (float)(mean && x.y > 0 ? x.x / x.y : x.x);
+}
+
+// Up to two gradients and the loss in one launch: workgroups of the first, of
+// the second, and one.
+struct FinishAll {
+  Finish a, b;
+  unsigned first, second;
+  const float* scale;
+  const double2* sums; int nsums, mean;
+  float* loss;
+};
+
+__global__ __launch_bounds__(256) void k_finish(FinishAll f) {
+  __shared__ float4 buf[256];
+  if (blockIdx.x >= f.first + f.second) return sum_shares(f.sums, f.nsums, f.mean, f.loss, reinterpret_cast<double2*>(buf));
+  const bool is_a = blockIdx.x < f.first;
+  const Finish w = is_a ? f.a : f.b;
+  const int64_t b = is_a ? blockIdx.x : blockIdx.x - f.first, blocks = is_a ? f.first : f.second;
+  const float k = *f.scale;
+  if (w.slices > 8) finish_part<16>(w, k, b, blocks, buf);
+  else finish_part<1>(w, k, b, blocks, buf);
 }
 
 }  // namespace
 
-void finish(const float* part, int slices, int64_t rows, int64_t cols, int64_t ldp, const float* scale, void* out,
-            int type, int64_t ldo, hipStream_t s) {
-  const int64_t items = rows * ((cols + 3) / 4);
-  const unsigned most = 8192;
-  if (slices > 8)
-    k_finish<16><<<(unsigned)std::min<int64_t>(most, (items + 15) / 16), 256, 0, s>>>(part, slices, rows, cols, ldp, scale, out, type, ldo);
-  else
-    k_finish<1><<<(unsigned)std::min<int64_t>(most, (items + 255) / 256), 256, 0, s>>>(part, slices, rows, cols, ldp, scale, out, type, ldo);
+void finish(const Finish& a, const Finish& b, const float* scale, const double2* sums, int nsums, int mean,
+            float* loss, hipStream_t s) {
+  auto blocks = [](const Finish& f) {
+    const int64_t items = f.part ? f.rows * ((f.cols + 3) / 4) : 0, per = f.slices > 8 ? 16 : 256;
+    return (unsigned)std::min<int64_t>(8192, (items + per - 1) / per);
+  };
+  const FinishAll f{a, b, blocks(a), blocks(b), scale, sums, nsums, mean, loss};
+  const unsigned grid = f.first + f.second + (sums ? 1 : 0);
+  if (grid) k_finish<<<grid, 256, 0, s>>>(f);
 }
 
 namespace {
@@ -641,18 +681,30 @@ Layout layout_of(int64_t T, int64_t D, int64_t V, int type, bool grads) {
   return l;
 }
 
-// X as it lies, where the tiles can read it, else packed into ws with zeros
-// to the next multiple of BK columns.  Of the two operands of the scores one
-// has to hold zeros there: H (whole), which is the smaller one as a rule.
-Panel panel_of(const Mat& X, const Layout& l, bool whole, char* ws, hipStream_t s) {
-  if (l.planes == 1 && X.cols % (whole ? l.step : 8) == 0 && X.ld % 8 == 0 && X.ld < (int64_t(1) << 22) &&
-      (reinterpret_cast<uintptr_t>(X.data) & 15) == 0)
-    return Panel{static_cast<const uint16_t*>(X.data), X.ld, X.rows, X.cols};
-  uint16_t* to = reinterpret_cast<uint16_t*>(ws);
-  const unsigned grid = grid_of(X.rows * (l.width / 4), 1024);
-  if (l.planes == 1) k_pack<false><<<grid, 256, 0, s>>>(X, to, l.width);
-  else k_pack<true><<<grid, 256, 0, s>>>(X, to, l.width);
-  return Panel{to, l.planes * l.width, X.rows, l.width};
+// Whether the tiles can read X as it lies.  Of the two operands of the scores
+// one has to hold zeros up to the next multiple of BK columns: H (whole), which
+// is the smaller one as a rule.
+bool lies_well(const Mat& X, const Layout& l, bool whole) {
+  return l.planes == 1 && X.cols % (whole ? l.step : 8) == 0 && X.ld % 8 == 0 && X.ld < (int64_t(1) << 22) &&
+         (reinterpret_cast<uintptr_t>(X.data) & 15) == 0;
+}
+
+// The operands as they lie, else packed into the workspace with zeros past
+// their columns.
+void panels_of(const Mat& H, const Mat& W, const Layout& l, char* ws, Panel& h, Panel& w, hipStream_t s) {
+  const bool ph = !lies_well(H, l, true), pw = !lies_well(W, l, false);
+  auto panel = [&](const Mat& X, bool packed, int64_t at) {
+    return packed ? Panel{reinterpret_cast<uint16_t*>(ws + at), l.planes * l.width, X.rows, l.width}
+                  : Panel{static_cast<const uint16_t*>(X.data), X.ld, X.rows, X.cols};
+  };
+  h = panel(H, ph, l.h);
+  w = panel(W, pw, l.w);
+  if (!ph && !pw) return;
+  Pack a{ph ? H : W, W, (uint16_t*)(ws + (ph ? l.h : l.w)), (uint16_t*)(ws + l.w), l.width, 0};
+  a.first = grid_of(a.X.rows * (l.width / 4), 1024);
+  const unsigned grid = a.first + (ph && pw ? grid_of(W.rows * (l.width / 4), 1024) : 0);
+  if (l.planes == 1) k_pack<false><<<grid, 256, 0, s>>>(a);
+  else k_pack<true><<<grid, 256, 0, s>>>(a);
 }
 
 template <bool GRAD, int TYPE>
@@ -690,8 +742,7 @@ hipError_t linear_xent(const XentArgs& x, hipStream_t s) {
   float* scale = (float*)(ws + l.scale);
   Scores sc{};
   if (T > 0) {
-    sc.H = panel_of(x.H, l, true, ws + l.h, s);
-    sc.W = panel_of(x.W, l, false, ws + l.w, s);
+    panels_of(x.H, x.W, l, ws, sc.H, sc.W, s);
     sc.T = T; sc.V = V;
     sc.steps = (int)(l.width / l.step);
     sc.labels = x.labels; sc.i64 = x.labels_i64;
@@ -739,9 +790,11 @@ hipError_t linear_xent(const XentArgs& x, hipStream_t s) {
     if (type == DT_F32) gradients<DT_F32>(g, l.G, s);
     else if (type == DT_BF16) gradients<DT_BF16>(g, l.G, s);
     else gradients<DT_F16>(g, l.G, s);
-    if (l.dw) finish((float*)(ws + l.dw), l.dw_slices, n, D, l.width, scale, out.data, type, out.ld, s);
+    Finish dh{}, dw{};
+    if (l.dw) dw = Finish{(float*)(ws + l.dw), l.dw_slices, n, D, l.width, out.data, type, out.ld};
+    if (l.dh && v0 + n == V) dh = Finish{(float*)(ws + l.dh), l.dh_slices, T, D, l.width, x.dH.data, type, x.dH.ld};
+    finish(dh, dw, scale, nullptr, 0, 0, nullptr, s);
   }
-  if (l.dh) finish((float*)(ws + l.dh), l.dh_slices, T, D, l.width, scale, x.dH.data, type, x.dH.ld, s);
   return hipGetLastError();
 }
 

@@ -11,6 +11,7 @@ namespace {
 
 constexpr int COUNT_BLOCK = 1024;   // labels a workgroup of k_count looks at, at least
 constexpr int MAX_COUNTS = 256;
+constexpr int COUNT_ALL = 4096;    // so few labels every workgroup of k_few counts by itself: a launch less
 
 // Labelled rows among each workgroup's share.
 __global__ __launch_bounds__(256) void k_count(const void* labels, int i64, int64_t T, int64_t V, int* counts) {
@@ -25,20 +26,6 @@ __global__ __launch_bounds__(256) void k_count(const void* labels, int i64, int6
   if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = n;
   __syncthreads();
   if (threadIdx.x == 0) counts[blockIdx.x] = buf[0] + buf[1] + buf[2] + buf[3];
-}
-
-// The loss from the workgroups' shares (512 at most), in a fixed order.
-__global__ __launch_bounds__(512) void k_total(const double* sums, int n, float* loss) {
-  __shared__ double buf[8];
-  double x = (int)threadIdx.x < n ? sums[threadIdx.x] : 0.0;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o);
-  if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = x;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int i = 1; i < 8; ++i) x += buf[i];
-    *loss = (float)x;
-  }
 }
 
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
@@ -59,7 +46,7 @@ Layout layout_of(int64_t T, int64_t D, int64_t V, bool grads) {
   l.counts = take(4 * MAX_COUNTS);
   l.scale = take(4);
   l.rows = take(4 * T);
-  l.sums = take(8 * g);
+  l.sums = take(16 * g);
   if (grads) l.part = take(4 * g * V * up(D, 16));
   l.bytes = at;
   return l;
@@ -83,20 +70,22 @@ hipError_t xent_few(const XentArgs& x, hipStream_t s) {
   f.scale = (float*)(ws + l.scale);
   f.part = grads ? (float*)(ws + l.part) : nullptr;
   f.counts = (const int*)(ws + l.counts);
-  f.ncounts = (int)std::min<int64_t>(MAX_COUNTS, (T + COUNT_BLOCK - 1) / COUNT_BLOCK);
+  // (the gradients need the number of labelled rows first)
+  f.ncounts = grads && T > COUNT_ALL ? (int)std::min<int64_t>(MAX_COUNTS, (T + COUNT_BLOCK - 1) / COUNT_BLOCK) : 0;
   f.mean = x.mean; f.grad_scale = x.grad_scale;
   f.row_loss = x.row_loss ? x.row_loss : (float*)(ws + l.rows);
-  f.sums = (double*)(ws + l.sums);
-  k_count<<<(unsigned)f.ncounts, 256, 0, s>>>(x.labels, x.labels_i64, T, V, (int*)(ws + l.counts));
+  f.sums = (double2*)(ws + l.sums);
+  if (f.ncounts > 0) k_count<<<(unsigned)f.ncounts, 256, 0, s>>>(x.labels, x.labels_i64, T, V, (int*)(ws + l.counts));
   const FewShape sh = few_shape(D, V);
   const unsigned grid = (unsigned)few_groups(sh, T);
+  Finish dw{};
   if (!grads) {
     few_launch<FEW_CLASSES>(sh, f, grid, s);
   } else {
     few_launch<FEW_CLASSES_TRAIN>(sh, f, grid, s);
-    finish(f.part, (int)grid, V, D, f.Dp, f.scale, x.dW.data, x.dW.type, x.dW.ld, s);
+    dw = Finish{f.part, (int)grid, V, D, f.Dp, x.dW.data, x.dW.type, x.dW.ld};
   }
-  k_total<<<1, 512, 0, s>>>(f.sums, (int)grid, x.loss);
+  finish(dw, Finish{}, f.scale, f.sums, (int)grid, x.mean, x.loss, s);
   return hipGetLastError();
 }
 

@@ -69,7 +69,7 @@ hipError_t xent_rows(const XentArgs& x, hipStream_t s) {
                 x.row_loss ? x.row_loss : (float*)(ws + l.rows), ws + l.sums, f.ticket, x.grad_scale, f.scale, s);
   if (grads) {
     few_launch<FEW_DZ>(sh, f, grid, s);
-    finish(f.part, (int)grid, T, D, f.Dp, f.scale, x.dH.data, x.dH.type, x.dH.ld, s);
+    finish(Finish{f.part, (int)grid, T, D, f.Dp, x.dH.data, x.dH.type, x.dH.ld}, Finish{}, f.scale, nullptr, 0, 0, nullptr, s);
   }
   return hipGetLastError();
 }
