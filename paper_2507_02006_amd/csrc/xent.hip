@@ -89,6 +89,38 @@ __global__ __launch_bounds__(256) void k_pack(Pack a) {
 
 // ------------------------------------------------------------------ scores
 
+// The loss, and what dz is multiplied with, from workgroups' losses and
+// labelled rows in a fixed order, by one workgroup.
+struct Total {
+  const double2* sums; int64_t n;
+  int mean; float grad_scale;
+  float* scale; float* loss;
+};
+
+template <int THREADS>
+__device__ __forceinline__ void total_loss(const Total& a) {
+  __shared__ double2 buf[THREADS / 64];
+  double2 v = {0, 0};
+  for (int64_t i = threadIdx.x; i < a.n; i += THREADS) {
+    v.x += a.sums[i].x;
+    v.y += a.sums[i].y;
+  }
+  v = wave_sum2(v);
+  if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < THREADS / 64; ++i) {
+      v.x += buf[i].x;
+      v.y += buf[i].y;
+    }
+    const double div = a.mean && v.y > 0 ? v.y : 1.0;
+    *a.scale = (float)(a.grad_scale / div);
+    *a.loss = (float)(v.x / div);
+  }
+}
+
+__global__ __launch_bounds__(256) void k_total(Total a) { total_loss<256>(a); }
+
 struct Scores {
   Panel W, H;
   int64_t T, V, v0, v1;   // the piece [v0, v1) of the table
@@ -98,6 +130,7 @@ struct Scores {
   const void* labels; int i64;
   uint16_t* dz; int64_t ldz;  // of 16-bit elements
   uint32_t* ticket;       // cleared here for the workgroups of k_rows
+  Total total;            // n > 0: made by a workgroup more, the first one
 };
 
 // TT rows of H a tile.  256: eight wavefronts of 128 x 64; 128: of 64 x 64;
@@ -117,8 +150,9 @@ __global__ __launch_bounds__(score_threads(TYPE, TT), 2) void k_scores(Scores s)
   using T_ = ScoreTile<TT, TYPE>;
   constexpr int SPAN = T_::MT * 32, NWM = TV / SPAN;  // table entries of a wavefront, wavefronts along the table
   __shared__ __attribute__((aligned(16))) char lds[T_::LDS];
+  if (GRAD && s.total.n > 0 && blockIdx.x == 0) return total_loss<T_::THREADS>(s.total);
   int64_t vt, tt;
-  place_tile(blockIdx.x, (s.v1 - s.v0 + TV - 1) / TV, (s.T + TT - 1) / TT, 8, vt, tt);
+  place_tile(blockIdx.x - (GRAD && s.total.n > 0 ? 1 : 0), (s.v1 - s.v0 + TV - 1) / TV, (s.T + TT - 1) / TT, 8, vt, tt);
   const int64_t v0 = s.v0 + vt * TV, t0 = tt * TT;
   f32x16 acc[T_::MT][T_::NT];
   T_::run(s.W, v0, s.H, t0, 0, s.steps, lds, acc);
@@ -259,9 +293,8 @@ struct Rows {
   const float2* part; int64_t tiles;
   float* top; float* inv; float* row_loss;
   double2* sums;      // a workgroup's losses and labelled rows
-  uint32_t* ticket;
-  int mean; float grad_scale;
-  float* scale; float* loss;
+  uint32_t* ticket;   // with it the last workgroup to finish adds up the loss
+  Total total;
 };
 
 // Sum over d of H(row, d) W(label, d), LPR lanes a row, in each of them.
@@ -287,31 +320,6 @@ __device__ __forceinline__ float label_score(const Rows& a, int64_t row, int64_t
   return group_sum_f32<LPR>(s);
 }
 
-// The workgroups' shares of the loss in a fixed order, by one workgroup.
-template <int THREADS>
-__device__ __forceinline__ void total_loss(const Rows& a, int64_t n) {
-  __shared__ double2 buf[THREADS / 64];
-  double2 v = {0, 0};
-  for (int64_t i = threadIdx.x; i < n; i += THREADS) {
-    v.x += a.sums[i].x;
-    v.y += a.sums[i].y;
-  }
-  v = wave_sum2(v);
-  if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int i = 1; i < THREADS / 64; ++i) {
-      v.x += buf[i].x;
-      v.y += buf[i].y;
-    }
-    const double div = a.mean && v.y > 0 ? v.y : 1.0;
-    *a.scale = (float)(a.grad_scale / div);
-    *a.loss = (float)(v.x / div);
-  }
-}
-
-__global__ __launch_bounds__(256) void k_total(Rows a, int64_t n) { total_loss<256>(a, n); }
-
 // Maximum and sum of each row from its tiles', and its loss: ROWS rows a
 // workgroup, SLICES threads to a row's tiles, then lanes to each row's label
 // score.  With a ticket the last workgroup to finish adds up the loss.  It waits
@@ -326,6 +334,13 @@ __global__ __launch_bounds__(ROWS * SLICES) void k_rows(Rows a) {
   __shared__ bool last;
   const int tid = threadIdx.x, r = tid % ROWS, slice = tid / ROWS;
   const int64_t T = a.H.rows, t0 = (int64_t)blockIdx.x * ROWS, t = t0 + r;
+  constexpr int ITERS = (ROWS * LPR + THREADS - 1) / THREADS;
+  int64_t label[ITERS];  // (on their way while the statistics come)
+#pragma unroll
+  for (int it = 0; it < ITERS; ++it) {
+    const int64_t row = t0 + tid / LPR + it * (THREADS / LPR);
+    label[it] = T > 0 ? label_at(a.labels, a.i64, row < T ? row : T - 1) : -1;
+  }
   float m = -INFINITY, s = 0.f;
   if (t < T) {
 #pragma unroll 8
@@ -350,16 +365,17 @@ __global__ __launch_bounds__(ROWS * SLICES) void k_rows(Rows a) {
   }
   __syncthreads();
   double2 mine = {0, 0};
-  for (int i = tid / LPR; i < ROWS; i += THREADS / LPR) {
+#pragma unroll
+  for (int it = 0; it < ITERS; ++it) {
+    const int i = tid / LPR + it * (THREADS / LPR);
     const int64_t row = t0 + i;
-    if (row >= T) break;
-    const int64_t label = label_at(a.labels, a.i64, row);
+    if (i >= ROWS || row >= T) break;
     float x = 0.f;
-    if (label >= 0 && label < a.W.rows) {
+    if (label[it] >= 0 && label[it] < a.W.rows) {
       const int l = tid % LPR;
-      x = a.H.type == DT_F32    ? label_score<DT_F32, LPR>(a, row, label, l)
-          : a.H.type == DT_BF16 ? label_score<DT_BF16, LPR>(a, row, label, l)
-                                : label_score<DT_F16, LPR>(a, row, label, l);
+      x = a.H.type == DT_F32    ? label_score<DT_F32, LPR>(a, row, label[it], l)
+          : a.H.type == DT_BF16 ? label_score<DT_BF16, LPR>(a, row, label[it], l)
+                                : label_score<DT_F16, LPR>(a, row, label[it], l);
       x = lse[i] - x;
       if (l == 0) {
         mine.x += x;
@@ -378,13 +394,13 @@ __global__ __launch_bounds__(ROWS * SLICES) void k_rows(Rows a) {
     }
     a.sums[blockIdx.x] = mine;
     // the share is visible to whoever draws a later number
-    last = gridDim.x == 1 ||
+    last = (a.ticket && gridDim.x == 1) ||
            (a.ticket && __hip_atomic_fetch_add(a.ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1);
   }
   __syncthreads();
   if (!last) return;
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-  total_loss<THREADS>(a, gridDim.x);
+  total_loss<THREADS>(a.total);
 }
 
 // Rows of a workgroup: 8 with 128 threads each for few rows, 16 with 64 where
@@ -396,19 +412,32 @@ int rows_of(int64_t T, int64_t tiles) { return T <= 2048 ? 8 : tiles >= 32 && T 
 
 int64_t rows_and_loss_workspace(int64_t T) { return 16 * std::max<int64_t>(1, (T + 7) / 8); }
 
-void rows_and_loss(const XentArgs& x, const float2* part, int64_t tiles, float* top, float* inv, float* row_loss,
-                   void* sums, uint32_t* ticket, float grad_scale, float* scale, hipStream_t s) {
+namespace {
+
+// The rows; Total's n is 0 where the loss has been added up with them.
+Total rows_of_all(const XentArgs& x, const float2* part, int64_t tiles, float* top, float* inv, float* row_loss,
+                  void* sums, uint32_t* ticket, float grad_scale, float* scale, hipStream_t s) {
   const int64_t T = x.H.rows;
   const int rows = rows_of(T, tiles);
   const unsigned blocks = (unsigned)std::max<int64_t>(1, (T + rows - 1) / rows);
   // A ticket costs 20 ns a workgroup, one after the other, another launch 5 us.
-  const bool drawn = blocks <= 128;
+  const bool drawn = ticket && blocks <= 128;
+  Total total{(double2*)sums, blocks, x.mean, grad_scale, scale, x.loss};
   const Rows rw{x.H, x.W, x.labels, x.labels_i64, part, tiles, top, inv, row_loss, (double2*)sums,
-                drawn ? ticket : nullptr, x.mean, grad_scale, scale, x.loss};
+                drawn ? ticket : nullptr, total};
   if (rows == 8) k_rows<8, 128><<<blocks, 1024, 0, s>>>(rw);
   else if (rows == 16) k_rows<16, 64><<<blocks, 1024, 0, s>>>(rw);
   else k_rows<64, 4><<<blocks, 256, 0, s>>>(rw);
-  if (!drawn) k_total<<<1, 256, 0, s>>>(rw, blocks);
+  if (drawn) total.n = 0;
+  return total;
+}
+
+}  // namespace
+
+void rows_and_loss(const XentArgs& x, const float2* part, int64_t tiles, float* top, float* inv, float* row_loss,
+                   void* sums, uint32_t* ticket, float grad_scale, float* scale, hipStream_t s) {
+  const Total total = rows_of_all(x, part, tiles, top, inv, row_loss, sums, ticket, grad_scale, scale, s);
+  if (total.n > 0) k_total<<<1, 256, 0, s>>>(total);
 }
 
 namespace {
@@ -709,7 +738,7 @@ void panels_of(const Mat& H, const Mat& W, const Layout& l, char* ws, Panel& h, 
 
 template <bool GRAD, int TYPE>
 void scores(const Scores& sc, int TT, hipStream_t s) {
-  const unsigned grid = (unsigned)(up(sc.v1 - sc.v0, TV) / TV * (up(sc.T, TT) / TT));
+  const unsigned grid = (unsigned)(up(sc.v1 - sc.v0, TV) / TV * (up(sc.T, TT) / TT)) + (sc.total.n > 0 ? 1 : 0);
   if (TT == 32) k_scores<GRAD, TYPE, 32><<<grid, 256, 0, s>>>(sc);
   else if (TT == 128) k_scores<GRAD, TYPE, 128><<<grid, score_threads(TYPE, 128), 0, s>>>(sc);
   else k_scores<GRAD, TYPE, 256><<<grid, 512, 0, s>>>(sc);
@@ -757,8 +786,14 @@ hipError_t linear_xent(const XentArgs& x, hipStream_t s) {
   }
   float *top = (float*)(ws + l.top), *inv = (float*)(ws + l.inv);
   // fp16 dz is held times F16_UP
-  rows_and_loss(x, (float2*)(ws + l.part), up(V, TV) / TV, top, inv, x.row_loss ? x.row_loss : (float*)(ws + l.rows), ws + l.sums,
-                sc.ticket, x.grad_scale * (f16 ? 1.f / F16_UP : 1.f), scale, s);
+  const float gs = x.grad_scale * (f16 ? 1.f / F16_UP : 1.f);
+  float* row_loss = x.row_loss ? x.row_loss : (float*)(ws + l.rows);
+  const float2* part = (float2*)(ws + l.part);
+  const int64_t tiles = up(V, TV) / TV;
+  if (grads && T > 0)  // dz does not need the loss: it is made next to it
+    sc.total = rows_of_all(x, part, tiles, top, inv, row_loss, ws + l.sums, nullptr, gs, scale, s);
+  else
+    rows_and_loss(x, part, tiles, top, inv, row_loss, ws + l.sums, (uint32_t*)(ws + l.ticket), gs, scale, s);
   if (!grads) return hipGetLastError();
   if (T == 0) {
     if (V > 0 && D > 0) k_zero<<<grid_of(V * D, 1024), 256, 0, s>>>(x.dW.data, type, V, D, x.dW.ld);
@@ -774,6 +809,7 @@ hipError_t linear_xent(const XentArgs& x, hipStream_t s) {
     const int64_t n = std::min(l.piece, V - v0);
     sc.v0 = v0; sc.v1 = v0 + n;
     scores<true>(sc, type, l.TT, s);
+    sc.total.n = 0;
     Gradients g{};
     g.scale = scale;
     Panel w = sc.W;
