@@ -82,82 +82,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_few(Few a) {
   const int64_t N = a.S.rows;
   const int D = a.D, NK = a.NK;
 
-  float scale = 1.f;
-  if constexpr (MODE == FEW_CLASSES_TRAIN) {
-    int c = 0;
-    if (a.ncounts == 0) {
-      for (int64_t t = tid; t < N; t += THREADS) {
-        const int64_t l = label_at(a.labels, a.i64, t);
-        c += l >= 0 && l < NK;
-      }
-    } else if (wave == 0) {
-      for (int i = lane; i < a.ncounts; i += 64) c += a.counts[i];
-    }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) c += __shfl_xor(c, o);
-    if (lane == 0) totals[wave] = c;
-    __syncthreads();
-    c = 0;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) c += totals[w];
-    scale = (float)(a.grad_scale / (a.mean && c > 0 ? (double)c : 1.0));
-    if (blockIdx.x == 0 && tid == 0) *a.scale = scale;
-  }
-  if constexpr (MODE == FEW_DZ) scale = *a.scale;
-  if constexpr (MODE == FEW_STATS)
-    if (blockIdx.x == 0 && tid == 0) *a.ticket = 0;  // for the workgroups that join the statistics
-
-  // what this thread knows of its kept rows (H's, where those are kept)
-  float top[KT], inv[KT];
-  int64_t label[KT];
-#pragma unroll
-  for (int k = 0; k < KT; ++k) {
-    const int t = p16 + 16 * k;
-    top[k] = MODE == FEW_STATS ? -INFINITY : 0.f;
-    inv[k] = 0.f;  // STATS: the sum
-    label[k] = -1;
-    if constexpr (MODE == FEW_DZ)
-      if (t < NK) {
-        const int64_t l = label_at(a.labels, a.i64, t);
-        if (l >= 0 && l < N) {
-          label[k] = l;
-          top[k] = a.top[t];
-          inv[k] = a.inv[t];
-        }
-      }
-  }
-
-  // this wavefront's columns of K, for the scores (row n16, columns 4 q ...)
-  // and for dS (rows 16 i + 4 q + j, column n16)
   const int c0 = wave * DT * 16;
-  float wn[KT][DT][4], wk[GRAD ? DT : 1][KT][4];
-  f32x4 acc[GRAD ? KT : 1][DT];
-  // (all of a type's loads in one branch, none of them conditional: they are
-  // in flight together)
-  auto keep = [&](auto type) {
-    constexpr int TYPE = decltype(type)::value;
-    auto at = [&](int v, int c) {
-      const float x = load1<TYPE>(a.K.data, (int64_t)(v < NK ? v : NK - 1) * a.K.ld + (c < D ? c : D - 1));
-      return v < NK && c < D ? x : 0.f;
-    };
-#pragma unroll
-    for (int v = 0; v < KT; ++v)
-#pragma unroll
-      for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          wn[v][d][j] = at(v * 16 + n16, c0 + d * 16 + 4 * q + j);
-          if constexpr (GRAD) wk[d][v][j] = at(16 * v + 4 * q + j, c0 + d * 16 + n16);
-        }
-  };
-  if constexpr (WIDE) keep(std::integral_constant<int, DT_F32>{});
-  else if (a.K.type == DT_BF16) keep(std::integral_constant<int, DT_BF16>{});
-  else keep(std::integral_constant<int, DT_F16>{});
-  if constexpr (GRAD)
-#pragma unroll
-    for (int v = 0; v < KT; ++v)
-#pragma unroll
-      for (int d = 0; d < DT; ++d) acc[v][d] = f32x4{0.f, 0.f, 0.f, 0.f};
 
   // Rows n16 of each row tile, columns 4 q ... of each column tile, as they
   // come: converting them waits for them, so that is left to their use.  Rows
@@ -203,10 +128,89 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_few(Few a) {
     else return f32x4{f16_to_f32(v[0]), f16_to_f32(v[1]), f16_to_f32(v[2]), f16_to_f32(v[3])};
   };
 
+  // The first rows are asked for before anything else: the kept rows, and what
+  // is known of them, come at the same time.
   const int64_t blocks = (N + TB - 1) / TB;
-  double2 loss = {0, 0};
   int64_t b = blockIdx.x;
   if (b < blocks) fetch(b * TB);
+
+  // this wavefront's columns of K, for the scores (row n16, columns 4 q ...)
+  // and for dS (rows 16 i + 4 q + j, column n16)
+  float wn[KT][DT][4], wk[GRAD ? DT : 1][KT][4];
+  f32x4 acc[GRAD ? KT : 1][DT];
+  // (all of a type's loads in one branch, none of them conditional: they are
+  // in flight together)
+  auto keep = [&](auto type) {
+    constexpr int TYPE = decltype(type)::value;
+    auto at = [&](int v, int c) {
+      const float x = load1<TYPE>(a.K.data, (int64_t)(v < NK ? v : NK - 1) * a.K.ld + (c < D ? c : D - 1));
+      return v < NK && c < D ? x : 0.f;
+    };
+#pragma unroll
+    for (int v = 0; v < KT; ++v)
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          wn[v][d][j] = at(v * 16 + n16, c0 + d * 16 + 4 * q + j);
+          if constexpr (GRAD) wk[d][v][j] = at(16 * v + 4 * q + j, c0 + d * 16 + n16);
+        }
+  };
+  if constexpr (WIDE) keep(std::integral_constant<int, DT_F32>{});
+  else if (a.K.type == DT_BF16) keep(std::integral_constant<int, DT_BF16>{});
+  else keep(std::integral_constant<int, DT_F16>{});
+  if constexpr (GRAD)
+#pragma unroll
+    for (int v = 0; v < KT; ++v)
+#pragma unroll
+      for (int d = 0; d < DT; ++d) acc[v][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  // what this thread knows of its kept rows (H's, where those are kept)
+  float top[KT], inv[KT];
+  int64_t label[KT];
+#pragma unroll
+  for (int k = 0; k < KT; ++k) {
+    const int t = p16 + 16 * k;
+    top[k] = MODE == FEW_STATS ? -INFINITY : 0.f;
+    inv[k] = 0.f;  // STATS: the sum
+    label[k] = -1;
+    if constexpr (MODE == FEW_DZ)
+      if (t < NK) {
+        const int64_t l = label_at(a.labels, a.i64, t);
+        if (l >= 0 && l < N) {
+          label[k] = l;
+          top[k] = a.top[t];
+          inv[k] = a.inv[t];
+        }
+      }
+  }
+
+  float scale = 1.f;
+  if constexpr (MODE == FEW_CLASSES_TRAIN) {
+    int c = 0;
+    if (a.ncounts == 0) {
+      for (int64_t t = tid; t < N; t += THREADS) {
+        const int64_t l = label_at(a.labels, a.i64, t);
+        c += l >= 0 && l < NK;
+      }
+    } else if (wave == 0) {
+      for (int i = lane; i < a.ncounts; i += 64) c += a.counts[i];
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) c += __shfl_xor(c, o);
+    if (lane == 0) totals[wave] = c;
+    __syncthreads();
+    c = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) c += totals[w];
+    scale = (float)(a.grad_scale / (a.mean && c > 0 ? (double)c : 1.0));
+    if (blockIdx.x == 0 && tid == 0) *a.scale = scale;
+  }
+  if constexpr (MODE == FEW_DZ) scale = *a.scale;
+  if constexpr (MODE == FEW_STATS)
+    if (blockIdx.x == 0 && tid == 0) *a.ticket = 0;  // for the workgroups that join the statistics
+
+  double2 loss = {0, 0};
   for (; b < blocks; b += gridDim.x) {
     const int64_t r0 = b * TB;
     // scores over this wavefront's columns
