@@ -17,16 +17,17 @@
 // while the next block's are on their way.  A workgroup's dK is written once,
 // at the end; a second launch adds them up in a fixed order.
 //
-// Products run in fp32 on the matrix cores (16 x 16 x 4) for every type: fp32
-// rows are not rounded anywhere.  A lane's k within a step is free as long as
+// Products run on the matrix cores, the scores of 16-bit rows in those bits (16
+// x 16 x 16), everything else in fp32 (16 x 16 x 4): nothing is rounded on its
+// way.  A lane's k within a step is free as long as
 // both operands agree on it: k = 16 i + 4 (lane / 16) + j for step j of group i,
 // so that a lane's four steps are one 16-byte read.  Strides that are 4 modulo
 // 16 words keep both directions of reading free of bank conflicts.
 //
-// Measured: 150001 x 256, 41 classes, f32, loss and both gradients 147 us (308 MB
-// at 2.1 TB/s).  Its three products, of 48 classes as they are padded, are 71 us
-// of the matrix cores, which the counters find busy 53 % of the time; the rest
-// is waiting where the wavefronts meet over the scores.
+// Measured, loss and both gradients, 150001 x 256, 41 classes: the call takes 140 us in f32
+// (308 MB at 2.2 TB/s), of which the three products, of 48 classes as they are
+// padded, keep the matrix cores busy for 71, and 106 us in bf16 (135 with scores
+// in fp32).  The rest is waiting where the wavefronts meet over the scores.
 #pragma once
 #include <type_traits>
 
@@ -39,6 +40,15 @@ namespace kern {
 namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+
+// 16 columns of 16-bit rows, four a lane
+template <int TYPE>
+__device__ __forceinline__ f32x4 mfma16(s16x4 a, s16x4 b, f32x4 c) {
+  if constexpr (TYPE == DT_BF16) return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a, b, c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(f16x4, a), __builtin_bit_cast(f16x4, b), c, 0, 0, 0);
+}
 
 // CLASSES: softmax along the kept rows, loss; TRAIN: and both gradients.
 // STATS: maximum and sum of exponentials along the streamed rows; DZ: both
@@ -63,12 +73,12 @@ struct Few {
 };
 
 // KT tiles of 16 kept rows, DT tiles of 16 columns to each of WAVES
-// wavefronts, RT tiles of 16 streamed rows a block; WIDE: S is fp32.  Two
-// wavefronts a SIMD:
-// two workgroups of four a CU, whose meetings do not coincide, where their
+// wavefronts, RT tiles of 16 streamed rows a block; TYPE: of S, K and dS.  Two
+// wavefronts a SIMD: two workgroups of four a CU, whose meetings do not coincide, where their
 // registers hold KT DT <= 12 tiles, else one of eight.
-template <int KT, int DT, int WAVES, int RT, int MODE, bool WIDE>
+template <int KT, int DT, int WAVES, int RT, int MODE, int TYPE>
 __global__ __launch_bounds__(WAVES * 64, 2) void k_few(Few a) {
+  constexpr bool WIDE = TYPE == DT_F32;
   constexpr bool GRAD = MODE == FEW_CLASSES_TRAIN || MODE == FEW_DZ;
   constexpr bool CLASSES = MODE == FEW_CLASSES || MODE == FEW_CLASSES_TRAIN;
   constexpr int THREADS = WAVES * 64, TB = RT * 16, ZS = KT * 16 + 4, HS = DT * 16 + 4;
@@ -122,11 +132,12 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_few(Few a) {
         return v;
       });
   };
-  auto values = [&](Raw v) {
-    if constexpr (WIDE) return f32x4{v[0], v[1], v[2], v[3]};
-    else if (a.S.type == DT_BF16) return f32x4{bf16_to_f32(v[0]), bf16_to_f32(v[1]), bf16_to_f32(v[2]), bf16_to_f32(v[3])};
-    else return f32x4{f16_to_f32(v[0]), f16_to_f32(v[1]), f16_to_f32(v[2]), f16_to_f32(v[3])};
+  auto number = [](E x) {
+    if constexpr (WIDE) return x;
+    else if constexpr (TYPE == DT_BF16) return bf16_to_f32(x);
+    else return f16_to_f32(x);
   };
+  auto values = [&](Raw v) { return f32x4{number(v[0]), number(v[1]), number(v[2]), number(v[3])}; };
 
   // The first rows are asked for before anything else: the kept rows, and what
   // is known of them, come at the same time.
@@ -136,15 +147,14 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_few(Few a) {
 
   // this wavefront's columns of K, for the scores (row n16, columns 4 q ...)
   // and for dS (rows 16 i + 4 q + j, column n16)
-  float wn[KT][DT][4], wk[GRAD ? DT : 1][KT][4];
+  // (none of the loads conditional: they are in flight together)
+  std::conditional_t<WIDE, float[4], s16x4> wn[KT][DT];  // (no vectors of f32: the products take single registers)
+  float wk[GRAD ? DT : 1][KT][4];
   f32x4 acc[GRAD ? KT : 1][DT];
-  // (all of a type's loads in one branch, none of them conditional: they are
-  // in flight together)
-  auto keep = [&](auto type) {
-    constexpr int TYPE = decltype(type)::value;
+  auto keep = [&]() {
     auto at = [&](int v, int c) {
-      const float x = load1<TYPE>(a.K.data, (int64_t)(v < NK ? v : NK - 1) * a.K.ld + (c < D ? c : D - 1));
-      return v < NK && c < D ? x : 0.f;
+      const E x = static_cast<const E*>(a.K.data)[(int64_t)(v < NK ? v : NK - 1) * a.K.ld + (c < D ? c : D - 1)];
+      return (v < NK) & (c < D) ? x : E(0);  // (&: a branch would take the load with it)
     };
 #pragma unroll
     for (int v = 0; v < KT; ++v)
@@ -153,12 +163,10 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_few(Few a) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           wn[v][d][j] = at(v * 16 + n16, c0 + d * 16 + 4 * q + j);
-          if constexpr (GRAD) wk[d][v][j] = at(16 * v + 4 * q + j, c0 + d * 16 + n16);
+          if constexpr (GRAD) wk[d][v][j] = number(at(16 * v + 4 * q + j, c0 + d * 16 + n16));
         }
   };
-  if constexpr (WIDE) keep(std::integral_constant<int, DT_F32>{});
-  else if (a.K.type == DT_BF16) keep(std::integral_constant<int, DT_BF16>{});
-  else keep(std::integral_constant<int, DT_F16>{});
+  keep();
   if constexpr (GRAD)
 #pragma unroll
     for (int v = 0; v < KT; ++v)
@@ -213,6 +221,13 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_few(Few a) {
   double2 loss = {0, 0};
   for (; b < blocks; b += gridDim.x) {
     const int64_t r0 = b * TB;
+    // Four wavefronts make their places in LDS anew each time: kept, they push
+    // other values to scratch memory (150001 x 256, 41 classes, f32: 140 us, 149
+    // with them kept; eight, whose registers spill either way, 412 and 376 with 60
+    // rows, 500 columns).
+    int here = tid;
+    if constexpr (WAVES == 4) asm("" : "+v"(here));
+    const int n16 = here & 15, q = (here >> 4) & 3, p16 = n16;
     // scores over this wavefront's columns
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
@@ -221,15 +236,25 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_few(Few a) {
       for (int v = 0; v < KT; ++v) s[v] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
-        f32x4 x = values(raw[rt][d]);
-        if (D % 4 != 0)
+        if constexpr (WIDE) {
+          f32x4 x = values(raw[rt][d]);
+          if (D % 4 != 0)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) x[j] = c0 + d * 16 + 4 * q + j < D ? x[j] : 0.f;
+            for (int j = 0; j < 4; ++j) x[j] = c0 + d * 16 + 4 * q + j < D ? x[j] : 0.f;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+          for (int j = 0; j < 4; ++j)
 #pragma unroll
-          for (int v = 0; v < KT; ++v) s[v] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], wn[v][d][j], s[v], 0, 0, 0);
-        if constexpr (GRAD) *reinterpret_cast<f32x4*>(&h[rt * 16 + n16][d * 16 + 4 * q]) = x;
+            for (int v = 0; v < KT; ++v) s[v] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], wn[v][d][j], s[v], 0, 0, 0);
+          if constexpr (GRAD) *reinterpret_cast<f32x4*>(&h[rt * 16 + n16][d * 16 + 4 * q]) = x;
+        } else {
+          Raw x = raw[rt][d];
+          if (D % 4 != 0)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = c0 + d * 16 + 4 * q + j < D ? x[j] : E(0);
+#pragma unroll
+          for (int v = 0; v < KT; ++v) s[v] = mfma16<TYPE>(__builtin_bit_cast(s16x4, x), wn[v][d], s[v]);
+          if constexpr (GRAD) *reinterpret_cast<f32x4*>(&h[rt * 16 + n16][d * 16 + 4 * q]) = values(x);
+        }
       }
 #pragma unroll
       for (int v = 0; v < KT; ++v)
@@ -435,32 +460,33 @@ inline int64_t few_groups(const FewShape& f, int64_t rows) {
   return std::max<int64_t>(1, std::min<int64_t>(fill, blocks));
 }
 
-template <int KT, int MODE, bool WIDE>
+template <int KT, int MODE, int TYPE>
 void few_launch(const FewShape& f, const Few& a, unsigned grid, hipStream_t s) {
   if (f.waves == 4) {
-    if (f.DT == 1) k_few<KT, 1, 4, 2, MODE, WIDE><<<grid, 256, 0, s>>>(a);
-    else if (f.DT == 2) k_few<KT, 2, 4, 2, MODE, WIDE><<<grid, 256, 0, s>>>(a);
-    else if constexpr (KT <= 3) k_few<KT, 4, 4, 2, MODE, WIDE><<<grid, 256, 0, s>>>(a);
+    if (f.DT == 1) k_few<KT, 1, 4, 2, MODE, TYPE><<<grid, 256, 0, s>>>(a);
+    else if (f.DT == 2) k_few<KT, 2, 4, 2, MODE, TYPE><<<grid, 256, 0, s>>>(a);
+    else if constexpr (KT <= 3) k_few<KT, 4, 4, 2, MODE, TYPE><<<grid, 256, 0, s>>>(a);
   } else {
     if constexpr (KT == 4)
-      if (f.DT == 2) k_few<KT, 2, 8, 2, MODE, WIDE><<<grid, 512, 0, s>>>(a);  // (fewer tiles: four wavefronts)
-    if (f.DT == 4) k_few<KT, 4, 8, 2, MODE, WIDE><<<grid, 512, 0, s>>>(a);
+      if (f.DT == 2) k_few<KT, 2, 8, 2, MODE, TYPE><<<grid, 512, 0, s>>>(a);  // (fewer tiles: four wavefronts)
+    if (f.DT == 4) k_few<KT, 4, 8, 2, MODE, TYPE><<<grid, 512, 0, s>>>(a);
     else if constexpr (KT <= 2)
-      if (f.DT == 8) k_few<KT, 8, 8, 1, MODE, WIDE><<<grid, 512, 0, s>>>(a);
+      if (f.DT == 8) k_few<KT, 8, 8, 1, MODE, TYPE><<<grid, 512, 0, s>>>(a);
   }
 }
 
 template <int MODE>
 void few_launch(const FewShape& f, const Few& a, unsigned grid, hipStream_t s) {
-  auto wide = [&](auto w) {
-    constexpr bool WIDE = decltype(w)::value;
-    if (f.KT == 1) few_launch<1, MODE, WIDE>(f, a, grid, s);
-    else if (f.KT == 2) few_launch<2, MODE, WIDE>(f, a, grid, s);
-    else if (f.KT == 3) few_launch<3, MODE, WIDE>(f, a, grid, s);
-    else few_launch<4, MODE, WIDE>(f, a, grid, s);
+  auto of = [&](auto t) {
+    constexpr int TYPE = decltype(t)::value;
+    if (f.KT == 1) few_launch<1, MODE, TYPE>(f, a, grid, s);
+    else if (f.KT == 2) few_launch<2, MODE, TYPE>(f, a, grid, s);
+    else if (f.KT == 3) few_launch<3, MODE, TYPE>(f, a, grid, s);
+    else few_launch<4, MODE, TYPE>(f, a, grid, s);
   };
-  if (a.S.type == DT_F32) wide(std::true_type{});
-  else wide(std::false_type{});
+  if (a.S.type == DT_F32) of(std::integral_constant<int, DT_F32>{});
+  else if (a.S.type == DT_BF16) of(std::integral_constant<int, DT_BF16>{});
+  else of(std::integral_constant<int, DT_F16>{});
 }
 
 }  // namespace
