@@ -652,12 +652,15 @@ void slices_of(int steps, int64_t ideal, int& per, int& slices) {
   slices = std::max(1, (steps + per - 1) / per);
 }
 
-// Rows of a tile of scores: no more than there are, and as many as still make
-// a tile for every other CU (500 x 2000 scores, 64 columns, f32: the
-// whole call 80 us so, 102 in tiles of 256 rows).
+// Rows of a tile of scores: no more than there are, as many as still make a
+// tile for every other CU (500 x 2000 scores, 64 columns, f32: the whole call 80
+// us so, 102 in tiles of 256 rows), and not 256 where that leaves a seventh or more
+// of them empty that 128 would not (loss of 258 x 124296 scores, 423 columns, f32:
+// 329 us so, 360 with 256; 1100 x 60000, 512 columns, bf16, with gradients: 384 with
+// 128, 370 with 256).
 int score_rows(int64_t T, int64_t V) {
   for (int TT : {256, 128})
-    if (T > TT / 2 && up(T, TT) / TT * (up(V, TV) / TV) >= 128) return TT;
+    if (T > TT / 2 && up(T, TT) / TT * (up(V, TV) / TV) >= 128 && 7 * up(T, 128) > 6 * up(T, TT)) return TT;
   return 32;
 }
 
@@ -684,7 +687,9 @@ Layout layout_of(int64_t T, int64_t D, int64_t V, int type, bool grads) {
   l.h = take(2 * l.planes * T * l.width);
   l.w = take(2 * l.planes * V * l.width);
   if (grads) {
-    l.piece = std::min(up(V, TV), std::max<int64_t>(TV, kPieceBytes / (2 * l.planes * std::max<int64_t>(l.Tp, 1)) / TV * TV));
+    const int64_t most = std::max<int64_t>(TV, kPieceBytes / (2 * l.planes * std::max<int64_t>(l.Tp, 1)) / TV * TV);
+    const int64_t pieces = std::max<int64_t>(1, (V + most - 1) / most);
+    l.piece = up((V + pieces - 1) / pieces, TV);  // (of one size: a small last one costs more than its share)
     const int dh_steps = (int)(up(std::min(l.piece, V), l.step) / l.step), dw_steps = (int)(up(T, l.step) / l.step);
     // Shares of k of about equal length, one workgroup a CU with large tiles,
     // two with small ones; none shorter than `least` steps.  Small tiles where
