@@ -17,9 +17,9 @@
 // need a single exchange between lanes.
 //
 // What bounds it is the matrix cores where rows, columns and table are all
-// long.  8192 rows, 100003 x 512 table, bf16, both gradients: 3.8 ms, of which
-// the first scores take 874 us (960 TFLOP/s), the seven pieces' dz 169 us each
-// and their gradients 274 (870); 4099 rows, 30011 x 256, f32: 1.6 ms.
+// long.  8192 rows, 100003 x 512 table, bf16, both gradients: 3.6 ms, of which
+// the first scores take 886 us (950 TFLOP/s), the seven pieces' dz 158 us each
+// and their gradients 254 (940); 4099 rows, 30011 x 256, f32: 1.6 ms.
 #include "train.h"
 
 #include <algorithm>
