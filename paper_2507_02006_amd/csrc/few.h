@@ -68,7 +68,8 @@ struct Few {
   float* row_loss;
   double2* sums;                    // a workgroup's losses and labelled rows
   // STATS, DZ
-  float2* stats;                    // [workgroup][NK]: maximum, sum (base 2)
+  float2* stats;                    // [workgroup][NK]: maximum, sum
+  float* target;                    // scores of the kept rows' labels: written by STATS
   const float* top; const float* inv;
 };
 
@@ -182,13 +183,15 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_few(Few a) {
     top[k] = MODE == FEW_STATS ? -INFINITY : 0.f;
     inv[k] = 0.f;  // STATS: the sum
     label[k] = -1;
-    if constexpr (MODE == FEW_DZ)
+    if constexpr (!CLASSES)
       if (t < NK) {
         const int64_t l = label_at(a.labels, a.i64, t);
         if (l >= 0 && l < N) {
           label[k] = l;
-          top[k] = a.top[t];
-          inv[k] = a.inv[t];
+          if constexpr (MODE == FEW_DZ) {
+            top[k] = a.top[t];
+            inv[k] = a.inv[t];
+          }
         }
       }
   }
@@ -292,13 +295,13 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_few(Few a) {
           if (v >= NK) y[k] = -INFINITY;
           big = fmaxf(big, y[k]);
         }
-        big = group16_max_f32(big) * LOG2E;
+        big = group16_max_f32(big);
         target = group_sum_f32<16>(target);
         const float from = big == -INFINITY ? 0.f : big;
         float sum = 0.f;
 #pragma unroll
         for (int k = 0; k < KT; ++k) {
-          y[k] = exp2_fast(fmaf(y[k], LOG2E, -from));
+          y[k] = exp_from(y[k], from);
           sum += y[k];
         }
         sum = group_sum_f32<16>(sum);
@@ -311,7 +314,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_few(Few a) {
           }
         }
         if (p16 == 0 && row < N) {
-          const float x = there ? (big + log2f(sum)) * LN2 - target : 0.f;
+          const float x = there ? loss_of(big, sum, target) : 0.f;
           a.row_loss[row] = x;
           loss.x += x;
           loss.y += there ? 1.0 : 0.0;
@@ -321,16 +324,17 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_few(Few a) {
         if (row < N)
 #pragma unroll
           for (int k = 0; k < KT; ++k) {
-            const float up = fmaxf(top[k], y[k] * LOG2E), from = up == -INFINITY ? 0.f : up;
-            inv[k] = (top[k] == up ? inv[k] : inv[k] * exp2_fast(top[k] - up)) + exp2_fast(fmaf(y[k], LOG2E, -from));
+            const float up = fmaxf(top[k], y[k]), from = up == -INFINITY ? 0.f : up;
+            inv[k] = (top[k] == up ? inv[k] : inv[k] * exp_from(top[k], up)) + exp_from(y[k], from);
             top[k] = up;
+            if (row == label[k]) a.target[p16 + k * 16] = y[k];
           }
       }
       if constexpr (MODE == FEW_DZ) {
 #pragma unroll
         for (int k = 0; k < KT; ++k)
           dz[r][p16 + k * 16] = row < N && label[k] >= 0
-                                    ? exp2_fast(fmaf(y[k], LOG2E, -top[k])) * inv[k] - (row == label[k] ? 1.f : 0.f)
+                                    ? exp_from(y[k], top[k]) * inv[k] - (row == label[k] ? 1.f : 0.f)
                                     : 0.f;
       }
     }

@@ -5,8 +5,10 @@
 // dz_ij = scale (exp(z_ij - s_i) - [j = label(i)]) for labelled rows and 0 for
 // others, dH = dz W, dW = dz^T H.  2 T V D flops make the scores and as many
 // each gradient.  The scores are made twice, 8 T V D in all: once for each
-// tile's row maxima and sums of exponentials, joined to those of the row, and
-// once more in pieces of the table for dz, which goes to the workspace in 16
+// tile's row maxima and sums of exponentials, joined to those of the row, and the
+// labels' scores, which the tile that holds them writes (the loss of a row whose
+// label dominates is a difference of equal numbers: they have to be the same
+// ones), and once more in pieces of the table for dz, which goes to the workspace in 16
 // bits (a piece fits the 256 MB cache) and is read by both gradient products.
 //
 // All four products run on the matrix cores (tile.h).  fp32 operands are
@@ -125,7 +127,8 @@ struct Scores {
   Panel W, H;
   int64_t T, V, v0, v1;   // the piece [v0, v1) of the table
   int steps;
-  float2* part;           // [tile][t]: maximum, sum (base 2)
+  float2* part;           // [tile][t]: maximum, sum
+  float* target;          // labels' scores
   const float* top; const float* inv;  // of whole rows
   const void* labels; int i64;
   uint16_t* dz; int64_t ldz;  // of 16-bit elements
@@ -155,6 +158,16 @@ __global__ __launch_bounds__(score_threads(TYPE, TT), 2) void k_scores(Scores s)
   place_tile(blockIdx.x - (GRAD && s.total.n > 0 ? 1 : 0), (s.v1 - s.v0 + TV - 1) / TV, (s.T + TT - 1) / TT, 8, vt, tt);
   const int64_t v0 = s.v0 + vt * TV, t0 = tt * TT;
   f32x16 acc[T_::MT][T_::NT];
+  // Labels, as they come: they are on their way during the products.
+  uint32_t low[GRAD ? 1 : T_::NT], high[GRAD ? 1 : T_::NT];
+  if constexpr (!GRAD)
+#pragma unroll
+    for (int j = 0; j < T_::NT; ++j) {
+      const int64_t t = t0 + T_::col(j), at = t < s.T ? t : s.T - 1;
+      const uint32_t* const l = static_cast<const uint32_t*>(s.labels) + (s.i64 ? 2 * at : at);
+      low[j] = l[0];
+      high[j] = l[s.i64 ? 1 : 0];
+    }
   T_::run(s.W, v0, s.H, t0, 0, s.steps, lds, acc);
   const int lane = threadIdx.x & 63, wm = (threadIdx.x >> 6) / (T_::WAVES / NWM);
   __syncthreads();  // the stages' LDS changes its use
@@ -178,15 +191,28 @@ __global__ __launch_bounds__(score_threads(TYPE, TT), 2) void k_scores(Scores s)
       for (int i = 0; i < T_::MT; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) top = fmaxf(top, acc[i][j][r]);
-      top = fmaxf(top, __shfl_xor(top, 32)) * LOG2E;
+      top = fmaxf(top, __shfl_xor(top, 32));
       const float from = top == -INFINITY ? 0.f : top;  // a NaN still reaches the sum
       float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < T_::MT; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sum += exp2_fast(fmaf(acc[i][j][r], LOG2E, -from));
+        for (int r = 0; r < 16; ++r) sum += exp_from(acc[i][j][r], from);
       sum += __shfl_xor(sum, 32);
       const int c = T_::col(j);
+      // the label's score, where it is among this wavefront's, by the lane that has it
+      const int64_t label = s.i64 && high[j] != 0 ? -1 : (int64_t)(int32_t)low[j];
+      const int64_t first = v0 + wm * SPAN;
+      const bool mine = label >= first && label < first + SPAN && label < s.V && ((label >> 2) & 1) == lane >> 5;
+      if (__any(mine)) {
+        const int at = mine ? (int)(label - v0) : -1;
+        float z = 0.f;
+#pragma unroll
+        for (int i = 0; i < T_::MT; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) z = T_::row(i, r) == at ? acc[i][j][r] : z;
+        if (mine && t0 + c < s.T) s.target[t0 + c] = z;
+      }
       if (wm > 0 && lane < 32) others[(wm - 1) * TT + c] = make_float2(top, sum);
       acc[0][j][0] = top;
       acc[0][j][1] = sum;
@@ -212,7 +238,7 @@ __global__ __launch_bounds__(score_threads(TYPE, TT), 2) void k_scores(Scores s)
       for (int i = 0; i < T_::MT; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const float p = exp2_fast(fmaf(acc[i][j][r], LOG2E, -top)) * inv;
+          const float p = exp_from(acc[i][j][r], top) * inv;
           acc[i][j][r] = there ? p : 0.f;  // a score that is no number stays out of rows without a label
         }
       const int64_t first = v0 + wm * SPAN;
@@ -288,58 +314,32 @@ __global__ __launch_bounds__(score_threads(TYPE, TT), 2) void k_scores(Scores s)
 // ---------------------------------------------------------- rows and loss
 
 struct Rows {
-  Mat H, W;
+  int64_t T, V;
   const void* labels; int i64;
   const float2* part; int64_t tiles;
+  const float* target;
   float* top; float* inv; float* row_loss;
   double2* sums;      // a workgroup's losses and labelled rows
   uint32_t* ticket;   // with it the last workgroup to finish adds up the loss
   Total total;
 };
 
-// Sum over d of H(row, d) W(label, d), LPR lanes a row, in each of them.
-template <int TYPE, int LPR>
-__device__ __forceinline__ float label_score(const Rows& a, int64_t row, int64_t label, int lane) {
-  const int64_t h = row * a.H.ld, w = label * a.W.ld, D = a.H.cols;
-  float s = 0.f;
-#pragma unroll 2
-  for (int64_t d = 4 * lane; d < D; d += 4 * LPR) {
-    float x[4] = {}, y[4] = {};
-    if (d + 4 <= D) {
-      load4<TYPE>(a.H.data, h + d, x);
-      load4<TYPE>(a.W.data, w + d, y);
-    } else {
-      for (int k = 0; d + k < D; ++k) {
-        x[k] = load1<TYPE>(a.H.data, h + d + k);
-        y[k] = load1<TYPE>(a.W.data, w + d + k);
-      }
-    }
-#pragma unroll
-    for (int k = 0; k < 4; ++k) s = fmaf(x[k], y[k], s);
-  }
-  return group_sum_f32<LPR>(s);
-}
-
 // Maximum and sum of each row from its tiles', and its loss: ROWS rows a
-// workgroup, SLICES threads to a row's tiles, then lanes to each row's label
-// score.  With a ticket the last workgroup to finish adds up the loss.  It waits
-// for two dependent reads (statistics, then the label's row): 8 us for a row's
-// 1024 tiles, 11 us for 8192 rows of 391.
+// workgroup, SLICES threads to a row's tiles.  With a ticket the last workgroup
+// to finish adds up the loss.
 template <int ROWS, int SLICES>
 __global__ __launch_bounds__(ROWS * SLICES) void k_rows(Rows a) {
-  constexpr int THREADS = ROWS * SLICES, LPR = SLICES > 64 ? 64 : SLICES < 16 ? 16 : SLICES;
+  static_assert(ROWS <= 64, "the rows' losses are one wavefront's");
+  constexpr int THREADS = ROWS * SLICES;
   __shared__ float2 buf[SLICES][ROWS];
-  __shared__ float lse[ROWS];
-  __shared__ double2 sums[THREADS / 64];
   __shared__ bool last;
   const int tid = threadIdx.x, r = tid % ROWS, slice = tid / ROWS;
-  const int64_t T = a.H.rows, t0 = (int64_t)blockIdx.x * ROWS, t = t0 + r;
-  constexpr int ITERS = (ROWS * LPR + THREADS - 1) / THREADS;
-  int64_t label[ITERS];  // (on their way while the statistics come)
-#pragma unroll
-  for (int it = 0; it < ITERS; ++it) {
-    const int64_t row = t0 + tid / LPR + it * (THREADS / LPR);
-    label[it] = T > 0 ? label_at(a.labels, a.i64, row < T ? row : T - 1) : -1;
+  const int64_t T = a.T, t = (int64_t)blockIdx.x * ROWS + r;
+  int64_t label = -1;
+  float target = 0.f;  // (without a label: what the array happens to hold)
+  if (slice == 0 && t < T) {
+    label = label_at(a.labels, a.i64, t);
+    target = a.target[t];
   }
   float m = -INFINITY, s = 0.f;
   if (t < T) {
@@ -358,44 +358,23 @@ __global__ __launch_bounds__(ROWS * SLICES) void k_rows(Rows a) {
     }
     __syncthreads();
   }
-  if (slice == 0 && t < T) {
-    a.top[t] = m;
-    a.inv[t] = 1.f / s;
-    lse[r] = (m + log2f(s)) * LN2;
-  }
-  __syncthreads();
-  double2 mine = {0, 0};
-#pragma unroll
-  for (int it = 0; it < ITERS; ++it) {
-    const int i = tid / LPR + it * (THREADS / LPR);
-    const int64_t row = t0 + i;
-    if (i >= ROWS || row >= T) break;
-    float x = 0.f;
-    if (label[it] >= 0 && label[it] < a.W.rows) {
-      const int l = tid % LPR;
-      x = a.H.type == DT_F32    ? label_score<DT_F32, LPR>(a, row, label[it], l)
-          : a.H.type == DT_BF16 ? label_score<DT_BF16, LPR>(a, row, label[it], l)
-                                : label_score<DT_F16, LPR>(a, row, label[it], l);
-      x = lse[i] - x;
-      if (l == 0) {
-        mine.x += x;
-        mine.y += 1;
-      }
+  if (tid < 64) {
+    double2 mine = {0, 0};
+    if (slice == 0 && t < T) {
+      const bool there = label >= 0 && label < a.V;
+      const float x = there ? loss_of(m, s, target) : 0.f;
+      a.top[t] = m;
+      a.inv[t] = 1.f / s;
+      a.row_loss[t] = x;
+      mine = {x, there ? 1.0 : 0.0};
     }
-    if (tid % LPR == 0) a.row_loss[row] = x;
-  }
-  mine = wave_sum2(mine);
-  if ((tid & 63) == 0) sums[tid >> 6] = mine;
-  __syncthreads();
-  if (tid == 0) {
-    for (int i = 1; i < THREADS / 64; ++i) {
-      mine.x += sums[i].x;
-      mine.y += sums[i].y;
+    mine = wave_sum2(mine);
+    if (tid == 0) {
+      a.sums[blockIdx.x] = mine;
+      // the share is visible to whoever draws a later number
+      last = (a.ticket && gridDim.x == 1) ||
+             (a.ticket && __hip_atomic_fetch_add(a.ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1);
     }
-    a.sums[blockIdx.x] = mine;
-    // the share is visible to whoever draws a later number
-    last = (a.ticket && gridDim.x == 1) ||
-           (a.ticket && __hip_atomic_fetch_add(a.ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1);
   }
   __syncthreads();
   if (!last) return;
@@ -415,15 +394,15 @@ int64_t rows_and_loss_workspace(int64_t T) { return 16 * std::max<int64_t>(1, (T
 namespace {
 
 // The rows; Total's n is 0 where the loss has been added up with them.
-Total rows_of_all(const XentArgs& x, const float2* part, int64_t tiles, float* top, float* inv, float* row_loss,
-                  void* sums, uint32_t* ticket, float grad_scale, float* scale, hipStream_t s) {
+Total rows_of_all(const XentArgs& x, const float2* part, int64_t tiles, const float* target, float* top, float* inv,
+                  float* row_loss, void* sums, uint32_t* ticket, float grad_scale, float* scale, hipStream_t s) {
   const int64_t T = x.H.rows;
   const int rows = rows_of(T, tiles);
   const unsigned blocks = (unsigned)std::max<int64_t>(1, (T + rows - 1) / rows);
   // A ticket costs 20 ns a workgroup, one after the other, another launch 5 us.
   const bool drawn = ticket && blocks <= 128;
   Total total{(double2*)sums, blocks, x.mean, grad_scale, scale, x.loss};
-  const Rows rw{x.H, x.W, x.labels, x.labels_i64, part, tiles, top, inv, row_loss, (double2*)sums,
+  const Rows rw{T, x.W.rows, x.labels, x.labels_i64, part, tiles, target, top, inv, row_loss, (double2*)sums,
                 drawn ? ticket : nullptr, total};
   if (rows == 8) k_rows<8, 128><<<blocks, 1024, 0, s>>>(rw);
   else if (rows == 16) k_rows<16, 64><<<blocks, 1024, 0, s>>>(rw);
@@ -434,9 +413,9 @@ Total rows_of_all(const XentArgs& x, const float2* part, int64_t tiles, float* t
 
 }  // namespace
 
-void rows_and_loss(const XentArgs& x, const float2* part, int64_t tiles, float* top, float* inv, float* row_loss,
-                   void* sums, uint32_t* ticket, float grad_scale, float* scale, hipStream_t s) {
-  const Total total = rows_of_all(x, part, tiles, top, inv, row_loss, sums, ticket, grad_scale, scale, s);
+void rows_and_loss(const XentArgs& x, const float2* part, int64_t tiles, const float* target, float* top, float* inv,
+                   float* row_loss, void* sums, uint32_t* ticket, float grad_scale, float* scale, hipStream_t s) {
+  const Total total = rows_of_all(x, part, tiles, target, top, inv, row_loss, sums, ticket, grad_scale, scale, s);
   if (total.n > 0) k_total<<<1, 256, 0, s>>>(total);
 }
 
@@ -643,7 +622,7 @@ struct Layout {
   int TT, G;                           // tiles
   int64_t piece, Tp, ldz;              // table entries of a piece, rows of dz and their stride
   int dh_per, dh_slices, dw_per, dw_slices;
-  int64_t ticket, scale, top, inv, rows, sums, part, h, w, dh, dw, dz, bytes;
+  int64_t ticket, scale, target, top, inv, rows, sums, part, h, w, dh, dw, dz, bytes;
 };
 
 void slices_of(int steps, int64_t ideal, int& per, int& slices) {
@@ -679,6 +658,7 @@ Layout layout_of(int64_t T, int64_t D, int64_t V, int type, bool grads) {
   l.Tp = up(T, std::max<int64_t>(l.TT, l.step));
   l.ticket = take(4);
   l.scale = take(4);
+  l.target = take(4 * T);
   l.top = take(4 * T);
   l.inv = take(4 * T);
   l.rows = take(4 * T);
@@ -781,6 +761,7 @@ hipError_t linear_xent(const XentArgs& x, hipStream_t s) {
     sc.steps = (int)(l.width / l.step);
     sc.labels = x.labels; sc.i64 = x.labels_i64;
     sc.ticket = (uint32_t*)(ws + l.ticket);
+    sc.target = (float*)(ws + l.target);
     // (a launch holds fewer than 2^32 threads)
     const int64_t most = std::max<int64_t>(1, (int64_t(1) << 22) / (up(T, l.TT) / l.TT)) * TV;
     for (int64_t v0 = 0; v0 < V; v0 += most) {
@@ -794,11 +775,12 @@ hipError_t linear_xent(const XentArgs& x, hipStream_t s) {
   const float gs = x.grad_scale * (f16 ? 1.f / F16_UP : 1.f);
   float* row_loss = x.row_loss ? x.row_loss : (float*)(ws + l.rows);
   const float2* part = (float2*)(ws + l.part);
+  const float* target = (float*)(ws + l.target);
   const int64_t tiles = up(V, TV) / TV;
   if (grads && T > 0)  // dz does not need the loss: it is made next to it
-    sc.total = rows_of_all(x, part, tiles, top, inv, row_loss, ws + l.sums, nullptr, gs, scale, s);
+    sc.total = rows_of_all(x, part, tiles, target, top, inv, row_loss, ws + l.sums, nullptr, gs, scale, s);
   else
-    rows_and_loss(x, part, tiles, top, inv, row_loss, ws + l.sums, (uint32_t*)(ws + l.ticket), gs, scale, s);
+    rows_and_loss(x, part, tiles, target, top, inv, row_loss, ws + l.sums, (uint32_t*)(ws + l.ticket), gs, scale, s);
   if (!grads) return hipGetLastError();
   if (T == 0) {
     if (V > 0 && D > 0) k_zero<<<grid_of(V * D, 1024), 256, 0, s>>>(x.dW.data, type, V, D, x.dW.ld);

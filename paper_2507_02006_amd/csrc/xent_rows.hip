@@ -13,7 +13,7 @@ namespace {
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
 struct Layout {
-  int64_t ticket, scale, top, inv, rows, sums, stats, part, bytes;
+  int64_t ticket, scale, target, top, inv, rows, sums, stats, part, bytes;
 };
 
 Layout layout_of(int64_t T, int64_t D, int64_t V, bool grads) {
@@ -27,6 +27,7 @@ Layout layout_of(int64_t T, int64_t D, int64_t V, bool grads) {
   const int64_t g = few_groups(few_shape(D, T), V);
   l.ticket = take(4);
   l.scale = take(4);
+  l.target = take(4 * T);
   l.top = take(4 * T);
   l.inv = take(4 * T);
   l.rows = take(4 * T);
@@ -63,9 +64,10 @@ hipError_t xent_rows(const XentArgs& x, hipStream_t s) {
   f.scale = (float*)(ws + l.scale); f.ticket = (uint32_t*)(ws + l.ticket);
   f.part = grads ? (float*)(ws + l.part) : nullptr;
   f.stats = (float2*)(ws + l.stats);
+  f.target = (float*)(ws + l.target);
   f.top = (const float*)(ws + l.top); f.inv = (const float*)(ws + l.inv);
   few_launch<FEW_STATS>(sh, f, grid, s);
-  rows_and_loss(x, f.stats, grid, (float*)(ws + l.top), (float*)(ws + l.inv),
+  rows_and_loss(x, f.stats, grid, f.target, (float*)(ws + l.top), (float*)(ws + l.inv),
                 x.row_loss ? x.row_loss : (float*)(ws + l.rows), ws + l.sums, f.ticket, x.grad_scale, f.scale, s);
   if (grads) {
     few_launch<FEW_DZ>(sh, f, grid, s);

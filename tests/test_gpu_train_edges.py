@@ -1,0 +1,52 @@
+"""Layer norm, cross entropy and AdamW at the edges of what they take (GPU).
+
+U = 2^-24 is the unit roundoff of fp32: a sum of any order, in chains of at
+most c additions, is off by c U times the sum of magnitudes.
+"""
+import pytest
+
+torch = pytest.importorskip("torch")
+import paper_2507_02006_amd as aires  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+# ----------------------------------------------------------- cross entropy
+
+@pytest.mark.parametrize("dt", [F32, BF16, F16])
+@pytest.mark.parametrize("t,d,v", [(300, 64, 40), (70, 800, 20), (20, 131, 3000), (64, 256, 3000), (1, 512, 5000),
+                                   (500, 96, 2000), (2100, 72, 300), (140, 256, 60013)])
+def test_loss_of_rows_whose_label_dominates(t, d, v, dt):
+    """Scores that are multiples of 1/16 of up to eight times the columns, exact
+    in every type and order; the label's is the largest, and one other is k, 1 to 8,
+    below it or all are far below.  The loss is then log(1 + e^-k + ...) with
+    nothing lost to the scores' size, and never negative."""
+    g = gen(t + d + v)
+    W = torch.randint(0, 2, (v, d), generator=g).mul(2).sub(1).double()
+    W[v // 2] = W[3]
+    W[v // 2, 0] = 0  # next to class 3: k less
+    y = torch.randint(0, v, (t,), generator=g)
+    y[::3] = 3
+    k = torch.randint(16, 128, (t,), generator=g).double() / 16
+    H = W[y] * k[:, None]
+    z = H @ W.t()
+    top = z.amax(1, keepdim=True)
+    assert bool((z.abs() < 2 ** 14).all())
+    total = torch.exp(z - top).sum(1)
+    want = (top[:, 0] - z[torch.arange(t), y]) + torch.log1p((total - 1).clamp(min=0))
+    H, W = H.to(dt).cuda(), W.to(dt).cuda()
+    for grads in (False, True):
+        got = aires.linear_xent(H, W, y.cuda(), grads=grads)
+        rows = got.row_loss.double().cpu()
+        # a sum of at least 1 in chains of at most 256 additions, exponentials and a logarithm in fp32
+        tol = 256 * U * (1 + want)
+        assert bool((rows >= 0).all()), float(rows.min())
+        assert bool(((rows - want).abs() <= tol).all()), float(((rows - want).abs() / tol).max())
+        assert abs(float(got.loss) - float(want.mean())) <= 256 * U * (1 + float(want.mean()))
