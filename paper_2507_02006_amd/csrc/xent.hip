@@ -38,7 +38,10 @@ namespace {
 
 constexpr int TV = 256;  // table entries of a tile of scores
 constexpr int64_t kPieceBytes = int64_t(256) << 20;  // dz of one piece of the table
-constexpr float F16_UP = 1024.f;       // dz in fp16 is held times this: 2^-35 is its least step
+// dz in fp16, which is 1 at most, is held times this: as high as fp16 goes.  A
+// probability keeps its 11 bits down to 2^-29 (times 2^10: to 2^-24, which a
+// large gradient scale brings into an fp16 result's range).
+constexpr float F16_UP = 32768.f;
 
 // ---------------------------------------------------------------- operands
 

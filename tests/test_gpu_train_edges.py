@@ -50,3 +50,24 @@ def test_loss_of_rows_whose_label_dominates(t, d, v, dt):
         assert bool((rows >= 0).all()), float(rows.min())
         assert bool(((rows - want).abs() <= tol).all()), float(((rows - want).abs() / tol).max())
         assert abs(float(got.loss) - float(want.mean())) <= 256 * U * (1 + float(want.mean()))
+
+
+def test_small_probabilities_in_half_precision():
+    """dW of classes whose probability is below 2^-24 with a large gradient
+    scale: they keep all the bits that an fp16 result has."""
+    t, d, v, scale = 100, 64, 300, 2.0 ** 15
+    H = torch.ones(t, d)
+    a = torch.arange(v).double() * 2.0 ** -10 + 17.0 / d  # scores of -17 to -36, exact in fp16 and in any order
+    a = -(a * 2 ** 10).round() / 2 ** 10
+    a[0] = 0
+    W = a[:, None].expand(v, d).contiguous()
+    assert torch.equal(W.half().double(), W)
+    y = torch.zeros(t, dtype=torch.int64)
+    got = aires.linear_xent(H.half().cuda(), W.half().cuda(), y.cuda(), reduction="sum", grad_scale=scale)
+    p = torch.softmax(d * a, 0)
+    want = (t * scale * p)[1:, None]
+    some = p[1:] >= 2.0 ** -29  # (below them dz is not a normal number of 16 bits)
+    assert int(some.sum()) > 40
+    # dz and the result are rounded to 11 bits; the exponent's argument is off by 4 U of 36 log2 e
+    tol = (2 * 2.0 ** -11 + 4 * 52 * U + 64 * U) * want
+    assert bool(((got.dW.double().cpu()[1:] - want).abs() <= tol)[some].all())
