@@ -614,6 +614,7 @@ typedef struct aires_dense {
  * fp32 values each, both NULL if not wanted (the backward pass reads them).
  * A row whose values are all equal gives y = beta up to the rounding of mu
  * (r = eps^-1/2); a NaN or an infinity makes its own row NaN and no other.
+ * Rows without columns have mu = 0 and r = eps^-1/2.
  * Errors: AIRES_E_INVALID_ARG (NULL, bad type, ld < ncols, eps negative or
  * not finite, only one of mean and rstd), AIRES_E_DIM (sizes differ),
  * AIRES_E_UNSUPPORTED (m > 2^40, n > 2^30), AIRES_E_HIP.

@@ -355,6 +355,14 @@ __global__ __launch_bounds__(1024) void k_ln_columns(const float* part, int64_t 
   }
 }
 
+// Statistics of rows without columns: those of a row of equal values, 0.
+__global__ __launch_bounds__(TEAM_BLOCK) void k_ln_no_columns(float* mean, float* rstd, int64_t m, float eps) {
+  for (int64_t i = (int64_t)blockIdx.x * TEAM_BLOCK + threadIdx.x; i < m; i += (int64_t)gridDim.x * TEAM_BLOCK) {
+    mean[i] = 0.f;
+    rstd[i] = 1.f / sqrtf(eps);
+  }
+}
+
 // Lanes a row, chunks of four columns a lane, threads of a workgroup.
 struct Shape {
   int L, E, threads;
@@ -417,7 +425,12 @@ int64_t backward_groups(int64_t m, int64_t n) {
 
 hipError_t layer_norm(const Mat& X, const void* gamma, const void* beta, int wt, float eps, const Mat& Y, float* mean,
                       float* rstd, hipStream_t s) {
-  if (X.rows == 0 || X.cols == 0) return hipSuccess;
+  if (X.rows == 0 || (X.cols == 0 && !mean)) return hipSuccess;
+  if (X.cols == 0) {
+    k_ln_no_columns<<<(unsigned)std::min<int64_t>((X.rows + TEAM_BLOCK - 1) / TEAM_BLOCK, 1 << 16), TEAM_BLOCK, 0, s>>>(
+        mean, rstd, X.rows, eps);
+    return hipGetLastError();
+  }
   Args a{};
   a.x = X.data; a.ldx = X.ld; a.xt = X.type;
   a.out = Y.data; a.ldo = Y.ld; a.ot = Y.type;

@@ -18,6 +18,19 @@ def gen(seed):
     return torch.Generator().manual_seed(seed)
 
 
+# -------------------------------------------------------------- layer norm
+
+@pytest.mark.parametrize("m", [1, 4, 300, 70001])
+def test_layer_norm_statistics_of_rows_without_columns(m):
+    X = torch.empty(m, 0, device="cuda")
+    held = torch.full((2 * m + 64,), float("nan"), device="cuda")  # what the results' memory may hold before
+    del held
+    for eps in (1e-5, 0.25):
+        Y, mean, rstd = aires.layer_norm(X, eps=eps)
+        assert Y.shape == (m, 0) and mean.shape == rstd.shape == (m,)
+        assert not mean.any() and torch.allclose(rstd, torch.full_like(rstd, eps ** -0.5), rtol=4 * U, atol=0)
+
+
 # ----------------------------------------------------------- cross entropy
 
 @pytest.mark.parametrize("dt", [F32, BF16, F16])
