@@ -332,26 +332,33 @@ __global__ __launch_bounds__(TEAM_BLOCK) void k_ln_columns_wide(Args a) {
 }
 
 // dgamma and dbeta: the workgroups' partial sums, 32 shares of them side by
-// side for 32 columns, added in a fixed order.  count = 0 writes zeros.
+// side for 32 columns, added in a fixed order.  count = 0 writes zeros.  A launch
+// holds fewer than 2^32 threads along a side, so more than kColumnBlocks groups of
+// columns are gone through in turn.
+constexpr int64_t kColumnBlocks = int64_t(1) << 20;
+
 __global__ __launch_bounds__(1024) void k_ln_columns(const float* part, int64_t count, int n, void* dgamma,
                                                      void* dbeta, int wt) {
   __shared__ float buf[32][33];
   const int c = threadIdx.x & 31, w = threadIdx.x >> 5;
-  const int64_t col = (int64_t)blockIdx.x * 32 + c;
   const int which = blockIdx.y;
-  float v = 0.f;
-  if (col < n) {
+  for (int64_t at = (int64_t)blockIdx.x * 32; at < n; at += (int64_t)gridDim.x * 32) {
+    const int64_t col = at + c;
+    float v = 0.f;
+    if (col < n) {
 #pragma unroll 8
-    for (int64_t i = w; i < count; i += 32) v += part[(i * 2 + which) * n + col];
-  }
-  buf[w][c] = v;
-  __syncthreads();
-  if (w == 0 && col < n) {
-    v = 0.f;
+      for (int64_t i = w; i < count; i += 32) v += part[(i * 2 + which) * n + col];
+    }
+    buf[w][c] = v;
+    __syncthreads();
+    if (w == 0 && col < n) {
+      v = 0.f;
 #pragma unroll
-    for (int i = 0; i < 32; ++i) v += buf[i][c];
-    void* dst = which ? dbeta : dgamma;
-    if (dst) store1(dst, wt, col, v);
+      for (int i = 0; i < 32; ++i) v += buf[i][c];
+      void* dst = which ? dbeta : dgamma;
+      if (dst) store1(dst, wt, col, v);
+    }
+    __syncthreads();
   }
 }
 
@@ -458,7 +465,7 @@ hipError_t layer_norm_backward(const Mat& dY, const Mat& X, const float* mean, c
                                int wt, const Mat& dX, void* dgamma, void* dbeta, float* ws, hipStream_t s) {
   const bool weights = dgamma || dbeta;
   const int n = (int)X.cols;
-  const dim3 cgrid((unsigned)((n + 31) / 32), 2);
+  const dim3 cgrid((unsigned)std::min<int64_t>(((int64_t)n + 31) / 32, kColumnBlocks), 2);
   if (n == 0 || (X.rows == 0 && !weights)) return hipSuccess;
   if (X.rows == 0) {
     k_ln_columns<<<cgrid, 1024, 0, s>>>(nullptr, 0, n, dgamma, dbeta, wt);

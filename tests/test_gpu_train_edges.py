@@ -31,6 +31,20 @@ def test_layer_norm_statistics_of_rows_without_columns(m):
         assert not mean.any() and torch.allclose(rstd, torch.full_like(rstd, eps ** -0.5), rtol=4 * U, atol=0)
 
 
+def test_layer_norm_gradients_of_more_columns_than_a_launch_has_threads_for():
+    n = (1 << 27) + 37
+    g = torch.Generator(device="cuda").manual_seed(1)
+    X, dY = (torch.randint(-4, 5, (2, n), generator=g, device="cuda", dtype=torch.int8).to(F16) for _ in range(2))
+    mean, rstd = torch.tensor([0.5, 0.0], device="cuda"), torch.tensor([0.25, 2.0], device="cuda")
+    dX, dgamma, dbeta = aires.layer_norm_backward(dY, X, mean, rstd, need_dx=False)  # (small numbers: all exact)
+    assert dX is None
+    assert torch.equal(dbeta, dY[0].float() + dY[1].float())
+    assert torch.equal(dgamma, dY[0].float() * ((X[0].float() - 0.5) * 0.25) + dY[1].float() * (X[1].float() * 2))
+    none = torch.empty(0, n, dtype=F16, device="cuda")
+    for t in aires.layer_norm_backward(none, none, mean[:0], rstd[:0], need_dx=False)[1:]:
+        assert t.shape == (n,) and not t.any()
+
+
 # ----------------------------------------------------------- cross entropy
 
 @pytest.mark.parametrize("dt", [F32, BF16, F16])
