@@ -55,6 +55,12 @@ void same_device(const at::Tensor& first, const at::Tensor& x) {
 
 using Maybe = std::optional<at::Tensor>;
 
+// x was written through its address: a backward pass that has kept it is to
+// notice.  (Inference tensors count no versions.)
+void written(const at::Tensor& x) {
+  if (!x.is_inference()) x.unsafeGetTensorImpl()->bump_version();
+}
+
 py::tuple layer_norm(const at::Tensor& X, const Maybe& gamma, const Maybe& beta, double eps,
                      std::optional<at::ScalarType> out_dtype, bool stats, const Maybe& out, uintptr_t stream) {
   const aires_dense x = dense(X, "X");
@@ -84,6 +90,7 @@ py::tuple layer_norm(const at::Tensor& X, const Maybe& gamma, const Maybe& beta,
   check(aires_layer_norm(&x, g, b, wt, eps, &y, st ? mean.data_ptr<float>() : nullptr,
                          st ? rstd.data_ptr<float>() : nullptr, (void*)stream),
         "aires_layer_norm");
+  if (out) written(*out);
   if (!stats) return py::make_tuple(Y, py::none(), py::none());
   return py::make_tuple(Y, mean, rstd);
 }
@@ -224,6 +231,18 @@ void adamw(const py::sequence& params, const py::sequence& grads, const py::sequ
   }
   const aires_adamw_opts o{sizeof(aires_adamw_opts), seed, step, lr, beta1, beta2, eps, weight_decay, grad_scale};
   check(aires_adamw(table.data(), (int64_t)n, &o, (void*)stream), "aires_adamw");
+  for (size_t k = 0; k < n; ++k) {
+    const py::object po = params[k], mo = m[k], vo = v[k];
+    written(tensor(po));
+    for (const py::handle x : {mo.ptr(), vo.ptr()})
+      if (!PyTuple_Check(x.ptr())) written(tensor(x));
+      else
+        for (int i = 0; i < 2; ++i) written(tensor(PyTuple_GET_ITEM(x.ptr(), i)));
+    if (table[k].copy) {
+      const py::object co = c[k];
+      written(tensor(co));
+    }
+  }
 }
 
 }  // namespace

@@ -98,3 +98,32 @@ def test_small_probabilities_in_half_precision():
     # dz and the result are rounded to 11 bits; the exponent's argument is off by 4 U of 36 log2 e
     tol = (2 * 2.0 ** -11 + 4 * 52 * U + 64 * U) * want
     assert bool(((got.dW.double().cpu()[1:] - want).abs() <= tol)[some].all())
+
+
+# --------------------------------------------------------- tensors of torch's
+
+def test_tensors_that_are_written_count_a_version():
+    """A backward pass that kept a value from before raises instead of reading the new one."""
+    p = [torch.ones(300, device="cuda", requires_grad=True), torch.ones(5, 7, device="cuda")]
+    q = [torch.full_like(x, 0.1) for x in p]
+    copies = [torch.empty(300, dtype=BF16, device="cuda"), None]
+    for bits in (32, 8):
+        M, V = aires.adamw_state(p, bits=bits)
+        all_of = [*p, copies[0], *(y for x in (M + V) for y in (x if bits == 8 else (x,)))]
+        kept = (p[0] * p[0]).sum()
+        before, untouched = [x._version for x in all_of], [x._version for x in q]
+        aires.adamw(p, q, M, V, step=1, lr=0.1, copies=copies)
+        assert all(x._version > b for x, b in zip(all_of, before))
+        assert [x._version for x in q] == untouched
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            kept.backward()
+    X, out = torch.randn(4, 6, device="cuda"), torch.empty(4, 6, device="cuda")
+    before = out._version, X._version
+    aires.layer_norm(X, out=out)
+    assert out._version > before[0] and X._version == before[1]
+    with torch.inference_mode():  # (no versions there)
+        x = [torch.ones(8, device="cuda")]
+        M, V = aires.adamw_state(x)
+        aires.adamw(x, [torch.ones(8, device="cuda")], M, V, step=1, lr=0.5, weight_decay=0.0)
+        aires.layer_norm(X, out=torch.empty(4, 6, device="cuda"))
+    assert torch.allclose(x[0], torch.full((8,), 0.5, device="cuda"))
