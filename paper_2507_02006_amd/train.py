@@ -6,7 +6,8 @@ Matrices are device torch tensors of float32, bfloat16 or float16 with unit
 column stride (any row stride).  Work is enqueued on ``stream`` (torch's
 current stream by default), where inputs must be ready; outputs and
 workspaces are allocated for that stream and valid once it reaches the
-enqueued kernels.
+enqueued kernels.  Tensors given to a call with ``stream`` may be released
+before that: their memory is not reused until then.
 """
 from __future__ import annotations
 
@@ -83,7 +84,20 @@ def _run(call, x, stream, *args):
     if x.get_device() < 0:
         raise ValueError("expected device tensors")
     with _other_stream(x.device, stream) as s:
+        _keep(args, _torch.cuda.current_stream(x.device))
         return call(*args, s)
+
+
+def _keep(args, stream):
+    """Tells torch's allocator that the tensors in ``args`` (sequences and pairs
+    of them too) are in use on ``stream``, which may not be the one that they
+    were made on."""
+    for x in args:
+        if isinstance(x, _torch.Tensor):
+            if x.is_cuda:
+                x.record_stream(stream)
+        elif hasattr(x, "__getitem__"):
+            _keep(x, stream)
 
 
 def layer_norm(X, gamma=None, beta=None, *, eps: float = 1e-5, out_dtype=None, stats: bool = True, out=None,

@@ -127,3 +127,52 @@ def test_tensors_that_are_written_count_a_version():
         aires.adamw(x, [torch.ones(8, device="cuda")], M, V, step=1, lr=0.5, weight_decay=0.0)
         aires.layer_norm(X, out=torch.empty(4, 6, device="cuda"))
     assert torch.allclose(x[0], torch.full((8,), 0.5, device="cuda"))
+
+
+@pytest.mark.parametrize("what", ["layer_norm", "layer_norm_backward", "linear_xent", "adamw", "adamw_8"])
+def test_inputs_released_before_another_stream_reads_them(what):
+    """The call is behind other work on its stream when its inputs' last
+    references go; their memory is not handed out before it has run."""
+    m, n = 2048, 640
+    x, gamma = torch.randn(m, n, generator=gen(1)).cuda(), torch.ones(n, device="cuda")
+    W, y = torch.randn(300, n, generator=gen(2)).cuda(), torch.arange(m, device="cuda") % 300
+    _, mean, rstd = aires.layer_norm(x, gamma)
+    p, bits = [torch.ones(m, n, device="cuda")], 8 if what == "adamw_8" else 32
+    M, V = aires.adamw_state(p, bits=bits)
+
+    def call(X, **kw):
+        if what == "layer_norm":
+            return list(aires.layer_norm(X, gamma, **kw))
+        if what == "layer_norm_backward":
+            return list(aires.layer_norm_backward(X, x, mean, rstd, gamma, **kw))
+        if what == "linear_xent":
+            r = aires.linear_xent(X, W, y, **kw)
+            return [r.loss, r.row_loss, r.dH, r.dW]
+        # (any sequence will do)
+        aires.adamw(torch.nn.ParameterList(p), torch.nn.ParameterList([X]), M, V, step=1, lr=0.5, **kw)
+        return [p[0]]
+
+    def reset():
+        p[0].fill_(1.0)
+        for state in (M, V):
+            for t in (state[0] if bits == 8 else state):
+                t.zero_()
+
+    reset()
+    want = [t.clone() for t in call(x.clone())]
+    big = torch.randn(4096, 4096, device="cuda")
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    for stream in (s, s.cuda_stream):
+        X = x.clone()
+        reset()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(s):
+            for _ in range(20):
+                big @ big
+        got = call(X, stream=stream)
+        del X
+        over = [torch.full((m, n), float("nan"), device="cuda") for _ in range(3)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        del over
