@@ -35,7 +35,7 @@ void rows_and_loss(const XentArgs& x, const float2* part, int64_t tiles, const f
 bool xent_few_fits(int64_t T, int64_t D, int64_t V);
 int64_t xent_few_workspace(int64_t T, int64_t D, int64_t V, bool grads);
 hipError_t xent_few(const XentArgs& x, hipStream_t s);
-bool xent_rows_fits(int64_t T, int64_t D, int64_t V, int type);
+bool xent_rows_fits(int64_t T, int64_t D, int64_t V, int type, bool grads);
 int64_t xent_rows_workspace(int64_t T, int64_t D, int64_t V, bool grads);
 hipError_t xent_rows(const XentArgs& x, hipStream_t s);
 

@@ -743,7 +743,7 @@ void scores(const Scores& sc, int type, int TT, hipStream_t s) {
 
 int64_t linear_xent_workspace(int64_t T, int64_t D, int64_t V, int type, bool grads) {
   if (xent_few_fits(T, D, V)) return xent_few_workspace(T, D, V, grads);
-  if (xent_rows_fits(T, D, V, type)) return xent_rows_workspace(T, D, V, grads);
+  if (xent_rows_fits(T, D, V, type, grads)) return xent_rows_workspace(T, D, V, grads);
   return layout_of(T, D, V, type, grads).bytes;
 }
 
@@ -753,7 +753,7 @@ hipError_t linear_xent(const XentArgs& x, hipStream_t s) {
   const int type = x.H.type;
   const bool f16 = type == DT_F16;
   if (xent_few_fits(T, D, V)) return xent_few(x, s);
-  if (xent_rows_fits(T, D, V, type)) return xent_rows(x, s);
+  if (xent_rows_fits(T, D, V, type, grads)) return xent_rows(x, s);
   const Layout l = layout_of(T, D, V, type, grads);
   char* ws = static_cast<char*>(x.ws);
   float* scale = (float*)(ws + l.scale);

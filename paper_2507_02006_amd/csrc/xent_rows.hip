@@ -42,10 +42,17 @@ Layout layout_of(int64_t T, int64_t D, int64_t V, bool grads) {
 
 // fp32 tables would be split into planes (16 bytes moved for each 4), tables
 // of an odd number of columns copied (6 for 2): with few rows that is the whole
-// work.  16-bit tables that the tiles read as they lie stay with them.
-bool xent_rows_fits(int64_t T, int64_t D, int64_t V, int type) {
+// work.  16-bit tables that the tiles read as they lie stay with them, and so do
+// calls whose gradients, fp32 products here, cost more than the copy.  Loss, and
+// loss and gradients, in us, here and in tiles:
+//   f32, 60013 x 256:   1 row 20, 53 and 49, 110;  32 rows 31, 82 and 50, 117;
+//                       64 rows 43, 118 and 53, 132 (60013 x 333: 65, 233 and 66, 183)
+//   f16, 60013 x 333:  16 rows 30, 79 and 33, 83;  32 rows 34, 103 and 34, 84;
+//                       64 rows 43, 165 and 34, 85
+//   f16, 261215 x 815: 16 rows 150, 469 and 283, 682;  32 rows 168, 782 and 283, 681
+bool xent_rows_fits(int64_t T, int64_t D, int64_t V, int type, bool grads) {
   if (T < 1 || few_shape(D, T).DT == 0) return false;
-  return type == DT_F32 ? T <= 64 : D % 8 != 0 && T <= 32;
+  return type == DT_F32 ? T <= 64 : D % 8 != 0 && T <= (grads ? 16 : 32);
 }
 
 int64_t xent_rows_workspace(int64_t T, int64_t D, int64_t V, bool grads) { return layout_of(T, D, V, grads).bytes; }
