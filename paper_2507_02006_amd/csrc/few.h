@@ -479,14 +479,20 @@ void few_launch(const FewShape& f, const Few& a, unsigned grid, hipStream_t s) {
   }
 }
 
+// (16-bit rows come kept by 32 at most, by 16 with gradients: xent_rows_fits)
 template <int MODE>
 void few_launch(const FewShape& f, const Few& a, unsigned grid, hipStream_t s) {
   auto of = [&](auto t) {
     constexpr int TYPE = decltype(t)::value;
+    constexpr int MOST = TYPE == DT_F32 || MODE == FEW_CLASSES || MODE == FEW_CLASSES_TRAIN ? 4 : MODE == FEW_STATS ? 2 : 1;
     if (f.KT == 1) few_launch<1, MODE, TYPE>(f, a, grid, s);
-    else if (f.KT == 2) few_launch<2, MODE, TYPE>(f, a, grid, s);
-    else if (f.KT == 3) few_launch<3, MODE, TYPE>(f, a, grid, s);
-    else few_launch<4, MODE, TYPE>(f, a, grid, s);
+    else if constexpr (MOST >= 2) {
+      if (f.KT == 2) few_launch<2, MODE, TYPE>(f, a, grid, s);
+      else if constexpr (MOST >= 4) {
+        if (f.KT == 3) few_launch<3, MODE, TYPE>(f, a, grid, s);
+        else few_launch<4, MODE, TYPE>(f, a, grid, s);
+      }
+    }
   };
   if (a.S.type == DT_F32) of(std::integral_constant<int, DT_F32>{});
   else if (a.S.type == DT_BF16) of(std::integral_constant<int, DT_BF16>{});

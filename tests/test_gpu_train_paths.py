@@ -1,8 +1,10 @@
-"""Sizes of every path, tile and kernel shape of the training calls, each against
+"""Sizes chosen so that every kernel of the training calls runs, each against
 64 bits, in a workspace of exactly the stated size that held NaNs (GPU)."""
 import ctypes
 import math
+import os
 import random
+import re
 
 import pytest
 
@@ -10,6 +12,7 @@ torch = pytest.importorskip("torch")
 import paper_2507_02006_amd as aires  # noqa: E402
 from paper_2507_02006_amd import _binding as B_  # noqa: E402
 from test_gpu_train import norm_data, xent_check, xent_data, xent_ref  # noqa: E402
+from test_kernel_resources import code_objects, kernels  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -146,3 +149,59 @@ def test_layer_norm(m, n):
                                            torch.cuda.current_stream().cuda_stream), "aires_layer_norm_backward")
     assert bool((work[need.value:] == 255).all()), "written past the workspace"
     assert torch.equal(out, dX) and torch.equal(dg, dgamma) and torch.equal(db, dbeta)
+
+
+OURS = re.compile(r"^k_(ln_|adamw_|few$|count$|scores$|rows$|total$|gradients$|finish$|zero$|pack$)")
+
+
+def built():
+    """(name, template arguments) of the training calls' kernels in the library."""
+    with open(os.path.join(os.path.dirname(B_.__file__), "libaires.so"), "rb") as f:
+        names = {n for elf in code_objects(f.read()) for n in kernels(elf)}
+    found = set()
+    for n in names:
+        m = re.search(r"_GLOBAL__N_1(\d+)(k_\w*)", n)
+        if m:
+            name, rest = m[2][:int(m[1])], m[2][int(m[1]):]
+            args = re.match(r"I((?:L[a-z]\d+E)+)E", rest)
+            if OURS.match(name):
+                found.add((name, tuple(int(x) for x in re.findall(r"L[a-z](\d+)E", args[1])) if args else ()))
+    return found
+
+
+def test_every_kernel_runs():
+    """The sizes above, and the few calls that have none, launch every kernel
+    that the library holds for these calls."""
+    from torch.profiler import ProfilerActivity, profile
+    want = built()
+    assert len(want) > 200
+
+    def calls():
+        for t, d, v in XENT:
+            for dt in (F32, BF16, F16):
+                H, W = torch.zeros(t, d, dtype=dt, device="cuda"), torch.zeros(v, d, dtype=dt, device="cuda")
+                y = torch.zeros(t, dtype=torch.int64, device="cuda")
+                for grads in (True, False):
+                    aires.linear_xent(H, W, y, grads=grads)
+        aires.linear_xent(torch.zeros(0, 8, device="cuda"), torch.zeros(300, 8, device="cuda"), y[:0])
+        for m, n in NORM:
+            X = torch.zeros(m, n, dtype=F16, device="cuda")
+            _, mean, rstd = aires.layer_norm(X)
+            aires.layer_norm_backward(X, X, mean, rstd)
+        aires.layer_norm(torch.empty(3, 0, device="cuda"))
+        for bits in (8, 32):
+            p = [torch.zeros(300, device="cuda")]
+            aires.adamw(p, [p[0].clone()], *aires.adamw_state(p, bits=bits), step=1, lr=0.1)
+        torch.cuda.synchronize()
+
+    calls()
+    with profile(activities=[ProfilerActivity.CUDA]) as trace:
+        calls()
+    ran = set()
+    for e in trace.events():
+        m = re.search(r"aires::kern::\(anonymous namespace\)::(k_\w+)(?:<([^>]*)>)?\(", e.name)
+        if m and OURS.match(m[1]):
+            args = [x.strip() for x in (m[2] or "").split(",") if x.strip()]
+            ran.add((m[1], tuple({"true": 1, "false": 0}.get(x) if x in ("true", "false") else int(x) for x in args)))
+    assert ran <= want, sorted(ran - want)
+    assert ran == want, sorted(want - ran)
