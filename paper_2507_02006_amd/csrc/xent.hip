@@ -163,7 +163,7 @@ __global__ __launch_bounds__(score_threads(TYPE, TT), 2) void k_scores(Scores s)
   f32x16 acc[T_::MT][T_::NT];
   // Labels, as they come: they are on their way during the products.
   uint32_t low[GRAD ? 1 : T_::NT], high[GRAD ? 1 : T_::NT];
-  if constexpr (!GRAD)
+  if constexpr (!GRAD) {
 #pragma unroll
     for (int j = 0; j < T_::NT; ++j) {
       const int64_t t = t0 + T_::col(j), at = t < s.T ? t : s.T - 1;
@@ -171,6 +171,9 @@ __global__ __launch_bounds__(score_threads(TYPE, TT), 2) void k_scores(Scores s)
       low[j] = l[0];
       high[j] = l[s.i64 ? 1 : 0];
     }
+    // They stay before the stages' loads, which are waited for by their number.
+    asm volatile("" ::: "memory");
+  }
   T_::run(s.W, v0, s.H, t0, 0, s.steps, lds, acc);
   const int lane = threadIdx.x & 63, wm = (threadIdx.x >> 6) / (T_::WAVES / NWM);
   __syncthreads();  // the stages' LDS changes its use
