@@ -673,7 +673,8 @@ aires_status aires_linear_xent_workspace(int64_t t, int64_t d, int64_t v, int32_
  * is gone through in pieces, whose dz goes to the workspace in the operands'
  * precision (16 bits for 16-bit operands, all of fp32's for fp32).  A NaN in a
  * row of H makes that row's loss and dH NaN, if it has a label, and dW in any
- * case (its share of dW is 0 times NaN).  W is finite.
+ * case (its share of dW is 0 times NaN); so does an infinity.  W is finite: a
+ * row of it with an infinity may give NaN where its scores are -infinity.
  * Errors: AIRES_E_INVALID_ARG (NULL, bad type or reduction, ld < ncols, one
  * of dH and dW, grad_scale not finite), AIRES_E_DIM (sizes or types differ,
  * v or d = 0 with t > 0), AIRES_E_UNSUPPORTED (t > 2^29, v >= 2^31, d >= 2^21,

@@ -98,9 +98,10 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_few(Few a) {
   // Rows n16 of each row tile, columns 4 q ... of each column tile, as they
   // come: converting them waits for them, so that is left to their use.  Rows
   // past the end repeat the last one, whose dz is not used again, columns the
-  // last group of four, which meets zeros of K; of a group that D cuts the
-  // values past D are taken out at their use (in the last rows they might lie
-  // past the array: read one by one there).
+  // last group of four, which meets zeros of K (so an infinity in it makes its
+  // row's scores NaN: W has none, and a row of H with one has no finite loss); of
+  // a group that D cuts the values past D are taken out at their use (in the last
+  // rows they might lie past the array: read one by one there).
   using E = std::conditional_t<WIDE, float, uint16_t>;
   using Raw = std::conditional_t<WIDE, f32x4_el, u16x4_el>;
   Raw raw[RT][DT];

@@ -36,7 +36,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 // A 16-bit operand in memory, rows 16-byte aligned, `cols` a multiple of 8.
 // K-contiguous: `rows` are m, `cols` k; k past `cols` repeats the row's last
-// chunk (the other operand holds zeros there).  K-major: `rows` are k, `cols` m.
+// chunk (the other operand holds zeros there, so that chunk has to be finite).  K-major: `rows` are k, `cols` m.
 struct Panel {
   const uint16_t* data;
   int64_t ld, rows, cols;
