@@ -650,7 +650,10 @@ typedef enum aires_reduction {
 } aires_reduction;
 
 /* Bytes of workspace that aires_linear_xent needs for H (t x d) and W (v x
-   d) of one type; grads = 0 for the loss alone.
+   d) of one type, at any alignment and stride; grads = 0 for the loss alone.
+   It holds a copy of H, a copy of W or of a piece of it (1 GiB at most), dz of a
+   piece (256 MB, or 256 entries if those are more) and 8 bytes for each row and
+   256 entries.
    Errors: AIRES_E_INVALID_ARG, AIRES_E_DIM, AIRES_E_UNSUPPORTED. */
 aires_status aires_linear_xent_workspace(int64_t t, int64_t d, int64_t v, int32_t dtype, int32_t grads,
                                          int64_t *bytes);

@@ -38,6 +38,7 @@ namespace {
 
 constexpr int TV = 256;  // table entries of a tile of scores
 constexpr int64_t kPieceBytes = int64_t(256) << 20;  // dz of one piece of the table
+constexpr int64_t kCopyBytes = int64_t(1) << 30;     // packed rows of the table
 // dz in fp16, which is 1 at most, is held times this: as high as fp16 goes.  A
 // probability keeps its 11 bits down to 2^-29 (times 2^10: to 2^-24, which a
 // large gradient scale brings into an fp16 result's range).
@@ -625,6 +626,7 @@ unsigned grid_of(int64_t items, int64_t per) {
 // Sizes and places in the workspace.
 struct Layout {
   int64_t width, planes, step;         // columns and planes of the packed operands, k of a step
+  int64_t copy;                        // table entries that the workspace has room to pack
   int TT, G;                           // tiles
   int64_t piece, Tp, ldz;              // table entries of a piece, rows of dz and their stride
   int dh_per, dh_slices, dw_per, dw_slices;
@@ -671,11 +673,16 @@ Layout layout_of(int64_t T, int64_t D, int64_t V, int type, bool grads) {
   l.sums = take(rows_and_loss_workspace(T));
   l.part = take(8 * T * (up(V, TV) / TV));
   l.h = take(2 * l.planes * T * l.width);
-  l.w = take(2 * l.planes * V * l.width);
+  // A table whose copy would be larger than kCopyBytes is packed in pieces, once
+  // for the first scores and again for dz: the workspace does not grow with it.
+  const bool whole = 2 * l.planes * l.width * V <= kCopyBytes;
+  l.copy = whole ? V : std::max<int64_t>(TV, kCopyBytes / (2 * l.planes * l.width) / TV * TV);
   if (grads) {
-    const int64_t most = std::max<int64_t>(TV, kPieceBytes / (2 * l.planes * std::max<int64_t>(l.Tp, 1)) / TV * TV);
+    const int64_t most = std::min(std::max<int64_t>(TV, kPieceBytes / (2 * l.planes * std::max<int64_t>(l.Tp, 1)) / TV * TV),
+                                  up(l.copy, TV));
     const int64_t pieces = std::max<int64_t>(1, (V + most - 1) / most);
     l.piece = up((V + pieces - 1) / pieces, TV);  // (of one size: a small last one costs more than its share)
+    if (!whole) l.copy = l.piece;
     const int dh_steps = (int)(up(std::min(l.piece, V), l.step) / l.step), dw_steps = (int)(up(T, l.step) / l.step);
     // Shares of k of about equal length, one workgroup a CU with large tiles,
     // two with small ones; none shorter than `least` steps.  Small tiles where
@@ -697,6 +704,7 @@ Layout layout_of(int64_t T, int64_t D, int64_t V, int type, bool grads) {
     l.ldz = l.planes * l.piece + 64;
     l.dz = take(2 * l.Tp * l.ldz);
   }
+  l.w = take(2 * l.planes * std::min(l.copy, V) * l.width);
   l.bytes = at;
   return l;
 }
@@ -709,22 +717,40 @@ bool lies_well(const Mat& X, const Layout& l, bool whole) {
          (reinterpret_cast<uintptr_t>(X.data) & 15) == 0;
 }
 
+// Rows of X, and of Y where that has any, packed to x and y.
+void pack(const Mat& X, const Mat& Y, const Layout& l, char* x, char* y, hipStream_t s) {
+  Pack a{X, Y, (uint16_t*)x, (uint16_t*)y, l.width, 0};
+  a.first = grid_of(X.rows * (l.width / 4), 1024);
+  const unsigned grid = a.first + (Y.rows > 0 ? grid_of(Y.rows * (l.width / 4), 1024) : 0);
+  if (l.planes == 1) k_pack<false><<<grid, 256, 0, s>>>(a);
+  else k_pack<true><<<grid, 256, 0, s>>>(a);
+}
+
 // The operands as they lie, else packed into the workspace with zeros past
-// their columns.
+// their columns; a table that is packed in pieces is left to piece_of.
 void panels_of(const Mat& H, const Mat& W, const Layout& l, char* ws, Panel& h, Panel& w, hipStream_t s) {
-  const bool ph = !lies_well(H, l, true), pw = !lies_well(W, l, false);
+  const bool ph = !lies_well(H, l, true), pw = !lies_well(W, l, false) && l.copy >= W.rows;
   auto panel = [&](const Mat& X, bool packed, int64_t at) {
     return packed ? Panel{reinterpret_cast<uint16_t*>(ws + at), l.planes * l.width, X.rows, l.width}
                   : Panel{static_cast<const uint16_t*>(X.data), X.ld, X.rows, X.cols};
   };
   h = panel(H, ph, l.h);
   w = panel(W, pw, l.w);
-  if (!ph && !pw) return;
-  Pack a{ph ? H : W, W, (uint16_t*)(ws + (ph ? l.h : l.w)), (uint16_t*)(ws + l.w), l.width, 0};
-  a.first = grid_of(a.X.rows * (l.width / 4), 1024);
-  const unsigned grid = a.first + (ph && pw ? grid_of(W.rows * (l.width / 4), 1024) : 0);
-  if (l.planes == 1) k_pack<false><<<grid, 256, 0, s>>>(a);
-  else k_pack<true><<<grid, 256, 0, s>>>(a);
+  const Mat none{};
+  if (ph && pw) pack(H, W, l, ws + l.h, ws + l.w, s);
+  else if (ph) pack(H, none, l, ws + l.h, nullptr, s);
+  else if (pw) pack(W, none, l, ws + l.w, nullptr, s);
+}
+
+// Packs entries [v0, v0 + n) of a table that is packed in pieces and points w at
+// them by their numbers in the whole table.
+void piece_of(const Mat& W, const Layout& l, char* ws, int64_t v0, int64_t n, Panel& w, hipStream_t s) {
+  if (l.copy >= W.rows || lies_well(W, l, false)) return;
+  Mat some = W;
+  some.data = (char*)W.data + v0 * W.ld * dtype_bytes(W.type);
+  some.rows = n;
+  pack(some, Mat{}, l, ws + l.w, nullptr, s);
+  w = Panel{reinterpret_cast<uint16_t*>(ws + l.w) - v0 * l.planes * l.width, l.planes * l.width, v0 + n, l.width};
 }
 
 template <bool GRAD, int TYPE>
@@ -769,9 +795,11 @@ hipError_t linear_xent(const XentArgs& x, hipStream_t s) {
     sc.ticket = (uint32_t*)(ws + l.ticket);
     sc.target = (float*)(ws + l.target);
     // (a launch holds fewer than 2^32 threads)
-    const int64_t most = std::max<int64_t>(1, (int64_t(1) << 22) / (up(T, l.TT) / l.TT)) * TV;
+    const int64_t most = std::min(std::max<int64_t>(1, (int64_t(1) << 22) / (up(T, l.TT) / l.TT)) * TV,
+                                  lies_well(x.W, l, false) ? up(V, TV) : up(l.copy, TV));
     for (int64_t v0 = 0; v0 < V; v0 += most) {
       sc.v0 = v0; sc.v1 = std::min(V, v0 + most);
+      piece_of(x.W, l, ws, v0, sc.v1 - v0, sc.W, s);
       sc.part = (float2*)(ws + l.part) + v0 / TV * T;
       scores<false>(sc, type, l.TT, s);
     }
@@ -801,6 +829,7 @@ hipError_t linear_xent(const XentArgs& x, hipStream_t s) {
   for (int64_t v0 = 0; v0 < V; v0 += l.piece) {
     const int64_t n = std::min(l.piece, V - v0);
     sc.v0 = v0; sc.v1 = v0 + n;
+    piece_of(x.W, l, ws, v0, n, sc.W, s);
     scores<true>(sc, type, l.TT, s);
     sc.total.n = 0;
     Gradients g{};

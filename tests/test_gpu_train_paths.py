@@ -112,6 +112,63 @@ def test_linear_xent_of_rows_that_are_no_numbers_and_have_no_label(t, d, v, dt):
             assert torch.equal(got.dH, clean.dH) and not got.dH[off.cuda()].any()
 
 
+@pytest.mark.parametrize("t,d,v", [(70, 9, 9000013), (300, 9, 9000013)])
+def test_linear_xent_table_packed_in_pieces(t, d, v):
+    """Columns that have to be copied and a copy of more than 1 GiB: the same
+    bits as where the table is read as it lies, in as many columns as a step has."""
+    g = torch.Generator(device="cuda").manual_seed(t)
+    for dt in (BF16, F16):
+        wide = [torch.zeros(n, 64, dtype=dt, device="cuda") for n in (t, v)]
+        for x in wide:
+            x[:, :d] = torch.randn(x.shape[0], d, generator=g, device="cuda")
+        H, W = (x[:, :d].contiguous() for x in wide)
+        y = torch.randint(-1, v, (t,), generator=g, device="cuda")
+        for grads in (True, False):
+            a, b = aires.linear_xent(H, W, y, grads=grads), aires.linear_xent(*wide, y, grads=grads)
+            assert torch.equal(a.loss, b.loss) and torch.equal(a.row_loss, b.row_loss)
+            assert bool(a.row_loss[y >= 0].isfinite().all()) and bool((a.row_loss[y >= 0] > 0).all())
+            if grads:
+                assert torch.equal(a.dH, b.dH[:, :d]) and torch.equal(a.dW, b.dW[:, :d])
+
+
+def test_linear_xent_planes_of_a_table_made_in_pieces():
+    t, d, v = 70, 8, 12000007  # (planes of 1.2e9 bytes)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    H, W = torch.randn(t, d, generator=g, device="cuda"), torch.randn(v, d, generator=g, device="cuda")
+    y = torch.randint(0, v, (t,), generator=g, device="cuda")
+    y[0], y[1], y[2] = 0, v - 1, -1
+    got = aires.linear_xent(H, W, y)
+    alone = aires.linear_xent(H, W, y, grads=False)
+    assert torch.equal(alone.row_loss, got.row_loss)
+    h, there = H.double(), (y >= 0).double()
+    lse = torch.full((t,), -math.inf, dtype=torch.float64, device="cuda")
+    step = 1 << 20
+    for v0 in range(0, v, step):
+        lse = torch.logaddexp(lse, torch.logsumexp(h @ W[v0:v0 + step].double().t(), 1))
+    target = (h * W[y.clamp(min=0)].double()).sum(1)
+    ez = (d + 8) * U * (h.abs() @ W.abs().amax(0).double())
+    el = ez + 256 * U * (1 + lse.abs() + 40)  # (no score is above 40)
+    assert bool(((got.row_loss.double() - (lse - target) * there).abs() <= 2 * el * there).all())
+    c = there.sum()
+    dH, eH = torch.zeros(t, d, dtype=torch.float64, device="cuda"), torch.zeros(t, d, dtype=torch.float64, device="cuda")
+    for v0 in range(0, v, step):
+        w = W[v0:v0 + step].double()
+        z = h @ w.t()
+        assert float(z.abs().max()) < 40
+        p = torch.exp(z - lse[:, None])
+        hot = torch.zeros_like(p)
+        here = ((y >= v0) & (y < v0 + w.shape[0])).nonzero().squeeze(1)
+        hot[here, y[here] - v0] = 1
+        dz = (p - hot) * there[:, None] / c
+        # as for any size: a score off by ez, lse by el; dz kept in planes; chains of 1024 additions
+        e = (p * (2 * (ez + el)[:, None] + 16 * U) + U * (p - hot).abs() + 2.0 ** -40 + 2 * U * hot) * there[:, None] / c
+        dH += dz @ w
+        eH += e @ w.abs() + 1024 * U * (dz.abs() @ w.abs())
+        dW, eW = dz.t() @ h, e.t() @ h.abs() + 1024 * U * (dz.abs().t() @ h.abs())
+        assert bool(((got.dW[v0:v0 + step].double() - dW).abs() <= eW + U * dW.abs()).all()), v0
+    assert bool(((got.dH.double() - dH).abs() <= eH + U * dH.abs()).all())
+
+
 @pytest.mark.parametrize("m,n", NORM)
 def test_layer_norm(m, n):
     """Rows of a large matrix as on their own (those are held against 64 bits
