@@ -676,7 +676,7 @@ Layout layout_of(int64_t T, int64_t D, int64_t V, int type, bool grads) {
   // A table whose copy would be larger than kCopyBytes is packed in pieces, once
   // for the first scores and again for dz: the workspace does not grow with it.
   const bool whole = 2 * l.planes * l.width * V <= kCopyBytes;
-  l.copy = whole ? V : std::max<int64_t>(TV, kCopyBytes / (2 * l.planes * l.width) / TV * TV);
+  l.copy = whole ? std::max<int64_t>(V, 1) : std::max<int64_t>(TV, kCopyBytes / (2 * l.planes * l.width) / TV * TV);
   if (grads) {
     const int64_t most = std::min(std::max<int64_t>(TV, kPieceBytes / (2 * l.planes * std::max<int64_t>(l.Tp, 1)) / TV * TV),
                                   up(l.copy, TV));
