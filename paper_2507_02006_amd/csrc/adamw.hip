@@ -255,11 +255,10 @@ __global__ __launch_bounds__(BLOCK) void k_adamw_8(Table tab) {
     const float bm = block_max(m[q]), bv = block_max(v[q]);
     big = lane == 2 * q ? bm : lane == 2 * q + 1 ? bv : big;
   }
-  // all scales and their inverses at once, each rounded once: the divisions are
-  // what they cost
+  // all scales and their inverses at once: the division is what they cost
   const bool used = big >= TINY;
-  const float top = lane & 1 ? TOP_V : TOP_M;
-  const float scale = used ? big / top : 0.f, inverse = used ? top / big : 0.f;
+  const float top = lane & 1 ? TOP_V : TOP_M, one = lane & 1 ? 1.f / TOP_V : 1.f / TOP_M;
+  const float scale = used ? big * one : 0.f, inverse = used ? 1.f / big * top : 0.f;
   auto of = [](float x, int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), l)); };
 #pragma unroll
   for (int q = 0; q < PER; ++q) {

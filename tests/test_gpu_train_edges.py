@@ -100,21 +100,6 @@ def test_small_probabilities_in_half_precision():
     assert bool(((got.dW.double().cpu()[1:] - want).abs() <= tol)[some].all())
 
 
-# ------------------------------------------------------------------- AdamW
-
-def test_adamw_scales_of_8_bit_moments_are_rounded_once():
-    """Without a past (betas 0) the moments are g and g^2 as fp32 has them: a
-    block's scale is the fp32 quotient of its largest and the largest code."""
-    n = 256 * 4000 + 77
-    g = torch.randn(n, generator=gen(3)) * torch.randn(n, generator=gen(4)).mul(2).exp()
-    P = [torch.zeros(n, device="cuda")]
-    M, V = aires.adamw_state(P, bits=8)
-    aires.adamw(P, [g.cuda()], M, V, step=1, lr=1e-3, betas=(0.0, 0.0))
-    for x, top, got in ((g.abs(), 448.0, M[0][1]), (g * g, 57344.0, V[0][1])):
-        big = torch.nn.functional.pad(x, (0, -n % 256)).view(-1, 256).amax(1)
-        assert torch.equal(got.cpu(), big / torch.full_like(big, top))
-
-
 # --------------------------------------------------------- tensors of torch's
 
 def test_tensors_that_are_written_count_a_version():
