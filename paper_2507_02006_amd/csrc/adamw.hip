@@ -255,7 +255,10 @@ __global__ __launch_bounds__(BLOCK) void k_adamw_8(Table tab) {
     const float bm = block_max(m[q]), bv = block_max(v[q]);
     big = lane == 2 * q ? bm : lane == 2 * q + 1 ? bv : big;
   }
-  // all scales and their inverses at once: the division is what they cost
+  // All scales and their inverses at once: the division is what they cost.  Both
+  // are rounded as torch rounds such quotients on the device (x / constant as a
+  // product with its reciprocal, constant / x as one with x's): rounded once
+  // instead, codes next to a boundary come out otherwise than there.
   const bool used = big >= TINY;
   const float top = lane & 1 ? TOP_V : TOP_M, one = lane & 1 ? 1.f / TOP_V : 1.f / TOP_M;
   const float scale = used ? big * one : 0.f, inverse = used ? 1.f / big * top : 0.f;
