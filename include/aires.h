@@ -735,7 +735,9 @@ typedef struct aires_adamw_opts {
  * value's index, its tensor's position in the call and opts->seed (the low
  * half for m, the high half for v), so a step's result is a function of its
  * inputs.  A positive second moment is never rounded to 0.  Values that are
- * not finite are stored as NaN and leave their block's scale alone.
+ * not finite are stored as NaN and leave their block's scale alone.  The step,
+ * the options and the seed are the call's own: a graph that captured it repeats
+ * them, and with them one bias correction and one pattern of rounding.
  * Errors: AIRES_E_INVALID_ARG (NULL, bad type or struct_size, step < 1,
  * betas outside [0, 1), options not finite, eps < 0, one scale without the
  * other), AIRES_E_DIM (negative n), AIRES_E_UNSUPPORTED (n above 2^35),

@@ -16,9 +16,10 @@
 //
 // Measured: forward 262144 x 512, f32 -> bf16, 149 us (5.4 TB/s); backward with
 // dgamma and dbeta, 1048576 x 256, dY bf16, X and dX f32, 473 us (5.7 TB/s);
-// 4001 x 6001, f16, 57 us (2.5 TB/s: rows of an odd length lie at odd addresses,
-// and a workgroup shares a row, whose two sums wait for all of its wavefronts).
-// 128 x 64 takes 3 us, which is a launch.
+// 4001 x 6001, f16, 57 us (2.5 TB/s: a 16-bit chunk is converted in the branch that
+// guards its load, so each is waited for before the next is asked for, four a
+// row here; and the wavefronts that share a row meet over its sums).  128 x 64
+// takes 3 us, which is a launch.
 #include "train.h"
 
 #include <algorithm>
@@ -34,7 +35,8 @@ constexpr int TEAM_BLOCK = 256;    // threads of a workgroup of teams
 constexpr int MAX_BLOCK = 1024;    // threads of a workgroup that shares a row
 constexpr int MAX_E = 8;           // chunks of four columns a lane holds
 // Widest rows held in registers: 1024 threads have 128 registers each, and the
-// backward pass holds five rows' worth.
+// backward pass holds five rows' worth.  (The widest forward shape, E = 8 by a
+// workgroup, keeps three of its 96 values in scratch memory.)
 constexpr int64_t kForwardCols = (int64_t)MAX_BLOCK * MAX_E * 4;
 constexpr int64_t kBackwardCols = (int64_t)MAX_BLOCK * 4 * 4;
 

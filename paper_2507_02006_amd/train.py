@@ -3,7 +3,9 @@ a table, AdamW (the dense-array calls of include/aires.h; argument
 marshalling only).
 
 Matrices are device torch tensors of float32, bfloat16 or float16 with unit
-column stride (any row stride).  Work is enqueued on ``stream`` (torch's
+column stride (any row stride).  The calls take no part in autograd: gradients
+are asked for by their own calls, and tensors that are written count a version.
+Work is enqueued on ``stream`` (torch's
 current stream by default), where inputs must be ready; outputs and
 workspaces are allocated for that stream and valid once it reaches the
 enqueued kernels.  Tensors given to a call with ``stream`` may be released
@@ -167,7 +169,8 @@ def adamw(params, grads, exp_avg, exp_avg_sq, *, step: int, lr: float, betas=(0.
     exp_avg, exp_avg_sq: as from ``adamw_state``, in 32 or 8 bits (``seed``
     then drives their rounding: pass another one each step); copies:
     tensors that receive the updated parameters in their own type (or None,
-    also for single entries).  ``step`` counts from 1."""
+    also for single entries).  ``step`` counts from 1.  A graph that captured
+    the call repeats its step, options and seed."""
     c = _calls or _load()
     if len(params) == 0 and len(grads) == len(exp_avg) == len(exp_avg_sq) == 0:
         return
