@@ -1,0 +1,441 @@
+"""The operators of a deeper node model's trunk, answers and update, as cases that can be timed and compared.
+
+Next to the layer norm, the loss and the update of `operators.py`, a model with
+several layers on top of the aggregated features keeps a residual stream, holds
+its weights and what they multiply in 8 bits, answers with probabilities, and
+clips its gradients.  Kinds of work:
+
+  rms        S = X + R (a residual stream), Y = S / root mean square of its
+             rows * gamma, in a float type or in 8 bits
+  rms_back   gradients of it; dS is what reaches S past the norm
+  hold       a matrix in 8 bits with its scales, as it lies, transposed, or both
+  product    Y = A B^T of two matrices held in 8 bits
+  logp       log probability of a label, entropy and the most probable classes
+             of each row of scores
+  logp_back  gradient of the scores from those of log probability and entropy
+  clip       norm over the gradients of all tensors; gradients scaled to a norm
+             of `MAX_NORM` at most
+
+8 bits are e4m3 with one float32 scale for 128 consecutive values of a row, or
+for 128 x 128 values ("tiles"): the largest magnitude is 448 scales.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False  # False: the plain forms; True: the framework's operators
+
+DEV = "cuda" if torch.cuda.is_available() else "cpu"
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16, "e4m3": torch.float8_e4m3fn}
+SIZE = {"f32": 4, "bf16": 2, "f16": 2, "e4m3": 1 + 4 / 128}
+EPS = 1e-6
+BLOCK = 128
+TOP8 = 448.0
+TINY = 2.0 ** -110  # a block with no larger value is held as zeros
+MAX_NORM = 1.0
+
+
+def listed():
+    return [
+        # one node answered at a time: launches and latency
+        dict(name="rms-node", kind="rms", m=1, n=512, x="bf16", r="bf16", y="e4m3"),
+        # every node of the mid-sized graph, normalised into the operand of a product in 8 bits
+        dict(name="rms-features", kind="rms", m=262144, n=512, x="bf16", r="bf16", y="e4m3"),
+        # backward pass over wide rows of an odd length, with the residual stream's own gradient
+        dict(name="rms-back-words", kind="rms_back", m=4001, n=6001, x="f16", y="f16", ds="f16"),
+        # activations of a training step, for the forward product and for the weights' gradient
+        dict(name="hold-both", kind="hold", m=65536, n=1000, x="bf16", tiles=False, order="both"),
+        # a few queried nodes through one layer: bound by the weights' bytes
+        dict(name="product-query", kind="product", m=5, n=8192, k=2048, tiles=True, y="bf16"),
+        # a layer over a large batch of nodes
+        dict(name="product-layer", kind="product", m=16384, n=8192, k=4096, tiles=True, y="bf16"),
+        # a layer's weight gradient: sums over an odd number of nodes, both operands scaled by row
+        dict(name="product-weights", kind="product", m=1000, n=520, k=65537, tiles=False, y="f32"),
+        # three nodes scored against every node of the mid-sized graph
+        dict(name="logp-query", kind="logp", t=3, v=262144, x="bf16", top=10, mask=0.0),
+        # node classification over a whole graph: few classes, many rows, some classes ruled out
+        dict(name="logp-classes", kind="logp", t=150001, v=41, x="f32", top=5, mask=0.2),
+        # training on answers: a large batch against a mid-sized table, an odd number of classes
+        dict(name="logp-back-table", kind="logp_back", t=4099, v=30011, x="bf16", mask=0.0),
+        # every weight of six layers at once: many small tensors
+        dict(name="clip-layers", kind="clip", rows=4096, f=256, layers=6, g="f32", out=True),
+        # the gradient of a node table; the update takes the scale, nothing is written
+        dict(name="clip-table", kind="clip", rows=262144, f=512, layers=2, g="bf16", out=False),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind = rng.choice(["rms", "rms_back", "hold", "product", "product", "product", "logp", "logp", "logp_back", "clip"])
+    any_type = lambda: rng.choice(["f32", "bf16", "f16"])  # noqa: E731
+    if kind == "rms":
+        n = _log(rng, 16, 12000)
+        m = _log(rng, 1, min(1048576, 1.3e8 / n))
+        return dict(kind=kind, m=m, n=n, x=any_type(), r=rng.choice(["", "f32", "bf16", "f16"]),
+                    y=rng.choice(["f32", "bf16", "f16", "e4m3", "e4m3"]))
+    if kind == "rms_back":
+        n = _log(rng, 16, 12000)
+        m = _log(rng, 1, min(1048576, 1.3e8 / n))
+        return dict(kind=kind, m=m, n=n, x=any_type(), y=any_type(), ds=rng.choice(["", "f32", "bf16", "f16"]))
+    if kind == "hold":
+        n = _log(rng, 16, 12000)
+        return dict(kind=kind, m=_log(rng, 1, min(262144, 1.3e8 / n)), n=n, x=any_type(), tiles=rng.random() < 0.4,
+                    order=rng.choice(["rows", "columns", "both"]))
+    if kind == "product":
+        if rng.random() < 0.3:  # a weight gradient: few rows and columns, long sums
+            m, n = _log(rng, 16, 2048), _log(rng, 16, 2048)
+            k, tiles = _log(rng, 4096, min(262144, 5.0e11 / (m * n))), False
+        else:
+            n, k = _log(rng, 16, 8192), _log(rng, 16, 8192)
+            m, tiles = _log(rng, 1, min(32768, max(2.0, 5.0e11 / (n * k)))), rng.random() < 0.8
+        # rows of whole chunks most of the time, as layers have them
+        if rng.random() < 0.6:
+            k = max(16, k // 16 * 16)
+        return dict(kind=kind, m=m, n=n, k=k, tiles=tiles, y=any_type())
+    if kind in ("logp", "logp_back"):
+        v = _log(rng, 2, 262144)
+        t = _log(rng, 1, max(2.0, min(200000, 1.2e8 / v)))
+        case = dict(kind=kind, t=t, v=v, x=any_type(), mask=rng.choice([0.0, 0.0, 0.3]))
+        return dict(case, top=min(v, rng.choice([0, 1, 5, 20]))) if kind == "logp" else case
+    f = _log(rng, 8, 512)
+    return dict(kind=kind, rows=_log(rng, 10, 1.3e8 / f), f=f, layers=rng.choice([0, 2, 5]), g=any_type(),
+                out=rng.random() < 0.5)
+
+
+# ----------------------------------------------------------------- inputs
+
+def _gen(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(int(seed))
+    return g
+
+
+def _shapes(case):
+    f = case["f"]
+    return [(case["rows"], f)] + [s for _ in range(case["layers"]) for s in ((f, f), (f,), (f,))]
+
+
+def _rows(m, n, g):
+    """Rows of different size."""
+    x = torch.randn((m, n), generator=g, device=DEV)
+    return x.mul_(torch.exp(0.7 * torch.randn((m, 1), generator=g, device=DEV)))
+
+
+def _labels(t, v, g):
+    labels = (v * torch.rand(t, generator=g, device=DEV) ** 2).long().clamp_(max=v - 1)
+    off = torch.rand(t, generator=g, device=DEV) < 0.05  # rows without a label
+    off[0] = False
+    return torch.where(off, torch.full_like(labels, -1), labels)
+
+
+def prepare(case, seed):
+    g, kind = _gen(seed), case["kind"]
+    s = dict(case)
+    if kind in ("rms", "rms_back"):
+        m, n = case["m"], case["n"]
+        s["X"] = _rows(m, n, g).to(TYPES[case["x"]])
+        s["gamma"] = 1 + 0.2 * torch.randn(n, generator=g, device=DEV)
+        if kind == "rms":
+            s["R"] = _rows(m, n, g).to(TYPES[case["r"]]) if case["r"] else None
+            return s
+        x = s["X"].float()
+        s["rstd"] = 1 / torch.sqrt((x * x).sum(1) / n + EPS)
+        s["dY"] = torch.randn((m, n), generator=g, device=DEV).to(TYPES[case["y"]])
+        s["dS"] = torch.randn((m, n), generator=g, device=DEV).to(TYPES[case["ds"]]) if case["ds"] else None
+        return s
+    if kind == "hold":
+        s["X"] = _rows(case["m"], case["n"], g).to(TYPES[case["x"]])
+        return s
+    if kind == "product":
+        s["A"] = _hold(_rows(case["m"], case["k"], g), False)
+        s["B"] = _hold(_rows(case["n"], case["k"], g).mul_(case["k"] ** -0.5), case["tiles"])
+        return s
+    if kind in ("logp", "logp_back"):
+        t, v = case["t"], case["v"]
+        Z = torch.randn((t, v), generator=g, device=DEV).mul_(2.5)
+        if case["mask"]:  # classes ruled out for a row
+            Z.masked_fill_(torch.rand((t, v), generator=g, device=DEV) < case["mask"], -math.inf)
+        s["Z"] = Z.to(TYPES[case["x"]])
+        s["labels"] = _labels(t, v, g)
+        if kind == "logp_back":
+            s["lse"], s["entropy"], _ = _statistics(s["Z"].float())
+            s["dlogp"] = torch.randn(t, generator=g, device=DEV) / t
+            s["dentropy"] = 0.1 * torch.randn(t, generator=g, device=DEV) / t
+        return s
+    s["grads"] = []
+    for shape in _shapes(case):
+        size = 1e-3 * torch.exp(torch.randn(shape[:1] + (1,) * (len(shape) - 1), generator=g, device=DEV))
+        s["grads"].append((size * torch.randn(shape, generator=g, device=DEV)).to(TYPES[case["g"]]))
+    s["outs"] = [torch.empty_like(x) for x in s["grads"]] if case["out"] else None
+    return s
+
+
+# ------------------------------------------------------------ plain forms
+
+def _pad(x):
+    return torch.nn.functional.pad(x, (0, -x.shape[1] % BLOCK))
+
+
+def _hold(x, tiles):
+    """x (float32) in 8 bits: codes, and the scales of its blocks."""
+    m, n = x.shape
+    x = _pad(x)
+    if tiles:
+        x = torch.nn.functional.pad(x, (0, 0, 0, -m % BLOCK))
+    b = x.view(x.shape[0] // BLOCK, BLOCK, -1, BLOCK) if tiles else x.view(m, 1, -1, BLOCK)
+    big = torch.where(torch.isfinite(b), b.abs(), 0.0).amax((1, 3), keepdim=True)
+    used = big >= TINY
+    scale = torch.where(used, big / TOP8, 0.0)
+    code = (b * torch.where(used, TOP8 / big, 0.0)).clamp_(-TOP8, TOP8).to(TYPES["e4m3"])
+    return code.view(x.shape)[:m, :n].contiguous(), scale.view(scale.shape[0], -1)
+
+
+def _values(held):
+    """The values that a matrix held in 8 bits stands for (float32)."""
+    codes, scales = held
+    m, n = codes.shape
+    each = scales if scales.shape[0] == m else scales.repeat_interleave(BLOCK, 0)[:m]
+    x = _pad(codes.float())
+    return (x.view(m, -1, BLOCK) * each[:, :, None]).view(m, -1)[:, :n]
+
+
+def _plain_rms(s):
+    x, total = s["X"].float(), None
+    if s["R"] is not None:
+        total = (x + s["R"].float()).to(s["R"].dtype)
+        x = total.float()
+    rstd = 1 / torch.sqrt((x * x).sum(1) / s["n"] + EPS)
+    y = x * rstd[:, None] * s["gamma"]
+    return {"Y": _hold(y, False) if s["y"] == "e4m3" else y.to(TYPES[s["y"]]), "S": total, "rstd": rstd}
+
+
+def _plain_rms_back(s):
+    rstd = s["rstd"][:, None]
+    xh, dy = s["X"].float() * rstd, s["dY"].float()
+    dgamma = (dy * xh).sum(0)
+    dy = dy * s["gamma"]
+    dx = rstd * (dy - xh * ((dy * xh).sum(1, keepdim=True) / s["n"]))
+    if s["dS"] is not None:
+        dx = dx + s["dS"].float()
+    return {"dX": dx.to(TYPES[s["x"]]), "dgamma": dgamma}
+
+
+def _plain_hold(s):
+    x, out = s["X"].float(), {}
+    if s["order"] != "columns":
+        out["rows"] = _hold(x, s["tiles"])
+    if s["order"] != "rows":
+        out["columns"] = _hold(x.t(), s["tiles"])
+    return out
+
+
+def _plain_product(s):
+    return {"Y": (_values(s["A"]) @ _values(s["B"]).t()).to(TYPES[s["y"]])}
+
+
+def _statistics(z):
+    """log of the sum of exponentials and entropy of each row; probabilities."""
+    top = z.amax(1, keepdim=True)
+    top = torch.where(top == -math.inf, 0.0, top)
+    z = z - top
+    p = torch.exp(z)
+    total = p.sum(1, keepdim=True)
+    p = p / torch.where(total > 0, total, 1.0)
+    mean = torch.where(p > 0, p * z, 0.0).sum(1)
+    log = torch.log(total)
+    entropy = torch.where(total[:, 0] > 0, log[:, 0] - mean, 0.0)
+    return (log + top)[:, 0], entropy, p
+
+
+def _plain_logp(s):
+    Z, labels = s["Z"], s["labels"]
+    z = Z.float()
+    lse, entropy, _ = _statistics(z)
+    there = (labels >= 0) & (labels < s["v"])
+    at = z.gather(1, torch.where(there, labels, 0)[:, None])[:, 0]
+    logp = torch.where(there, torch.where(at == -math.inf, at, at - lse), 0.0)
+    out = {"logp": logp, "entropy": entropy, "lse": lse}
+    if s["top"]:
+        z, at = torch.sort(Z, dim=1, descending=True, stable=True)
+        z = z[:, :s["top"]].float()
+        out["top_logp"] = torch.where(z == -math.inf, z, z - lse[:, None])
+        out["top_index"] = at[:, :s["top"]].contiguous()
+    return out
+
+
+def _plain_logp_back(s):
+    z, labels = s["Z"].float(), s["labels"]
+    rows = torch.arange(s["t"], device=z.device)
+    there = (labels >= 0) & (labels < s["v"])
+    dlogp = torch.where(there, s["dlogp"], 0.0)
+    logp = z - s["lse"][:, None]
+    p = torch.exp(logp)
+    dz = p * (-dlogp[:, None] - s["dentropy"][:, None] * (torch.where(p > 0, logp, 0.0) + s["entropy"][:, None]))
+    dz[rows, torch.where(there, labels, 0)] += dlogp
+    return {"dZ": dz.to(s["Z"].dtype)}
+
+
+def _plain_clip(s):
+    grads = s["grads"]
+    norm = torch.sqrt(torch.stack([g.float().square().sum() for g in grads]).sum())
+    scale = torch.where(norm > MAX_NORM, MAX_NORM / norm, 1.0)
+    if not s["out"]:
+        return {"norm": norm, "scale": scale}
+    torch._foreach_copy_(s["outs"], torch._foreach_mul([g.float() for g in grads], scale))
+    return {"norm": norm, "grads": s["outs"]}
+
+
+# -------------------------------------------------------------------- run
+
+PLAIN = {"rms": _plain_rms, "rms_back": _plain_rms_back, "hold": _plain_hold, "product": _plain_product,
+         "logp": _plain_logp, "logp_back": _plain_logp_back, "clip": _plain_clip}
+
+
+def run(state):
+    s, kind = state, state["kind"]
+    if not own:
+        return PLAIN[kind](s)
+    import paper_2507_02006_amd as aires
+    if kind == "rms":
+        Y, S, rstd = aires.rms_norm(s["X"], s["gamma"], residual=s["R"], eps=EPS, out_dtype=TYPES[s["y"]])
+        return {"Y": Y, "S": S, "rstd": rstd}
+    if kind == "rms_back":
+        dX, dgamma = aires.rms_norm_backward(s["dY"], s["X"], s["rstd"], s["gamma"], dS=s["dS"])
+        return {"dX": dX, "dgamma": dgamma}
+    if kind == "hold":
+        held = aires.quantize_8bit(s["X"], tiles=s["tiles"], order=s["order"])
+        return dict(zip(("rows", "columns"), held)) if s["order"] == "both" else {s["order"]: held}
+    if kind == "product":
+        return {"Y": aires.matmul_8bit(s["A"], s["B"], out_dtype=TYPES[s["y"]])}
+    if kind == "logp":
+        r = aires.log_probs(s["Z"], s["labels"], top=s["top"])
+        out = {"logp": r.logp, "entropy": r.entropy, "lse": r.lse}
+        if s["top"]:
+            out["top_logp"], out["top_index"] = r.top_logp, r.top_index
+        return out
+    if kind == "logp_back":
+        return {"dZ": aires.log_probs_backward(s["Z"], s["labels"], s["lse"], s["entropy"], dlogp=s["dlogp"],
+                                               dentropy=s["dentropy"])}
+    if s["out"]:
+        return {"norm": aires.clip_grads(s["grads"], MAX_NORM, out=s["outs"]), "grads": s["outs"]}
+    norm, scale = aires.grad_norm(s["grads"], max_norm=MAX_NORM)
+    return {"norm": norm, "scale": scale}
+
+
+def work(case):
+    kind = case["kind"]
+    if kind == "rms":
+        m, n = case["m"], case["n"]
+        size = SIZE[case["x"]] + (2 * SIZE[case["r"]] if case["r"] else 0) + SIZE[case["y"]]
+        return {"bytes": m * n * size + 4 * m + 4 * n, "flops": 5.0 * m * n}
+    if kind == "rms_back":
+        m, n = case["m"], case["n"]
+        size = 2 * SIZE[case["x"]] + SIZE[case["y"]] + (SIZE[case["ds"]] if case["ds"] else 0)
+        return {"bytes": m * n * size + 4 * m + 8 * n, "flops": 11.0 * m * n}
+    if kind == "hold":
+        size = SIZE[case["x"]] + (2 if case["order"] == "both" else 1) * (1 if case["tiles"] else SIZE["e4m3"])
+        return {"bytes": case["m"] * case["n"] * size, "flops": 4.0 * case["m"] * case["n"]}
+    if kind == "product":
+        m, n, k = case["m"], case["n"], case["k"]
+        held = m * k * SIZE["e4m3"] + n * k * (1 if case["tiles"] else SIZE["e4m3"])
+        return {"bytes": held + m * n * SIZE[case["y"]], "flops": 2.0 * m * n * k}
+    if kind == "logp":
+        t, v = case["t"], case["v"]
+        return {"bytes": t * v * SIZE[case["x"]] + t * (8 + 12 + 12 * case["top"]), "flops": 6.0 * t * v}
+    if kind == "logp_back":
+        t, v = case["t"], case["v"]
+        return {"bytes": 2 * t * v * SIZE[case["x"]] + 24 * t, "flops": 7.0 * t * v}
+    n = sum(math.prod(s) for s in _shapes(case))
+    return {"bytes": n * SIZE[case["g"]] * (2 if case["out"] else 1), "flops": 3.0 * n}
+
+
+# ------------------------------------------------------ results in 64 bits
+
+def _exact_held(y, tiles):
+    """What the codes of y (64 bits) are rounded from, and the scales."""
+    m, n = y.shape
+    rows = BLOCK if tiles else 1
+    wide = torch.zeros((-(-m // rows) * rows, -(-n // BLOCK) * BLOCK), dtype=torch.float64, device=y.device)
+    wide[:m, :n] = y
+    blocks = wide.unflatten(1, (-1, BLOCK)).unflatten(0, (-1, rows))
+    scale = blocks.abs().amax(dim=(1, 3)) / TOP8
+    wide /= scale.clamp(min=1e-300).repeat_interleave(rows, 0).repeat_interleave(BLOCK, 1)
+    return wide[:m, :n], scale
+
+
+def _exact_product(s):
+    def values(held):
+        codes, scales = held
+        codes = codes.double()
+        for b in range(scales.shape[1]):
+            each = scales[:, b].double()
+            if scales.shape[0] != codes.shape[0]:
+                each = each[torch.arange(codes.shape[0], device=each.device) // BLOCK]
+            codes[:, b * BLOCK:(b + 1) * BLOCK] *= each[:, None]
+        return codes
+    return {"Y": values(s["A"]) @ values(s["B"]).t()}
+
+
+def _exact_logp(case, s):
+    z = s["Z"].double()
+    lse = torch.logsumexp(z, 1)
+    logp = torch.log_softmax(z, 1)
+    entropy = torch.special.entr(torch.softmax(z, 1)).sum(1)
+    empty = (z == -math.inf).all(1)
+    there = (s["labels"] >= 0) & (s["labels"] < case["v"])
+    chosen = logp[torch.arange(case["t"], device=DEV), s["labels"].clamp(0, case["v"] - 1)]
+    out = {"logp": torch.where(there, torch.where(empty, -math.inf, chosen), 0.0), "lse": lse,
+           "entropy": torch.where(empty, 0.0, entropy)}
+    if case["top"]:
+        best = torch.topk(logp, case["top"], 1)[0]
+        out["top_logp"] = torch.where(empty[:, None], -math.inf, best)
+        out["top_index"] = None
+    return out
+
+
+def exact(case, seed):
+    s, kind = prepare(case, seed), case["kind"]
+    if kind == "product":
+        return _exact_product(s)
+    if kind == "hold":
+        x = s["X"].double()
+        out = {} if case["order"] == "columns" else {"rows": _exact_held(x, case["tiles"])}
+        if case["order"] != "rows":
+            out["columns"] = _exact_held(x.t(), case["tiles"])
+        return out
+    if kind == "logp":
+        return _exact_logp(case, s)
+    if kind == "logp_back":
+        z, lse, H = s["Z"].double(), s["lse"].double()[:, None], s["entropy"].double()[:, None]
+        ok = ((s["labels"] >= 0) & (s["labels"] < case["v"])).double()
+        a, b = (s["dlogp"].double() * ok)[:, None], s["dentropy"].double()[:, None]
+        p = torch.exp(z - lse)
+        dz = -a * p + b * (torch.special.entr(p) - p * H)
+        return {"dZ": dz.scatter_add_(1, s["labels"].clamp(min=0)[:, None], a)}
+    if kind == "clip":
+        norm = math.sqrt(math.fsum(float(g.double().pow(2).sum()) for g in s["grads"]))
+        scale = min(1.0, MAX_NORM / norm) if norm else 1.0
+        norm = torch.tensor(norm, dtype=torch.float64)
+        if not case["out"]:
+            return {"norm": norm, "scale": torch.tensor(scale, dtype=torch.float64)}
+        return {"norm": norm, "grads": [g.double() * scale for g in s["grads"]]}
+    x, gamma = s["X"].double(), s["gamma"].double()
+    if kind == "rms":
+        total, stored = None, x
+        if s["R"] is not None:
+            total = x + s["R"].double()
+            stored = total.to(s["R"].dtype).double()  # the norm is that of the sum as it is kept
+        rstd = (stored.square().mean(1) + EPS) ** -0.5
+        y = stored * (rstd[:, None] * gamma)
+        return {"Y": _exact_held(y, False) if case["y"] == "e4m3" else y, "S": total, "rstd": rstd}
+    rstd, dy = s["rstd"].double()[:, None], s["dY"].double()
+    xh = x * rstd
+    dgamma = (dy * xh).sum(0)
+    g = dy * gamma
+    dx = rstd * (g - xh * (g * xh).mean(1, keepdim=True))
+    return {"dX": dx if s["dS"] is None else dx + s["dS"].double(), "dgamma": dgamma}
