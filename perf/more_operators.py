@@ -271,9 +271,9 @@ def _plain_logp(s):
 def _plain_logp_back(s):
     z, labels = s["Z"].float(), s["labels"]
     rows = torch.arange(s["t"], device=z.device)
-    there = (labels >= 0) & (labels < s["v"])
-    dlogp = torch.where(there, s["dlogp"], 0.0)
-    logp = z - s["lse"][:, None]
+    there, some = (labels >= 0) & (labels < s["v"]), s["lse"] != -math.inf
+    dlogp = torch.where(there & some, s["dlogp"], 0.0)
+    logp = z - torch.where(some, s["lse"], 0.0)[:, None]
     p = torch.exp(logp)
     dz = p * (-dlogp[:, None] - s["dentropy"][:, None] * (torch.where(p > 0, logp, 0.0) + s["entropy"][:, None]))
     dz[rows, torch.where(there, labels, 0)] += dlogp
@@ -412,7 +412,8 @@ def exact(case, seed):
         return _exact_logp(case, s)
     if kind == "logp_back":
         z, lse, H = s["Z"].double(), s["lse"].double()[:, None], s["entropy"].double()[:, None]
-        ok = ((s["labels"] >= 0) & (s["labels"] < case["v"])).double()
+        lse = lse.nan_to_num(neginf=math.inf)  # a row with no class left has no gradient
+        ok = ((s["labels"] >= 0) & (s["labels"] < case["v"]) & (lse[:, 0] < math.inf)).double()
         a, b = (s["dlogp"].double() * ok)[:, None], s["dentropy"].double()[:, None]
         p = torch.exp(z - lse)
         dz = -a * p + b * (torch.special.entr(p) - p * H)
