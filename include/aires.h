@@ -746,6 +746,204 @@ typedef struct aires_adamw_opts {
 aires_status aires_adamw(const aires_adamw_tensor *tensors, int64_t count, const aires_adamw_opts *opts,
                          void *stream);
 
+/*
+ * aires_adamw_scaled -- aires_adamw with a factor of the gradients in device
+ * memory: they are multiplied with opts->grad_scale times *grad_scale (one
+ * fp32 value, read when the kernels run; NULL: 1).  aires_grad_norm writes
+ * such a factor.  Errors: as aires_adamw.
+ */
+aires_status aires_adamw_scaled(const aires_adamw_tensor *tensors, int64_t count, const aires_adamw_opts *opts,
+                                const float *grad_scale, void *stream);
+
+/* One tensor whose gradient is measured or clipped: n values, contiguous.
+   out: n values of out_dtype that aires_clip_grads writes (grad itself, or
+   memory that overlaps no gradient). */
+typedef struct aires_grad_tensor {
+    int64_t n;
+    const void *grad;           /* of grad_dtype                           */
+    void *out;                  /* of out_dtype                            */
+    int32_t grad_dtype, out_dtype;
+} aires_grad_tensor;
+
+/* Bytes of workspace that aires_grad_norm and aires_clip_grads need for
+   `count` tensors.  Errors: AIRES_E_INVALID_ARG, AIRES_E_UNSUPPORTED (count
+   above 2^24). */
+aires_status aires_grad_norm_workspace(int64_t count, int64_t *bytes);
+
+/*
+ * aires_grad_norm -- the norm of all gradients together, and the factor that
+ * brings it to max_norm at most:
+ *   norm = sqrt(sum over tensors and values of g^2),
+ *   scale = max_norm / norm where norm > max_norm, else 1.
+ * Squares and sums are in 64 bits, in an order that depends on the sizes
+ * only; norm and scale (one fp32 value each; scale may be NULL) are rounded
+ * once, so no size of gradient overflows the sum.  An infinity among the
+ * gradients gives norm = infinity and scale = 0, a NaN makes both NaN.
+ * max_norm may be infinite (scale = 1 where the norm is not NaN).
+ * workspace: 16-byte aligned.
+ * Errors: AIRES_E_INVALID_ARG (NULL, bad type, max_norm negative or NaN),
+ * AIRES_E_DIM (negative n), AIRES_E_UNSUPPORTED (n above 2^35),
+ * AIRES_E_CAPACITY, AIRES_E_OOM (host memory), AIRES_E_HIP.
+ */
+aires_status aires_grad_norm(const aires_grad_tensor *tensors, int64_t count, double max_norm, float *norm,
+                             float *scale, void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * aires_clip_grads -- out = grad * scale for every tensor, with aires_grad_norm's
+ * scale, rounded once to out's type; *norm is the norm before.  Where scale is 1 a
+ * tensor whose out is its own gradient is not written.  With a scale of 0 or NaN
+ * every value is still multiplied: infinities and NaNs come out as NaN.
+ * Errors: as aires_grad_norm, and AIRES_E_INVALID_ARG (out is grad, of another type;
+ * an out overlaps another one, or a gradient other than exactly its own).
+ */
+aires_status aires_clip_grads(const aires_grad_tensor *tensors, int64_t count, double max_norm, float *norm,
+                              void *workspace, int64_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Layers on top of the aggregated features: a norm with a residual stream,
+ * matrices held in 8 bits and their product, and log probabilities of
+ * classes.  The rules of the training calls above hold.
+ */
+
+/* Values along a row that share one scale in a matrix held in 8 bits. */
+#define AIRES_BLOCK8 128
+
+/*
+ * A matrix held in 8 bits (borrowed): value (i, j) = code (i, j), an OCP e4m3
+ * number (largest 448), times scales[(i / tile) * ld_scales + j / 128].
+ * Code (i, j) is at codes[i*ld + j].  tile: 1 (each row has scales of its
+ * own) or 128.  ld >= ncols, ld_scales >= ceil(ncols / 128); codes need no
+ * alignment, products are faster where codes, ld and ncols are multiples of 16.
+ */
+typedef struct aires_dense8 {
+    int64_t nrows, ncols, ld;
+    uint8_t *codes;
+    float *scales;
+    int64_t ld_scales;
+    int32_t tile, _reserved;
+} aires_dense8;
+
+/*
+ * aires_quantize8 -- X held in 8 bits, as it lies (Q, m x n), transposed (Qt,
+ * n x m, its blocks being runs of X's columns), or both in one pass; NULL
+ * where not wanted.  Per block: scale = largest finite magnitude / 448 (0
+ * where that magnitude is below 2^-110, and then all codes are 0), codes =
+ * value * (448 / that magnitude) rounded to nearest even.  Values that are not
+ * finite are stored as NaN and leave their block's scale alone.  Blocks at the
+ * ends are smaller.  Q and Qt have the same tile; with tile = 128 Qt's scales
+ * are Q's transposed.
+ * Errors: AIRES_E_INVALID_ARG (NULL, bad type or tile, ld too small),
+ * AIRES_E_DIM (sizes differ), AIRES_E_UNSUPPORTED (m or n above 2^30),
+ * AIRES_E_HIP.
+ */
+aires_status aires_quantize8(const aires_dense *X, const aires_dense8 *Q, const aires_dense8 *Qt, void *stream);
+
+/* Bytes of workspace that aires_matmul8 needs for A (m x k) and B (n x k): partial
+   sums of a k split over workgroups, 64 MB at most.
+   Errors: AIRES_E_INVALID_ARG, AIRES_E_DIM, AIRES_E_UNSUPPORTED. */
+aires_status aires_matmul8_workspace(int64_t m, int64_t n, int64_t k, int64_t *bytes);
+
+/*
+ * aires_matmul8 -- Y = A B^T of matrices held in 8 bits (Y: m x n, any type):
+ *   y_ij = sum over blocks b of sA(i, b) sB(j, b) sum_{k in b} a_ik b_jk.
+ * The products of a block are added in fp32 on the matrix cores, the blocks'
+ * sums in fp32 in an order that depends on the sizes and the alignment only; Y is
+ * rounded once.  A has tile = 1, B 1 or 128: with B = W (out x in, tile 128) this is a
+ * layer's Y = X W^T, with B = W transposed its dX, with both operands transposed
+ * activations and gradients its dW.  A NaN in a row of A or B makes that row or
+ * column of Y NaN; so does a scale that is not finite, for the rows or columns that
+ * it belongs to; others are as without.  Without columns (k = 0)
+ * Y is zeros.
+ * Errors: AIRES_E_INVALID_ARG (NULL, bad type or tile, ld too small, workspace not
+ * 16-byte aligned), AIRES_E_DIM (sizes differ), AIRES_E_UNSUPPORTED (m or n above
+ * 2^26, k or a row's stride above 2^23, more than 2^22 tiles of 128 x 128 of Y),
+ * AIRES_E_CAPACITY, AIRES_E_HIP.
+ */
+aires_status aires_matmul8(const aires_dense8 *A, const aires_dense8 *B, const aires_dense *Y, void *workspace,
+                           int64_t workspace_bytes, void *stream);
+
+/*
+ * aires_rms_norm -- a residual stream's addition and the norm of its rows:
+ *   s_ij = x_ij + r_ij (rounded to S's type),  q = 1 / sqrt(sum_j s_j^2 / n + eps),
+ *   y_j = s_j * q * gamma_j,
+ * the norm being that of S as it is stored.  Without R (NULL) S is NULL and
+ * the norm is X's.  S may be R's or X's own memory (same type, address and
+ * stride).  Y or Y8 (tile = 1) receives y; Y8 as aires_quantize8 of y in
+ * fp32.  gamma: n values of w_dtype, or NULL for ones.  rstd: m fp32 values q
+ * (for the backward pass), or NULL.  Sums are fp32.  A NaN or an infinity makes its
+ * own row NaN (infinities among finite values: NaN, the others 0) and no other.
+ * Rows without columns have q = eps^-1/2.
+ * Errors: AIRES_E_INVALID_ARG (NULL, bad type, ld < ncols, eps negative or not
+ * finite, not exactly one of Y and Y8, one of R and S), AIRES_E_DIM,
+ * AIRES_E_UNSUPPORTED (m > 2^40, n > 2^30), AIRES_E_HIP.
+ */
+aires_status aires_rms_norm(const aires_dense *X, const aires_dense *R, const void *gamma, int32_t w_dtype, double eps,
+                            const aires_dense *S, const aires_dense *Y, const aires_dense8 *Y8, float *rstd,
+                            void *stream);
+
+/* Bytes of workspace that aires_rms_norm_backward needs for m rows of n
+   columns (0 where gamma's gradient is not asked for).
+   Errors: AIRES_E_INVALID_ARG, AIRES_E_DIM, AIRES_E_UNSUPPORTED. */
+aires_status aires_rms_norm_workspace(int64_t m, int64_t n, int64_t *bytes);
+
+/*
+ * aires_rms_norm_backward -- gradients of aires_rms_norm from dY, the rows S that
+ * were normalised (X without a residual) and the q that it returned.  With
+ * sh = s q and g = dy gamma:
+ *   dx = q (g - sh mean_j(g sh)) + ds,  dgamma_j = sum over rows of dy sh.
+ * dS (NULL for none) is the gradient that reaches S past the norm; dX is the
+ * gradient of X and of R alike, of any type, and may be dS's own memory.  dgamma
+ * has n values of w_dtype, summed in fp32 in an order that depends on the sizes
+ * only and rounded once.  Either may be NULL; so may gamma (ones).  With no rows
+ * dgamma is zeros.  workspace (16-byte aligned) is scratch.
+ * Errors: as aires_rms_norm, and AIRES_E_CAPACITY.
+ */
+aires_status aires_rms_norm_backward(const aires_dense *dY, const aires_dense *S, const float *rstd,
+                                     const void *gamma, int32_t w_dtype, const aires_dense *dS,
+                                     const aires_dense *dX, void *dgamma, void *workspace, int64_t workspace_bytes,
+                                     void *stream);
+
+/* Most alternatives a row that aires_log_probs lists. */
+#define AIRES_MAX_TOP 64
+
+/* Bytes of workspace that aires_log_probs needs for t rows of v scores and `top`
+   alternatives.  Errors: AIRES_E_INVALID_ARG, AIRES_E_DIM, AIRES_E_UNSUPPORTED. */
+aires_status aires_log_probs_workspace(int64_t t, int64_t v, int32_t top, int64_t *bytes);
+
+/*
+ * aires_log_probs -- of each row of scores z (t x v), with p = softmax(z):
+ *   lse = log sum_j exp(z_j),  logp = z_label - lse,  entropy = -sum_j p_j log p_j,
+ * and its `top` highest scores: top_logp = z_j - lse and top_index = j (int64), t x
+ * top each, highest first, equal scores by their index.  labels: t values, int32 or
+ * int64 (labels_i64), or NULL; logp of a label outside [0, v) is 0.  logp, entropy and
+ * lse are t fp32 values each, NULL where not wanted (logp goes with labels).
+ * A score of -infinity has probability 0.  A row with no other scores has lse =
+ * -infinity, entropy 0 and log probabilities of -infinity.  In a row with a NaN or
+ * +infinity every log probability, the entropy and lse are NaN; its top indices
+ * take a NaN for +infinity.
+ * Errors: AIRES_E_INVALID_ARG (NULL, bad type, ld < ncols, only one of top_logp and
+ * top_index, only one of labels and logp, top outside [0, 64]), AIRES_E_DIM (v = 0 with
+ * t > 0, top > v), AIRES_E_UNSUPPORTED (t > 2^40, v >= 2^30), AIRES_E_CAPACITY, AIRES_E_HIP.
+ */
+aires_status aires_log_probs(const aires_dense *Z, const void *labels, int32_t labels_i64, int32_t top, float *logp,
+                             float *entropy, float *lse, float *top_logp, int64_t *top_index, void *workspace,
+                             int64_t workspace_bytes, void *stream);
+
+/*
+ * aires_log_probs_backward -- gradient of the scores from those of logp and
+ * entropy (dlogp, dentropy: t fp32 values each, NULL for zeros), with lse and
+ * entropy as aires_log_probs returned them:
+ *   dz_j = dlogp ([j = label] - p_j) - dentropy p_j (log p_j + entropy).
+ * A label outside [0, v) takes no part (its dlogp is not used).  Rows of -infinity
+ * alone have no gradient (zeros); rows whose lse is NaN have NaN.  dZ has Z's size, any
+ * type; it may be Z's own memory (same type, address and stride).  entropy may be NULL
+ * without dentropy, labels without dlogp.
+ * Errors: as aires_log_probs.
+ */
+aires_status aires_log_probs_backward(const aires_dense *Z, const void *labels, int32_t labels_i64, const float *lse,
+                                      const float *entropy, const float *dlogp, const float *dentropy,
+                                      const aires_dense *dZ, void *stream);
+
 /* Release C's arrays through the allocator that made them; zeroes *C. */
 void aires_csr_out_free(aires_csr_out *C);
 void aires_plan_destroy(aires_plan *plan);

@@ -13,6 +13,11 @@ Training on the aggregated features (train.py):
   layer_norm / layer_norm_backward                (aires_layer_norm...)
   linear_xent(H, W, labels, ...)    -> Xent       (aires_linear_xent)
   adamw(params, grads, m, v, ...)                 (aires_adamw)
+  grad_norm / clip_grads                          (aires_grad_norm, aires_clip_grads)
+Layers on top of them (layers.py):
+  rms_norm / rms_norm_backward                    (aires_rms_norm...)
+  quantize_8bit / matmul_8bit                     (aires_quantize8, aires_matmul8)
+  log_probs / log_probs_backward    -> LogProbs   (aires_log_probs...)
 A and B are (nrows, ncols, row_ptr, col_idx, vals) tuples or objects with
 those attributes (``nrows, ncols, rp, col, val``); arrays are device torch
 tensors, pinned host torch tensors, or numpy arrays (planning only).
@@ -27,7 +32,8 @@ from . import _binding as B_
 __all__ = ["tile_plan", "tile_plan_file", "read_csr_file", "spgemm", "spmm", "stream_tiles", "plan_info",
            "plan_tile", "plan_stats", "plan_tile_stats", "spgemm_noalloc", "Plan", "Output", "AiresError",
            "to_device", "to_pinned", "layer_norm", "layer_norm_backward", "linear_xent", "Xent", "adamw",
-           "adamw_state"]
+           "adamw_state", "grad_norm", "clip_grads", "rms_norm", "rms_norm_backward", "quantize_8bit", "matmul_8bit",
+           "log_probs", "log_probs_backward", "LogProbs"]
 
 AiresError = B_.AiresError
 
@@ -377,4 +383,6 @@ def to_pinned(M):
             torch.from_numpy(val).pin_memory())
 
 
+from .layers import (LogProbs, clip_grads, grad_norm, log_probs, log_probs_backward, matmul_8bit,  # noqa: E402
+                     quantize_8bit, rms_norm, rms_norm_backward)
 from .train import Xent, adamw, adamw_state, layer_norm, layer_norm_backward, linear_xent  # noqa: E402

@@ -104,6 +104,7 @@ class ReadStats(ctypes.Structure):
 DTYPE_F32, DTYPE_BF16, DTYPE_F16 = 0, 1, 2
 REDUCE_MEAN, REDUCE_SUM = 0, 1
 ADAMW_BLOCK = 256  # AIRES_ADAMW_BLOCK
+BLOCK8, MAX_TOP = 128, 64  # AIRES_BLOCK8, AIRES_MAX_TOP
 
 
 class Dense(ctypes.Structure):
@@ -116,6 +117,15 @@ class AdamWTensor(ctypes.Structure):
                [(n, c_vp) for n in ("param", "grad", "exp_avg", "exp_avg_sq", "exp_avg_scale", "exp_avg_sq_scale",
                                     "copy")] + \
                [(n, c_i32) for n in ("param_dtype", "grad_dtype", "copy_dtype", "_reserved")]
+
+
+class Dense8(ctypes.Structure):
+    _fields_ = [("nrows", c_i64), ("ncols", c_i64), ("ld", c_i64), ("codes", c_vp), ("scales", c_vp),
+                ("ld_scales", c_i64), ("tile", c_i32), ("_reserved", c_i32)]
+
+
+class GradTensor(ctypes.Structure):
+    _fields_ = [("n", c_i64), ("grad", c_vp), ("out", c_vp), ("grad_dtype", c_i32), ("out_dtype", c_i32)]
 
 
 class AdamWOpts(ctypes.Structure):
@@ -169,6 +179,22 @@ def load() -> ctypes.CDLL:
         "aires_linear_xent": (ctypes.c_int, [P(Dense), P(Dense), c_vp, c_i32, c_i32, c_dbl, c_vp, c_vp, P(Dense),
                                              P(Dense), c_vp, c_i64, c_vp]),
         "aires_adamw": (ctypes.c_int, [c_vp, c_i64, P(AdamWOpts), c_vp]),
+        "aires_adamw_scaled": (ctypes.c_int, [c_vp, c_i64, P(AdamWOpts), c_vp, c_vp]),
+        "aires_grad_norm_workspace": (ctypes.c_int, [c_i64, P(c_i64)]),
+        "aires_grad_norm": (ctypes.c_int, [c_vp, c_i64, c_dbl, c_vp, c_vp, c_vp, c_i64, c_vp]),
+        "aires_clip_grads": (ctypes.c_int, [c_vp, c_i64, c_dbl, c_vp, c_vp, c_i64, c_vp]),
+        "aires_quantize8": (ctypes.c_int, [P(Dense), P(Dense8), P(Dense8), c_vp]),
+        "aires_matmul8_workspace": (ctypes.c_int, [c_i64, c_i64, c_i64, P(c_i64)]),
+        "aires_matmul8": (ctypes.c_int, [P(Dense8), P(Dense8), P(Dense), c_vp, c_i64, c_vp]),
+        "aires_rms_norm": (ctypes.c_int, [P(Dense), P(Dense), c_vp, c_i32, c_dbl, P(Dense), P(Dense), P(Dense8), c_vp,
+                                          c_vp]),
+        "aires_rms_norm_workspace": (ctypes.c_int, [c_i64, c_i64, P(c_i64)]),
+        "aires_rms_norm_backward": (ctypes.c_int, [P(Dense), P(Dense), c_vp, c_vp, c_i32, P(Dense), P(Dense), c_vp,
+                                                   c_vp, c_i64, c_vp]),
+        "aires_log_probs_workspace": (ctypes.c_int, [c_i64, c_i64, c_i32, P(c_i64)]),
+        "aires_log_probs": (ctypes.c_int, [P(Dense), c_vp, c_i32, c_i32, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_i64,
+                                           c_vp]),
+        "aires_log_probs_backward": (ctypes.c_int, [P(Dense), c_vp, c_i32, c_vp, c_vp, c_vp, c_vp, P(Dense), c_vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)

@@ -44,6 +44,7 @@ struct Table {
   uint32_t first[MAX_TENSORS + 1];    // first workgroup of each tensor
   int count;
   AdamWStep o;
+  const float* scale;                 // factor of the gradients, or NULL
 };
 static_assert(sizeof(Table) <= 4096, "kernel arguments hold 4 KiB");
 
@@ -56,6 +57,13 @@ __device__ __forceinline__ int find(const Table& tab, uint32_t b) {
     else hi = mid;
   }
   return lo;
+}
+
+// The step's constants, with the factor that device memory holds.
+__device__ __forceinline__ AdamWStep step_of(const Table& tab) {
+  AdamWStep o = tab.o;
+  if (tab.scale) o.grad_scale *= *tab.scale;
+  return o;
 }
 
 template <int T, int STRIDE>
@@ -98,6 +106,7 @@ __device__ __forceinline__ void update(const AdamWStep& o, float g, float& p, fl
 }
 
 __global__ __launch_bounds__(BLOCK) void k_adamw_32(Table tab) {
+  const AdamWStep o = step_of(tab);
   const int k = find(tab, blockIdx.x);
   const AdamWTensor& t = tab.t[k];
   const int64_t base = (int64_t)(blockIdx.x - tab.first[k]) * CHUNK;
@@ -113,7 +122,7 @@ __global__ __launch_bounds__(BLOCK) void k_adamw_32(Table tab) {
 #pragma unroll
     for (int q = 0; q < PER; ++q)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) update(tab.o, g[q][j], p[q][j], m[q][j], v[q][j]);
+      for (int j = 0; j < 4; ++j) update(o, g[q][j], p[q][j], m[q][j], v[q][j]);
     store_all_t<DT_F32, 4 * BLOCK>(m_, i, m);
     store_all_t<DT_F32, 4 * BLOCK>(v_, i, v);
     store_all<4 * BLOCK>(t.p, t.pt, i, p);
@@ -122,7 +131,7 @@ __global__ __launch_bounds__(BLOCK) void k_adamw_32(Table tab) {
   }
   for (int64_t i = base + threadIdx.x; i < t.n; i += BLOCK) {
     float p = load1(t.p, t.pt, i), m = m_[i], v = v_[i];
-    update(tab.o, load1(t.g, t.gt, i), p, m, v);
+    update(o, load1(t.g, t.gt, i), p, m, v);
     m_[i] = m;
     v_[i] = v;
     store1(t.p, t.pt, i, p);
@@ -201,6 +210,7 @@ __device__ __forceinline__ uint32_t noise(uint32_t x) {
 constexpr uint32_t kIndexStep = 0x9E3779B1u;
 
 __global__ __launch_bounds__(BLOCK) void k_adamw_8(Table tab) {
+  const AdamWStep o = step_of(tab);
   const int k = find(tab, blockIdx.x);
   const AdamWTensor& t = tab.t[k];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -250,7 +260,7 @@ __global__ __launch_bounds__(BLOCK) void k_adamw_8(Table tab) {
     decode<false>(cm[q], sm[q], m[q]);
     decode<true>(cv[q], sv[q], v[q]);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) update(tab.o, g[q][j], p[q][j], m[q][j], v[q][j]);
+    for (int j = 0; j < 4; ++j) update(o, g[q][j], p[q][j], m[q][j], v[q][j]);
     // lane 2 q keeps block q's largest first moment, lane 2 q + 1 its second
     const float bm = block_max(m[q]), bv = block_max(v[q]);
     big = lane == 2 * q ? bm : lane == 2 * q + 1 ? bv : big;
@@ -315,11 +325,13 @@ uint32_t adamw_seed(uint32_t seed, int64_t tensor) {
   return (seed + (uint32_t)tensor * 0x632BE5ABu) * 0x85157AF5u;
 }
 
-hipError_t adamw(const AdamWTensor* tensors, int64_t count, const AdamWStep& step, hipStream_t s) {
+hipError_t adamw(const AdamWTensor* tensors, int64_t count, const AdamWStep& step, const float* device_scale,
+                 hipStream_t s) {
   constexpr int64_t kMost = int64_t(1) << 23;  // workgroups of a launch (2^31 threads), and of a tensor at most
   for (int eight = 0; eight < 2; ++eight) {
     Table tab;
     tab.o = step;
+    tab.scale = device_scale;
     tab.count = 0;
     tab.first[0] = 0;
     auto launch = [&]() {

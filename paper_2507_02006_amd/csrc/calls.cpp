@@ -61,6 +61,8 @@ void written(const at::Tensor& x) {
   if (!x.is_inference()) x.unsafeGetTensorImpl()->bump_version();
 }
 
+py::object or_none(const at::Tensor& t) { return t.defined() ? py::cast(t) : py::none(); }
+
 py::tuple layer_norm(const at::Tensor& X, const Maybe& gamma, const Maybe& beta, double eps,
                      std::optional<at::ScalarType> out_dtype, bool stats, const Maybe& out, uintptr_t stream) {
   const aires_dense x = dense(X, "X");
@@ -128,7 +130,6 @@ py::tuple layer_norm_backward(const at::Tensor& dY, const at::Tensor& X, const a
                                   need_weights ? dg.data_ptr() : nullptr, need_weights ? db.data_ptr() : nullptr,
                                   need_weights ? work.data_ptr() : nullptr, need, (void*)stream),
         "aires_layer_norm_backward");
-  const auto or_none = [](const at::Tensor& t) -> py::object { return t.defined() ? py::cast(t) : py::none(); };
   return py::make_tuple(or_none(dX), or_none(dg), or_none(db));
 }
 
@@ -158,13 +159,286 @@ py::tuple linear_xent(const at::Tensor& H, const at::Tensor& W, const at::Tensor
                           grad_scale, loss.data_ptr<float>(), (float*)rows.data_ptr(), grads ? &dh : nullptr,
                           grads ? &dw : nullptr, work.data_ptr(), need, (void*)stream),
         "aires_linear_xent");
-  const auto or_none = [](const at::Tensor& t) -> py::object { return t.defined() ? py::cast(t) : py::none(); };
   return py::make_tuple(loss, rows, or_none(dH), or_none(dW));
+}
+
+constexpr at::ScalarType kCodes = at::kFloat8_e4m3fn;
+
+int64_t blocks(int64_t n) { return (n + AIRES_BLOCK8 - 1) / AIRES_BLOCK8; }
+
+// A matrix held in 8 bits: a pair of codes and scales.  tile = 0: from the scales' number.
+aires_dense8 held(const at::Tensor& codes, const at::Tensor& scales, int32_t tile, const std::string& name) {
+  if (codes.dim() != 2 || !codes.is_cuda() || codes.scalar_type() != kCodes)
+    bad_value(name + ": codes must be a device matrix of float8_e4m3fn");
+  const int64_t m = codes.size(0), n = codes.size(1), ld = m > 1 ? codes.stride(0) : n;
+  if ((n > 1 && m > 0 && codes.stride(1) != 1) || (m > 1 && n > 0 && ld < n))
+    bad_value(name + ": codes need unit column stride and rows that do not overlap");
+  if (scales.dim() != 2 || scales.scalar_type() != at::kFloat || scales.device() != codes.device())
+    bad_value(name + ": scales must be a float32 matrix on the codes' device");
+  const int64_t rows = scales.size(0), b = blocks(n), lds = rows > 1 ? scales.stride(0) : b;
+  if (tile == 0) tile = rows == m ? 1 : AIRES_BLOCK8;
+  if (rows != (tile == 1 ? m : blocks(m)) || scales.size(1) != b)
+    bad_value(name + ": " + std::to_string(rows) + " x " + std::to_string(scales.size(1)) + " scales for " +
+              std::to_string(m) + " x " + std::to_string(n) + " codes");
+  if ((b > 1 && rows > 0 && scales.stride(1) != 1) || (rows > 1 && b > 0 && lds < b))
+    bad_value(name + ": scales need unit column stride and rows that do not overlap");
+  return aires_dense8{m, n, ld, (uint8_t*)codes.data_ptr(), (float*)scales.data_ptr(), lds, tile, 0};
+}
+
+const at::Tensor& part(const py::tuple& pair, int i, const char* name) {
+  const PyObject* x = PyTuple_GET_SIZE(pair.ptr()) == 2 ? PyTuple_GET_ITEM(pair.ptr(), i) : nullptr;
+  if (!x || !THPVariable_Check(const_cast<PyObject*>(x))) bad_value(std::string(name) + " must be a pair of codes and scales");
+  return THPVariable_Unpack(const_cast<PyObject*>(x));
+}
+
+struct New8 {
+  at::Tensor codes, scales;
+  aires_dense8 q;
+  New8() : q{} {}
+  New8(int64_t m, int64_t n, bool tiles, const at::TensorOptions& o)
+      : codes(at::empty({m, n}, o.dtype(kCodes))),
+        scales(at::empty({tiles ? blocks(m) : m, blocks(n)}, o.dtype(at::kFloat))) {
+    q = aires_dense8{m, n, n, (uint8_t*)codes.data_ptr(), (float*)scales.data_ptr(), blocks(n), tiles ? AIRES_BLOCK8 : 1, 0};
+  }
+  py::tuple pair() const { return py::make_tuple(codes, scales); }
+};
+
+py::object quantize_8bit(const at::Tensor& X, bool tiles, bool rows, bool columns, uintptr_t stream) {
+  const aires_dense x = dense(X, "X");
+  New8 q, t;
+  if (rows) q = New8(x.nrows, x.ncols, tiles, X.options());
+  if (columns) t = New8(x.ncols, x.nrows, tiles, X.options());
+  check(aires_quantize8(&x, rows ? &q.q : nullptr, columns ? &t.q : nullptr, (void*)stream), "aires_quantize8");
+  if (!columns) return q.pair();
+  if (!rows) return t.pair();
+  return py::make_tuple(q.pair(), t.pair());
+}
+
+at::Tensor matmul_8bit(const py::tuple& A, const py::tuple& B, std::optional<at::ScalarType> out_dtype, const Maybe& out,
+                       uintptr_t stream) {
+  const at::Tensor &ac = part(A, 0, "A"), &as = part(A, 1, "A"), &bc = part(B, 0, "B"), &bs = part(B, 1, "B");
+  const aires_dense8 a = held(ac, as, 1, "A"), b = held(bc, bs, 0, "B");
+  if (a.ncols != b.ncols) bad_value("A and B differ in columns");
+  same_device(ac, bc);
+  if (out) same_device(ac, *out);
+  if (out && out_dtype && out->scalar_type() != *out_dtype) throw py::type_error("out has another type than out_dtype");
+  const at::Tensor Y = out ? *out : at::empty({a.nrows, b.nrows}, ac.options().dtype(out_dtype.value_or(at::kBFloat16)));
+  const aires_dense y = dense(Y, "out");
+  if (y.nrows != a.nrows || y.ncols != b.nrows) bad_value("out must have A's rows and a column for each of B's");
+  int64_t need = 0;
+  check(aires_matmul8_workspace(a.nrows, b.nrows, a.ncols, &need), "aires_matmul8_workspace");
+  at::Tensor work;
+  if (need > 0) work = at::empty({need}, ac.options().dtype(at::kByte));
+  check(aires_matmul8(&a, &b, &y, need > 0 ? work.data_ptr() : nullptr, need, (void*)stream), "aires_matmul8");
+  if (out) written(*out);
+  return Y;
+}
+
+py::tuple rms_norm(const at::Tensor& X, const Maybe& gamma, const Maybe& residual, double eps,
+                   std::optional<at::ScalarType> out_dtype, bool stats, const Maybe& out, const Maybe& sum_out,
+                   uintptr_t stream) {
+  const aires_dense x = dense(X, "X");
+  const int64_t m = x.nrows, n = x.ncols;
+  const void* g = gamma ? vector(*gamma, n, "gamma") : nullptr;
+  const int32_t wt = gamma ? dtype_of(gamma->scalar_type()) : (int32_t)AIRES_F32;
+  if (gamma) same_device(X, *gamma);
+  if (out && out_dtype && out->scalar_type() != *out_dtype) throw py::type_error("out has another type than out_dtype");
+  if (sum_out && !residual) bad_value("sum_out without residual");
+  at::Tensor S, Y, rstd;
+  aires_dense r{}, s{}, y{};
+  if (residual) {
+    same_device(X, *residual);
+    r = dense(*residual, "residual");
+    if (r.nrows != m || r.ncols != n) bad_value("X and residual differ in size");
+    if (sum_out) same_device(X, *sum_out);
+    S = sum_out ? *sum_out : at::empty({m, n}, residual->options());
+    s = dense(S, "sum_out");
+    if (s.nrows != m || s.ncols != n) bad_value("X and sum_out differ in size");
+  }
+  if (stats) rstd = at::empty({m}, X.options().dtype(at::kFloat));
+  const bool eight = !out && out_dtype && *out_dtype == kCodes;
+  New8 q;
+  if (eight) {
+    q = New8(m, n, false, X.options());
+  } else {
+    if (out) same_device(X, *out);
+    Y = out ? *out : at::empty({m, n}, X.options().dtype(out_dtype.value_or(X.scalar_type())));
+    y = dense(Y, "out");
+    if (y.nrows != m || y.ncols != n) bad_value("X and out differ in size");
+  }
+  // (an empty vector has no address: nothing is written then)
+  check(aires_rms_norm(&x, residual ? &r : nullptr, g, wt, eps, residual ? &s : nullptr, eight ? nullptr : &y,
+                       eight ? &q.q : nullptr, stats && m > 0 ? rstd.data_ptr<float>() : nullptr, (void*)stream),
+        "aires_rms_norm");
+  if (out) written(*out);
+  if (sum_out) written(*sum_out);
+  return py::make_tuple(eight ? py::object(q.pair()) : py::cast(Y), or_none(S), or_none(rstd));
+}
+
+py::tuple rms_norm_backward(const at::Tensor& dY, const at::Tensor& S, const at::Tensor& rstd, const Maybe& gamma,
+                            const Maybe& dS, bool need_dx, bool need_weights, std::optional<at::ScalarType> dx_dtype,
+                            uintptr_t stream) {
+  const aires_dense dy = dense(dY, "dY"), x = dense(S, "S");
+  const int64_t m = x.nrows, n = x.ncols;
+  if (dy.nrows != m || dy.ncols != n) bad_value("dY and S differ in size");
+  const void* g = gamma ? vector(*gamma, n, "gamma") : nullptr;
+  const void* q = vector(rstd, m, "rstd");
+  if (rstd.scalar_type() != at::kFloat) throw py::type_error("rstd must be float32");
+  same_device(S, dY);
+  same_device(S, rstd);
+  if (gamma) same_device(S, *gamma);
+  aires_dense ds{}, dx{};
+  if (dS) {
+    same_device(S, *dS);
+    ds = dense(*dS, "dS");
+    if (ds.nrows != m || ds.ncols != n) bad_value("dS and S differ in size");
+  }
+  const at::ScalarType w = gamma ? gamma->scalar_type() : at::kFloat;
+  const int32_t wt = dtype_of(w);
+  at::Tensor dX, dg, work;
+  if (need_dx) {
+    dX = at::empty({m, n}, S.options().dtype(dx_dtype.value_or(S.scalar_type())));
+    dx = dense(dX, "dX");
+  }
+  int64_t need = 0;
+  if (need_weights) {
+    check(aires_rms_norm_workspace(m, n, &need), "aires_rms_norm_workspace");
+    dg = at::empty({n}, S.options().dtype(w));
+    work = at::empty({need}, S.options().dtype(at::kByte));
+  }
+  check(aires_rms_norm_backward(&dy, &x, (const float*)q, g, wt, dS ? &ds : nullptr, need_dx ? &dx : nullptr,
+                                need_weights ? dg.data_ptr() : nullptr, need_weights ? work.data_ptr() : nullptr, need,
+                                (void*)stream),
+        "aires_rms_norm_backward");
+  return py::make_tuple(or_none(dX), or_none(dg));
+}
+
+const void* labels_of(const at::Tensor& labels, int64_t t) {
+  if (labels.scalar_type() != at::kInt && labels.scalar_type() != at::kLong)
+    throw py::type_error("labels must be int32 or int64");
+  return vector(labels, t, "labels");
+}
+
+py::tuple log_probs(const at::Tensor& Z, const Maybe& labels, int64_t top, uintptr_t stream) {
+  const aires_dense z = dense(Z, "Z");
+  const int64_t t = z.nrows;
+  if (top < 0 || top > AIRES_MAX_TOP) bad_value("top must be between 0 and " + std::to_string(AIRES_MAX_TOP));
+  const void* y = labels ? labels_of(*labels, t) : nullptr;
+  if (labels) same_device(Z, *labels);
+  int64_t need = 0;
+  check(aires_log_probs_workspace(t, z.ncols, (int32_t)top, &need), "aires_log_probs_workspace");
+  const at::TensorOptions f = Z.options().dtype(at::kFloat);
+  at::Tensor work, logp, entropy = at::empty({t}, f), lse = at::empty({t}, f), top_logp, top_index;
+  if (need > 0) work = at::empty({need}, Z.options().dtype(at::kByte));
+  if (labels) logp = at::empty({t}, f);
+  if (top > 0) {
+    top_logp = at::empty({t, top}, f);
+    top_index = at::empty({t, top}, Z.options().dtype(at::kLong));
+  }
+  check(aires_log_probs(&z, y, labels && labels->scalar_type() == at::kLong, (int32_t)top,
+                        labels ? (float*)logp.data_ptr() : nullptr, (float*)entropy.data_ptr(), (float*)lse.data_ptr(),
+                        top > 0 ? (float*)top_logp.data_ptr() : nullptr,
+                        top > 0 ? (int64_t*)top_index.data_ptr() : nullptr, need > 0 ? work.data_ptr() : nullptr, need,
+                        (void*)stream),
+        "aires_log_probs");
+  return py::make_tuple(or_none(logp), entropy, lse, or_none(top_logp), or_none(top_index));
+}
+
+at::Tensor log_probs_backward(const at::Tensor& Z, const Maybe& labels, const at::Tensor& lse, const Maybe& entropy,
+                              const Maybe& dlogp, const Maybe& dentropy, std::optional<at::ScalarType> dz_dtype,
+                              const Maybe& out, uintptr_t stream) {
+  const aires_dense z = dense(Z, "Z");
+  const int64_t t = z.nrows;
+  if (dlogp && !labels) bad_value("dlogp without labels");
+  if (dentropy && !entropy) bad_value("dentropy without entropy");
+  const auto numbers = [&](const at::Tensor& x, const char* name) {
+    const void* p = vector(x, t, name);
+    if (x.scalar_type() != at::kFloat) throw py::type_error(std::string(name) + " must be float32");
+    same_device(Z, x);
+    return (const float*)p;
+  };
+  const void* y = labels ? labels_of(*labels, t) : nullptr;
+  if (labels) same_device(Z, *labels);
+  const float *l = numbers(lse, "lse"), *h = entropy ? numbers(*entropy, "entropy") : nullptr;
+  const float *da = dlogp ? numbers(*dlogp, "dlogp") : nullptr, *db = dentropy ? numbers(*dentropy, "dentropy") : nullptr;
+  if (out) same_device(Z, *out);
+  if (out && dz_dtype && out->scalar_type() != *dz_dtype) throw py::type_error("out has another type than dz_dtype");
+  const at::Tensor dZ = out ? *out : at::empty({t, z.ncols}, Z.options().dtype(dz_dtype.value_or(Z.scalar_type())));
+  const aires_dense dz = dense(dZ, "out");
+  if (dz.nrows != t || dz.ncols != z.ncols) bad_value("Z and out differ in size");
+  check(aires_log_probs_backward(&z, y, labels && labels->scalar_type() == at::kLong, l, h, da, db, &dz, (void*)stream),
+        "aires_log_probs_backward");
+  if (out) written(*out);
+  return dZ;
 }
 
 const at::Tensor& tensor(py::handle x) {
   if (!THPVariable_Check(x.ptr())) throw py::type_error("expected tensors");
   return THPVariable_Unpack(x.ptr());
+}
+
+// Gradients and where they go (outs: None for a norm alone).
+std::vector<aires_grad_tensor> grad_table(const py::sequence& grads, const py::object& outs, at::Tensor& first) {
+  const size_t n = grads.size();
+  if (n == 0) bad_value("no gradients");
+  const bool with = !outs.is_none();
+  const py::sequence o = with ? py::reinterpret_borrow<py::sequence>(outs) : py::sequence();
+  if (with && o.size() != n) bad_value("grads and out differ in number");
+  std::vector<aires_grad_tensor> table(n);
+  for (size_t k = 0; k < n; ++k) {
+    const py::object go = grads[k];
+    const at::Tensor& g = tensor(go);
+    if (k == 0) {
+      first = g;
+      if (!g.is_cuda()) bad_value("gradients must be on a device");
+    }
+    if (!g.is_contiguous()) bad_value("gradient " + std::to_string(k) + " must be contiguous");
+    same_device(first, g);
+    aires_grad_tensor& t = table[k];
+    t = aires_grad_tensor{g.numel(), g.data_ptr(), nullptr, dtype_of(g.scalar_type()), 0};
+    if (with) {
+      const py::object x = o[k];
+      const at::Tensor& out = tensor(x);
+      if (out.sizes() != g.sizes() || !out.is_contiguous())
+        bad_value("out " + std::to_string(k) + " must be contiguous and of its gradient's shape");
+      same_device(first, out);
+      t.out = out.data_ptr();
+      t.out_dtype = dtype_of(out.scalar_type());
+    }
+  }
+  return table;
+}
+
+at::Tensor norm_workspace(int64_t count, const at::Tensor& first) {
+  int64_t need = 0;
+  check(aires_grad_norm_workspace(count, &need), "aires_grad_norm_workspace");
+  return at::empty({need}, first.options().dtype(at::kByte));
+}
+
+py::tuple grad_norm(const py::sequence& grads, double max_norm, uintptr_t stream) {
+  at::Tensor first;
+  const auto table = grad_table(grads, py::none(), first);
+  const at::Tensor work = norm_workspace((int64_t)table.size(), first);
+  const at::Tensor norm = at::empty({}, first.options().dtype(at::kFloat)), scale = at::empty_like(norm);
+  check(aires_grad_norm(table.data(), (int64_t)table.size(), max_norm, norm.data_ptr<float>(), scale.data_ptr<float>(),
+                        work.data_ptr(), work.numel(), (void*)stream),
+        "aires_grad_norm");
+  return py::make_tuple(norm, scale);
+}
+
+at::Tensor clip_grads(const py::sequence& grads, const py::sequence& outs, double max_norm, uintptr_t stream) {
+  at::Tensor first;
+  const auto table = grad_table(grads, outs, first);
+  const at::Tensor work = norm_workspace((int64_t)table.size(), first);
+  const at::Tensor norm = at::empty({}, first.options().dtype(at::kFloat));
+  check(aires_clip_grads(table.data(), (int64_t)table.size(), max_norm, norm.data_ptr<float>(), work.data_ptr(),
+                         work.numel(), (void*)stream),
+        "aires_clip_grads");
+  for (size_t k = 0; k < table.size(); ++k) {
+    const py::object x = outs[k];
+    written(tensor(x));
+  }
+  return norm;
 }
 
 // One moment of parameter p: its address and that of its scales.
@@ -192,7 +466,7 @@ void moment(py::handle x, const at::Tensor& p, at::ScalarType codes_type, void*&
 
 void adamw(const py::sequence& params, const py::sequence& grads, const py::sequence& m, const py::sequence& v,
            const py::object& copies, int64_t step, double lr, double beta1, double beta2, double eps,
-           double weight_decay, double grad_scale, uint32_t seed, uintptr_t stream) {
+           double weight_decay, const py::object& grad_scale, uint32_t seed, uintptr_t stream) {
   const size_t n = params.size();
   const bool with = !copies.is_none();
   const py::sequence c = with ? py::reinterpret_borrow<py::sequence>(copies) : py::sequence();
@@ -229,8 +503,17 @@ void adamw(const py::sequence& params, const py::sequence& grads, const py::sequ
       }
     }
   }
-  const aires_adamw_opts o{sizeof(aires_adamw_opts), seed, step, lr, beta1, beta2, eps, weight_decay, grad_scale};
-  check(aires_adamw(table.data(), (int64_t)n, &o, (void*)stream), "aires_adamw");
+  const bool on_device = THPVariable_Check(grad_scale.ptr());
+  const float* factor = nullptr;
+  if (on_device) {
+    const at::Tensor& x = THPVariable_Unpack(grad_scale.ptr());
+    if (x.scalar_type() != at::kFloat || x.numel() != 1 || x.device() != device)
+      bad_value("grad_scale must be a number, or one float32 value on the parameters' device");
+    factor = (const float*)x.data_ptr();
+  }
+  const aires_adamw_opts o{sizeof(aires_adamw_opts), seed, step, lr, beta1, beta2, eps, weight_decay,
+                           on_device ? 1.0 : grad_scale.cast<double>()};
+  check(aires_adamw_scaled(table.data(), (int64_t)n, &o, factor, (void*)stream), "aires_adamw");
   for (size_t k = 0; k < n; ++k) {
     const py::object po = params[k], mo = m[k], vo = v[k];
     written(tensor(po));
@@ -254,6 +537,14 @@ PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
   m.def("layer_norm_backward", &layer_norm_backward);
   m.def("linear_xent", &linear_xent);
   m.def("adamw", &adamw);
+  m.def("grad_norm", &grad_norm);
+  m.def("clip_grads", &clip_grads);
+  m.def("quantize_8bit", &quantize_8bit);
+  m.def("matmul_8bit", &matmul_8bit);
+  m.def("rms_norm", &rms_norm);
+  m.def("rms_norm_backward", &rms_norm_backward);
+  m.def("log_probs", &log_probs);
+  m.def("log_probs_backward", &log_probs_backward);
   // the error class goes before the interpreter does
   m.add_object("_cleanup", py::capsule(+[] { g_error.release(); }));
 }

@@ -7,7 +7,7 @@
 #include <exception>
 #include <vector>
 
-#include "status.h"
+#include "arguments.h"
 #include "train.h"
 
 using namespace aires;
@@ -15,33 +15,6 @@ using namespace aires;
 namespace {
 
 constexpr int64_t kMaxSize = int64_t(1) << 31;
-
-bool type_ok(int32_t t) { return t == AIRES_F32 || t == AIRES_BF16 || t == AIRES_F16; }
-
-aires_status check_dense(const aires_dense* m, const char* name) {
-  if (!m) return fail(AIRES_E_INVALID_ARG, "%s is NULL", name);
-  if (!type_ok(m->dtype)) return fail(AIRES_E_INVALID_ARG, "%s: type %d invalid", name, (int)m->dtype);
-  if (m->nrows < 0 || m->ncols < 0)
-    return fail(AIRES_E_DIM, "%s is %lld x %lld", name, (long long)m->nrows, (long long)m->ncols);
-  if (m->nrows > 0 && m->ncols > 0) {
-    if (!m->data) return fail(AIRES_E_INVALID_ARG, "%s has no data", name);
-    if (m->ld < m->ncols)
-      return fail(AIRES_E_INVALID_ARG, "%s: ld %lld below %lld columns", name, (long long)m->ld, (long long)m->ncols);
-  }
-  return AIRES_OK;
-}
-
-aires_status check_same(const aires_dense* a, const char* an, const aires_dense* b, const char* bn) {
-  if (a->nrows != b->nrows || a->ncols != b->ncols)
-    return fail(AIRES_E_DIM, "%s is %lld x %lld, %s %lld x %lld", an, (long long)a->nrows, (long long)a->ncols, bn,
-                (long long)b->nrows, (long long)b->ncols);
-  return AIRES_OK;
-}
-
-kern::Mat mat(const aires_dense* m) {
-  if (!m) return kern::Mat{nullptr, 0, 0, 0, 0};
-  return kern::Mat{m->data, m->nrows, m->ncols, m->ld, m->dtype};
-}
 
 aires_status check_norm_size(int64_t m, int64_t n) {
   if (m < 0 || n < 0) return fail(AIRES_E_DIM, "%lld rows of %lld columns", (long long)m, (long long)n);
@@ -158,6 +131,11 @@ aires_status aires_linear_xent(const aires_dense* H, const aires_dense* W, const
 
 aires_status aires_adamw(const aires_adamw_tensor* tensors, int64_t count, const aires_adamw_opts* opts,
                          void* stream) {
+  return aires_adamw_scaled(tensors, count, opts, nullptr, stream);
+}
+
+aires_status aires_adamw_scaled(const aires_adamw_tensor* tensors, int64_t count, const aires_adamw_opts* opts,
+                                const float* grad_scale, void* stream) {
   if (!opts || opts->struct_size != sizeof(aires_adamw_opts)) return fail(AIRES_E_INVALID_ARG, "bad options");
   if (count < 0 || (count > 0 && !tensors)) return fail(AIRES_E_INVALID_ARG, "%lld tensors", (long long)count);
   const aires_adamw_opts& o = *opts;
@@ -199,7 +177,7 @@ aires_status aires_adamw(const aires_adamw_tensor* tensors, int64_t count, const
   s.rate = (float)(o.lr / (1.0 - std::pow(o.beta1, (double)o.step)));
   s.inv_root = (float)(1.0 / std::sqrt(1.0 - std::pow(o.beta2, (double)o.step)));
   s.grad_scale = (float)o.grad_scale;
-  HIP_TRY(kern::adamw(list.data(), (int64_t)list.size(), s, (hipStream_t)stream));
+  HIP_TRY(kern::adamw(list.data(), (int64_t)list.size(), s, grad_scale, (hipStream_t)stream));
   return AIRES_OK;
 }
 

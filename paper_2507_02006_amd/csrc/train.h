@@ -46,7 +46,9 @@ struct AdamWStep {
 };
 // What the rounding of a tensor's 8-bit moments is drawn from.
 uint32_t adamw_seed(uint32_t seed, int64_t tensor);
-hipError_t adamw(const AdamWTensor* tensors, int64_t count, const AdamWStep& step, hipStream_t s);
+// device_scale: a factor of the gradients in device memory, or NULL.
+hipError_t adamw(const AdamWTensor* tensors, int64_t count, const AdamWStep& step, const float* device_scale,
+                 hipStream_t s);
 
 }  // namespace kern
 }  // namespace aires

@@ -163,13 +163,14 @@ def adamw_state(params, bits: int = 32):
 
 
 def adamw(params, grads, exp_avg, exp_avg_sq, *, step: int, lr: float, betas=(0.9, 0.999), eps: float = 1e-8,
-          weight_decay: float = 0.01, grad_scale: float = 1.0, seed: int = 0, copies=None, stream=None) -> None:
+          weight_decay: float = 0.01, grad_scale=1.0, seed: int = 0, copies=None, stream=None) -> None:
     """One AdamW step over lists of tensors, in place (aires_adamw).  params:
     contiguous float32, bfloat16 or float16; grads: of any of these types;
     exp_avg, exp_avg_sq: as from ``adamw_state``, in 32 or 8 bits (``seed``
     then drives their rounding: pass another one each step); copies:
     tensors that receive the updated parameters in their own type (or None,
-    also for single entries).  ``step`` counts from 1.  A graph that captured
+    also for single entries).  ``grad_scale``: a number, or a float32 scalar on
+    the device (as ``grad_norm`` returns).  ``step`` counts from 1.  A graph that captured
     the call repeats its step, options and seed."""
     c = _calls or _load()
     if len(params) == 0 and len(grads) == len(exp_avg) == len(exp_avg_sq) == 0:

@@ -1,0 +1,748 @@
+"""Norm with a residual stream, matrices held in 8 bits and their product, log
+probabilities and gradient clipping against their formulas in 64 bits (GPU).
+
+Tolerances are bounds, derived before the kernels ran.  U = 2^-24 is the unit
+roundoff of fp32: a sum whose longest chain has c additions is off by c U times
+the sum of magnitudes.  A result rounded to a type is off by half a step of its
+own more (bf16 2^-8, fp16 2^-11, e4m3 2^-4, and half the smallest step).
+"""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+import paper_2507_02006_amd as aires  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+F32, BF16, F16, F8 = torch.float32, torch.bfloat16, torch.float16, torch.float8_e4m3fn
+ROUND = {F32: U, BF16: 2.0 ** -8, F16: 2.0 ** -11}
+LEAST = {F32: 2.0 ** -149, BF16: 2.0 ** -133, F16: 2.0 ** -25}
+INF = math.inf
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def rand(shape, seed, kind=F32):
+    return torch.randn(shape, generator=gen(seed)).to(kind)
+
+
+def near(got, want, tol, what):
+    got, want, tol = got.double().cpu(), want.double().cpu(), torch.as_tensor(tol, dtype=torch.float64).cpu()
+    assert got.shape == want.shape, (what, got.shape, want.shape)
+    same = (got == want) | (torch.isnan(got) & torch.isnan(want))
+    bad = ~(((got - want).abs() <= tol) | same)
+    assert not bad.any(), "%s: %d of %d off, worst %g" % (what, int(bad.sum()), bad.numel(),
+                                                          float((got - want).abs()[bad].max()))
+
+
+def rounded(x, kind):
+    return ROUND[kind] * x.abs() + LEAST[kind]
+
+
+def equal(a, b):
+    """The same values, a NaN being one whatever its sign."""
+    a, b = a.float(), b.float()
+    return a.shape == b.shape and bool(((a == b) | ((a != a) & (b != b))).all())
+
+
+# --------------------------------------------------------------- 8 bits held
+
+def hold(x, tiles=False):
+    """Codes and scales from the definition, in IEEE arithmetic of fp32."""
+    m, n = x.shape
+    rows = 128 if tiles else 1
+    wide = torch.zeros(-(-m // rows) * rows, -(-n // 128) * 128)
+    wide[:m, :n] = x.float()
+    b = wide.view(-1, rows, wide.shape[1] // 128, 128)
+    big = torch.where(b.isfinite(), b.abs(), torch.zeros(())).amax((1, 3))
+    used = big >= 2.0 ** -110
+    scale = torch.where(used, big / torch.full_like(big, 448), torch.zeros(()))
+    # (a quotient of two tensors: a number over a tensor is the number times its reciprocal)
+    inv = torch.where(used, torch.full_like(big, 448) / big, torch.zeros(()))
+    code = torch.where(b.isfinite(), b * inv[:, None, :, None], torch.tensor(math.nan)).to(F8)
+    return code.view(torch.uint8).view(wide.shape)[:m, :n].contiguous().view(F8), scale
+
+
+def values(held):
+    """What a matrix held in 8 bits stands for, in 64 bits."""
+    codes, scales = held[0].cpu().float().double(), held[1].cpu().double()
+    m, n = codes.shape
+    if scales.shape[0] != m:
+        scales = scales.repeat_interleave(128, 0)[:m]
+    return codes * scales.repeat_interleave(128, 1)[:, :n]
+
+
+SHAPES8 = [(1, 1), (1, 128), (3, 127), (5, 129), (128, 128), (129, 130), (200, 333), (257, 1000), (40, 4096), (1000, 17)]
+
+
+@pytest.mark.parametrize("m,n", SHAPES8)
+@pytest.mark.parametrize("kind", [F32, BF16, F16])
+@pytest.mark.parametrize("tiles", [False, True])
+def test_quantize(m, n, kind, tiles):
+    """The definition is in operations that round once each: bit for bit."""
+    x = (rand((m, n), m + n) * torch.exp(rand((m, 1), n))).to(kind)
+    rows, columns = aires.quantize_8bit(x.cuda(), tiles=tiles, order="both")
+    for got, want in ((rows, hold(x, tiles)), (columns, hold(x.t().contiguous(), tiles)),
+                      (aires.quantize_8bit(x.cuda(), tiles=tiles), hold(x, tiles)),
+                      (aires.quantize_8bit(x.cuda(), tiles=tiles, order="columns"), hold(x.t().contiguous(), tiles))):
+        assert got[0].dtype == F8 and got[1].dtype == F32
+        assert equal(got[0].cpu(), want[0]) and torch.equal(got[1].cpu(), want[1])
+
+
+@pytest.mark.parametrize("tiles", [False, True])
+def test_quantize_special_values(tiles):
+    x = rand((300, 300), 1)
+    x[3, 7], x[4, 200], x[150, 10] = math.nan, INF, -INF
+    x[20:40, 128:256] = 0
+    x[41, :128] = 2.0 ** -112
+    x[42, :128] = -(2.0 ** -110)
+    x[43, 128:256] = 3e38
+    x[256:, 256:] = math.nan                   # blocks that hold no finite value
+    x[130, :128] = 1e-30
+    rows, columns = aires.quantize_8bit(x.cuda(), tiles=tiles, order="both")
+    for got, want in ((rows, hold(x, tiles)), (columns, hold(x.t().contiguous(), tiles))):
+        assert equal(got[0].cpu(), want[0]) and torch.equal(got[1].cpu(), want[1])
+
+
+def test_quantize_forms():
+    x = rand((70, 200), 2, BF16)
+    wide = torch.zeros(70, 333, dtype=BF16, device="cuda")
+    wide[:, 5:205] = x.cuda()
+    for a, b in zip(aires.quantize_8bit(wide[:, 5:205], order="both"), aires.quantize_8bit(x.cuda(), order="both")):
+        assert equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    for m, n in ((0, 5), (5, 0), (0, 0)):
+        r, c = aires.quantize_8bit(torch.empty(m, n, device="cuda"), order="both")
+        assert r[0].shape == (m, n) and c[0].shape == (n, m) and r[1].shape == (m, -(-n // 128))
+    with pytest.raises(ValueError):
+        aires.quantize_8bit(x.cuda(), order="diagonal")
+    with pytest.raises(ValueError):
+        aires.quantize_8bit(x)
+    with pytest.raises(ValueError):
+        aires.quantize_8bit(x.cuda().t())
+
+
+# ------------------------------------------------------------------ product
+
+def operand(m, k, seed, tiles, kind="cuda"):
+    x = rand((m, k), seed) * torch.exp(0.5 * rand((m, 1), seed + 1))
+    c, s = hold(x, tiles)
+    return c.to(kind), s.to(kind)
+
+
+def product_tolerance(A, B, y, kind):
+    """128 products, exact in fp32, added in any order, with room for a matrix
+    core that rounds each addition by a whole step; a scale's product and the
+    blocks' sums, also over splits.
+
+    For 16-bit results of more than 64 rows the products are made in 8 bits: the
+    matrix cores add eight neighbours of k with each of them cut off below 2^-13 of
+    the largest one's power of two, so eight such units are off at most."""
+    a, b = values(A).abs(), values(B).abs()
+    k = a.shape[1]
+    tol = (256 + -(-k // 128) + 16) * U * (a @ b.t()) + rounded(y, kind)
+    if kind != F32 and a.shape[0] > 64:
+        for g in range(0, k, 8):
+            tol += 8 * 2.0 ** -13 * (a[:, None, g:g + 8] * b[None, :, g:g + 8]).amax(2)
+    return tol
+
+
+def check_product(A, B, kind, what):
+    y = values(A) @ values(B).t()
+    got = aires.matmul_8bit(A, B, out_dtype=kind)
+    assert got.dtype == kind
+    near(got, y, product_tolerance(A, B, y, kind), what)
+    return got
+
+
+SIZES = [(1, 1, 1), (1, 16, 128), (2, 17, 15), (5, 40, 300), (16, 130, 127), (17, 16, 129), (33, 257, 1000), (64, 33, 2048),
+         (65, 64, 128), (66, 1, 16), (70, 129, 333), (128, 128, 256), (129, 300, 1024), (200, 65, 16), (300, 257, 144),
+         (256, 512, 4097), (130, 200, 9000), (100, 70, 12304)]
+
+
+@pytest.mark.parametrize("m,n,k", SIZES)
+@pytest.mark.parametrize("tiles", [False, True])
+def test_product(m, n, k, tiles):
+    A, B = operand(m, k, m + k, False), operand(n, k, n + k + 1, tiles)
+    for kind in (F32, BF16, F16):
+        check_product(A, B, kind, (m, n, k, tiles, kind))
+
+
+@pytest.mark.parametrize("tiles", [False, True])
+@pytest.mark.parametrize("k", [272, 272 - 7])
+def test_product_of_large_tiles(tiles, k):
+    m, n = 3600, 3700
+    A, B = operand(m, k, 5, False), operand(n, k, 6, tiles)
+    a, b = values(A).cuda(), values(B).cuda()
+    y, tol = a @ b.t(), (256 + 3 + 16) * U * (a.abs() @ b.abs().t())
+    got = aires.matmul_8bit(A, B, out_dtype=F32)
+    assert bool(((got - y).abs() <= tol + U * y.abs()).all())
+    for g in range(0, k, 8):  # as in product_tolerance
+        tol += 8 * 2.0 ** -13 * torch.stack([torch.outer(a[:, i].abs(), b[:, i].abs()) for i in range(g, min(g + 8, k))]).amax(0)
+    for kind in (BF16, F16):
+        got = aires.matmul_8bit(A, B, out_dtype=kind)
+        assert bool(((got.double() - y).abs() <= tol + rounded(y, kind)).all())
+
+
+@pytest.mark.parametrize("m,n,k,tiles", [(5, 70, 260, True), (5, 70, 260, False), (100, 90, 272, True), (100, 90, 4112, False)])
+def test_product_forms(m, n, k, tiles):
+    """Strides, addresses of any alignment, an output of the caller's."""
+    A, B = operand(m, k, 1, False), operand(n, k, 2, tiles)
+    steps = -(-k // 128)
+
+    def moved(held, pad, at):
+        codes = torch.full((held[0].shape[0], k + pad), 0x7f, dtype=torch.uint8, device="cuda").view(F8)  # NaNs around it
+        codes.view(torch.uint8)[:, at:at + k] = held[0].view(torch.uint8)
+        scales = torch.full((held[1].shape[0], steps + 3), math.nan, device="cuda")
+        scales[:, 1:1 + steps] = held[1]
+        return codes[:, at:at + k], scales[:, 1:1 + steps]
+
+    want = values(A) @ values(B).t()
+    for pad, at in ((16, 0), (48, 16), (5, 3), (32, 1)):
+        for kind in (F32, BF16):
+            got = aires.matmul_8bit(moved(A, pad, at), moved(B, pad, at), out_dtype=kind)
+            near(got, want, product_tolerance(A, B, want, kind), (pad, at, kind))
+    for kind in (F32, BF16, F16):
+        hold_ = torch.full((m + 2, n + 7), 9.0, dtype=kind, device="cuda")
+        r = aires.matmul_8bit(A, B, out=hold_[1:m + 1, 3:n + 3])
+        assert r.data_ptr() == hold_[1:, 3:].data_ptr()
+        assert torch.equal(hold_[1:m + 1, 3:n + 3], aires.matmul_8bit(A, B, out_dtype=kind))
+        hold_[1:m + 1, 3:n + 3] = 9.0
+        assert bool((hold_ == 9).all())
+
+
+@pytest.mark.parametrize("m,n,k", [(5, 40, 300), (100, 90, 400), (100, 90, 4000), (70, 80, 333)])
+@pytest.mark.parametrize("tiles", [False, True])
+@pytest.mark.parametrize("kind", [F32, BF16])
+def test_product_keeps_rows_apart(m, n, k, tiles, kind):
+    """NaNs stay in their row of A and of B, also in the last, partial block."""
+    A, B = operand(m, k, 3, False), operand(n, k, 4, tiles)
+    clean = aires.matmul_8bit(A, B, out_dtype=kind)
+    a, b = A[0].clone(), B[0].clone()
+    a.view(torch.uint8)[2, k - 1] = 0x7f
+    b.view(torch.uint8)[11, 0] = 0xff
+    got = aires.matmul_8bit((a, A[1]), (b, B[1]), out_dtype=kind)
+    want = clean.clone()
+    want[2], want[:, 11] = math.nan, math.nan
+    assert equal(got, want)
+    s = A[1].clone()
+    s[3, -1] = math.nan
+    got = aires.matmul_8bit((A[0], s), B, out_dtype=kind)
+    want = clean.clone()
+    want[3] = math.nan
+    assert equal(got, want)
+    got = aires.matmul_8bit((A[0], torch.zeros_like(A[1])), B, out_dtype=kind)
+    assert not got.any()
+
+
+def test_product_without_values():
+    e = lambda m, k: (torch.empty(m, k, device="cuda").to(F8), torch.empty(m, -(-k // 128), device="cuda"))  # noqa: E731
+    y = aires.matmul_8bit(e(5, 0), e(7, 0))
+    assert y.shape == (5, 7) and y.dtype == BF16 and not y.any()
+    assert aires.matmul_8bit(e(0, 9), e(7, 9)).shape == (0, 7)
+    assert aires.matmul_8bit(e(4, 9), e(0, 9)).shape == (4, 0)
+
+
+def test_product_refusals():
+    A, B = operand(5, 200, 1, False), operand(7, 200, 2, True)
+    for a, b in ((operand(5, 200, 1, True), B), (A, operand(7, 201, 2, True)), (A[0], B), ((A[0].float(), A[1]), B),
+                 ((A[0], A[1][:, :1]), B), ((A[0], A[1].double()), B), ((A[0].cpu(), A[1]), B), ((A[0], A[1].cpu()), B),
+                 (A, (B[0], B[1].expand(3, -1))), ((A[0].t(), A[1]), B)):
+        with pytest.raises((ValueError, TypeError)):
+            aires.matmul_8bit(a, b)
+    with pytest.raises(ValueError):
+        aires.matmul_8bit(A, B, out=torch.empty(5, 8, device="cuda"))
+    with pytest.raises(TypeError):
+        aires.matmul_8bit(A, B, out=torch.empty(5, 7, device="cuda"), out_dtype=BF16)
+
+
+# ---------------------------------------------------------------- rms norm
+
+NORMS = [(1, 1), (3, 2), (70, 5), (64, 64), (129, 65), (33, 100), (70, 128), (31, 200), (17, 256), (65, 511), (9, 512), (12, 1000),
+         (40, 1024), (11, 2047), (7, 2049), (5, 6001), (3, 12000), (2, 16384), (3, 16390), (2, 40000), (4099, 48)]
+# chain of a row's sum: its lane's columns, the lanes, the wavefronts (wider rows: 1024 lanes)
+CHAIN = 400
+
+
+def rms_check(x, r, gamma, Y, S, q, yt):
+    s = x.double()
+    if r is not None:
+        near(S, x.double() + r.double(), rounded(x.double() + r.double(), r.dtype) + U * (x.double().abs() + r.double().abs()), "S")
+        s = S.double().cpu()
+    want = (s.square().mean(1) + 1e-6).rsqrt()
+    near(q, want, CHAIN * U * want, "rstd")
+    y = s * want[:, None] * (1.0 if gamma is None else gamma.double())
+    if yt != F8:
+        assert Y.dtype == yt
+        near(Y, y, (CHAIN + 8) * U * y.abs() + rounded(y, yt), "Y")
+        return
+    n = y.shape[1]
+    big = torch.nn.functional.pad(y, (0, -n % 128)).view(y.shape[0], -1, 128).abs().amax(2)
+    near(Y[1], big / 448, (CHAIN + 16) * U * big / 448, "scales")
+    each = big.repeat_interleave(128, 1)[:, :n]
+    # half a step of a code, normal or not, and what the value and its scale are off by
+    near(values(Y), y, 2.0 ** -4 * y.abs() + each / 448 * 2.0 ** -10 + 4 * (CHAIN + 16) * U * each, "values")
+
+
+@pytest.mark.parametrize("m,n", NORMS)
+@pytest.mark.parametrize("xt,rt,yt", [(F32, None, F32), (BF16, BF16, F8), (F16, F32, BF16), (F32, F16, F8), (BF16, None, F8),
+                                      (F16, F16, F16)])
+def test_rms_norm(m, n, xt, rt, yt):
+    x = (rand((m, n), m + n) * torch.exp(rand((m, 1), n))).to(xt)
+    r = None if rt is None else rand((m, n), n + 7, rt)
+    gamma = 1 + 0.3 * rand(n, 3)
+    Y, S, q = aires.rms_norm(x.cuda(), gamma.cuda(), residual=None if r is None else r.cuda(), out_dtype=yt)
+    assert (S is None) == (r is None) and (r is None or S.dtype == rt) and q.dtype == F32
+    rms_check(x, r, gamma, Y, S, q, yt)
+    # the norm of the sum as it is stored: the same as of that sum by itself, bit for bit
+    if r is not None and xt == rt:
+        Z, _, p = aires.rms_norm(S, gamma.cuda(), out_dtype=yt)
+        assert torch.equal(p, q) and (equal(Z[0], Y[0]) and torch.equal(Z[1], Y[1]) if yt == F8 else equal(Z, Y))
+
+
+def test_rms_norm_forms():
+    x, r, gamma = rand((50, 77), 1), rand((50, 77), 2), rand(77, 3)
+    X, R, G = x.cuda(), r.cuda(), gamma.cuda()
+    Y, S, q = aires.rms_norm(X, G, residual=R)
+    wide = torch.zeros(50, 99, device="cuda")
+    wide[:, 5:82] = X
+    hold_ = torch.full((50, 101), 7.0, device="cuda")
+    acc = R.clone()
+    v = acc._version
+    Y1, S1, none = aires.rms_norm(wide[:, 5:82], G, residual=acc, sum_out=acc, out=hold_[:, 3:80], stats=False)
+    assert none is None and S1.data_ptr() == acc.data_ptr() and acc._version > v
+    assert torch.equal(acc, S) and torch.equal(hold_[:, 3:80], Y)
+    assert bool((hold_[:, :3] == 7).all()) and bool((hold_[:, 80:] == 7).all())
+    own = X.clone()                              # the sum in X's own place
+    Y2, S2, _ = aires.rms_norm(own, G, residual=R, sum_out=own)
+    assert torch.equal(own, S) and torch.equal(Y2, Y)
+    Y3, _, _ = aires.rms_norm(X, G.to(BF16), residual=R)
+    Y4, _, _ = aires.rms_norm(X, G.to(BF16).float(), residual=R)
+    assert torch.equal(Y3, Y4)
+    assert torch.equal(aires.rms_norm(X)[0], aires.rms_norm(X, torch.ones(77, device="cuda"))[0])
+    big = rand((2, 40000), 5, BF16).cuda()       # wide rows, the sum in the residual's place
+    acc = big.clone()
+    Y5, S5, _ = aires.rms_norm(big, residual=acc, sum_out=acc)
+    Y6, S6, _ = aires.rms_norm(big, residual=big)
+    assert torch.equal(Y5, Y6) and torch.equal(acc, S6)
+
+
+def test_rms_norm_edges():
+    e = torch.empty(0, 9, device="cuda")
+    Y, S, q = aires.rms_norm(e, residual=e)
+    assert Y.shape == (0, 9) and q.numel() == 0
+    dX, dg = aires.rms_norm_backward(e, e, q, torch.ones(9, device="cuda"))
+    assert dX.shape == (0, 9) and not dg.any()
+    z = torch.empty(4, 0, device="cuda")
+    Y, _, q = aires.rms_norm(z, eps=0.25)
+    assert Y.shape == (4, 0) and bool((q == 2).all())
+    Y, _, q = aires.rms_norm(z, out_dtype=F8)
+    assert Y[0].shape == (4, 0) and Y[1].shape == (4, 0)
+    # zeros, a NaN and an infinity stay in their rows
+    x = rand((6, 200), 1)
+    x[1] = 0
+    x[2, 3] = math.nan
+    x[4, 199] = INF
+    for kind in (F32, F8):
+        Y, _, q = aires.rms_norm(x.cuda(), out_dtype=kind)
+        clean, _, p = aires.rms_norm(x[[0, 3, 5]].cuda(), out_dtype=kind)
+        v = values(Y) if kind == F8 else Y.cpu()
+        w = values(clean) if kind == F8 else clean.cpu()
+        assert equal(v[[0, 3, 5]], w) and not v[1].any() and bool(v[2].isnan().all())
+        assert bool(v[4, 199].isnan()) and not v[4, :199].any()
+        assert float(q[4]) == 0 and math.isnan(float(q[2])) and float(q[1]) == pytest.approx(1e3, rel=1e-6)
+
+
+def test_rms_norm_refusals():
+    x = rand((5, 8), 1).cuda()
+    for call in (lambda: aires.rms_norm(x.cpu()), lambda: aires.rms_norm(x.t()), lambda: aires.rms_norm(x, x[0, :7]),
+                 lambda: aires.rms_norm(x, residual=x[:4]), lambda: aires.rms_norm(x, sum_out=x),
+                 lambda: aires.rms_norm(x, residual=x, sum_out=x[:, :7]), lambda: aires.rms_norm(x, out=x[:, :7]),
+                 lambda: aires.rms_norm(x, out=x, out_dtype=BF16), lambda: aires.rms_norm(x.double()),
+                 lambda: aires.rms_norm(x, out_dtype=torch.float64), lambda: aires.rms_norm(x, eps=-1.0),
+                 lambda: aires.rms_norm_backward(x, x, x[0], None), lambda: aires.rms_norm_backward(x, x[:4], x[:4, 0].clone()),
+                 lambda: aires.rms_norm_backward(x, x, x[:, 0].to(BF16)),
+                 lambda: aires.rms_norm_backward(x, x, x[:, 0].clone(), dS=x[:3])):
+        with pytest.raises((ValueError, TypeError, aires.AiresError)):
+            call()
+
+
+@pytest.mark.parametrize("m,n", NORMS)
+@pytest.mark.parametrize("xt,yt,dt", [(F32, F32, None), (F32, BF16, F32), (F16, F16, F16), (BF16, F32, F16)])
+def test_rms_norm_backward(m, n, xt, yt, dt):
+    s = (rand((m, n), m * 3 + n) * torch.exp(rand((m, 1), n))).to(xt)
+    dy, ds, gamma = rand((m, n), n + 1, yt), None if dt is None else rand((m, n), n + 2, dt), 1 + 0.3 * rand(n, 3)
+    q = (s.double().square().mean(1) + 1e-6).rsqrt().float()
+    dX, dg = aires.rms_norm_backward(dy.cuda(), s.cuda(), q.cuda(), gamma.cuda(), dS=None if ds is None else ds.cuda())
+    assert dX.dtype == xt and dg.dtype == F32
+    D, Q, G = dy.double(), q.double()[:, None], gamma.double()
+    sh, g = s.double() * Q, D * G
+    mean, am = (g * sh).mean(1, keepdim=True), (g * sh).abs().mean(1, keepdim=True)
+    dx = Q * (g - sh * mean)
+    tol = Q * (8 * U * g.abs() + sh.abs() * (CHAIN + 8) * U * am)
+    if ds is not None:
+        dx = dx + ds.double()
+        tol = tol + U * ds.double().abs()
+    near(dX, dx, tol + rounded(dx, xt) + U * dx.abs(), "dX")
+    near(dg, (D * sh).sum(0), CHAIN * U * (D * sh).abs().sum(0) + 4 * U * (D * sh).abs().sum(0), "dgamma")
+
+
+def test_rms_norm_backward_forms():
+    s, dy, ds, gamma = (rand((50, 77), i).cuda() for i in range(4))
+    gamma = gamma[0].contiguous()
+    _, _, q = aires.rms_norm(s, gamma)
+    dX, dg = aires.rms_norm_backward(dy, s, q, gamma, dS=ds)
+    a, none = aires.rms_norm_backward(dy, s, q, gamma, dS=ds, need_weights=False)
+    assert none is None and torch.equal(a, dX)
+    none, b = aires.rms_norm_backward(dy, s, q, gamma, need_dx=False)
+    assert none is None and torch.equal(b, dg)
+    c = aires.rms_norm_backward(dy, s, q, gamma.to(BF16), dx_dtype=F16)
+    assert c[0].dtype == F16 and c[1].dtype == BF16
+    wide = torch.zeros(50, 99, device="cuda")
+    wide[:, 5:82] = s
+    d = aires.rms_norm_backward(dy, wide[:, 5:82], q, gamma, dS=ds)
+    assert torch.equal(d[0], dX) and torch.equal(d[1], dg)
+
+
+def test_rms_norm_backward_against_differences():
+    m, n, h = 5, 37, 1e-6
+    x, gamma, c = rand((m, n), 1).double(), (1 + 0.3 * rand(n, 2)).double(), rand((m, n), 3).double()
+
+    def value(x, gamma):
+        return (x * (x.square().mean(1, keepdim=True) + 1e-6).rsqrt() * gamma * c).sum()
+
+    def slope(f, at):
+        out = torch.empty_like(at)
+        for i in range(at.numel()):
+            d = torch.zeros_like(at).view(-1)
+            d[i] = h
+            d = d.view(at.shape)
+            out.view(-1)[i] = (f(at + d) - f(at - d)) / (2 * h)
+        return out
+
+    _, _, q = aires.rms_norm(x.float().cuda(), gamma.float().cuda())
+    dX, dg = aires.rms_norm_backward(c.float().cuda(), x.float().cuda(), q, gamma.float().cuda())
+    # differences: h^2 f''' and 2^-52 |f| / h, below 1e-7 here; sums of 37 terms in fp32
+    for got, want in ((dX, slope(lambda v: value(v, gamma), x)), (dg, slope(lambda v: value(x, v), gamma))):
+        near(got, want, 1e-5 * (1 + want.abs()), "slope")
+
+
+# -------------------------------------------------------- log probabilities
+
+def logp_ref(z, labels):
+    z = z.double()
+    lse = torch.logsumexp(z, 1)
+    empty = lse == -INF
+    lp = torch.where(empty[:, None], torch.full_like(z, -INF), z - lse[:, None])
+    p = torch.exp(lp)
+    H = torch.where(p > 0, -p * lp, torch.zeros_like(p)).sum(1)
+    v = z.shape[1]
+    there = (labels >= 0) & (labels < v)
+    chosen = lp.gather(1, torch.where(there, labels, torch.zeros_like(labels)).long()[:, None])[:, 0]
+    return lse, torch.where(there, chosen, torch.zeros_like(chosen)), H, lp, p
+
+
+def logp_tolerance(z, p):
+    """exp(z - m) is off by 3 U |z - m| + 8 U of itself (the difference, its
+    product with log2 e, the exponential), its sums by their chains and by the
+    factors that a part's sums are brought to the row's maximum with."""
+    z = z.double()
+    m = z.amax(1, keepdim=True)
+    d = torch.where(p > 0, (m - z).abs(), torch.zeros_like(z))
+    c = 512 + 8 * (z.shape[1] // 2048)
+    d1, d2 = (p * d).sum(1), (p * d * d).sum(1)
+    log_s = (3 * d1 + c) * U
+    return log_s + U * m[:, 0].abs().nan_to_num(0, 0, 0), log_s + (3 * d2 + c * (d1 + 1)) * U
+
+
+SCORES = [(1, 1), (7, 2), (100, 5), (300, 41), (65, 64), (33, 65), (50, 128), (20, 130), (40, 256), (9, 500), (30, 512), (21, 513),
+          (17, 1024), (5, 1500), (6, 2048), (5, 2049), (3, 4100), (600, 2100), (1, 30011), (2, 100003), (513, 2500)]
+
+
+@pytest.mark.parametrize("t,v", SCORES)
+@pytest.mark.parametrize("kind", [F32, BF16, F16])
+def test_log_probs(t, v, kind):
+    z = (3 * rand((t, v), t + v)).to(kind)
+    if v > 2:
+        z.masked_fill_(torch.rand((t, v), generator=gen(v)) < 0.2, -INF)
+    labels = torch.randint(-1, v + 1, (t,), generator=gen(t))
+    top = min(v, (1, 5, 20, 64)[(t + v) % 4])
+    r = aires.log_probs(z.cuda(), labels.cuda(), top=top)
+    lse, logp, H, lp, p = logp_ref(z, labels)
+    base, ent = logp_tolerance(z, p)
+    near(r.lse, lse, base + 2 * U * lse.abs(), "lse")
+    near(r.entropy, H, ent + 4 * U * (H + 1), "entropy")
+    near(r.logp, logp, base + 4 * U * logp.abs(), "logp")
+    order = torch.sort(z, dim=1, descending=True, stable=True)[1][:, :top]
+    assert r.top_index.dtype == torch.int64 and torch.equal(r.top_index.cpu(), order)
+    best = lp.gather(1, order)
+    near(r.top_logp, best, base[:, None] + 4 * U * best.abs().nan_to_num(0, 0, 0), "top")
+    # no alternatives, no labels, labels of 32 bits
+    a = aires.log_probs(z.cuda())
+    assert a.logp is None and a.top_logp is None and a.top_index is None
+    b = aires.log_probs(z.cuda(), labels.int().cuda(), top=1)
+    assert equal(b.logp, r.logp) or v > 2048  # (rows may be split otherwise)
+    near(b.logp, logp, base + 4 * U * logp.abs(), "logp")
+    near(a.lse, lse, base + 2 * U * lse.abs(), "lse")
+
+
+@pytest.mark.parametrize("t,v", [(5, 41), (5, 700), (3, 5000), (600, 3000), (2, 70000)])
+@pytest.mark.parametrize("kind", [F32, BF16, F16])
+def test_log_probs_of_masked_and_equal_scores(t, v, kind):
+    low = torch.finfo(kind).min
+    z = rand((t, v), 1, kind)
+    z[0] = -INF                               # no class left
+    z[1] = low                                # every class at the type's lowest value: all equal
+    z[1, v - 1] = -INF
+    if t > 2:
+        z[2] = 0
+        z[2, ::2] = -0.0                      # equal scores
+    if t > 3:
+        z[3] = -INF
+        z[3, v // 2] = 5                      # one class
+        z[4] = torch.arange(v).to(kind)       # rising, with equal neighbours where the type has no more bits
+    labels = torch.full((t,), v // 2)
+    top = min(v, 33)
+    r = aires.log_probs(z.cuda(), labels.cuda(), top=top)
+    order = torch.sort(z.float(), dim=1, descending=True, stable=True)[1][:, :top]
+    assert torch.equal(r.top_index.cpu(), order)
+    assert float(r.lse[0]) == -INF and float(r.entropy[0]) == 0 and float(r.logp[0]) == -INF
+    assert bool((r.top_logp[0] == -INF).all())
+    # a sum of up to 70000 ones is exact, its logarithm off by 2 U
+    want = math.log(v - 1)
+    assert abs(float(r.entropy[1]) - want) <= 4 * U * want and abs(float(r.logp[1]) + want) <= 4 * U * want
+    if t > 2:
+        assert abs(float(r.entropy[2]) - math.log(v)) <= 4 * U * math.log(v)
+    if t > 3:
+        assert float(r.logp[3]) == 0 and float(r.entropy[3]) == 0 and float(r.lse[3]) == 5
+        assert bool((r.top_logp[3, 1:] == -INF).all())
+        lse, logp, H, lp, p = logp_ref(z, labels)
+        base, ent = logp_tolerance(z[4:], p[4:])
+        near(r.entropy[4:], H[4:], ent + 4 * U * (H[4:] + 1), "entropy")
+
+
+@pytest.mark.parametrize("t,v", [(6, 50), (6, 900), (6, 5000), (600, 2500)])
+def test_log_probs_of_rows_that_are_not_finite(t, v):
+    z = rand((t, v), 3)
+    z[1, 7], z[2, v - 1], z[3, 0], z[3, 9] = math.nan, INF, INF, math.nan
+    labels = torch.zeros(t, dtype=torch.int64)
+    r = aires.log_probs(z.cuda(), labels.cuda(), top=3)
+    clean = z.clone()
+    clean[1:4] = 0
+    c = aires.log_probs(clean.cuda(), labels.cuda(), top=3)
+    keep = [0, 4, 5]
+    for name in ("logp", "entropy", "lse", "top_logp", "top_index"):
+        assert torch.equal(getattr(r, name)[keep], getattr(c, name)[keep]), name
+    for name in ("logp", "entropy", "lse", "top_logp"):
+        assert bool(getattr(r, name)[1:4].isnan().all()), name
+    assert r.top_index[1, 0] == 7 and r.top_index[2, 0] == v - 1 and r.top_index[3, :2].tolist() == [0, 9]
+    dz = aires.log_probs_backward(z.cuda(), labels.cuda(), r.lse, r.entropy, dlogp=torch.ones(t, device="cuda"),
+                                  dentropy=torch.ones(t, device="cuda"))
+    assert bool(dz[1:4].isnan().all()) and bool(dz[keep].isfinite().all())
+
+
+def test_log_probs_of_large_scores():
+    """Differences from the maximum are what counts: scores of any size."""
+    for v in (30, 3000):
+        for kind in (F32, BF16):
+            z = torch.zeros(4, v, dtype=kind)
+            z[0], z[1, 0], z[2] = 3e38, 3e38, -3e38
+            z[3, 0], z[3, 1] = -3e38, 3e38
+            r = aires.log_probs(z.cuda(), torch.zeros(4, dtype=torch.int64, device="cuda"), top=2)
+            assert abs(float(r.entropy[0]) - math.log(v)) <= 4 * U * math.log(v)
+            assert float(r.entropy[1]) == 0 and float(r.logp[1]) == 0 and r.top_index[1].tolist() == [0, 1]
+            assert abs(float(r.logp[2]) + math.log(v)) <= 4 * U * math.log(v)
+            assert float(r.entropy[3]) == 0 and float(r.top_logp[3, 0]) == 0 and r.top_index[3].tolist() == [1, 2]
+
+
+def test_log_probs_forms():
+    z = rand((20, 77), 1)
+    Z, labels = z.cuda(), torch.arange(20).cuda()
+    r = aires.log_probs(Z, labels, top=4)
+    wide = torch.zeros(20, 99, device="cuda")
+    wide[:, 5:82] = Z
+    s = aires.log_probs(wide[:, 5:82], labels, top=4)
+    for name in ("logp", "entropy", "lse", "top_logp", "top_index"):
+        assert torch.equal(getattr(r, name), getattr(s, name))
+    e = aires.log_probs(torch.empty(0, 5, device="cuda"), torch.empty(0, dtype=torch.int64, device="cuda"), top=3)
+    assert e.logp.shape == (0,) and e.top_index.shape == (0, 3)
+    for call in (lambda: aires.log_probs(z), lambda: aires.log_probs(Z, labels[:3]), lambda: aires.log_probs(Z, labels.float()),
+                 lambda: aires.log_probs(Z, top=78), lambda: aires.log_probs(Z, top=-1), lambda: aires.log_probs(Z, top=65),
+                 lambda: aires.log_probs(Z.t()), lambda: aires.log_probs(Z.double()), lambda: aires.log_probs(Z[:, :0]),
+                 lambda: aires.log_probs_backward(Z, labels, r.lse, dentropy=r.lse),
+                 lambda: aires.log_probs_backward(Z, None, r.lse, dlogp=r.lse),
+                 lambda: aires.log_probs_backward(Z, labels, r.lse[:3], dlogp=r.lse),
+                 lambda: aires.log_probs_backward(Z, labels, r.lse.to(BF16), dlogp=r.lse),
+                 lambda: aires.log_probs_backward(Z, labels, r.lse, dlogp=r.lse, out=Z[:, :5])):
+        with pytest.raises((ValueError, TypeError, aires.AiresError)):
+            call()
+
+
+@pytest.mark.parametrize("t,v", SCORES)
+@pytest.mark.parametrize("zt,dt", [(F32, F32), (BF16, BF16), (F16, F32)])
+def test_log_probs_backward(t, v, zt, dt):
+    z = (2 * rand((t, v), t * 3 + v)).to(zt)
+    if v > 2:
+        z.masked_fill_(torch.rand((t, v), generator=gen(v)) < 0.2, -INF)
+    labels = torch.randint(-1, v + 1, (t,), generator=gen(t))
+    a, b = rand(t, 5), rand(t, 6)
+    lse, _, H, lp, p = logp_ref(z, labels)
+    l32, h32 = lse.float(), H.float()
+    got = aires.log_probs_backward(z.cuda(), labels.cuda(), l32.cuda(), h32.cuda(), dlogp=a.cuda(), dentropy=b.cuda(), dz_dtype=dt)
+    assert got.dtype == dt
+    some = l32 > -INF
+    L = torch.where(some, l32, torch.zeros_like(l32)).double()[:, None]
+    d = torch.where(z == -INF, torch.zeros(()), z.float()).double() - L
+    p = torch.where((z == -INF) | ~some[:, None], torch.zeros((), dtype=torch.float64), torch.exp(d))
+    there = (labels >= 0) & (labels < v) & some
+    A = torch.where(there, a, torch.zeros(())).double()[:, None]
+    Bd, Hd = b.double()[:, None], h32.double()[:, None]
+    hot = torch.zeros(t, v, dtype=torch.float64).scatter_(1, labels.clamp(0, v - 1)[:, None], there.double()[:, None])
+    inner = A + Bd * (d + Hd)
+    want = A * hot - p * inner
+    size = A.abs() + Bd.abs() * (d.abs() + Hd)
+    tol = p * (size * (3 * d.abs() + 10) * U + 4 * U * size) + U * (A.abs() * hot + p * size)
+    near(got, want, tol + rounded(want, dt), "dZ")
+    # one gradient alone, in Z's own place
+    own = z.cuda()
+    one = aires.log_probs_backward(own, labels.cuda(), l32.cuda(), dlogp=a.cuda(), out=own)
+    assert one.data_ptr() == own.data_ptr()
+    want = A * hot - p * A
+    near(own, want, p * A.abs() * (3 * d.abs() + 14) * U + U * A.abs() * hot + rounded(want, zt), "dZ of logp")
+    none = aires.log_probs_backward(z.cuda(), None, l32.cuda())
+    assert not none.any()
+
+
+def test_log_probs_backward_against_differences():
+    t, v, h = 4, 19, 1e-5
+    z, a, b = rand((t, v), 1).double(), rand(t, 2).double(), rand(t, 3).double()
+    labels = torch.tensor([3, -1, 18, 0])
+
+    def value(z):
+        _, logp, H, _, _ = logp_ref(z, labels)
+        return (a * logp + b * H).sum()
+
+    want = torch.empty_like(z)
+    for i in range(z.numel()):
+        d = torch.zeros_like(z).view(-1)
+        d[i] = h
+        d = d.view(z.shape)
+        want.view(-1)[i] = (value(z + d) - value(z - d)) / (2 * h)
+    r = aires.log_probs(z.float().cuda(), labels.cuda())
+    got = aires.log_probs_backward(z.float().cuda(), labels.cuda(), r.lse, r.entropy, dlogp=a.float().cuda(), dentropy=b.float().cuda())
+    # differences: h^2 f''' and 2^-52 |f| / h, below 1e-8 here; a dozen roundings in fp32 of values of a few units
+    near(got, want, 1e-5 * (1 + want.abs()), "dZ")
+
+
+# ------------------------------------------------------------ gradient norm
+
+SETS = [[1], [5, 1, 8191, 8192, 8193], [3, 0, 100000], [1000] * 250, [2000003, 17, 65536], [7] * 5]
+
+
+@pytest.mark.parametrize("kind", [F32, BF16, F16])
+@pytest.mark.parametrize("sizes", SETS, ids=str)
+def test_grad_norm(kind, sizes):
+    grads = [rand(n, n + i, kind) for i, n in enumerate(sizes)]
+    if sizes == [7] * 5:
+        grads = [torch.zeros(n, dtype=kind) for n in sizes]
+    want = math.sqrt(math.fsum(float(g.double().square().sum()) for g in grads))
+    for most in (INF, want / 3, want * 2, 0.0):
+        norm, scale = aires.grad_norm([g.cuda() for g in grads], max_norm=most)
+        assert norm.dtype == scale.dtype == F32 and norm.dim() == scale.dim() == 0
+        # sums in 64 bits: the norm is rounded once, the scale once
+        assert abs(float(norm) - want) <= 1.01 * U * want
+        wants = most / want if want > most else 1.0
+        assert abs(float(scale) - wants) <= 1.01 * U * wants
+    # clipped in place, to other types, and left alone
+    most = want / 3
+    scale = float(aires.grad_norm([g.cuda() for g in grads], max_norm=most)[1])
+    for out_kind in (kind, F32, BF16):
+        mine = [g.cuda() for g in grads]
+        outs = [torch.full(g.shape, 9.0, dtype=out_kind, device="cuda") for g in grads]
+        n1 = aires.clip_grads(mine, most, out=outs)
+        assert float(n1) == float(norm)
+        for g, m, o in zip(grads, mine, outs):
+            assert torch.equal(m.cpu(), g) and torch.equal(o.cpu(), (g.float() * scale).to(out_kind))
+    mine = [g.cuda() for g in grads]
+    v = mine[0]._version
+    aires.clip_grads(mine, most)
+    assert mine[0]._version > v
+    for g, m in zip(grads, mine):
+        assert torch.equal(m.cpu(), (g.float() * scale).to(kind))
+    mine = [g.cuda() for g in grads]
+    aires.clip_grads(mine, want * 2)
+    outs = [torch.empty_like(m) for m in mine]
+    aires.clip_grads(mine, want * 2, out=outs)
+    for g, m, o in zip(grads, mine, outs):
+        assert torch.equal(m.cpu(), g) and torch.equal(o.cpu(), g)
+
+
+def test_grad_norm_of_any_size():
+    for size in (1e-30, 1e25, 3e38):
+        g = torch.full((5000,), size)
+        norm, scale = aires.grad_norm([g.cuda()], max_norm=1.0)
+        want = math.sqrt(float(g.double().square().sum()))
+        if want <= 3.4e38:
+            assert abs(float(norm) - want) <= 1.01 * U * want
+        else:
+            assert float(norm) == INF
+        assert abs(float(scale) - min(1.0, 1 / want)) <= 1.01 * U * min(1.0, 1 / want) + 2.0 ** -149
+    g = torch.ones(10)
+    g[3] = INF
+    norm, scale = aires.grad_norm([g.cuda()], max_norm=1.0)
+    assert float(norm) == INF and float(scale) == 0
+    c = g.cuda()
+    assert float(aires.clip_grads([c], 1.0)) == INF
+    assert math.isnan(float(c[3])) and not c[:3].any()
+    g[4] = math.nan
+    norm, scale = aires.grad_norm([g.cuda()], max_norm=1.0)
+    assert math.isnan(float(norm)) and math.isnan(float(scale))
+    c = g.cuda()
+    aires.clip_grads([c], 1.0)
+    assert bool(c.isnan().all())
+
+
+def test_grad_norm_forms():
+    base = rand(1001, 1, F16).cuda()
+    odd = base[1:]                               # an odd address
+    a, b = aires.grad_norm([odd])[0], aires.grad_norm([odd.clone()])[0]
+    assert torch.equal(a, b)
+    first, second = aires.grad_norm([odd, base])[0], aires.grad_norm([odd, base])[0]
+    assert torch.equal(first, second)
+    x = rand(100, 2).cuda()
+    for call in (lambda: aires.grad_norm([]), lambda: aires.grad_norm([x.cpu()]), lambda: aires.grad_norm([x[::2]]),
+                 lambda: aires.grad_norm([x.double()]), lambda: aires.grad_norm([x], max_norm=-1.0),
+                 lambda: aires.grad_norm([x], max_norm=math.nan), lambda: aires.clip_grads([x], 1.0, out=[]),
+                 lambda: aires.clip_grads([x], 1.0, out=[x[:50]]), lambda: aires.clip_grads([x, x], 1.0),
+                 lambda: aires.clip_grads([x[:50], x[40:90]], 1.0), lambda: aires.clip_grads([x[:50]], 1.0, out=[x[10:60]]),
+                 lambda: aires.clip_grads([x[:50], x[50:]], 1.0, out=[torch.empty_like(x[:50]), x[:50]]),
+                 lambda: aires.clip_grads([x[:50].to(BF16)], 1.0, out=[x[:50].double()])):
+        with pytest.raises((ValueError, TypeError, aires.AiresError)):
+            call()
+    keep = x.clone()
+    aires.clip_grads([x[:50], x[50:]], 1e-3)
+    want = keep.double() * 1e-3 / float(keep.double().norm())
+    near(x, want, 4 * U * want.abs(), "neighbours")
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_with_a_scale_on_the_device(bits):
+    def step(**kw):
+        params = [rand((33, 70), 1).cuda(), rand(300, 2).cuda()]
+        grads = [rand((33, 70), 3, BF16).cuda(), rand(300, 4, F16).cuda()]
+        m, v = aires.adamw_state(params, bits=bits)
+        for k in (1, 2):
+            aires.adamw(params, grads, m, v, step=k, lr=1e-2, seed=k, **kw)
+        return params + [x for y in (m, v) for z in y for x in (z if bits == 8 else (z,))]
+
+    grads = [rand((33, 70), 3, BF16).cuda(), rand(300, 4, F16).cuda()]
+    _, scale = aires.grad_norm(grads, max_norm=1.5)
+    assert float(scale) < 0.1
+    for a, b in zip(step(grad_scale=scale), step(grad_scale=float(scale))):
+        assert equal(a, b)
+    for bad in (scale.cpu(), scale.double(), torch.ones(2, device="cuda"), "1"):
+        with pytest.raises((ValueError, TypeError, RuntimeError)):
+            step(grad_scale=bad)
