@@ -838,10 +838,12 @@ typedef struct aires_dense8 {
  */
 aires_status aires_quantize8(const aires_dense *X, const aires_dense8 *Q, const aires_dense8 *Qt, void *stream);
 
-/* Bytes of workspace that aires_matmul8 needs for A (m x k) and B (n x k): partial
-   sums of a k split over workgroups, 64 MB at most.
+/* Bytes of workspace that aires_matmul8 needs for these operands (codes and scales
+   are not read) and a Y of type dtype: partial sums of a k split over workgroups, 64
+   MB at most, and copies of operands whose codes, ld or ncols are no multiple of
+   16 (none for up to 64 rows of A).
    Errors: AIRES_E_INVALID_ARG, AIRES_E_DIM, AIRES_E_UNSUPPORTED. */
-aires_status aires_matmul8_workspace(int64_t m, int64_t n, int64_t k, int64_t *bytes);
+aires_status aires_matmul8_workspace(const aires_dense8 *A, const aires_dense8 *B, int32_t dtype, int64_t *bytes);
 
 /*
  * aires_matmul8 -- Y = A B^T of matrices held in 8 bits (Y: m x n, any type):
@@ -856,7 +858,8 @@ aires_status aires_matmul8_workspace(int64_t m, int64_t n, int64_t k, int64_t *b
  * Y is zeros.
  * Errors: AIRES_E_INVALID_ARG (NULL, bad type or tile, ld too small, workspace not
  * 16-byte aligned), AIRES_E_DIM (sizes differ), AIRES_E_UNSUPPORTED (m or n above
- * 2^26, k or a row's stride above 2^23, more than 2^22 tiles of 128 x 128 of Y),
+ * 2^26, k or a row's stride above 2^23, that of its scales above 2^21, more than 2^22
+ * tiles of 128 x 128 of Y),
  * AIRES_E_CAPACITY, AIRES_E_HIP.
  */
 aires_status aires_matmul8(const aires_dense8 *A, const aires_dense8 *B, const aires_dense *Y, void *workspace,

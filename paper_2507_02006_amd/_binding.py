@@ -184,7 +184,7 @@ def load() -> ctypes.CDLL:
         "aires_grad_norm": (ctypes.c_int, [c_vp, c_i64, c_dbl, c_vp, c_vp, c_vp, c_i64, c_vp]),
         "aires_clip_grads": (ctypes.c_int, [c_vp, c_i64, c_dbl, c_vp, c_vp, c_i64, c_vp]),
         "aires_quantize8": (ctypes.c_int, [P(Dense), P(Dense8), P(Dense8), c_vp]),
-        "aires_matmul8_workspace": (ctypes.c_int, [c_i64, c_i64, c_i64, P(c_i64)]),
+        "aires_matmul8_workspace": (ctypes.c_int, [P(Dense8), P(Dense8), c_i32, P(c_i64)]),
         "aires_matmul8": (ctypes.c_int, [P(Dense8), P(Dense8), P(Dense), c_vp, c_i64, c_vp]),
         "aires_rms_norm": (ctypes.c_int, [P(Dense), P(Dense), c_vp, c_i32, c_dbl, P(Dense), P(Dense), P(Dense8), c_vp,
                                           c_vp]),

@@ -226,7 +226,7 @@ at::Tensor matmul_8bit(const py::tuple& A, const py::tuple& B, std::optional<at:
   const aires_dense y = dense(Y, "out");
   if (y.nrows != a.nrows || y.ncols != b.nrows) bad_value("out must have A's rows and a column for each of B's");
   int64_t need = 0;
-  check(aires_matmul8_workspace(a.nrows, b.nrows, a.ncols, &need), "aires_matmul8_workspace");
+  check(aires_matmul8_workspace(&a, &b, y.dtype, &need), "aires_matmul8_workspace");
   at::Tensor work;
   if (need > 0) work = at::empty({need}, ac.options().dtype(at::kByte));
   check(aires_matmul8(&a, &b, &y, need > 0 ? work.data_ptr() : nullptr, need, (void*)stream), "aires_matmul8");

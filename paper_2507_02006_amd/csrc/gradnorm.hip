@@ -23,11 +23,13 @@ namespace kern {
 namespace {
 
 constexpr int BLOCK = 256;               // threads of a workgroup
-constexpr int PER = 4;                   // chunks of eight values a lane holds
-constexpr int CHUNK = BLOCK * 8 * PER;   // values a workgroup reads at once
 constexpr int MAX_TENSORS = 96;          // descriptors that fit the kernel arguments
 constexpr int64_t kGroups = 4096;        // workgroups over all tensors, about
-constexpr int64_t kFewPartials = 512;    // partial sums that every workgroup adds by itself
+constexpr int64_t kFewPartials = 1024;   // partial sums that every workgroup adds by itself
+// Chunks of eight values a lane reads at once: four, or one where the tensors are so
+// small that more workgroups hide more of the way to memory.
+constexpr int64_t chunk_of(int per) { return BLOCK * 8 * per; }
+constexpr int64_t kSmall = kFewPartials * chunk_of(1);
 
 struct Table {
   GradTensor t[MAX_TENSORS];
@@ -66,6 +68,13 @@ __device__ __forceinline__ double block_sum(double v, double* buf) {
   return v;
 }
 
+template <int PER, bool ONCE>
+__device__ __forceinline__ void load_chunk(const GradTensor& t, int64_t at, int64_t end, Raw8 (&r)[PER]) {
+#pragma unroll
+  for (int q = 0; q < PER; ++q) load_raw<ONCE>(t.g, t.gt, at + q * BLOCK * 8, end - at - q * BLOCK * 8, r[q]);
+}
+
+template <int PER>
 __global__ __launch_bounds__(BLOCK) void k_grad_squares(Table tab, double* part) {
   __shared__ double buf[BLOCK / 64];
   const int k = find(tab, blockIdx.x);
@@ -73,10 +82,9 @@ __global__ __launch_bounds__(BLOCK) void k_grad_squares(Table tab, double* part)
   const int64_t begin = (int64_t)(blockIdx.x - tab.first[k]) * tab.span;
   const int64_t end = begin + tab.span < t.n ? begin + tab.span : t.n;
   double sum = 0.0;
-  for (int64_t at = begin + threadIdx.x * 8; at < end; at += CHUNK) {
+  for (int64_t at = begin + threadIdx.x * 8; at < end; at += chunk_of(PER)) {
     Raw8 r[PER];
-#pragma unroll
-    for (int q = 0; q < PER; ++q) load_raw<true>(t.g, t.gt, at + q * BLOCK * 8, end - at - q * BLOCK * 8, r[q]);
+    load_chunk<PER, (PER > 1)>(t, at, end, r);
 #pragma unroll
     for (int q = 0; q < PER; ++q) {
       float x[8];
@@ -111,9 +119,18 @@ __global__ __launch_bounds__(BLOCK) void k_grad_norm(Final f) {
   }
 }
 
-// out = g * scale, scale from the partial sums or (parts = 0) from memory.
+// out = g * scale, scale from the partial sums or (parts = 0) from memory.  The
+// first gradients are asked for before it.
+template <int PER>
 __global__ __launch_bounds__(BLOCK) void k_grad_scale(Table tab, Final f) {
   __shared__ double buf[BLOCK / 64];
+  const int k = find(tab, blockIdx.x);
+  const GradTensor& t = tab.t[k];
+  const int64_t begin = (int64_t)(blockIdx.x - tab.first[k]) * tab.span;
+  const int64_t end = begin + tab.span < t.n ? begin + tab.span : t.n;
+  int64_t at = begin + threadIdx.x * 8;
+  Raw8 r[PER];
+  load_chunk<PER, (PER > 1)>(t, at, end, r);
   float scale;
   if (f.parts > 0) {
     const double sum = add_parts(f, buf);
@@ -122,15 +139,8 @@ __global__ __launch_bounds__(BLOCK) void k_grad_scale(Table tab, Final f) {
   } else {
     scale = *f.scale;
   }
-  const int k = find(tab, blockIdx.x);
-  const GradTensor& t = tab.t[k];
   if (scale == 1.f && t.out == t.g) return;
-  const int64_t begin = (int64_t)(blockIdx.x - tab.first[k]) * tab.span;
-  const int64_t end = begin + tab.span < t.n ? begin + tab.span : t.n;
-  for (int64_t at = begin + threadIdx.x * 8; at < end; at += CHUNK) {
-    Raw8 r[PER];
-#pragma unroll
-    for (int q = 0; q < PER; ++q) load_raw<true>(t.g, t.gt, at + q * BLOCK * 8, end - at - q * BLOCK * 8, r[q]);
+  while (at < end) {
 #pragma unroll
     for (int q = 0; q < PER; ++q) {
       float x[8];
@@ -139,17 +149,17 @@ __global__ __launch_bounds__(BLOCK) void k_grad_scale(Table tab, Final f) {
       for (int j = 0; j < 8; ++j) x[j] *= scale;
       Raw8 p;
       pack(x, t.ot, p);
-      store_raw<true>(t.out, t.ot, at + q * BLOCK * 8, end - at - q * BLOCK * 8, p);
+      store_raw<(PER > 1)>(t.out, t.ot, at + q * BLOCK * 8, end - at - q * BLOCK * 8, p);
     }
+    at += chunk_of(PER);
+    if (at < end) load_chunk<PER, (PER > 1)>(t, at, end, r);
   }
 }
 
 // Values a workgroup goes through: at most kGroups workgroups, and one for each tensor.
-int64_t span_of(const GradTensor* tensors, int64_t count) {
-  int64_t total = 0;
-  for (int64_t k = 0; k < count; ++k) total += tensors[k].n;
+int64_t span_of(int64_t total, int64_t chunk) {
   const int64_t each = (total + kGroups - 1) / kGroups;
-  return std::max<int64_t>(1, (each + CHUNK - 1) / CHUNK) * CHUNK;
+  return std::max<int64_t>(1, (each + chunk - 1) / chunk) * chunk;
 }
 
 // Launches over all tensors, a table of them at a time; `go` gets the number
@@ -186,10 +196,14 @@ int64_t grad_norm_workspace(int64_t count) { return (kGroups + count + 1) * (int
 hipError_t grad_norm(const GradTensor* tensors, int64_t count, double max_norm, float* norm, float* scale, bool clip,
                      void* ws, hipStream_t s) {
   double* part = static_cast<double*>(ws);
-  const int64_t span = span_of(tensors, count);
+  int64_t total = 0;
+  for (int64_t k = 0; k < count; ++k) total += tensors[k].n;
+  const bool small = total <= kSmall;
+  const int64_t span = span_of(total, chunk_of(small ? 1 : 4));
   Final f{part, 0, max_norm, norm, scale};
   hipError_t e = for_tables(tensors, count, span, [&](const Table& tab, uint32_t groups, int64_t before) {
-    k_grad_squares<<<groups, BLOCK, 0, s>>>(tab, part + before);
+    if (small) k_grad_squares<1><<<groups, BLOCK, 0, s>>>(tab, part + before);
+    else k_grad_squares<4><<<groups, BLOCK, 0, s>>>(tab, part + before);
     f.parts = before + groups;
   });
   if (e != hipSuccess) return e;
@@ -203,7 +217,8 @@ hipError_t grad_norm(const GradTensor* tensors, int64_t count, double max_norm, 
   return for_tables(tensors, count, span, [&](const Table& tab, uint32_t groups, int64_t before) {
     Final g = f;
     if (before > 0) g.norm = nullptr;
-    k_grad_scale<<<groups, BLOCK, 0, s>>>(tab, g);
+    if (small) k_grad_scale<1><<<groups, BLOCK, 0, s>>>(tab, g);
+    else k_grad_scale<4><<<groups, BLOCK, 0, s>>>(tab, g);
   });
 }
 

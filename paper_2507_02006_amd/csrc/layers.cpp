@@ -71,6 +71,21 @@ aires_status check_product(int64_t m, int64_t n, int64_t k) {
   return AIRES_OK;
 }
 
+aires_status check_operands(const aires_dense8* A, const aires_dense8* B) {
+  ST_TRY(check_held(A, "A"));
+  ST_TRY(check_held(B, "B"));
+  if (A->ncols != B->ncols)
+    return fail(AIRES_E_DIM, "A has %lld columns, B %lld", (long long)A->ncols, (long long)B->ncols);
+  ST_TRY(check_product(A->nrows, B->nrows, A->ncols));
+  if (A->tile != 1) return fail(AIRES_E_INVALID_ARG, "A has scales for each row (tile 1)");
+  // (offsets within a tile are 32 bits wide)
+  if (A->ncols > 0)
+    for (const aires_dense8* q : {A, B})
+      if (q->nrows > 1 && (q->ld > (int64_t(1) << 23) || q->ld_scales > (int64_t(1) << 21)))
+        return fail(AIRES_E_UNSUPPORTED, "strides of %lld and %lld", (long long)q->ld, (long long)q->ld_scales);
+  return AIRES_OK;
+}
+
 aires_status check_scores(int64_t t, int64_t v, int32_t top) {
   if (t < 0 || v < 0 || (t > 0 && v == 0))
     return fail(AIRES_E_DIM, "%lld rows of %lld scores", (long long)t, (long long)v);
@@ -193,30 +208,22 @@ aires_status aires_quantize8(const aires_dense* X, const aires_dense8* Q, const 
   return AIRES_OK;
 }
 
-aires_status aires_matmul8_workspace(int64_t m, int64_t n, int64_t k, int64_t* bytes) {
+aires_status aires_matmul8_workspace(const aires_dense8* A, const aires_dense8* B, int32_t dtype, int64_t* bytes) {
   if (!bytes) return fail(AIRES_E_INVALID_ARG, "bytes is NULL");
-  ST_TRY(check_product(m, n, k));
-  *bytes = kern::matmul8_workspace(m, n, k);
+  ST_TRY(check_operands(A, B));
+  if (!type_ok(dtype)) return fail(AIRES_E_INVALID_ARG, "dtype %d invalid", (int)dtype);
+  *bytes = kern::matmul8_workspace(held(A), held(B), dtype);
   return AIRES_OK;
 }
 
 aires_status aires_matmul8(const aires_dense8* A, const aires_dense8* B, const aires_dense* Y, void* workspace,
                            int64_t workspace_bytes, void* stream) {
-  ST_TRY(check_held(A, "A"));
-  ST_TRY(check_held(B, "B"));
+  ST_TRY(check_operands(A, B));
   ST_TRY(check_dense(Y, "Y"));
-  if (A->ncols != B->ncols || Y->nrows != A->nrows || Y->ncols != B->nrows)
-    return fail(AIRES_E_DIM, "A is %lld x %lld, B %lld x %lld, Y %lld x %lld", (long long)A->nrows,
-                (long long)A->ncols, (long long)B->nrows, (long long)B->ncols, (long long)Y->nrows,
-                (long long)Y->ncols);
-  ST_TRY(check_product(A->nrows, B->nrows, A->ncols));
-  if (A->tile != 1) return fail(AIRES_E_INVALID_ARG, "A has scales for each row (tile 1)");
-  // (offsets within a tile are 32 bits wide)
-  if (A->ncols > 0)
-    for (const aires_dense8* q : {A, B})
-      if (q->nrows > 1 && q->ld > (int64_t(1) << 23))
-        return fail(AIRES_E_UNSUPPORTED, "stride of %lld", (long long)q->ld);
-  ST_TRY(check_workspace(workspace, workspace_bytes, kern::matmul8_workspace(A->nrows, B->nrows, A->ncols)));
+  if (Y->nrows != A->nrows || Y->ncols != B->nrows)
+    return fail(AIRES_E_DIM, "A has %lld rows, B %lld, Y is %lld x %lld", (long long)A->nrows, (long long)B->nrows,
+                (long long)Y->nrows, (long long)Y->ncols);
+  ST_TRY(check_workspace(workspace, workspace_bytes, kern::matmul8_workspace(held(A), held(B), Y->dtype)));
   HIP_TRY(kern::matmul8(held(A), held(B), mat(Y), workspace, (hipStream_t)stream));
   return AIRES_OK;
 }

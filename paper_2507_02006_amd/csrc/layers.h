@@ -25,7 +25,7 @@ hipError_t rms_norm_backward(const Mat& dY, const Mat& S, const float* rstd, con
 
 // X in 8 bits, as it lies and transposed (codes NULL: not wanted)
 hipError_t quantize8(const Mat& X, const Held& Q, const Held& Qt, hipStream_t s);
-int64_t matmul8_workspace(int64_t m, int64_t n, int64_t k);
+int64_t matmul8_workspace(const Held& A, const Held& B, int type);  // of Y
 hipError_t matmul8(const Held& A, const Held& B, const Mat& Y, void* ws, hipStream_t s);
 
 // log probabilities

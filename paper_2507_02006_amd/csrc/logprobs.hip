@@ -91,8 +91,10 @@ __device__ __forceinline__ int group_best(int v) {
   v = op(v, dpp_i32<0x4E>(v));
   v = op(v, dpp_i32<0x141>(v));
   if constexpr (W >= 16) v = op(v, dpp_i32<0x140>(v));
-  if constexpr (W >= 32) v = op(v, __shfl_xor(v, 16));
-  if constexpr (W == 64) v = op(v, __shfl_xor(v, 32));
+  if constexpr (W == 32) v = op(v, __shfl_xor(v, 16));
+  if constexpr (W == 64)  // one lane of each row of 16, in scalar registers
+    v = op(op(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16)),
+           op(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
   return v;
 }
 
@@ -270,13 +272,12 @@ struct List {
       col = lane > place ? pc : lane == place ? c : col;
       count += count < top;
       if (count == top) last = __builtin_amdgcn_readlane(key, top - 1);
-      if (lane == owner) {
-        best = NONE;
+      at = lane == owner ? at : 8;
+      best = NONE;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          k[j] = j == at ? NONE : k[j];
-          best = k[j] > best ? k[j] : best;
-        }
+      for (int j = 0; j < 8; ++j) {
+        k[j] = j == at ? NONE : k[j];
+        best = k[j] > best ? k[j] : best;
       }
     }
   }
@@ -388,9 +389,11 @@ __global__ __launch_bounds__(BLOCK) void k_logp_back(Back a) {
       else y = -1;
     }
     const bool none = lse == -__builtin_inff();
+    Raw8 next;
+    load_raw<ONCE>(a.z, a.zt, row * a.ldz + first, a.v - first, next);
     for (int64_t c = first; c < a.v; c += step) {
-      Raw8 r;
-      load_raw<ONCE>(a.z, a.zt, row * a.ldz + c, a.v - c, r);
+      Raw8 r = next;
+      load_raw<ONCE>(a.z, a.zt, row * a.ldz + c + step, a.v - c - step, next);
       float z[8];
       convert(r, a.zt, z);
 #pragma unroll

@@ -16,13 +16,12 @@
 // anyway, the codes are converted to bf16, which holds them exactly, and multiplied
 // at half the rate with sums that are fp32's.
 //
-// Three forms.  Up to 64 rows of A ("rows"): bound by B's bytes, which go from
-// memory to the matrix cores' registers, no LDS; a workgroup owns 16 rows of B and
-// its wavefronts share k.  Else tiles: stages of 128 k go from global memory
-// straight to LDS, their 16-byte chunks placed as in tile.h.  Where the
-// operands' rows are not chunks of 16 bytes they go through registers, which
-// put zeros past the last k.  Where there are few tiles k is split over
-// workgroups, whose partial sums a second launch adds in a fixed order.
+// Two forms.  Up to 64 rows of A: bound by B's bytes, which go from memory to the
+// matrix cores' registers, no LDS; a workgroup owns 16 rows of B and its wavefronts
+// share k.  Else tiles: stages of 128 k go from global memory straight to LDS.  Where
+// an operand's rows are not chunks of 16 bytes it is copied so first.  Where there are few
+// tiles k is split over workgroups, whose partial sums a second launch adds in a fixed
+// order.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -44,7 +43,7 @@ struct Args {
   Held x, w;        // A (rows of Y) and B (columns of Y)
   Mat y;
   float* part;      // [split][rows][columns] sums, or NULL
-  int64_t k, steps; // steps of 128 k
+  int64_t k, steps; // k (in tiles: a multiple of 16), steps of 128 k
   int64_t per;      // steps of a split
 };
 
@@ -71,12 +70,11 @@ __device__ __forceinline__ i32x4 load16(const uint8_t* p, int64_t have) {
   return v;
 }
 
-__device__ __forceinline__ void store_y(const Args& a, int64_t row, int64_t col, int split, const float (&v)[4]) {
+__device__ __forceinline__ void store_y(const Args& a, int64_t row, int64_t col, const float (&v)[4]) {
   if (row >= a.y.rows || col >= a.y.cols) return;
-  const bool part = a.part != nullptr;
-  void* const to = part ? a.part : a.y.data;
-  const int64_t at = part ? ((int64_t)split * a.y.rows + row) * a.y.cols + col : row * a.y.ld + col;
-  const int t = part ? (int)DT_F32 : a.y.type;
+  void* const to = a.y.data;
+  const int64_t at = row * a.y.ld + col;
+  const int t = a.y.type;
   if (col + 4 <= a.y.cols) {
     if (t == DT_F32) store4<DT_F32>(to, at, v);
     else if (t == DT_BF16) store4<DT_BF16>(to, at, v);
@@ -90,52 +88,78 @@ __device__ __forceinline__ void store_y(const Args& a, int64_t row, int64_t col,
 
 // ------------------------------------------------------------------- tiles
 
-// One operand's share of a stage through registers: SPAN rows of 128 k.
+// One operand's share of a stage: SPAN rows of 128 k.  Load j of a wavefront fills
+// 1 KB, 8 rows, of the stage; its 16-byte chunks are placed XORed with their row
+// so that neither writes nor reads of LDS meet bank conflicts.  Rows past the last repeat it (their results
+// are not used).
 template <int SPAN, int WAVES>
-struct Copier {
-  static constexpr int TOTAL = SPAN / 8, COUNT = (TOTAL + WAVES - 1) / WAVES;
-  const uint8_t* base;
-  int64_t left;
-  uint32_t off[COUNT];
-  int at[COUNT];
-  i32x4 held[COUNT];
+struct Share {
+  static constexpr int COUNT = SPAN / 8 / WAVES;
+  static_assert(SPAN % (8 * WAVES) == 0, "a wavefront loads whole parts");
+  const uint8_t* base;  // first row of the tile, advanced along k
+  int64_t ld, left;     // left: k that there are from the next stage's first on
+  int last;             // last row that there is
+  uint32_t off;         // of this lane in the first part
+
+  __device__ static int row(int wave, int lane) { return wave * 8 + lane / 8; }
+  __device__ static int chunk(int wave, int lane) { return ((lane % 8) ^ (row(wave, lane) / 2 % 8)) * 16; }
 
   __device__ void init(const Held& h, int64_t r0, int64_t k0, int64_t k, int wave, int lane) {
     base = h.codes + r0 * h.ld + k0;
+    ld = h.ld;
     left = k - k0;
-    const int64_t last = h.rows - 1 - r0;
-#pragma unroll
-    for (int j = 0; j < COUNT; ++j) {
-      const int r = part_of<TOTAL, WAVES>(j, wave) * 8 + lane / 8;
-      at[j] = ((lane % 8) ^ (r / 2 % 8)) * 16;
-      off[j] = (uint32_t)((r < last ? r : last) * h.ld + at[j]);
-    }
+    last = h.rows - 1 - r0 < SPAN ? (int)(h.rows - 1 - r0) : SPAN;
+    off = (uint32_t)(row(wave, lane) * ld + chunk(wave, lane));
   }
-  __device__ __forceinline__ void load() {
+  // Straight to LDS.  k past the last repeats the row's last chunk (the other operand
+  // holds zeros there).
+  __device__ __forceinline__ void issue(char* lds, int wave, int lane) {
+    const uint64_t b = reinterpret_cast<uint64_t>(base);
+    const uint8_t* from = reinterpret_cast<const uint8_t*>(
+        ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(b >> 32)) << 32) |
+        (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)b));
+    const auto load = [&](int j, const uint8_t* p) {
+      __builtin_amdgcn_global_load_lds((global_void*)p, (lds_void*)(lds + (j * WAVES + wave) * 1024), 16, 0, 0);
+    };
+    if (last >= SPAN - 1 && left >= 128) {
 #pragma unroll
-    for (int j = 0; j < COUNT; ++j) held[j] = load16(base + off[j], left - at[j]);
+      for (int j = 0; j < COUNT; ++j, from += WAVES * 8 * ld) load(j, from + off);
+    } else {
+      const int at = chunk(wave, lane), c = at < left ? at : (int)left - 16;
+#pragma unroll
+      for (int j = 0; j < COUNT; ++j) {
+        const int r = row(wave, lane) + j * WAVES * 8;
+        load(j, from + (uint32_t)((r < last ? r : last) * ld + c));
+      }
+    }
     base += 128;
     left -= 128;
   }
-  __device__ __forceinline__ void store(char* lds, int wave, int lane) const {
-#pragma unroll
-    for (int j = 0; j < COUNT; ++j)
-      *reinterpret_cast<i32x4*>(lds + part_of<TOTAL, WAVES>(j, wave) * 1024 + lane * 16) = held[j];
-  }
 };
 
+// Where a lane reads its row's chunk h of 128 k, h = 0..3: 16 k each of the lane's half
+// (32 rows on: the same place 4 KB on).
+__device__ __forceinline__ uint32_t place_of(int first, int lane) {
+  const int r = first + (lane & 31);
+  return (uint32_t)(r * 128 + (((lane >> 5) ^ (r / 2 % 8)) << 4));
+}
+
 // TW x TX: rows of B and of A in a tile, WW x WX a wavefront's.  ROWS: B has scales
-// for each row.  DIRECT: rows are chunks of 16 bytes and go straight to LDS.  WIDE:
-// the products are made in bf16.
-template <int TW, int TX, int WW, int WX, int STAGES, bool ROWS, bool DIRECT, bool WIDE>
+// for each row.  WIDE: the products are made in bf16.
+template <int TW, int TX, int WW, int WX, int STAGES, bool ROWS, bool WIDE>
 struct Tile8 {
   static constexpr int WAVES = TW / WW * (TX / WX), THREADS = 64 * WAVES;
   static constexpr int MT = WW / 32, NT = WX / 32;
-  static constexpr int CODES = (TW + TX) * 128, STAGE = CODES + (TW + TX) * 4, LDS = STAGES * STAGE;
-  static constexpr int SCALES = (TW + TX) / 64;  // loads of 64 scales
-  static_assert(SCALES <= WAVES, "a wavefront loads 64 scales a stage");
+  static constexpr int STAGE = (TW + TX) * 128;
+  // Scales of four steps at a time, [step][row], twice: a row's lie next to each other
+  // in memory, and each line that is fetched for them gives four.
+  static constexpr int SCALES = (TW + TX) * 16, LDS = STAGES * STAGE + 2 * SCALES;
+  static constexpr int SHARES = (TW + TX) / 64;  // of 64 rows
+  static constexpr int EACH = SHARES > WAVES ? SHARES / WAVES : 1;  // a wavefront's
   static_assert(WW <= BLOCK8, "a wavefront's rows of B share a scale");
-  static constexpr int LOADS = Stager<TW, WAVES, false>::COUNT + Stager<TX, WAVES, false>::COUNT + 1;
+  typedef Share<TW, WAVES> ShareW;
+  typedef Share<TX, WAVES> ShareX;
+  static constexpr int LOADS = ShareW::COUNT + ShareX::COUNT;
 
   static __device__ __forceinline__ void run(const Args& a, int64_t w0, int64_t x0, int64_t s0, int64_t s1, char* lds,
                                              f32x16 (&acc)[MT][NT]) {
@@ -147,96 +171,74 @@ struct Tile8 {
       for (int j = 0; j < NT; ++j)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-    const Reader<TW, WW, false> rw(ww * WW, lane);
-    const Reader<TX, WX, false> rx(wx0, lane);
+    const uint32_t at_w = place_of(ww * WW, lane), at_x = TW * 128 + place_of(wx0, lane);
     const int total = (int)(s1 - s0);
-    // this wavefront's scales: 64 rows of the tile, B's first
-    const int sp = wave % SCALES;
-    const float* scale;
-    {
+    // this wavefront's shares of the scales: 64 rows of the tile, B's first
+    const float* scale[EACH];
+    uint32_t scale_off[EACH];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+      const int sp = (wave * EACH + e) % SHARES;
       const bool of_w = sp < TW / 64;
       const Held& h = of_w ? a.w : a.x;
-      const int64_t r = (of_w ? w0 + sp * 64 : x0 + (sp - TW / 64) * 64) + lane;
-      scale = h.scales + (r < h.rows ? r : h.rows - 1) / h.tile * h.lds + s0;
+      const int64_t r0 = of_w ? w0 : x0, r = r0 + (of_w ? sp : sp - TW / 64) * 64 + lane;
+      const int64_t q0 = r0 / h.tile;
+      scale[e] = h.scales + q0 * h.lds + s0;
+      scale_off[e] = (uint32_t)(((r < h.rows ? r : h.rows - 1) / h.tile - q0) * h.lds * 4);
     }
-    Stager<TW, WAVES, false> sw;
-    Stager<TX, WAVES, false> sx;
-    Copier<TW, WAVES> copy_w;
-    Copier<TX, WAVES> copy_x;
-    float held = 0.f;
-    if constexpr (DIRECT) {
-      const Panel pw{reinterpret_cast<const uint16_t*>(a.w.codes), a.w.ld / 2, a.w.rows, a.k / 2};
-      const Panel px{reinterpret_cast<const uint16_t*>(a.x.codes), a.x.ld / 2, a.x.rows, a.k / 2};
-      sw.init(pw, w0, s0 * 64, wave, lane);
-      sx.init(px, x0, s0 * 64, wave, lane);
-    } else {
-      copy_w.init(a.w, w0, s0 * 128, a.k, wave, lane);
-      copy_x.init(a.x, x0, s0 * 128, a.k, wave, lane);
-    }
-    auto issue = [&](int stage) {  // DIRECT
-      char* to = lds + stage * STAGE;
-      if (sw.left < BK) {
-        const Panel pw{nullptr, a.w.ld / 2, a.w.rows, a.k / 2}, px{nullptr, a.x.ld / 2, a.x.rows, a.k / 2};
-        sw.place(pw, w0, wave, lane);
-        sx.place(px, x0, wave, lane);
-      }
-      sw.issue(to, wave);
-      sx.issue(to + TW * 128, wave);
-      __builtin_amdgcn_global_load_lds((global_void*)scale, (lds_void*)(to + CODES + sp * 256), 4, 0, 0);
-      sw.base += sw.step;
-      sx.base += sx.step;
-      sw.left -= BK;
-      sx.left -= BK;
-      ++scale;
-    };
-    auto load = [&]() {  // not DIRECT
-      copy_w.load();
-      copy_x.load();
-      held = *scale++;
-    };
-    auto store = [&](int stage) {
-      char* to = lds + stage * STAGE;
-      copy_w.store(to, wave, lane);
-      copy_x.store(to + TW * 128, wave, lane);
-      reinterpret_cast<float*>(to + CODES)[sp * 64 + lane] = held;
-    };
-    if constexpr (DIRECT) {
+    // (steps past the last repeat it)
+    const auto issue_scales = [&](int group) {
 #pragma unroll
-      for (int s = 0; s < STAGES - 1; ++s)
-        if (s < total) issue(s);
-    } else {
-      load();
-      store(0);
-      if (total > 1) load();
-    }
+      for (int e = 0; e < EACH; ++e) {
+        char* to = lds + STAGES * STAGE + (group & 1) * SCALES + (wave * EACH + e) % SHARES * 256;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int s = group * 4 + q < total ? group * 4 + q : total - 1;
+          __builtin_amdgcn_global_load_lds((global_void*)(reinterpret_cast<const char*>(scale[e] + s) + scale_off[e]),
+                                           (lds_void*)(to + q * (TW + TX) * 4), 4, 0, 0);
+        }
+      }
+    };
+    ShareW sw;
+    ShareX sx;
+    sw.init(a.w, w0, s0 * 128, a.k, wave, lane);
+    sx.init(a.x, x0, s0 * 128, a.k, wave, lane);
+    const auto issue = [&](int stage) {
+      char* to = lds + stage * STAGE;
+      sw.issue(to, wave, lane);
+      sx.issue(to + TW * 128, wave, lane);
+    };
+    issue_scales(0);
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s)
+      if (s < total) issue(s);
     int cur = 0;
     for (int s = 0; s < total; ++s) {
       // this step's loads are the oldest ones; the reads of the step before are
       // done in every wavefront before any overwrites their stage
-      if constexpr (DIRECT) {
-        if (s + STAGES - 2 < total) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LOADS * (STAGES - 2)) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-      } else {
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      }
+      if (s + STAGES - 2 < total) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LOADS * (STAGES - 2)) : "memory");
+      else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
       char* const codes_w = lds + cur * STAGE;
-      if constexpr (DIRECT) {
-        const int tail = (int)((a.k - (s0 + s) * 128) / 16);  // chunks there are
-        if (tail < 8) {
-          // what was loaded past the last k counts 0 (A's finite codes there, or
-          // NaNs of a row that has one anyway, are multiplied with B's zeros)
-          for (int i = threadIdx.x; i < TW * 8; i += THREADS)
-            if (i % 8 >= tail) *reinterpret_cast<i32x4*>(codes_w + (i / 8) * 128 + (((i % 8) ^ (i / 16 % 8)) << 4)) = i32x4{0, 0, 0, 0};
-          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-          __builtin_amdgcn_s_barrier();
-          asm volatile("" ::: "memory");
-        }
-        if (s + STAGES - 1 < total) issue(cur == 0 ? STAGES - 1 : cur - 1);
+      const int tail = (int)((a.k - (s0 + s) * 128) / 16);  // chunks there are
+      if (tail < 8) {
+        // what was loaded past the last k counts 0 (A's finite codes there, or NaNs of a
+        // row that has one anyway, are multiplied with B's zeros)
+        for (int i = threadIdx.x; i < TW * 8; i += THREADS)
+          if (i % 8 >= tail) *reinterpret_cast<i32x4*>(codes_w + (i / 8) * 128 + (((i % 8) ^ (i / 16 % 8)) << 4)) = i32x4{0, 0, 0, 0};
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
       }
-      const char* const codes_x = codes_w + TW * 128;
-      const float* const scales = reinterpret_cast<const float*>(codes_w + CODES);
+      if (s + STAGES - 1 < total) issue(cur == 0 ? STAGES - 1 : cur - 1);
+      // (the other half was last read before this step's barrier)
+      if (s % 4 == 0 && s + 4 < total) issue_scales(s / 4 + 1);
+      const float* const scales = reinterpret_cast<const float*>(lds + STAGES * STAGE + (s / 4 & 1) * SCALES) + s % 4 * (TW + TX);
+      const uint32_t stage_w = (uint32_t)(cur * STAGE) + at_w, stage_x = (uint32_t)(cur * STAGE) + at_x;
+      const auto read = [&](uint32_t at, int block, int h) {  // (stages lie at multiples of 256)
+        return *reinterpret_cast<const i32x4*>(lds + (at ^ (h << 5)) + block * 4096);
+      };
       float f[NT];
       const float fw = ROWS ? 1.f : scales[ww * WW];
       i32x4 cx[4][NT];      // this lane's codes of A: chunks of 16 k
@@ -246,81 +248,131 @@ struct Tile8 {
         f[j] = scales[TW + wx0 + j * 32 + (lane & 31)] * fw;
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
-          cx[h][j] = __builtin_bit_cast(i32x4, rx.get(codes_x, j, h));
+          cx[h][j] = read(stage_x, j, h);
           if constexpr (WIDE) {
             wx[2 * h][j] = widen(cx[h][j], 0);
             wx[2 * h + 1][j] = widen(cx[h][j], 1);
           }
         }
       }
+      // Products of a 32 x 32 block run while the sums of the one before are scaled.
+      f32x16 t[2];
+      float row[ROWS ? 16 : 1];  // the scales of this lane's rows
+      const auto scale_sums = [&](int i, int j) {
+        if constexpr (ROWS)
+          if (j == 0)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const f32x4 v = *reinterpret_cast<const f32x4*>(scales + ww * WW + i * 32 + 8 * q + 4 * (lane >> 5));
+              row[4 * q] = v[0]; row[4 * q + 1] = v[1]; row[4 * q + 2] = v[2]; row[4 * q + 3] = v[3];
+            }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[i][j][r] += t[(i * NT + j) & 1][r] * (ROWS ? row[ROWS ? r : 0] * f[j] : f[j]);
+      };
+      i32x4 cw[2][4];
+      const auto read_w = [&](int i) {
+#pragma unroll
+        for (int h = 0; h < 4; ++h) cw[i & 1][h] = read(stage_w, i, h);
+      };
+      read_w(0);
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
-        i32x4 cw[4];
+        if constexpr (!WIDE)
+          if (i + 1 < MT) read_w(i + 1);
+        bf16x8 w[WIDE ? 8 : 1];
+        if constexpr (WIDE)
 #pragma unroll
-        for (int h = 0; h < 4; ++h) cw[h] = __builtin_bit_cast(i32x4, rw.get(codes_w, i, h));
-        f32x4 row[4];  // ROWS: the scales of this lane's rows
-        if constexpr (ROWS)
+          for (int h = 0; h < 8; ++h) w[h] = widen(cw[i & 1][h / 2], h % 2);
 #pragma unroll
-          for (int q = 0; q < 4; ++q)
-            row[q] = *reinterpret_cast<const f32x4*>(scales + ww * WW + i * 32 + 8 * q + 4 * (lane >> 5));
-        f32x16 t[NT];
-        if constexpr (WIDE) {
+        for (int j = 0; j < NT; ++j) {
+          f32x16& p = t[(i * NT + j) & 1];
+          if constexpr (WIDE) {
 #pragma unroll
-          for (int h = 0; h < 8; ++h) {
-            const bf16x8 w = widen(cw[h / 2], h % 2);
-#pragma unroll
-            for (int j = 0; j < NT; ++j)
-              t[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, wx[h][j], h ? t[j] : f32x16{}, 0, 0, 0);
+            for (int h = 0; h < 8; ++h)
+              p = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w[h], wx[h][j], h ? p : f32x16{}, 0, 0, 0);
+            if (j == 0 && i + 1 < MT) read_w(i + 1);
+          } else {
+            const i32x4* const c = cw[i & 1];
+            p = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(join(c[0], c[1]), join(cx[0][j], cx[1][j]), f32x16{}, 0, 0, 0, 0, 0, 0);
+            p = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(join(c[2], c[3]), join(cx[2][j], cx[3][j]), p, 0, 0, 0, 0, 0, 0);
           }
-        } else {
-#pragma unroll
-          for (int j = 0; j < NT; ++j)
-            t[j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(join(cw[0], cw[1]), join(cx[0][j], cx[1][j]), f32x16{}, 0, 0, 0, 0, 0, 0);
-#pragma unroll
-          for (int j = 0; j < NT; ++j)
-            t[j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(join(cw[2], cw[3]), join(cx[2][j], cx[3][j]), t[j], 0, 0, 0, 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
+          if (j > 0) scale_sums(i, j - 1);
+          else if (i > 0) scale_sums(i - 1, NT - 1);
+          __builtin_amdgcn_sched_barrier(0);
         }
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            if constexpr (ROWS) acc[i][j][r] += t[j][r] * (row[r / 4][r % 4] * f[j]);
-            else acc[i][j][r] += t[j][r] * f[j];
-          }
       }
-      if constexpr (!DIRECT)
-        if (s + 1 < total) {
-          store(cur ^ 1);
-          if (s + 2 < total) load();
-        }
+      scale_sums(MT - 1, NT - 1);
       cur = cur == STAGES - 1 ? 0 : cur + 1;
+    }
+  }
+
+  // Results in type Y to rows [r0, rows) and columns [c0, cols) of a matrix whose row
+  // `first` is the tile's matrix's first.
+  template <int Y>
+  static __device__ __forceinline__ void write(const f32x16 (&acc)[MT][NT], char* to, int64_t first, int64_t ld, int64_t r0,
+                                               int64_t c0, int64_t rows, int64_t cols, char* lds) {
+    constexpr int SIZE = dtype_bytes(Y), ROW = WW * SIZE + 16, LANES = WW * SIZE / 16, EACH = 16 / SIZE;
+    static_assert(WAVES * WX * ROW <= LDS, "a tile's results fit the stages' LDS");
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int ww = wave / (TX / WX), wx = wave % (TX / WX);
+    char* const mine = lds + wave * WX * ROW;
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float v[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+          char* p = mine + (j * 32 + (lane & 31)) * ROW + (i * 32 + 8 * q + 4 * (lane >> 5)) * SIZE;
+          if constexpr (Y == DT_F32) *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
+          else store4<Y>(p, 0, v);
+        }
+    wave_sync();
+    const int64_t col = c0 + ww * WW + lane % LANES * EACH;
+    const int64_t have = cols - col;
+#pragma unroll 4
+    for (int r = lane / LANES; r < WX; r += 64 / LANES) {
+      const int64_t row = r0 + wx * WX + r;
+      if (row >= rows || have <= 0) continue;
+      const u32x4 v = *reinterpret_cast<const u32x4*>(mine + r * ROW + lane % LANES * 16);
+      char* const at = to + ((first + row) * ld + col) * SIZE;
+      if (have >= EACH) {
+        store_vec<true>(reinterpret_cast<u32x4_el2*>(at), (u32x4_el2)v);
+      } else if constexpr (Y == DT_F32) {
+#pragma unroll
+        for (int q = 0; q < EACH - 1; ++q)
+          if (q < have) reinterpret_cast<uint32_t*>(at)[q] = v[q];
+      } else {
+#pragma unroll
+        for (int q = 0; q < EACH - 1; ++q)
+          if (q < have) reinterpret_cast<uint16_t*>(at)[q] = (uint16_t)(v[q / 2] >> (16 * (q & 1)));
+      }
     }
   }
 };
 
-template <int TW, int TX, int WW, int WX, int STAGES, bool ROWS, bool DIRECT, bool WIDE>
-__global__ __launch_bounds__(TW / WW * (TX / WX) * 64) void k_tiles8(Args a) {
-  typedef Tile8<TW, TX, WW, WX, STAGES, ROWS, DIRECT, WIDE> T;
-  static_assert(DIRECT || STAGES == 2, "through registers: two stages");
+template <int TW, int TX, int WW, int WX, int STAGES, bool ROWS, bool WIDE>
+__global__ __launch_bounds__(TW / WW * (TX / WX) * 64, WX == 128 ? 1 : 2) void k_tiles8(Args a) {
+  typedef Tile8<TW, TX, WW, WX, STAGES, ROWS, WIDE> T;
   __shared__ __attribute__((aligned(16))) char lds[T::LDS];
   int64_t ty, tx;
   place_tile(blockIdx.x, (a.y.rows + TX - 1) / TX, (a.y.cols + TW - 1) / TW, 8, ty, tx);
   const int64_t s0 = blockIdx.y * a.per, s1 = s0 + a.per < a.steps ? s0 + a.per : a.steps;
   f32x16 acc[T::MT][T::NT];
   T::run(a, tx * TW, ty * TX, s0, s1, lds, acc);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int ww = wave / (TX / WX), wx = wave % (TX / WX);
-#pragma unroll
-  for (int j = 0; j < T::NT; ++j) {
-    const int64_t row = ty * TX + wx * WX + j * 32 + (lane & 31);
-#pragma unroll
-    for (int i = 0; i < T::MT; ++i)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const float v[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-        store_y(a, row, tx * TW + ww * WW + i * 32 + 8 * q + 4 * (lane >> 5), blockIdx.y, v);
-      }
-  }
+  // Each wavefront's results through LDS, so that rows of Y are written in runs of
+  // its WW columns.
+  const bool part = a.part != nullptr;
+  const int type = part ? (int)DT_F32 : a.y.type;
+  char* const to = static_cast<char*>(part ? (void*)a.part : a.y.data);
+  const int64_t ld = part ? a.y.cols : a.y.ld, r0 = ty * TX, c0 = tx * TW;
+  const int64_t first = part ? (int64_t)blockIdx.y * a.y.rows : 0;
+  __syncthreads();  // the stages' LDS changes its use
+  if constexpr (TW < 256)  // (the largest tiles have 16-bit results and share no k)
+    if (type == DT_F32) return T::template write<DT_F32>(acc, to, first, ld, r0, c0, a.y.rows, a.y.cols, lds);
+  if (type == DT_BF16) T::template write<DT_BF16>(acc, to, first, ld, r0, c0, a.y.rows, a.y.cols, lds);
+  else T::template write<DT_F16>(acc, to, first, ld, r0, c0, a.y.rows, a.y.cols, lds);
 }
 
 // Y: the splits' sums, added in their order.
@@ -436,7 +488,7 @@ __global__ __launch_bounds__(64 * ROW_WAVES) void k_rows8(Args a) {
     for (int u = 0; u < ROW_WAVES; ++u)
 #pragma unroll
       for (int q = 0; q < 4; ++q) v[q] += sums[u][t][l][q];
-    store_y(a, t * 16 + (l & 15), w0 + (l >> 4) * 4, 0, v);
+    store_y(a, t * 16 + (l & 15), w0 + (l >> 4) * 4, v);
   }
 }
 
@@ -444,6 +496,15 @@ __global__ __launch_bounds__(256) void k_zero8(Mat y) {
   const int64_t values = y.rows * y.cols;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < values; i += (int64_t)gridDim.x * 256)
     store1(y.data, y.type, i / y.cols * y.ld + i % y.cols, 0.f);
+}
+
+// Rows of codes as chunks of 16 bytes, zeros past the last column.
+__global__ __launch_bounds__(256) void k_pack8(Held h, uint8_t* to, int64_t chunks) {
+  const int64_t total = h.rows * chunks;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / chunks, c = i % chunks * 16;
+    reinterpret_cast<i32x4*>(to)[i] = load16(h.codes + r * h.ld + c, h.cols - c);
+  }
 }
 
 // What a product of these sizes is made with.
@@ -454,11 +515,11 @@ struct Way {
 
 constexpr int64_t kPartBytes = int64_t(64) << 20;
 
-Way way_of(int64_t m, int64_t n, int64_t k, bool direct, bool wide) {
+Way way_of(int64_t m, int64_t n, int64_t k, bool rows, bool wide) {
   const int64_t steps = (k + 127) / 128;
   if (m <= kFewRows) return {0, 1, steps};
   const auto tiles = [&](int64_t t) { return (m + t - 1) / t * ((n + t - 1) / t); };
-  if (direct && !wide && tiles(256) >= 200) return {256, 1, steps};
+  if (!rows && !wide && tiles(256) >= 200) return {256, 1, steps};
   const int tile = tiles(128) >= 256 || steps >= 64 ? 128 : 64;
   const int64_t want = 512 / tiles(tile);
   int64_t splits = std::max<int64_t>(1, std::min({want, steps / 8, kPartBytes / (m * n * 4)}));
@@ -467,38 +528,56 @@ Way way_of(int64_t m, int64_t n, int64_t k, bool direct, bool wide) {
   return {tile, splits, per};
 }
 
-template <int TW, int TX, int WW, int WX, int STAGES, bool DIRECT, bool WIDE>
+template <int TW, int TX, int WW, int WX, int STAGES, bool ROWS, bool WIDE>
 hipError_t launch(const Args& a, const Way& w, hipStream_t s) {
   const int64_t tiles = (a.y.rows + TX - 1) / TX * ((a.y.cols + TW - 1) / TW);
   const dim3 grid((unsigned)tiles, (unsigned)w.splits);
-  constexpr int threads = TW / WW * (TX / WX) * 64;
-  if (a.w.tile == 1) k_tiles8<TW, TX, WW, WX, STAGES, true, DIRECT, WIDE><<<grid, threads, 0, s>>>(a);
-  else k_tiles8<TW, TX, WW, WX, STAGES, false, DIRECT, WIDE><<<grid, threads, 0, s>>>(a);
+  k_tiles8<TW, TX, WW, WX, STAGES, ROWS, WIDE><<<grid, TW / WW * (TX / WX) * 64, 0, s>>>(a);
   return hipGetLastError();
 }
 
-template <bool WIDE>
-hipError_t launch(const Args& a, const Way& w, bool direct, hipStream_t s) {
-  if (w.tile == 128)
-    return direct ? launch<128, 128, 64, 64, 2, true, WIDE>(a, w, s) : launch<128, 128, 64, 64, 2, false, WIDE>(a, w, s);
-  return direct ? launch<64, 64, 32, 32, 3, true, WIDE>(a, w, s) : launch<64, 64, 32, 32, 2, false, WIDE>(a, w, s);
+template <bool ROWS, bool WIDE>
+hipError_t launch(const Args& a, const Way& w, hipStream_t s) {
+  if constexpr (!ROWS && !WIDE)
+    if (w.tile == 256) return launch<256, 256, 128, 64, 2, ROWS, WIDE>(a, w, s);
+  if (w.tile == 128) return launch<128, 128, 64, 64, 2, ROWS, WIDE>(a, w, s);
+  return launch<64, 64, 32, 32, 3, ROWS, WIDE>(a, w, s);
 }
 
-// Rows that are chunks of 16 bytes.
+template <int XT>
+hipError_t launch_rows(const Args& a, hipStream_t s) {
+  const dim3 grid((unsigned)((a.y.cols + 15) / 16));
+  if (a.w.tile == 1) k_rows8<XT, true><<<grid, 64 * ROW_WAVES, 0, s>>>(a);
+  else k_rows8<XT, false><<<grid, 64 * ROW_WAVES, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+// Whether h's rows are chunks of 16 bytes, and the bytes of a copy that is.
 bool chunks(const Held& h) {
   return reinterpret_cast<uintptr_t>(h.codes) % 16 == 0 && h.cols % 16 == 0 && (h.ld % 16 == 0 || h.rows == 1);
+}
+int64_t packed_bytes(const Held& h) { return chunks(h) ? 0 : h.rows * ((h.cols + 15) / 16 * 16); }
+
+// The copy's place, where there is one, and the next place in the workspace.
+hipError_t pack(Held& h, char*& ws, hipStream_t s) {
+  const int64_t bytes = packed_bytes(h);
+  if (bytes == 0) return hipSuccess;
+  uint8_t* const to = reinterpret_cast<uint8_t*>(ws);
+  k_pack8<<<(unsigned)std::min<int64_t>((bytes / 16 + 255) / 256, 1 << 16), 256, 0, s>>>(h, to, bytes / 16 / h.rows);
+  h.codes = to;
+  h.ld = bytes / h.rows;
+  ws += bytes;
+  return hipGetLastError();
 }
 
 }  // namespace
 
-int64_t matmul8_workspace(int64_t m, int64_t n, int64_t k) {
+int64_t matmul8_workspace(const Held& A, const Held& B, int type) {
+  const int64_t m = A.rows, n = B.rows, k = A.cols;
   if (m == 0 || n == 0 || k == 0) return 0;
-  int64_t most = 0;
-  for (int i = 0; i < 4; ++i) {
-    const Way w = way_of(m, n, k, i & 1, i & 2);
-    if (w.splits > 1) most = std::max(most, w.splits * m * n * (int64_t)sizeof(float));
-  }
-  return most;
+  const Way w = way_of(m, n, k, B.tile == 1, type == DT_F32);
+  const int64_t part = w.splits > 1 ? (w.splits * m * n * (int64_t)sizeof(float) + 15) / 16 * 16 : 0;
+  return part + (w.tile ? packed_bytes(A) + packed_bytes(B) : 0);
 }
 
 hipError_t matmul8(const Held& A, const Held& B, const Mat& Y, void* ws, hipStream_t s) {
@@ -508,27 +587,21 @@ hipError_t matmul8(const Held& A, const Held& B, const Mat& Y, void* ws, hipStre
     k_zero8<<<(unsigned)std::min<int64_t>((m * n + 255) / 256, 1 << 16), 256, 0, s>>>(Y);
     return hipGetLastError();
   }
-  const bool direct = chunks(A) && chunks(B);
-  const bool wide = Y.type == DT_F32;
-  const Way w = way_of(m, n, k, direct, wide);
-  Args a{A, B, Y, w.splits > 1 ? static_cast<float*>(ws) : nullptr, k, (k + 127) / 128, w.per};
-  if (w.tile == 0) {
-    const dim3 grid((unsigned)((n + 15) / 16));
-    const int xt = m <= 16 ? 1 : m <= 32 ? 2 : 4;
-    if (B.tile == 1) {
-      if (xt == 1) k_rows8<1, true><<<grid, 64 * ROW_WAVES, 0, s>>>(a);
-      else if (xt == 2) k_rows8<2, true><<<grid, 64 * ROW_WAVES, 0, s>>>(a);
-      else k_rows8<4, true><<<grid, 64 * ROW_WAVES, 0, s>>>(a);
-    } else {
-      if (xt == 1) k_rows8<1, false><<<grid, 64 * ROW_WAVES, 0, s>>>(a);
-      else if (xt == 2) k_rows8<2, false><<<grid, 64 * ROW_WAVES, 0, s>>>(a);
-      else k_rows8<4, false><<<grid, 64 * ROW_WAVES, 0, s>>>(a);
-    }
-    return hipGetLastError();
+  const bool rows = B.tile == 1, wide = Y.type == DT_F32;
+  const Way w = way_of(m, n, k, rows, wide);
+  Args a{A, B, Y, nullptr, k, (k + 127) / 128, w.per};
+  if (w.tile == 0) return m <= 16 ? launch_rows<1>(a, s) : m <= 32 ? launch_rows<2>(a, s) : launch_rows<4>(a, s);
+  char* place = static_cast<char*>(ws);
+  if (w.splits > 1) {
+    a.part = static_cast<float*>(ws);
+    place += (w.splits * m * n * (int64_t)sizeof(float) + 15) / 16 * 16;
   }
-  hipError_t e;
-  if (w.tile == 256) e = launch<256, 256, 128, 64, 2, true, false>(a, w, s);
-  else e = wide ? launch<true>(a, w, direct, s) : launch<false>(a, w, direct, s);
+  hipError_t e = pack(a.x, place, s);
+  if (e == hipSuccess) e = pack(a.w, place, s);
+  if (e != hipSuccess) return e;
+  a.k = (k + 15) / 16 * 16;
+  if (rows) e = wide ? launch<true, true>(a, w, s) : launch<true, false>(a, w, s);
+  else e = wide ? launch<false, true>(a, w, s) : launch<false, false>(a, w, s);
   if (e != hipSuccess || w.splits == 1) return e;
   k_join8<<<(unsigned)std::min<int64_t>((m * n + 1023) / 1024, 2048), 256, 0, s>>>(Y, a.part, (int)w.splits);
   return hipGetLastError();
