@@ -68,10 +68,44 @@ __device__ __forceinline__ double block_sum(double v, double* buf) {
   return v;
 }
 
-template <int PER, bool ONCE>
-__device__ __forceinline__ void load_chunk(const GradTensor& t, int64_t at, int64_t end, Raw8 (&r)[PER]) {
+// A number of values as far as it matters for one chunk.
+__device__ __forceinline__ int left(int64_t n) { return (int)(n < -(1 << 30) ? -(1 << 30) : n > (1 << 30) ? 1 << 30 : n); }
+
+// WHOLE: the workgroup's chunks are all there.
+template <int PER, int T, bool WHOLE>
+__device__ __forceinline__ void load_chunk(const GradTensor& t, int64_t at, int64_t end, Raw<T> (&r)[PER]) {
 #pragma unroll
-  for (int q = 0; q < PER; ++q) load_raw<ONCE>(t.g, t.gt, at + q * BLOCK * 8, end - at - q * BLOCK * 8, r[q]);
+  for (int q = 0; q < PER; ++q)
+    load_raw<(PER > 1)>(t.g, type_of<T>(t.gt), at + q * BLOCK * 8, WHOLE ? 8 : left(end - at - q * BLOCK * 8),
+                        T == MIXED ? left(t.n) : 8, r[q]);
+}
+
+template <int T, bool WHOLE>
+__device__ __forceinline__ void values_of(const GradTensor& t, int64_t have, Raw<T>& r, float (&x)[8]) {
+  if constexpr (!WHOLE) settle(r, type_of<T>(t.gt), left(have), T == MIXED ? left(t.n) : 8);
+  convert(r, type_of<T>(t.gt), x);
+}
+
+template <int PER, int T, bool WHOLE>
+__device__ __forceinline__ void add_squares(const GradTensor& t, int64_t at, int64_t end, double& sum) {
+  Raw<T> r[PER];
+  load_chunk<PER, T, WHOLE>(t, at, end, r);
+#pragma unroll
+  for (int q = 0; q < PER; ++q) {
+    float x[8];
+    values_of<T, WHOLE>(t, end - at - q * BLOCK * 8, r[q], x);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum += (double)x[j] * (double)x[j];
+  }
+}
+
+// Squares of [begin, end) of a tensor.
+template <int PER, int T>
+__device__ __forceinline__ double squares(const GradTensor& t, int64_t begin, int64_t end) {
+  double sum = 0.0;
+  for (; begin + chunk_of(PER) <= end; begin += chunk_of(PER)) add_squares<PER, T, T != MIXED>(t, begin + threadIdx.x * 8, end, sum);
+  if (begin < end) add_squares<PER, T, false>(t, begin + threadIdx.x * 8, end, sum);
+  return sum;
 }
 
 template <int PER>
@@ -81,18 +115,11 @@ __global__ __launch_bounds__(BLOCK) void k_grad_squares(Table tab, double* part)
   const GradTensor& t = tab.t[k];
   const int64_t begin = (int64_t)(blockIdx.x - tab.first[k]) * tab.span;
   const int64_t end = begin + tab.span < t.n ? begin + tab.span : t.n;
-  double sum = 0.0;
-  for (int64_t at = begin + threadIdx.x * 8; at < end; at += chunk_of(PER)) {
-    Raw8 r[PER];
-    load_chunk<PER, (PER > 1)>(t, at, end, r);
-#pragma unroll
-    for (int q = 0; q < PER; ++q) {
-      float x[8];
-      convert(r[q], t.gt, x);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) sum += (double)x[j] * (double)x[j];
-    }
-  }
+  double sum;
+  if (t.n < 8) sum = squares<PER, MIXED>(t, begin, end);
+  else if (t.gt == DT_F32) sum = squares<PER, DT_F32>(t, begin, end);
+  else if (t.gt == DT_BF16) sum = squares<PER, DT_BF16>(t, begin, end);
+  else sum = squares<PER, DT_F16>(t, begin, end);
   sum = block_sum(sum, buf);
   if (threadIdx.x == 0) part[blockIdx.x] = sum;
 }
@@ -119,8 +146,34 @@ __global__ __launch_bounds__(BLOCK) void k_grad_norm(Final f) {
   }
 }
 
-// out = g * scale, scale from the partial sums or (parts = 0) from memory.  The
-// first gradients are asked for before it.
+// The first chunk of [begin, end) is asked for; then the factor is made by `scale`, which
+// returns whether it has to be applied; then the rest.  T: the type of g and out (or MIXED).
+template <int PER, int T, typename F>
+__device__ __forceinline__ void scale_all(const GradTensor& t, int64_t begin, int64_t end, F scale) {
+  int64_t at = begin + threadIdx.x * 8;
+  Raw<T> r[PER];
+  load_chunk<PER, T, false>(t, at, end, r);
+  float by;
+  if (!scale(by)) return;
+  while (true) {
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+      float x[8];
+      values_of<T, false>(t, end - at - q * BLOCK * 8, r[q], x);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] *= by;
+      Raw<T> p;
+      pack(x, type_of<T>(t.ot), p);
+      store_raw<(PER > 1)>(t.out, type_of<T>(t.ot), at + q * BLOCK * 8, end - at - q * BLOCK * 8, p);
+    }
+    begin += chunk_of(PER);
+    if (begin >= end) return;
+    at += chunk_of(PER);
+    load_chunk<PER, T, false>(t, at, end, r);
+  }
+}
+
+// out = g * scale, scale from the partial sums or (parts = 0) from memory.
 template <int PER>
 __global__ __launch_bounds__(BLOCK) void k_grad_scale(Table tab, Final f) {
   __shared__ double buf[BLOCK / 64];
@@ -128,32 +181,20 @@ __global__ __launch_bounds__(BLOCK) void k_grad_scale(Table tab, Final f) {
   const GradTensor& t = tab.t[k];
   const int64_t begin = (int64_t)(blockIdx.x - tab.first[k]) * tab.span;
   const int64_t end = begin + tab.span < t.n ? begin + tab.span : t.n;
-  int64_t at = begin + threadIdx.x * 8;
-  Raw8 r[PER];
-  load_chunk<PER, (PER > 1)>(t, at, end, r);
-  float scale;
-  if (f.parts > 0) {
-    const double sum = add_parts(f, buf);
-    scale = scale_of(sum, f.max_norm);
-    if (f.norm && blockIdx.x == 0 && threadIdx.x == 0) *f.norm = (float)sqrt(sum);
-  } else {
-    scale = *f.scale;
-  }
-  if (scale == 1.f && t.out == t.g) return;
-  while (at < end) {
-#pragma unroll
-    for (int q = 0; q < PER; ++q) {
-      float x[8];
-      convert(r[q], t.gt, x);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] *= scale;
-      Raw8 p;
-      pack(x, t.ot, p);
-      store_raw<(PER > 1)>(t.out, t.ot, at + q * BLOCK * 8, end - at - q * BLOCK * 8, p);
+  const auto scale = [&](float& by) {
+    if (f.parts > 0) {
+      const double sum = add_parts(f, buf);
+      by = scale_of(sum, f.max_norm);
+      if (f.norm && blockIdx.x == 0 && threadIdx.x == 0) *f.norm = (float)sqrt(sum);
+    } else {
+      by = *f.scale;
     }
-    at += chunk_of(PER);
-    if (at < end) load_chunk<PER, (PER > 1)>(t, at, end, r);
-  }
+    return by != 1.f || t.out != t.g;
+  };
+  if (t.n < 8 || t.gt != t.ot) scale_all<PER, MIXED>(t, begin, end, scale);
+  else if (t.gt == DT_F32) scale_all<PER, DT_F32>(t, begin, end, scale);
+  else if (t.gt == DT_BF16) scale_all<PER, DT_BF16>(t, begin, end, scale);
+  else scale_all<PER, DT_F16>(t, begin, end, scale);
 }
 
 // Values a workgroup goes through: at most kGroups workgroups, and one for each tensor.

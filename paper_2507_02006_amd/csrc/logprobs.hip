@@ -18,6 +18,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "layers.h"
 #include "rows8.h"
@@ -137,22 +138,24 @@ __device__ __forceinline__ void store_top(const Args& a, int64_t row, int at, fl
 // ------------------------------------------------------------- short rows
 
 // L lanes hold a row, 8 E scores a lane: chunk e is columns (e L + lane) 8 on.
-template <int L, int E>
+template <int L, int E, int T>
 __global__ __launch_bounds__(BLOCK) void k_logp_short(Args a) {
+  const int zt = type_of<T>(a.zt), n8 = row_of<T>(a.v);
   constexpr int TEAMS = BLOCK / L;
   const int lane = threadIdx.x % L;
   for (int64_t row = (int64_t)blockIdx.x * TEAMS + threadIdx.x / L; row < a.t; row += (int64_t)gridDim.x * TEAMS) {
-    Raw8 r[E];
+    Raw<T> r[E];
     float z[E][8];
     Stats t = EMPTY;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const int c = (e * L + lane) * 8;
-      load_raw(a.z, a.zt, row * a.ldz + c, a.v - c, r[e]);
+      load_raw(a.z, zt, row * a.ldz + c, a.v - c, n8, r[e]);
     }
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      convert(r[e], a.zt, z[e]);
+      settle(r[e], zt, a.v - (e * L + lane) * 8, n8);
+      convert(r[e], zt, z[e]);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         if ((e * L + lane) * 8 + k >= a.v) z[e][k] = -__builtin_inff();
@@ -284,8 +287,9 @@ struct List {
 };
 
 // A workgroup streams columns [part * per, + per) of a row.
-template <bool TOP>
+template <bool TOP, int T>
 __global__ __launch_bounds__(BLOCK) void k_logp_long(Args a) {
+  const int zt = type_of<T>(a.zt), n8 = row_of<T>(a.v);
   constexpr int WAVES = BLOCK / 64;
   __shared__ Stats stats[WAVES];
   __shared__ uint64_t lists[TOP ? WAVES * 64 : 1];
@@ -295,14 +299,16 @@ __global__ __launch_bounds__(BLOCK) void k_logp_long(Args a) {
   const int64_t base = row * a.ldz;
   Stats t = EMPTY;
   List list;
-  Raw8 next;
-  load_raw<true>(a.z, a.zt, base + begin + (int)threadIdx.x * 8, end - begin - (int)threadIdx.x * 8, next);
+  Raw<T> next;
+  // (a chunk past the row's end is moved back into the row, one past the part's not)
+  load_raw<true>(a.z, zt, base + begin + (int)threadIdx.x * 8, a.v - begin - (int)threadIdx.x * 8, n8, next);
   for (int at = begin; at < end; at += BLOCK * 8) {
-    const Raw8 now = next;
+    Raw<T> now = next;
     const int c = at + threadIdx.x * 8;
-    load_raw<true>(a.z, a.zt, base + c + BLOCK * 8, (int64_t)end - c - BLOCK * 8, next);
+    load_raw<true>(a.z, zt, base + c + BLOCK * 8, a.v - c - BLOCK * 8, n8, next);
     float z[8];
-    convert(now, a.zt, z);
+    settle(now, zt, a.v - c, n8);
+    convert(now, zt, z);
     if (c + 8 > end)
 #pragma unroll
       for (int k = 0; k < 8; ++k)
@@ -374,9 +380,11 @@ struct Back {
 };
 
 // L lanes a row (a workgroup for long rows, blockIdx.y of gridDim.y runs of it).
-template <int L, bool ONCE>
+// T: the type of Z and dZ (or MIXED).
+template <int L, int T>
 __global__ __launch_bounds__(BLOCK) void k_logp_back(Back a) {
   constexpr int TEAMS = BLOCK / L;
+  const int zt = type_of<T>(a.zt), dt = type_of<T>(a.dt), n8 = row_of<T>(a.v);
   const int lane = threadIdx.x % L;
   const int64_t first = ((int64_t)blockIdx.y * L + lane) * 8, step = (int64_t)gridDim.y * L * 8;
   for (int64_t row = (int64_t)blockIdx.x * TEAMS + threadIdx.x / L; row < a.t; row += (int64_t)gridDim.x * TEAMS) {
@@ -389,13 +397,14 @@ __global__ __launch_bounds__(BLOCK) void k_logp_back(Back a) {
       else y = -1;
     }
     const bool none = lse == -__builtin_inff();
-    Raw8 next;
-    load_raw<ONCE>(a.z, a.zt, row * a.ldz + first, a.v - first, next);
+    Raw<T> next;
+    load_raw<T != MIXED>(a.z, zt, row * a.ldz + first, (int)(a.v - first), n8, next);
     for (int64_t c = first; c < a.v; c += step) {
-      Raw8 r = next;
-      load_raw<ONCE>(a.z, a.zt, row * a.ldz + c + step, a.v - c - step, next);
+      Raw<T> r = next;
+      load_raw<T != MIXED>(a.z, zt, row * a.ldz + c + step, (int)(a.v - c - step), n8, next);
       float z[8];
-      convert(r, a.zt, z);
+      settle(r, zt, (int)(a.v - c), n8);
+      convert(r, zt, z);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         const float lp = z[k] - lse, p = exp_of(lp);
@@ -403,13 +412,22 @@ __global__ __launch_bounds__(BLOCK) void k_logp_back(Back a) {
         d = c + k == y ? d + da : d;
         z[k] = none ? 0.f : d;
       }
-      pack(z, a.dt, r);
-      store_raw<ONCE>(a.dz, a.dt, row * a.ldd + c, a.v - c, r);
+      pack(z, dt, r);
+      store_raw<T != MIXED>(a.dz, dt, row * a.ldd + c, a.v - c, r);
     }
   }
 }
 
 constexpr int64_t kShortCols = 2048;
+
+// f(type) with the type as a constant (rows of fewer than eight scores: MIXED).
+template <typename F>
+void with_type(int t, int64_t v, F f) {
+  if (v < 8 || t == MIXED) f(std::integral_constant<int, MIXED>());
+  else if (t == DT_F32) f(std::integral_constant<int, DT_F32>());
+  else if (t == DT_BF16) f(std::integral_constant<int, DT_BF16>());
+  else f(std::integral_constant<int, DT_F16>());
+}
 
 // Workgroups that share a row: where rows are fewer than what fills the chip, as
 // many as have a step of columns each, of which the lists can be joined.
@@ -443,13 +461,18 @@ hipError_t log_probs(const LogProbs& x, void* ws, hipStream_t s) {
     const int64_t rows = BLOCK / lanes;
     return dim3((unsigned)std::min<int64_t>((a.t + rows - 1) / rows, 1 << 20));
   };
-  if (a.v <= 64) k_logp_short<8, 1><<<grid(8), BLOCK, 0, s>>>(a);
-  else if (a.v <= 128) k_logp_short<16, 1><<<grid(16), BLOCK, 0, s>>>(a);
-  else if (a.v <= 256) k_logp_short<32, 1><<<grid(32), BLOCK, 0, s>>>(a);
-  else if (a.v <= 512) k_logp_short<64, 1><<<grid(64), BLOCK, 0, s>>>(a);
-  else if (a.v <= 1024) k_logp_short<64, 2><<<grid(64), BLOCK, 0, s>>>(a);
-  else if (a.v <= kShortCols) k_logp_short<64, 4><<<grid(64), BLOCK, 0, s>>>(a);
-  if (a.v <= kShortCols) return hipGetLastError();
+  if (a.v <= kShortCols) {
+    with_type(a.zt, a.v, [&](auto type) {
+      constexpr int T = decltype(type)::value;
+      if (a.v <= 64) k_logp_short<8, 1, T><<<grid(8), BLOCK, 0, s>>>(a);
+      else if (a.v <= 128) k_logp_short<16, 1, T><<<grid(16), BLOCK, 0, s>>>(a);
+      else if (a.v <= 256) k_logp_short<32, 1, T><<<grid(32), BLOCK, 0, s>>>(a);
+      else if (a.v <= 512) k_logp_short<64, 1, T><<<grid(64), BLOCK, 0, s>>>(a);
+      else if (a.v <= 1024) k_logp_short<64, 2, T><<<grid(64), BLOCK, 0, s>>>(a);
+      else k_logp_short<64, 4, T><<<grid(64), BLOCK, 0, s>>>(a);
+    });
+    return hipGetLastError();
+  }
   a.parts = parts_of(a.t, a.v, a.top);
   const int64_t steps = ((int64_t)a.v + BLOCK * 8 - 1) / (BLOCK * 8);
   a.per = (int)((steps + a.parts - 1) / a.parts * (BLOCK * 8));
@@ -471,8 +494,11 @@ hipError_t log_probs(const LogProbs& x, void* ws, hipStream_t s) {
       if (a.top_index) b.top_index += r0 * a.top;
     }
     const dim3 g((unsigned)(b.t * b.parts));
-    if (a.top > 0) k_logp_long<true><<<g, BLOCK, 0, s>>>(b);
-    else k_logp_long<false><<<g, BLOCK, 0, s>>>(b);
+    with_type(a.zt, a.v, [&](auto type) {
+      constexpr int T = decltype(type)::value;
+      if (a.top > 0) k_logp_long<true, T><<<g, BLOCK, 0, s>>>(b);
+      else k_logp_long<false, T><<<g, BLOCK, 0, s>>>(b);
+    });
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -484,23 +510,19 @@ hipError_t log_probs_backward(const Mat& Z, const void* labels, int labels_i64, 
                               const float* dlogp, const float* dentropy, const Mat& dZ, hipStream_t s) {
   if (Z.rows == 0 || Z.cols == 0) return hipSuccess;
   Back a{Z.data, Z.ld, Z.type, dZ.data, dZ.ld, dZ.type, Z.rows, (int)Z.cols, labels, labels_i64, lse, entropy, dlogp, dentropy};
-  const bool once = Z.rows * Z.cols * dtype_bytes(Z.type) > (int64_t(32) << 20);
-  const auto go = [&](auto wide, auto past, int lanes, int64_t shares) {
-    const int64_t rows = BLOCK / lanes;
+  const auto go = [&](auto wide, auto type, int64_t shares) {
+    constexpr int L = decltype(wide)::value;
+    const int64_t rows = BLOCK / L;
     const dim3 g((unsigned)std::min<int64_t>((a.t + rows - 1) / rows, 1 << 20), (unsigned)shares);
-    k_logp_back<decltype(wide)::value, decltype(past)::value><<<g, BLOCK, 0, s>>>(a);
+    k_logp_back<L, decltype(type)::value><<<g, BLOCK, 0, s>>>(a);
   };
-  const auto pick = [&](auto past) {
-    if (a.v <= 64) go(std::integral_constant<int, 8>(), past, 8, 1);
-    else if (a.v <= 128) go(std::integral_constant<int, 16>(), past, 16, 1);
-    else if (a.v <= 512) go(std::integral_constant<int, 64>(), past, 64, 1);
-    else {
-      const int64_t steps = ((int64_t)a.v + BLOCK * 8 - 1) / (BLOCK * 8);
-      go(std::integral_constant<int, BLOCK>(), past, BLOCK, std::min<int64_t>(steps, std::max<int64_t>(1, (4096 + a.t - 1) / a.t)));
-    }
-  };
-  if (once) pick(std::true_type());
-  else pick(std::false_type());
+  with_type(a.zt == a.dt ? a.zt : MIXED, a.v, [&](auto type) {
+    if (a.v <= 64) return go(std::integral_constant<int, 8>(), type, 1);
+    if (a.v <= 128) return go(std::integral_constant<int, 16>(), type, 1);
+    if (a.v <= 512) return go(std::integral_constant<int, 64>(), type, 1);
+    const int64_t steps = ((int64_t)a.v + BLOCK * 8 - 1) / (BLOCK * 8);
+    go(std::integral_constant<int, BLOCK>(), type, std::min<int64_t>(steps, std::max<int64_t>(1, (4096 + a.t - 1) / a.t)));
+  });
   return hipGetLastError();
 }
 

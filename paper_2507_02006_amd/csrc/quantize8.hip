@@ -15,6 +15,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "layers.h"
 #include "rows8.h"
@@ -31,8 +32,62 @@ struct Args {
   Held q, t;
 };
 
-__device__ __forceinline__ float magnitude(const float (&x)[8]) {
-  float big = 0.f;
+// Magnitudes of a row's eight values as integers of the same order (signs cut
+// off): packed pairs of 16-bit ones, or eight of 32 bits.  What is not finite is
+// above all others.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
+template <bool HALF>
+struct Sizes {
+  uint32_t v[HALF ? 4 : 8] = {};
+
+  template <typename R>
+  __device__ __forceinline__ void add(const R& r) {
+    if constexpr (HALF) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        v[k] = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, v[k]),
+                                                                      __builtin_bit_cast(u16x2, r.lo[k] & 0x7fff7fffu)));
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        v[k] = max(v[k], r.lo[k] & 0x7fffffffu);
+        v[k + 4] = max(v[k + 4], r.hi[k] & 0x7fffffffu);
+      }
+    }
+  }
+  // value k's, as an integer
+  __device__ __forceinline__ uint32_t bits(int k) const {
+    if constexpr (HALF) return v[k / 2] >> (16 * (k & 1)) & 0xffffu;
+    else return v[k];
+  }
+  __device__ __forceinline__ uint32_t most() const {
+    uint32_t m = bits(0);
+#pragma unroll
+    for (int k = 1; k < 8; ++k) m = max(m, bits(k));
+    return m;
+  }
+};
+
+template <bool HALF>
+__device__ __forceinline__ bool is_finite(uint32_t bits, int t) {
+  return bits < (!HALF ? 0x7f800000u : t == DT_BF16 ? 0x7f80u : 0x7c00u);
+}
+template <bool HALF>
+__device__ __forceinline__ float size_of(uint32_t bits, int t) {
+  if constexpr (!HALF) return __uint_as_float(bits);
+  return t == DT_BF16 ? bf16_to_f32((uint16_t)bits) : f16_to_f32((uint16_t)bits);
+}
+
+// Largest finite magnitude of a row's eight values.
+template <bool HALF, typename R>
+__device__ __forceinline__ float magnitude(const R& r, int t) {
+  Sizes<HALF> z;
+  z.add(r);
+  const uint32_t most = z.most();
+  if (is_finite<HALF>(most, t)) return size_of<HALF>(most, t);
+  float x[8], big = 0.f;
+  convert(r, t, x);
 #pragma unroll
   for (int k = 0; k < 8; ++k) big = fmaxf(big, finite_abs(x[k]));
   return big;
@@ -44,9 +99,14 @@ __device__ __forceinline__ float max_over_rows(float v) {
   return fmaxf(v, __shfl_xor(v, 32));
 }
 
-// ROWS, COLUMNS: which orders are written; TILES: one scale a tile.
-template <bool ROWS, bool COLUMNS, bool TILES>
+// ROWS, COLUMNS: which orders are written; TILES: one scale a tile; T: X's
+// type.  A value that is not finite is NaN or an infinity after its product
+// with the inverse scale too, and the conversion makes both NaN.
+template <bool ROWS, bool COLUMNS, bool TILES, int T>
 __global__ __launch_bounds__(BLOCK) void k_quantize(Args a) {
+  typedef Raw<T> Raw;
+  constexpr bool HALF = T == DT_BF16 || T == DT_F16;
+  const int xt = T == MIXED ? (int)DT_F32 : T, n8 = row_of<T>((int)a.n);  // (MIXED: made fp32 below)
   __shared__ float big_of[BLOCK / 64][BLOCK8];
   __shared__ float inverse_of[BLOCK8];
   __shared__ uint64_t turned[COLUMNS ? BLOCK8 * 16 : 1];
@@ -55,21 +115,44 @@ __global__ __launch_bounds__(BLOCK) void k_quantize(Args a) {
   for (int64_t at = blockIdx.x; at < tiles; at += gridDim.x) {
     const int64_t r0 = at / wide * BLOCK8, c0 = at % wide * BLOCK8;
     const int64_t row = r0 + g * 8, col = c0 + j * 8;
-    Raw8 x[8];
+    Raw x[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) load_raw<true>(a.x, a.xt, (row + i) * a.ldx + col, row + i < a.m ? a.n - col : 0, x[i]);
-    float big[8] = {}, inv_tile = 0.f;
-    if constexpr (TILES || COLUMNS) {
+    for (int i = 0; i < 8; ++i)  // (rows past the last: the last again)
+      load_raw<true>(a.x, type_of<T>(a.xt), (row + i < a.m ? row + i : a.m - 1) * a.ldx + col, (int)(a.n - col), n8, x[i]);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 8; ++i) {
+      settle(x[i], type_of<T>(a.xt), (int)(a.n - col), n8);
+      if constexpr (T == MIXED) {
         float v[8];
         convert(x[i], a.xt, v);
+        pack(v, DT_F32, x[i]);
+      }
+      if (row + i >= a.m) x[i] = Raw{};
+    }
+    float big[8] = {}, inv_tile = 0.f;
+    if constexpr (TILES || COLUMNS) {
+      Sizes<HALF> z;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) big[k] = fmaxf(big[k], finite_abs(v[k]));
+      for (int i = 0; i < 8; ++i) z.add(x[i]);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) big[k] = size_of<HALF>(z.bits(k), xt);
+      if (!is_finite<HALF>(z.most(), xt)) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) big[k] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          float v[8];
+          convert(x[i], xt, v);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) big[k] = fmaxf(big[k], finite_abs(v[k]));
+        }
       }
     }
     if constexpr (TILES) {
-      float most = max_over_rows(group16_max_f32(magnitude(big)));
+      float most = big[0];
+#pragma unroll
+      for (int k = 1; k < 8; ++k) most = fmaxf(most, big[k]);
+      most = max_over_rows(group16_max_f32(most));
       if ((threadIdx.x & 63) == 0) big_of[wave][0] = most;
       __syncthreads();
       most = fmaxf(fmaxf(big_of[0][0], big_of[1][0]), fmaxf(big_of[2][0], big_of[3][0]));
@@ -96,18 +179,26 @@ __global__ __launch_bounds__(BLOCK) void k_quantize(Args a) {
       __syncthreads();
     }
     if constexpr (ROWS) {
+      // eight of the 16 lanes of a row make the quotients of its eight rows
+      float inverse = 0.f;
+      if constexpr (!TILES) {
+        float mine = 0.f, scale;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float most = group16_max_f32(magnitude<HALF>(x[i], xt));
+          mine = (j & 7) == i ? most : mine;
+        }
+        block_scale(mine, scale, inverse);
+        if (j < 8 && row + j < a.m) a.q.scales[(row + j) * a.q.lds + c0 / BLOCK8] = scale;
+      }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        float v[8], inv = inv_tile;
-        convert(x[i], a.xt, v);
-        if constexpr (!TILES) {
-          float scale;
-          block_scale(group16_max_f32(magnitude(v)), scale, inv);
-          if (j == 0 && row + i < a.m) a.q.scales[(row + i) * a.q.lds + c0 / BLOCK8] = scale;
-        }
+        float v[8];
+        convert(x[i], xt, v);
+        const float inv = TILES ? inv_tile : __shfl(inverse, (threadIdx.x & 48) + i);
         u32x2_el1 w;
-        w[0] = encode4(scaled(v[0], inv), scaled(v[1], inv), scaled(v[2], inv), scaled(v[3], inv));
-        w[1] = encode4(scaled(v[4], inv), scaled(v[5], inv), scaled(v[6], inv), scaled(v[7], inv));
+        w[0] = encode4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+        w[1] = encode4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv);
         if (row + i < a.m) {
           uint8_t* to = a.q.codes + (row + i) * a.q.ld + col;
           if (col + 8 <= a.n) {
@@ -127,11 +218,11 @@ __global__ __launch_bounds__(BLOCK) void k_quantize(Args a) {
       for (int h = 0; h < 2; ++h) {
         float v[4][8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) convert(x[h * 4 + i], a.xt, v[i]);
+        for (int i = 0; i < 4; ++i) convert(x[h * 4 + i], xt, v[i]);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
           const float inv = TILES ? inv_tile : inverse_of[j * 8 + k];
-          word[h][k] = encode4(scaled(v[0][k], inv), scaled(v[1][k], inv), scaled(v[2][k], inv), scaled(v[3][k], inv));
+          word[h][k] = encode4(v[0][k] * inv, v[1][k] * inv, v[2][k] * inv, v[3][k] * inv);
         }
       }
 #pragma unroll
@@ -166,16 +257,21 @@ hipError_t quantize8(const Mat& X, const Held& Q, const Held& Qt, hipStream_t s)
   const int64_t tiles = (X.rows + BLOCK8 - 1) / BLOCK8 * ((X.cols + BLOCK8 - 1) / BLOCK8);
   const dim3 grid((unsigned)std::min<int64_t>(tiles, 1 << 20));
   const bool many = (Q.codes ? Q.tile : Qt.tile) == BLOCK8;
-  if (Q.codes && Qt.codes) {
-    if (many) k_quantize<true, true, true><<<grid, BLOCK, 0, s>>>(a);
-    else k_quantize<true, true, false><<<grid, BLOCK, 0, s>>>(a);
-  } else if (Q.codes) {
-    if (many) k_quantize<true, false, true><<<grid, BLOCK, 0, s>>>(a);
-    else k_quantize<true, false, false><<<grid, BLOCK, 0, s>>>(a);
-  } else {
-    if (many) k_quantize<false, true, true><<<grid, BLOCK, 0, s>>>(a);
-    else k_quantize<false, true, false><<<grid, BLOCK, 0, s>>>(a);
-  }
+  const auto orders = [&](auto tiles, auto type) {
+    constexpr bool M = decltype(tiles)::value;
+    constexpr int T = decltype(type)::value;
+    if (Q.codes && Qt.codes) k_quantize<true, true, M, T><<<grid, BLOCK, 0, s>>>(a);
+    else if (Q.codes) k_quantize<true, false, M, T><<<grid, BLOCK, 0, s>>>(a);
+    else k_quantize<false, true, M, T><<<grid, BLOCK, 0, s>>>(a);
+  };
+  const auto typed = [&](auto tiles) {
+    if (X.cols < 8) orders(tiles, std::integral_constant<int, MIXED>());
+    else if (X.type == DT_F32) orders(tiles, std::integral_constant<int, DT_F32>());
+    else if (X.type == DT_BF16) orders(tiles, std::integral_constant<int, DT_BF16>());
+    else orders(tiles, std::integral_constant<int, DT_F16>());
+  };
+  if (many) typed(std::true_type());
+  else typed(std::false_type());
   return hipGetLastError();
 }
 

@@ -16,6 +16,8 @@
 #include "layers.h"
 
 #include <algorithm>
+#include <initializer_list>
+#include <type_traits>
 
 #include "rows8.h"
 
@@ -25,6 +27,9 @@ namespace {
 
 constexpr int TEAM_BLOCK = 256;    // threads of a workgroup of teams
 constexpr int MAX_BLOCK = 1024;    // threads of a workgroup that shares a row
+// Two kinds of those (L = 0 and 1 where a team has L lanes): up to 512 threads have
+// 256 registers each, 1024 have 128.
+constexpr int group_threads(int L) { return L == 1 ? MAX_BLOCK / 2 : MAX_BLOCK; }
 // Widest rows held in registers (1024 threads have 128 registers each).
 constexpr int64_t kRegisterCols = (int64_t)MAX_BLOCK * 2 * 8;
 
@@ -42,12 +47,12 @@ struct Args {
   int64_t m; int n; float eps, inv_n;
 };
 
-// Sum over a team, in every lane.  L = 0: over the workgroup, through `buf` (two
+// Sum over a team, in every lane.  L < 8: over the workgroup, through `buf` (two
 // halves used in turn, so one barrier a call is enough).
 template <int L>
 __device__ __forceinline__ float team_sum(float v, float* buf, int& turn) {
-  v = group_sum_f32<L == 0 ? 64 : L>(v);
-  if constexpr (L == 0) {
+  v = group_sum_f32<L < 8 ? 64 : L>(v);
+  if constexpr (L < 8) {
     const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     float* b = buf + (turn & 1) * (MAX_BLOCK / 64);
     turn ^= 1;
@@ -64,7 +69,7 @@ struct Team {
   int lane, W;
   int64_t first, step;
   __device__ Team() {
-    if constexpr (L == 0) {
+    if constexpr (L < 8) {
       lane = threadIdx.x; W = blockDim.x; first = blockIdx.x; step = gridDim.x;
     } else {
       constexpr int teams = TEAM_BLOCK / L;
@@ -76,10 +81,17 @@ struct Team {
   __device__ int col(int e) const { return (e * W + lane) * 8; }
 };
 
-template <int E, bool ONCE, typename T>
-__device__ __forceinline__ void load_row(const void* p, int t, int64_t at, int n, const T& tm, Raw8 (&x)[E]) {
+template <int T, int E, typename M, typename R>
+__device__ __forceinline__ void load_row(const void* p, int t, int64_t at, int n, const M& tm, R (&x)[E]) {
 #pragma unroll
-  for (int e = 0; e < E; ++e) load_raw<ONCE>(p, t, at + tm.col(e), n - tm.col(e), x[e]);
+  for (int e = 0; e < E; ++e) load_raw<T != MIXED>(p, type_of<T>(t), at + tm.col(e), n - tm.col(e), row_of<T>(n), x[e]);
+}
+
+// A lane's eight columns of a row in fp32 (zeros past the last).
+template <typename R>
+__device__ __forceinline__ void values_of(R& r, int t, int have, int n, float (&x)[8]) {
+  settle(r, t, have, n);
+  convert(r, t, x);
 }
 
 template <int E, typename T>
@@ -88,8 +100,8 @@ __device__ __forceinline__ void load_gamma(const Args& a, const T& tm, float (&g
   for (int e = 0; e < E; ++e) {
     if (a.gamma) {
       Raw8 r;
-      load_raw(a.gamma, a.wt, tm.col(e), a.n - tm.col(e), r);
-      convert(r, a.wt, g[e]);
+      load_raw(a.gamma, a.wt, tm.col(e), a.n - tm.col(e), a.n, r);
+      values_of(r, a.wt, a.n - tm.col(e), a.n, g[e]);
     } else {
 #pragma unroll
       for (int k = 0; k < 8; ++k) g[e][k] = 1.f;
@@ -119,30 +131,45 @@ __device__ __forceinline__ void store_codes(const Args& a, int64_t row, int c, c
   }
 }
 
-template <int L, int E, bool ONCE>
-__global__ __launch_bounds__(L == 0 ? MAX_BLOCK : TEAM_BLOCK) void k_rms_forward(Args a) {
-  __shared__ float buf[L == 0 ? 2 * (MAX_BLOCK / 64) : 1];
+// T: the type of X, R, S and Y (or MIXED).  The next row is asked for before this one
+// is used.
+template <int L, int E, int T, bool RESIDUAL, bool CODES>
+__global__ __launch_bounds__(L < 8 ? group_threads(L) : TEAM_BLOCK) void k_rms_forward(Args a) {
+  __shared__ float buf[L < 8 ? 2 * (MAX_BLOCK / 64) : 1];
   const Team<L> tm;
+  const int n = a.n, n8 = row_of<T>(n);
+  const bool residual = T == MIXED ? a.r != nullptr : RESIDUAL, codes = T == MIXED ? a.codes != nullptr : CODES;
   int turn = 0;
   float g[E][8];
+  Raw<T> xr[E], rr[E];
+  const auto load = [&](int64_t row) {  // (past the last row: the last again)
+    row = row < a.m ? row : a.m - 1;
+    load_row<T>(a.x, a.xt, row * a.ldx, n, tm, xr);
+    if (residual) load_row<T>(a.r, a.rt, row * a.ldr, n, tm, rr);
+  };
+  load(tm.first);
   load_gamma<E>(a, tm, g);
   for (int64_t row = tm.first; row < a.m; row += tm.step) {
-    Raw8 xr[E], rr[E];
-    load_row<E, ONCE>(a.x, a.xt, row * a.ldx, a.n, tm, xr);
-    if (a.r) load_row<E, ONCE>(a.r, a.rt, row * a.ldr, a.n, tm, rr);
     float x[E][8], sum = 0.f;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      convert(xr[e], a.xt, x[e]);
-      if (a.r) {
+      const int have = n - tm.col(e);
+      values_of(xr[e], type_of<T>(a.xt), have, n8, x[e]);
+      if (residual) {
         float r[8];
-        convert(rr[e], a.rt, r);
+        values_of(rr[e], type_of<T>(a.rt), have, n8, r);
 #pragma unroll
         for (int k = 0; k < 8; ++k) x[e][k] += r[k];
-        Raw8 p;
-        pack(x[e], a.st, p);
-        store_raw<ONCE>(a.s, a.st, row * a.lds + tm.col(e), a.n - tm.col(e), p);
-        convert(p, a.st, x[e]);  // the norm is that of what is stored
+      }
+    }
+    if constexpr (T != MIXED) load(row + tm.step);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      if (residual) {
+        Raw<T> p;
+        pack(x[e], type_of<T>(a.st), p);
+        store_raw<T != MIXED>(a.s, type_of<T>(a.st), row * a.lds + tm.col(e), n - tm.col(e), p);
+        convert(p, type_of<T>(a.st), x[e]);  // the norm is that of what is stored
       }
 #pragma unroll
       for (int k = 0; k < 8; ++k) sum += x[e][k] * x[e][k];
@@ -154,15 +181,16 @@ __global__ __launch_bounds__(L == 0 ? MAX_BLOCK : TEAM_BLOCK) void k_rms_forward
       for (int k = 0; k < 8; ++k) x[e][k] = x[e][k] * q * g[e][k];
       const int c = tm.col(e);
       if constexpr (L != 8)
-        if (a.codes) {
+        if (codes) {
           store_codes(a, row, c, x[e]);
           continue;
         }
-      Raw8 p;
-      pack(x[e], a.ot, p);
-      store_raw<ONCE>(a.out, a.ot, row * a.ldo + c, a.n - c, p);
+      Raw<T> p;
+      pack(x[e], type_of<T>(a.ot), p);
+      store_raw<T != MIXED>(a.out, type_of<T>(a.ot), row * a.ldo + c, n - c, p);
     }
     if (a.rstd && tm.lane == 0) a.rstd[row] = q;
+    if constexpr (T == MIXED) load(row + tm.step);
   }
 }
 
@@ -178,12 +206,12 @@ __global__ __launch_bounds__(MAX_BLOCK) void k_rms_forward_wide(Args a) {
       const int c = i * 8;
       Raw8 p;
       float x[8];
-      load_raw(a.x, a.xt, row * a.ldx + c, a.n - c, p);
-      convert(p, a.xt, x);
+      load_raw(a.x, a.xt, row * a.ldx + c, a.n - c, a.n, p);
+      values_of(p, a.xt, a.n - c, a.n, x);
       if (a.r) {
         float r[8];
-        load_raw(a.r, a.rt, row * a.ldr + c, a.n - c, p);
-        convert(p, a.rt, r);
+        load_raw(a.r, a.rt, row * a.ldr + c, a.n - c, a.n, p);
+        values_of(p, a.rt, a.n - c, a.n, r);
 #pragma unroll
         for (int k = 0; k < 8; ++k) x[k] += r[k];
         pack(x, a.st, p);
@@ -198,12 +226,13 @@ __global__ __launch_bounds__(MAX_BLOCK) void k_rms_forward_wide(Args a) {
       const int c = i * 8;
       Raw8 p;
       float x[8], g[8];
-      if (a.r) load_raw(a.s, a.st, row * a.lds + c, a.n - c, p);
-      else load_raw(a.x, a.xt, row * a.ldx + c, a.n - c, p);
-      convert(p, a.r ? a.st : a.xt, x);
+      // (a chunk past the row's end holds zeros, whatever its load brings)
+      if (a.r) load_raw(a.s, a.st, row * a.lds + c, a.n - c, a.n, p);
+      else load_raw(a.x, a.xt, row * a.ldx + c, a.n - c, a.n, p);
+      values_of(p, a.r ? a.st : a.xt, a.n - c, a.n, x);
       if (a.gamma) {
-        load_raw(a.gamma, a.wt, c, a.n - c, p);
-        convert(p, a.wt, g);
+        load_raw(a.gamma, a.wt, c, a.n - c, a.n, p);
+        values_of(p, a.wt, a.n - c, a.n, g);
       }
 #pragma unroll
       for (int k = 0; k < 8; ++k) x[k] = x[k] * q * (a.gamma ? g[k] : 1.f);
@@ -224,7 +253,7 @@ template <int L, int E>
 __device__ __forceinline__ void join_columns(float (&acc)[E][8], const Args& a, const Team<L>& tm, float* buf) {
   const int n = a.n;
   float* part = a.part ? a.part + (int64_t)blockIdx.x * n : nullptr;
-  if constexpr (L == 0) {
+  if constexpr (L < 8) {
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const int c = tm.col(e), t = part ? (int)DT_F32 : a.wt;
@@ -254,47 +283,78 @@ __device__ __forceinline__ void join_columns(float (&acc)[E][8], const Args& a, 
   }
 }
 
-template <int L, int E, bool ONCE>
-__global__ __launch_bounds__(L == 0 ? MAX_BLOCK : TEAM_BLOCK) void k_rms_backward(Args a) {
-  __shared__ float buf[L == 0 ? 2 * (MAX_BLOCK / 64) : (TEAM_BLOCK / 64) * L * E * 8];
+// T: the type of S, dY, dS and dX (or MIXED); PAST: dS is given.
+template <int L, int E, int T, bool PAST>
+__global__ __launch_bounds__(L < 8 ? group_threads(L) : TEAM_BLOCK) void k_rms_backward(Args a) {
+  __shared__ float buf[L < 8 ? 2 * (MAX_BLOCK / 64) : (TEAM_BLOCK / 64) * L * E * 8];
   const Team<L> tm;
+  const int n = a.n, n8 = row_of<T>(n);
+  const bool past = T == MIXED ? a.r && a.out : PAST;
   int turn = 0;
   float g[E][8], acc[E][8] = {};
+  Raw<T> xr[E], yr[E], sr[E];
+  float q = 0.f;
+  const auto load = [&](int64_t row) {  // (past the last row: the last again)
+    row = row < a.m ? row : a.m - 1;
+    load_row<T>(a.x, a.xt, row * a.ldx, n, tm, xr);
+    load_row<T>(a.dy, a.dyt, row * a.lddy, n, tm, yr);
+    q = a.crstd[row];
+  };
+  const auto load_past = [&](int64_t row) {
+    row = row < a.m ? row : a.m - 1;
+    if (past) load_row<T>(a.r, a.rt, row * a.ldr, n, tm, sr);
+  };
+  // the next row is asked for before this one is used (1024 threads have no
+  // registers for that)
+  constexpr bool EARLY = T != MIXED && L != 0;
+  if constexpr (EARLY) {
+    load(tm.first);
+    load_past(tm.first);
+  }
   load_gamma<E>(a, tm, g);
   for (int64_t row = tm.first; row < a.m; row += tm.step) {
-    Raw8 xr[E], yr[E], sr[E];
-    load_row<E, false>(a.x, a.xt, row * a.ldx, a.n, tm, xr);
-    load_row<E, false>(a.dy, a.dyt, row * a.lddy, a.n, tm, yr);
-    if (a.r && a.out) load_row<E, false>(a.r, a.rt, row * a.ldr, a.n, tm, sr);
-    const float q = a.crstd[row];
-    float x[E][8], dy[E][8], sum = 0.f;
+    float x[E][8], dy[E][8], ds[PAST || T == MIXED ? E : 1][8], sum = 0.f;
+    if constexpr (!EARLY) {
+      load(row);
+      load_past(row);
+    }
+    const float rq = q;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      convert(xr[e], a.xt, x[e]);
-      convert(yr[e], a.dyt, dy[e]);
+      const int have = n - tm.col(e);
+      values_of(xr[e], type_of<T>(a.xt), have, n8, x[e]);
+      values_of(yr[e], type_of<T>(a.dyt), have, n8, dy[e]);
+    }
+    if constexpr (EARLY) load(row + tm.step);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        x[e][k] *= q;
+        x[e][k] *= rq;
         acc[e][k] += dy[e][k] * x[e][k];
         dy[e][k] *= g[e][k];
         sum += dy[e][k] * x[e][k];
       }
     }
-    if (!a.out) continue;
-    const float mean = team_sum<L>(sum, buf, turn) * a.inv_n;
+    if (a.out) {
+      const float mean = team_sum<L>(sum, buf, turn) * a.inv_n;
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
+      for (int e = 0; e < E; ++e) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) dy[e][k] = q * (dy[e][k] - x[e][k] * mean);
-      if (a.r) {
-        float ds[8];
-        convert(sr[e], a.rt, ds);
+        for (int k = 0; k < 8; ++k) dy[e][k] = rq * (dy[e][k] - x[e][k] * mean);
+        if (past) {
+          values_of(sr[e], type_of<T>(a.rt), n - tm.col(e), n8, ds[PAST || T == MIXED ? e : 0]);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) dy[e][k] += ds[k];
+          for (int k = 0; k < 8; ++k) dy[e][k] += ds[PAST || T == MIXED ? e : 0][k];
+        }
       }
-      Raw8 p;
-      pack(dy[e], a.ot, p);
-      store_raw<ONCE>(a.out, a.ot, row * a.ldo + tm.col(e), a.n - tm.col(e), p);
+      if constexpr (EARLY) load_past(row + tm.step);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        Raw<T> p;
+        pack(dy[e], type_of<T>(a.ot), p);
+        store_raw<T != MIXED>(a.out, type_of<T>(a.ot), row * a.ldo + tm.col(e), n - tm.col(e), p);
+      }
     }
   }
   if (!a.dgamma) return;
@@ -365,48 +425,54 @@ struct Shape {
   int L, E, threads;
 };
 
-Shape shape_of(int64_t n, bool codes) {
+// (A wavefront that holds four chunks a lane has no registers left for the backward
+// pass's next row: two wavefronts share it.)
+Shape shape_of(int64_t n, bool codes, bool back) {
   const int64_t chunks = (n + 7) / 8;
   if (chunks <= 8 && !codes) return {8, 1, TEAM_BLOCK};
   if (chunks <= 16) return {16, 1, TEAM_BLOCK};
   if (chunks <= 32) return {32, 1, TEAM_BLOCK};
   if (chunks <= 64) return {64, 1, TEAM_BLOCK};
   if (chunks <= 128) return {64, 2, TEAM_BLOCK};
-  if (chunks <= 256) return {64, 4, TEAM_BLOCK};
-  return {0, 2, (int)(((chunks + 1) / 2 + 63) / 64 * 64)};
+  if (chunks <= 256 && !back) return {64, 4, TEAM_BLOCK};
+  const int threads = (int)(((chunks + 1) / 2 + 63) / 64 * 64);
+  return {threads <= MAX_BLOCK / 2 ? 1 : 0, 2, threads};
 }
 
-#define RMS_LAUNCH(kernel, L_, E_)                                             \
-  do {                                                                         \
-    if (once) kernel<L_, E_, true><<<g_, b_, 0, s>>>(a);                       \
-    else kernel<L_, E_, false><<<g_, b_, 0, s>>>(a);                           \
-  } while (0)
-#define RMS_DISPATCH(kernel, sh, grid)                                         \
-  do {                                                                         \
-    const dim3 g_((unsigned)(grid)), b_((unsigned)(sh).threads);               \
-    if ((sh).L == 8) RMS_LAUNCH(kernel, 8, 1);                                 \
-    else if ((sh).L == 16) RMS_LAUNCH(kernel, 16, 1);                          \
-    else if ((sh).L == 32) RMS_LAUNCH(kernel, 32, 1);                          \
-    else if ((sh).L == 64 && (sh).E == 1) RMS_LAUNCH(kernel, 64, 1);           \
-    else if ((sh).L == 64 && (sh).E == 2) RMS_LAUNCH(kernel, 64, 2);           \
-    else if ((sh).L == 64) RMS_LAUNCH(kernel, 64, 4);                          \
-    else RMS_LAUNCH(kernel, 0, 2);                                             \
-  } while (0)
+// One of a kernel's shapes; f(L, E) launches it.
+template <int V>
+using Int = std::integral_constant<int, V>;
+template <typename F>
+void with_shape(const Shape& sh, F f) {
+  if (sh.L == 8) f(Int<8>(), Int<1>());
+  else if (sh.L == 16) f(Int<16>(), Int<1>());
+  else if (sh.L == 32) f(Int<32>(), Int<1>());
+  else if (sh.L == 64 && sh.E == 1) f(Int<64>(), Int<1>());
+  else if (sh.L == 64 && sh.E == 2) f(Int<64>(), Int<2>());
+  else if (sh.L == 64) f(Int<64>(), Int<4>());
+  else if (sh.L == 1) f(Int<1>(), Int<2>());
+  else f(Int<0>(), Int<2>());
+}
 
-// An array that the second-level caches (8 x 4 MB) cannot keep is read and
-// written past them.
-bool too_large_to_keep(const Mat& m) { return m.rows * m.cols * dtype_bytes(m.type) > (int64_t(32) << 20); }
+// The type that all of these have, or MIXED.  (Rows of fewer than eight values are
+// left to the kernels for MIXED types.)
+int common_type(int64_t n, std::initializer_list<const Mat*> all) {
+  int t = -1;
+  for (const Mat* m : all)
+    if (m->data) t = t < 0 || t == m->type ? m->type : MIXED;
+  return n < 8 ? MIXED : t;
+}
 
-int64_t rows_at_once(const Shape& sh) { return sh.L == 0 ? 1 : TEAM_BLOCK / sh.L; }
+int64_t rows_at_once(const Shape& sh) { return sh.L < 8 ? 1 : TEAM_BLOCK / sh.L; }
 
 // Workgroups of the backward pass: what fills the chip, but eight rows a team
 // at least once there are many rows (each workgroup writes n partial sums).
 int64_t backward_groups(int64_t m, int64_t n) {
   if (n > kRegisterCols) return std::max<int64_t>(1, std::min<int64_t>(32, m / 8));
-  const Shape sh = shape_of(n, false);
+  const Shape sh = shape_of(n, false, true);
   const int64_t rows = rows_at_once(sh);
   const int64_t need = (m + rows - 1) / rows;
-  const int64_t fill = sh.L == 0 ? 256 * std::max(1, 1536 / sh.threads) : 1024;
+  const int64_t fill = sh.L < 8 ? 256 * std::max(1, 1536 / sh.threads) : 1024;
   return std::max<int64_t>(1, std::min({need, fill, std::max<int64_t>(256, need / 8)}));
 }
 
@@ -433,11 +499,33 @@ hipError_t rms_norm(const Mat& X, const Mat& R, const void* gamma, int wt, float
     k_rms_forward_wide<<<(unsigned)std::min<int64_t>(a.m, 1 << 20), MAX_BLOCK, 0, s>>>(a);
     return hipGetLastError();
   }
-  const Shape sh = shape_of(X.cols, a.codes != nullptr);
+  const Shape sh = shape_of(X.cols, a.codes != nullptr, false);
   const int64_t rows = rows_at_once(sh);
-  const int64_t grid = std::min<int64_t>((a.m + rows - 1) / rows, sh.L == 0 ? 256 * std::max(1, 2048 / sh.threads) : 2048);
-  const bool once = too_large_to_keep(X);
-  RMS_DISPATCH(k_rms_forward, sh, grid);
+  const int64_t grid = std::min<int64_t>((a.m + rows - 1) / rows, sh.L < 8 ? 256 * std::max(1, 2048 / sh.threads) : 2048);
+  // (eight lanes hold no block of 128 columns: their kernels have no codes)
+  const dim3 g((unsigned)grid), b((unsigned)sh.threads);
+  with_shape(sh, [&](auto l, auto e) {
+    constexpr int L = decltype(l)::value, E = decltype(e)::value;
+    const auto typed = [&](auto t) {
+      constexpr int T = decltype(t)::value;
+      if (a.codes) {
+        if constexpr (L != 8) {
+          if (a.r) k_rms_forward<L, E, T, true, true><<<g, b, 0, s>>>(a);
+          else k_rms_forward<L, E, T, false, true><<<g, b, 0, s>>>(a);
+        }
+      } else if (a.r) {
+        k_rms_forward<L, E, T, true, false><<<g, b, 0, s>>>(a);
+      } else {
+        k_rms_forward<L, E, T, false, false><<<g, b, 0, s>>>(a);
+      }
+    };
+    switch (common_type(a.n, {&X, &R, &S, &Y})) {
+      case DT_F32: return typed(Int<DT_F32>());
+      case DT_BF16: return typed(Int<DT_BF16>());
+      case DT_F16: return typed(Int<DT_F16>());
+      default: k_rms_forward<L, E, MIXED, false, false><<<g, b, 0, s>>>(a);
+    }
+  });
   return hipGetLastError();
 }
 
@@ -473,9 +561,22 @@ hipError_t rms_norm_backward(const Mat& dY, const Mat& S, const float* rstd, con
     if (dgamma) k_rms_columns_wide<<<dim3((unsigned)((n + TEAM_BLOCK - 1) / TEAM_BLOCK), (unsigned)groups), TEAM_BLOCK, 0, s>>>(a);
     if (a.out) k_rms_backward_wide<<<(unsigned)std::min<int64_t>(a.m, 1 << 20), MAX_BLOCK, 0, s>>>(a);
   } else {
-    const Shape sh = shape_of(n, false);
-    const bool once = too_large_to_keep(S);
-    RMS_DISPATCH(k_rms_backward, sh, groups);
+    const Shape sh = shape_of(n, false, true);
+    const dim3 g((unsigned)groups), b((unsigned)sh.threads);
+    with_shape(sh, [&](auto l, auto e) {
+      constexpr int L = decltype(l)::value, E = decltype(e)::value > 2 ? 2 : decltype(e)::value;  // (shape_of)
+      const auto typed = [&](auto t) {
+        constexpr int T = decltype(t)::value;
+        if (a.r && a.out) k_rms_backward<L, E, T, true><<<g, b, 0, s>>>(a);
+        else k_rms_backward<L, E, T, false><<<g, b, 0, s>>>(a);
+      };
+      switch (common_type(n, {&S, &dY, &dS, &dX})) {
+        case DT_F32: return typed(Int<DT_F32>());
+        case DT_BF16: return typed(Int<DT_BF16>());
+        case DT_F16: return typed(Int<DT_F16>());
+        default: k_rms_backward<L, E, MIXED, false><<<g, b, 0, s>>>(a);
+      }
+    });
   }
   if (a.part) k_rms_columns<<<cgrid, 1024, 0, s>>>(a.part, groups, n, dgamma, wt);
   return hipGetLastError();
