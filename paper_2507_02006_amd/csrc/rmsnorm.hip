@@ -306,7 +306,7 @@ __global__ __launch_bounds__(L < 8 ? group_threads(L) : TEAM_BLOCK) void k_rms_b
   };
   // the next row is asked for before this one is used (1024 threads have no
   // registers for that)
-  constexpr bool EARLY = T != MIXED && L != 0;
+  constexpr bool EARLY = T != MIXED && (L != 0 || E == 1);
   if constexpr (EARLY) {
     load(tm.first);
     load_past(tm.first);
@@ -435,22 +435,24 @@ Shape shape_of(int64_t n, bool codes, bool back) {
   if (chunks <= 64) return {64, 1, TEAM_BLOCK};
   if (chunks <= 128) return {64, 2, TEAM_BLOCK};
   if (chunks <= 256 && !back) return {64, 4, TEAM_BLOCK};
-  const int threads = (int)(((chunks + 1) / 2 + 63) / 64 * 64);
-  return {threads <= MAX_BLOCK / 2 ? 1 : 0, 2, threads};
+  const int E = chunks <= MAX_BLOCK ? 1 : 2;
+  const int threads = (int)(((chunks + E - 1) / E + 63) / 64 * 64);
+  return {threads <= MAX_BLOCK / 2 ? 1 : 0, E, threads};
 }
 
 // One of a kernel's shapes; f(L, E) launches it.
 template <int V>
 using Int = std::integral_constant<int, V>;
-template <typename F>
+template <bool BACK, typename F>
 void with_shape(const Shape& sh, F f) {
   if (sh.L == 8) f(Int<8>(), Int<1>());
   else if (sh.L == 16) f(Int<16>(), Int<1>());
   else if (sh.L == 32) f(Int<32>(), Int<1>());
   else if (sh.L == 64 && sh.E == 1) f(Int<64>(), Int<1>());
   else if (sh.L == 64 && sh.E == 2) f(Int<64>(), Int<2>());
-  else if (sh.L == 64) f(Int<64>(), Int<4>());
-  else if (sh.L == 1) f(Int<1>(), Int<2>());
+  else if (sh.L == 64) f(Int<64>(), Int<BACK ? 2 : 4>());  // (the backward pass has two at most)
+  else if (sh.L == 1) f(Int<1>(), Int<1>());
+  else if (sh.E == 1) f(Int<0>(), Int<1>());
   else f(Int<0>(), Int<2>());
 }
 
@@ -504,7 +506,7 @@ hipError_t rms_norm(const Mat& X, const Mat& R, const void* gamma, int wt, float
   const int64_t grid = std::min<int64_t>((a.m + rows - 1) / rows, sh.L < 8 ? 256 * std::max(1, 2048 / sh.threads) : 2048);
   // (eight lanes hold no block of 128 columns: their kernels have no codes)
   const dim3 g((unsigned)grid), b((unsigned)sh.threads);
-  with_shape(sh, [&](auto l, auto e) {
+  with_shape<false>(sh, [&](auto l, auto e) {
     constexpr int L = decltype(l)::value, E = decltype(e)::value;
     const auto typed = [&](auto t) {
       constexpr int T = decltype(t)::value;
@@ -563,8 +565,8 @@ hipError_t rms_norm_backward(const Mat& dY, const Mat& S, const float* rstd, con
   } else {
     const Shape sh = shape_of(n, false, true);
     const dim3 g((unsigned)groups), b((unsigned)sh.threads);
-    with_shape(sh, [&](auto l, auto e) {
-      constexpr int L = decltype(l)::value, E = decltype(e)::value > 2 ? 2 : decltype(e)::value;  // (shape_of)
+    with_shape<true>(sh, [&](auto l, auto e) {
+      constexpr int L = decltype(l)::value, E = decltype(e)::value;
       const auto typed = [&](auto t) {
         constexpr int T = decltype(t)::value;
         if (a.r && a.out) k_rms_backward<L, E, T, true><<<g, b, 0, s>>>(a);
