@@ -5,7 +5,9 @@
 // Every value is read once and each code written once, for about a dozen
 // operations a value and order: bound by bytes.
 //
-// A workgroup holds a tile of 128 x 128 in registers, a thread 8 rows by 8
+// As it lies with scales for each row: 16 lanes hold a block, a workgroup 128 blocks
+// that follow each other in memory, so a block's maximum is four lane exchanges.
+// Else a workgroup holds a tile of 128 x 128 in registers, a thread 8 rows by 8
 // columns of it: 16 lanes hold a row of the tile, so a row's maximum is four lane
 // exchanges, and a column's is the thread's own, two lane exchanges and one
 // exchange between the four wavefronts.  Both orders come from one read of the
@@ -112,7 +114,10 @@ __global__ __launch_bounds__(BLOCK) void k_quantize(Args a) {
   __shared__ uint64_t turned[COLUMNS ? BLOCK8 * 16 : 1];
   const int j = threadIdx.x & 15, g = threadIdx.x >> 4, wave = threadIdx.x >> 6;
   const int64_t wide = (a.n + BLOCK8 - 1) / BLOCK8, tiles = (a.m + BLOCK8 - 1) / BLOCK8 * wide;
-  for (int64_t at = blockIdx.x; at < tiles; at += gridDim.x) {
+  for (int64_t id = blockIdx.x; id < tiles; id += gridDim.x) {
+    // workgroups go round-robin to the 8 XCDs: each gets a run of tiles, whose
+    // neighbours share lines where rows are no multiples of 128 bytes
+    const int64_t per = tiles / 8, at = id < per * 8 ? id % 8 * per + id / 8 : id;
     const int64_t r0 = at / wide * BLOCK8, c0 = at % wide * BLOCK8;
     const int64_t row = r0 + g * 8, col = c0 + j * 8;
     Raw x[8];
@@ -178,6 +183,8 @@ __global__ __launch_bounds__(BLOCK) void k_quantize(Args a) {
       }
       __syncthreads();
     }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) made_again(x[i]);
     if constexpr (ROWS) {
       // eight of the 16 lanes of a row make the quotients of its eight rows
       float inverse = 0.f;
@@ -191,6 +198,8 @@ __global__ __launch_bounds__(BLOCK) void k_quantize(Args a) {
         block_scale(mine, scale, inverse);
         if (j < 8 && row + j < a.m) a.q.scales[(row + j) * a.q.lds + c0 / BLOCK8] = scale;
       }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) made_again(x[i]);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         float v[8];
@@ -211,6 +220,9 @@ __global__ __launch_bounds__(BLOCK) void k_quantize(Args a) {
         }
       }
     }
+    if constexpr (ROWS && COLUMNS)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) made_again(x[i]);
     if constexpr (COLUMNS) {
       // rows of four at a time: their codes of each column are one word
       uint32_t word[2][8];
@@ -249,6 +261,68 @@ __global__ __launch_bounds__(BLOCK) void k_quantize(Args a) {
   }
 }
 
+// X as it lies, a scale for each block of a row.
+template <int T>
+__global__ __launch_bounds__(BLOCK) void k_quantize_rows(Args a) {
+  const int lane = threadIdx.x & 63, j = threadIdx.x & 15, g = threadIdx.x >> 4, n8 = row_of<T>((int)a.n);
+  const int64_t wide = (a.n + BLOCK8 - 1) / BLOCK8, blocks = a.m * wide;
+  const int64_t rows16 = 16 / wide, rest16 = 16 % wide;  // 16 blocks on
+  for (int64_t at = (int64_t)blockIdx.x * 128 + g; at - g < blocks; at += (int64_t)gridDim.x * 128) {
+    int64_t row = at / wide, block = at % wide, to[8];
+    Raw<T> x[8];
+    float mine = 0.f, scale, inverse;
+    int have[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t col = block * BLOCK8 + j * 8;
+      const bool in = row < a.m;
+      to[i] = in ? row * a.q.ld + col : -1;
+      have[i] = (int)(a.n - col);
+      load_raw<true>(a.x, type_of<T>(a.xt), (in ? row : a.m - 1) * a.ldx + col, have[i], n8, x[i]);
+      row += rows16;
+      block += rest16;
+      if (block >= wide) {
+        block -= wide;
+        ++row;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      settle(x[i], type_of<T>(a.xt), have[i], n8);
+      if constexpr (T == MIXED) {
+        float v[8];
+        convert(x[i], a.xt, v);
+        pack(v, DT_F32, x[i]);
+      }
+      const float most = group16_max_f32(magnitude<T == DT_BF16 || T == DT_F16>(x[i], T == MIXED ? (int)DT_F32 : T));
+      mine = (j & 7) == i ? most : mine;
+    }
+    // eight of the 16 lanes make the quotients of the group's eight blocks
+    block_scale(mine, scale, inverse);
+    const int64_t own = at + (j & 7) * 16;
+    if (j < 8 && own < blocks) a.q.scales[own / wide * a.q.lds + own % wide] = scale;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) made_again(x[i]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float v[8];
+      convert(x[i], T == MIXED ? (int)DT_F32 : T, v);
+      const float inv = __shfl(inverse, (lane & 48) + i);
+      u32x2_el1 w;
+      w[0] = encode4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+      w[1] = encode4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv);
+      if (to[i] < 0) continue;
+      if (have[i] >= 8) {
+        *reinterpret_cast<u32x2_el1*>(a.q.codes + to[i]) = w;
+      } else {
+#pragma unroll
+        for (int k = 0; k < 7; ++k)
+          if (k < have[i]) a.q.codes[to[i] + k] = (uint8_t)(w[k / 4] >> (8 * (k & 3)));
+      }
+    }
+  }
+}
+
 }  // namespace
 
 hipError_t quantize8(const Mat& X, const Held& Q, const Held& Qt, hipStream_t s) {
@@ -260,9 +334,12 @@ hipError_t quantize8(const Mat& X, const Held& Q, const Held& Qt, hipStream_t s)
   const auto orders = [&](auto tiles, auto type) {
     constexpr bool M = decltype(tiles)::value;
     constexpr int T = decltype(type)::value;
-    if (Q.codes && Qt.codes) k_quantize<true, true, M, T><<<grid, BLOCK, 0, s>>>(a);
-    else if (Q.codes) k_quantize<true, false, M, T><<<grid, BLOCK, 0, s>>>(a);
-    else k_quantize<false, true, M, T><<<grid, BLOCK, 0, s>>>(a);
+    if (Q.codes && Qt.codes) {
+      k_quantize<true, true, M, T><<<grid, BLOCK, 0, s>>>(a);
+    } else if (Q.codes) {
+      if constexpr (M) k_quantize<true, false, M, T><<<grid, BLOCK, 0, s>>>(a);
+      else k_quantize_rows<T><<<(unsigned)std::min<int64_t>((X.rows * ((X.cols + BLOCK8 - 1) / BLOCK8) + 127) / 128, 1 << 20), BLOCK, 0, s>>>(a);
+    } else k_quantize<false, true, M, T><<<grid, BLOCK, 0, s>>>(a);
   };
   const auto typed = [&](auto tiles) {
     if (X.cols < 8) orders(tiles, std::integral_constant<int, MIXED>());

@@ -203,6 +203,11 @@ __device__ __forceinline__ void store_raw(void* p, int, int64_t i, int64_t have,
   store_raw<ONCE>(p, DT_F16, i, have, Raw8{r.lo, r.lo});
 }
 
+// The words as if read anew: what was made of them before is made again rather
+// than kept in registers.
+__device__ __forceinline__ void made_again(Raw8& r) { asm volatile("" : "+v"(r.lo), "+v"(r.hi)); }
+__device__ __forceinline__ void made_again(Raw8Half& r) { asm volatile("" : "+v"(r.lo)); }
+
 // Matrices held in 8 bits: runs of BLOCK8 values of a row share a scale.
 constexpr int BLOCK8 = 128;
 constexpr float TOP8 = 448.f;       // largest e4m3 number
