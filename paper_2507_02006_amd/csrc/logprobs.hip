@@ -8,13 +8,13 @@
 // lowered to it; about a dozen operations a score, an exponential among them:
 // bound by the scores' bytes, near the rate of exponentials for 16-bit ones.
 //
-// Rows of up to 2048 scores are held in the registers of 8 to 64 lanes; the
-// highest scores are taken out one after the other.  Longer rows are streamed by
-// a workgroup each, or by several where there are few rows, which a second launch
-// joins.  There every wavefront keeps its highest scores as a list over its
-// lanes and looks at a chunk of 512 scores only where one is above the list's
-// last; chunks come in rising order of columns, so equal scores stay in the order
-// of their index.  Scores are compared as integers of the same order.
+// Rows of up to 512 scores are held in the registers of 8 to 64 lanes; the
+// highest scores are taken out one after the other.  Longer rows are streamed, by
+// a wavefront or a workgroup each, or by several workgroups where there are few rows,
+// which a second launch joins.  There every wavefront keeps its highest scores as a
+// list over its lanes and looks at a chunk of 512 scores only where one is above the
+// list's last; chunks come in rising order of columns, so equal scores stay in the
+// order of their index.  Scores are compared as integers of the same order.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -137,72 +137,55 @@ __device__ __forceinline__ void store_top(const Args& a, int64_t row, int at, fl
 
 // ------------------------------------------------------------- short rows
 
-// L lanes hold a row, 8 E scores a lane: chunk e is columns (e L + lane) 8 on.
-template <int L, int E, int T>
+// L lanes hold a row, eight scores a lane.
+template <int L, int T>
 __global__ __launch_bounds__(BLOCK) void k_logp_short(Args a) {
-  const int zt = type_of<T>(a.zt), n8 = row_of<T>(a.v);
   constexpr int TEAMS = BLOCK / L;
-  const int lane = threadIdx.x % L;
+  const int zt = type_of<T>(a.zt), n8 = row_of<T>(a.v);
+  const int lane = threadIdx.x % L, first = lane * 8;
   for (int64_t row = (int64_t)blockIdx.x * TEAMS + threadIdx.x / L; row < a.t; row += (int64_t)gridDim.x * TEAMS) {
-    Raw<T> r[E];
-    float z[E][8];
+    Raw<T> r;
+    float z[8];
     Stats t = EMPTY;
+    load_raw(a.z, zt, row * a.ldz + first, a.v - first, n8, r);
+    settle(r, zt, a.v - first, n8);
+    convert(r, zt, z);
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int c = (e * L + lane) * 8;
-      load_raw(a.z, zt, row * a.ldz + c, a.v - c, n8, r[e]);
-    }
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      settle(r[e], zt, a.v - (e * L + lane) * 8, n8);
-      convert(r[e], zt, z[e]);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        if ((e * L + lane) * 8 + k >= a.v) z[e][k] = -__builtin_inff();
-        t.m = fmaxf(t.m, z[e][k]);
-      }
+    for (int k = 0; k < 8; ++k) {
+      if (first + k >= a.v) z[k] = -__builtin_inff();
+      t.m = fmaxf(t.m, z[k]);
     }
     t.m = group_max<L>(t.m);
 #pragma unroll
-    for (int e = 0; e < E; ++e)
-#pragma unroll
-      for (int k = 0; k < 8; ++k) add(t, z[e][k]);
+    for (int k = 0; k < 8; ++k) add(t, z[k]);
     t.s = group_sum_f32<L>(t.s);
     t.w = group_sum_f32<L>(t.w);
     const float log_s = logf(t.s);
     if (lane == 0) finish_row(a, row, t, log_s);
     if (a.top == 0) continue;
-    int key[E][8];
+    int key[8];
 #pragma unroll
-    for (int e = 0; e < E; ++e)
-#pragma unroll
-      for (int k = 0; k < 8; ++k) key[e][k] = (e * L + lane) * 8 + k < a.v ? key_of(z[e][k]) : NONE;
+    for (int k = 0; k < 8; ++k) key[k] = first + k < a.v ? key_of(z[k]) : NONE;
     float mine = 0.f;  // what the round of this lane's number found
     int mine_col = 0;
     for (int i = 0; i < a.top; ++i) {
       int best = NONE;
 #pragma unroll
-      for (int e = 0; e < E; ++e)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) best = key[e][k] > best ? key[e][k] : best;
+      for (int k = 0; k < 8; ++k) best = key[k] > best ? key[k] : best;
       best = group_best<L, true>(best);
       int col = 0x7fffffff;
 #pragma unroll
-      for (int e = E - 1; e >= 0; --e)
-#pragma unroll
-        for (int k = 7; k >= 0; --k) col = key[e][k] == best ? (e * L + lane) * 8 + k : col;
+      for (int k = 7; k >= 0; --k) col = key[k] == best ? first + k : col;
       col = group_best<L, false>(col);
 #pragma unroll
-      for (int e = 0; e < E; ++e)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) key[e][k] = (e * L + lane) * 8 + k == col ? NONE : key[e][k];
+      for (int k = 0; k < 8; ++k) key[k] = first + k == col ? NONE : key[k];
       if (lane == i % L) {
         mine = score_of(best);
         mine_col = col;
       }
       if (i % L == L - 1 || i == a.top - 1) {
-        const int first = i / L * L;
-        if (first + lane <= i) store_top(a, row, first + lane, mine, mine_col, t, log_s);
+        const int begin = i / L * L;
+        if (begin + lane <= i) store_top(a, row, begin + lane, mine, mine_col, t, log_s);
       }
     }
   }
@@ -223,35 +206,40 @@ __device__ __forceinline__ uint64_t wave_best(uint64_t v) {
   return (uint64_t)((uint32_t)hi ^ 0x80000000u) << 32 | ((uint32_t)lo ^ 0x80000000u);
 }
 
+__device__ __forceinline__ int key_of_entry(uint64_t x) { return (int)((uint32_t)(x >> 32) ^ 0x80000000u); }
+
 // The wavefront's `top` highest entries, highest first: lane i gets the i-th (0 if
-// there are not so many).  buf: 64 entries of LDS of the wavefront's own.  The
-// top-th highest of the lanes' best entries is a bound that the wanted ones are not
-// below; what is not below it, `top` entries and few more in any order but
-// a sorted one, is ranked by comparing each with all.  (One by one, `top` times a maximum
-// over the wavefront: 0.3 us each, where two rankings take about 0.6.)
+// there are not so many).  buf: 64 entries of LDS of the wavefront's own.  No wanted
+// score is below the top-th highest of the lanes' best ones; what is not below that,
+// `top` entries and few more in any order but a sorted one, is ranked by comparing
+// each with all.
 template <int E>
 __device__ __forceinline__ uint64_t wave_top(const uint64_t (&x)[E], int top, uint64_t* buf) {
   const int lane = threadIdx.x & 63;
   uint64_t best = x[0];
 #pragma unroll
   for (int e = 1; e < E; ++e) best = x[e] > best ? x[e] : best;
-  wave_sync();
-  buf[lane] = best;
-  wave_sync();
-  int rank = 0;
+  int bound = NONE, rest = key_of_entry(best);
+  if (top <= 8) {
+    for (int i = 0; i < top; ++i) {
+      bound = group_best<64, true>(rest);
+      rest = lane == __ffsll((unsigned long long)__ballot(rest == bound)) - 1 ? NONE : rest;
+    }
+  } else {
+    int* const keys = reinterpret_cast<int*>(buf);
+    wave_sync();
+    keys[lane] = rest;
+    wave_sync();
+    int rank = 0;
 #pragma unroll 16
-  for (int l = 0; l < 64; ++l) rank += buf[l] > best;
-  // (entries are different from each other)
-  const uint64_t at = __ballot(rank == top - 1 && best != 0);
-  uint64_t bound = 1;
-  if (at) {
-    const int l = __ffsll((unsigned long long)at) - 1;
-    bound = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(best >> 32), l) << 32 |
-            (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)best, l);
+    for (int l = 0; l < 64; ++l) rank += keys[l] > rest;
+    bound = group_best<64, false>(rank < top ? rest : 0x7fffffff);
   }
+  // (an entry that is none is below all)
+  const uint32_t least = bound == NONE ? 1u : (uint32_t)bound ^ 0x80000000u;
   int mine = 0;
 #pragma unroll
-  for (int e = 0; e < E; ++e) mine += x[e] >= bound;
+  for (int e = 0; e < E; ++e) mine += (uint32_t)(x[e] >> 32) >= least;
   const int upto = wave_incl_scan(mine), total = wave_last(upto);
   uint64_t out = 0;
   if (total <= 64) {
@@ -259,10 +247,10 @@ __device__ __forceinline__ uint64_t wave_top(const uint64_t (&x)[E], int top, ui
     int place = upto - mine;
 #pragma unroll
     for (int e = 0; e < E; ++e)
-      if (x[e] >= bound) buf[place++] = x[e];
+      if ((uint32_t)(x[e] >> 32) >= least) buf[place++] = x[e];
     wave_sync();
     const uint64_t y = lane < total ? buf[lane] : 0;
-    rank = 0;
+    int rank = 0;  // (entries are different from each other)
     for (int l = 0; l < total; ++l) rank += buf[l] > y;
     wave_sync();
     if (lane < total) buf[rank] = y;
@@ -299,79 +287,85 @@ __device__ __forceinline__ void store_entry(const Args& a, int64_t row, int at, 
   store_top(a, row, at, score_of((int)((uint32_t)(entry >> 32) ^ 0x80000000u)), (int)~(uint32_t)entry, t, log_s);
 }
 
-// The wavefront's highest scores: lane i holds the i-th.
+// The wavefront's highest scores: lane i holds the i-th as an entry.  Scores above the
+// last of a full list wait in LDS and are ranked together with it when 64 do not hold
+// them.
 struct List {
-  int key, col, count, last;  // last: the lowest key of a full list, or NONE
-  __device__ List() : key(NONE), col(0), count(0), last(NONE) {}
+  uint64_t entry;
+  int last, waiting;  // last: the lowest key of a full list, or NONE
+  __device__ List() : entry(0), last(NONE), waiting(0) {}
 
-  // The chunk that begins at column `first` of this lane.  More than two new scores are
-  // ranked together with the list, fewer put in their places one by one.
-  __device__ __forceinline__ void take(const float (&z)[8], int first, int end, int top, uint64_t* buf) {
+  template <int E>
+  __device__ __forceinline__ void rank(const uint64_t (&x)[E], int top, uint64_t* buf) {
+    entry = wave_top(x, top, buf);
+    waiting = 0;
+    last = __builtin_amdgcn_readlane(key_of_entry(entry), top - 1);  // (no entry: NONE)
+  }
+
+  // The chunk that begins at column `first` of this lane.  floor: a key below which no
+  // score is wanted.  Equal scores that are there already have lower columns.
+  __device__ __forceinline__ void take(const float (&z)[8], int first, int end, int floor, int top, uint64_t* wait, uint64_t* buf) {
     const int lane = threadIdx.x & 63;
-    int k[8], best = NONE;
+    int k[8], total = waiting;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       k[j] = first + j < end ? key_of(z[j]) : NONE;
-      best = k[j] > best ? k[j] : best;
+      k[j] = k[j] >= floor ? k[j] : NONE;
+      total += __popcll(__ballot(k[j] > last));
     }
-    if (__popcll(__ballot(best > last)) > 2) {
-      uint64_t x[9];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = k[j] == NONE ? 0 : entry_of(k[j], first + j);
-      x[8] = lane < count ? entry_of(key, col) : 0;
-      const uint64_t y = wave_top(x, top, buf);
-      key = (int)((uint32_t)(y >> 32) ^ 0x80000000u);  // (none: NONE)
-      col = (int)~(uint32_t)y;
-      count = __popcll(__ballot(y != 0));
-      if (count == top) last = __builtin_amdgcn_readlane(key, top - 1);
-      return;
-    }
-    while (true) {
-      const int most = group_best<64, true>(best);
-      if (most <= last) break;  // (a list that is not full ends with NONE)
-      const int owner = __ffsll((unsigned long long)__ballot(best == most)) - 1;
-      int at = 0;
-#pragma unroll
-      for (int j = 7; j >= 0; --j) at = k[j] == most ? j : at;
-      const int c = __builtin_amdgcn_readlane(first + at, owner);
-      // equal scores that are there already have lower columns
-      const int place = __popcll(__ballot(lane < count && key >= most));
-      const int pk = dpp_move<0x138, 0xf>(key), pc = dpp_move<0x138, 0xf>(col);
-      key = lane > place ? pk : lane == place ? most : key;
-      col = lane > place ? pc : lane == place ? c : col;
-      count += count < top;
-      if (count == top) last = __builtin_amdgcn_readlane(key, top - 1);
-      at = lane == owner ? at : 8;
-      best = NONE;
+    if (total <= 64) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        k[j] = j == at ? NONE : k[j];
-        best = k[j] > best ? k[j] : best;
+        const uint64_t who = __ballot(k[j] > last);
+        const int at = waiting + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
+        if (k[j] > last) wait[at] = entry_of(k[j], first + j);
+        waiting += __popcll(who);
       }
+      return;
     }
+    wave_sync();
+    uint64_t x[10];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = k[j] == NONE ? 0 : entry_of(k[j], first + j);
+    x[8] = entry;
+    x[9] = lane < waiting ? wait[lane] : 0;
+    rank(x, top, buf);
+  }
+
+  __device__ __forceinline__ void finish(int top, const uint64_t* wait, uint64_t* buf) {
+    if (waiting == 0) return;
+    wave_sync();
+    const uint64_t x[2] = {entry, (int)(threadIdx.x & 63) < waiting ? wait[threadIdx.x & 63] : 0};
+    rank(x, top, buf);
   }
 };
 
-// A workgroup streams columns [part * per, + per) of a row.
-template <bool TOP, int T>
-__global__ __launch_bounds__(BLOCK) void k_logp_long(Args a) {
+// A workgroup of W threads streams columns [part * per, + per) of a row.  Its
+// wavefronts tell each other how high the scores of a full list are.
+template <int W, bool TOP, int T>
+__global__ __launch_bounds__(W) void k_logp_long(Args a) {
+  constexpr int WAVES = W / 64;
   const int zt = type_of<T>(a.zt), n8 = row_of<T>(a.v);
-  constexpr int WAVES = BLOCK / 64;
   __shared__ Stats stats[WAVES];
-  __shared__ uint64_t lists[TOP ? WAVES * 64 : 1], bufs[TOP ? WAVES : 1][64];
+  __shared__ uint64_t lists[TOP ? WAVES * 64 : 1], bufs[TOP ? WAVES : 1][64], waits[TOP ? WAVES : 1][64];
+  __shared__ int floor_of;
   const int64_t row = blockIdx.x / a.parts;
   const int part = (int)(blockIdx.x % a.parts), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int begin = part * a.per, end = a.v - begin < a.per ? a.v : begin + a.per;
   const int64_t base = row * a.ldz;
   Stats t = EMPTY;
   List list;
+  if constexpr (TOP && WAVES > 1) {
+    if (threadIdx.x == 0) floor_of = NONE;
+    __syncthreads();
+  }
   Raw<T> next;
   // (a chunk past the row's end is moved back into the row, one past the part's not)
   load_raw<true>(a.z, zt, base + begin + (int)threadIdx.x * 8, a.v - begin - (int)threadIdx.x * 8, n8, next);
-  for (int at = begin; at < end; at += BLOCK * 8) {
+  for (int at = begin; at < end; at += W * 8) {
     Raw<T> now = next;
     const int c = at + threadIdx.x * 8;
-    load_raw<true>(a.z, zt, base + c + BLOCK * 8, a.v - c - BLOCK * 8, n8, next);
+    load_raw<true>(a.z, zt, base + c + W * 8, a.v - c - W * 8, n8, next);
     float z[8];
     settle(now, zt, a.v - c, n8);
     convert(now, zt, z);
@@ -387,7 +381,14 @@ __global__ __launch_bounds__(BLOCK) void k_logp_long(Args a) {
     for (int k = 0; k < 8; ++k) add(t, z[k]);
     if constexpr (TOP)
       // (a NaN, which no comparison sees, has made the sum one)
-      if (__any(list.count < a.top || t.s != t.s || key_of(most) > list.last)) list.take(z, c, end, a.top, bufs[wave]);
+      if (__any(list.last == NONE || t.s != t.s || key_of(most) > list.last)) {
+        int floor = NONE;
+        if constexpr (WAVES > 1) floor = __hip_atomic_load(&floor_of, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        const int before = list.last;
+        list.take(z, c, end, floor, a.top, waits[wave], bufs[wave]);
+        if constexpr (WAVES > 1)
+          if (list.last != before && lane == 0) atomicMax(&floor_of, list.last);
+      }
   }
   // the lanes' statistics, then the wavefronts'
   {
@@ -396,28 +397,30 @@ __global__ __launch_bounds__(BLOCK) void k_logp_long(Args a) {
     t.s = group_sum_f32<64>(t.s);
     t.w = group_sum_f32<64>(t.w);
   }
-  if (lane == 0) stats[wave] = t;
+  uint64_t best = 0;
   if constexpr (TOP) {
-    if (lane < a.top) lists[wave * a.top + lane] = list.key == NONE ? 0 : entry_of(list.key, list.col);
+    list.finish(a.top, waits[wave], bufs[wave]);
+    best = list.entry;
   }
-  __syncthreads();
-  if (wave != 0) return;
-  t = stats[0];
+  if constexpr (WAVES > 1) {
+    if (lane == 0) stats[wave] = t;
+    if constexpr (TOP) {
+      if (lane < a.top) lists[wave * a.top + lane] = best;
+    }
+    __syncthreads();
+    if (wave != 0) return;
+    t = stats[0];
 #pragma unroll
-  for (int w = 1; w < WAVES; ++w) t = merge(t, stats[w]);
+    for (int w = 1; w < WAVES; ++w) t = merge(t, stats[w]);
+    if constexpr (TOP) best = take_top<WAVES>(lists, WAVES * a.top, a.top, bufs[0]);
+  }
   const float log_s = logf(t.s);
   if (a.parts == 1) {
     if (lane == 0) finish_row(a, row, t, log_s);
-    if constexpr (TOP) {
-      const uint64_t x = take_top<4>(lists, WAVES * a.top, a.top, bufs[0]);
-      if (lane < a.top) store_entry(a, row, lane, x, t, log_s);
-    }
+    if (TOP && lane < a.top) store_entry(a, row, lane, best, t, log_s);
   } else {
     if (lane == 0) a.stats[blockIdx.x] = t;
-    if constexpr (TOP) {
-      const uint64_t x = take_top<4>(lists, WAVES * a.top, a.top, bufs[0]);
-      if (lane < a.top) a.lists[(int64_t)blockIdx.x * a.top + lane] = x;
-    }
+    if (TOP && lane < a.top) a.lists[(int64_t)blockIdx.x * a.top + lane] = best;
   }
 }
 
@@ -490,7 +493,7 @@ __global__ __launch_bounds__(BLOCK) void k_logp_back(Back a) {
   }
 }
 
-constexpr int64_t kShortCols = 2048;
+constexpr int64_t kShortCols = 512;
 
 // f(type) with the type as a constant (rows of fewer than eight scores: MIXED).
 template <typename F>
@@ -501,10 +504,14 @@ void with_type(int t, int64_t v, F f) {
   else f(std::integral_constant<int, DT_F16>());
 }
 
+// Rows that a wavefront streams by itself: of up to 2048 scores, or 16384 where there are
+// enough rows to fill the chip with them.
+constexpr int64_t kWaveCols = 2048, kManyWaveCols = 16384, kManyRows = 4096;
+
 // Workgroups that share a row: where rows are fewer than what fills the chip, as
 // many as have a step of columns each, of which the lists can be joined.
 int parts_of(int64_t t, int64_t v, int top) {
-  if (v <= kShortCols || t >= 512) return 1;
+  if (v <= kWaveCols || t >= 512) return 1;
   const int64_t steps = (v + BLOCK * 8 - 1) / (BLOCK * 8);
   const int64_t most = std::min<int64_t>(kMostParts, top > 0 ? kMostEntries / top : kMostParts);
   const int64_t parts = std::max<int64_t>(1, std::min({steps, most, (1024 + t - 1) / t}));
@@ -536,15 +543,14 @@ hipError_t log_probs(const LogProbs& x, void* ws, hipStream_t s) {
   if (a.v <= kShortCols) {
     with_type(a.zt, a.v, [&](auto type) {
       constexpr int T = decltype(type)::value;
-      if (a.v <= 64) k_logp_short<8, 1, T><<<grid(8), BLOCK, 0, s>>>(a);
-      else if (a.v <= 128) k_logp_short<16, 1, T><<<grid(16), BLOCK, 0, s>>>(a);
-      else if (a.v <= 256) k_logp_short<32, 1, T><<<grid(32), BLOCK, 0, s>>>(a);
-      else if (a.v <= 512) k_logp_short<64, 1, T><<<grid(64), BLOCK, 0, s>>>(a);
-      else if (a.v <= 1024) k_logp_short<64, 2, T><<<grid(64), BLOCK, 0, s>>>(a);
-      else k_logp_short<64, 4, T><<<grid(64), BLOCK, 0, s>>>(a);
+      if (a.v <= 64) k_logp_short<8, T><<<grid(8), BLOCK, 0, s>>>(a);
+      else if (a.v <= 128) k_logp_short<16, T><<<grid(16), BLOCK, 0, s>>>(a);
+      else if (a.v <= 256) k_logp_short<32, T><<<grid(32), BLOCK, 0, s>>>(a);
+      else k_logp_short<64, T><<<grid(64), BLOCK, 0, s>>>(a);
     });
     return hipGetLastError();
   }
+  const bool wave = a.v <= kWaveCols || (a.v <= kManyWaveCols && a.t >= kManyRows);
   a.parts = parts_of(a.t, a.v, a.top);
   const int64_t steps = ((int64_t)a.v + BLOCK * 8 - 1) / (BLOCK * 8);
   a.per = (int)((steps + a.parts - 1) / a.parts * (BLOCK * 8));
@@ -568,8 +574,10 @@ hipError_t log_probs(const LogProbs& x, void* ws, hipStream_t s) {
     const dim3 g((unsigned)(b.t * b.parts));
     with_type(a.zt, a.v, [&](auto type) {
       constexpr int T = decltype(type)::value;
-      if (a.top > 0) k_logp_long<true, T><<<g, BLOCK, 0, s>>>(b);
-      else k_logp_long<false, T><<<g, BLOCK, 0, s>>>(b);
+      if (wave && a.top > 0) k_logp_long<64, true, T><<<g, 64, 0, s>>>(b);
+      else if (wave) k_logp_long<64, false, T><<<g, 64, 0, s>>>(b);
+      else if (a.top > 0) k_logp_long<BLOCK, true, T><<<g, BLOCK, 0, s>>>(b);
+      else k_logp_long<BLOCK, false, T><<<g, BLOCK, 0, s>>>(b);
     });
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
