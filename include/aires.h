@@ -841,7 +841,7 @@ aires_status aires_quantize8(const aires_dense *X, const aires_dense8 *Q, const 
 /* Bytes of workspace that aires_matmul8 needs for these operands (codes and scales
    are not read) and a Y of type dtype: partial sums of a k split over workgroups, 64
    MB at most, and copies of operands whose codes, ld or ncols are no multiple of
-   16 (none for up to 64 rows of A).
+   16 (none for up to 16 rows of A).
    Errors: AIRES_E_INVALID_ARG, AIRES_E_DIM, AIRES_E_UNSUPPORTED. */
 aires_status aires_matmul8_workspace(const aires_dense8 *A, const aires_dense8 *B, int32_t dtype, int64_t *bytes);
 

@@ -16,7 +16,7 @@
 // anyway, the codes are converted to bf16, which holds them exactly, and multiplied
 // at half the rate with sums that are fp32's.
 //
-// Two forms.  Up to 64 rows of A: bound by B's bytes, which go from memory to the
+// Two forms.  Up to 16 rows of A: bound by B's bytes, which go from memory to the
 // matrix cores' registers, no LDS; a workgroup owns 16 rows of B and its wavefronts
 // share k.  Else tiles: stages of 128 k go from global memory straight to LDS.  Where
 // an operand's rows are not chunks of 16 bytes it is copied so first.  Where there are few
@@ -375,29 +375,34 @@ __global__ __launch_bounds__(TW / WW * (TX / WX) * 64, WX == 128 ? 1 : 2) void k
   else T::template write<DT_F16>(acc, to, first, ld, r0, c0, a.y.rows, a.y.cols, lds);
 }
 
-// Y: the splits' sums, added in their order.
+// Y: the splits' sums, added in their order.  (64 MB of them at most: 32-bit places.)
 __global__ __launch_bounds__(256) void k_join8(Mat y, const float* part, int splits) {
-  const int64_t values = y.rows * y.cols;
-  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < values; i += (int64_t)gridDim.x * 1024) {
+  const uint32_t cols = (uint32_t)y.cols, values = (uint32_t)y.rows * cols;
+  for (uint32_t i = (blockIdx.x * 256 + threadIdx.x) * 4; i < values; i += gridDim.x * 1024) {
     float v[4] = {};
     const int have = values - i < 4 ? (int)(values - i) : 4;
-    for (int s = 0; s < splits; ++s) {
-      const float* p = part + s * values + i;
-      if (have == 4) {
+    if (have == 4) {
+#pragma unroll 4
+      for (int s = 0; s < splits; ++s) {
         float x[4];
-        load4<DT_F32>(p, 0, x);
+        load4<DT_F32>(part + (int64_t)s * values, i, x);
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[q] += x[q];
-      } else {
-        for (int q = 0; q < have; ++q) v[q] += p[q];
       }
+    } else {
+      for (int s = 0; s < splits; ++s)
+        for (int q = 0; q < have; ++q) v[q] += part[(int64_t)s * values + i + q];
     }
-    int64_t row = i / y.cols, col = i % y.cols;
-    for (int q = 0; q < have; ++q) {
-      store1(y.data, y.type, row * y.ld + col, v[q]);
-      if (++col == y.cols) {
-        col = 0;
-        ++row;
+    const uint32_t row = i / cols, col = i % cols;
+    if (col + 4 <= cols && have == 4) {
+      const int64_t at = row * y.ld + col;
+      if (y.type == DT_F32) store4<DT_F32>(y.data, at, v);
+      else if (y.type == DT_BF16) store4<DT_BF16>(y.data, at, v);
+      else store4<DT_F16>(y.data, at, v);
+    } else {
+      for (int q = 0; q < have; ++q) {
+        const uint32_t r = (i + q) / cols;
+        store1(y.data, y.type, r * y.ld + (i + q - r * cols), v[q]);
       }
     }
   }
@@ -410,47 +415,39 @@ struct Codes {  // of a lane: chunks of 16 k
 };
 
 constexpr int ROW_WAVES = 8;
-constexpr int kFewRows = 64;
+constexpr int kFewRows = 16;
 
-// XT x 16 rows of A against 16 rows of B a workgroup; its wavefronts take steps
-// of 128 k in turn, two at a time.  A lane holds 32 k of its row: chunks of 16 bytes,
-// 64 bytes apart, so that a load covers 64 contiguous bytes of a row.
-template <int XT, bool ROWS>
+// All rows of A against 16 rows of B a workgroup; its wavefronts take steps of 128 k
+// in turn, two at a time.  A lane holds 32 k of its row: chunks of 16 bytes, 64 bytes
+// apart, so that a load covers 64 contiguous bytes of a row.  (With two or four times
+// 16 rows of A the tiles are faster: 17 x 8192 x 8192 18 us against 23, 64 x 8192 x 2048 9
+// against 16.)
+template <bool ROWS>
 __global__ __launch_bounds__(64 * ROW_WAVES) void k_rows8(Args a) {
-  __shared__ float sums[ROW_WAVES][XT][64][4];
+  __shared__ float sums[ROW_WAVES][64][4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t w0 = (int64_t)blockIdx.x * 16;
-  const int64_t wr = w0 + (lane & 15) < a.w.rows ? w0 + (lane & 15) : a.w.rows - 1;
-  const uint8_t* const wp = a.w.codes + wr * a.w.ld + (lane >> 4) * 16;
-  const uint8_t* xp[XT];
-  const float* xs[XT];
+  const auto clamp = [](int64_t r, const Held& h) { return r < h.rows ? r : h.rows - 1; };
+  const int64_t xr = clamp(lane & 15, a.x);
+  const uint8_t* const wp = a.w.codes + clamp(w0 + (lane & 15), a.w) * a.w.ld + (lane >> 4) * 16;
+  const uint8_t* const xp = a.x.codes + xr * a.x.ld + (lane >> 4) * 16;
+  const float* const xs = a.x.scales + xr * a.x.lds;
   const float* ws[ROWS ? 4 : 1];
 #pragma unroll
-  for (int t = 0; t < XT; ++t) {
-    const int64_t r = t * 16 + (lane & 15) < a.x.rows ? t * 16 + (lane & 15) : a.x.rows - 1;
-    xp[t] = a.x.codes + r * a.x.ld + (lane >> 4) * 16;
-    xs[t] = a.x.scales + r * a.x.lds;
-  }
-#pragma unroll
-  for (int q = 0; q < (ROWS ? 4 : 1); ++q) {
-    const int64_t r = ROWS ? w0 + (lane >> 4) * 4 + q : w0;
-    ws[q] = a.w.scales + (r < a.w.rows ? r : a.w.rows - 1) / a.w.tile * a.w.lds;
-  }
-  f32x4 acc[XT] = {};
-  const auto step = [&](int64_t s, const Codes& w, const Codes (&x)[XT]) {
+  for (int q = 0; q < (ROWS ? 4 : 1); ++q)
+    ws[q] = a.w.scales + clamp(ROWS ? w0 + (lane >> 4) * 4 + q : w0, a.w) / a.w.tile * a.w.lds;
+  f32x4 acc = {};
+  const auto step = [&](int64_t s, const Codes& w, const Codes& x) {
     float f[ROWS ? 4 : 1];
 #pragma unroll
     for (int q = 0; q < (ROWS ? 4 : 1); ++q) f[q] = ws[q][s];
+    const float fx = xs[s];
+    f32x4 v = {};
 #pragma unroll
-    for (int t = 0; t < XT; ++t) {
-      const float fx = xs[t][s];
-      f32x4 v = {};
+    for (int h = 0; h < 4; ++h)
+      v = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(w.c[h / 2], h % 2), widen(x.c[h / 2], h % 2), v, 0, 0, 0);
 #pragma unroll
-      for (int h = 0; h < 4; ++h)
-        v = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(w.c[h / 2], h % 2), widen(x[t].c[h / 2], h % 2), v, 0, 0, 0);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) acc[t][q] += v[q] * (f[ROWS ? q : 0] * fx);
-    }
+    for (int q = 0; q < 4; ++q) acc[q] += v[q] * (f[ROWS ? q : 0] * fx);
   };
   const auto whole = [&](const uint8_t* p, int64_t s) {
     return Codes{*reinterpret_cast<const i32x4_el1*>(p + s * 128), *reinterpret_cast<const i32x4_el1*>(p + s * 128 + 64)};
@@ -459,37 +456,25 @@ __global__ __launch_bounds__(64 * ROW_WAVES) void k_rows8(Args a) {
   int64_t s = wave;
   for (; s + ROW_WAVES < full; s += 2 * ROW_WAVES) {
     const int64_t u = s + ROW_WAVES;
-    const Codes w0v = whole(wp, s), w1v = whole(wp, u);
-    Codes x0v[XT], x1v[XT];
-#pragma unroll
-    for (int t = 0; t < XT; ++t) {
-      x0v[t] = whole(xp[t], s);
-      x1v[t] = whole(xp[t], u);
-    }
+    const Codes w0v = whole(wp, s), w1v = whole(wp, u), x0v = whole(xp, s), x1v = whole(xp, u);
     step(s, w0v, x0v);
     step(u, w1v, x1v);
   }
   for (; s < a.steps; s += ROW_WAVES) {
     const int64_t have = a.k - s * 128 - (lane >> 4) * 16;
-    Codes x[XT];
-#pragma unroll
-    for (int t = 0; t < XT; ++t) x[t] = Codes{load16(xp[t] + s * 128, have), load16(xp[t] + s * 128 + 64, have - 64)};
-    step(s, Codes{load16(wp + s * 128, have), load16(wp + s * 128 + 64, have - 64)}, x);
+    const auto some = [&](const uint8_t* p) { return Codes{load16(p + s * 128, have), load16(p + s * 128 + 64, have - 64)}; };
+    step(s, some(wp), some(xp));
   }
 #pragma unroll
-  for (int t = 0; t < XT; ++t)
-#pragma unroll
-    for (int q = 0; q < 4; ++q) sums[wave][t][lane][q] = acc[t][q];
+  for (int q = 0; q < 4; ++q) sums[wave][lane][q] = acc[q];
   __syncthreads();
-  for (int i = threadIdx.x; i < XT * 64; i += 64 * ROW_WAVES) {
-    const int t = i / 64, l = i % 64;
-    float v[4] = {};
+  if (wave != 0) return;
+  float v[4] = {};
 #pragma unroll
-    for (int u = 0; u < ROW_WAVES; ++u)
+  for (int u = 0; u < ROW_WAVES; ++u)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) v[q] += sums[u][t][l][q];
-    store_y(a, t * 16 + (l & 15), w0 + (l >> 4) * 4, v);
-  }
+    for (int q = 0; q < 4; ++q) v[q] += sums[u][lane][q];
+  store_y(a, lane & 15, w0 + (lane >> 4) * 4, v);
 }
 
 __global__ __launch_bounds__(256) void k_zero8(Mat y) {
@@ -515,14 +500,24 @@ struct Way {
 
 constexpr int64_t kPartBytes = int64_t(64) << 20;
 
+// Tiles of 256 where there are enough for the chip (not where B's rows have scales of their
+// own, or the products are wide: those need the registers: 16384 x 8192 x 4096 722 us against
+// 798), of 128 where there are enough of those (2048 x 2048 x 2048 17 us, 22 with 64, 26
+// with 128 and k in two), else of 64 (300 x 4096 x 2048 12.5 us, 15 with 128); k is split
+// where there are few tiles and many steps (256 x 256 x 8192 14 us in 8 shares, 31 in
+// one; 300 x 1024 x 1024 6.5 in one, 9 in two), and with much work in tiles of 128 (1000 x 520 x
+// 65536).
 Way way_of(int64_t m, int64_t n, int64_t k, bool rows, bool wide) {
   const int64_t steps = (k + 127) / 128;
   if (m <= kFewRows) return {0, 1, steps};
   const auto tiles = [&](int64_t t) { return (m + t - 1) / t * ((n + t - 1) / t); };
   if (!rows && !wide && tiles(256) >= 200) return {256, 1, steps};
-  const int tile = tiles(128) >= 256 || steps >= 64 ? 128 : 64;
-  const int64_t want = 512 / tiles(tile);
-  int64_t splits = std::max<int64_t>(1, std::min({want, steps / 8, kPartBytes / (m * n * 4)}));
+  if (tiles(128) >= 192) return {128, 1, steps};
+  const bool much = tiles(128) * steps >= 4096;
+  const int tile = much ? 128 : 64;
+  // (two workgroups of tiles of 128 to a CU: one more than 512 of them takes twice the time)
+  const int64_t fill = much ? 512 / tiles(128) : tiles(64) <= 160 ? (512 + tiles(64) / 2) / tiles(64) : 1;
+  int64_t splits = std::max<int64_t>(1, std::min({fill, steps / 8, kPartBytes / (m * n * 4)}));
   const int64_t per = (steps + splits - 1) / splits;
   splits = (steps + per - 1) / per;
   return {tile, splits, per};
@@ -542,14 +537,6 @@ hipError_t launch(const Args& a, const Way& w, hipStream_t s) {
     if (w.tile == 256) return launch<256, 256, 128, 64, 2, ROWS, WIDE>(a, w, s);
   if (w.tile == 128) return launch<128, 128, 64, 64, 2, ROWS, WIDE>(a, w, s);
   return launch<64, 64, 32, 32, 3, ROWS, WIDE>(a, w, s);
-}
-
-template <int XT>
-hipError_t launch_rows(const Args& a, hipStream_t s) {
-  const dim3 grid((unsigned)((a.y.cols + 15) / 16));
-  if (a.w.tile == 1) k_rows8<XT, true><<<grid, 64 * ROW_WAVES, 0, s>>>(a);
-  else k_rows8<XT, false><<<grid, 64 * ROW_WAVES, 0, s>>>(a);
-  return hipGetLastError();
 }
 
 // Whether h's rows are chunks of 16 bytes, and the bytes of a copy that is.
@@ -590,7 +577,12 @@ hipError_t matmul8(const Held& A, const Held& B, const Mat& Y, void* ws, hipStre
   const bool rows = B.tile == 1, wide = Y.type == DT_F32;
   const Way w = way_of(m, n, k, rows, wide);
   Args a{A, B, Y, nullptr, k, (k + 127) / 128, w.per};
-  if (w.tile == 0) return m <= 16 ? launch_rows<1>(a, s) : m <= 32 ? launch_rows<2>(a, s) : launch_rows<4>(a, s);
+  if (w.tile == 0) {
+    const dim3 grid((unsigned)((n + 15) / 16));
+    if (rows) k_rows8<true><<<grid, 64 * ROW_WAVES, 0, s>>>(a);
+    else k_rows8<false><<<grid, 64 * ROW_WAVES, 0, s>>>(a);
+    return hipGetLastError();
+  }
   char* place = static_cast<char*>(ws);
   if (w.splits > 1) {
     a.part = static_cast<float*>(ws);
