@@ -1,0 +1,340 @@
+"""The layers' calls as they are used (GPU): one after the other, in graphs, on other
+streams, at once, in workspaces of exactly the stated size; and at sizes drawn at
+random with fixed seeds."""
+import ctypes
+import math
+import os
+import random
+import sys
+
+import pytest
+
+torch = pytest.importorskip("torch")
+import paper_2507_02006_amd as aires  # noqa: E402
+from paper_2507_02006_amd import _binding as B_  # noqa: E402
+from test_gpu_layers import (BF16, CHAIN, F16, F32, F8, U, check_product, equal, hold, logp_ref, logp_tolerance,  # noqa: E402
+                             near, operand, product_tolerance, rand, rms_check, rounded, values)
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+from examples import residual_layers as example  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------ a run of them
+
+def test_layers_one_after_the_other():
+    """Forward and backward of the example's layers: every stage against its formula
+    in 64 bits, from what it was given."""
+    n, d, classes = 333, 200, 19
+    params = example.model(d, classes, 2)
+    x = rand((n, d), 1, BF16).cuda()
+    labels = torch.randint(-1, classes, (n,), generator=torch.Generator().manual_seed(2)).cuda()
+    z, kept = example.forward(params, x)
+    loss, dz = example.loss_and_gradient(z, labels, 0.1)
+    grads, dx = example.backward(params, kept, dz)
+    assert z.dtype == F32 and z.shape == (n, classes) and dx.shape == x.shape
+    assert [g.shape for g in grads] == [p.shape for p in params]
+
+    came, r = x, None
+    for k, c in enumerate(kept):
+        gamma = params[2 * k].cpu()
+        y, s, q = aires.rms_norm(came, params[2 * k], residual=r)
+        rms_check(came.cpu(), None if r is None else r.cpu(), gamma, y, s, q, BF16)
+        assert torch.equal(c["s"], came if s is None else s) and torch.equal(c["rstd"], q)
+        for pair, want in ((c["y8"], hold(y.cpu())), (c["y8t"], hold(y.cpu().t().contiguous())),
+                           (c["W8"], hold(params[2 * k + 1].cpu(), True)),
+                           (c["W8t"], hold(params[2 * k + 1].cpu().t().contiguous(), True))):
+            assert equal(pair[0].cpu(), want[0]) and torch.equal(pair[1].cpu(), want[1])
+        out = values(c["y8"]) @ values(c["W8"]).t()
+        near(c["out"], out, product_tolerance(c["y8"], c["W8"], out, c["out"].dtype), "out %d" % k)
+        came, r = c["out"], c["s"]
+
+    lse, logp, H, lp, p = logp_ref(z.cpu(), labels.cpu())
+    there = labels.cpu() >= 0
+    want = -(logp.sum() + 0.1 * H[there].sum()) / there.sum()
+    base, ent = logp_tolerance(z.cpu(), p)
+    assert abs(float(loss) - float(want)) <= float((base + 0.1 * ent + 16 * U * (logp.abs() + H + 1)).sum() / there.sum())
+
+    down, ds = dz, None
+    for k in reversed(range(len(kept))):
+        c = kept[k]
+        for pair, want in ((c["dx8"], hold(down.cpu())), (c["dx8t"], hold(down.cpu().t().contiguous()))):
+            assert equal(pair[0].cpu(), want[0]) and torch.equal(pair[1].cpu(), want[1])
+        dW = values(c["dx8t"]) @ values(c["y8t"]).t()
+        near(grads[2 * k + 1], dW, product_tolerance(c["dx8t"], c["y8t"], dW, F32), "dW %d" % k)
+        dy = values(c["dx8"]) @ values(c["W8t"]).t()
+        near(c["dy"], dy, product_tolerance(c["dx8"], c["W8t"], dy, BF16), "dy %d" % k)
+        D, Q, G = c["dy"].double().cpu(), c["rstd"].double().cpu()[:, None], params[2 * k].double().cpu()
+        sh, g = c["s"].double().cpu() * Q, D * G
+        want = Q * (g - sh * (g * sh).mean(1, keepdim=True))
+        tol = Q * (8 * U * g.abs() + sh.abs() * (CHAIN + 8) * U * (g * sh).abs().mean(1, keepdim=True))
+        if c["ds"] is not None:
+            want = want + c["ds"].double().cpu()
+            tol = tol + U * c["ds"].double().cpu().abs()
+        now, dgamma = aires.rms_norm_backward(c["dy"], c["s"], c["rstd"], params[2 * k], dS=c["ds"])
+        near(now, want, tol + rounded(want, BF16) + U * want.abs(), "ds %d" % k)
+        assert torch.equal(dgamma, grads[2 * k])
+        near(dgamma, (D * sh).sum(0), (CHAIN + 4) * U * (D * sh).abs().sum(0), "dgamma %d" % k)
+        down = now
+    assert torch.equal(down, dx)
+
+    norm, scale = aires.grad_norm(grads, max_norm=1e-3)
+    m, v = aires.adamw_state(params)
+    before = [p.clone() for p in params]
+    aires.adamw(params, grads, m, v, step=1, lr=1e-2, weight_decay=0.0, grad_scale=scale)
+    for p, b, g, mm in zip(params, before, grads, m):
+        near(mm, 0.1 * g.double().cpu() * float(scale), 8 * U * mm.abs().double().cpu() + 2.0 ** -126, "first moment")
+        assert not torch.equal(p, b)
+
+
+def test_gradient_of_the_layers_against_differences():
+    """The backward calls against differences of the forward formula in 64 bits, in
+    fp32 all through (the products' own gradients are products)."""
+    n, d, v, h = 4, 24, 7, 1e-5
+    x, r, gamma, W = (rand(s, i).double() for i, s in enumerate([(n, d), (n, d), (d,), (v, d)]))
+    labels = torch.tensor([1, -1, 6, 0])
+    a, b = rand(n, 8).double(), rand(n, 9).double()
+
+    def value(x, r, gamma):
+        s = x + r
+        z = (s * (s.square().mean(1, keepdim=True) + 1e-6).rsqrt() * gamma) @ W.t()
+        _, logp, H, _, _ = logp_ref(z, labels)
+        return (a * logp + b * H).sum() + 0.5 * s.square().sum()
+
+    def slope(f, at):
+        out = torch.empty_like(at)
+        for i in range(at.numel()):
+            e = torch.zeros_like(at).view(-1)
+            e[i] = h
+            e = e.view(at.shape)
+            out.view(-1)[i] = (f(at + e) - f(at - e)) / (2 * h)
+        return out
+
+    c = lambda t: t.float().cuda()  # noqa: E731
+    y, s, q = aires.rms_norm(c(x), c(gamma), residual=c(r))
+    z = (y.double() @ W.cuda().t()).float()
+    st = aires.log_probs(z, labels.cuda())
+    dz = aires.log_probs_backward(z, labels.cuda(), st.lse, st.entropy, dlogp=c(a), dentropy=c(b))
+    dy = (dz.double() @ W.cuda()).float()
+    dx, dg = aires.rms_norm_backward(dy, s, q, c(gamma), dS=s)
+    # differences: h^2 f''' and 2^-52 |f| / h, below 1e-8 here; a few dozen fp32 roundings of values up to 20
+    for got, want in ((dx, slope(lambda t: value(t, r, gamma), x)), (dx, slope(lambda t: value(x, t, gamma), r)),
+                      (dg, slope(lambda t: value(x, r, t), gamma))):
+        near(got, want, 3e-5 * (1 + want.abs()), "slope")
+
+
+def test_example_runs():
+    losses, right = example.main(["--nodes", "600", "--features", "40", "--classes", "5", "--degree", "8", "--steps", "4"])
+    assert len(losses) == 4 and all(math.isfinite(x) for x in losses) and 0 <= right <= 1
+
+
+# ------------------------------------------------------- streams and graphs
+
+def everything(x, r, gamma, W8, labels, grads, outs):
+    """Each call once, over inputs that stay where they are: all outputs."""
+    y8, s, q = aires.rms_norm(x, gamma, residual=r, out_dtype=F8)
+    z = aires.matmul_8bit(y8, W8, out_dtype=F32)
+    few = aires.matmul_8bit((y8[0][:7], y8[1][:7]), W8)
+    p = aires.log_probs(z, labels, top=5)
+    long = aires.log_probs(z.view(3, -1), None, top=3)
+    dz = aires.log_probs_backward(z, labels, p.lse, p.entropy, dlogp=p.logp, dentropy=p.entropy)
+    rows, cols = aires.quantize_8bit(dz, order="both")
+    dW = aires.matmul_8bit(cols, aires.quantize_8bit(s, order="columns"), out_dtype=F32)
+    ds, dg = aires.rms_norm_backward(s, s, q, gamma, dS=r)
+    norm, scale = aires.grad_norm(grads, max_norm=1.0)
+    clipped = aires.clip_grads(grads, 1.0, out=outs)
+    return [*y8, s, q, z, few, p.logp, p.entropy, p.lse, p.top_logp, p.top_index, long.lse, long.top_logp, long.top_index,
+            dz, *rows, *cols, dW, ds, dg, norm, scale, clipped, *outs]
+
+
+def inputs(seed=1, n=300, d=272, v=3001):
+    g = lambda *a: rand(a[:-1], a[-1] + seed).cuda()  # noqa: E731
+    labels = torch.randint(-1, v, (n,), generator=torch.Generator().manual_seed(seed)).cuda()
+    grads = [g(1000, 17, 3), g(70001, 4).to(BF16), g(5, 5).to(F16)]
+    W8 = aires.quantize_8bit(g(v, d, 6) * d ** -0.5, tiles=True)
+    return g(n, d, 1).to(BF16), g(n, d, 2).to(BF16), g(d, 7), W8, labels, grads, [torch.empty_like(t, dtype=F32) for t in grads]
+
+
+def test_in_a_graph():
+    a, b = inputs(1), inputs(50)
+    want = [[t.clone() for t in everything(*x)] for x in (a, b)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        everything(*a)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = everything(*a)
+    flat = lambda x: [t for e in x for t in (e if isinstance(e, (tuple, list)) else (e,))]  # noqa: E731
+    first = [t.clone() for t in flat(a)]
+    for k in range(4):
+        which = k % 2
+        for t, new in zip(flat(a), flat(b) if which else first):
+            t.copy_(new)
+        everything(*b)                            # eager work of the program's own in between
+        graph.replay()
+        torch.cuda.synchronize()
+        for i, (x, y) in enumerate(zip(got, want[which])):
+            assert equal(x, y), (k, i)
+
+
+def test_on_other_streams_and_at_once():
+    a, b = inputs(1), inputs(90)
+    want = [[t.clone() for t in everything(*x)] for x in (a, b)]
+    torch.cuda.synchronize()
+    one, two = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(3):
+        out = []
+        for s, x in ((one, a), (two, b)):
+            with torch.cuda.stream(s):
+                out.append(everything(*x))
+        torch.cuda.synchronize()
+        for x, y in zip(out, want):
+            for i, (p, q) in enumerate(zip(x, y)):
+                assert equal(p, q), i
+    # stream=, as a stream and as its address; what the call was given is released before it runs
+    x, r, gamma, W8, labels, grads, _ = a
+    for s in (one, two.cuda_stream):
+        y8, S, q = aires.rms_norm(x.clone(), gamma.clone(), residual=r.clone(), out_dtype=F8, stream=s)
+        z = aires.matmul_8bit((y8[0], y8[1]), (W8[0].clone(), W8[1].clone()), out_dtype=F32, stream=s)
+        del y8
+        p = aires.log_probs(z, labels.clone(), top=5, stream=s)
+        dz = aires.log_probs_backward(z, labels.clone(), p.lse, p.entropy, dlogp=p.logp, dentropy=p.entropy, stream=s)
+        norm, scale = aires.grad_norm([g.clone() for g in grads], max_norm=1.0, stream=s)
+        rows, cols = aires.quantize_8bit(dz, order="both", stream=s)
+        ds, dg = aires.rms_norm_backward(S, S, q, gamma, dS=r, stream=s)
+        junk = [torch.full((1 << 18,), math.nan, device="cuda") for _ in range(40)]
+        torch.cuda.synchronize()
+        del junk
+        w = want[0]
+        for got, at in ((S, 2), (q, 3), (z, 4), (p.logp, 6), (p.entropy, 7), (p.lse, 8), (p.top_logp, 9), (p.top_index, 10), (dz, 14),
+                        (rows[0], 15), (rows[1], 16), (cols[0], 17), (cols[1], 18), (ds, 20), (dg, 21), (norm, 22), (scale, 23)):
+            assert equal(got, w[at]), at
+
+
+# ---------------------------------------------- workspaces of the stated size
+
+def c_dense(x):
+    return B_.Dense(x.shape[0], x.shape[1], x.stride(0), {F32: 0, BF16: 1, F16: 2}[x.dtype], 0, x.data_ptr())
+
+
+def c_held(pair, tile):
+    c, s = pair
+    return B_.Dense8(c.shape[0], c.shape[1], c.stride(0), c.data_ptr(), s.data_ptr(), s.stride(0), tile, 0)
+
+
+class Room:
+    """A workspace of `need` bytes full of NaNs, and what lies behind it."""
+
+    def __init__(self, need):
+        self.need = need
+        self.all = torch.full((need // 4 + 1024,), math.nan, device="cuda").view(torch.uint8)
+        self.tail = self.all[need:].clone()
+
+    def check(self):
+        torch.cuda.synchronize()
+        assert torch.equal(self.all[self.need:], self.tail)
+
+
+def test_workspaces_are_as_large_as_stated():
+    lib, need = B_.load(), ctypes.c_int64()
+    ref = ctypes.byref
+    for m, n, k, tile, kind in ((100, 90, 4096, 128, F32), (100, 90, 4099, 1, BF16), (300, 40, 12345, 128, F16), (1000, 520, 8200, 1, F32),
+                                (300, 3000, 333, 128, BF16), (17, 17, 100000, 1, F32)):
+        A, B = operand(m, k, 1, False), operand(n, k, 2, tile == 128)
+        Y = torch.empty(m, n, dtype=kind, device="cuda")
+        a, b, y = c_held(A, 1), c_held(B, tile), c_dense(Y)
+        assert lib.aires_matmul8_workspace(ref(a), ref(b), y.dtype, ref(need)) == B_.OK and need.value > 0
+        room = Room(need.value)
+        assert lib.aires_matmul8(ref(a), ref(b), ref(y), room.all.data_ptr(), need.value, None) == B_.OK
+        room.check()
+        want = values(A) @ values(B).t()
+        near(Y, want, product_tolerance(A, B, want, kind), (m, n, k))
+    for t, v, top in ((3, 100003, 10), (1, 262144, 64), (200, 5000, 1), (511, 20000, 0), (2, 4100, 20)):
+        z = rand((t, v), 3).cuda()
+        assert lib.aires_log_probs_workspace(t, v, top, ref(need)) == B_.OK and need.value > 0
+        room = Room(need.value)
+        lse, tl = torch.empty(t, device="cuda"), torch.empty(t, max(1, top), device="cuda")
+        ti = torch.empty(t, max(1, top), dtype=torch.int64, device="cuda")
+        assert lib.aires_log_probs(ref(c_dense(z)), None, 0, top, None, None, lse.data_ptr(), tl.data_ptr(), ti.data_ptr(),
+                                   room.all.data_ptr(), need.value, None) == B_.OK
+        room.check()
+        r = aires.log_probs(z, top=top)
+        assert torch.equal(r.lse, lse) and (top == 0 or (torch.equal(r.top_logp, tl) and torch.equal(r.top_index, ti)))
+    for m, n in ((4099, 48), (300, 6001), (3, 17000), (1, 5), (70000, 300)):
+        s, dy = rand((m, n), 1).cuda(), rand((m, n), 2).cuda()
+        q = torch.ones(m, device="cuda")
+        assert lib.aires_rms_norm_workspace(m, n, ref(need)) == B_.OK
+        room, dg = Room(need.value), torch.empty(n, device="cuda")
+        assert lib.aires_rms_norm_backward(ref(c_dense(dy)), ref(c_dense(s)), q.data_ptr(), None, 0, None, None, dg.data_ptr(),
+                                           room.all.data_ptr(), need.value, None) == B_.OK
+        room.check()
+        assert torch.equal(dg, aires.rms_norm_backward(dy, s, q, need_dx=False)[1])
+    for sizes in ([5], [3000000, 1, 70000], [9] * 300):
+        grads = [rand(k, 1).cuda() for k in sizes]
+        table = (B_.GradTensor * len(sizes))(*[B_.GradTensor(k, g.data_ptr(), g.data_ptr(), 0, 0) for k, g in zip(sizes, grads)])
+        assert lib.aires_grad_norm_workspace(len(sizes), ref(need)) == B_.OK
+        room, norm = Room(need.value), torch.empty((), device="cuda")
+        want = aires.grad_norm(grads)[0]
+        assert lib.aires_clip_grads(table, len(sizes), 0.5, norm.data_ptr(), room.all.data_ptr(), need.value, None) == B_.OK
+        room.check()
+        assert torch.equal(norm, want)
+
+
+# ------------------------------------------------------------- drawn sizes
+
+def log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+@pytest.mark.parametrize("seed", range(60))
+def test_products_of_drawn_sizes(seed):
+    rng = random.Random(seed)
+    near_ = rng.choice([0, 0, -1, 1])
+    m, n, k = (max(1, log(rng, 1, top) // r * r + near_) for top, r in ((700, rng.choice([1, 16, 64])), (700, rng.choice([1, 64, 128])),
+                                                                        (4000, rng.choice([1, 16, 128]))))
+    tiles = rng.random() < 0.5
+    check_product(operand(m, k, seed, False), operand(n, k, seed + 100, tiles), rng.choice([F32, BF16, F16]), (m, n, k, tiles))
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_norms_of_drawn_sizes(seed):
+    rng = random.Random(seed)
+    n = log(rng, 1, 20000)
+    m = log(rng, 1, max(2, 300000 // n))
+    xt, yt = rng.choice([F32, BF16, F16]), rng.choice([F32, BF16, F16, F8])
+    rt = rng.choice([None, xt, F32])
+    x, r, gamma = rand((m, n), seed, xt), None if rt is None else rand((m, n), seed + 1, rt), 1 + 0.3 * rand(n, 3)
+    Y, S, q = aires.rms_norm(x.cuda(), gamma.cuda(), residual=None if r is None else r.cuda(), out_dtype=yt)
+    rms_check(x, r, gamma, Y, S, q, yt)
+    tiles = rng.random() < 0.5
+    rows, cols = aires.quantize_8bit(x.cuda(), tiles=tiles, order="both")
+    for got, want in ((rows, hold(x, tiles)), (cols, hold(x.t().contiguous(), tiles))):
+        assert equal(got[0].cpu(), want[0]) and torch.equal(got[1].cpu(), want[1])
+
+
+@pytest.mark.parametrize("seed", range(60))
+def test_log_probs_of_drawn_sizes(seed):
+    rng = random.Random(seed)
+    v = log(rng, 1, 60000)
+    t = log(rng, 1, max(2, 1000000 // v))
+    kind, top = rng.choice([F32, BF16, F16]), min(v, rng.choice([1, 3, 9, 17, 64]))
+    z = (rng.choice([0.1, 3.0, 20.0]) * rand((t, v), seed)).to(kind)
+    order = rng.choice(["any", "rising", "falling", "equal"])
+    if order != "any":
+        z = z.sort(1, descending=order == "falling")[0]
+    if order == "equal":
+        z = (z / 8).round() * 8
+    labels = torch.randint(0, v, (t,), generator=torch.Generator().manual_seed(seed))
+    r = aires.log_probs(z.cuda(), labels.cuda(), top=top)
+    lse, logp, H, lp, p = logp_ref(z, labels)
+    base, ent = logp_tolerance(z, p)
+    # a part's maximum that rises with every chunk brings its sums to the new one as often
+    more = 8 * U * (1 + H) * (v // 512 + 1) if order == "rising" else 0
+    near(r.lse, lse, base + more + 2 * U * lse.abs(), "lse")
+    near(r.entropy, H, ent + more * (1 + H) + 4 * U * (H + 1), "entropy")
+    near(r.logp, logp, base + more + 4 * U * logp.abs(), "logp")
+    best = torch.sort(z, dim=1, descending=True, stable=True)[1][:, :top]
+    assert torch.equal(r.top_index.cpu(), best), order
