@@ -57,14 +57,30 @@ __device__ __forceinline__ int find(const Table& tab, uint32_t b) {
   return lo;
 }
 
-// Sum over the workgroup, in every thread.
+// x of the lane that CTRL names (see device.h).
+template <int CTRL>
+__device__ __forceinline__ double dpp_f64(double x) {
+  return __builtin_bit_cast(double, dpp_move<CTRL, 0xf>(__builtin_bit_cast(uint64_t, x)));
+}
+__device__ __forceinline__ double lane_f64(double x, int lane) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  return __builtin_bit_cast(double, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(u >> 32), lane) << 32 |
+                                        (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, lane));
+}
+
+// Sum over the workgroup, in every thread: by lane exchanges within 16 lanes, then
+// one lane of each 16, then the wavefronts.
 __device__ __forceinline__ double block_sum(double v, double* buf) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  v += dpp_f64<0xB1>(v);
+  v += dpp_f64<0x4E>(v);
+  v += dpp_f64<0x141>(v);
+  v += dpp_f64<0x140>(v);
+  v = (lane_f64(v, 0) + lane_f64(v, 16)) + (lane_f64(v, 32) + lane_f64(v, 48));
   if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
   __syncthreads();
   v = 0.0;
-  for (int w = 0; w < (int)(blockDim.x >> 6); ++w) v += buf[w];
+#pragma unroll
+  for (int w = 0; w < BLOCK / 64; ++w) v += buf[w];
   return v;
 }
 
@@ -126,9 +142,12 @@ __global__ __launch_bounds__(BLOCK) void k_grad_squares(Table tab, double* part)
 
 // The partial sums, in an order of their number alone.
 __device__ __forceinline__ double add_parts(const Final& f, double* buf) {
-  double v = 0.0;
-  for (int64_t i = threadIdx.x; i < f.parts; i += blockDim.x) v += f.part[i];
-  return block_sum(v, buf);
+  double v[4] = {};
+  for (int64_t i = threadIdx.x; i < f.parts; i += 4 * BLOCK)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (i + q * BLOCK < f.parts) v[q] += f.part[i + q * BLOCK];
+  return block_sum((v[0] + v[1]) + (v[2] + v[3]), buf);
 }
 
 // A NaN gives NaN (the comparison is false), an infinity 0.
