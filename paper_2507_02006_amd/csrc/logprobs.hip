@@ -345,7 +345,6 @@ struct List {
 template <int W, bool TOP, int T>
 __global__ __launch_bounds__(W) void k_logp_long(Args a) {
   constexpr int WAVES = W / 64;
-  const int zt = type_of<T>(a.zt), n8 = row_of<T>(a.v);
   __shared__ Stats stats[WAVES];
   __shared__ uint64_t lists[TOP ? WAVES * 64 : 1], bufs[TOP ? WAVES : 1][64], waits[TOP ? WAVES : 1][64];
   __shared__ int floor_of;
@@ -361,14 +360,14 @@ __global__ __launch_bounds__(W) void k_logp_long(Args a) {
   }
   Raw<T> next;
   // (a chunk past the row's end is moved back into the row, one past the part's not)
-  load_raw<true>(a.z, zt, base + begin + (int)threadIdx.x * 8, a.v - begin - (int)threadIdx.x * 8, n8, next);
+  load_raw<true>(a.z, T, base + begin + (int)threadIdx.x * 8, a.v - begin - (int)threadIdx.x * 8, 8, next);
   for (int at = begin; at < end; at += W * 8) {
     Raw<T> now = next;
     const int c = at + threadIdx.x * 8;
-    load_raw<true>(a.z, zt, base + c + W * 8, a.v - c - W * 8, n8, next);
+    load_raw<true>(a.z, T, base + c + W * 8, a.v - c - W * 8, 8, next);
     float z[8];
-    settle(now, zt, a.v - c, n8);
-    convert(now, zt, z);
+    settle(now, T, a.v - c, 8);
+    convert(now, T, z);
     if (c + 8 > end)
 #pragma unroll
       for (int k = 0; k < 8; ++k)
@@ -495,11 +494,10 @@ __global__ __launch_bounds__(BLOCK) void k_logp_back(Back a) {
 
 constexpr int64_t kShortCols = 512;
 
-// f(type) with the type as a constant (rows of fewer than eight scores: MIXED).
+// f(type) with the type as a constant.
 template <typename F>
-void with_type(int t, int64_t v, F f) {
-  if (v < 8 || t == MIXED) f(std::integral_constant<int, MIXED>());
-  else if (t == DT_F32) f(std::integral_constant<int, DT_F32>());
+void with_type(int t, F f) {
+  if (t == DT_F32) f(std::integral_constant<int, DT_F32>());
   else if (t == DT_BF16) f(std::integral_constant<int, DT_BF16>());
   else f(std::integral_constant<int, DT_F16>());
 }
@@ -540,8 +538,12 @@ hipError_t log_probs(const LogProbs& x, void* ws, hipStream_t s) {
     const int64_t rows = BLOCK / lanes;
     return dim3((unsigned)std::min<int64_t>((a.t + rows - 1) / rows, 1 << 20));
   };
+  if (a.v < 8) {
+    k_logp_short<8, MIXED><<<grid(8), BLOCK, 0, s>>>(a);
+    return hipGetLastError();
+  }
   if (a.v <= kShortCols) {
-    with_type(a.zt, a.v, [&](auto type) {
+    with_type(a.zt, [&](auto type) {
       constexpr int T = decltype(type)::value;
       if (a.v <= 64) k_logp_short<8, T><<<grid(8), BLOCK, 0, s>>>(a);
       else if (a.v <= 128) k_logp_short<16, T><<<grid(16), BLOCK, 0, s>>>(a);
@@ -572,7 +574,7 @@ hipError_t log_probs(const LogProbs& x, void* ws, hipStream_t s) {
       if (a.top_index) b.top_index += r0 * a.top;
     }
     const dim3 g((unsigned)(b.t * b.parts));
-    with_type(a.zt, a.v, [&](auto type) {
+    with_type(a.zt, [&](auto type) {
       constexpr int T = decltype(type)::value;
       if (wave && a.top > 0) k_logp_long<64, true, T><<<g, 64, 0, s>>>(b);
       else if (wave) k_logp_long<64, false, T><<<g, 64, 0, s>>>(b);
@@ -596,13 +598,15 @@ hipError_t log_probs_backward(const Mat& Z, const void* labels, int labels_i64, 
     const dim3 g((unsigned)std::min<int64_t>((a.t + rows - 1) / rows, 1 << 20), (unsigned)shares);
     k_logp_back<L, decltype(type)::value><<<g, BLOCK, 0, s>>>(a);
   };
-  with_type(a.zt == a.dt ? a.zt : MIXED, a.v, [&](auto type) {
+  const auto typed = [&](auto type) {
     if (a.v <= 64) return go(std::integral_constant<int, 8>(), type, 1);
     if (a.v <= 128) return go(std::integral_constant<int, 16>(), type, 1);
     if (a.v <= 512) return go(std::integral_constant<int, 64>(), type, 1);
     const int64_t steps = ((int64_t)a.v + BLOCK * 8 - 1) / (BLOCK * 8);
     go(std::integral_constant<int, BLOCK>(), type, std::min<int64_t>(steps, std::max<int64_t>(1, (4096 + a.t - 1) / a.t)));
-  });
+  };
+  if (a.v < 8 || a.zt != a.dt) typed(std::integral_constant<int, MIXED>());
+  else with_type(a.zt, typed);
   return hipGetLastError();
 }
 

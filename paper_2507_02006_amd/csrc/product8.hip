@@ -155,7 +155,7 @@ struct Tile8 {
   // in memory, and each line that is fetched for them gives four.
   static constexpr int SCALES = (TW + TX) * 16, LDS = STAGES * STAGE + 2 * SCALES;
   static constexpr int SHARES = (TW + TX) / 64;  // of 64 rows
-  static constexpr int EACH = SHARES > WAVES ? SHARES / WAVES : 1;  // a wavefront's
+  static_assert(SHARES <= WAVES, "a wavefront loads one share of the scales");
   static_assert(WW <= BLOCK8, "a wavefront's rows of B share a scale");
   typedef Share<TW, WAVES> ShareW;
   typedef Share<TX, WAVES> ShareX;
@@ -173,30 +173,22 @@ struct Tile8 {
         for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
     const uint32_t at_w = place_of(ww * WW, lane), at_x = TW * 128 + place_of(wx0, lane);
     const int total = (int)(s1 - s0);
-    // this wavefront's shares of the scales: 64 rows of the tile, B's first
-    const float* scale[EACH];
-    uint32_t scale_off[EACH];
-#pragma unroll
-    for (int e = 0; e < EACH; ++e) {
-      const int sp = (wave * EACH + e) % SHARES;
-      const bool of_w = sp < TW / 64;
-      const Held& h = of_w ? a.w : a.x;
-      const int64_t r0 = of_w ? w0 : x0, r = r0 + (of_w ? sp : sp - TW / 64) * 64 + lane;
-      const int64_t q0 = r0 / h.tile;
-      scale[e] = h.scales + q0 * h.lds + s0;
-      scale_off[e] = (uint32_t)(((r < h.rows ? r : h.rows - 1) / h.tile - q0) * h.lds * 4);
-    }
+    // this wavefront's share of the scales: 64 rows of the tile, B's first (where there
+    // are more wavefronts than shares, some write the same to the same place)
+    const int sp = wave % SHARES;
+    const bool of_w = sp < TW / 64;
+    const Held& h = of_w ? a.w : a.x;
+    const int64_t h0 = of_w ? w0 : x0, hr = h0 + (of_w ? sp : sp - TW / 64) * 64 + lane;
+    const float* const scale = h.scales + h0 / h.tile * h.lds + s0;
+    const uint32_t scale_off = (uint32_t)(((hr < h.rows ? hr : h.rows - 1) / h.tile - h0 / h.tile) * h.lds * 4);
     // (steps past the last repeat it)
     const auto issue_scales = [&](int group) {
+      char* to = lds + STAGES * STAGE + (group & 1) * SCALES + sp * 256;
 #pragma unroll
-      for (int e = 0; e < EACH; ++e) {
-        char* to = lds + STAGES * STAGE + (group & 1) * SCALES + (wave * EACH + e) % SHARES * 256;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int s = group * 4 + q < total ? group * 4 + q : total - 1;
-          __builtin_amdgcn_global_load_lds((global_void*)(reinterpret_cast<const char*>(scale[e] + s) + scale_off[e]),
-                                           (lds_void*)(to + q * (TW + TX) * 4), 4, 0, 0);
-        }
+      for (int q = 0; q < 4; ++q) {
+        const int s = group * 4 + q < total ? group * 4 + q : total - 1;
+        __builtin_amdgcn_global_load_lds((global_void*)(reinterpret_cast<const char*>(scale + s) + scale_off),
+                                         (lds_void*)(to + q * (TW + TX) * 4), 4, 0, 0);
       }
     };
     ShareW sw;
@@ -353,7 +345,7 @@ struct Tile8 {
 };
 
 template <int TW, int TX, int WW, int WX, int STAGES, bool ROWS, bool WIDE>
-__global__ __launch_bounds__(TW / WW * (TX / WX) * 64, WX == 128 ? 1 : 2) void k_tiles8(Args a) {
+__global__ __launch_bounds__(TW / WW * (TX / WX) * 64, 2) void k_tiles8(Args a) {
   typedef Tile8<TW, TX, WW, WX, STAGES, ROWS, WIDE> T;
   __shared__ __attribute__((aligned(16))) char lds[T::LDS];
   int64_t ty, tx;
