@@ -150,7 +150,7 @@ __global__ __launch_bounds__(L < 8 ? group_threads(L) : TEAM_BLOCK) void k_rms_f
   load(tm.first);
   load_gamma<E>(a, tm, g);
   for (int64_t row = tm.first; row < a.m; row += tm.step) {
-    float x[E][8], sum = 0.f;
+    float x[E][8], sum[L == 64 ? E : 1] = {};
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const int have = n - tm.col(e);
@@ -172,9 +172,15 @@ __global__ __launch_bounds__(L < 8 ? group_threads(L) : TEAM_BLOCK) void k_rms_f
         convert(p, type_of<T>(a.st), x[e]);  // the norm is that of what is stored
       }
 #pragma unroll
-      for (int k = 0; k < 8; ++k) sum += x[e][k] * x[e][k];
+      for (int k = 0; k < 8; ++k) sum[L == 64 ? e : 0] += x[e][k] * x[e][k];
     }
-    const float q = 1.f / sqrtf(team_sum<L>(sum, buf, turn) * a.inv_n + a.eps);
+    // (a wavefront's chunks in the order in which several wavefronts' are added: the same
+    // bits with a residual and without)
+    float all = team_sum<L>(sum[0], buf, turn);
+    if constexpr (L == 64)
+#pragma unroll
+      for (int e = 1; e < E; ++e) all += team_sum<L>(sum[e], buf, turn);
+    const float q = 1.f / sqrtf(all * a.inv_n + a.eps);
 #pragma unroll
     for (int e = 0; e < E; ++e) {
 #pragma unroll
@@ -425,16 +431,19 @@ struct Shape {
   int L, E, threads;
 };
 
-// (A wavefront that holds four chunks a lane has no registers left for the backward
-// pass's next row: two wavefronts share it.)
-Shape shape_of(int64_t n, bool codes, bool back) {
+// A wavefront holds its row where a lane has `most` chunks of it at most, else several
+// share it.  More than that leaves no registers for the next row's loads: 8192 x 2048 with a
+// residual 26 us with four wavefronts a row, 35 with one (bf16), 61 and 75 (fp32); fp32
+// without one 30 and 37; types that are looked at as it runs, X in bf16 and R in fp32, 41 and
+// 61, and 8192 x 1024 20 and 24.  32768 x 2048 in bf16 without a residual: 51 and 46.
+Shape shape_of(int64_t n, bool codes, int most) {
   const int64_t chunks = (n + 7) / 8;
   if (chunks <= 8 && !codes) return {8, 1, TEAM_BLOCK};
   if (chunks <= 16) return {16, 1, TEAM_BLOCK};
   if (chunks <= 32) return {32, 1, TEAM_BLOCK};
   if (chunks <= 64) return {64, 1, TEAM_BLOCK};
-  if (chunks <= 128) return {64, 2, TEAM_BLOCK};
-  if (chunks <= 256 && !back) return {64, 4, TEAM_BLOCK};
+  if (chunks <= 128 && most >= 2) return {64, 2, TEAM_BLOCK};
+  if (chunks <= 256 && most >= 4) return {64, 4, TEAM_BLOCK};
   const int E = chunks <= MAX_BLOCK ? 1 : 2;
   const int threads = (int)(((chunks + E - 1) / E + 63) / 64 * 64);
   return {threads <= MAX_BLOCK / 2 ? 1 : 0, E, threads};
@@ -468,14 +477,15 @@ int common_type(int64_t n, std::initializer_list<const Mat*> all) {
 int64_t rows_at_once(const Shape& sh) { return sh.L < 8 ? 1 : TEAM_BLOCK / sh.L; }
 
 // Workgroups of the backward pass: what fills the chip, but eight rows a team
-// at least once there are many rows (each workgroup writes n partial sums).
+// at least once there are 512 (each workgroup writes n partial sums: 8192 x 2048 in
+// bf16 32 us so, 35 with four rows; 2110 x 1564 15 us in 512 workgroups, 18 in 256).
 int64_t backward_groups(int64_t m, int64_t n) {
   if (n > kRegisterCols) return std::max<int64_t>(1, std::min<int64_t>(32, m / 8));
-  const Shape sh = shape_of(n, false, true);
+  const Shape sh = shape_of(n, false, 2);
   const int64_t rows = rows_at_once(sh);
   const int64_t need = (m + rows - 1) / rows;
   const int64_t fill = sh.L < 8 ? 256 * std::max(1, 1536 / sh.threads) : 1024;
-  return std::max<int64_t>(1, std::min({need, fill, std::max<int64_t>(256, need / 8)}));
+  return std::max<int64_t>(1, std::min({need, fill, std::max<int64_t>(512, need / 8)}));
 }
 
 }  // namespace
@@ -501,31 +511,37 @@ hipError_t rms_norm(const Mat& X, const Mat& R, const void* gamma, int wt, float
     k_rms_forward_wide<<<(unsigned)std::min<int64_t>(a.m, 1 << 20), MAX_BLOCK, 0, s>>>(a);
     return hipGetLastError();
   }
-  const Shape sh = shape_of(X.cols, a.codes != nullptr, false);
+  const int type = common_type(a.n, {&X, &R, &S, &Y});
+  const Shape sh = shape_of(X.cols, a.codes != nullptr, type == MIXED ? 1 : type == DT_F32 || a.r ? 2 : 4);
   const int64_t rows = rows_at_once(sh);
   const int64_t grid = std::min<int64_t>((a.m + rows - 1) / rows, sh.L < 8 ? 256 * std::max(1, 2048 / sh.threads) : 2048);
   // (eight lanes hold no block of 128 columns: their kernels have no codes)
   const dim3 g((unsigned)grid), b((unsigned)sh.threads);
   with_shape<false>(sh, [&](auto l, auto e) {
     constexpr int L = decltype(l)::value, E = decltype(e)::value;
+    // (what a lane may hold: see shape_of)
     const auto typed = [&](auto t) {
       constexpr int T = decltype(t)::value;
-      if (a.codes) {
-        if constexpr (L != 8) {
-          if (a.r) k_rms_forward<L, E, T, true, true><<<g, b, 0, s>>>(a);
-          else k_rms_forward<L, E, T, false, true><<<g, b, 0, s>>>(a);
+      if constexpr (E <= (T == DT_F32 ? 2 : 4)) {
+        if (a.codes) {
+          if constexpr (L != 8) {
+            if constexpr (E <= 2)
+              if (a.r) return k_rms_forward<L, E, T, true, true><<<g, b, 0, s>>>(a);
+            k_rms_forward<L, E, T, false, true><<<g, b, 0, s>>>(a);
+          }
+        } else {
+          if constexpr (E <= 2)
+            if (a.r) return k_rms_forward<L, E, T, true, false><<<g, b, 0, s>>>(a);
+          k_rms_forward<L, E, T, false, false><<<g, b, 0, s>>>(a);
         }
-      } else if (a.r) {
-        k_rms_forward<L, E, T, true, false><<<g, b, 0, s>>>(a);
-      } else {
-        k_rms_forward<L, E, T, false, false><<<g, b, 0, s>>>(a);
       }
     };
-    switch (common_type(a.n, {&X, &R, &S, &Y})) {
+    switch (type) {
       case DT_F32: return typed(Int<DT_F32>());
       case DT_BF16: return typed(Int<DT_BF16>());
       case DT_F16: return typed(Int<DT_F16>());
-      default: k_rms_forward<L, E, MIXED, false, false><<<g, b, 0, s>>>(a);
+      default:
+        if constexpr (E == 1 || L == 0) k_rms_forward<L, E, MIXED, false, false><<<g, b, 0, s>>>(a);
     }
   });
   return hipGetLastError();
@@ -563,7 +579,7 @@ hipError_t rms_norm_backward(const Mat& dY, const Mat& S, const float* rstd, con
     if (dgamma) k_rms_columns_wide<<<dim3((unsigned)((n + TEAM_BLOCK - 1) / TEAM_BLOCK), (unsigned)groups), TEAM_BLOCK, 0, s>>>(a);
     if (a.out) k_rms_backward_wide<<<(unsigned)std::min<int64_t>(a.m, 1 << 20), MAX_BLOCK, 0, s>>>(a);
   } else {
-    const Shape sh = shape_of(n, false, true);
+    const Shape sh = shape_of(n, false, 2);
     const dim3 g((unsigned)groups), b((unsigned)sh.threads);
     with_shape<true>(sh, [&](auto l, auto e) {
       constexpr int L = decltype(l)::value, E = decltype(e)::value;
