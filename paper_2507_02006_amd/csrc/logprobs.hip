@@ -341,12 +341,15 @@ struct List {
 };
 
 // A workgroup of W threads streams columns [part * per, + per) of a row.  Its
-// wavefronts tell each other how high the scores of a full list are.
-template <int W, bool TOP, int T>
+// wavefronts tell each other how high the scores of a full list are.  TOP: NO, LISTS, or
+// ONE, the highest score alone, of which each lane keeps its own (1500 x 16000 in fp16 21
+// us, 26 with lists).
+enum Top { NO, ONE, LISTS };
+template <int W, Top TOP, int T>
 __global__ __launch_bounds__(W) void k_logp_long(Args a) {
   constexpr int WAVES = W / 64;
   __shared__ Stats stats[WAVES];
-  __shared__ uint64_t lists[TOP ? WAVES * 64 : 1], bufs[TOP ? WAVES : 1][64], waits[TOP ? WAVES : 1][64];
+  __shared__ uint64_t lists[TOP == LISTS ? WAVES * 64 : WAVES], bufs[TOP != NO ? WAVES : 1][64], waits[TOP == LISTS ? WAVES : 1][64];
   __shared__ int floor_of;
   const int64_t row = blockIdx.x / a.parts;
   const int part = (int)(blockIdx.x % a.parts), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -354,7 +357,8 @@ __global__ __launch_bounds__(W) void k_logp_long(Args a) {
   const int64_t base = row * a.ldz;
   Stats t = EMPTY;
   List list;
-  if constexpr (TOP && WAVES > 1) {
+  int high = NONE, high_col = 0;
+  if constexpr (TOP == LISTS && WAVES > 1) {
     if (threadIdx.x == 0) floor_of = NONE;
     __syncthreads();
   }
@@ -378,7 +382,17 @@ __global__ __launch_bounds__(W) void k_logp_long(Args a) {
     if (__any(most > t.m)) raise(t, fmaxf(t.m, most));
 #pragma unroll
     for (int k = 0; k < 8; ++k) add(t, z[k]);
-    if constexpr (TOP)
+    if constexpr (TOP == ONE)
+      // (a NaN, as below)
+      if (__any(high == NONE || t.s != t.s || key_of(most) > high)) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int key = c + k < end ? key_of(z[k]) : NONE;
+          high_col = key > high ? c + k : high_col;
+          high = key > high ? key : high;
+        }
+      }
+    if constexpr (TOP == LISTS)
       // (a NaN, which no comparison sees, has made the sum one)
       if (__any(list.last == NONE || t.s != t.s || key_of(most) > list.last)) {
         int floor = NONE;
@@ -397,13 +411,14 @@ __global__ __launch_bounds__(W) void k_logp_long(Args a) {
     t.w = group_sum_f32<64>(t.w);
   }
   uint64_t best = 0;
-  if constexpr (TOP) {
+  if constexpr (TOP == ONE) best = wave_best(high == NONE ? 0 : entry_of(high, high_col));
+  if constexpr (TOP == LISTS) {
     list.finish(a.top, waits[wave], bufs[wave]);
     best = list.entry;
   }
   if constexpr (WAVES > 1) {
     if (lane == 0) stats[wave] = t;
-    if constexpr (TOP) {
+    if constexpr (TOP != NO) {
       if (lane < a.top) lists[wave * a.top + lane] = best;
     }
     __syncthreads();
@@ -411,15 +426,15 @@ __global__ __launch_bounds__(W) void k_logp_long(Args a) {
     t = stats[0];
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) t = merge(t, stats[w]);
-    if constexpr (TOP) best = take_top<WAVES>(lists, WAVES * a.top, a.top, bufs[0]);
+    if constexpr (TOP != NO) best = take_top<WAVES>(lists, WAVES * a.top, a.top, bufs[0]);
   }
   const float log_s = logf(t.s);
   if (a.parts == 1) {
     if (lane == 0) finish_row(a, row, t, log_s);
-    if (TOP && lane < a.top) store_entry(a, row, lane, best, t, log_s);
+    if (TOP != NO && lane < a.top) store_entry(a, row, lane, best, t, log_s);
   } else {
     if (lane == 0) a.stats[blockIdx.x] = t;
-    if (TOP && lane < a.top) a.lists[(int64_t)blockIdx.x * a.top + lane] = best;
+    if (TOP != NO && lane < a.top) a.lists[(int64_t)blockIdx.x * a.top + lane] = best;
   }
 }
 
@@ -503,8 +518,9 @@ void with_type(int t, F f) {
 }
 
 // Rows that a wavefront streams by itself: of up to 2048 scores, or 16384 where there are
-// enough rows to fill the chip with them.
-constexpr int64_t kWaveCols = 2048, kManyWaveCols = 16384, kManyRows = 4096;
+// enough rows to fill the chip with them (10 alternatives, 3770 x 16000 in bf16: 56 us, 67
+// with workgroups; 20 alternatives, 1500 x 16000: 43, 37).
+constexpr int64_t kWaveCols = 2048, kManyWaveCols = 16384, kManyRows = 2048;
 
 // Workgroups that share a row: where rows are fewer than what fills the chip, as
 // many as have a step of columns each, of which the lists can be joined.
@@ -576,10 +592,14 @@ hipError_t log_probs(const LogProbs& x, void* ws, hipStream_t s) {
     const dim3 g((unsigned)(b.t * b.parts));
     with_type(a.zt, [&](auto type) {
       constexpr int T = decltype(type)::value;
-      if (wave && a.top > 0) k_logp_long<64, true, T><<<g, 64, 0, s>>>(b);
-      else if (wave) k_logp_long<64, false, T><<<g, 64, 0, s>>>(b);
-      else if (a.top > 0) k_logp_long<BLOCK, true, T><<<g, BLOCK, 0, s>>>(b);
-      else k_logp_long<BLOCK, false, T><<<g, BLOCK, 0, s>>>(b);
+      const auto go = [&](auto top) {
+        constexpr Top TOP = decltype(top)::value;
+        if (wave) k_logp_long<64, TOP, T><<<g, 64, 0, s>>>(b);
+        else k_logp_long<BLOCK, TOP, T><<<g, BLOCK, 0, s>>>(b);
+      };
+      if (a.top == 0) go(std::integral_constant<Top, NO>());
+      else if (a.top == 1) go(std::integral_constant<Top, ONE>());
+      else go(std::integral_constant<Top, LISTS>());
     });
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

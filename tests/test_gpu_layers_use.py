@@ -338,3 +338,26 @@ def test_log_probs_of_drawn_sizes(seed):
     near(r.logp, logp, base + more + 4 * U * logp.abs(), "logp")
     best = torch.sort(z, dim=1, descending=True, stable=True)[1][:, :top]
     assert torch.equal(r.top_index.cpu(), best), order
+
+
+@pytest.mark.parametrize("t,v", [(7, 600), (2100, 2049), (3000, 5000), (600, 20001), (3, 200001), (1, 513), (5, 64)])
+@pytest.mark.parametrize("kind", [F32, BF16, F16])
+def test_highest_alone_is_first_of_several(t, v, kind):
+    """One alternative a row against the first of three, and the first column of the
+    highest score: equal scores, rows of -infinity, NaNs and infinities."""
+    z = (rand((t, v), v) * 3).round().to(kind)
+    z[0] = -math.inf
+    if t > 6:
+        z[1, v // 2:] = -math.inf
+        z[2, [v // 3, v - 1]] = math.nan
+        z[3, [v // 2, v - 2]] = math.inf
+        z[4, v - 1], z[4, v // 2] = math.nan, math.inf
+        z[5, : v - 1] = -math.inf
+    one, three = aires.log_probs(z.cuda(), top=1), aires.log_probs(z.cuda(), top=3)
+    scores = z.float().nan_to_num(nan=math.inf, posinf=math.inf, neginf=-math.inf)
+    first = (scores == scores.amax(1, keepdim=True)).int().argmax(1)
+    assert torch.equal(one.top_index[:, 0].cpu(), first) and torch.equal(one.top_index[:, 0], three.top_index[:, 0])
+    for name in ("top_logp", "lse", "entropy"):
+        a, b = getattr(one, name), getattr(three, name)
+        a, b = (a, b[:, :1]) if name == "top_logp" else (a, b)
+        assert equal(a.cpu(), b.cpu()), name
