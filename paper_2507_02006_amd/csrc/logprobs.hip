@@ -8,13 +8,20 @@
 // lowered to it; about a dozen operations a score, an exponential among them:
 // bound by the scores' bytes, near the rate of exponentials for 16-bit ones.
 //
-// Rows of up to 512 scores are held in the registers of 8 to 64 lanes; the
+// Rows of up to 512 scores are held in the registers of 8 to 64 lanes, and a few
 // highest scores are taken out one after the other.  Longer rows are streamed, by
 // a wavefront or a workgroup each, or by several workgroups where there are few rows,
 // which a second launch joins.  There every wavefront keeps its highest scores as a
 // list over its lanes and looks at a chunk of 512 scores only where one is above the
 // list's last; chunks come in rising order of columns, so equal scores stay in the
 // order of their index.  Scores are compared as integers of the same order.
+//
+// Statistics are fp32; what is rounded to fewer bits is dz alone, to the type asked for.
+//
+// Measured: 150001 x 41 in fp32, 5 alternatives, 17 us (2.2 TB/s: five rounds over a
+// wavefront's eight rows); 3 x 262144 in bf16, 10 alternatives, 9 us and 4 for the join (the
+// way to memory, six times one after the other); gradient of 4099 x 30011 in bf16 114 us
+// (4.3 TB/s; 98 at 30016 columns, whose rows lie at multiples of 16 bytes).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -30,6 +37,8 @@ namespace {
 constexpr int BLOCK = 256;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float LOWEST = -3.402823466e38f;
+// A few alternatives: taken out one after the other.
+constexpr int kFewTop = 8;
 constexpr int NONE = (int)0x80000000;  // key of no score: below that of -infinity
 
 // Integers in the order of the scores (0 and -0 are equal, a NaN is +infinity).
@@ -135,63 +144,7 @@ __device__ __forceinline__ void store_top(const Args& a, int64_t row, int at, fl
   a.top_index[row * a.top + at] = col;
 }
 
-// ------------------------------------------------------------- short rows
-
-// L lanes hold a row, eight scores a lane.
-template <int L, int T>
-__global__ __launch_bounds__(BLOCK) void k_logp_short(Args a) {
-  constexpr int TEAMS = BLOCK / L;
-  const int zt = type_of<T>(a.zt), n8 = row_of<T>(a.v);
-  const int lane = threadIdx.x % L, first = lane * 8;
-  for (int64_t row = (int64_t)blockIdx.x * TEAMS + threadIdx.x / L; row < a.t; row += (int64_t)gridDim.x * TEAMS) {
-    Raw<T> r;
-    float z[8];
-    Stats t = EMPTY;
-    load_raw(a.z, zt, row * a.ldz + first, a.v - first, n8, r);
-    settle(r, zt, a.v - first, n8);
-    convert(r, zt, z);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      if (first + k >= a.v) z[k] = -__builtin_inff();
-      t.m = fmaxf(t.m, z[k]);
-    }
-    t.m = group_max<L>(t.m);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) add(t, z[k]);
-    t.s = group_sum_f32<L>(t.s);
-    t.w = group_sum_f32<L>(t.w);
-    const float log_s = logf(t.s);
-    if (lane == 0) finish_row(a, row, t, log_s);
-    if (a.top == 0) continue;
-    int key[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) key[k] = first + k < a.v ? key_of(z[k]) : NONE;
-    float mine = 0.f;  // what the round of this lane's number found
-    int mine_col = 0;
-    for (int i = 0; i < a.top; ++i) {
-      int best = NONE;
-#pragma unroll
-      for (int k = 0; k < 8; ++k) best = key[k] > best ? key[k] : best;
-      best = group_best<L, true>(best);
-      int col = 0x7fffffff;
-#pragma unroll
-      for (int k = 7; k >= 0; --k) col = key[k] == best ? first + k : col;
-      col = group_best<L, false>(col);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) key[k] = first + k == col ? NONE : key[k];
-      if (lane == i % L) {
-        mine = score_of(best);
-        mine_col = col;
-      }
-      if (i % L == L - 1 || i == a.top - 1) {
-        const int begin = i / L * L;
-        if (begin + lane <= i) store_top(a, row, begin + lane, mine, mine_col, t, log_s);
-      }
-    }
-  }
-}
-
-// -------------------------------------------------------------- long rows
+// --------------------------------------------------- highest of a wavefront
 
 // A score and its column as one number: higher scores first, then lower columns.
 __device__ __forceinline__ uint64_t entry_of(int key, int col) {
@@ -212,7 +165,8 @@ __device__ __forceinline__ int key_of_entry(uint64_t x) { return (int)((uint32_t
 // there are not so many).  buf: 64 entries of LDS of the wavefront's own.  No wanted
 // score is below the top-th highest of the lanes' best ones; what is not below that,
 // `top` entries and few more in any order but a sorted one, is ranked by comparing
-// each with all.
+// each with all.  The best ones' top-th is found by ranking too where there are more than
+// a few (50000 x 2000 in bf16: 20 alternatives 127 us, 156 by taking out; 5 115 and 110).
 template <int E>
 __device__ __forceinline__ uint64_t wave_top(const uint64_t (&x)[E], int top, uint64_t* buf) {
   const int lane = threadIdx.x & 63;
@@ -220,7 +174,7 @@ __device__ __forceinline__ uint64_t wave_top(const uint64_t (&x)[E], int top, ui
 #pragma unroll
   for (int e = 1; e < E; ++e) best = x[e] > best ? x[e] : best;
   int bound = NONE, rest = key_of_entry(best);
-  if (top <= 8) {
+  if (top <= kFewTop) {
     for (int i = 0; i < top; ++i) {
       bound = group_best<64, true>(rest);
       rest = lane == __ffsll((unsigned long long)__ballot(rest == bound)) - 1 ? NONE : rest;
@@ -286,6 +240,75 @@ __device__ __forceinline__ uint64_t take_top(const uint64_t* from, int count, in
 __device__ __forceinline__ void store_entry(const Args& a, int64_t row, int at, uint64_t entry, const Stats& t, float log_s) {
   store_top(a, row, at, score_of((int)((uint32_t)(entry >> 32) ^ 0x80000000u)), (int)~(uint32_t)entry, t, log_s);
 }
+
+// ------------------------------------------------------------- short rows
+
+// L lanes hold a row, eight scores a lane.  MANY: a wavefront ranks more than a few
+// alternatives (20 of 100000 x 500 in bf16: 97 us, 225 by taking them out; 5: 88).
+template <int L, int T, bool MANY = false>
+__global__ __launch_bounds__(BLOCK) void k_logp_short(Args a) {
+  static_assert(!MANY || L == 64);
+  constexpr int TEAMS = BLOCK / L;
+  __shared__ uint64_t bufs[MANY ? TEAMS : 1][64];
+  const int zt = type_of<T>(a.zt), n8 = row_of<T>(a.v);
+  const int lane = threadIdx.x % L, first = lane * 8;
+  for (int64_t row = (int64_t)blockIdx.x * TEAMS + threadIdx.x / L; row < a.t; row += (int64_t)gridDim.x * TEAMS) {
+    Raw<T> r;
+    float z[8];
+    Stats t = EMPTY;
+    load_raw(a.z, zt, row * a.ldz + first, a.v - first, n8, r);
+    settle(r, zt, a.v - first, n8);
+    convert(r, zt, z);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (first + k >= a.v) z[k] = -__builtin_inff();
+      t.m = fmaxf(t.m, z[k]);
+    }
+    t.m = group_max<L>(t.m);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) add(t, z[k]);
+    t.s = group_sum_f32<L>(t.s);
+    t.w = group_sum_f32<L>(t.w);
+    const float log_s = logf(t.s);
+    if (lane == 0) finish_row(a, row, t, log_s);
+    if (a.top == 0) continue;
+    int key[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) key[k] = first + k < a.v ? key_of(z[k]) : NONE;
+    if constexpr (MANY) {
+      uint64_t x[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] = key[k] == NONE ? 0 : entry_of(key[k], first + k);
+      const uint64_t best = wave_top(x, a.top, bufs[threadIdx.x / L]);
+      if (lane < a.top) store_entry(a, row, lane, best, t, log_s);
+      continue;
+    }
+    float mine = 0.f;  // what the round of this lane's number found
+    int mine_col = 0;
+    for (int i = 0; i < a.top; ++i) {
+      int best = NONE;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) best = key[k] > best ? key[k] : best;
+      best = group_best<L, true>(best);
+      int col = 0x7fffffff;
+#pragma unroll
+      for (int k = 7; k >= 0; --k) col = key[k] == best ? first + k : col;
+      col = group_best<L, false>(col);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) key[k] = first + k == col ? NONE : key[k];
+      if (lane == i % L) {
+        mine = score_of(best);
+        mine_col = col;
+      }
+      if (i % L == L - 1 || i == a.top - 1) {
+        const int begin = i / L * L;
+        if (begin + lane <= i) store_top(a, row, begin + lane, mine, mine_col, t, log_s);
+      }
+    }
+  }
+}
+
+// -------------------------------------------------------------- long rows
 
 // The wavefront's highest scores: lane i holds the i-th as an entry.  Scores above the
 // last of a full list wait in LDS and are ranked together with it when 64 do not hold
@@ -507,6 +530,7 @@ __global__ __launch_bounds__(BLOCK) void k_logp_back(Back a) {
   }
 }
 
+// Rows held in registers (64 lanes of eight scores); longer ones are streamed.
 constexpr int64_t kShortCols = 512;
 
 // f(type) with the type as a constant.
@@ -564,7 +588,8 @@ hipError_t log_probs(const LogProbs& x, void* ws, hipStream_t s) {
       if (a.v <= 64) k_logp_short<8, T><<<grid(8), BLOCK, 0, s>>>(a);
       else if (a.v <= 128) k_logp_short<16, T><<<grid(16), BLOCK, 0, s>>>(a);
       else if (a.v <= 256) k_logp_short<32, T><<<grid(32), BLOCK, 0, s>>>(a);
-      else k_logp_short<64, T><<<grid(64), BLOCK, 0, s>>>(a);
+      else if (a.top <= kFewTop) k_logp_short<64, T><<<grid(64), BLOCK, 0, s>>>(a);
+      else k_logp_short<64, T, true><<<grid(64), BLOCK, 0, s>>>(a);
     });
     return hipGetLastError();
   }
@@ -621,6 +646,7 @@ hipError_t log_probs_backward(const Mat& Z, const void* labels, int labels_i64, 
   const auto typed = [&](auto type) {
     if (a.v <= 64) return go(std::integral_constant<int, 8>(), type, 1);
     if (a.v <= 128) return go(std::integral_constant<int, 16>(), type, 1);
+    if (a.v <= 256) return go(std::integral_constant<int, 32>(), type, 1);
     if (a.v <= 512) return go(std::integral_constant<int, 64>(), type, 1);
     const int64_t steps = ((int64_t)a.v + BLOCK * 8 - 1) / (BLOCK * 8);
     go(std::integral_constant<int, BLOCK>(), type, std::min<int64_t>(steps, std::max<int64_t>(1, (4096 + a.t - 1) / a.t)));
