@@ -22,6 +22,13 @@
 // an operand's rows are not chunks of 16 bytes it is copied so first.  Where there are few
 // tiles k is split over workgroups, whose partial sums a second launch adds in a fixed
 // order.
+//
+// What is rounded to fewer bits: nothing but Y, once (the codes are the operands).
+//
+// Measured: 16384 x 8192 x 4096, 128 x 128 scales, bf16 545 us (2020 TFLOP/s, with random
+// codes; the power limit holds the clock below what codes of one value reach, 468 us); 5 x
+// 8192 x 2048 6 us (2.7 TB/s); 1000 x 520 x 65537, row scales, fp32 in bf16 products 115 us
+// and 46 for copies and sums.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -427,8 +434,8 @@ struct Codes {  // of a lane: chunks of 16 k
 constexpr int ROW_WAVES = 8;
 constexpr int kFewRows = 16;
 
-// All rows of A against 16 rows of B a workgroup; its wavefronts take steps of 128 k
-// in turn, two at a time.  A lane holds 32 k of its row: chunks of 16 bytes, 64 bytes
+// All rows of A against 16 rows of B a workgroup; its wavefronts (eight; four and sixteen
+// make no difference) take steps of 128 k in turn, two at a time.  A lane holds 32 k of its row: chunks of 16 bytes, 64 bytes
 // apart, so that a load covers 64 contiguous bytes of a row.  (With two or four times
 // 16 rows of A the tiles are faster: 17 x 8192 x 8192 18 us against 23, 64 x 8192 x 2048 9
 // against 16.)
@@ -493,7 +500,9 @@ __global__ __launch_bounds__(256) void k_zero8(Mat y) {
     store1(y.data, y.type, i / y.cols * y.ld + i % y.cols, 0.f);
 }
 
-// Rows of codes as chunks of 16 bytes, zeros past the last column.
+// Rows of codes as chunks of 16 bytes, zeros past the last column (1000 x 65537: 25 us, 5.3
+// TB/s; the tiles read codes that lie so straight to LDS, which by way of registers took
+// more of them than there are).
 __global__ __launch_bounds__(256) void k_pack8(Held h, uint8_t* to, int64_t chunks) {
   const int64_t total = h.rows * chunks;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {

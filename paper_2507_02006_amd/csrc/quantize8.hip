@@ -14,6 +14,9 @@
 // matrix.  The transposed codes go through LDS, eight of a column at a time,
 // their place exchanged with the column's number against bank conflicts, and are
 // written as rows of 128 bytes.
+//
+// Measured, X in bf16: 65536 x 1000, scales along rows, both orders 56 us (4.8 TB/s); 16384 x
+// 4096 as it lies 36 us (5.6 TB/s), 128 x 128 scales, both orders, 50 us (5.4 TB/s).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -261,7 +264,8 @@ __global__ __launch_bounds__(BLOCK) void k_quantize(Args a) {
   }
 }
 
-// X as it lies, a scale for each block of a row.
+// X as it lies, a scale for each block of a row.  (The tiles' kernel, whose
+// reads are runs of 256 bytes, took 54 us for 65536 x 1000 in bf16, this 35.)
 template <int T>
 __global__ __launch_bounds__(BLOCK) void k_quantize_rows(Args a) {
   const int lane = threadIdx.x & 63, j = threadIdx.x & 15, g = threadIdx.x >> 4, n8 = row_of<T>((int)a.n);
