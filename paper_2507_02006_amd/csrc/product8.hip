@@ -77,6 +77,22 @@ __device__ __forceinline__ i32x4 load16(const uint8_t* p, int64_t have) {
   return v;
 }
 
+// The same of a row that has 16 bytes before p + have: loaded as one chunk that ends with
+// the row and moved to its place.
+__device__ __forceinline__ i32x4 load16_moved(const uint8_t* p, int64_t have) {
+  const int by = have >= 16 ? 0 : have <= 0 ? 16 : 16 - (int)have;
+  const i32x4 w = *reinterpret_cast<const i32x4_el1*>(have >= 16 ? p : p + have - 16);
+  uint64_t lo = (uint64_t)(uint32_t)w[1] << 32 | (uint32_t)w[0], hi = (uint64_t)(uint32_t)w[3] << 32 | (uint32_t)w[2];
+  if (by >= 8) {
+    lo = hi;
+    hi = 0;
+  }
+  const int bits = (by & 7) * 8;
+  lo = by == 16 ? 0 : bits == 0 ? lo : lo >> bits | hi << (64 - bits);
+  hi = hi >> bits;
+  return i32x4{(int)(uint32_t)lo, (int)(uint32_t)(lo >> 32), (int)(uint32_t)hi, (int)(uint32_t)(hi >> 32)};
+}
+
 __device__ __forceinline__ void store_y(const Args& a, int64_t row, int64_t col, const float (&v)[4]) {
   if (row >= a.y.rows || col >= a.y.cols) return;
   void* const to = a.y.data;
@@ -439,7 +455,11 @@ constexpr int kFewRows = 16;
 // apart, so that a load covers 64 contiguous bytes of a row.  (With two or four times
 // 16 rows of A the tiles are faster: 17 x 8192 x 8192 18 us against 23, 64 x 8192 x 2048 9
 // against 16.)
-template <bool ROWS>
+// ODD: rows begin at any address (the first at a multiple of 4).  The words that a chunk's
+// bytes lie in are loaded and moved to their places, five words a chunk: a load of 16 bytes
+// at an odd address takes several times as long (2 x 4868 x 5311 15 us, 23 by such loads;
+// at multiples of 4 it makes no difference).
+template <bool ROWS, bool ODD>
 __global__ __launch_bounds__(64 * ROW_WAVES) void k_rows8(Args a) {
   __shared__ float sums[ROW_WAVES][64][4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -464,12 +484,24 @@ __global__ __launch_bounds__(64 * ROW_WAVES) void k_rows8(Args a) {
     for (int h = 0; h < 4; ++h)
       v = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(w.c[h / 2], h % 2), widen(x.c[h / 2], h % 2), v, 0, 0, 0);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) acc[q] += v[q] * (f[ROWS ? q : 0] * fx);
+    for (int q = 0; q < 4; ++q) acc[q] = fmaf(v[q], f[ROWS ? q : 0] * fx, acc[q]);
+  };
+  const auto words = [&](const uint8_t* p) {
+    const uint32_t by = (uint32_t)reinterpret_cast<uintptr_t>(p) & 3;
+    const uint32_t* const q = reinterpret_cast<const uint32_t*>(p - by);
+    const u32x4 w = *reinterpret_cast<const u32x4_el4*>(q);
+    const uint32_t last = q[4];
+    i32x4 c;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c[i] = (int)__builtin_amdgcn_alignbyte(i < 3 ? w[i < 3 ? i + 1 : 3] : last, w[i], by);
+    return c;
   };
   const auto whole = [&](const uint8_t* p, int64_t s) {
+    if constexpr (ODD) return Codes{words(p + s * 128), words(p + s * 128 + 64)};
     return Codes{*reinterpret_cast<const i32x4_el1*>(p + s * 128), *reinterpret_cast<const i32x4_el1*>(p + s * 128 + 64)};
   };
-  const int64_t full = a.k / 128;
+  // (the words of a chunk end at most 4 bytes behind it: those are the row's own)
+  const int64_t full = ODD ? (a.k >= 4 ? a.k - 4 : 0) / 128 : a.k / 128;
   int64_t s = wave;
   for (; s + ROW_WAVES < full; s += 2 * ROW_WAVES) {
     const int64_t u = s + ROW_WAVES;
@@ -479,8 +511,9 @@ __global__ __launch_bounds__(64 * ROW_WAVES) void k_rows8(Args a) {
   }
   for (; s < a.steps; s += ROW_WAVES) {
     const int64_t have = a.k - s * 128 - (lane >> 4) * 16;
-    const auto some = [&](const uint8_t* p) { return Codes{load16(p + s * 128, have), load16(p + s * 128 + 64, have - 64)}; };
-    step(s, some(wp), some(xp));
+    const auto some = [&](const uint8_t* p, auto load) { return Codes{load(p + s * 128, have), load(p + s * 128 + 64, have - 64)}; };
+    if (a.k >= 16) step(s, some(wp, load16_moved), some(xp, load16_moved));
+    else step(s, some(wp, load16), some(xp, load16));
   }
 #pragma unroll
   for (int q = 0; q < 4; ++q) sums[wave][lane][q] = acc[q];
@@ -598,8 +631,13 @@ hipError_t matmul8(const Held& A, const Held& B, const Mat& Y, void* ws, hipStre
   Args a{A, B, Y, nullptr, k, (k + 127) / 128, w.per};
   if (w.tile == 0) {
     const dim3 grid((unsigned)((n + 15) / 16));
-    if (rows) k_rows8<true><<<grid, 64 * ROW_WAVES, 0, s>>>(a);
-    else k_rows8<false><<<grid, 64 * ROW_WAVES, 0, s>>>(a);
+    const auto at4 = [](const Held& h) { return reinterpret_cast<uintptr_t>(h.codes) % 4 == 0; };
+    const auto rows4 = [](const Held& h) { return h.ld % 4 == 0 || h.rows == 1; };
+    const bool odd = at4(A) && at4(B) && !(rows4(A) && rows4(B));
+    if (rows && odd) k_rows8<true, true><<<grid, 64 * ROW_WAVES, 0, s>>>(a);
+    else if (rows) k_rows8<true, false><<<grid, 64 * ROW_WAVES, 0, s>>>(a);
+    else if (odd) k_rows8<false, true><<<grid, 64 * ROW_WAVES, 0, s>>>(a);
+    else k_rows8<false, false><<<grid, 64 * ROW_WAVES, 0, s>>>(a);
     return hipGetLastError();
   }
   char* place = static_cast<char*>(ws);

@@ -361,3 +361,25 @@ def test_highest_alone_is_first_of_several(t, v, kind):
         a, b = getattr(one, name), getattr(three, name)
         a, b = (a, b[:, :1]) if name == "top_logp" else (a, b)
         assert equal(a.cpu(), b.cpu()), name
+
+
+@pytest.mark.parametrize("m", [1, 3, 16])
+@pytest.mark.parametrize("k", [1, 3, 4, 127, 129, 130, 131, 132, 133, 257, 1155, 2051, 4094, 5311])
+@pytest.mark.parametrize("tiles", [False, True])
+def test_few_rows_at_any_address(m, k, tiles):
+    """Codes whose rows begin at odd addresses, next to each other, in wider rows, and in
+    rows of whole chunks: the same bits."""
+    n = 37
+    A, B = aires.quantize_8bit(rand((m, k), k).cuda()), aires.quantize_8bit(rand((n, k), k + 1).cuda(), tiles=tiles)
+    out = [aires.matmul_8bit(A, B, out_dtype=F32)]
+    for first, wide in ((0, k + 5), (0, -(-k // 16) * 16), (1, k + 7), (4, k + 6)):
+        copies = []
+        for codes, scales in (A, B):
+            room = torch.full((codes.shape[0] * wide + first,), 0x7f, dtype=torch.uint8, device="cuda")  # NaNs around
+            place = room[first:].view(codes.shape[0], wide)[:, :k]
+            place.copy_(codes.view(torch.uint8))
+            copies.append((place.view(F8), scales))
+        out.append(aires.matmul_8bit(copies[0], copies[1], out_dtype=F32))
+    want = values(A) @ values(B).t()
+    near(out[0], want, product_tolerance(A, B, want, F32), "few rows")
+    assert all(torch.equal(out[0], x) for x in out[1:])
