@@ -547,7 +547,9 @@ void with_type(int t, F f) {
 constexpr int64_t kWaveCols = 2048, kManyWaveCols = 16384, kManyRows = 2048;
 
 // Workgroups that share a row: where rows are fewer than what fills the chip, as
-// many as have a step of columns each, of which the lists can be joined.
+// many as have a step of columns each, of which the lists can be joined (37 x 258440 in bf16,
+// 5 alternatives: 21 us with 1024 workgroups, 23 with 2048; 679 x 20159, 20 alternatives: 26
+// with a workgroup a row, 37 with two or more).
 int parts_of(int64_t t, int64_t v, int top) {
   if (v <= kWaveCols || t >= 512) return 1;
   const int64_t steps = (v + BLOCK * 8 - 1) / (BLOCK * 8);
