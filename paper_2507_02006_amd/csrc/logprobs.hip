@@ -367,8 +367,8 @@ struct List {
 // wavefronts tell each other how high the scores of a full list are.  TOP: NO, LISTS, or
 // ONE, the highest score alone, of which each lane keeps its own (1500 x 16000 in fp16 21
 // us, 26 with lists).
-enum Top { NO, ONE, LISTS };
-template <int W, Top TOP, int T>
+constexpr int NO = 0, ONE = 1, LISTS = 2;
+template <int W, int TOP, int T>
 __global__ __launch_bounds__(W) void k_logp_long(Args a) {
   constexpr int WAVES = W / 64;
   __shared__ Stats stats[WAVES];
@@ -620,13 +620,13 @@ hipError_t log_probs(const LogProbs& x, void* ws, hipStream_t s) {
     with_type(a.zt, [&](auto type) {
       constexpr int T = decltype(type)::value;
       const auto go = [&](auto top) {
-        constexpr Top TOP = decltype(top)::value;
+        constexpr int TOP = decltype(top)::value;
         if (wave) k_logp_long<64, TOP, T><<<g, 64, 0, s>>>(b);
         else k_logp_long<BLOCK, TOP, T><<<g, BLOCK, 0, s>>>(b);
       };
-      if (a.top == 0) go(std::integral_constant<Top, NO>());
-      else if (a.top == 1) go(std::integral_constant<Top, ONE>());
-      else go(std::integral_constant<Top, LISTS>());
+      if (a.top == 0) go(std::integral_constant<int, NO>());
+      else if (a.top == 1) go(std::integral_constant<int, ONE>());
+      else go(std::integral_constant<int, LISTS>());
     });
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
