@@ -27,8 +27,8 @@
 //
 // Measured: 16384 x 8192 x 4096, 128 x 128 scales, bf16 545 us (2020 TFLOP/s, with random
 // codes; the power limit holds the clock below what codes of one value reach, 468 us); 5 x
-// 8192 x 2048 6 us (2.7 TB/s); 1000 x 520 x 65537, row scales, fp32 in bf16 products 115 us
-// and 46 for copies and sums.
+// 8192 x 2048 6 us (2.7 TB/s); 1000 x 520 x 65537, row scales, fp32 in bf16 products 117 us
+// and 42 for copies and sums.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -533,14 +533,16 @@ __global__ __launch_bounds__(256) void k_zero8(Mat y) {
     store1(y.data, y.type, i / y.cols * y.ld + i % y.cols, 0.f);
 }
 
-// Rows of codes as chunks of 16 bytes, zeros past the last column (1000 x 65537: 25 us, 5.3
+// Rows of codes as chunks of 16 bytes, zeros past the last column (1520 x 65537: 36 us, 5.6
 // TB/s; the tiles read codes that lie so straight to LDS, which by way of registers took
 // more of them than there are).
-__global__ __launch_bounds__(256) void k_pack8(Held h, uint8_t* to, int64_t chunks) {
-  const int64_t total = h.rows * chunks;
+// Both operands in one launch; one that is not copied has no rows here.
+__global__ __launch_bounds__(256) void k_pack8(Held a, Held b, uint8_t* to, int64_t chunks) {
+  const int64_t total = (a.rows + b.rows) * chunks;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
     const int64_t r = i / chunks, c = i % chunks * 16;
-    reinterpret_cast<i32x4*>(to)[i] = load16(h.codes + r * h.ld + c, h.cols - c);
+    const uint8_t* const row = r < a.rows ? a.codes + r * a.ld : b.codes + (r - a.rows) * b.ld;
+    reinterpret_cast<i32x4*>(to)[i] = load16(row + c, a.cols - c);
   }
 }
 
@@ -597,15 +599,16 @@ bool chunks(const Held& h) {
 }
 int64_t packed_bytes(const Held& h) { return chunks(h) ? 0 : h.rows * ((h.cols + 15) / 16 * 16); }
 
-// The copy's place, where there is one, and the next place in the workspace.
-hipError_t pack(Held& h, char*& ws, hipStream_t s) {
-  const int64_t bytes = packed_bytes(h);
-  if (bytes == 0) return hipSuccess;
-  uint8_t* const to = reinterpret_cast<uint8_t*>(ws);
-  k_pack8<<<(unsigned)std::min<int64_t>((bytes / 16 + 255) / 256, 1 << 16), 256, 0, s>>>(h, to, bytes / 16 / h.rows);
-  h.codes = to;
-  h.ld = bytes / h.rows;
-  ws += bytes;
+// Operands that are copied, to `to`.
+hipError_t pack(Held& a, Held& b, uint8_t* to, hipStream_t s) {
+  const int64_t of_a = packed_bytes(a), of_b = packed_bytes(b), chunks = (a.cols + 15) / 16;
+  if (of_a + of_b == 0) return hipSuccess;
+  Held x = a, y = b;
+  if (of_a == 0) x.rows = 0;
+  if (of_b == 0) y.rows = 0;
+  k_pack8<<<(unsigned)std::min<int64_t>(((of_a + of_b) / 16 + 255) / 256, 1 << 16), 256, 0, s>>>(x, y, to, chunks);
+  if (of_a) a.codes = to, a.ld = chunks * 16;
+  if (of_b) b.codes = to + of_a, b.ld = chunks * 16;
   return hipGetLastError();
 }
 
@@ -640,13 +643,12 @@ hipError_t matmul8(const Held& A, const Held& B, const Mat& Y, void* ws, hipStre
     else k_rows8<false, false><<<grid, 64 * ROW_WAVES, 0, s>>>(a);
     return hipGetLastError();
   }
-  char* place = static_cast<char*>(ws);
+  uint8_t* place = static_cast<uint8_t*>(ws);
   if (w.splits > 1) {
     a.part = static_cast<float*>(ws);
     place += (w.splits * m * n * (int64_t)sizeof(float) + 15) / 16 * 16;
   }
-  hipError_t e = pack(a.x, place, s);
-  if (e == hipSuccess) e = pack(a.w, place, s);
+  hipError_t e = pack(a.x, a.w, place, s);
   if (e != hipSuccess) return e;
   a.k = (k + 15) / 16 * 16;
   if (rows) e = wide ? launch<true, true>(a, w, s) : launch<true, false>(a, w, s);
