@@ -551,7 +551,7 @@ constexpr int64_t kWaveCols = 2048, kManyWaveCols = 16384, kManyRows = 2048;
 // 5 alternatives: 21 us with 1024 workgroups, 23 with 2048; 679 x 20159, 20 alternatives: 26
 // with a workgroup a row, 37 with two or more).
 int parts_of(int64_t t, int64_t v, int top) {
-  if (v <= kWaveCols || t >= 512) return 1;
+  if (t == 0 || v <= kWaveCols || t >= 512) return 1;
   const int64_t steps = (v + BLOCK * 8 - 1) / (BLOCK * 8);
   const int64_t most = std::min<int64_t>(kMostParts, top > 0 ? kMostEntries / top : kMostParts);
   const int64_t parts = std::max<int64_t>(1, std::min({steps, most, (1024 + t - 1) / t}));
@@ -563,7 +563,7 @@ int parts_of(int64_t t, int64_t v, int top) {
 
 int64_t log_probs_workspace(int64_t t, int64_t v, int top) {
   const int64_t parts = parts_of(t, v, top);
-  if (t == 0 || parts == 1) return 0;
+  if (parts == 1) return 0;
   return t * parts * ((int64_t)sizeof(Stats) + top * (int64_t)sizeof(uint64_t)) + 16;
 }
 
