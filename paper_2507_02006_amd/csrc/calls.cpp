@@ -503,16 +503,22 @@ void adamw(const py::sequence& params, const py::sequence& grads, const py::sequ
       }
     }
   }
-  const bool on_device = THPVariable_Check(grad_scale.ptr());
+  // One fp32 value on the parameters' device is read when the kernels run; all else that
+  // has a float value, tensors too, now.
   const float* factor = nullptr;
-  if (on_device) {
+  double number = 1.0;
+  if (THPVariable_Check(grad_scale.ptr())) {
     const at::Tensor& x = THPVariable_Unpack(grad_scale.ptr());
-    if (x.scalar_type() != at::kFloat || x.numel() != 1 || x.device() != device)
-      bad_value("grad_scale must be a number, or one float32 value on the parameters' device");
-    factor = (const float*)x.data_ptr();
+    if (x.scalar_type() == at::kFloat && x.numel() == 1 && x.device() == device) factor = (const float*)x.data_ptr();
   }
-  const aires_adamw_opts o{sizeof(aires_adamw_opts), seed, step, lr, beta1, beta2, eps, weight_decay,
-                           on_device ? 1.0 : grad_scale.cast<double>()};
+  if (!factor) {
+    number = PyFloat_AsDouble(grad_scale.ptr());
+    if (number == -1.0 && PyErr_Occurred()) {
+      PyErr_Clear();
+      throw py::type_error("grad_scale must be a number or a tensor of one value");
+    }
+  }
+  const aires_adamw_opts o{sizeof(aires_adamw_opts), seed, step, lr, beta1, beta2, eps, weight_decay, number};
   check(aires_adamw_scaled(table.data(), (int64_t)n, &o, factor, (void*)stream), "aires_adamw");
   for (size_t k = 0; k < n; ++k) {
     const py::object po = params[k], mo = m[k], vo = v[k];

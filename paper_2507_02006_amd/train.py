@@ -170,8 +170,10 @@ def adamw(params, grads, exp_avg, exp_avg_sq, *, step: int, lr: float, betas=(0.
     then drives their rounding: pass another one each step); copies:
     tensors that receive the updated parameters in their own type (or None,
     also for single entries).  ``grad_scale``: a number, or a float32 scalar on
-    the device (as ``grad_norm`` returns).  ``step`` counts from 1.  A graph that captured
-    the call repeats its step, options and seed."""
+    the device (as ``grad_norm`` returns), which the kernels read; another tensor
+    of one value is read now, which waits for the device if it is there.  ``step``
+    counts from 1.  A graph that captured the call repeats its step, options and
+    seed."""
     c = _calls or _load()
     if len(params) == 0 and len(grads) == len(exp_avg) == len(exp_avg_sq) == 0:
         return

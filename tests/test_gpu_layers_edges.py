@@ -19,3 +19,46 @@ def test_log_probs_of_no_rows(v):
         assert r.logp.shape == r.entropy.shape == r.lse.shape == (0,)
         assert top == 0 or r.top_index.shape == r.top_logp.shape == (0, top)
     assert aires.log_probs_backward(z, labels, r.lse, r.entropy, dlogp=r.logp, dentropy=r.entropy).shape == (0, v)
+
+
+# ------------------------------------------------- AdamW's factor of the gradients
+
+def step(bits, steps=2, grads=None, copies=False, start=0, **kw):
+    """Steps over tensors with a whole and a partial span: parameters, moments and copies."""
+    shapes = [(33, 170), (300,), (4096,)]
+    params = [rand(s, 1 + i).cuda().to(t) for i, (s, t) in enumerate(zip(shapes, (F32, BF16, F32)))]
+    if grads is None:
+        grads = [rand(s, 5 + i, t).cuda() for i, (s, t) in enumerate(zip(shapes, (BF16, F16, F32)))]
+    m, v = aires.adamw_state(params, bits=bits)
+    c = [torch.zeros_like(p, dtype=F16) for p in params] if copies else None
+    for k in range(1, steps + 1):
+        now = dict(kw) if k > start else {}
+        aires.adamw(params, grads, m, v, step=k, lr=1e-2, seed=k, copies=c, **now)
+    return params + [x for y in (m, v) for z in y for x in (z if bits == 8 else (z,))] + (c or [])
+
+
+def same(a, b):
+    assert len(a) == len(b) and all(equal(x, y) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_takes_any_number(bits):
+    """A factor on the device gives the bits of the number; so does every other tensor of one
+    value, whatever its type and place, and every number of any kind."""
+    import numpy as np
+    grads = [rand((33, 170), 3, BF16).cuda(), rand(300, 4, F16).cuda()]
+    _, scale = aires.grad_norm(grads, max_norm=1.5)
+    assert float(scale) < 0.1
+    want = step(bits, grad_scale=float(scale))
+    for x in (scale, scale.view(1), scale.cpu(), scale.double(), scale.cpu().double(), scale.view(1, 1).cpu(), np.float32(float(scale))):
+        same(step(bits, grad_scale=x), want)
+    want = step(bits, grad_scale=0.5)
+    for x in (scale.new_full((), 0.5).to(BF16), torch.tensor(0.5, dtype=F16), np.float64(0.5), np.array(0.5)):
+        same(step(bits, grad_scale=x), want)
+    same(step(bits, grad_scale=torch.tensor(2)), step(bits, grad_scale=2))
+    for bad in (torch.ones(2, device="cuda"), torch.ones(2), torch.empty(0, device="cuda"), "1", None):
+        with pytest.raises((ValueError, TypeError)):
+            step(bits, grad_scale=bad)
+    for bad in (math.inf, math.nan, torch.tensor(math.nan), torch.tensor(math.inf, dtype=torch.float64).cuda()):
+        with pytest.raises(aires.AiresError):
+            step(bits, grad_scale=bad)
