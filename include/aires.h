@@ -750,7 +750,11 @@ aires_status aires_adamw(const aires_adamw_tensor *tensors, int64_t count, const
  * aires_adamw_scaled -- aires_adamw with a factor of the gradients in device
  * memory: they are multiplied with opts->grad_scale times *grad_scale (one
  * fp32 value, read when the kernels run; NULL: 1).  aires_grad_norm writes
- * such a factor.  Errors: as aires_adamw.
+ * such a factor.  Where the product is 0 all gradients count 0, infinite ones
+ * and NaNs too (aires_grad_norm's factor is 0 where a gradient is infinite): the
+ * step goes on from the moments alone.  Where it is not finite (a NaN among the
+ * gradients) the step is left out: parameters and moments stay as they are,
+ * copies receive the parameters.  Errors: as aires_adamw.
  */
 aires_status aires_adamw_scaled(const aires_adamw_tensor *tensors, int64_t count, const aires_adamw_opts *opts,
                                 const float *grad_scale, void *stream);

@@ -59,11 +59,27 @@ __device__ __forceinline__ int find(const Table& tab, uint32_t b) {
   return lo;
 }
 
-// The step's constants, with the factor that device memory holds.
-__device__ __forceinline__ AdamWStep step_of(const Table& tab) {
-  AdamWStep o = tab.o;
-  if (tab.scale) o.grad_scale *= *tab.scale;
-  return o;
+struct Step : AdamWStep {
+  bool none;  // gradients count 0, whatever they are
+};
+
+// The step's constants, with the factor that device memory holds: false where that is
+// not finite, and the step is left out.  A factor of 0 is what an infinite gradient's norm
+// gives; multiplied, it would make NaNs of that gradient's parameter and moments.
+__device__ __forceinline__ bool step_of(const Table& tab, Step& o) {
+  static_cast<AdamWStep&>(o) = tab.o;
+  o.none = false;
+  if (!tab.scale) return true;
+  o.grad_scale *= *tab.scale;
+  o.none = o.grad_scale == 0.f;
+  return fabsf(o.grad_scale) <= 3.402823466e38f;
+}
+
+// This workgroup's share of a step that is left out: copies receive the parameters all the same.
+__device__ __forceinline__ void copy_only(const AdamWTensor& t, int64_t base) {
+  if (!t.c) return;
+  const int64_t end = base + CHUNK < t.n ? base + CHUNK : t.n;
+  for (int64_t i = base + threadIdx.x; i < end; i += BLOCK) store1(t.c, t.ct, i, load1(t.p, t.pt, i));
 }
 
 template <int T, int STRIDE>
@@ -95,8 +111,8 @@ __device__ __forceinline__ void store_all(void* p, int t, int64_t i, const float
 // New moments, and the parameter from them.  The square root and the
 // reciprocal are the hardware's, within one unit in the last place; the square
 // root takes denormal numbers for 0, so small ones are raised by 2^64 before.
-__device__ __forceinline__ void update(const AdamWStep& o, float g, float& p, float& m, float& v) {
-  g *= o.grad_scale;
+__device__ __forceinline__ void update(const Step& o, float g, float& p, float& m, float& v) {
+  g = o.none ? 0.f : g * o.grad_scale;
   m = m * o.beta1 + g * o.one_beta1;
   v = v * o.beta2 + (g * g) * o.one_beta2;
   const bool low = v < 0x1p-96f;
@@ -106,10 +122,11 @@ __device__ __forceinline__ void update(const AdamWStep& o, float g, float& p, fl
 }
 
 __global__ __launch_bounds__(BLOCK) void k_adamw_32(Table tab) {
-  const AdamWStep o = step_of(tab);
   const int k = find(tab, blockIdx.x);
   const AdamWTensor& t = tab.t[k];
   const int64_t base = (int64_t)(blockIdx.x - tab.first[k]) * CHUNK;
+  Step o;
+  if (!step_of(tab, o)) return copy_only(t, base);
   float* const m_ = static_cast<float*>(t.m);
   float* const v_ = static_cast<float*>(t.v);
   if (base + CHUNK <= t.n) {
@@ -210,12 +227,14 @@ __device__ __forceinline__ uint32_t noise(uint32_t x) {
 constexpr uint32_t kIndexStep = 0x9E3779B1u;
 
 __global__ __launch_bounds__(BLOCK) void k_adamw_8(Table tab) {
-  const AdamWStep o = step_of(tab);
   const int k = find(tab, blockIdx.x);
   const AdamWTensor& t = tab.t[k];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t begin = (int64_t)(blockIdx.x - tab.first[k]) * CHUNK;
+  Step o;
+  if (!step_of(tab, o)) return copy_only(t, begin);
   // this wavefront's PER blocks
-  const int64_t base = (int64_t)(blockIdx.x - tab.first[k]) * CHUNK + wave * (PER * BLOCK);
+  const int64_t base = begin + wave * (PER * BLOCK);
   if (base >= t.n) return;
   const int64_t i0 = base + lane * 4;
   uint8_t* const mc = static_cast<uint8_t*>(t.m);

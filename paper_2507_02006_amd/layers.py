@@ -99,7 +99,9 @@ def grad_norm(grads, *, max_norm: float = float("inf"), stream=None):
     """Norm over a list of gradients (aires_grad_norm), contiguous float32,
     bfloat16 or float16.  Returns (norm, scale), float32 scalars on the device:
     scale = max_norm / norm where norm is larger, else 1.  ``adamw`` takes it as
-    its ``grad_scale``, which spares a pass over the gradients."""
+    its ``grad_scale``, which spares a pass over the gradients.  An infinite
+    gradient gives scale = 0 and a NaN gives NaN: ``adamw`` then takes no gradient,
+    or leaves its step out."""
     grads = list(grads)
     if not grads:
         raise ValueError("no gradients")

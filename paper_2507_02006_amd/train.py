@@ -171,8 +171,9 @@ def adamw(params, grads, exp_avg, exp_avg_sq, *, step: int, lr: float, betas=(0.
     tensors that receive the updated parameters in their own type (or None,
     also for single entries).  ``grad_scale``: a number, or a float32 scalar on
     the device (as ``grad_norm`` returns), which the kernels read; another tensor
-    of one value is read now, which waits for the device if it is there.  ``step``
-    counts from 1.  A graph that captured the call repeats its step, options and
+    of one value is read now, which waits for the device if it is there.  With a
+    factor of 0 on the device all gradients count 0, infinite ones too; with one
+    that is not finite the step is left out.  ``step`` counts from 1.  A graph that captured the call repeats its step, options and
     seed."""
     c = _calls or _load()
     if len(params) == 0 and len(grads) == len(exp_avg) == len(exp_avg_sq) == 0:

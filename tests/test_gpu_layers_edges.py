@@ -62,3 +62,68 @@ def test_adamw_takes_any_number(bits):
     for bad in (math.inf, math.nan, torch.tensor(math.nan), torch.tensor(math.inf, dtype=torch.float64).cuda()):
         with pytest.raises(aires.AiresError):
             step(bits, grad_scale=bad)
+
+
+def moments(bits):
+    return slice(3, 3 + (12 if bits == 8 else 6))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_after_an_infinite_gradient(bits):
+    """The norm's factor is 0: gradients count 0, and nothing that is kept becomes NaN."""
+    shapes = [(33, 170), (300,), (4096,)]
+    grads = [rand(s, 5 + i, t).cuda() for i, (s, t) in enumerate(zip(shapes, (BF16, F16, F32)))]
+    bad = [g.clone() for g in grads]
+    bad[0][3, 7], bad[2][4095] = math.inf, -math.inf
+    norm, scale = aires.grad_norm(bad, max_norm=1.0)
+    assert float(norm) == math.inf and float(scale) == 0
+    nothing = [torch.zeros_like(g) for g in grads]
+
+    def run(last, **kw):
+        params = [rand(s, 1 + i).cuda() for i, s in enumerate(shapes)]
+        m, v = aires.adamw_state(params, bits=bits)
+        aires.adamw(params, grads, m, v, step=1, lr=1e-2, seed=1)
+        aires.adamw(params, last, m, v, step=2, lr=1e-2, seed=2, **kw)
+        return params + [x for y in (m, v) for z in y for x in (z if bits == 8 else (z,))]
+
+    got = run(bad, grad_scale=scale)
+    assert all(bool(x.float().isfinite().all()) for x in got)
+    same(got, run(nothing))
+    # of finite gradients: what a number gives; a NaN counts 0 too
+    zero = torch.zeros((), device="cuda")
+    same(run(grads, grad_scale=zero), run(grads, grad_scale=0.0))
+    bad[1][0] = math.nan
+    same(run(bad, grad_scale=zero), run(nothing))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("factor", [math.nan, math.inf, -math.inf])
+def test_adamw_leaves_out_a_step_without_a_finite_factor(bits, factor):
+    """Parameters and moments stay, bit for bit; copies receive the parameters."""
+    scale = torch.full((), factor, device="cuda")
+    one = step(bits, steps=1, copies=True)
+    got = step(bits, steps=2, start=1, grad_scale=scale, copies=True)
+    for a, b in zip(one[:-3], got[:-3]):
+        assert bool((a.view(torch.uint8) == b.view(torch.uint8)).all())
+    # (a step rounds its fp32 result to a parameter's type and to its copy's; here the copy
+    # is the stored parameter's)
+    for p, c in zip(got[:3], got[-3:]):
+        assert bool((c == p.to(F16)).all())
+    first = step(bits, steps=1, grad_scale=scale, copies=True)
+    for p, c in zip(first[:3], first[-3:]):
+        assert torch.equal(c, p.to(F16)) and bool(c.any())
+    assert not any(bool(x.float().any()) for x in first[moments(bits)])
+
+
+def test_adamw_leaves_out_a_step_after_a_nan():
+    grads = [rand((33, 170), 3).cuda(), rand(300, 4).cuda()]
+    params = [torch.ones_like(g) for g in grads]
+    m, v = aires.adamw_state(params)
+    grads[1][299] = math.nan
+    _, scale = aires.grad_norm(grads, max_norm=1.0)
+    aires.adamw(params, grads, m, v, step=1, lr=1e-2, grad_scale=scale)
+    assert all(bool((p == 1).all()) for p in params) and not any(bool(x.any()) for x in m + v)
+    grads[1][299] = 0
+    _, scale = aires.grad_norm(grads, max_norm=1.0)
+    aires.adamw(params, grads, m, v, step=1, lr=1e-2, grad_scale=scale)
+    assert all(bool((p != 1).any()) and bool(p.isfinite().all()) for p in params)
