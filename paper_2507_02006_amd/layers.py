@@ -60,7 +60,9 @@ def matmul_8bit(A, B, *, out_dtype=None, out=None, stream=None):
     codes, scales for each row); B: a pair (n x k codes, scales for each row or for
     128 rows).  Y has ``out_dtype`` (bfloat16 by default) unless ``out`` is given.
     A layer's Y = X W^T takes X's rows and W in tiles, its dX takes dY's rows and W
-    transposed in tiles, its dW the columns of dY and of X."""
+    transposed in tiles, its dW the columns of dY and of X.  Sums are in fp32, but
+    for a 16-bit Y of more than 16 rows: there each eight neighbours of k are added
+    with an error of up to 8 * 2^-13 of their largest product."""
     if not (isinstance(A, tuple) and len(A) == 2 and isinstance(B, tuple) and len(B) == 2):
         raise ValueError("A and B must be pairs of codes and scales")
     return T._run(_call().matmul_8bit, A[0], stream, A, B, out_dtype, out)

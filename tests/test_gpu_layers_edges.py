@@ -127,3 +127,31 @@ def test_adamw_leaves_out_a_step_after_a_nan():
     _, scale = aires.grad_norm(grads, max_norm=1.0)
     aires.adamw(params, grads, m, v, step=1, lr=1e-2, grad_scale=scale)
     assert all(bool((p != 1).any()) and bool(p.isfinite().all()) for p in params)
+
+
+# ------------------------------------------------------------- products' sums
+
+@pytest.mark.parametrize("m", [16, 17, 300, 3600])
+@pytest.mark.parametrize("tiles", [False, True])
+@pytest.mark.parametrize("kind", [F32, BF16, F16])
+def test_product_of_sums_that_cancel(m, tiles, kind):
+    """Each eight of k holds a large product and its negative, and six small ones, which are
+    all that is left.  The sums of fp32 results and of up to 16 rows are fp32's: 128
+    products, exact, in any order, with a whole step of the sum's size each.  Others may be
+    off by 8 * 2^-13 of the largest product of each eight."""
+    n, k = (3700, 272) if m == 3600 else (40, 656)
+    g = torch.Generator(device="cuda").manual_seed(m)
+    a = torch.randn((m, k), generator=g, device="cuda").to(F8).float()
+    b = torch.randn((n, k), generator=g, device="cuda").to(F8).float()
+    a[:, 0::8], a[:, 5::8], b[:, 0::8], b[:, 5::8] = 448, 448, 448, -448
+    sa = torch.exp2(torch.randint(-3, 4, (m, -(-k // 128)), generator=g, device="cuda").float())
+    sb = torch.exp2(torch.randint(-3, 4, (-(-n // 128) if tiles else n, -(-k // 128)), generator=g, device="cuda").float())
+    got = aires.matmul_8bit((a.to(F8), sa), (b.to(F8), sb), out_dtype=kind).double()
+    each = (sb.repeat_interleave(128, 0)[:n] if tiles else sb).repeat_interleave(128, 1)[:, :k].double()
+    A, B = a.double() * sa.repeat_interleave(128, 1)[:, :k].double(), b.double() * each
+    y = A @ B.t()
+    tol = (256 + 6 + 16) * U * (A.abs() @ B.abs().t()) + rounded(y, kind)
+    if kind != F32 and m > 16:
+        for c in range(0, k, 8):  # the eight's largest product is that of two codes of 448
+            tol += 8 * 2.0 ** -13 * A[:, c, None].abs() * B[None, :, c].abs()
+    assert bool(((got - y).abs() <= tol).all()), float(((got - y).abs() / tol).max())
