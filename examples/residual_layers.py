@@ -71,12 +71,14 @@ def backward(params, kept, dz):
 
 def loss_and_gradient(z, labels, entropy_weight):
     """-(sum of log probabilities + w entropy) / number of labels, and dz."""
-    r = aires.log_probs(z, labels)
+    r = aires.log_probs(z, labels, rest=True)
     there = labels >= 0
     count = there.sum().clamp(min=1)
     loss = -(r.logp.sum() + entropy_weight * (r.entropy * there).sum()) / count
     dlogp = -(there / count).float()
-    return loss, aires.log_probs_backward(z, labels, r.lse, r.entropy, dlogp=dlogp, dentropy=entropy_weight * dlogp)
+    dz = aires.log_probs_backward(z, labels, r.lse, r.entropy, lse_rest=r.lse_rest, dlogp=dlogp,
+                                  dentropy=entropy_weight * dlogp)
+    return loss, dz
 
 
 def main(argv=None):

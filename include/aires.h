@@ -943,6 +943,17 @@ aires_status aires_log_probs(const aires_dense *Z, const void *labels, int32_t l
                              int64_t workspace_bytes, void *stream);
 
 /*
+ * aires_log_probs_rest -- aires_log_probs, and what the rounding of lse to fp32
+ * leaves (lse_rest: t fp32 values, not without lse; NULL: not wanted): lse +
+ * lse_rest is the logarithm of the sum to fp32's precision of its distance from
+ * the row's maximum, however far from zero the scores lie.  0 where lse is not
+ * finite.  Errors: as aires_log_probs.
+ */
+aires_status aires_log_probs_rest(const aires_dense *Z, const void *labels, int32_t labels_i64, int32_t top,
+                                  float *logp, float *entropy, float *lse, float *lse_rest, float *top_logp,
+                                  int64_t *top_index, void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
  * aires_log_probs_backward -- gradient of the scores from those of logp and
  * entropy (dlogp, dentropy: t fp32 values each, NULL for zeros), with lse and
  * entropy as aires_log_probs returned them:
@@ -950,12 +961,25 @@ aires_status aires_log_probs(const aires_dense *Z, const void *labels, int32_t l
  * A label outside [0, v) takes no part (its dlogp is not used).  Rows of -infinity
  * alone have no gradient (zeros); rows whose lse is NaN have NaN.  dZ has Z's size, any
  * type; it may be Z's own memory (same type, address and stride).  entropy may be NULL
- * without dentropy, labels without dlogp.
+ * without dentropy, labels without dlogp.  p is exp(z - lse) with lse as it was
+ * rounded to fp32, which leaves it off by up to |lse| 2^-24 of itself (3e-5 at 1000; rows
+ * of 3e38 lose all of log sum): aires_log_probs_backward_rest is not.
  * Errors: as aires_log_probs.
  */
 aires_status aires_log_probs_backward(const aires_dense *Z, const void *labels, int32_t labels_i64, const float *lse,
                                       const float *entropy, const float *dlogp, const float *dentropy,
                                       const aires_dense *dZ, void *stream);
+
+/*
+ * aires_log_probs_backward_rest -- the same with lse in two parts, as
+ * aires_log_probs_rest returned them (lse_rest NULL: zeros): p = exp(z - lse -
+ * lse_rest), to fp32's precision for scores of any size.
+ * Errors: as aires_log_probs.
+ */
+aires_status aires_log_probs_backward_rest(const aires_dense *Z, const void *labels, int32_t labels_i64,
+                                           const float *lse, const float *lse_rest, const float *entropy,
+                                           const float *dlogp, const float *dentropy, const aires_dense *dZ,
+                                           void *stream);
 
 /* Release C's arrays through the allocator that made them; zeroes *C. */
 void aires_csr_out_free(aires_csr_out *C);

@@ -194,6 +194,10 @@ def load() -> ctypes.CDLL:
         "aires_log_probs_workspace": (ctypes.c_int, [c_i64, c_i64, c_i32, P(c_i64)]),
         "aires_log_probs": (ctypes.c_int, [P(Dense), c_vp, c_i32, c_i32, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_i64,
                                            c_vp]),
+        "aires_log_probs_rest": (ctypes.c_int, [P(Dense), c_vp, c_i32, c_i32, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp,
+                                                c_i64, c_vp]),
+        "aires_log_probs_backward_rest": (ctypes.c_int, [P(Dense), c_vp, c_i32, c_vp, c_vp, c_vp, c_vp, c_vp, P(Dense),
+                                                         c_vp]),
         "aires_log_probs_backward": (ctypes.c_int, [P(Dense), c_vp, c_i32, c_vp, c_vp, c_vp, c_vp, P(Dense), c_vp]),
     }
     for name, (res, args) in sig.items():

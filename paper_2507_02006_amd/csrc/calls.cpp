@@ -319,7 +319,7 @@ const void* labels_of(const at::Tensor& labels, int64_t t) {
   return vector(labels, t, "labels");
 }
 
-py::tuple log_probs(const at::Tensor& Z, const Maybe& labels, int64_t top, uintptr_t stream) {
+py::tuple log_probs(const at::Tensor& Z, const Maybe& labels, int64_t top, bool with_rest, uintptr_t stream) {
   const aires_dense z = dense(Z, "Z");
   const int64_t t = z.nrows;
   if (top < 0 || top > AIRES_MAX_TOP) bad_value("top must be between 0 and " + std::to_string(AIRES_MAX_TOP));
@@ -328,25 +328,27 @@ py::tuple log_probs(const at::Tensor& Z, const Maybe& labels, int64_t top, uintp
   int64_t need = 0;
   check(aires_log_probs_workspace(t, z.ncols, (int32_t)top, &need), "aires_log_probs_workspace");
   const at::TensorOptions f = Z.options().dtype(at::kFloat);
-  at::Tensor work, logp, entropy = at::empty({t}, f), lse = at::empty({t}, f), top_logp, top_index;
+  at::Tensor work, logp, entropy = at::empty({t}, f), lse = at::empty({t}, f), rest, top_logp, top_index;
   if (need > 0) work = at::empty({need}, Z.options().dtype(at::kByte));
   if (labels) logp = at::empty({t}, f);
+  if (with_rest) rest = at::empty({t}, f);
   if (top > 0) {
     top_logp = at::empty({t, top}, f);
     top_index = at::empty({t, top}, Z.options().dtype(at::kLong));
   }
-  check(aires_log_probs(&z, y, labels && labels->scalar_type() == at::kLong, (int32_t)top,
-                        labels ? (float*)logp.data_ptr() : nullptr, (float*)entropy.data_ptr(), (float*)lse.data_ptr(),
-                        top > 0 ? (float*)top_logp.data_ptr() : nullptr,
-                        top > 0 ? (int64_t*)top_index.data_ptr() : nullptr, need > 0 ? work.data_ptr() : nullptr, need,
-                        (void*)stream),
+  check(aires_log_probs_rest(&z, y, labels && labels->scalar_type() == at::kLong, (int32_t)top,
+                             labels ? (float*)logp.data_ptr() : nullptr, (float*)entropy.data_ptr(),
+                             (float*)lse.data_ptr(), with_rest ? (float*)rest.data_ptr() : nullptr,
+                             top > 0 ? (float*)top_logp.data_ptr() : nullptr,
+                             top > 0 ? (int64_t*)top_index.data_ptr() : nullptr,
+                             need > 0 ? work.data_ptr() : nullptr, need, (void*)stream),
         "aires_log_probs");
-  return py::make_tuple(or_none(logp), entropy, lse, or_none(top_logp), or_none(top_index));
+  return py::make_tuple(or_none(logp), entropy, lse, or_none(top_logp), or_none(top_index), or_none(rest));
 }
 
-at::Tensor log_probs_backward(const at::Tensor& Z, const Maybe& labels, const at::Tensor& lse, const Maybe& entropy,
-                              const Maybe& dlogp, const Maybe& dentropy, std::optional<at::ScalarType> dz_dtype,
-                              const Maybe& out, uintptr_t stream) {
+at::Tensor log_probs_backward(const at::Tensor& Z, const Maybe& labels, const at::Tensor& lse, const Maybe& lse_rest,
+                              const Maybe& entropy, const Maybe& dlogp, const Maybe& dentropy,
+                              std::optional<at::ScalarType> dz_dtype, const Maybe& out, uintptr_t stream) {
   const aires_dense z = dense(Z, "Z");
   const int64_t t = z.nrows;
   if (dlogp && !labels) bad_value("dlogp without labels");
@@ -359,14 +361,16 @@ at::Tensor log_probs_backward(const at::Tensor& Z, const Maybe& labels, const at
   };
   const void* y = labels ? labels_of(*labels, t) : nullptr;
   if (labels) same_device(Z, *labels);
-  const float *l = numbers(lse, "lse"), *h = entropy ? numbers(*entropy, "entropy") : nullptr;
+  const float *l = numbers(lse, "lse"), *lr = lse_rest ? numbers(*lse_rest, "lse_rest") : nullptr;
+  const float *h = entropy ? numbers(*entropy, "entropy") : nullptr;
   const float *da = dlogp ? numbers(*dlogp, "dlogp") : nullptr, *db = dentropy ? numbers(*dentropy, "dentropy") : nullptr;
   if (out) same_device(Z, *out);
   if (out && dz_dtype && out->scalar_type() != *dz_dtype) throw py::type_error("out has another type than dz_dtype");
   const at::Tensor dZ = out ? *out : at::empty({t, z.ncols}, Z.options().dtype(dz_dtype.value_or(Z.scalar_type())));
   const aires_dense dz = dense(dZ, "out");
   if (dz.nrows != t || dz.ncols != z.ncols) bad_value("Z and out differ in size");
-  check(aires_log_probs_backward(&z, y, labels && labels->scalar_type() == at::kLong, l, h, da, db, &dz, (void*)stream),
+  check(aires_log_probs_backward_rest(&z, y, labels && labels->scalar_type() == at::kLong, l, lr, h, da, db, &dz,
+                                      (void*)stream),
         "aires_log_probs_backward");
   if (out) written(*out);
   return dZ;

@@ -300,14 +300,22 @@ aires_status aires_log_probs_workspace(int64_t t, int64_t v, int32_t top, int64_
 aires_status aires_log_probs(const aires_dense* Z, const void* labels, int32_t labels_i64, int32_t top, float* logp,
                              float* entropy, float* lse, float* top_logp, int64_t* top_index, void* workspace,
                              int64_t workspace_bytes, void* stream) {
+  return aires_log_probs_rest(Z, labels, labels_i64, top, logp, entropy, lse, nullptr, top_logp, top_index, workspace,
+                              workspace_bytes, stream);
+}
+
+aires_status aires_log_probs_rest(const aires_dense* Z, const void* labels, int32_t labels_i64, int32_t top,
+                                  float* logp, float* entropy, float* lse, float* lse_rest, float* top_logp,
+                                  int64_t* top_index, void* workspace, int64_t workspace_bytes, void* stream) {
   ST_TRY(check_dense(Z, "Z"));
   ST_TRY(check_scores(Z->nrows, Z->ncols, top));
   if (Z->nrows > 0) {
     if (!labels != !logp) return fail(AIRES_E_INVALID_ARG, "labels and logp go together");
     if (top > 0 && (!top_logp || !top_index)) return fail(AIRES_E_INVALID_ARG, "top_logp or top_index is NULL");
+    if (lse_rest && !lse) return fail(AIRES_E_INVALID_ARG, "lse_rest without lse");
   }
   ST_TRY(check_workspace(workspace, workspace_bytes, kern::log_probs_workspace(Z->nrows, Z->ncols, top)));
-  const kern::LogProbs a{mat(Z), labels, labels_i64, top, logp, entropy, lse, top_logp, top_index};
+  const kern::LogProbs a{mat(Z), labels, labels_i64, top, logp, entropy, lse, lse_rest, top_logp, top_index};
   HIP_TRY(kern::log_probs(a, workspace, (hipStream_t)stream));
   return AIRES_OK;
 }
@@ -315,6 +323,13 @@ aires_status aires_log_probs(const aires_dense* Z, const void* labels, int32_t l
 aires_status aires_log_probs_backward(const aires_dense* Z, const void* labels, int32_t labels_i64, const float* lse,
                                       const float* entropy, const float* dlogp, const float* dentropy,
                                       const aires_dense* dZ, void* stream) {
+  return aires_log_probs_backward_rest(Z, labels, labels_i64, lse, nullptr, entropy, dlogp, dentropy, dZ, stream);
+}
+
+aires_status aires_log_probs_backward_rest(const aires_dense* Z, const void* labels, int32_t labels_i64,
+                                           const float* lse, const float* lse_rest, const float* entropy,
+                                           const float* dlogp, const float* dentropy, const aires_dense* dZ,
+                                           void* stream) {
   ST_TRY(check_dense(Z, "Z"));
   ST_TRY(check_dense(dZ, "dZ"));
   ST_TRY(check_same(Z, "Z", dZ, "dZ"));
@@ -322,8 +337,8 @@ aires_status aires_log_probs_backward(const aires_dense* Z, const void* labels, 
   ST_TRY(check_scores(Z->nrows, Z->ncols, 0));
   if (Z->nrows > 0 && (!lse || (dentropy && !entropy) || (dlogp && !labels)))
     return fail(AIRES_E_INVALID_ARG, "lse, entropy or labels is NULL");
-  HIP_TRY(kern::log_probs_backward(mat(Z), labels, labels_i64, lse, entropy, dlogp, dentropy, mat(dZ),
-                                   (hipStream_t)stream));
+  HIP_TRY(kern::log_probs_backward(mat(Z), labels, labels_i64, lse, lse_rest, entropy, dlogp, dentropy,
+                                   mat(dZ), (hipStream_t)stream));
   return AIRES_OK;
 }
 

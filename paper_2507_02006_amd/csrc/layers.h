@@ -33,13 +33,14 @@ struct LogProbs {
   Mat Z;
   const void* labels; int labels_i64;
   int top;
-  float *logp, *entropy, *lse;
+  float *logp, *entropy, *lse, *rest;  // rest: what lse's rounding leaves
   float* top_logp; int64_t* top_index;
 };
 int64_t log_probs_workspace(int64_t t, int64_t v, int top);
 hipError_t log_probs(const LogProbs& a, void* ws, hipStream_t s);
-hipError_t log_probs_backward(const Mat& Z, const void* labels, int labels_i64, const float* lse, const float* entropy,
-                              const float* dlogp, const float* dentropy, const Mat& dZ, hipStream_t s);
+hipError_t log_probs_backward(const Mat& Z, const void* labels, int labels_i64, const float* lse, const float* rest,
+                              const float* entropy, const float* dlogp, const float* dentropy, const Mat& dZ,
+                              hipStream_t s);
 
 // norm over many gradients
 struct GradTensor {

@@ -4,6 +4,8 @@
 // With m the row's maximum, s = sum exp(z - m) and w = sum (z - m) exp(z - m):
 //   lse = m + log s,  logp = (z_label - m) - log s,  entropy = log s - w / s;
 // dz_j = dlogp ([j = label] - p_j) - dentropy p_j (log p_j + entropy).
+// lse in fp32 is off by up to half a step of its own, which far from zero is more than
+// the rest of p's error (3e-5 of p at 1000): what its rounding leaves is handed on too.
 // One pass over the scores, a running maximum per lane with the sums raised or
 // lowered to it; about a dozen operations a score, an exponential among them:
 // bound by the scores' bytes, near the rate of exponentials for 16-bit ones.
@@ -113,7 +115,7 @@ struct Args {
   int64_t t; int v;
   const void* labels; int i64;
   int top;
-  float *logp, *entropy, *lse, *top_logp;
+  float *logp, *entropy, *lse, *rest, *top_logp;
   int64_t* top_index;
   // parts of a row: columns each, their number, statistics and lists of all parts
   int per, parts;
@@ -126,7 +128,12 @@ __device__ __forceinline__ int64_t label_of(const void* labels, int i64, int64_t
 
 // What a row's statistics give.
 __device__ __forceinline__ void finish_row(const Args& a, int64_t row, const Stats& t, float log_s) {
-  if (a.lse) a.lse[row] = t.m + log_s;
+  const float lse = t.m + log_s;
+  if (a.lse) a.lse[row] = lse;
+  if (a.rest) {  // what the sum's rounding leaves, exactly
+    const float b = lse - t.m;
+    a.rest[row] = finite_f32(lse) ? (t.m - (lse - b)) + (log_s - b) : 0.f;
+  }
   if (a.entropy) a.entropy[row] = t.s == 0.f ? 0.f : log_s - t.w / t.s;
   if (a.labels) {
     const int64_t y = label_of(a.labels, a.i64, row);
@@ -488,7 +495,7 @@ struct Back {
   void* dz; int64_t ldd; int dt;
   int64_t t; int v;
   const void* labels; int i64;
-  const float *lse, *entropy, *dlogp, *dentropy;
+  const float *lse, *rest, *entropy, *dlogp, *dentropy;
 };
 
 // L lanes a row (a workgroup for long rows, blockIdx.y of gridDim.y runs of it).
@@ -500,7 +507,10 @@ __global__ __launch_bounds__(BLOCK) void k_logp_back(Back a) {
   const int lane = threadIdx.x % L;
   const int64_t first = ((int64_t)blockIdx.y * L + lane) * 8, step = (int64_t)gridDim.y * L * 8;
   for (int64_t row = (int64_t)blockIdx.x * TEAMS + threadIdx.x / L; row < a.t; row += (int64_t)gridDim.x * TEAMS) {
-    const float lse = a.lse[row], db = a.dentropy ? a.dentropy[row] : 0.f, h = a.dentropy ? a.entropy[row] : 0.f;
+    const float lse = a.lse[row], rest = a.rest ? a.rest[row] : 0.f, db = a.dentropy ? a.dentropy[row] : 0.f;
+    // log p = z - lse - rest: the rest is taken off in the exponential's multiply-add, and
+    // off the entropy for log p + entropy
+    const float off = -rest * LOG2E, h = (a.dentropy ? a.entropy[row] : 0.f) - rest;
     int64_t y = -1;
     float da = 0.f;
     if (a.dlogp) {
@@ -519,7 +529,7 @@ __global__ __launch_bounds__(BLOCK) void k_logp_back(Back a) {
       convert(r, zt, z);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        const float lp = z[k] - lse, p = exp_of(lp);
+        const float lp = z[k] - lse, p = __builtin_amdgcn_exp2f(fmaf(lp, LOG2E, off));
         float d = p == 0.f ? 0.f : -p * (da + db * (lp + h));
         d = c + k == y ? d + da : d;
         z[k] = none ? 0.f : d;
@@ -574,7 +584,7 @@ hipError_t log_probs(const LogProbs& x, void* ws, hipStream_t s) {
   a.t = x.Z.rows; a.v = (int)x.Z.cols;
   a.labels = x.labels; a.i64 = x.labels_i64;
   a.top = x.top;
-  a.logp = x.logp; a.entropy = x.entropy; a.lse = x.lse; a.top_logp = x.top_logp; a.top_index = x.top_index;
+  a.logp = x.logp; a.entropy = x.entropy; a.lse = x.lse; a.rest = x.rest; a.top_logp = x.top_logp; a.top_index = x.top_index;
   a.parts = 1;
   const auto grid = [&](int lanes) {
     const int64_t rows = BLOCK / lanes;
@@ -613,6 +623,7 @@ hipError_t log_probs(const LogProbs& x, void* ws, hipStream_t s) {
       if (a.logp) b.logp += r0;
       if (a.entropy) b.entropy += r0;
       if (a.lse) b.lse += r0;
+      if (a.rest) b.rest += r0;
       if (a.top_logp) b.top_logp += r0 * a.top;
       if (a.top_index) b.top_index += r0 * a.top;
     }
@@ -635,10 +646,11 @@ hipError_t log_probs(const LogProbs& x, void* ws, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t log_probs_backward(const Mat& Z, const void* labels, int labels_i64, const float* lse, const float* entropy,
-                              const float* dlogp, const float* dentropy, const Mat& dZ, hipStream_t s) {
+hipError_t log_probs_backward(const Mat& Z, const void* labels, int labels_i64, const float* lse, const float* rest,
+                              const float* entropy, const float* dlogp, const float* dentropy, const Mat& dZ,
+                              hipStream_t s) {
   if (Z.rows == 0 || Z.cols == 0) return hipSuccess;
-  Back a{Z.data, Z.ld, Z.type, dZ.data, dZ.ld, dZ.type, Z.rows, (int)Z.cols, labels, labels_i64, lse, entropy, dlogp, dentropy};
+  Back a{Z.data, Z.ld, Z.type, dZ.data, dZ.ld, dZ.type, Z.rows, (int)Z.cols, labels, labels_i64, lse, rest, entropy, dlogp, dentropy};
   const auto go = [&](auto wide, auto type, int64_t shares) {
     constexpr int L = decltype(wide)::value;
     const int64_t rows = BLOCK / L;

@@ -71,30 +71,34 @@ def matmul_8bit(A, B, *, out_dtype=None, out=None, stream=None):
 @dataclass
 class LogProbs:
     """What ``log_probs`` returns, one float32 value a row: logp (None without
-    labels), entropy, lse; and top_logp (float32) and top_index (int64), rows x
-    top (None for top = 0)."""
+    labels), entropy, lse; top_logp (float32) and top_index (int64), rows x
+    top (None for top = 0); and lse_rest (None unless asked for)."""
     logp: Any
     entropy: Any
     lse: Any
     top_logp: Any = None
     top_index: Any = None
+    lse_rest: Any = None
 
 
-def log_probs(Z, labels=None, *, top: int = 0, stream=None) -> LogProbs:
+def log_probs(Z, labels=None, *, top: int = 0, rest: bool = False, stream=None) -> LogProbs:
     """Log probabilities of the rows of scores Z (aires_log_probs): that of each
     row's label (int32 or int64; 0 for a label outside the classes), the entropy,
     and the ``top`` most probable classes, highest first, equal scores by their
-    index.  A class of score -infinity is ruled out."""
-    return LogProbs(*T._run(_call().log_probs, Z, stream, Z, labels, top))
+    index.  A class of score -infinity is ruled out.  With ``rest``, lse_rest is
+    what the rounding of lse to float32 leaves, for ``log_probs_backward``."""
+    return LogProbs(*T._run(_call().log_probs, Z, stream, Z, labels, top, bool(rest)))
 
 
-def log_probs_backward(Z, labels, lse, entropy=None, *, dlogp=None, dentropy=None, dz_dtype=None, out=None,
-                       stream=None):
+def log_probs_backward(Z, labels, lse, entropy=None, *, lse_rest=None, dlogp=None, dentropy=None, dz_dtype=None,
+                       out=None, stream=None):
     """Gradient of the scores (aires_log_probs_backward) from those of logp and
     entropy (float32, one a row, or None), with lse and entropy as ``log_probs``
     returned them.  dZ has ``dz_dtype`` (Z's type by default) unless ``out`` is
-    given, which may be Z itself."""
-    return T._run(_call().log_probs_backward, Z, stream, Z, labels, lse, entropy, dlogp, dentropy, dz_dtype, out)
+    given, which may be Z itself.  Probabilities are exp(Z - lse - lse_rest);
+    without lse_rest they are off by up to |lse| 2^-24 of themselves, which matters
+    where scores lie far from zero."""
+    return T._run(_call().log_probs_backward, Z, stream, Z, labels, lse, lse_rest, entropy, dlogp, dentropy, dz_dtype, out)
 
 
 def grad_norm(grads, *, max_norm: float = float("inf"), stream=None):

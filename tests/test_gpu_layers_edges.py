@@ -6,7 +6,7 @@ import pytest
 
 torch = pytest.importorskip("torch")
 import paper_2507_02006_amd as aires  # noqa: E402
-from test_gpu_layers import BF16, F16, F32, F8, U, equal, near, rand, rounded  # noqa: E402,F401
+from test_gpu_layers import BF16, F16, F32, F8, U, equal, logp_ref, logp_tolerance, near, rand, rounded  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -155,3 +155,77 @@ def test_product_of_sums_that_cancel(m, tiles, kind):
         for c in range(0, k, 8):  # the eight's largest product is that of two codes of 448
             tol += 8 * 2.0 ** -13 * A[:, c, None].abs() * B[None, :, c].abs()
     assert bool(((got - y).abs() <= tol).all()), float(((got - y).abs() / tol).max())
+
+
+# ------------------------------------------------- gradients far from zero
+
+FAR = [(F32, 0.0), (F32, 1e3), (F32, -1e5), (F32, 2.0 ** 24), (BF16, 3e4), (BF16, -3e38), (F16, -6e4)]
+
+
+@pytest.mark.parametrize("t,v", [(5, 6), (40, 30), (40, 100), (9, 500), (30, 700), (600, 2100), (3, 30011)])
+@pytest.mark.parametrize("kind,offset", FAR)
+def test_gradient_of_scores_far_from_zero(t, v, kind, offset):
+    """Against p from 64 bits.  With what lse's rounding leaves, p is off by 3 U |log p| + 8 U
+    of itself (the difference, its product with log2 e, the exponential) and by the sum
+    that the forward pass made; without, by |lse| U more."""
+    z = (3 * rand((t, v), t + v) + offset).to(kind)
+    z[0] = torch.finfo(kind).min if offset <= 0 else torch.finfo(kind).max
+    z[1, : v // 2] = -math.inf
+    z[2] = -math.inf
+    labels = torch.randint(-1, v, (t,), generator=torch.Generator().manual_seed(t))
+    a, b = rand(t, 5), rand(t, 6)
+    # (64 bits lose the logarithm of a sum next to 3e38 too: all from the row's maximum)
+    m = z.double().amax(1)
+    some = m > -math.inf
+    m = torch.where(some, m, torch.zeros(()).double())
+    log_s, _, H, lp, p = logp_ref(z.double() - m[:, None], labels)
+    lse, log_s = m + log_s, torch.where(some, log_s, torch.zeros(()).double())
+    r = aires.log_probs(z.cuda(), labels.cuda(), rest=True)
+    plain = aires.log_probs(z.cuda(), labels.cuda())
+    assert plain.lse_rest is None and equal(plain.lse, r.lse) and equal(plain.entropy, r.entropy) and equal(plain.logp, r.logp)
+    base, _ = logp_tolerance(z.double() - m[:, None], p)
+    near((r.lse.double().cpu() - m) + r.lse_rest.double().cpu(), torch.where(some, log_s, lse), base + 2 * U * log_s.abs(),
+         "lse and its rest, from the maximum")
+    assert float(r.lse_rest[2]) == 0
+
+    d = torch.where(p > 0, lp, torch.zeros(()).double())
+    there = (labels >= 0) & some
+    A = torch.where(there, a, torch.zeros(())).double()[:, None]
+    B, h = b.double()[:, None], H.float()
+    hot = torch.zeros(t, v, dtype=torch.float64).scatter_(1, labels.clamp(0, v - 1)[:, None], there.double()[:, None])
+    want = A * hot - p * (A + B * (d + h.double()[:, None]))
+    size = A.abs() + B.abs() * (d.abs() + H[:, None])
+    off = (base + 2 * U * log_s.abs())[:, None]           # of lse and its rest
+    rest = r.lse_rest.double().cpu().abs()[:, None]
+
+    def tolerance(off):
+        return (p * (size * (torch.expm1(off) * 1.01 + (3 * d.abs() + 14 + 3 * rest) * U) + B.abs() * (off + 4 * U * (d.abs() + H[:, None] + rest)))
+                + U * (A.abs() * hot + p * size))
+
+    args = dict(dlogp=a.cuda(), dentropy=b.cuda())
+    got = aires.log_probs_backward(z.cuda(), labels.cuda(), r.lse, h.cuda(), lse_rest=r.lse_rest, **args)
+    assert got.dtype == kind
+    near(got, want, tolerance(off) + rounded(want, kind), "dZ")
+    wide = aires.log_probs_backward(z.cuda(), labels.cuda(), r.lse, h.cuda(), lse_rest=r.lse_rest, dz_dtype=F32, **args)
+    near(wide, want, tolerance(off) + rounded(want, F32), "dZ in fp32")
+    own = z.cuda()
+    aires.log_probs_backward(own, labels.cuda(), r.lse, h.cuda(), lse_rest=r.lse_rest, out=own, **args)
+    assert equal(own, got)
+    if abs(offset) <= 1e5:  # lse alone: the row at the end of its type's range (the first) has lost log sum
+        lone = aires.log_probs_backward(z.cuda(), labels.cuda(), r.lse, h.cuda(), dz_dtype=F32, **args)
+        more = off + (U * lse.abs().nan_to_num(posinf=0, neginf=0))[:, None]
+        near(lone[1:], want[1:], (tolerance(more) + rounded(want, F32))[1:], "dZ of lse alone")
+
+
+def test_what_the_rounding_of_lse_leaves():
+    z = rand((20, 77), 1).cuda()
+    r = aires.log_probs(z, top=3, rest=True)
+    assert r.lse_rest.shape == (20,) and r.lse_rest.dtype == F32 and r.top_index.shape == (20, 3)
+    z[3, 5], z[4, 6] = math.nan, math.inf
+    r = aires.log_probs(z, rest=True)
+    assert bool(r.lse[3:5].isnan().all()) and bool(r.lse_rest.isfinite().all())
+    dz = aires.log_probs_backward(z, None, r.lse, r.entropy, lse_rest=r.lse_rest, dentropy=r.lse_rest + 1)
+    assert bool(dz[3:5].isnan().all()) and bool(dz[:3].isfinite().all()) and bool(dz[5:].isfinite().all())
+    for bad in (r.lse_rest[:3], r.lse_rest.double(), r.lse_rest.cpu()):
+        with pytest.raises((ValueError, TypeError)):
+            aires.log_probs_backward(z, None, r.lse, lse_rest=bad)

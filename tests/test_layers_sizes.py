@@ -26,3 +26,25 @@ def test_log_probs_of_no_rows(v, top):
     own: one that divides by the number of rows ends)."""
     r = subprocess.run([sys.executable, "-c", NO_ROWS % (v, top)], cwd=ROOT, capture_output=True, text=True, timeout=120)
     assert r.returncode == 0, (r.returncode, r.stderr[-500:])
+
+
+def test_refusals_of_the_calls_with_a_rest():
+    """As the calls without it (CPU: each fails before anything is launched)."""
+    import ctypes
+
+    from paper_2507_02006_amd import _binding as B_
+    lib, fake = B_.load(), 4096
+    Z, other = B_.Dense(3, 50, 50, 0, 0, fake), B_.Dense(3, 50, 50, 0, 0, 8192)
+
+    def forward(Z=Z, lse=fake, rest=fake, top=0):
+        return lib.aires_log_probs_rest(ctypes.byref(Z), None, 0, top, None, None, lse, rest, None, None, None, 0, None)
+
+    def back(Z=Z, lse=fake, h=fake, dZ=other, labels=fake):
+        return lib.aires_log_probs_backward_rest(ctypes.byref(Z), labels, 0, lse, fake, h, fake, fake, ctypes.byref(dZ), None)
+
+    assert forward(lse=None) == forward(top=65) == forward(top=3) == forward(Z=B_.Dense(3, 50, 7, 0, 0, fake)) == B_.E_INVALID_ARG
+    assert forward(Z=B_.Dense(3, 0, 0, 0, 0, fake)) == B_.E_DIM
+    assert back(lse=None) == back(h=None) == back(labels=None) == back(dZ=B_.Dense(3, 50, 51, 0, 0, fake)) == B_.E_INVALID_ARG
+    assert back(dZ=B_.Dense(3, 51, 51, 0, 0, 8192)) == B_.E_DIM
+    none = B_.Dense(0, 50, 50, 0, 0, None)
+    assert forward(Z=none) == back(Z=none, dZ=none) == B_.OK
