@@ -863,8 +863,12 @@ aires_status aires_matmul8_workspace(const aires_dense8 *A, const aires_dense8 *
  * rounded once.  A has tile = 1, B 1 or 128: with B = W (out x in, tile 128) this is a
  * layer's Y = X W^T, with B = W transposed its dX, with both operands transposed
  * activations and gradients its dW.  A NaN in a row of A or B makes that row or
- * column of Y NaN; so does a scale that is not finite, for the rows or columns that
- * it belongs to; others are as without.  Without columns (k = 0)
+ * column of Y NaN; so does a scale of NaN, for the rows or columns that it belongs to,
+ * and an infinite scale makes them infinities or NaNs; others are as without.  A
+ * block's sA and sB are multiplied with each other in fp32 before its sum is: where that
+ * product is above fp32's range results are infinities or NaNs, and where it is below
+ * 2^-126 they lose its bits (of aires_quantize8's blocks, where their largest magnitudes
+ * multiply to less than 2.4e-33 or to more than 6.8e43).  Without columns (k = 0)
  * Y is zeros.
  * Errors: AIRES_E_INVALID_ARG (NULL, bad type or tile, ld too small, workspace not
  * 16-byte aligned), AIRES_E_DIM (sizes differ), AIRES_E_UNSUPPORTED (m or n above

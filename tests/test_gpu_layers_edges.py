@@ -157,6 +157,52 @@ def test_product_of_sums_that_cancel(m, tiles, kind):
     assert bool(((got - y).abs() <= tol).all()), float(((got - y).abs() / tol).max())
 
 
+WAYS = [(5, 40, 300), (17, 40, 300), (100, 90, 4000), (300, 257, 400), (1800, 1800, 300), (3600, 3700, 272)]
+
+
+@pytest.mark.parametrize("m,n,k", WAYS)
+@pytest.mark.parametrize("tiles", [False, True])
+@pytest.mark.parametrize("kind", [F32, BF16])
+def test_product_with_an_infinite_scale(m, n, k, tiles, kind):
+    """Infinities or NaNs in the rows and columns that the scales belong to, in others the
+    bits as without them."""
+    A = aires.quantize_8bit(rand((m, k), 1).cuda())
+    B = aires.quantize_8bit(rand((n, k), 2).cuda(), tiles=tiles)
+    clean = aires.matmul_8bit(A, B, out_dtype=kind)
+    a, b = A[1].clone(), B[1].clone()
+    a[3, -1], b[0, 0] = math.inf, math.inf
+    got = aires.matmul_8bit((A[0], a), (B[0], b), out_dtype=kind)
+    hit = torch.zeros(m, n, dtype=torch.bool, device="cuda")
+    hit[3], hit[:, :128 if tiles else 1] = True, True
+    assert not bool(got[hit].isfinite().any()) and bool((got == clean)[~hit].all())
+
+
+@pytest.mark.parametrize("m,n,k", WAYS)
+@pytest.mark.parametrize("tiles", [False, True])
+@pytest.mark.parametrize("kind", [F32, BF16])
+@pytest.mark.parametrize("low", [True, False])
+def test_product_at_the_ends_of_its_scales_range(m, n, k, tiles, kind, low):
+    """Scales that multiply to 2^-126 and 2^-125, and to 2^126 and 2^127 with codes that keep
+    the results finite (k 2^-12 2^127 at most): as products of ordinary scales, times that power."""
+    g = torch.Generator(device="cuda").manual_seed(m + k)
+    steps = -(-k // 128)
+    size = 1.0 if low else 2.0 ** -8                       # (codes of 2^-9 and 2^-8 and zeros)
+    a = (torch.randn((m, k), generator=g, device="cuda") * size).clamp(-size * 448, size * 448).to(F8)
+    b = (torch.randn((n, k), generator=g, device="cuda") * size).to(F8)
+    if not low:
+        a, b = (x.float().clamp(-2.0 ** -6, 2.0 ** -6).to(F8) for x in (a, b))
+    sa = torch.exp2(torch.randint(0, 2, (m, steps), generator=g, device="cuda").float())
+    sb = torch.ones((-(-n // 128) if tiles else n, steps), device="cuda")
+    ea, eb = (-60, -66) if low else (60, 66)
+    plain = aires.matmul_8bit((a, sa), (b, sb), out_dtype=kind).double()
+    got = aires.matmul_8bit((a, sa * 2.0 ** ea), (b, sb * 2.0 ** eb), out_dtype=kind).double()
+    want = plain * 2.0 ** (ea + eb)
+    assert bool(want.abs().amax() < 3e38)
+    # the same bits but for what falls below a type's normal numbers in each of the blocks' sums and the result
+    least = 2.0 ** -149 if kind == F32 else 2.0 ** -133
+    assert bool(((got - want).abs() <= (steps + 16) * 2.0 ** -149 + least).all())
+
+
 # ------------------------------------------------- gradients far from zero
 
 FAR = [(F32, 0.0), (F32, 1e3), (F32, -1e5), (F32, 2.0 ** 24), (BF16, 3e4), (BF16, -3e38), (F16, -6e4)]
