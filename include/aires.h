@@ -889,6 +889,8 @@ aires_status aires_matmul8(const aires_dense8 *A, const aires_dense8 *B, const a
  * fp32.  gamma: n values of w_dtype, or NULL for ones.  rstd: m fp32 values q
  * (for the backward pass), or NULL.  Sums are fp32.  A NaN or an infinity makes its
  * own row NaN (infinities among finite values: NaN, the others 0) and no other.
+ * A row of finite values whose squares add up to more than fp32's range (values of
+ * 1.8e19 and more) has q = 0 and a y of zeros.
  * Rows without columns have q = eps^-1/2.
  * Errors: AIRES_E_INVALID_ARG (NULL, bad type, ld < ncols, eps negative or not
  * finite, not exactly one of Y and Y8, one of R and S), AIRES_E_DIM,

@@ -21,6 +21,22 @@ def test_log_probs_of_no_rows(v):
     assert aires.log_probs_backward(z, labels, r.lse, r.entropy, dlogp=r.logp, dentropy=r.entropy).shape == (0, v)
 
 
+@pytest.mark.parametrize("n", [40, 1500, 20000])
+@pytest.mark.parametrize("kind", [F32, BF16])
+def test_norm_of_squares_past_the_range(n, kind):
+    """Finite values whose squares' sum is none: q = 0 and zeros, in that row alone."""
+    x = rand((5, n), n, kind)
+    want, _, p = aires.rms_norm(x.cuda())
+    x[1], x[3] = 3e19, 1e17                  # (20000 times 1e34 is in fp32's range)
+    for out in (kind, F8):
+        y, _, q = aires.rms_norm(x.cuda(), out_dtype=out)
+        y = y[0].float() if out == F8 else y
+        assert float(q[1]) == 0 and not bool(y[1].any()) and abs(float(q[3]) * float(x[3, 0]) - 1) < 400 * U
+        assert bool((q[::2] == p[::2]).all())
+    y = aires.rms_norm(x.cuda())[0]
+    assert bool((y[::2] == want[::2]).all())
+
+
 # ------------------------------------------------- AdamW's factor of the gradients
 
 def step(bits, steps=2, grads=None, copies=False, start=0, **kw):
