@@ -513,14 +513,12 @@ void adamw(const py::sequence& params, const py::sequence& grads, const py::sequ
   double number = 1.0;
   if (THPVariable_Check(grad_scale.ptr())) {
     const at::Tensor& x = THPVariable_Unpack(grad_scale.ptr());
-    if (x.scalar_type() == at::kFloat && x.numel() == 1 && x.device() == device) factor = (const float*)x.data_ptr();
+    if (x.numel() != 1) throw py::type_error("grad_scale must be a number or a tensor of one value");
+    if (x.scalar_type() == at::kFloat && x.device() == device) factor = (const float*)x.data_ptr();
   }
   if (!factor) {
     number = PyFloat_AsDouble(grad_scale.ptr());
-    if (number == -1.0 && PyErr_Occurred()) {
-      PyErr_Clear();
-      throw py::type_error("grad_scale must be a number or a tensor of one value");
-    }
+    if (number == -1.0 && PyErr_Occurred()) throw py::error_already_set();
   }
   const aires_adamw_opts o{sizeof(aires_adamw_opts), seed, step, lr, beta1, beta2, eps, weight_decay, number};
   check(aires_adamw_scaled(table.data(), (int64_t)n, &o, factor, (void*)stream), "aires_adamw");
