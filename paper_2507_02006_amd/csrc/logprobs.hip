@@ -21,7 +21,7 @@
 // Statistics are fp32; what is rounded to fewer bits is dz alone, to the type asked for.
 //
 // Measured: 150001 x 41 in fp32, 5 alternatives, 17 us (2.2 TB/s: five rounds over a
-// wavefront's eight rows); 3 x 262144 in bf16, 10 alternatives, 9 us and 4 for the join (the
+// wavefront's eight rows; 8 without alternatives); 3 x 262144 in bf16, 10 alternatives, 9 us and 4 for the join (the
 // way to memory, six times one after the other); gradient of 4099 x 30011 in bf16 114 us
 // (4.3 TB/s; 98 at 30016 columns, whose rows lie at multiples of 16 bytes).
 #include <hip/hip_runtime.h>

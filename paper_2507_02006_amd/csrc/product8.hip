@@ -25,9 +25,9 @@
 //
 // What is rounded to fewer bits: nothing but Y, once (the codes are the operands).
 //
-// Measured: 16384 x 8192 x 4096, 128 x 128 scales, bf16 545 us (2020 TFLOP/s, with random
-// codes; the power limit holds the clock below what codes of one value reach, 468 us); 5 x
-// 8192 x 2048 6 us (2.7 TB/s); 1000 x 520 x 65537, row scales, fp32 in bf16 products 117 us
+// Measured: 16384 x 8192 x 4096, 128 x 128 scales, bf16 550 us (2000 TFLOP/s, with random
+// codes; the power limit holds the clock below what codes of one value reach, 468 us), with
+// a scale for each row of B 725; 5 x 8192 x 2048 6 us (2.7 TB/s); 1000 x 520 x 65537, row scales, fp32 in bf16 products 117 us
 // and 42 for copies and sums.
 #include <hip/hip_runtime.h>
 

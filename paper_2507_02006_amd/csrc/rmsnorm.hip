@@ -17,7 +17,7 @@
 // Sums, statistics and the products between them are fp32.  What is rounded to fewer bits:
 // S and Y to the types asked for, once each; Y in 8 bits from fp32.
 //
-// Measured: 262144 x 512 with a residual, bf16, Y in 8 bits 160 us (5.9 TB/s); backward
+// Measured: 262144 x 512 with a residual, bf16, Y in 8 bits 168 us (5.6 TB/s); backward
 // pass of 4001 x 6001, fp16, 47 us (4.1 TB/s) and 5 for its second launch; one row of 512
 // 2.4 us.
 #include "layers.h"
